@@ -111,6 +111,54 @@ int dart_tree_attention_timed(const dart_attn_config *cfg, const void *q, const 
 int dart_ancestor_mask(const int32_t *parents, const int32_t *n_nodes, int nseq, int B, uint64_t *mask,
                        void *stream);
 
+/* ---- which branch the target keeps ---------------------------------------
+ *
+ * The tree's nodes are chosen by the drafter, not drawn, so a child is a point
+ * mass and this walk draws the next tokens exactly from the target's own
+ * distribution.  From row 0 (the last verified token) on, with the row's
+ * p = softmax(z / T) over its V logits z:
+ *   T > 0: the row's children c1, c2, ... in ascending order of node share
+ *     [0, 1) by p of their tokens: the child with
+ *       p(c1) + .. + p(c(i-1)) <= u < p(c1) + .. + p(ci),  u = u[s][row],
+ *     is kept and its row comes next.  If u lies beyond the children, the walk
+ *     stops with the token of the largest p / e among the tokens of no child
+ *     (ties: the lowest), e = noise[s][token] an Exp(1) number: a draw from
+ *     what the children leave.  (If they leave no token of finite logit, the
+ *     last child with p > 0 is kept instead.)
+ *   T = 0: the token of the largest logit (ties: the lowest) is next; the
+ *     child that has it is kept, else the walk stops.
+ * A child whose token an earlier sibling has, whose token is outside [0, V),
+ * whose parent is not an earlier node or -1, or that is not below n_nodes, is
+ * never kept.  A NaN logit counts as -inf, +inf as the largest float; a row
+ * without a finite logit keeps no child and gives the token -1.
+ */
+typedef struct {
+    int nseq;          /* sequences, >= 1 */
+    int B;             /* tree nodes per sequence, 1..1024; R = B + 1 rows */
+    int V;             /* vocabulary, 1 <= V < 2^24 */
+    int dtype;         /* of the logits: DART_F32 or DART_BF16 (include/dart.h) */
+    int64_t ld;        /* elements between two rows of logits, >= V */
+    float temperature; /* T: 0, or finite and >= 1e-6 */
+} dart_verify_config;
+
+/* The walk above.  logits [nseq][R][ld] of the target's pass, row 0 the last
+ * verified token's, row 1 + i node i's; tokens, parents [nseq][B] and n_nodes
+ * [nseq] int32 as emitted (n_nodes clamped to [0, B]); u [nseq][R] fp32 in
+ * [0, 1) and noise [nseq][V] fp32 > 0 (both may be NULL if T = 0).  Written:
+ *   n_rows [nseq]     rows kept, 1 (row 0 alone) .. B + 1
+ *   rows   [nseq][R]  the kept rows in order, then -1: what dart_cache_append
+ *                     takes as rows / n_rows
+ *   out_tokens [nseq][R]  the token after each kept row, then -1
+ *   logp   [nseq][R]  log p of that token at its row (T = 0: of softmax(z)),
+ *                     0 where the token is -1
+ * `logits` 16-byte aligned; the other pointers aligned to their type.
+ * Returns DART_ERR_INVALID for a bad configuration or pointer,
+ * DART_ERR_UNSUPPORTED on a device that is not sm_103a, DART_ERR_CUDA on a
+ * launch error. */
+int dart_verify_tree(const dart_verify_config *cfg, const void *logits, const int32_t *tokens,
+                     const int32_t *parents, const int32_t *n_nodes, const float *u, const float *noise,
+                     int32_t *n_rows, int32_t *rows, int32_t *out_tokens, float *logp, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

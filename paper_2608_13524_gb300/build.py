@@ -20,7 +20,8 @@ DEBUG_LIB = os.path.join(HERE, "libdart_debug.so")
 DEBUG_BUILD_DIR = os.path.join(HERE, "_build_debug")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["dart_abi.cu", "dart_tc.cu", "dart_f32.cu", "dart_select.cu", "dart_noalloc.cu", "dart_cand.cu",
-           "dart_attn.cu", "dart_heap.cu", "dart_round.cu", "dart_bound.cu"]
+           "dart_attn.cu", "dart_heap.cu", "dart_round.cu", "dart_bound.cu", "dart_cache.cu", "dart_paged.cu",
+           "dart_accept.cu"]
 
 
 def _nvcc() -> str:
@@ -46,7 +47,8 @@ def build(force: bool = False, verbose: bool = False, ptxas_verbose: bool = Fals
     lib_path = DEBUG_LIB if debug else LIB
     os.makedirs(build_dir, exist_ok=True)
     headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cuh"))]
-    headers.append(os.path.join(os.path.dirname(HERE), "include", "dart.h"))
+    include = os.path.join(os.path.dirname(HERE), "include")
+    headers += [os.path.join(include, f) for f in os.listdir(include) if f.endswith(".h")]
     flags = ARCH + ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
                     "--expt-relaxed-constexpr"]
     if ptxas_verbose:

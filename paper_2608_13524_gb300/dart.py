@@ -25,6 +25,7 @@ DART_ERR_UNSUPPORTED = -6
 DART_ERR_BOUNDS = -7
 DART_F32 = 0
 DART_BF16 = 1
+DART_KV_BF16, DART_KV_E4M3 = 0, 1
 DART_AUTO, DART_ON, DART_OFF = 0, 1, 2
 DART_VARIANT_CHAIN_DDTREE = 1
 DART_VARIANT_SEQ_HEAP = 2
@@ -48,6 +49,21 @@ class DartTreeOut(C.Structure):
 class DartAttnConfig(C.Structure):
     _fields_ = [("nseq", C.c_int), ("B", C.c_int), ("C", C.c_int), ("Hq", C.c_int), ("Hkv", C.c_int),
                 ("dh", C.c_int), ("rope_theta", C.c_float), ("scale", C.c_float)]
+
+
+class DartKvCache(C.Structure):
+    _fields_ = [("num_pages", C.c_int), ("page_size", C.c_int), ("Hkv", C.c_int), ("dh", C.c_int), ("dtype", C.c_int),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class DartPagedAttnConfig(C.Structure):
+    _fields_ = [("nseq", C.c_int), ("B", C.c_int), ("max_pages", C.c_int), ("Hq", C.c_int), ("rope_theta", C.c_float),
+                ("scale", C.c_float)]
+
+
+class DartVerifyConfig(C.Structure):
+    _fields_ = [("nseq", C.c_int), ("B", C.c_int), ("V", C.c_int), ("dtype", C.c_int), ("ld", C.c_int64),
+                ("temperature", C.c_float)]
 
 
 class DartError(RuntimeError):
@@ -75,7 +91,7 @@ def lib():
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} not found: build it with __graft_entry__.build()")
         L = C.CDLL(LIB_PATH)
-        vp, i, f = C.c_void_p, C.c_int, C.c_float
+        vp, i, f, i64 = C.c_void_p, C.c_int, C.c_float, C.c_int64
         sig = {
             "dart_init_head": (i, [C.POINTER(vp), C.POINTER(DartConfig), i, vp, vp, vp, vp]),
             "dart_expand_depth": (i, [vp, i, vp, vp, vp]),
@@ -107,6 +123,11 @@ def lib():
                                               C.c_size_t, vp, C.POINTER(f), C.POINTER(f), vp]),
             "dart_tree_attention_tiles": (i, [C.POINTER(DartAttnConfig), i]),
             "dart_ancestor_mask": (i, [vp, vp, i, i, vp, vp]),
+            "dart_cache_append": (i, [C.POINTER(DartKvCache), i, i, vp, vp, i, vp, i64, vp, i64, vp, vp, f, vp, vp]),
+            "dart_paged_attention_workspace": (C.c_size_t, [C.POINTER(DartPagedAttnConfig), C.POINTER(DartKvCache)]),
+            "dart_paged_attention": (i, [C.POINTER(DartPagedAttnConfig), C.POINTER(DartKvCache), vp, vp, vp, i64, vp, i64, vp,
+                                         i64, vp, vp, vp, vp, vp, C.c_size_t, vp, vp]),
+            "dart_verify_tree": (i, [C.POINTER(DartVerifyConfig), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
             "dart_destroy": (None, [vp]),
             "dart_status_string": (C.c_char_p, [i]),
             "dart_version": (i, []),
@@ -447,3 +468,143 @@ class TreeAttention:
     def timed(self, q, k_tree, v_tree, k_ctx, v_ctx, pos_ids, mask, n_nodes, status=None, stream=None):
         return dart_tree_attention_timed(self.cfg, q, k_tree, v_tree, k_ctx, v_ctx, pos_ids, mask, n_nodes,
                                          self.out, self.workspace, status, stream)
+
+
+# ------------------------------------------- paged cache (dart_cache.h)
+
+def _expect(t, name, dtype, shape, dense=True):
+    """Refuses a tensor that the C ABI, which sees a pointer, would misread."""
+    if t is None or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        got = "None" if t is None else f"{t.dtype} {tuple(t.shape)}"
+        raise ValueError(f"{name}: {dtype} {tuple(shape)} expected, got {got}")
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current device")
+    if dense and not t.is_contiguous():
+        raise ValueError(f"{name} is not contiguous")
+    return t.data_ptr()
+
+
+def _rows(t, name, nseq, R, heads, dh):
+    """Pointer and row stride of [nseq][R][heads][dh] bf16 whose heads lie one
+    after the other in each row (a slice of a fused projection, say)."""
+    p = _expect(t, name, torch.bfloat16, (nseq, R, heads, dh), dense=False)
+    ss, sr, sh, sd = t.stride()
+    if (dh > 1 and sd != 1) or (heads > 1 and sh != dh):
+        raise ValueError(f"{name}: the heads of a row have to lie one after the other")
+    if R == 1:
+        sr = ss if nseq > 1 else max(sr, heads * dh)
+    elif nseq > 1 and ss != R * sr:
+        raise ValueError(f"{name}: one stride between all rows of all sequences expected")
+    return p, sr
+
+
+class KVCache:
+    """Pages of keys and values: k, v [num_pages, Hkv, page_size, 128] bfloat16,
+    or float8_e4m3fn with fp32 scales [num_pages, Hkv, page_size]."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        if k.dim() != 4 or k.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            raise ValueError("k: [num_pages, Hkv, page_size, dh] bfloat16 or float8_e4m3fn expected")
+        n, heads, page, dh = k.shape
+        fp8 = k.dtype == torch.float8_e4m3fn
+        if fp8 != (k_scale is not None) or fp8 != (v_scale is not None):
+            raise ValueError("scales belong to float8_e4m3fn pages, and to those alone")
+        ptr = [_expect(k, "k", k.dtype, k.shape), _expect(v, "v", k.dtype, k.shape)]
+        ptr += [_expect(x, m, torch.float32, (n, heads, page)) if fp8 else None for x, m in ((k_scale, "k_scale"), (v_scale, "v_scale"))]
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.num_pages, self.Hkv, self.page_size, self.dh = n, heads, page, dh
+        self.c = DartKvCache(n, page, heads, dh, DART_KV_E4M3 if fp8 else DART_KV_BF16, *ptr)
+
+    @classmethod
+    def new(cls, num_pages, page_size, Hkv, dh=128, dtype=torch.bfloat16):
+        """An empty pool on the current device."""
+        shape, kw = (num_pages, Hkv, page_size, dh), dict(device="cuda")
+        scales = [torch.zeros(shape[:3], **kw) for _ in range(2)] if dtype == torch.float8_e4m3fn else []
+        return cls(torch.zeros(shape, dtype=dtype, **kw), torch.zeros(shape, dtype=dtype, **kw), *scales)
+
+    def append(self, k, v, page_table, lens, n_rows, rows=None, rope_theta=1.0e6, status=None, stream=None):
+        """Writes n_rows[s] tokens of every sequence from position lens[s] on:
+        the rows rows[s, :n_rows[s]] of k and v [nseq, R, Hkv, dh] bf16 (rows
+        None: the first ones).  lens is not advanced."""
+        nseq, R = k.shape[:2]
+        kp, ks = _rows(k, "k", nseq, R, self.Hkv, self.dh)
+        vp, vs = _rows(v, "v", nseq, R, self.Hkv, self.dh)
+        table = _expect(page_table, "page_table", torch.int32, (nseq, page_table.shape[-1]))
+        n = _expect(n_rows, "n_rows", torch.int32, (nseq,))
+        at = _expect(lens, "lens", torch.int32, (nseq,))
+        src = None if rows is None else _expect(rows, "rows", torch.int32, (nseq, R))
+        _check(lib().dart_cache_append(C.byref(self.c), nseq, page_table.shape[-1], table, at, R, kp, ks, vp, vs, src, n,
+                                       rope_theta, _ptr(status), _stream(stream)), "dart_cache_append")
+
+
+class PagedTreeAttention:
+    """Tree attention over a cache: owns the output and the workspace of one
+    shape (nseq sequences, B nodes each, B = 0: single tokens)."""
+
+    def __init__(self, cache, nseq, B, max_pages, Hq=32, rope_theta=1.0e6, scale=None):
+        self.cache = cache
+        self.cfg = DartPagedAttnConfig(int(nseq), int(B), int(max_pages), int(Hq), float(rope_theta),
+                                       float(scale if scale is not None else cache.dh ** -0.5))
+        n = int(lib().dart_paged_attention_workspace(C.byref(self.cfg), C.byref(cache.c)))
+        if n == 0:
+            raise DartError(DART_ERR_INVALID, "dart_paged_attention_workspace")
+        self.workspace = _empty((n,), dtype=torch.uint8, device="cuda")
+        self.out = _empty((nseq, B + 1, Hq, cache.dh), dtype=torch.bfloat16, device="cuda")
+
+    def __call__(self, q, k_tree, v_tree, page_table, lens, depths=None, mask=None, n_nodes=None, status=None, stream=None):
+        """q [nseq, B + 1, Hq, dh], k_tree, v_tree [nseq, B + 1, Hkv, dh] bf16
+        (row 0: the last verified token), page_table [nseq, max_pages] and
+        lens [nseq] int32; depths [nseq, B] int32, mask [nseq, B, ceil(B / 64)]
+        int64 and n_nodes [nseq] int32 as emitted.  Returns self.out."""
+        c, kv = self.cfg, self.cache
+        nseq, B, R = c.nseq, c.B, c.B + 1
+        qp, qs = _rows(q, "q", nseq, R, c.Hq, kv.dh)
+        kp, ks = _rows(k_tree, "k_tree", nseq, R, kv.Hkv, kv.dh)
+        vp, vs = _rows(v_tree, "v_tree", nseq, R, kv.Hkv, kv.dh)
+        table = _expect(page_table, "page_table", torch.int32, (nseq, c.max_pages))
+        at = _expect(lens, "lens", torch.int32, (nseq,))
+        tree = (None, None, None)
+        if B:
+            tree = (_expect(depths, "depths", torch.int32, (nseq, B)),
+                    _expect(mask, "mask", torch.int64, (nseq, B, (B + 63) // 64)),
+                    _expect(n_nodes, "n_nodes", torch.int32, (nseq,)))
+        _check(lib().dart_paged_attention(C.byref(c), C.byref(kv.c), table, at, qp, qs, kp, ks, vp, vs, *tree,
+                                          self.out.data_ptr(), self.workspace.data_ptr(), self.workspace.numel(),
+                                          _ptr(status), _stream(stream)), "dart_paged_attention")
+        return self.out
+
+
+# ------------------------------------------- which branch the target keeps (dart_verify.h)
+
+class TreeVerifier:
+    """Owns the outputs of one shape: n_rows [nseq], rows, tokens [nseq, B + 1]
+    int32 and logp [nseq, B + 1] fp32."""
+
+    def __init__(self, nseq, B, V, temperature=1.0):
+        self.nseq, self.B, self.V, self.temperature = int(nseq), int(B), int(V), float(temperature)
+        i32 = lambda *shape: _empty(shape, dtype=torch.int32, device="cuda")  # noqa: E731
+        self.out = dict(n_rows=i32(nseq), rows=i32(nseq, B + 1), tokens=i32(nseq, B + 1),
+                        logp=_empty((nseq, B + 1), dtype=torch.float32, device="cuda"))
+
+    def __call__(self, logits, tokens, parents, n_nodes, u=None, noise=None, stream=None):
+        """logits [nseq, B + 1, V] bf16 or fp32 (rows may be padded); tokens,
+        parents [nseq, B] and n_nodes [nseq] int32 as emitted; u [nseq, B + 1]
+        uniform and noise [nseq, V] Exp(1) fp32 (temperature 0: none).
+        Returns the dict of outputs: what KVCache.append takes is in it."""
+        nseq, B, V = self.nseq, self.B, self.V
+        if logits.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("logits: float32 or bfloat16 expected")
+        z = _expect(logits, "logits", logits.dtype, (nseq, B + 1, V), dense=False)
+        if logits.stride(2) != 1 and V > 1 or nseq > 1 and logits.stride(0) != (B + 1) * logits.stride(1):
+            raise ValueError("logits: dense rows, one stride between all of them expected")
+        cfg = DartVerifyConfig(nseq, B, V, DART_F32 if logits.dtype == torch.float32 else DART_BF16, logits.stride(1),
+                               self.temperature)
+        tree = [_expect(t, m, torch.int32, shape) for t, m, shape in
+                ((tokens, "tokens", (nseq, B)), (parents, "parents", (nseq, B)), (n_nodes, "n_nodes", (nseq,)))]
+        rnd = (None, None)
+        if self.temperature > 0:
+            rnd = (_expect(u, "u", torch.float32, (nseq, B + 1)), _expect(noise, "noise", torch.float32, (nseq, V)))
+        o = self.out
+        _check(lib().dart_verify_tree(C.byref(cfg), z, *tree, *rnd, o["n_rows"].data_ptr(), o["rows"].data_ptr(),
+                                      o["tokens"].data_ptr(), o["logp"].data_ptr(), _stream(stream)), "dart_verify_tree")
+        return o
