@@ -472,30 +472,41 @@ class TreeAttention:
 
 # ------------------------------------------- paged cache (dart_cache.h)
 
-def _expect(t, name, dtype, shape, dense=True):
-    """Refuses a tensor that the C ABI, which sees a pointer, would misread."""
-    if t is None or t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        got = "None" if t is None else f"{t.dtype} {tuple(t.shape)}"
-        raise ValueError(f"{name}: {dtype} {tuple(shape)} expected, got {got}")
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, not on the current device")
-    if dense and not t.is_contiguous():
-        raise ValueError(f"{name} is not contiguous")
+def _bad(t, name, dtype, shape):
+    got = "None" if t is None else f"{t.dtype} {tuple(t.shape)} on {t.device}"
+    return ValueError(f"{name}: contiguous {dtype} {tuple(shape)} on the current device expected, got {got}")
+
+
+def _expect(t, name, dtype, shape, dev):
+    """Pointer of a dense tensor on device `dev`; refuses one that the C ABI,
+    which sees the pointer alone, would misread."""
+    if t is None or t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise _bad(t, name, dtype, shape)
     return t.data_ptr()
 
 
-def _rows(t, name, nseq, R, heads, dh):
+def _rows(t, name, shape, dev):
     """Pointer and row stride of [nseq][R][heads][dh] bf16 whose heads lie one
     after the other in each row (a slice of a fused projection, say)."""
-    p = _expect(t, name, torch.bfloat16, (nseq, R, heads, dh), dense=False)
+    if t is None or t.dtype is not torch.bfloat16 or t.shape != shape or t.get_device() != dev:
+        raise _bad(t, name, torch.bfloat16, shape)
+    nseq, R, heads, dh = shape
     ss, sr, sh, sd = t.stride()
-    if (dh > 1 and sd != 1) or (heads > 1 and sh != dh):
+    if sd != 1 or (sh != dh and heads > 1):
         raise ValueError(f"{name}: the heads of a row have to lie one after the other")
     if R == 1:
         sr = ss if nseq > 1 else max(sr, heads * dh)
-    elif nseq > 1 and ss != R * sr:
+    elif ss != R * sr and nseq > 1:
         raise ValueError(f"{name}: one stride between all rows of all sequences expected")
-    return p, sr
+    return t.data_ptr(), sr
+
+
+def _current(stream):
+    """The current device and the CUDA handle of `stream` (None: its current one)."""
+    dev = torch.cuda.current_device()
+    if stream is None:
+        return dev, torch._C._cuda_getCurrentRawStream(dev)
+    return dev, stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 class KVCache:
@@ -509,11 +520,14 @@ class KVCache:
         fp8 = k.dtype == torch.float8_e4m3fn
         if fp8 != (k_scale is not None) or fp8 != (v_scale is not None):
             raise ValueError("scales belong to float8_e4m3fn pages, and to those alone")
-        ptr = [_expect(k, "k", k.dtype, k.shape), _expect(v, "v", k.dtype, k.shape)]
-        ptr += [_expect(x, m, torch.float32, (n, heads, page)) if fp8 else None for x, m in ((k_scale, "k_scale"), (v_scale, "v_scale"))]
+        dev = torch.cuda.current_device()
+        ptr = [_expect(k, "k", k.dtype, k.shape, dev), _expect(v, "v", k.dtype, k.shape, dev)]
+        ptr += [_expect(x, m, torch.float32, (n, heads, page), dev) if fp8 else None
+                for x, m in ((k_scale, "k_scale"), (v_scale, "v_scale"))]
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.num_pages, self.Hkv, self.page_size, self.dh = n, heads, page, dh
         self.c = DartKvCache(n, page, heads, dh, DART_KV_E4M3 if fp8 else DART_KV_BF16, *ptr)
+        self.ref = C.byref(self.c)
 
     @classmethod
     def new(cls, num_pages, page_size, Hkv, dh=128, dtype=torch.bfloat16):
@@ -526,15 +540,17 @@ class KVCache:
         """Writes n_rows[s] tokens of every sequence from position lens[s] on:
         the rows rows[s, :n_rows[s]] of k and v [nseq, R, Hkv, dh] bf16 (rows
         None: the first ones).  lens is not advanced."""
+        dev, st = _current(stream)
         nseq, R = k.shape[:2]
-        kp, ks = _rows(k, "k", nseq, R, self.Hkv, self.dh)
-        vp, vs = _rows(v, "v", nseq, R, self.Hkv, self.dh)
-        table = _expect(page_table, "page_table", torch.int32, (nseq, page_table.shape[-1]))
-        n = _expect(n_rows, "n_rows", torch.int32, (nseq,))
-        at = _expect(lens, "lens", torch.int32, (nseq,))
-        src = None if rows is None else _expect(rows, "rows", torch.int32, (nseq, R))
-        _check(lib().dart_cache_append(C.byref(self.c), nseq, page_table.shape[-1], table, at, R, kp, ks, vp, vs, src, n,
-                                       rope_theta, _ptr(status), _stream(stream)), "dart_cache_append")
+        shape = (nseq, R, self.Hkv, self.dh)
+        kp, ks = _rows(k, "k", shape, dev)
+        vp, vs = _rows(v, "v", shape, dev)
+        pages = page_table.shape[-1]
+        _check(lib().dart_cache_append(
+            self.ref, nseq, pages, _expect(page_table, "page_table", torch.int32, (nseq, pages), dev),
+            _expect(lens, "lens", torch.int32, (nseq,), dev), R, kp, ks, vp, vs,
+            None if rows is None else _expect(rows, "rows", torch.int32, (nseq, R), dev),
+            _expect(n_rows, "n_rows", torch.int32, (nseq,), dev), rope_theta, _ptr(status), st), "dart_cache_append")
 
 
 class PagedTreeAttention:
@@ -542,10 +558,11 @@ class PagedTreeAttention:
     shape (nseq sequences, B nodes each, B = 0: single tokens)."""
 
     def __init__(self, cache, nseq, B, max_pages, Hq=32, rope_theta=1.0e6, scale=None):
-        self.cache = cache
+        self.cache, self.max_pages = cache, int(max_pages)
         self.cfg = DartPagedAttnConfig(int(nseq), int(B), int(max_pages), int(Hq), float(rope_theta),
                                        float(scale if scale is not None else cache.dh ** -0.5))
-        n = int(lib().dart_paged_attention_workspace(C.byref(self.cfg), C.byref(cache.c)))
+        self.ref = C.byref(self.cfg)
+        n = int(lib().dart_paged_attention_workspace(self.ref, cache.ref))
         if n == 0:
             raise DartError(DART_ERR_INVALID, "dart_paged_attention_workspace")
         self.workspace = _empty((n,), dtype=torch.uint8, device="cuda")
@@ -556,21 +573,20 @@ class PagedTreeAttention:
         (row 0: the last verified token), page_table [nseq, max_pages] and
         lens [nseq] int32; depths [nseq, B] int32, mask [nseq, B, ceil(B / 64)]
         int64 and n_nodes [nseq] int32 as emitted.  Returns self.out."""
-        c, kv = self.cfg, self.cache
-        nseq, B, R = c.nseq, c.B, c.B + 1
-        qp, qs = _rows(q, "q", nseq, R, c.Hq, kv.dh)
-        kp, ks = _rows(k_tree, "k_tree", nseq, R, kv.Hkv, kv.dh)
-        vp, vs = _rows(v_tree, "v_tree", nseq, R, kv.Hkv, kv.dh)
-        table = _expect(page_table, "page_table", torch.int32, (nseq, c.max_pages))
-        at = _expect(lens, "lens", torch.int32, (nseq,))
+        dev, st = _current(stream)
+        kv, (nseq, R, Hq, dh) = self.cache, self.out.shape
+        qp, qs = _rows(q, "q", (nseq, R, Hq, dh), dev)
+        kp, ks = _rows(k_tree, "k_tree", (nseq, R, kv.Hkv, dh), dev)
+        vp, vs = _rows(v_tree, "v_tree", (nseq, R, kv.Hkv, dh), dev)
         tree = (None, None, None)
-        if B:
-            tree = (_expect(depths, "depths", torch.int32, (nseq, B)),
-                    _expect(mask, "mask", torch.int64, (nseq, B, (B + 63) // 64)),
-                    _expect(n_nodes, "n_nodes", torch.int32, (nseq,)))
-        _check(lib().dart_paged_attention(C.byref(c), C.byref(kv.c), table, at, qp, qs, kp, ks, vp, vs, *tree,
-                                          self.out.data_ptr(), self.workspace.data_ptr(), self.workspace.numel(),
-                                          _ptr(status), _stream(stream)), "dart_paged_attention")
+        if R > 1:
+            tree = (_expect(depths, "depths", torch.int32, (nseq, R - 1), dev),
+                    _expect(mask, "mask", torch.int64, (nseq, R - 1, (R + 62) // 64), dev),
+                    _expect(n_nodes, "n_nodes", torch.int32, (nseq,), dev))
+        _check(lib().dart_paged_attention(
+            self.ref, kv.ref, _expect(page_table, "page_table", torch.int32, (nseq, self.max_pages), dev),
+            _expect(lens, "lens", torch.int32, (nseq,), dev), qp, qs, kp, ks, vp, vs, *tree, self.out.data_ptr(),
+            self.workspace.data_ptr(), self.workspace.numel(), _ptr(status), st), "dart_paged_attention")
         return self.out
 
 
@@ -581,30 +597,34 @@ class TreeVerifier:
     int32 and logp [nseq, B + 1] fp32."""
 
     def __init__(self, nseq, B, V, temperature=1.0):
-        self.nseq, self.B, self.V, self.temperature = int(nseq), int(B), int(V), float(temperature)
+        self.nseq, self.B, self.V = int(nseq), int(B), int(V)
+        self.cfg = DartVerifyConfig(self.nseq, self.B, self.V, DART_F32, self.V, float(temperature))
+        self.ref = C.byref(self.cfg)
         i32 = lambda *shape: _empty(shape, dtype=torch.int32, device="cuda")  # noqa: E731
         self.out = dict(n_rows=i32(nseq), rows=i32(nseq, B + 1), tokens=i32(nseq, B + 1),
                         logp=_empty((nseq, B + 1), dtype=torch.float32, device="cuda"))
+        self.out_ptr = tuple(self.out[m].data_ptr() for m in ("n_rows", "rows", "tokens", "logp"))
 
     def __call__(self, logits, tokens, parents, n_nodes, u=None, noise=None, stream=None):
         """logits [nseq, B + 1, V] bf16 or fp32 (rows may be padded); tokens,
         parents [nseq, B] and n_nodes [nseq] int32 as emitted; u [nseq, B + 1]
         uniform and noise [nseq, V] Exp(1) fp32 (temperature 0: none).
         Returns the dict of outputs: what KVCache.append takes is in it."""
+        dev, st = _current(stream)
         nseq, B, V = self.nseq, self.B, self.V
-        if logits.dtype not in (torch.float32, torch.bfloat16):
-            raise ValueError("logits: float32 or bfloat16 expected")
-        z = _expect(logits, "logits", logits.dtype, (nseq, B + 1, V), dense=False)
-        if logits.stride(2) != 1 and V > 1 or nseq > 1 and logits.stride(0) != (B + 1) * logits.stride(1):
+        f32 = logits.dtype is torch.float32
+        if not f32 and logits.dtype is not torch.bfloat16 or logits.shape != (nseq, B + 1, V) or logits.get_device() != dev:
+            raise _bad(logits, "logits", "float32 or bfloat16", (nseq, B + 1, V))
+        ss, ld, one = logits.stride()
+        if one != 1 and V > 1 or ss != (B + 1) * ld and nseq > 1:
             raise ValueError("logits: dense rows, one stride between all of them expected")
-        cfg = DartVerifyConfig(nseq, B, V, DART_F32 if logits.dtype == torch.float32 else DART_BF16, logits.stride(1),
-                               self.temperature)
-        tree = [_expect(t, m, torch.int32, shape) for t, m, shape in
-                ((tokens, "tokens", (nseq, B)), (parents, "parents", (nseq, B)), (n_nodes, "n_nodes", (nseq,)))]
+        cfg = self.cfg
+        cfg.dtype, cfg.ld = DART_F32 if f32 else DART_BF16, ld
         rnd = (None, None)
-        if self.temperature > 0:
-            rnd = (_expect(u, "u", torch.float32, (nseq, B + 1)), _expect(noise, "noise", torch.float32, (nseq, V)))
-        o = self.out
-        _check(lib().dart_verify_tree(C.byref(cfg), z, *tree, *rnd, o["n_rows"].data_ptr(), o["rows"].data_ptr(),
-                                      o["tokens"].data_ptr(), o["logp"].data_ptr(), _stream(stream)), "dart_verify_tree")
-        return o
+        if cfg.temperature > 0:
+            rnd = _expect(u, "u", torch.float32, (nseq, B + 1), dev), _expect(noise, "noise", torch.float32, (nseq, V), dev)
+        _check(lib().dart_verify_tree(
+            self.ref, logits.data_ptr(), _expect(tokens, "tokens", torch.int32, (nseq, B), dev),
+            _expect(parents, "parents", torch.int32, (nseq, B), dev), _expect(n_nodes, "n_nodes", torch.int32, (nseq,), dev),
+            *rnd, *self.out_ptr, st), "dart_verify_tree")
+        return self.out
