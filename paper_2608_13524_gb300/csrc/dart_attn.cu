@@ -74,7 +74,7 @@ constexpr int kOCol = 128;
 constexpr int kPCol = 256;                // P tiles: 128 keys as 64 columns of bf16 pairs
 constexpr int kQCol = 384;                // rotated query tile: dh = 128 as 64 columns of bf16 pairs
 constexpr float kRescaleSlack = 8.0f;     // log2 units: P <= 2^8 between rescales
-constexpr int kNumBars = 1 + 2 * kKStages + 2 * kVStages + 2 + 5;
+constexpr int kNumBars = 1 + 2 * kKStages + 2 * kVStages + 2 + 6;
 constexpr int kSmemUsed = kTileBytes * (1 + kKStages + kVStages) + kNumBars * 8 + 4 * 4 + 2 * 128 * 4 + 8 * 4;  // Q, K/V rings, barriers, exchange
 constexpr int kAttnSmem = kSmemUsed + 1024;  // + alignment slack of the 1024-byte swizzle atoms
 
@@ -216,8 +216,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
     uint64_t* v_empty = v_full + kVStages;            // [kVStages] PV of the stage's tile done
     uint64_t* s_full = v_empty + kVStages;
     uint64_t* s_empty = s_full + 1;                   // softmax has S in registers
+    // [2] by P buffer: the softmax of tile i + 1 may be done before P(i) is waited for (the
+    // issuing thread fetching cold code), and one barrier would then be a phase too far
     uint64_t* p_full = s_empty + 1;
-    uint64_t* pv_done = p_full + 1;                   // [2] PV of a tile using P buffer b done
+    uint64_t* pv_done = p_full + 2;                   // [2] PV of a tile using P buffer b done
     uint64_t* tdown = pv_done + 2;
     uint64_t* q_ready = tdown + 1;                    // queries rotated in place
     int* misc = reinterpret_cast<int*>(bars + kNumBars);  // [0] TMEM base, [1] abort
@@ -250,7 +252,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
         }
         mbar_init(s_full, 1);
         mbar_init(s_empty, kSoftThreads);
-        mbar_init(p_full, kSoftThreads);
+        mbar_init(&p_full[0], kSoftThreads);
+        mbar_init(&p_full[1], kSoftThreads);
         mbar_init(&pv_done[0], 1);
         mbar_init(&pv_done[1], 1);
         mbar_init(tdown, 1);
@@ -376,7 +379,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                     break;
                 }
                 const int st = i % kVStages;
-                if (!mbar_wait_inline<kTilePolls>(p_full, static_cast<uint32_t>(i) & 1u, abort) ||
+                if (!mbar_wait_inline<kTilePolls>(&p_full[i & 1], static_cast<uint32_t>(i >> 1) & 1u, abort) ||
                     !mbar_wait_inline<kTilePolls>(&v_full[st], static_cast<uint32_t>(i / kVStages) & 1u, abort)) {
                     mok = false;
                     break;
@@ -555,7 +558,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
             tmem_wait_st();
             l += lsum;
             tc_fence_before();
-            mbar_arrive(p_full);
+            mbar_arrive(&p_full[i & 1]);
         }
         if (ok && nt > 0) {
             if (!warp_wait<kTilePolls>(&pv_done[(nt - 1) & 1], static_cast<uint32_t>((nt - 1) >> 1) & 1u, abort)) {
