@@ -29,20 +29,27 @@
 
 #include "../../include/dart.h"
 #include "../../include/dart_cache.h"
-#include "dart_cache.cuh"
 #include "dart_kernels.h"
+#include "dart_paged.cuh"
 
 namespace dart {
 
-bool valid_cache(const dart_kv_cache* c);
-bool valid_cache_pointers(const dart_kv_cache* c);
+bool encode_rows(CUtensorMap* m, const void* base, long long rows, bool fp8, int box_rows) {
+    EncodeTiledFn fn = tensor_map_encoder();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {kHeadDim, static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(kHeadDim) * (fp8 ? 1 : 2)};
+    const cuuint32_t box[2] = {fp8 ? 128u : 64u, static_cast<cuuint32_t>(box_rows)}, estr[2] = {1, 1};
+    return fn(m, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides,
+              box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 namespace {
 
 constexpr int kUnitRows = 16;
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
-constexpr int kMaxSms = 256;   // workspace: two partial results for each of this many SMs' warps
 constexpr float kSlack = 8.0f;  // log2 units a score may exceed the row's reference by
 
 struct Part {  // a unit's partial result
@@ -50,30 +57,7 @@ struct Part {  // a unit's partial result
     float2 ml[kUnitRows];  // reference (log2 units), sum
 };
 
-struct PagedArgs {
-    int nseq, B, Hq, Hkv, G, nrg, max_pages, page_log2, num_pages, mw;
-    long long pool_rows;
-    const int32_t *table, *lens, *depths, *n_nodes;
-    const uint64_t* mask;
-    const __nv_bfloat16 *q, *k, *v;
-    long long q_stride, k_stride, v_stride;
-    const float *ks, *vs;
-    __nv_bfloat16* out;
-    Part* parts;  // [warps][2]: of the unit begun before the warp's share, of the unit that goes on after it
-    int* status;
-    float sl2;  // scale * log2(e)
-    RopeTurns turns;
-};
-
 // ------------------------------------------------------------ the schedule
-
-__device__ __forceinline__ int seq_len(const PagedArgs& a, int s) {
-    const long long most = static_cast<long long>(a.max_pages) << a.page_log2;
-    return static_cast<int>(min(max(static_cast<long long>(__ldg(a.lens + s)), 0ll), most));
-}
-__device__ __forceinline__ int seq_nodes(const PagedArgs& a, int s) {
-    return a.B > 0 ? min(max(__ldg(a.n_nodes + s), 0), a.B) : 0;
-}
 
 // Chunk sizes, and what a unit costs beside its chunks (queries, tree rows,
 // the result), in chunks: its list is that much longer, so that warps with
@@ -159,17 +143,11 @@ __device__ __forceinline__ Place<kFp8> find_place(const PagedArgs& a, long long 
     return r;
 }
 
-// Shares: how many there are (each at least kMinShare long), where share i
-// begins and which one place x is in.
+// Shares: one per warp, each at least kMinShare long.
 constexpr int kMinShare = 2;
 __device__ __forceinline__ int share_count(long long all, int warps) {
     return static_cast<int>(min(static_cast<long long>(warps), (all + kMinShare - 1) / kMinShare));
 }
-__device__ __forceinline__ long long share_begin(long long all, int shares, int i) { return all * i / shares; }
-__device__ __forceinline__ int share_at(long long all, int shares, long long x) {
-    return static_cast<int>(((x + 1) * shares - 1) / all);
-}
-
 // ------------------------------------------------------------ fragments
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -183,11 +161,6 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
 }
 // Two e4m3 codes (low, high byte) as an f16 pair: exact.
 __device__ __forceinline__ uint32_t e4m3_to_f16(uint32_t two) {
@@ -268,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     int n_load = 0, n_use = 0;
     int failed = 0;
     volatile int* abort = &failed;
-    const uint64_t policy = a.nrg == 1 ? l2_policy_evict_first() : l2_policy_evict_last();
+    const uint64_t policy = (a.B + 1) * a.G <= kUnitRows ? l2_policy_evict_first() : l2_policy_evict_last();
     const int page_mask = (1 << a.page_log2) - 1;
 
     // Moves `load` to the next chunk of the cache in this share (or past it).
@@ -709,7 +682,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
         // ---- the result, or this part of it
         const bool whole = c0 == 0 && c1 == chunks;
-        Part* part = a.parts + 2 * static_cast<long long>(share) + (c0 > 0 ? 0 : 1);
+        Part* part = static_cast<Part*>(a.parts) + 2 * static_cast<long long>(share) + (c0 > 0 ? 0 : 1);
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             l[h] += __shfl_xor_sync(kFull, l[h], 1);
@@ -759,7 +732,7 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
     pdl_trigger();
     pdl_wait();
     const int tid = threadIdx.x, lane = tid & 31;
-    const int per = a.Hkv * a.nrg, s = blockIdx.x / per;
+    const int per = a.Hkv * (((a.B + 1) * a.G + kUnitRows - 1) / kUnitRows), s = blockIdx.x / per;
     Place<kFp8> p{};
     p.s = s;
     p.unit = blockIdx.x % per;
@@ -776,7 +749,7 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
     while (span < rows) span *= 2;
     const int slot_of_row = tid >> 4, d8 = tid & 15, r = slot_of_row % span, part0 = slot_of_row / span, step = kUnitRows / span;
     const bool live = r < rows;
-    auto slot = [&](int c) { return a.parts + 2 * static_cast<long long>(c) + (share_begin(all, shares, c) > first ? 0 : 1); };
+    auto slot = [&](int c) { return static_cast<const Part*>(a.parts) + 2 * static_cast<long long>(c) + (share_begin(all, shares, c) > first ? 0 : 1); };
     float top = -INFINITY, l = 0.0f, o[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     if (live)
         for (int c = c0 + part0; c <= c1; c += step) {
@@ -826,20 +799,13 @@ bool valid_cfg(const dart_paged_attn_config* c, const dart_kv_cache* cache) {
     if (!(c->rope_theta > 1.0f) || !std::isfinite(c->rope_theta) || !(c->scale > 0.0f) || !std::isfinite(c->scale)) return false;
     // positions (with the tree's depths) and the numbers of rows are 32-bit
     if (static_cast<long long>(c->max_pages) * cache->page_size > (1ll << 30)) return false;
-    return static_cast<long long>(c->nseq) * (c->B + 1) * c->Hq <= (1ll << 30);
+    return static_cast<long long>(c->nseq) * (c->B + 1) * c->Hq <= (1ll << 30) &&
+           static_cast<long long>(c->nseq) * cache->Hkv * (c->B + 256) <= (1ll << 30);
 }
 
-// Rows of dh elements (the whole pool) in boxes of box_rows rows by 128 bytes.
-bool encode_pool(CUtensorMap* m, const void* base, long long rows, bool fp8, int box_rows) {
-    EncodeTiledFn fn = tensor_map_encoder();
-    if (!fn) return false;
-    const cuuint64_t dims[2] = {kHeadDim, static_cast<cuuint64_t>(rows)};
-    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(kHeadDim) * (fp8 ? 1 : 2)};
-    const cuuint32_t box[2] = {fp8 ? 128u : 64u, static_cast<cuuint32_t>(box_rows)}, estr[2] = {1, 1};
-    return fn(m, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides,
-              box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
+// Which kernel: rows that fit one 16-row product are streamed from HBM, more
+// are 128-row tiles of the tensor-memory path.
+bool few_rows(const dart_paged_attn_config& c, const dart_kv_cache& cache) { return (c.B + 1) * (c.Hq / cache.Hkv) <= kUnitRows; }
 
 // The device's number of SMs; 0 if it is not sm_103a, -1 on an error.  The
 // shared-memory opt-in of the kernels is set on the first call per device.
@@ -857,6 +823,7 @@ int device_sms(int dev) {
     if (cudaFuncSetAttribute(paged_rows_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<false>::kSmem) != cudaSuccess ||
         cudaFuncSetAttribute(paged_rows_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<true>::kSmem) != cudaSuccess)
         return -1;
+    if (!paged_tiles_prepare_device()) return -1;
     known[dev].store(sms, std::memory_order_release);
     return sms;
 }
@@ -870,7 +837,8 @@ extern "C" {
 
 size_t dart_paged_attention_workspace(const dart_paged_attn_config* cfg, const dart_kv_cache* cache) {
     if (!valid_cfg(cfg, cache)) return 0;
-    return sizeof(Part) * 2 * kWarps * kMaxSms;
+    if (few_rows(*cfg, *cache)) return sizeof(Part) * 2 * kWarps * kMaxSms;
+    return paged_tiles_workspace(*cfg, *cache);
 }
 
 int dart_paged_attention(const dart_paged_attn_config* cfg, const dart_kv_cache* cache, const int32_t* page_table,
@@ -901,7 +869,6 @@ int dart_paged_attention(const dart_paged_attn_config* cfg, const dart_kv_cache*
     a.Hq = c.Hq;
     a.Hkv = cache->Hkv;
     a.G = c.Hq / cache->Hkv;
-    a.nrg = ((c.B + 1) * a.G + kUnitRows - 1) / kUnitRows;
     a.max_pages = c.max_pages;
     while ((1 << a.page_log2) < cache->page_size) a.page_log2++;
     a.num_pages = cache->num_pages;
@@ -921,19 +888,20 @@ int dart_paged_attention(const dart_paged_attn_config* cfg, const dart_kv_cache*
     a.ks = cache->k_scale;
     a.vs = cache->v_scale;
     a.out = static_cast<__nv_bfloat16*>(out);
-    a.parts = static_cast<Part*>(workspace);
+    a.parts = workspace;
     a.status = status;
     a.sl2 = static_cast<float>(static_cast<double>(c.scale) * 1.4426950408889634);
     a.turns = rope_turns(c.rope_theta);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (!few_rows(c, *cache)) return launch_paged_tiles(a, *cache, static_cast<uint8_t*>(workspace), std::min(sms, kMaxSms), st);
     const int box = fp8 && cache->page_size >= 32 ? 32 : 16;
     CUtensorMap tmK, tmV;
-    if (!encode_pool(&tmK, cache->k, a.pool_rows, fp8, box) || !encode_pool(&tmV, cache->v, a.pool_rows, fp8, box)) return DART_ERR_CUDA;
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (!encode_rows(&tmK, cache->k, a.pool_rows, fp8, box) || !encode_rows(&tmV, cache->v, a.pool_rows, fp8, box)) return DART_ERR_CUDA;
     const int ctas = std::min(sms, kMaxSms);
     cudaError_t e = fp8 ? launch_pdl(paged_rows_kernel<true>, dim3(ctas), dim3(kThreads), Geo<true>::kSmem, st, tmK, tmV, a)
                         : launch_pdl(paged_rows_kernel<false>, dim3(ctas), dim3(kThreads), Geo<false>::kSmem, st, tmK, tmV, a);
     if (e != cudaSuccess) return DART_ERR_CUDA;
-    const dim3 units(c.nseq * a.Hkv * a.nrg);
+    const dim3 units(c.nseq * a.Hkv * (((c.B + 1) * a.G + kUnitRows - 1) / kUnitRows));
     e = fp8 ? launch_pdl(paged_join_kernel<true>, units, dim3(kThreads), 0, st, a, kWarps * ctas)
             : launch_pdl(paged_join_kernel<false>, units, dim3(kThreads), 0, st, a, kWarps * ctas);
     if (e != cudaSuccess) return DART_ERR_CUDA;

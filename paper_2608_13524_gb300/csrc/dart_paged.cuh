@@ -1,0 +1,61 @@
+// What the two kernels of the paged attention share: arguments, and the even
+// division of a list of work over shares (a unit's place in the list is known
+// to everyone, so is who holds which part of it).
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include "../../include/dart_cache.h"
+#include "dart_cache.cuh"
+
+namespace dart {
+
+constexpr int kMaxSms = 160;  // shares are counted by SMs; the workspace has room for this many
+
+struct PagedArgs {
+    int nseq, B, Hq, Hkv, G, max_pages, page_log2, num_pages, mw;
+    long long pool_rows;
+    const int32_t *table, *lens, *depths, *n_nodes;
+    const uint64_t* mask;
+    const __nv_bfloat16 *q, *k, *v;
+    long long q_stride, k_stride, v_stride;
+    const float *ks, *vs;
+    __nv_bfloat16* out;
+    void* parts;  // partial results, two per share: of the unit begun before it, of the unit that goes on after it
+    int* status;
+    float sl2;  // scale * log2(e)
+    RopeTurns turns;
+};
+
+__device__ __forceinline__ int seq_len(const PagedArgs& a, int s) {
+    const long long most = static_cast<long long>(a.max_pages) << a.page_log2;
+    return static_cast<int>(min(max(static_cast<long long>(__ldg(a.lens + s)), 0ll), most));
+}
+__device__ __forceinline__ int seq_nodes(const PagedArgs& a, int s) {
+    return a.B > 0 ? min(max(__ldg(a.n_nodes + s), 0), a.B) : 0;
+}
+
+// Shares of a list of length `all`: where share i begins, which one place x is in.
+__device__ __forceinline__ long long share_begin(long long all, int shares, int i) { return all * i / shares; }
+__device__ __forceinline__ int share_at(long long all, int shares, long long x) {
+    return static_cast<int>(((x + 1) * shares - 1) / all);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+bool valid_cache(const dart_kv_cache* c);
+bool valid_cache_pointers(const dart_kv_cache* c);
+// Rows of dh elements (the whole pool) in boxes of box_rows rows by 128 bytes.
+bool encode_rows(CUtensorMap* m, const void* base, long long rows, bool fp8, int box_rows);
+
+// 128-row tiles on the tensor-memory path (dart_paged_tiles.cu).
+size_t paged_tiles_workspace(const dart_paged_attn_config& c, const dart_kv_cache& cache);
+bool paged_tiles_prepare_device();  // kernel attributes, once per device
+int launch_paged_tiles(PagedArgs a, const dart_kv_cache& cache, uint8_t* workspace, int sms, cudaStream_t st);
+
+}  // namespace dart

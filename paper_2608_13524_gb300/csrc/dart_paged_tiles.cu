@@ -1,0 +1,876 @@
+// Tree attention over the paged cache for more than 16 query rows per kv head:
+// 128-row tiles on the tensor cores (tcgen05, operands and accumulators in
+// tensor memory).  Contract: include/dart_cache.h.
+//
+// Launches of a call:
+//   paged_prep_kernel  rotated queries, one row per (kv head, tree row, head
+//       of the group); and, per sequence and kv head, the "side" keys and
+//       values: the last len % 128 cache tokens (in bf16), the tree rows
+//       (keys rotated), zeros up to a multiple of 128.  So all other cache
+//       tiles are whole, need no mask, and nothing unwritten is ever read.
+//   paged_tiles_kernel  a unit is 128 query rows of a kv head against the
+//       whole cache tiles and the side tiles that its rows may see.  The
+//       tiles of all units form one list that the CTAs (one per SM) share
+//       evenly: ragged lengths, one long sequence and many short ones load
+//       every SM alike.  A CTA runs through its units without a pause: loads
+//       run ahead across units, and a unit's queries are in tensor memory
+//       before the unit before it has ended.
+//   paged_tiles_join_kernel  joins the units that several CTAs shared.
+//
+// Roles in a CTA: warp 0 loads tiles by TMA, page by page (K ring, V ring);
+// warp 1 issues the MMAs; warps 2-9 are two softmax warpgroups (thread = query
+// row = TMEM lane; warpgroup wg owns key and output columns [64 wg, 64 wg +
+// 64), the two warps of a lane quarter exchange maxima and sums); e4m3 pages
+// have four more warps that turn raw tiles into bf16 operands (exact), while
+// the scales are applied to scores and probabilities.  TMEM (512 columns): S
+// [0,128), O [128,256), P [256,384) in two buffers, Q [384,512) in two.
+// A row's running maximum is raised (and O rescaled) only when a tile exceeds
+// it by more than 2^8.  Every wait is bounded.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <cstring>
+
+#include "../../include/dart.h"
+#include "dart_kernels.h"
+#include "dart_paged.cuh"
+#include "dart_tmem.cuh"
+
+namespace dart {
+namespace {
+
+constexpr int kRows = 128;               // query rows per unit (MMA M)
+constexpr int kKeys = 128;               // keys per tile
+constexpr int kHalf = kKeys * 128;       // 128 rows of one 128-byte swizzle column
+constexpr int kTile = 2 * kHalf;         // 128 keys of bf16
+constexpr int kSoft = 256;               // softmax threads
+constexpr int kPairBar = 2;              // named barriers 2 .. 5
+constexpr float kSlack8 = 8.0f;          // log2 units: P <= 2^8 between rescales
+constexpr int kTileCost = 1;             // of a unit beside its tiles, in tiles
+constexpr int kMinTiles = 2;             // of a share
+constexpr uint32_t kSCol = 0, kOCol = 128, kPCol = 256, kQCol = 384;
+
+struct TilePart {
+    float o[kRows][kHeadDim];
+    float2 ml[kRows];
+};
+
+struct TileArgs {
+    PagedArgs p;
+    int sk;                    // side keys per sequence and kv head (a multiple of 128)
+    __nv_bfloat16* qr;         // [nseq][Hkv][(B + 1) * G][128]
+    __nv_bfloat16 *side_k, *side_v;  // [nseq][Hkv][sk][128]
+};
+
+// ------------------------------------------------------------ preparation
+
+// One warp per (sequence, side row, kv head): the side row's key and value,
+// and, if it is a tree row, the rotated queries of its G heads.
+__global__ void __launch_bounds__(256) paged_prep_kernel(const __grid_constant__ TileArgs ta, const uint8_t* pool_k, const uint8_t* pool_v) {
+    const PagedArgs& a = ta.p;
+    pdl_trigger();
+    pdl_wait();
+    const int lane = threadIdx.x & 31;
+    const long long id = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) >> 5;
+    const int head = static_cast<int>(id % a.Hkv), j = static_cast<int>(id / a.Hkv % ta.sk);
+    const int s = static_cast<int>(id / a.Hkv / ta.sk);
+    if (s >= a.nseq) return;
+    const int len = seq_len(a, s), nodes = seq_nodes(a, s), tail = len % kKeys, b = j - tail;
+    uint32_t* ok = reinterpret_cast<uint32_t*>(ta.side_k + ((static_cast<long long>(s) * a.Hkv + head) * ta.sk + j) * kHeadDim) + lane;
+    uint32_t* ov = reinterpret_cast<uint32_t*>(ta.side_v + ((static_cast<long long>(s) * a.Hkv + head) * ta.sk + j) * kHeadDim) + lane;
+    uint32_t k[2] = {0u, 0u}, v[2] = {0u, 0u};  // elements 2 lane, 2 lane + 1 and the same 64 further
+    if (b < 0) {
+        const int key = len - tail + j;
+        const int page = __ldg(a.table + static_cast<long long>(s) * a.max_pages + (key >> a.page_log2));
+        if (page < 0 || page >= a.num_pages) {
+            if (a.status && lane == 0) atomicOr(a.status, kDevBounds);
+        } else {
+            const long long row = ((static_cast<long long>(page) * a.Hkv + head) << a.page_log2) + (key & ((1 << a.page_log2) - 1));
+            if (a.ks) {
+                const float ks = __ldg(a.ks + row), vs = __ldg(a.vs + row);
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const long long at = row * kHeadDim + 64 * h + 2 * lane;
+                    uint32_t x = *reinterpret_cast<const uint16_t*>(pool_k + at), y = *reinterpret_cast<const uint16_t*>(pool_v + at), f, g;
+                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f) : "h"(static_cast<uint16_t>(x)));
+                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(g) : "h"(static_cast<uint16_t>(y)));
+                    const float2 kf = __half22float2(*reinterpret_cast<const __half2*>(&f)), vf = __half22float2(*reinterpret_cast<const __half2*>(&g));
+                    k[h] = pack_bf16x2(kf.x * ks, kf.y * ks);
+                    v[h] = pack_bf16x2(vf.x * vs, vf.y * vs);
+                }
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    k[h] = *reinterpret_cast<const uint32_t*>(pool_k + (row * kHeadDim + 64 * h + 2 * lane) * 2);
+                    v[h] = *reinterpret_cast<const uint32_t*>(pool_v + (row * kHeadDim + 64 * h + 2 * lane) * 2);
+                }
+            }
+        }
+    } else if (b <= a.B) {
+        const long long in = static_cast<long long>(s) * (a.B + 1) + b;
+        uint32_t* qr = reinterpret_cast<uint32_t*>(
+                           ta.qr + ((static_cast<long long>(s) * a.Hkv + head) * (a.B + 1) * a.G + static_cast<long long>(b) * a.G) * kHeadDim) + lane;
+        if (b <= nodes) {
+            const uint32_t* kp = reinterpret_cast<const uint32_t*>(a.k + in * a.k_stride + head * kHeadDim) + lane;
+            const uint32_t* vp = reinterpret_cast<const uint32_t*>(a.v + in * a.v_stride + head * kHeadDim) + lane;
+            const uint32_t x = __ldg(kp), y = __ldg(kp + 32);
+            v[0] = __ldg(vp);
+            v[1] = __ldg(vp + 32);
+            const int pos = len + (b > 0 ? __ldg(a.depths + static_cast<long long>(s) * a.B + b - 1) : 0);
+            float s0, c0, s1, c1;
+            rope_sincos(a.turns.f[2 * lane], pos, &s0, &c0);
+            rope_sincos(a.turns.f[2 * lane + 1], pos, &s1, &c1);
+            auto turn = [&](uint32_t lo, uint32_t hi, uint32_t (&o)[2]) {
+                const float x0 = bf16_lo(lo), x1 = bf16_hi(lo), y0 = bf16_lo(hi), y1 = bf16_hi(hi);
+                o[0] = pack_bf16x2(x0 * c0 - y0 * s0, x1 * c1 - y1 * s1);
+                o[1] = pack_bf16x2(y0 * c0 + x0 * s0, y1 * c1 + x1 * s1);
+            };
+            turn(x, y, k);
+            const uint32_t* qp = reinterpret_cast<const uint32_t*>(a.q + in * a.q_stride + head * a.G * kHeadDim) + lane;
+#pragma unroll 4
+            for (int g = 0; g < a.G; g++) {
+                uint32_t o[2];
+                turn(__ldg(qp + g * 64), __ldg(qp + g * 64 + 32), o);
+                qr[g * 64] = o[0];
+                qr[g * 64 + 32] = o[1];
+            }
+        } else {
+            uint2* out = reinterpret_cast<uint2*>(a.out + (in * a.Hq + head * a.G) * kHeadDim) + lane;
+            for (int g = 0; g < a.G; g++) {
+                qr[g * 64] = qr[g * 64 + 32] = 0u;
+                out[g * 32] = make_uint2(0u, 0u);
+            }
+        }
+    }
+    ok[0] = k[0];
+    ok[32] = k[1];
+    ov[0] = v[0];
+    ov[32] = v[1];
+}
+
+// ------------------------------------------------------------ the schedule
+
+struct TilePlace {
+    int s, unit, tile;
+    int len, nodes, whole, tail, cost, nqt, units;  // of the sequence: whole cache tiles, cache tokens beside them, ...
+    __device__ __forceinline__ void load(const PagedArgs& a) {
+        len = seq_len(a, s);
+        nodes = seq_nodes(a, s);
+        whole = len / kKeys;
+        tail = len % kKeys;
+        cost = whole + (tail + nodes) / kKeys + 1 + kTileCost;
+        nqt = ((nodes + 1) * a.G + kRows - 1) / kRows;
+        units = a.Hkv * nqt;
+    }
+    // Tiles of the unit: its last row sees tree rows up to itself.
+    __device__ __forceinline__ int tiles(const PagedArgs& a) const {
+        const int last = min(((unit % nqt + 1) * kRows - 1) / a.G, nodes);
+        return whole + (tail + last) / kKeys + 1;
+    }
+    __device__ __forceinline__ void next_unit(const PagedArgs& a) {
+        tile = 0;
+        if (++unit == units) {
+            unit = 0;
+            if (++s < a.nseq) load(a);
+        }
+    }
+};
+
+__device__ __forceinline__ long long tile_cost_before(const PagedArgs& a, int upto, int lane) {
+    long long n = 0;
+    for (int s = lane; s < upto; s += 32) {
+        TilePlace p{};
+        p.s = s;
+        p.load(a);
+        n += static_cast<long long>(p.units) * p.cost;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(kFull, n, o);
+    return n;
+}
+
+__device__ __forceinline__ TilePlace find_tile(const PagedArgs& a, long long x, int lane) {
+    long long done = 0;
+    TilePlace r{};
+    for (int s0 = 0; s0 < a.nseq; s0 += 32) {
+        TilePlace p{};
+        p.s = s0 + lane;
+        long long n = 0;
+        if (p.s < a.nseq) {
+            p.load(a);
+            n = static_cast<long long>(p.units) * p.cost;
+        }
+        long long upto = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(kFull, upto, o);
+            if (lane >= o) upto += y;
+        }
+        const unsigned hit = __ballot_sync(kFull, p.s < a.nseq && x < done + upto);
+        if (hit) {
+            const int l = __ffs(hit) - 1;
+            const long long rest = x - done - __shfl_sync(kFull, upto - n, l);
+            r.s = s0 + l;
+            r.load(a);
+            r.unit = static_cast<int>(rest / r.cost);
+            r.tile = static_cast<int>(rest - static_cast<long long>(r.unit) * r.cost);
+            return r;
+        }
+        done += __shfl_sync(kFull, upto, 31);
+    }
+    r.s = a.nseq;
+    return r;
+}
+
+__device__ __forceinline__ int tile_shares(long long all, int ctas) {
+    return static_cast<int>(min(static_cast<long long>(ctas), (all + kMinTiles - 1) / kMinTiles));
+}
+
+// A share's parts of units, one after the other.
+struct Walk {
+    TilePlace p;
+    long long left;  // places of the share from p on
+    int s, head, qt, t0, t1, tiles, whole, tail, nodes;  // the part at hand: tiles [t0, t1) of a unit of `tiles`
+    __device__ __forceinline__ bool next(const PagedArgs& a) {
+        while (left > 0) {
+            tiles = p.tiles(a);
+            t0 = p.tile;
+            t1 = static_cast<int>(min(static_cast<long long>(tiles), t0 + left));
+            s = p.s;
+            head = p.unit / p.nqt;
+            qt = p.unit % p.nqt;
+            whole = p.whole;
+            tail = p.tail;
+            nodes = p.nodes;
+            left -= p.cost - p.tile;
+            p.next_unit(a);
+            if (t0 < t1) return true;
+        }
+        return false;
+    }
+};
+
+// ------------------------------------------------------------ the tiles
+
+template <bool kFp8>
+struct TGeo {
+    // bf16: three operand tiles of K and of V.  e4m3: two of each, and raw
+    // tiles of half the size before them.
+    static constexpr int kStages = kFp8 ? 2 : 3;
+    static constexpr int kRawK = kFp8 ? 3 : 0, kRawV = kFp8 ? 2 : 0;
+    static constexpr int kRing = 4;  // scales outlive their tiles' operands
+    static constexpr int kOps = 2 * kStages * kTile;
+    static constexpr int kRaw = (kRawK + kRawV) * kHalf;
+    static constexpr int kRawScales = kRawK * 2 * kKeys * 4;
+    static constexpr int kScales = kFp8 ? kRing * 2 * kKeys * 4 : 0;
+    static constexpr int kBars = 4 * kStages + 2 * (kRawK + kRawV) + (kFp8 ? kRing : 0) + 9 + 1;
+    static constexpr int kExchange = 2 * kRows * 4 + 8 * 4;
+    static constexpr int kSmem = kOps + kRaw + kRawScales + kScales + kBars * 8 + kExchange + 16;
+    static constexpr int kThreads = 64 + kSoft + (kFp8 ? 128 : 0);
+};
+
+__device__ __forceinline__ uint32_t tile_swz(int row, int piece) { return static_cast<uint32_t>(row * 128 + ((piece ^ (row & 7)) << 4)); }
+
+// Two e4m3 codes in bytes 1 and 3 of x (bytes 0 and 2: anything) as a bf16
+// pair: sign, then exponent and mantissa four bits down, and a product with
+// 2^120 for the difference of the exponents' biases (exact, subnormals too).
+__device__ __forceinline__ uint32_t codes_to_bf16(uint32_t x) {
+    const uint32_t y = ((x >> 4) & 0x07F007F0u) | (x & 0x80008000u);
+    const __nv_bfloat162 by = __halves2bfloat162(__ushort_as_bfloat16(0x7B80), __ushort_as_bfloat16(0x7B80));  // 2^120
+    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&y), by);
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+
+// Bits [o, o + 64) of a row of mask words (o >= -128; bits outside are 0).
+__device__ __forceinline__ uint64_t mask_bits(const uint64_t* m, int mw, int o) {
+    if (o <= -64) return 0ull;
+    if (o < 0) return __ldg(m) << -o;
+    const int w = o >> 6, sh = o & 63;
+    uint64_t r = w < mw ? __ldg(m + w) >> sh : 0ull;
+    if (sh && w + 1 < mw) r |= __ldg(m + w + 1) << (64 - sh);
+    return r;
+}
+
+template <bool kFp8>
+__global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
+    paged_tiles_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                       const __grid_constant__ CUtensorMap tmSk, const __grid_constant__ CUtensorMap tmSv,
+                       const __grid_constant__ TileArgs ta) {
+    using G_ = TGeo<kFp8>;
+    constexpr int kStages = G_::kStages;
+    const PagedArgs& a = ta.p;
+    extern __shared__ __align__(1024) uint8_t tiles_smem[];
+    uint8_t* sK = tiles_smem;
+    uint8_t* sV = sK + kStages * kTile;
+    uint8_t* rK = sV + kStages * kTile;  // raw tiles
+    uint8_t* rV = rK + G_::kRawK * kHalf;
+    float* raw_scales = reinterpret_cast<float*>(rV + G_::kRawV * kHalf);  // [raw K stage][K, V][key]
+    float* scales = raw_scales + G_::kRawK * 2 * kKeys;                    // [tile % 4][K * sl2, V][key]
+    uint64_t* k_full = reinterpret_cast<uint64_t*>(scales + G_::kScales / 4);
+    uint64_t* k_empty = k_full + kStages;   // S of the tile done
+    uint64_t* v_full = k_empty + kStages;
+    uint64_t* v_empty = v_full + kStages;   // PV of the tile done
+    uint64_t* rk_full = v_empty + kStages;
+    uint64_t* rk_empty = rk_full + G_::kRawK;
+    uint64_t* rv_full = rk_empty + G_::kRawK;
+    uint64_t* rv_empty = rv_full + G_::kRawV;
+    uint64_t* sc_full = rv_empty + G_::kRawV;
+    uint64_t* s_full = sc_full + (kFp8 ? G_::kRing : 0);
+    uint64_t* s_empty = s_full + 1;         // softmax has S in registers
+    uint64_t* p_full = s_empty + 1;         // [2] by P buffer (P(n + 1) may be there before P(n) is waited for)
+    uint64_t* pv_done = p_full + 2;         // [2] by P buffer
+    uint64_t* q_ready = pv_done + 2;        // [2] by Q buffer
+    uint64_t* o_free = q_ready + 2;         // the unit's O has been read
+    uint64_t* tdown = o_free + 1;
+    float* xch = reinterpret_cast<float*>(k_full + G_::kBars);  // [2][128] row max / sum exchange
+    int* xok = reinterpret_cast<int*>(xch + 2 * kRows);         // [2][4] "no wait failed"
+    int* misc = xok + 8;                                        // TMEM base, abort
+    volatile int* abort = &misc[1];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    pdl_trigger();
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; i++) {
+            mbar_init(&k_full[i], kFp8 ? 128 : 1);
+            mbar_init(&k_empty[i], 1);
+            mbar_init(&v_full[i], kFp8 ? 128 : 1);
+            mbar_init(&v_empty[i], 1);
+        }
+        for (int i = 0; i < G_::kRawK; i++) {
+            mbar_init(&rk_full[i], 1);
+            mbar_init(&rk_empty[i], 128);
+        }
+        for (int i = 0; i < G_::kRawV; i++) {
+            mbar_init(&rv_full[i], 1);
+            mbar_init(&rv_empty[i], 128);
+        }
+        if (kFp8)
+            for (int i = 0; i < G_::kRing; i++) mbar_init(&sc_full[i], 128);
+        mbar_init(s_full, 1);
+        mbar_init(s_empty, kSoft);
+        for (int i = 0; i < 2; i++) {
+            mbar_init(&p_full[i], kSoft);
+            mbar_init(&pv_done[i], 1);
+            mbar_init(&q_ready[i], kSoft);
+        }
+        mbar_init(o_free, kSoft);
+        mbar_init(tdown, 1);
+        misc[1] = 0;
+        fence_mbar_init();
+    }
+    if (warp == 1) {
+        tmem_alloc(reinterpret_cast<uint32_t*>(&misc[0]), 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = static_cast<uint32_t>(misc[0]);
+    pdl_wait();
+
+    const long long all = tile_cost_before(a, a.nseq, lane);
+    const int shares = tile_shares(all, gridDim.x);
+    Walk w{};
+    long long begin = 0;
+    if (static_cast<int>(blockIdx.x) < shares) {
+        begin = share_begin(all, shares, blockIdx.x);
+        w.left = share_begin(all, shares, blockIdx.x + 1) - begin;
+        w.p = find_tile(a, begin, lane);
+    }
+
+    if (warp == 0) {
+        // ---------------------------------------------------------- loads: the whole warp, a lane per page
+        const int per_tile = kKeys >> a.page_log2;  // pages of a tile
+        const uint64_t policy = (a.B + 1) * a.G <= kRows ? l2_policy_evict_first() : l2_policy_evict_last();
+        auto page_at = [&](int t) {
+            return t < w.whole && lane < per_tile
+                       ? __ldg(a.table + static_cast<long long>(w.s) * a.max_pages + static_cast<long long>(t) * per_tile + lane)
+                       : 0;
+        };
+        int n = 0;       // bf16: tiles so far; e4m3: whole cache tiles so far
+        bool have = w.next(a), ok = true;
+        int t = w.t0, page = have ? page_at(t) : 0;
+        while (have && ok) {
+            // this tile, then the next one's page numbers, which are there when it is its turn
+            const int head = w.head, s = w.s, tt = t, my_page = page;
+            const bool cache_tile = tt < w.whole;
+            const int side_row = (tt - w.whole) * kKeys;
+            if (++t == w.t1) {
+                have = w.next(a);
+                t = w.t0;
+            }
+            if (have) page = page_at(t);
+            if (kFp8 && !cache_tile) continue;  // (the converting warps read side tiles themselves)
+            long long row = a.pool_rows;  // past the pool: zeros
+            if (cache_tile && lane < per_tile) {
+                if (my_page >= 0 && my_page < a.num_pages)
+                    row = (static_cast<long long>(my_page) * a.Hkv + head) << a.page_log2;
+                else if (a.status)
+                    atomicOr(a.status, kDevBounds);
+            }
+            for (int kv = 0; kv < 2 && ok; kv++) {
+                const int stages = kFp8 ? (kv ? G_::kRawV : G_::kRawK) : kStages;
+                const int st = n % stages;
+                uint64_t* full = (kFp8 ? (kv ? rv_full : rk_full) : (kv ? v_full : k_full)) + st;
+                uint64_t* empty = (kFp8 ? (kv ? rv_empty : rk_empty) : (kv ? v_empty : k_empty)) + st;
+                uint8_t* dst = kFp8 ? (kv ? rV : rK) + st * kHalf : (kv ? sV : sK) + st * kTile;
+                const CUtensorMap* tm = cache_tile ? (kv ? &tmV : &tmK) : (kv ? &tmSv : &tmSk);
+                ok = warp_wait<kWaitPolls>(empty, (static_cast<uint32_t>(n / stages) & 1u) ^ 1u, abort);
+                if (!ok) break;
+                if (lane == 0)
+                    mbar_arrive_expect_tx(full, kFp8 ? kHalf + (kv ? 0 : 2 * kKeys * 4) : kTile);
+                __syncwarp();
+                if (!cache_tile) {
+                    if (lane < 2)
+                        tma_load_2d(dst + lane * kHalf, tm, full, 64 * lane, (s * a.Hkv + head) * ta.sk + side_row, policy);
+                } else if (lane < per_tile) {
+                    const uint32_t at = static_cast<uint32_t>(lane << a.page_log2) * 128;
+                    tma_load_2d(dst + at, tm, full, 0, static_cast<int>(row), policy);
+                    if (!kFp8) tma_load_2d(dst + kHalf + at, tm, full, 64, static_cast<int>(row), policy);
+                    if (kFp8 && kv == 0) {
+                        const long long sr = row < a.pool_rows ? row : 0;
+                        float* sc = raw_scales + st * 2 * kKeys + (lane << a.page_log2);
+                        bulk_load(sc, a.ks + sr, 4u << a.page_log2, full);
+                        bulk_load(sc + kKeys, a.vs + sr, 4u << a.page_log2, full);
+                    }
+                }
+            }
+            if (ok) n++;
+        }
+        if (!ok && lane == 0) attn_timeout(a.status, abort);
+        if (*abort) {
+            // copies still in flight must land before the CTA exits
+            for (int kv = 0; kv < 2; kv++) {
+                const int stages = kFp8 ? (kv ? G_::kRawV : G_::kRawK) : kStages;
+                uint64_t* full = kFp8 ? (kv ? rv_full : rk_full) : (kv ? v_full : k_full);
+                // (the tile at which a wait failed may have its K under way)
+                for (int i = max(n - stages, 0); i < n + (kv == 0 && !ok ? 1 : 0); i++)
+                    if (lane == 0) attn_drain(&full[i % stages], static_cast<uint32_t>(i / stages) & 1u);
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------------------------------------------------- MMAs
+        if (lane == 0) {
+            constexpr uint32_t idesc_s = idesc_bf16_f32(kRows, kKeys);
+            constexpr uint32_t idesc_pv = idesc_bf16_f32(kRows, kHeadDim) | (1u << 16);  // B (= V) MN-major
+            auto issue_s = [&](int n, int part) -> bool {
+                const int st = n % kStages;
+                if (!mbar_wait_inline(&k_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort) ||
+                    (n > 0 && !mbar_wait_inline(s_empty, static_cast<uint32_t>(n - 1) & 1u, abort)))
+                    return false;
+                tc_fence_after();
+                const uint32_t k_addr = smem_u32(sK + st * kTile);
+#pragma unroll
+                for (int kk = 0; kk < kHeadDim / 16; kk++)
+                    tc_mma_bf16_ts(tmem + kSCol, tmem + kQCol + (part & 1) * 64 + kk * 8,
+                                   sdesc_sw128(k_addr + (kk >> 2) * kHalf + (kk & 3) * 32), idesc_s, kk > 0 ? 1u : 0u);
+                tc_commit(s_full);
+                tc_commit(&k_empty[st]);
+                return true;
+            };
+            bool have = w.next(a), ok = true;
+            int n = 0, part = 0, t = w.t0, t1 = w.t1, t0 = w.t0;
+            if (have) {
+                ok = mbar_wait_inline(&q_ready[0], 0, abort);
+                tc_fence_after();
+                ok = ok && issue_s(0, 0);
+            }
+            while (have && ok) {
+                // tile t of part `part`; S of the tile after it first
+                const bool first = t == t0;
+                const int my_part = part;
+                if (++t == t1) {
+                    have = w.next(a);
+                    t = t0 = w.t0;
+                    t1 = w.t1;
+                    part++;
+                    if (have) ok = mbar_wait_inline(&q_ready[part & 1], static_cast<uint32_t>(part >> 1) & 1u, abort);
+                }
+                if (have && ok) {
+                    tc_fence_after();
+                    ok = issue_s(n + 1, part);
+                }
+                const int st = n % kStages;
+                ok = ok && mbar_wait_inline(&p_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, abort) &&
+                     mbar_wait_inline(&v_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort) &&
+                     (!first || my_part == 0 || mbar_wait_inline(o_free, static_cast<uint32_t>(my_part - 1) & 1u, abort));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t v_addr = smem_u32(sV + st * kTile);
+#pragma unroll
+                for (int kk = 0; kk < kKeys / 16; kk++)  // 16 keys = 8 columns of bf16 pairs
+                    tc_mma_bf16_ts(tmem + kOCol, tmem + kPCol + (n & 1) * 64 + kk * 8, sdesc_sw128_mn(v_addr + kk * 2048, kHalf),
+                                   idesc_pv, (!first || kk > 0) ? 1u : 0u);
+                tc_commit(&v_empty[st]);
+                tc_commit(&pv_done[n & 1]);
+                n++;
+            }
+            if (!ok) {
+                attn_timeout(a.status, abort);
+                tc_commit(tdown);
+                attn_drain(tdown, 0);
+            }
+        }
+    } else if (warp < 10) {
+        // ---------------------------------------------------------- softmax
+        const int qd = warp & 3, wg = (warp - 2) >> 2, cb = wg * 64;
+        const int r = qd * 32 + lane;  // query row of the unit = TMEM lane
+        const int pair_bar = kPairBar + qd;
+        const uint32_t tl = tmem + (static_cast<uint32_t>(qd * 32) << 16);
+        // this thread's half of its row's query into Q buffer `part & 1`
+        auto load_q = [&](const Walk& x, int part) {
+            const int rows = (x.nodes + 1) * a.G, row = x.qt * kRows + r;
+            uint32_t q[32];
+            const uint4* src = reinterpret_cast<const uint4*>(
+                ta.qr + ((static_cast<long long>(x.s) * a.Hkv + x.head) * (a.B + 1) * a.G + row) * kHeadDim + cb);
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const uint4 y = row < rows ? __ldg(src + e) : make_uint4(0u, 0u, 0u, 0u);
+                q[4 * e] = y.x;
+                q[4 * e + 1] = y.y;
+                q[4 * e + 2] = y.z;
+                q[4 * e + 3] = y.w;
+            }
+            tmem_st32(tl + kQCol + (part & 1) * 64 + wg * 32, q);
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(&q_ready[part & 1]);
+        };
+        bool have = w.next(a), ok = true;
+        if (have) load_q(w, 0);
+        int n = 0;
+        for (int part = 0; have; part++) {
+            const int s = w.s, head = w.head, t0 = w.t0, t1 = w.t1, whole = w.whole, tail = w.tail, nodes = w.nodes;
+            const bool full_unit = t0 == 0 && t1 == w.tiles;
+            const int row = w.qt * kRows + r, b = row / a.G;
+            const bool row_ok = b <= nodes;
+            float m_run = -INFINITY, l = 0.0f;
+            for (int t = t0; t < t1; t++, n++) {
+                // visible keys of this row among this warpgroup's 64 of the tile
+                uint64_t vis = row_ok ? ~0ull : 0ull;
+                if (t >= whole && row_ok) {
+                    const int o = (t - whole) * kKeys + cb - tail - 1;  // tree node of the first key (negative: cache, row 0)
+                    vis = 0ull;
+                    if (b > 0 && o < nodes) {
+                        vis = mask_bits(a.mask + (static_cast<long long>(s) * a.B + b - 1) * a.mw, a.mw, o);
+                        if (nodes - o < 64) vis &= (1ull << (nodes - o)) - 1ull;
+                    }
+                    if (o < 0) vis |= o <= -64 ? ~0ull : (1ull << -o) - 1ull;
+                }
+                const bool all_seen = __all_sync(kFull, vis == ~0ull);
+                // Both warps of the lane quarter reach both pair barriers of every
+                // iteration and leave the loop at the same point: a failed wait is
+                // exchanged with the row max and acted on after the barriers.
+                const float* ks = scales + (n % G_::kRing) * 2 * kKeys + cb;
+                if (kFp8 && ok && !warp_wait(&sc_full[n % G_::kRing], static_cast<uint32_t>(n / G_::kRing) & 1u, abort)) ok = false;
+                if (ok && !warp_wait<1>(s_full, static_cast<uint32_t>(n) & 1u, abort)) ok = false;
+                if (!ok) attn_timeout(a.status, abort);
+                float sv[64];
+                float mx = -INFINITY;
+                if (ok) {
+                    tc_fence_after();
+                    tmem_ld64(tl + kSCol + cb, sv);
+                    tc_fence_before();
+                    mbar_arrive(s_empty);
+                    if (kFp8) {
+#pragma unroll
+                        for (int c = 0; c < 64; c += 4) {
+                            const float4 y = *reinterpret_cast<const float4*>(ks + c);
+                            sv[c] *= y.x;
+                            sv[c + 1] *= y.y;
+                            sv[c + 2] *= y.z;
+                            sv[c + 3] *= y.w;
+                        }
+                    }
+                    if (all_seen) {
+#pragma unroll
+                        for (int c = 0; c < 64; c += 2) mx = fmaxf(mx, fmaxf(sv[c], sv[c + 1]));
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 64; c++) {
+                            if (!((vis >> c) & 1ull)) sv[c] = -INFINITY;
+                            mx = fmaxf(mx, sv[c]);
+                        }
+                    }
+                }
+                xch[wg * kRows + r] = mx;
+                if (lane == 0) xok[wg * 4 + qd] = ok ? 1 : 0;
+                named_bar_sync(pair_bar, 64);
+                mx = fmaxf(mx, xch[(1 - wg) * kRows + r]);
+                ok = ok && xok[(1 - wg) * 4 + qd] != 0;
+                named_bar_sync(pair_bar, 64);  // both read before the next tile's write
+                if (!ok) break;
+                const float mx2 = kFp8 ? mx : mx * a.sl2;
+                const bool resc = mx2 > m_run + kSlack8;
+                const float m_new = resc ? mx2 : m_run;
+                const float alpha = resc ? ex2(m_run - m_new) : 1.0f;
+                // P buffer n & 1 was last read by PV(n - 2); O must be stable (PV(n - 1)
+                // done) only when it is rescaled.  On a timeout this tile is
+                // skipped; the pair leaves the loop together at the next exchange.
+                if (n > 1 && !warp_wait<1>(&pv_done[n & 1], (static_cast<uint32_t>(n >> 1) & 1u) ^ 1u, abort)) {
+                    attn_timeout(a.status, abort);
+                    ok = false;
+                    continue;
+                }
+                tc_fence_after();
+                if (t > t0 && __any_sync(kFull, resc)) {
+                    if (!warp_wait<1>(&pv_done[(n - 1) & 1], static_cast<uint32_t>((n - 1) >> 1) & 1u, abort)) {
+                        attn_timeout(a.status, abort);
+                        ok = false;
+                        continue;
+                    }
+                    tc_fence_after();
+#pragma unroll
+                    for (int c0 = 0; c0 < 64; c0 += 16) {
+                        float o[16];
+                        tmem_ld16(tl + kOCol + cb + c0, o);
+#pragma unroll
+                        for (int e = 0; e < 16; e++) o[e] *= alpha;
+                        tmem_st16(tl + kOCol + cb + c0, o);
+                    }
+                    tmem_wait_st();
+                }
+                l *= alpha;
+                m_run = m_new;
+                // P = 2^(s - m) as bf16 pairs; hidden keys hold -inf and give 0 (so does
+                // every key of a row that has seen no visible key: m = -inf)
+                const float nm = m_run == -INFINITY ? 0.0f : -m_run;
+                float lsum = 0.0f;
+                uint32_t pk[32];
+#pragma unroll
+                for (int c = 0; c < 64; c += 4) {
+                    float4 y = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+                    if (kFp8) y = *reinterpret_cast<const float4*>(ks + kKeys + c);
+                    const float by[4] = {y.x, y.y, y.z, y.w};
+                    float p[4];
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        p[e] = kFp8 ? ex2(sv[c + e] + nm) : ex2(fmaf(sv[c + e], a.sl2, nm));
+                        lsum += p[e];
+                        if (kFp8) p[e] *= by[e];
+                    }
+                    pk[c >> 1] = pack_bf16x2(p[0], p[1]);
+                    pk[(c >> 1) + 1] = pack_bf16x2(p[2], p[3]);
+                }
+                tmem_st32(tl + kPCol + (n & 1) * 64 + wg * 32, pk);
+                tmem_wait_st();
+                l += lsum;
+                tc_fence_before();
+                mbar_arrive(&p_full[n & 1]);
+                if (t == t0) {
+                    // the next part's queries: that buffer's last reader, the part before
+                    // this one, is done, since this part's S has been seen
+                    have = w.next(a);
+                    if (have) load_q(w, part + 1);
+                }
+            }
+            // the pair leaves together: an `ok` lost after the last exchange is exchanged here
+            if (ok && !warp_wait<1>(&pv_done[(n - 1) & 1], static_cast<uint32_t>((n - 1) >> 1) & 1u, abort)) {
+                attn_timeout(a.status, abort);
+                ok = false;
+            }
+            xch[wg * kRows + r] = l;
+            if (lane == 0) xok[wg * 4 + qd] = ok ? 1 : 0;
+            named_bar_sync(pair_bar, 64);
+            l += xch[(1 - wg) * kRows + r];
+            ok = ok && xok[(1 - wg) * 4 + qd] != 0;
+            named_bar_sync(pair_bar, 64);
+            if (!ok) break;
+            tc_fence_after();
+            float o[64];
+            tmem_ld64(tl + kOCol + cb, o);
+            tc_fence_before();
+            mbar_arrive(o_free);
+            if (row_ok) {
+                if (full_unit) {
+                    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+                    uint4* d = reinterpret_cast<uint4*>(a.out + ((static_cast<long long>(s) * (a.B + 1) + b) * a.Hq + head * a.G + row % a.G) * kHeadDim + cb);
+#pragma unroll
+                    for (int e = 0; e < 8; e++)
+                        d[e] = make_uint4(pack_bf16x2(o[8 * e] * inv, o[8 * e + 1] * inv), pack_bf16x2(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
+                                          pack_bf16x2(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_bf16x2(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+                } else {
+                    TilePart* d = static_cast<TilePart*>(a.parts) + 2 * blockIdx.x + (t0 > 0 ? 0 : 1);
+                    float4* dst = reinterpret_cast<float4*>(&d->o[r][cb]);
+#pragma unroll
+                    for (int e = 0; e < 16; e++) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                    if (wg == 0) d->ml[r] = make_float2(m_run, l);
+                }
+            }
+        }
+    } else {
+        // ---------------------------------------------------------- raw tiles to operands (e4m3): a thread per key
+        const int key = threadIdx.x - 320;
+        bool ok = true;
+        int n = 0, raw = 0;  // tiles, whole cache tiles so far
+        while (ok && w.next(a)) {
+            for (int t = w.t0; t < w.t1 && ok; t++, n++) {
+                const bool cache_tile = t < w.whole;
+                const int st = n % kStages;
+                float* sc = scales + (n % G_::kRing) * 2 * kKeys;
+                for (int kv = 0; kv < 2 && ok; kv++) {
+                    const int stages = kv ? G_::kRawV : G_::kRawK, rs = cache_tile ? raw % stages : 0;
+                    uint4 x[8];
+                    if (cache_tile) {
+                        if (!warp_wait(&(kv ? rv_full : rk_full)[rs], static_cast<uint32_t>(raw / stages) & 1u, abort)) {
+                            ok = false;
+                            break;
+                        }
+                        const uint8_t* src = (kv ? rV : rK) + rs * kHalf;
+#pragma unroll
+                        for (int c = 0; c < 8; c++) x[c] = *reinterpret_cast<const uint4*>(src + tile_swz(key, c));
+                    }
+                    if (kv == 0) {
+                        sc[key] = cache_tile ? raw_scales[rs * 2 * kKeys + key] * a.sl2 : a.sl2;
+                        sc[kKeys + key] = cache_tile ? raw_scales[rs * 2 * kKeys + kKeys + key] : 1.0f;
+                        mbar_arrive(&sc_full[n % G_::kRing]);
+                    }
+                    if (cache_tile) mbar_arrive(&(kv ? rv_empty : rk_empty)[rs]);
+                    if (!warp_wait(&(kv ? v_empty : k_empty)[st], (static_cast<uint32_t>(n / kStages) & 1u) ^ 1u, abort)) {
+                        ok = false;
+                        break;
+                    }
+                    uint8_t* dst = (kv ? sV : sK) + st * kTile;
+                    if (cache_tile) {
+#pragma unroll
+                        for (int c = 0; c < 8; c++) {
+                            const uint32_t u[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+                            uint32_t y[8];
+#pragma unroll
+                            for (int e = 0; e < 4; e++) {
+                                y[2 * e] = codes_to_bf16(__byte_perm(u[e], 0u, 0x1000));
+                                y[2 * e + 1] = codes_to_bf16(__byte_perm(u[e], 0u, 0x3020));
+                            }
+                            uint8_t* d = dst + (c >> 2) * kHalf;
+                            *reinterpret_cast<uint4*>(d + tile_swz(key, (2 * c) & 7)) = make_uint4(y[0], y[1], y[2], y[3]);
+                            *reinterpret_cast<uint4*>(d + tile_swz(key, (2 * c + 1) & 7)) = make_uint4(y[4], y[5], y[6], y[7]);
+                        }
+                    } else {
+                        const uint4* src = reinterpret_cast<const uint4*>(
+                            (kv ? ta.side_v : ta.side_k) +
+                            ((static_cast<long long>(w.s) * a.Hkv + w.head) * ta.sk + (t - w.whole) * kKeys + key) * kHeadDim);
+#pragma unroll
+                        for (int h = 0; h < 2; h++) {
+                            uint4 y[8];
+#pragma unroll
+                            for (int c = 0; c < 8; c++) y[c] = __ldg(src + 8 * h + c);
+#pragma unroll
+                            for (int c = 0; c < 8; c++) *reinterpret_cast<uint4*>(dst + h * kHalf + tile_swz(key, c)) = y[c];
+                        }
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the MMAs read it
+                    mbar_arrive(&(kv ? v_full : k_full)[st]);
+                }
+                if (cache_tile) raw++;
+            }
+        }
+        if (!ok) attn_timeout(a.status, abort);
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// Joins the parts of the units that several CTAs shared, in the order of
+// their keys.  One block per 16 rows of a unit, 16 threads (8 elements each)
+// a row.
+__global__ void __launch_bounds__(256) paged_tiles_join_kernel(const __grid_constant__ PagedArgs a, int ctas) {
+    pdl_trigger();
+    pdl_wait();
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int most = ((a.B + 1) * a.G + kRows - 1) / kRows, eighth = blockIdx.x % 8, u = blockIdx.x / 8;
+    const int s = u / (a.Hkv * most);
+    TilePlace p{};
+    p.s = s;
+    p.load(a);
+    p.unit = u % (a.Hkv * most);
+    if (p.unit >= p.units) return;
+    const int tiles = p.tiles(a), head = p.unit / p.nqt, row0 = (p.unit % p.nqt) * kRows + eighth * 16;
+    if (row0 >= (p.nodes + 1) * a.G) return;
+    const long long all = tile_cost_before(a, a.nseq, lane);
+    const int shares = tile_shares(all, ctas);
+    const long long first = tile_cost_before(a, s, lane) + static_cast<long long>(p.unit) * p.cost;
+    const int c0 = share_at(all, shares, first), c1 = share_at(all, shares, first + tiles - 1);
+    if (c0 == c1) return;
+    const int r = eighth * 16 + (tid >> 4), d8 = tid & 15, row = row0 + (tid >> 4), b = row / a.G;
+    if (b > p.nodes) return;
+    float top = -INFINITY, l = 0.0f, o[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    for (int c = c0; c <= c1; c++) {
+        const TilePart* x = static_cast<const TilePart*>(a.parts) + 2 * c + (share_begin(all, shares, c) > first ? 0 : 1);
+        const float2 ml = x->ml[r];
+        const float4 y = *reinterpret_cast<const float4*>(&x->o[r][8 * d8]), z = *reinterpret_cast<const float4*>(&x->o[r][8 * d8 + 4]);
+        if (ml.x == -INFINITY) continue;
+        const float up = fmaxf(top, ml.x), old = top == -INFINITY ? 0.0f : ex2(top - up), by = ex2(ml.x - up);
+        top = up;
+        l = l * old + ml.y * by;
+        const float v[8] = {y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
+#pragma unroll
+        for (int k = 0; k < 8; k++) o[k] = o[k] * old + v[k] * by;
+    }
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    __nv_bfloat16* d = a.out + ((static_cast<long long>(s) * (a.B + 1) + b) * a.Hq + head * a.G + row % a.G) * kHeadDim + 8 * d8;
+    *reinterpret_cast<uint4*>(d) = make_uint4(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv),
+                                              pack_bf16x2(o[4] * inv, o[5] * inv), pack_bf16x2(o[6] * inv, o[7] * inv));
+}
+
+// Workspace: partial results, rotated queries, side keys, side values.
+struct TileWs {
+    int sk;
+    size_t q, k, v, total;
+};
+TileWs tile_ws(int nseq, int B, int Hq, int Hkv) {
+    TileWs w;
+    w.sk = (kKeys - 1 + B + 1 + kKeys - 1) / kKeys * kKeys;
+    auto up = [](size_t n) { return (n + 255) & ~static_cast<size_t>(255); };
+    const size_t side = up(static_cast<size_t>(nseq) * Hkv * w.sk * kHeadDim * 2);
+    w.q = up(sizeof(TilePart) * 2 * kMaxSms);
+    w.k = w.q + up(static_cast<size_t>(nseq) * (B + 1) * Hq * kHeadDim * 2);
+    w.v = w.k + side;
+    w.total = w.v + side;
+    return w;
+}
+
+}  // namespace
+
+size_t paged_tiles_workspace(const dart_paged_attn_config& c, const dart_kv_cache& cache) {
+    return tile_ws(c.nseq, c.B, c.Hq, cache.Hkv).total;
+}
+
+bool paged_tiles_prepare_device() {
+    return cudaFuncSetAttribute(paged_tiles_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, TGeo<false>::kSmem) == cudaSuccess &&
+           cudaFuncSetAttribute(paged_tiles_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, TGeo<true>::kSmem) == cudaSuccess;
+}
+
+int launch_paged_tiles(PagedArgs a, const dart_kv_cache& cache, uint8_t* workspace, int sms, cudaStream_t st) {
+    const bool fp8 = cache.dtype == DART_KV_E4M3;
+    const TileWs w = tile_ws(a.nseq, a.B, a.Hq, a.Hkv);
+    TileArgs ta{};
+    ta.p = a;
+    ta.sk = w.sk;
+    ta.qr = reinterpret_cast<__nv_bfloat16*>(workspace + w.q);
+    ta.side_k = reinterpret_cast<__nv_bfloat16*>(workspace + w.k);
+    ta.side_v = reinterpret_cast<__nv_bfloat16*>(workspace + w.v);
+    const long long side_rows = static_cast<long long>(a.nseq) * a.Hkv * w.sk;
+    CUtensorMap tmK, tmV, tmSk, tmSv;
+    if (!encode_rows(&tmK, cache.k, a.pool_rows, fp8, cache.page_size) || !encode_rows(&tmV, cache.v, a.pool_rows, fp8, cache.page_size) ||
+        !encode_rows(&tmSk, ta.side_k, side_rows, false, kKeys) || !encode_rows(&tmSv, ta.side_v, side_rows, false, kKeys))
+        return DART_ERR_CUDA;
+    const dim3 prep(static_cast<unsigned>((side_rows + 7) / 8));
+    if (launch_pdl(paged_prep_kernel, prep, dim3(256), 0, st, ta, static_cast<const uint8_t*>(cache.k), static_cast<const uint8_t*>(cache.v)) != cudaSuccess)
+        return DART_ERR_CUDA;
+    const cudaError_t e = fp8 ? launch_pdl(paged_tiles_kernel<true>, dim3(sms), dim3(TGeo<true>::kThreads), TGeo<true>::kSmem, st, tmK, tmV, tmSk, tmSv, ta)
+                              : launch_pdl(paged_tiles_kernel<false>, dim3(sms), dim3(TGeo<false>::kThreads), TGeo<false>::kSmem, st, tmK, tmV, tmSk, tmSv, ta);
+    if (e != cudaSuccess) return DART_ERR_CUDA;
+    const int units = a.nseq * a.Hkv * (((a.B + 1) * a.G + kRows - 1) / kRows);
+    return launch_pdl(paged_tiles_join_kernel, dim3(units * 8), dim3(256), 0, st, a, sms) == cudaSuccess ? DART_OK : DART_ERR_CUDA;
+}
+
+}  // namespace dart

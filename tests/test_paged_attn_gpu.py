@@ -245,6 +245,22 @@ def test_captured_and_replayed_for_other_lengths(dart):
     check(x, att.out)
 
 
+def test_calls_on_an_idle_gpu_give_up_no_wait(dart):
+    """Single calls with nothing before them and cold caches: no bounded wait
+    runs out (the issuing thread of the tiles may be late by more than a tile)."""
+    x = sd.attn_data(1, 16, [20000], 128, False, 8, 2, 7112)
+    cold = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    first = None
+    for i in range(6):
+        cold.fill_(i)
+        torch.cuda.synchronize()
+        out = run(dart, x, status=status)
+        assert int(status) == 0
+        first = out if first is None else first
+        assert torch.equal(out, first)
+
+
 def test_nothing_else_is_written(dart):
     x = sd.attn_data(2, 30, [100, 3], 16, True, 8, 2, 7110)
     cache = sd.guarded_cache(dart, x.pool)
