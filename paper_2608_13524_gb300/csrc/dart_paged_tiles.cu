@@ -20,9 +20,11 @@
 // Roles in a CTA: warp 0 loads tiles by TMA, page by page (K ring, V ring);
 // warp 1 issues the MMAs; warps 2-9 are two softmax warpgroups (thread = query
 // row = TMEM lane; warpgroup wg owns key and output columns [64 wg, 64 wg +
-// 64), the two warps of a lane quarter exchange maxima and sums); e4m3 pages
-// have four more warps that turn raw tiles into bf16 operands (exact), while
-// the scales are applied to scores and probabilities.  TMEM (512 columns): S
+// 64), the two warps of a lane quarter exchange maxima and sums).  With e4m3
+// pages all operands are f16: four more warps turn raw tiles into f16 codes
+// (exact, one conversion instruction per pair; bf16 took six), while the
+// scales are applied to scores and probabilities; queries and side rows are
+// f16 with a power of two per row, which no magnitude can overflow.  TMEM (512 columns): S
 // [0,128), O [128,256), P [256,384) in two buffers, Q [384,512) in two.
 // A row's running maximum is raised (and O rescaled) only when a tile exceeds
 // it by more than 2^8.  Every wait is bounded.
@@ -62,14 +64,55 @@ struct TilePart {
 struct TileArgs {
     PagedArgs p;
     int sk;                    // side keys per sequence and kv head (a multiple of 128)
-    __nv_bfloat16* qr;         // [nseq][Hkv][(B + 1) * G][128]
-    __nv_bfloat16 *side_k, *side_v;  // [nseq][Hkv][sk][128]
+    // bf16, or f16 (e4m3 pages) with a factor per row:
+    uint16_t* qr;               // [nseq][Hkv][(B + 1) * G][128]
+    uint16_t *side_k, *side_v;  // [nseq][Hkv][sk][128]
+    float* q_scale;             // [nseq][Hkv][(B + 1) * G], with scale * log2(e) in it
+    float *side_ks, *side_vs;   // [nseq][Hkv][sk]
 };
+
+// Two e4m3 codes as an f16 pair: exact.
+__device__ __forceinline__ uint32_t codes_to_f16(uint32_t two) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(static_cast<uint16_t>(two)));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
 
 // ------------------------------------------------------------ preparation
 
+// A row of 128 values, four to a lane (2 lane, 2 lane + 1 and the same 64
+// further), as bf16; or as f16 scaled by a power of two to a largest element
+// in [1, 2), and the factor that undoes it.
+template <bool kF16>
+__device__ __forceinline__ float put_row(uint16_t* row, int lane, const float (&x)[4]) {
+    uint32_t w[2];
+    float factor = 1.0f;
+    if (kF16) {
+        float mx = fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3])));
+        mx = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(mx)));
+        const int ex = min(max(static_cast<int>(__float_as_uint(mx) >> 23) - 127, -100), 120);
+        const float down = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+        factor = __uint_as_float(static_cast<uint32_t>(127 + ex) << 23);
+        const __half2 h0 = __floats2half2_rn(x[0] * down, x[1] * down), h1 = __floats2half2_rn(x[2] * down, x[3] * down);
+        w[0] = *reinterpret_cast<const uint32_t*>(&h0);
+        w[1] = *reinterpret_cast<const uint32_t*>(&h1);
+    } else {
+        w[0] = pack_bf16x2(x[0], x[1]);
+        w[1] = pack_bf16x2(x[2], x[3]);
+    }
+    uint32_t* d = reinterpret_cast<uint32_t*>(row) + lane;
+    d[0] = w[0];
+    d[32] = w[1];
+    return factor;
+}
+
 // One warp per (sequence, side row, kv head): the side row's key and value,
 // and, if it is a tree row, the rotated queries of its G heads.
+template <bool kFp8>
 __global__ void __launch_bounds__(256) paged_prep_kernel(const __grid_constant__ TileArgs ta, const uint8_t* pool_k, const uint8_t* pool_v) {
     const PagedArgs& a = ta.p;
     pdl_trigger();
@@ -80,76 +123,87 @@ __global__ void __launch_bounds__(256) paged_prep_kernel(const __grid_constant__
     const int s = static_cast<int>(id / a.Hkv / ta.sk);
     if (s >= a.nseq) return;
     const int len = seq_len(a, s), nodes = seq_nodes(a, s), tail = len % kKeys, b = j - tail;
-    uint32_t* ok = reinterpret_cast<uint32_t*>(ta.side_k + ((static_cast<long long>(s) * a.Hkv + head) * ta.sk + j) * kHeadDim) + lane;
-    uint32_t* ov = reinterpret_cast<uint32_t*>(ta.side_v + ((static_cast<long long>(s) * a.Hkv + head) * ta.sk + j) * kHeadDim) + lane;
-    uint32_t k[2] = {0u, 0u}, v[2] = {0u, 0u};  // elements 2 lane, 2 lane + 1 and the same 64 further
+    const long long side = (static_cast<long long>(s) * a.Hkv + head) * ta.sk + j;
+    uint16_t *sk = ta.side_k + side * kHeadDim, *sv = ta.side_v + side * kHeadDim;
+    float ks = 1.0f, vs = 1.0f;
     if (b < 0) {
+        // a token of the cache: its codes or values as they are
         const int key = len - tail + j;
         const int page = __ldg(a.table + static_cast<long long>(s) * a.max_pages + (key >> a.page_log2));
+        uint32_t k[2] = {0u, 0u}, v[2] = {0u, 0u};
         if (page < 0 || page >= a.num_pages) {
             if (a.status && lane == 0) atomicOr(a.status, kDevBounds);
         } else {
             const long long row = ((static_cast<long long>(page) * a.Hkv + head) << a.page_log2) + (key & ((1 << a.page_log2) - 1));
-            if (a.ks) {
-                const float ks = __ldg(a.ks + row), vs = __ldg(a.vs + row);
+            if (kFp8) {
+                ks = __ldg(a.ks + row);
+                vs = __ldg(a.vs + row);
+            }
 #pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    const long long at = row * kHeadDim + 64 * h + 2 * lane;
-                    uint32_t x = *reinterpret_cast<const uint16_t*>(pool_k + at), y = *reinterpret_cast<const uint16_t*>(pool_v + at), f, g;
-                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f) : "h"(static_cast<uint16_t>(x)));
-                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(g) : "h"(static_cast<uint16_t>(y)));
-                    const float2 kf = __half22float2(*reinterpret_cast<const __half2*>(&f)), vf = __half22float2(*reinterpret_cast<const __half2*>(&g));
-                    k[h] = pack_bf16x2(kf.x * ks, kf.y * ks);
-                    v[h] = pack_bf16x2(vf.x * vs, vf.y * vs);
-                }
-            } else {
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    k[h] = *reinterpret_cast<const uint32_t*>(pool_k + (row * kHeadDim + 64 * h + 2 * lane) * 2);
-                    v[h] = *reinterpret_cast<const uint32_t*>(pool_v + (row * kHeadDim + 64 * h + 2 * lane) * 2);
+            for (int h = 0; h < 2; h++) {
+                const long long at = row * kHeadDim + 64 * h + 2 * lane;
+                if (kFp8) {
+                    const uint16_t x = *reinterpret_cast<const uint16_t*>(pool_k + at), y = *reinterpret_cast<const uint16_t*>(pool_v + at);
+                    k[h] = codes_to_f16(x);
+                    v[h] = codes_to_f16(y);
+                } else {
+                    k[h] = *reinterpret_cast<const uint32_t*>(pool_k + at * 2);
+                    v[h] = *reinterpret_cast<const uint32_t*>(pool_v + at * 2);
                 }
             }
         }
-    } else if (b <= a.B) {
-        const long long in = static_cast<long long>(s) * (a.B + 1) + b;
-        uint32_t* qr = reinterpret_cast<uint32_t*>(
-                           ta.qr + ((static_cast<long long>(s) * a.Hkv + head) * (a.B + 1) * a.G + static_cast<long long>(b) * a.G) * kHeadDim) + lane;
-        if (b <= nodes) {
-            const uint32_t* kp = reinterpret_cast<const uint32_t*>(a.k + in * a.k_stride + head * kHeadDim) + lane;
-            const uint32_t* vp = reinterpret_cast<const uint32_t*>(a.v + in * a.v_stride + head * kHeadDim) + lane;
-            const uint32_t x = __ldg(kp), y = __ldg(kp + 32);
-            v[0] = __ldg(vp);
-            v[1] = __ldg(vp + 32);
-            const int pos = len + (b > 0 ? __ldg(a.depths + static_cast<long long>(s) * a.B + b - 1) : 0);
-            float s0, c0, s1, c1;
-            rope_sincos(a.turns.f[2 * lane], pos, &s0, &c0);
-            rope_sincos(a.turns.f[2 * lane + 1], pos, &s1, &c1);
-            auto turn = [&](uint32_t lo, uint32_t hi, uint32_t (&o)[2]) {
-                const float x0 = bf16_lo(lo), x1 = bf16_hi(lo), y0 = bf16_lo(hi), y1 = bf16_hi(hi);
-                o[0] = pack_bf16x2(x0 * c0 - y0 * s0, x1 * c1 - y1 * s1);
-                o[1] = pack_bf16x2(y0 * c0 + x0 * s0, y1 * c1 + x1 * s1);
+        reinterpret_cast<uint32_t*>(sk)[lane] = k[0];
+        reinterpret_cast<uint32_t*>(sk)[lane + 32] = k[1];
+        reinterpret_cast<uint32_t*>(sv)[lane] = v[0];
+        reinterpret_cast<uint32_t*>(sv)[lane + 32] = v[1];
+    } else {
+        float k[4] = {0.0f, 0.0f, 0.0f, 0.0f}, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (b <= a.B) {
+            const long long in = static_cast<long long>(s) * (a.B + 1) + b;
+            const long long q_row = (static_cast<long long>(s) * a.Hkv + head) * (a.B + 1) * a.G + static_cast<long long>(b) * a.G;
+            const bool node = b <= nodes;
+            float s0 = 0.0f, c0 = 0.0f, s1 = 0.0f, c1 = 0.0f;
+            auto get = [&](const __nv_bfloat16* src, float (&x)[4]) {
+                const uint32_t* p = reinterpret_cast<const uint32_t*>(src) + lane;
+                const uint32_t lo = __ldg(p), hi = __ldg(p + 32);
+                x[0] = bf16_lo(lo);
+                x[1] = bf16_hi(lo);
+                x[2] = bf16_lo(hi);
+                x[3] = bf16_hi(hi);
             };
-            turn(x, y, k);
-            const uint32_t* qp = reinterpret_cast<const uint32_t*>(a.q + in * a.q_stride + head * a.G * kHeadDim) + lane;
+            auto turn = [&](float (&x)[4]) {
+                const float y[4] = {x[0] * c0 - x[2] * s0, x[1] * c1 - x[3] * s1, x[2] * c0 + x[0] * s0, x[3] * c1 + x[1] * s1};
+#pragma unroll
+                for (int e = 0; e < 4; e++) x[e] = y[e];
+            };
+            if (node) {
+                get(a.k + in * a.k_stride + head * kHeadDim, k);
+                get(a.v + in * a.v_stride + head * kHeadDim, v);
+                const int pos = len + (b > 0 ? __ldg(a.depths + static_cast<long long>(s) * a.B + b - 1) : 0);
+                rope_sincos(a.turns.f[2 * lane], pos, &s0, &c0);
+                rope_sincos(a.turns.f[2 * lane + 1], pos, &s1, &c1);
+                turn(k);
+            }
 #pragma unroll 4
             for (int g = 0; g < a.G; g++) {
-                uint32_t o[2];
-                turn(__ldg(qp + g * 64), __ldg(qp + g * 64 + 32), o);
-                qr[g * 64] = o[0];
-                qr[g * 64 + 32] = o[1];
-            }
-        } else {
-            uint2* out = reinterpret_cast<uint2*>(a.out + (in * a.Hq + head * a.G) * kHeadDim) + lane;
-            for (int g = 0; g < a.G; g++) {
-                qr[g * 64] = qr[g * 64 + 32] = 0u;
-                out[g * 32] = make_uint2(0u, 0u);
+                float q[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (node) {
+                    get(a.q + in * a.q_stride + (head * a.G + g) * kHeadDim, q);
+                    turn(q);
+                } else {
+                    reinterpret_cast<uint2*>(a.out + (in * a.Hq + head * a.G + g) * kHeadDim)[lane] = make_uint2(0u, 0u);
+                }
+                const float factor = put_row<kFp8>(ta.qr + (q_row + g) * kHeadDim, lane, q);
+                if (kFp8 && lane == 0) ta.q_scale[q_row + g] = factor * a.sl2;
             }
         }
+        ks = put_row<kFp8>(sk, lane, k);
+        vs = put_row<kFp8>(sv, lane, v);
     }
-    ok[0] = k[0];
-    ok[32] = k[1];
-    ov[0] = v[0];
-    ov[32] = v[1];
+    if (kFp8 && lane == 0) {
+        ta.side_ks[side] = ks;
+        ta.side_vs[side] = vs;
+    }
 }
 
 // ------------------------------------------------------------ the schedule
@@ -256,6 +310,46 @@ struct Walk {
 
 // ------------------------------------------------------------ the tiles
 
+// Registers move between warpgroups, out of the 4 x 128 a thread that the
+// e4m3 kernel is launched with (128 are too few for the softmax's 64 scores a
+// thread).
+constexpr int kRegsIssue = 88, kRegsSoft = 168, kRegsConvert = 88;
+static_assert(kRegsIssue + 2 * kRegsSoft + kRegsConvert <= 4 * 128, "more than the launch has");
+template <int kRegs>
+__device__ __forceinline__ void reg_less() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs));
+}
+template <int kRegs>
+__device__ __forceinline__ void reg_more() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs));
+}
+
+// D[tmem] (+)= A[tmem] * B[smem] at fixed offsets from the operands' bases: the
+// descriptor is put together here, since a register pair for each of 32 of
+// them is more than the issuing thread has.  `lo`: address >> 4, and the
+// leading offset of an MN-major operand.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);  // stride, version, 128-byte swizzle
+template <int kAOff, int kBOff>
+__device__ __forceinline__ void mma_at(uint32_t tmem_d, uint32_t tmem_a, uint32_t lo, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n .reg .pred p;\n .reg .b32 x, y;\n .reg .b64 d;\n setp.ne.b32 p, %4, 0;\n add.u32 x, %1, %5;\n add.u32 y, %2, %6;\n"
+        " mov.b64 d, {y, %7};\n tcgen05.mma.cta_group::1.kind::f16 [%0], [x], d, %3, p;\n}\n" ::"r"(tmem_d),
+        "r"(tmem_a), "r"(lo), "r"(idesc), "r"(accumulate), "n"(kAOff), "n"(kBOff), "r"(kDescHigh)
+        : "memory");
+}
+// S = Q K^T (K-major K: 32 bytes a step, 64 elements a swizzle column) and
+// O += P V (MN-major V: 16 keys of 128 bytes a step).
+template <int kk = 0>
+__device__ __forceinline__ void mma_s(uint32_t d, uint32_t q, uint32_t k_lo, uint32_t idesc) {
+    mma_at<kk * 8, ((kk >> 2) * kHalf + (kk & 3) * 32) / 16>(d, q, k_lo, idesc, kk > 0 ? 1u : 0u);
+    if constexpr (kk + 1 < kHeadDim / 16) mma_s<kk + 1>(d, q, k_lo, idesc);
+}
+template <int kk = 0>
+__device__ __forceinline__ void mma_pv(uint32_t d, uint32_t p, uint32_t v_lo, uint32_t idesc, uint32_t first) {
+    mma_at<kk * 8, kk * 2048 / 16>(d, p, v_lo, idesc, kk > 0 ? 1u : 1u - first);
+    if constexpr (kk + 1 < kKeys / 16) mma_pv<kk + 1>(d, p, v_lo, idesc, first);
+}
+
 template <bool kFp8>
 struct TGeo {
     // bf16: three operand tiles of K and of V.  e4m3: two of each, and raw
@@ -268,22 +362,14 @@ struct TGeo {
     static constexpr int kRawScales = kRawK * 2 * kKeys * 4;
     static constexpr int kScales = kFp8 ? kRing * 2 * kKeys * 4 : 0;
     static constexpr int kBars = 4 * kStages + 2 * (kRawK + kRawV) + (kFp8 ? kRing : 0) + 9 + 1;
-    static constexpr int kExchange = 2 * kRows * 4 + 8 * 4;
+    static constexpr int kExchange = 2 * kRows * 4 + 8 * 4 + kRing * 4 * 4;
     static constexpr int kSmem = kOps + kRaw + kRawScales + kScales + kBars * 8 + kExchange + 16;
-    static constexpr int kThreads = 64 + kSoft + (kFp8 ? 128 : 0);
+    // e4m3: warpgroups (producer, MMA, two idle warps), softmax, softmax, converters
+    static constexpr int kThreads = kFp8 ? 512 : 64 + kSoft;
+    static constexpr int kFirstSoft = kFp8 ? 4 : 2;
 };
 
 __device__ __forceinline__ uint32_t tile_swz(int row, int piece) { return static_cast<uint32_t>(row * 128 + ((piece ^ (row & 7)) << 4)); }
-
-// Two e4m3 codes in bytes 1 and 3 of x (bytes 0 and 2: anything) as a bf16
-// pair: sign, then exponent and mantissa four bits down, and a product with
-// 2^120 for the difference of the exponents' biases (exact, subnormals too).
-__device__ __forceinline__ uint32_t codes_to_bf16(uint32_t x) {
-    const uint32_t y = ((x >> 4) & 0x07F007F0u) | (x & 0x80008000u);
-    const __nv_bfloat162 by = __halves2bfloat162(__ushort_as_bfloat16(0x7B80), __ushort_as_bfloat16(0x7B80));  // 2^120
-    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&y), by);
-    return *reinterpret_cast<const uint32_t*>(&r);
-}
 
 // Bits [o, o + 64) of a row of mask words (o >= -128; bits outside are 0).
 __device__ __forceinline__ uint64_t mask_bits(const uint64_t* m, int mw, int o) {
@@ -309,7 +395,7 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
     uint8_t* rK = sV + kStages * kTile;  // raw tiles
     uint8_t* rV = rK + G_::kRawK * kHalf;
     float* raw_scales = reinterpret_cast<float*>(rV + G_::kRawV * kHalf);  // [raw K stage][K, V][key]
-    float* scales = raw_scales + G_::kRawK * 2 * kKeys;                    // [tile % 4][K * sl2, V][key]
+    float* scales = raw_scales + G_::kRawK * 2 * kKeys;                    // [tile % 4][K, V][key]
     uint64_t* k_full = reinterpret_cast<uint64_t*>(scales + G_::kScales / 4);
     uint64_t* k_empty = k_full + kStages;   // S of the tile done
     uint64_t* v_full = k_empty + kStages;
@@ -328,7 +414,8 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
     uint64_t* tdown = o_free + 1;
     float* xch = reinterpret_cast<float*>(k_full + G_::kBars);  // [2][128] row max / sum exchange
     int* xok = reinterpret_cast<int*>(xch + 2 * kRows);         // [2][4] "no wait failed"
-    int* misc = xok + 8;                                        // TMEM base, abort
+    float* vtop = reinterpret_cast<float*>(xok + 8);            // [tile % 4][converting warp] largest value scale
+    int* misc = reinterpret_cast<int*>(vtop + G_::kRing * 4);   // TMEM base, abort
     volatile int* abort = &misc[1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_trigger();
@@ -382,142 +469,141 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
         w.p = find_tile(a, begin, lane);
     }
 
-    if (warp == 0) {
-        // ---------------------------------------------------------- loads: the whole warp, a lane per page
-        const int per_tile = kKeys >> a.page_log2;  // pages of a tile
-        const uint64_t policy = (a.B + 1) * a.G <= kRows ? l2_policy_evict_first() : l2_policy_evict_last();
-        auto page_at = [&](int t) {
-            return t < w.whole && lane < per_tile
-                       ? __ldg(a.table + static_cast<long long>(w.s) * a.max_pages + static_cast<long long>(t) * per_tile + lane)
-                       : 0;
-        };
-        int n = 0;       // bf16: tiles so far; e4m3: whole cache tiles so far
-        bool have = w.next(a), ok = true;
-        int t = w.t0, page = have ? page_at(t) : 0;
-        while (have && ok) {
-            // this tile, then the next one's page numbers, which are there when it is its turn
-            const int head = w.head, s = w.s, tt = t, my_page = page;
-            const bool cache_tile = tt < w.whole;
-            const int side_row = (tt - w.whole) * kKeys;
-            if (++t == w.t1) {
-                have = w.next(a);
-                t = w.t0;
-            }
-            if (have) page = page_at(t);
-            if (kFp8 && !cache_tile) continue;  // (the converting warps read side tiles themselves)
-            long long row = a.pool_rows;  // past the pool: zeros
-            if (cache_tile && lane < per_tile) {
-                if (my_page >= 0 && my_page < a.num_pages)
-                    row = (static_cast<long long>(my_page) * a.Hkv + head) << a.page_log2;
-                else if (a.status)
-                    atomicOr(a.status, kDevBounds);
-            }
-            for (int kv = 0; kv < 2 && ok; kv++) {
-                const int stages = kFp8 ? (kv ? G_::kRawV : G_::kRawK) : kStages;
-                const int st = n % stages;
-                uint64_t* full = (kFp8 ? (kv ? rv_full : rk_full) : (kv ? v_full : k_full)) + st;
-                uint64_t* empty = (kFp8 ? (kv ? rv_empty : rk_empty) : (kv ? v_empty : k_empty)) + st;
-                uint8_t* dst = kFp8 ? (kv ? rV : rK) + st * kHalf : (kv ? sV : sK) + st * kTile;
-                const CUtensorMap* tm = cache_tile ? (kv ? &tmV : &tmK) : (kv ? &tmSv : &tmSk);
-                ok = warp_wait<kWaitPolls>(empty, (static_cast<uint32_t>(n / stages) & 1u) ^ 1u, abort);
-                if (!ok) break;
-                if (lane == 0)
-                    mbar_arrive_expect_tx(full, kFp8 ? kHalf + (kv ? 0 : 2 * kKeys * 4) : kTile);
-                __syncwarp();
-                if (!cache_tile) {
-                    if (lane < 2)
-                        tma_load_2d(dst + lane * kHalf, tm, full, 64 * lane, (s * a.Hkv + head) * ta.sk + side_row, policy);
-                } else if (lane < per_tile) {
-                    const uint32_t at = static_cast<uint32_t>(lane << a.page_log2) * 128;
-                    tma_load_2d(dst + at, tm, full, 0, static_cast<int>(row), policy);
-                    if (!kFp8) tma_load_2d(dst + kHalf + at, tm, full, 64, static_cast<int>(row), policy);
-                    if (kFp8 && kv == 0) {
-                        const long long sr = row < a.pool_rows ? row : 0;
-                        float* sc = raw_scales + st * 2 * kKeys + (lane << a.page_log2);
-                        bulk_load(sc, a.ks + sr, 4u << a.page_log2, full);
-                        bulk_load(sc + kKeys, a.vs + sr, 4u << a.page_log2, full);
+    if (warp < G_::kFirstSoft) {
+        if (kFp8) reg_less<kRegsIssue>();
+        if (warp == 0) {
+            // ---------------------------------------------------------- loads: the whole warp, a lane per page
+            const int per_tile = kKeys >> a.page_log2;  // pages of a tile
+            const uint64_t policy = (a.B + 1) * a.G <= kRows ? l2_policy_evict_first() : l2_policy_evict_last();
+            auto page_at = [&](int t) {
+                return t < w.whole && lane < per_tile
+                           ? __ldg(a.table + static_cast<long long>(w.s) * a.max_pages + static_cast<long long>(t) * per_tile + lane)
+                           : 0;
+            };
+            int n = 0;       // bf16: tiles so far; e4m3: whole cache tiles so far
+            bool have = w.next(a), ok = true;
+            int t = w.t0, page = have ? page_at(t) : 0;
+            while (have && ok) {
+                // this tile, then the next one's page numbers, which are there when it is its turn
+                const int head = w.head, s = w.s, tt = t, my_page = page;
+                const bool cache_tile = tt < w.whole;
+                const int side_row = (tt - w.whole) * kKeys;
+                if (++t == w.t1) {
+                    have = w.next(a);
+                    t = w.t0;
+                }
+                if (have) page = page_at(t);
+                if (kFp8 && !cache_tile) continue;  // (the converting warps read side tiles themselves)
+                long long row = a.pool_rows;  // past the pool: zeros
+                if (cache_tile && lane < per_tile) {
+                    if (my_page >= 0 && my_page < a.num_pages)
+                        row = (static_cast<long long>(my_page) * a.Hkv + head) << a.page_log2;
+                    else if (a.status)
+                        atomicOr(a.status, kDevBounds);
+                }
+                for (int kv = 0; kv < 2 && ok; kv++) {
+                    const int stages = kFp8 ? (kv ? G_::kRawV : G_::kRawK) : kStages;
+                    const int st = n % stages;
+                    uint64_t* full = (kFp8 ? (kv ? rv_full : rk_full) : (kv ? v_full : k_full)) + st;
+                    uint64_t* empty = (kFp8 ? (kv ? rv_empty : rk_empty) : (kv ? v_empty : k_empty)) + st;
+                    uint8_t* dst = kFp8 ? (kv ? rV : rK) + st * kHalf : (kv ? sV : sK) + st * kTile;
+                    const CUtensorMap* tm = cache_tile ? (kv ? &tmV : &tmK) : (kv ? &tmSv : &tmSk);
+                    ok = warp_wait<kWaitPolls>(empty, (static_cast<uint32_t>(n / stages) & 1u) ^ 1u, abort);
+                    if (!ok) break;
+                    if (lane == 0)
+                        mbar_arrive_expect_tx(full, kFp8 ? kHalf + (kv ? 0 : 2 * kKeys * 4) : kTile);
+                    __syncwarp();
+                    if (!cache_tile) {
+                        if (lane < 2)
+                            tma_load_2d(dst + lane * kHalf, tm, full, 64 * lane, (s * a.Hkv + head) * ta.sk + side_row, policy);
+                    } else if (lane < per_tile) {
+                        const uint32_t at = static_cast<uint32_t>(lane << a.page_log2) * 128;
+                        tma_load_2d(dst + at, tm, full, 0, static_cast<int>(row), policy);
+                        if (!kFp8) tma_load_2d(dst + kHalf + at, tm, full, 64, static_cast<int>(row), policy);
+                        if (kFp8 && kv == 0) {
+                            const long long sr = row < a.pool_rows ? row : 0;
+                            float* sc = raw_scales + st * 2 * kKeys + (lane << a.page_log2);
+                            bulk_load(sc, a.ks + sr, 4u << a.page_log2, full);
+                            bulk_load(sc + kKeys, a.vs + sr, 4u << a.page_log2, full);
+                        }
                     }
                 }
+                if (ok) n++;
             }
-            if (ok) n++;
-        }
-        if (!ok && lane == 0) attn_timeout(a.status, abort);
-        if (*abort) {
-            // copies still in flight must land before the CTA exits
-            for (int kv = 0; kv < 2; kv++) {
-                const int stages = kFp8 ? (kv ? G_::kRawV : G_::kRawK) : kStages;
-                uint64_t* full = kFp8 ? (kv ? rv_full : rk_full) : (kv ? v_full : k_full);
-                // (the tile at which a wait failed may have its K under way)
-                for (int i = max(n - stages, 0); i < n + (kv == 0 && !ok ? 1 : 0); i++)
-                    if (lane == 0) attn_drain(&full[i % stages], static_cast<uint32_t>(i / stages) & 1u);
-            }
-        }
-    } else if (warp == 1) {
-        // ---------------------------------------------------------- MMAs
-        if (lane == 0) {
-            constexpr uint32_t idesc_s = idesc_bf16_f32(kRows, kKeys);
-            constexpr uint32_t idesc_pv = idesc_bf16_f32(kRows, kHeadDim) | (1u << 16);  // B (= V) MN-major
-            auto issue_s = [&](int n, int part) -> bool {
-                const int st = n % kStages;
-                if (!mbar_wait_inline(&k_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort) ||
-                    (n > 0 && !mbar_wait_inline(s_empty, static_cast<uint32_t>(n - 1) & 1u, abort)))
-                    return false;
-                tc_fence_after();
-                const uint32_t k_addr = smem_u32(sK + st * kTile);
-#pragma unroll
-                for (int kk = 0; kk < kHeadDim / 16; kk++)
-                    tc_mma_bf16_ts(tmem + kSCol, tmem + kQCol + (part & 1) * 64 + kk * 8,
-                                   sdesc_sw128(k_addr + (kk >> 2) * kHalf + (kk & 3) * 32), idesc_s, kk > 0 ? 1u : 0u);
-                tc_commit(s_full);
-                tc_commit(&k_empty[st]);
-                return true;
-            };
-            bool have = w.next(a), ok = true;
-            int n = 0, part = 0, t = w.t0, t1 = w.t1, t0 = w.t0;
-            if (have) {
-                ok = mbar_wait_inline(&q_ready[0], 0, abort);
-                tc_fence_after();
-                ok = ok && issue_s(0, 0);
-            }
-            while (have && ok) {
-                // tile t of part `part`; S of the tile after it first
-                const bool first = t == t0;
-                const int my_part = part;
-                if (++t == t1) {
-                    have = w.next(a);
-                    t = t0 = w.t0;
-                    t1 = w.t1;
-                    part++;
-                    if (have) ok = mbar_wait_inline(&q_ready[part & 1], static_cast<uint32_t>(part >> 1) & 1u, abort);
+            if (!ok && lane == 0) attn_timeout(a.status, abort);
+            if (*abort) {
+                // copies still in flight must land before the CTA exits
+                for (int kv = 0; kv < 2; kv++) {
+                    const int stages = kFp8 ? (kv ? G_::kRawV : G_::kRawK) : kStages;
+                    uint64_t* full = kFp8 ? (kv ? rv_full : rk_full) : (kv ? v_full : k_full);
+                    // (the tile at which a wait failed may have its K under way)
+                    for (int i = max(n - stages, 0); i < n + (kv == 0 && !ok ? 1 : 0); i++)
+                        if (lane == 0) attn_drain(&full[i % stages], static_cast<uint32_t>(i / stages) & 1u);
                 }
-                if (have && ok) {
+            }
+        } else if (warp == 1) {
+            // ---------------------------------------------------------- MMAs
+            if (lane == 0) {
+                // (operand types: bf16 1, f16 0 in bits 7 and 10)
+                constexpr uint32_t idesc_s = idesc_bf16_f32(kRows, kKeys) & (kFp8 ? ~((1u << 7) | (1u << 10)) : ~0u);
+                constexpr uint32_t idesc_pv = (idesc_bf16_f32(kRows, kHeadDim) & (kFp8 ? ~((1u << 7) | (1u << 10)) : ~0u)) | (1u << 16);  // B (= V) MN-major
+                const uint32_t k_lo = smem_u32(sK) >> 4, v_lo = smem_u32(sV) >> 4;
+                auto issue_s = [&](int n, int part) -> bool {
+                    const int st = n % kStages;
+                    if (!mbar_wait_inline(&k_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort) ||
+                        (n > 0 && !mbar_wait_inline(s_empty, static_cast<uint32_t>(n - 1) & 1u, abort)))
+                        return false;
                     tc_fence_after();
-                    ok = issue_s(n + 1, part);
+                    mma_s(tmem + kSCol, tmem + kQCol + (part & 1) * 64, (k_lo + st * (kTile >> 4)) & 0x3FFFu, idesc_s);
+                    tc_commit(s_full);
+                    tc_commit(&k_empty[st]);
+                    return true;
+                };
+                bool have = w.next(a), ok = true;
+                int n = 0, part = 0, t = w.t0, t1 = w.t1, t0 = w.t0;
+                if (have) {
+                    ok = mbar_wait_inline(&q_ready[0], 0, abort);
+                    tc_fence_after();
+                    ok = ok && issue_s(0, 0);
                 }
-                const int st = n % kStages;
-                ok = ok && mbar_wait_inline(&p_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, abort) &&
-                     mbar_wait_inline(&v_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort) &&
-                     (!first || my_part == 0 || mbar_wait_inline(o_free, static_cast<uint32_t>(my_part - 1) & 1u, abort));
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t v_addr = smem_u32(sV + st * kTile);
-#pragma unroll
-                for (int kk = 0; kk < kKeys / 16; kk++)  // 16 keys = 8 columns of bf16 pairs
-                    tc_mma_bf16_ts(tmem + kOCol, tmem + kPCol + (n & 1) * 64 + kk * 8, sdesc_sw128_mn(v_addr + kk * 2048, kHalf),
-                                   idesc_pv, (!first || kk > 0) ? 1u : 0u);
-                tc_commit(&v_empty[st]);
-                tc_commit(&pv_done[n & 1]);
-                n++;
-            }
-            if (!ok) {
-                attn_timeout(a.status, abort);
-                tc_commit(tdown);
-                attn_drain(tdown, 0);
+                while (have && ok) {
+                    // tile t of part `part`; S of the tile after it first
+                    const bool first = t == t0;
+                    const int my_part = part;
+                    if (++t == t1) {
+                        have = w.next(a);
+                        t = t0 = w.t0;
+                        t1 = w.t1;
+                        part++;
+                        if (have) ok = mbar_wait_inline(&q_ready[part & 1], static_cast<uint32_t>(part >> 1) & 1u, abort);
+                    }
+                    if (have && ok) {
+                        tc_fence_after();
+                        ok = issue_s(n + 1, part);
+                    }
+                    const int st = n % kStages;
+                    ok = ok && mbar_wait_inline(&p_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, abort) &&
+                         mbar_wait_inline(&v_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort) &&
+                         (!first || my_part == 0 || mbar_wait_inline(o_free, static_cast<uint32_t>(my_part - 1) & 1u, abort));
+                    if (!ok) break;
+                    tc_fence_after();
+                    mma_pv(tmem + kOCol, tmem + kPCol + (n & 1) * 64, ((v_lo + st * (kTile >> 4)) & 0x3FFFu) | ((kHalf >> 4) << 16), idesc_pv,
+                           first ? 1u : 0u);
+                    tc_commit(&v_empty[st]);
+                    tc_commit(&pv_done[n & 1]);
+                    n++;
+                }
+                if (!ok) {
+                    attn_timeout(a.status, abort);
+                    tc_commit(tdown);
+                    attn_drain(tdown, 0);
+                }
             }
         }
-    } else if (warp < 10) {
+    } else if (warp < G_::kFirstSoft + 8) {
         // ---------------------------------------------------------- softmax
-        const int qd = warp & 3, wg = (warp - 2) >> 2, cb = wg * 64;
+        if (kFp8) reg_more<kRegsSoft>();
+        const int qd = warp & 3, wg = (warp - G_::kFirstSoft) >> 2, cb = wg * 64;
         const int r = qd * 32 + lane;  // query row of the unit = TMEM lane
         const int pair_bar = kPairBar + qd;
         const uint32_t tl = tmem + (static_cast<uint32_t>(qd * 32) << 16);
@@ -548,7 +634,12 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
             const bool full_unit = t0 == 0 && t1 == w.tiles;
             const int row = w.qt * kRows + r, b = row / a.G;
             const bool row_ok = b <= nodes;
-            float m_run = -INFINITY, l = 0.0f;
+            // m_run: the row's reference; e4m3: vref, a power of two above every value
+            // scale so far, joins it as vshift, so that P = 2^(s - m) / vref * 2^7 times a
+            // scale stays below 2^15 in f16, and 2^-31 of the largest weight still counts
+            float m_run = -INFINITY, l = 0.0f, vref = 0.0f, vshift = 0.0f;
+            float rs = a.sl2;  // scores in log2 units = products (with the keys' scales) * rs
+            if (kFp8 && row_ok) rs = __ldg(ta.q_scale + (static_cast<long long>(s) * a.Hkv + head) * (a.B + 1) * a.G + row);
             for (int t = t0; t < t1; t++, n++) {
                 // visible keys of this row among this warpgroup's 64 of the tile
                 uint64_t vis = row_ok ? ~0ull : 0ull;
@@ -604,10 +695,22 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                 ok = ok && xok[(1 - wg) * 4 + qd] != 0;
                 named_bar_sync(pair_bar, 64);  // both read before the next tile's write
                 if (!ok) break;
-                const float mx2 = kFp8 ? mx : mx * a.sl2;
-                const bool resc = mx2 > m_run + kSlack8;
+                const float mx2 = mx * rs;
+                bool resc = mx2 > m_run + kSlack8;
                 const float m_new = resc ? mx2 : m_run;
-                const float alpha = resc ? ex2(m_run - m_new) : 1.0f;
+                float shift = vshift;
+                if (kFp8) {
+                    const float4 y = *reinterpret_cast<const float4*>(vtop + (n % G_::kRing) * 4);
+                    const float top = fmaxf(fmaxf(y.x, y.y), fmaxf(y.z, y.w));
+                    if (top > vref) {  // (the same in every thread)
+                        const uint32_t ex = min(max(__float_as_uint(top) >> 23, 27u), 252u) + 1u;
+                        vref = __uint_as_float(ex << 23);
+                        shift = static_cast<float>(static_cast<int>(ex) - 127) - 7.0f;
+                        resc = true;
+                    }
+                }
+                const float alpha = resc ? (m_run == -INFINITY ? 0.0f : ex2((m_run + vshift) - (m_new + shift))) : 1.0f;
+                vshift = shift;
                 // P buffer n & 1 was last read by PV(n - 2); O must be stable (PV(n - 1)
                 // done) only when it is rescaled.  On a timeout this tile is
                 // skipped; the pair leaves the loop together at the next exchange.
@@ -638,7 +741,7 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                 m_run = m_new;
                 // P = 2^(s - m) as bf16 pairs; hidden keys hold -inf and give 0 (so does
                 // every key of a row that has seen no visible key: m = -inf)
-                const float nm = m_run == -INFINITY ? 0.0f : -m_run;
+                const float nm = m_run == -INFINITY ? 0.0f : -(m_run + vshift);
                 float lsum = 0.0f;
                 uint32_t pk[32];
 #pragma unroll
@@ -649,12 +752,12 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                     float p[4];
 #pragma unroll
                     for (int e = 0; e < 4; e++) {
-                        p[e] = kFp8 ? ex2(sv[c + e] + nm) : ex2(fmaf(sv[c + e], a.sl2, nm));
+                        p[e] = ex2(fmaf(sv[c + e], rs, nm));
                         lsum += p[e];
                         if (kFp8) p[e] *= by[e];
                     }
-                    pk[c >> 1] = pack_bf16x2(p[0], p[1]);
-                    pk[(c >> 1) + 1] = pack_bf16x2(p[2], p[3]);
+                    pk[c >> 1] = kFp8 ? pack_f16x2(p[0], p[1]) : pack_bf16x2(p[0], p[1]);
+                    pk[(c >> 1) + 1] = kFp8 ? pack_f16x2(p[2], p[3]) : pack_bf16x2(p[2], p[3]);
                 }
                 tmem_st32(tl + kPCol + (n & 1) * 64 + wg * 32, pk);
                 tmem_wait_st();
@@ -698,13 +801,14 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                     float4* dst = reinterpret_cast<float4*>(&d->o[r][cb]);
 #pragma unroll
                     for (int e = 0; e < 16; e++) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-                    if (wg == 0) d->ml[r] = make_float2(m_run, l);
+                    if (wg == 0) d->ml[r] = make_float2(m_run + vshift, l);
                 }
             }
         }
     } else {
         // ---------------------------------------------------------- raw tiles to operands (e4m3): a thread per key
-        const int key = threadIdx.x - 320;
+        reg_less<kRegsConvert>();
+        const int key = threadIdx.x - (G_::kFirstSoft + 8) * 32;
         bool ok = true;
         int n = 0, raw = 0;  // tiles, whole cache tiles so far
         while (ok && w.next(a)) {
@@ -724,9 +828,14 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
 #pragma unroll
                         for (int c = 0; c < 8; c++) x[c] = *reinterpret_cast<const uint4*>(src + tile_swz(key, c));
                     }
+                    const long long side = (static_cast<long long>(w.s) * a.Hkv + w.head) * ta.sk + (t - w.whole) * kKeys + key;
                     if (kv == 0) {
-                        sc[key] = cache_tile ? raw_scales[rs * 2 * kKeys + key] * a.sl2 : a.sl2;
-                        sc[kKeys + key] = cache_tile ? raw_scales[rs * 2 * kKeys + kKeys + key] : 1.0f;
+                        const float vsc = cache_tile ? raw_scales[rs * 2 * kKeys + kKeys + key] : __ldg(ta.side_vs + side);
+                        sc[key] = cache_tile ? raw_scales[rs * 2 * kKeys + key] : __ldg(ta.side_ks + side);
+                        sc[kKeys + key] = vsc;
+                        const float top = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(fmaxf(vsc, 0.0f))));
+                        if (lane == 0) vtop[(n % G_::kRing) * 4 + (warp & 3)] = top;
+                        __syncwarp();
                         mbar_arrive(&sc_full[n % G_::kRing]);
                     }
                     if (cache_tile) mbar_arrive(&(kv ? rv_empty : rk_empty)[rs]);
@@ -742,17 +851,15 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                             uint32_t y[8];
 #pragma unroll
                             for (int e = 0; e < 4; e++) {
-                                y[2 * e] = codes_to_bf16(__byte_perm(u[e], 0u, 0x1000));
-                                y[2 * e + 1] = codes_to_bf16(__byte_perm(u[e], 0u, 0x3020));
+                                y[2 * e] = codes_to_f16(u[e]);
+                                y[2 * e + 1] = codes_to_f16(u[e] >> 16);
                             }
                             uint8_t* d = dst + (c >> 2) * kHalf;
                             *reinterpret_cast<uint4*>(d + tile_swz(key, (2 * c) & 7)) = make_uint4(y[0], y[1], y[2], y[3]);
                             *reinterpret_cast<uint4*>(d + tile_swz(key, (2 * c + 1) & 7)) = make_uint4(y[4], y[5], y[6], y[7]);
                         }
                     } else {
-                        const uint4* src = reinterpret_cast<const uint4*>(
-                            (kv ? ta.side_v : ta.side_k) +
-                            ((static_cast<long long>(w.s) * a.Hkv + w.head) * ta.sk + (t - w.whole) * kKeys + key) * kHeadDim);
+                        const uint4* src = reinterpret_cast<const uint4*>((kv ? ta.side_v : ta.side_k) + side * kHeadDim);
 #pragma unroll
                         for (int h = 0; h < 2; h++) {
                             uint4 y[8];
@@ -824,7 +931,7 @@ __global__ void __launch_bounds__(256) paged_tiles_join_kernel(const __grid_cons
 // Workspace: partial results, rotated queries, side keys, side values.
 struct TileWs {
     int sk;
-    size_t q, k, v, total;
+    size_t q, k, v, qs, ks, vs, total;
 };
 TileWs tile_ws(int nseq, int B, int Hq, int Hkv) {
     TileWs w;
@@ -834,7 +941,10 @@ TileWs tile_ws(int nseq, int B, int Hq, int Hkv) {
     w.q = up(sizeof(TilePart) * 2 * kMaxSms);
     w.k = w.q + up(static_cast<size_t>(nseq) * (B + 1) * Hq * kHeadDim * 2);
     w.v = w.k + side;
-    w.total = w.v + side;
+    w.qs = w.v + side;
+    w.ks = w.qs + up(static_cast<size_t>(nseq) * (B + 1) * Hq * 4);
+    w.vs = w.ks + up(static_cast<size_t>(nseq) * Hkv * w.sk * 4);
+    w.total = w.vs + up(static_cast<size_t>(nseq) * Hkv * w.sk * 4);
     return w;
 }
 
@@ -855,19 +965,24 @@ int launch_paged_tiles(PagedArgs a, const dart_kv_cache& cache, uint8_t* workspa
     TileArgs ta{};
     ta.p = a;
     ta.sk = w.sk;
-    ta.qr = reinterpret_cast<__nv_bfloat16*>(workspace + w.q);
-    ta.side_k = reinterpret_cast<__nv_bfloat16*>(workspace + w.k);
-    ta.side_v = reinterpret_cast<__nv_bfloat16*>(workspace + w.v);
+    ta.qr = reinterpret_cast<uint16_t*>(workspace + w.q);
+    ta.side_k = reinterpret_cast<uint16_t*>(workspace + w.k);
+    ta.side_v = reinterpret_cast<uint16_t*>(workspace + w.v);
+    ta.q_scale = reinterpret_cast<float*>(workspace + w.qs);
+    ta.side_ks = reinterpret_cast<float*>(workspace + w.ks);
+    ta.side_vs = reinterpret_cast<float*>(workspace + w.vs);
     const long long side_rows = static_cast<long long>(a.nseq) * a.Hkv * w.sk;
     CUtensorMap tmK, tmV, tmSk, tmSv;
     if (!encode_rows(&tmK, cache.k, a.pool_rows, fp8, cache.page_size) || !encode_rows(&tmV, cache.v, a.pool_rows, fp8, cache.page_size) ||
         !encode_rows(&tmSk, ta.side_k, side_rows, false, kKeys) || !encode_rows(&tmSv, ta.side_v, side_rows, false, kKeys))
         return DART_ERR_CUDA;
     const dim3 prep(static_cast<unsigned>((side_rows + 7) / 8));
-    if (launch_pdl(paged_prep_kernel, prep, dim3(256), 0, st, ta, static_cast<const uint8_t*>(cache.k), static_cast<const uint8_t*>(cache.v)) != cudaSuccess)
-        return DART_ERR_CUDA;
-    const cudaError_t e = fp8 ? launch_pdl(paged_tiles_kernel<true>, dim3(sms), dim3(TGeo<true>::kThreads), TGeo<true>::kSmem, st, tmK, tmV, tmSk, tmSv, ta)
-                              : launch_pdl(paged_tiles_kernel<false>, dim3(sms), dim3(TGeo<false>::kThreads), TGeo<false>::kSmem, st, tmK, tmV, tmSk, tmSv, ta);
+    const uint8_t *pk = static_cast<const uint8_t*>(cache.k), *pv = static_cast<const uint8_t*>(cache.v);
+    cudaError_t e = fp8 ? launch_pdl(paged_prep_kernel<true>, prep, dim3(256), 0, st, ta, pk, pv)
+                        : launch_pdl(paged_prep_kernel<false>, prep, dim3(256), 0, st, ta, pk, pv);
+    if (e != cudaSuccess) return DART_ERR_CUDA;
+    e = fp8 ? launch_pdl(paged_tiles_kernel<true>, dim3(sms), dim3(TGeo<true>::kThreads), TGeo<true>::kSmem, st, tmK, tmV, tmSk, tmSv, ta)
+            : launch_pdl(paged_tiles_kernel<false>, dim3(sms), dim3(TGeo<false>::kThreads), TGeo<false>::kSmem, st, tmK, tmV, tmSk, tmSv, ta);
     if (e != cudaSuccess) return DART_ERR_CUDA;
     const int units = a.nseq * a.Hkv * (((a.B + 1) * a.G + kRows - 1) / kRows);
     return launch_pdl(paged_tiles_join_kernel, dim3(units * 8), dim3(256), 0, st, a, sms) == cudaSuccess ? DART_OK : DART_ERR_CUDA;
