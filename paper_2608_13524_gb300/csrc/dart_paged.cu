@@ -81,7 +81,7 @@ struct Place {
         ctx_chunks = (len + kKeys - 1) / kKeys;
         chunks = ctx_chunks + (nodes + 1 + 15) / 16;  // (tree rows: 16 at a time)
         cost = chunks + Chunk<kFp8>::kUnitCost;
-        units = a.Hkv * (((nodes + 1) * a.G + kUnitRows - 1) / kUnitRows);
+        units = a.Hkv * ((((nodes + 1) << a.g_log2) + kUnitRows - 1) / kUnitRows);
     }
     __device__ __forceinline__ int groups(const PagedArgs& a) const { return units / a.Hkv; }
     __device__ __forceinline__ void next_unit(const PagedArgs& a) {
@@ -93,61 +93,57 @@ struct Place {
     }
 };
 
-// List length of all sequences before sequence `upto`, by one warp.
+// By one warp: the list's length and, then, the place x of it (of its first 32
+// sequences the lengths are kept).
 template <bool kFp8>
-__device__ __forceinline__ long long cost_before(const PagedArgs& a, int upto, int lane) {
-    long long n = 0;
-    for (int s = lane; s < upto; s += 32) {
+struct List {
+    long long all, own;  // own: length of sequence `lane`
+    __device__ __forceinline__ static long long length(const PagedArgs& a, int s) {
+        if (s >= a.nseq) return 0;
         Place<kFp8> p{};
         p.s = s;
         p.load(a);
-        n += static_cast<long long>(p.units) * p.cost;
+        return static_cast<long long>(p.units) * p.cost;
     }
+    __device__ __forceinline__ List(const PagedArgs& a, int lane) {
+        own = length(a, lane);
+        long long n = own;
+        for (int s = lane + 32; s < a.nseq; s += 32) n += length(a, s);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(kFull, n, o);
-    return n;
-}
-
-// The place x of the list (0 <= x < all), by one warp.
-template <bool kFp8>
-__device__ __forceinline__ Place<kFp8> find_place(const PagedArgs& a, long long x, int lane) {
-    long long done = 0;
-    Place<kFp8> r{};
-    for (int s0 = 0; s0 < a.nseq; s0 += 32) {
-        Place<kFp8> p{};
-        p.s = s0 + lane;
-        long long n = 0;
-        if (p.s < a.nseq) {
-            p.load(a);
-            n = static_cast<long long>(p.units) * p.cost;
-        }
-        long long upto = n;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long y = __shfl_up_sync(kFull, upto, o);
-            if (lane >= o) upto += y;
-        }
-        const unsigned hit = __ballot_sync(kFull, p.s < a.nseq && x < done + upto);
-        if (hit) {
-            const int l = __ffs(hit) - 1;
-            const long long rest = x - done - __shfl_sync(kFull, upto - n, l);
-            r.s = s0 + l;
-            r.load(a);
-            r.unit = static_cast<int>(rest / r.cost);
-            r.chunk = static_cast<int>(rest - static_cast<long long>(r.unit) * r.cost);
-            return r;
-        }
-        done += __shfl_sync(kFull, upto, 31);
+        for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(kFull, n, o);
+        all = n;
     }
-    r.s = a.nseq;
-    return r;
-}
+    __device__ __forceinline__ Place<kFp8> find(const PagedArgs& a, long long x, int lane) const {
+        long long done = 0;
+        Place<kFp8> r{};
+        for (int s0 = 0; s0 < a.nseq; s0 += 32) {
+            const long long n = s0 == 0 ? own : length(a, s0 + lane);
+            long long upto = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long y = __shfl_up_sync(kFull, upto, o);
+                if (lane >= o) upto += y;
+            }
+            const unsigned hit = __ballot_sync(kFull, x < done + upto);
+            if (hit) {
+                const int l = __ffs(hit) - 1;
+                const long long rest = x - done - __shfl_sync(kFull, upto - n, l);
+                r.s = s0 + l;
+                r.load(a);
+                r.unit = place_div(rest, r.cost);
+                r.chunk = static_cast<int>(rest - static_cast<long long>(r.unit) * r.cost);
+                return r;
+            }
+            done += __shfl_sync(kFull, upto, 31);
+        }
+        r.s = a.nseq;
+        return r;
+    }
+};
 
 // Shares: one per warp, each at least kMinShare long.
 constexpr int kMinShare = 2;
-__device__ __forceinline__ int share_count(long long all, int warps) {
-    return static_cast<int>(min(static_cast<long long>(warps), (all + kMinShare - 1) / kMinShare));
-}
+
 // ------------------------------------------------------------ fragments
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -231,12 +227,16 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int j = tid; j < a.Hq * kHeadDim / 8; j += kThreads) o[j] = make_uint4(0, 0, 0, 0);
         }
 
-    const long long all = cost_before<kFp8>(a, a.nseq, lane);
-    const int share = warp * gridDim.x + blockIdx.x, shares = share_count(all, kWarps * gridDim.x);
-    if (share >= shares) return;
-    const long long begin = share_begin(all, shares, share);
-    long long left = share_begin(all, shares, share + 1) - begin;  // places of this share not yet worked on
-    Place<kFp8> use = find_place<kFp8>(a, begin, lane), load = use;
+    const List<kFp8> list(a, lane);
+    const int share = warp * gridDim.x + blockIdx.x;
+    const Shares shares(list.all, kWarps * gridDim.x, kMinShare);
+    if (share >= shares.count) return;
+    long long left = shares.length(share);  // places of this share not yet worked on
+    Place<kFp8> use = list.find(a, shares.begin(share), lane), load = use;
+    if (lane == 0) {
+        a.plan->places[share] = make_int4(use.s, use.unit, use.chunk, 0);
+        if (share == 0) a.plan->count = shares.count;
+    }
     long long to_load = left;  // places not yet loaded
     int n_load = 0, n_use = 0;
     int failed = 0;
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         float rs[2];  // scores in log2 units = products * rs
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            const int r = row0 + g + 8 * h, b = r / a.G;
+            const int r = row0 + g + 8 * h, b = r >> a.g_log2;
             float x[4][8];
 #pragma unroll
             for (int i = 0; i < 4; i++)
@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int e = 0; e < 8; e++) x[i][e] = 0.0f;
             if (b <= nodes) {
                 const int pos = len + (b > 0 ? __ldg(a.depths + static_cast<long long>(s) * a.B + b - 1) : 0);
-                const __nv_bfloat16* src = a.q + (seq_row + b) * a.q_stride + (head * a.G + r % a.G) * kHeadDim;
+                const __nv_bfloat16* src = a.q + (seq_row + b) * a.q_stride + (head * a.G + (r & (a.G - 1))) * kHeadDim;
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
                     const int d0 = 8 * k_piece<kFp8>(i, t);
@@ -656,7 +656,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int e = 0; e < 2; e++)
 #pragma unroll
                     for (int h = 0; h < 2; h++) {
-                        const int j = key0 + slot_row(qq, 2 * t + e), b = (row0 + g + 8 * h) / a.G;
+                        const int j = key0 + slot_row(qq, 2 * t + e), b = (row0 + g + 8 * h) >> a.g_log2;
                         bool see = j <= nodes && b <= nodes;
                         if (see && j > 0)
                             see = b > 0 && ((__ldg(a.mask + (static_cast<long long>(s) * a.B + b - 1) * a.mw + ((j - 1) >> 6)) >> ((j - 1) & 63)) & 1ull);
@@ -687,7 +687,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int h = 0; h < 2; h++) {
             l[h] += __shfl_xor_sync(kFull, l[h], 1);
             l[h] += __shfl_xor_sync(kFull, l[h], 2);
-            const int r = row0 + g + 8 * h, b = r / a.G;
+            const int r = row0 + g + 8 * h, b = r >> a.g_log2;
             if (b > nodes) continue;
             float by = kFp8 ? vref * 0.0078125f : 1.0f;
             if (whole) by = l[h] > 0.0f ? by / l[h] : 0.0f;
@@ -701,7 +701,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int k = 0; k < 8; k++) o[k] = acc[8 * half + k][2 * h + e] * by;
                     if (whole) {
-                        __nv_bfloat16* dst = a.out + ((seq_row + b) * a.Hq + head * a.G + r % a.G) * kHeadDim + d;
+                        __nv_bfloat16* dst = a.out + ((seq_row + b) * a.Hq + head * a.G + (r & (a.G - 1))) * kHeadDim + d;
                         *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]),
                                                                     pack_bf16x2(o[4], o[5]), pack_bf16x2(o[6], o[7]));
                     } else {
@@ -722,34 +722,55 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // Joins the parts of the units that several warps shared, in the order of
-// their keys.  One block per unit: 16 threads (8 elements each) per row, and
-// where a unit has fewer than 16 rows as many more groups of threads, each
-// with every n-th part, joined in order through shared memory.
+// their keys.  Block i works if share i begins inside a unit that share i - 1
+// began: 16 threads (8 elements each) per row, and where a unit has fewer than
+// 16 rows as many more groups of threads, each with every n-th part, joined in
+// order through shared memory.
 template <bool kFp8>
-__global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_constant__ PagedArgs a, int warps) {
+__global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_constant__ PagedArgs a) {
     __shared__ float2 ml_of[kUnitRows];
     __shared__ float sum_of[kUnitRows][kHeadDim];
+    __shared__ int ends[kThreads / 32];
     pdl_trigger();
+    const int tid = threadIdx.x, lane = tid & 31, i = blockIdx.x + 1;
     pdl_wait();
-    const int tid = threadIdx.x, lane = tid & 31;
-    const int per = a.Hkv * (((a.B + 1) * a.G + kUnitRows - 1) / kUnitRows), s = blockIdx.x / per;
+    const int count = a.plan->count;
+    if (i >= count) return;
+    const int4 at = a.plan->places[i], prev = a.plan->places[i - 1];
+    if (at.z == 0 || (prev.x == at.x && prev.y == at.y && prev.z > 0)) return;
     Place<kFp8> p{};
-    p.s = s;
-    p.unit = blockIdx.x % per;
+    p.s = at.x;
     p.load(a);
-    if (p.unit >= p.units) return;
-    const long long all = cost_before<kFp8>(a, a.nseq, lane);
-    const int shares = share_count(all, warps);
-    const long long first = cost_before<kFp8>(a, s, lane) + static_cast<long long>(p.unit) * p.cost;
-    const int c0 = share_at(all, shares, first), c1 = share_at(all, shares, first + p.chunks - 1);
-    if (c0 == c1) return;
-    const int groups = p.groups(a), head = p.unit / groups, row0 = (p.unit % groups) * kUnitRows;
-    const int rows = min(kUnitRows, (p.nodes + 1) * a.G - row0);
+    if (at.z >= p.chunks) return;  // (the unit ended in share i - 1; what is left of it in the list is its other costs)
+    // the last share that holds chunks of the unit
+    int end = i;
+    for (int c0 = i + 1;; c0 += kThreads) {
+        bool in = false;
+        if (c0 + tid < count) {
+            const int4 x = a.plan->places[c0 + tid];
+            in = x.x == at.x && x.y == at.y && x.z < p.chunks;
+        }
+        const unsigned out = __ballot_sync(kFull, !in);
+        if (lane == 0) ends[tid >> 5] = out ? __ffs(out) - 1 : 32;
+        __syncthreads();
+        int n = 0;
+        for (int w = 0; w < kThreads / 32; w++) {
+            n += ends[w];
+            if (ends[w] < 32) break;
+        }
+        end += n;
+        __syncthreads();
+        if (n < kThreads) break;
+    }
+    const int s = p.s, groups = p.groups(a), head = at.y / groups, row0 = (at.y % groups) * kUnitRows;
+    const int rows = min(kUnitRows, ((p.nodes + 1) << a.g_log2) - row0);
     int span = 1;  // rows rounded up to a power of two; 16 / span thread groups
     while (span < rows) span *= 2;
     const int slot_of_row = tid >> 4, d8 = tid & 15, r = slot_of_row % span, part0 = slot_of_row / span, step = kUnitRows / span;
     const bool live = r < rows;
-    auto slot = [&](int c) { return static_cast<const Part*>(a.parts) + 2 * static_cast<long long>(c) + (share_begin(all, shares, c) > first ? 0 : 1); };
+    // share i - 1 began the unit (its second slot), the others went on with it
+    auto slot = [&](int c) { return static_cast<const Part*>(a.parts) + 2 * static_cast<long long>(c) + (c < i ? 1 : 0); };
+    const int c0 = i - 1, c1 = end;
     float top = -INFINITY, l = 0.0f, o[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     if (live)
         for (int c = c0 + part0; c <= c1; c += step) {
@@ -765,9 +786,9 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
             for (int k = 0; k < 8; k++) o[k] = o[k] * old + w[k] * by;
         }
     // the groups' results, one after the other
-    for (int i = 1; i < step; i++) {
+    for (int q = 1; q < step; q++) {
         __syncthreads();
-        if (part0 == i) {
+        if (part0 == q) {
 #pragma unroll
             for (int k = 0; k < 8; k++) sum_of[r][8 * d8 + k] = o[k];
             if (d8 == 0) ml_of[r] = make_float2(top, l);
@@ -784,7 +805,7 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
     }
     if (part0 != 0 || !live) return;
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-    __nv_bfloat16* d = a.out + ((static_cast<long long>(s) * (a.B + 1) + (row0 + r) / a.G) * a.Hq + head * a.G + (row0 + r) % a.G) * kHeadDim + 8 * d8;
+    __nv_bfloat16* d = a.out + ((static_cast<long long>(s) * (a.B + 1) + ((row0 + r) >> a.g_log2)) * a.Hq + head * a.G + ((row0 + r) & (a.G - 1))) * kHeadDim + 8 * d8;
     *reinterpret_cast<uint4*>(d) = make_uint4(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv),
                                               pack_bf16x2(o[4] * inv, o[5] * inv), pack_bf16x2(o[6] * inv, o[7] * inv));
 }
@@ -837,7 +858,7 @@ extern "C" {
 
 size_t dart_paged_attention_workspace(const dart_paged_attn_config* cfg, const dart_kv_cache* cache) {
     if (!valid_cfg(cfg, cache)) return 0;
-    if (few_rows(*cfg, *cache)) return sizeof(Part) * 2 * kWarps * kMaxSms;
+    if (few_rows(*cfg, *cache)) return sizeof(SharePlan) + sizeof(Part) * 2 * kWarps * kMaxSms;
     return paged_tiles_workspace(*cfg, *cache);
 }
 
@@ -869,6 +890,7 @@ int dart_paged_attention(const dart_paged_attn_config* cfg, const dart_kv_cache*
     a.Hq = c.Hq;
     a.Hkv = cache->Hkv;
     a.G = c.Hq / cache->Hkv;
+    while ((1 << a.g_log2) < a.G) a.g_log2++;
     a.max_pages = c.max_pages;
     while ((1 << a.page_log2) < cache->page_size) a.page_log2++;
     a.num_pages = cache->num_pages;
@@ -888,7 +910,8 @@ int dart_paged_attention(const dart_paged_attn_config* cfg, const dart_kv_cache*
     a.ks = cache->k_scale;
     a.vs = cache->v_scale;
     a.out = static_cast<__nv_bfloat16*>(out);
-    a.parts = workspace;
+    a.plan = static_cast<SharePlan*>(workspace);
+    a.parts = static_cast<uint8_t*>(workspace) + sizeof(SharePlan);
     a.status = status;
     a.sl2 = static_cast<float>(static_cast<double>(c.scale) * 1.4426950408889634);
     a.turns = rope_turns(c.rope_theta);
@@ -901,9 +924,8 @@ int dart_paged_attention(const dart_paged_attn_config* cfg, const dart_kv_cache*
     cudaError_t e = fp8 ? launch_pdl(paged_rows_kernel<true>, dim3(ctas), dim3(kThreads), Geo<true>::kSmem, st, tmK, tmV, a)
                         : launch_pdl(paged_rows_kernel<false>, dim3(ctas), dim3(kThreads), Geo<false>::kSmem, st, tmK, tmV, a);
     if (e != cudaSuccess) return DART_ERR_CUDA;
-    const dim3 units(c.nseq * a.Hkv * (((c.B + 1) * a.G + kUnitRows - 1) / kUnitRows));
-    e = fp8 ? launch_pdl(paged_join_kernel<true>, units, dim3(kThreads), 0, st, a, kWarps * ctas)
-            : launch_pdl(paged_join_kernel<false>, units, dim3(kThreads), 0, st, a, kWarps * ctas);
+    const dim3 seams(kWarps * ctas - 1);
+    e = fp8 ? launch_pdl(paged_join_kernel<true>, seams, dim3(kThreads), 0, st, a) : launch_pdl(paged_join_kernel<false>, seams, dim3(kThreads), 0, st, a);
     if (e != cudaSuccess) return DART_ERR_CUDA;
     return DART_OK;
 }

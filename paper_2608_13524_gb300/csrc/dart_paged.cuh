@@ -13,8 +13,15 @@ namespace dart {
 
 constexpr int kMaxSms = 160;  // shares are counted by SMs; the workspace has room for this many
 
+// Where the shares of a call begin, for the kernel that joins split units:
+// places[i] = sequence, unit, place in the unit, 0 of share i.
+struct SharePlan {
+    int count, pad[3];
+    int4 places[8 * kMaxSms];
+};
+
 struct PagedArgs {
-    int nseq, B, Hq, Hkv, G, max_pages, page_log2, num_pages, mw;
+    int nseq, B, Hq, Hkv, G, g_log2, max_pages, page_log2, num_pages, mw;
     long long pool_rows;
     const int32_t *table, *lens, *depths, *n_nodes;
     const uint64_t* mask;
@@ -23,6 +30,7 @@ struct PagedArgs {
     const float *ks, *vs;
     __nv_bfloat16* out;
     void* parts;  // partial results, two per share: of the unit begun before it, of the unit that goes on after it
+    SharePlan* plan;
     int* status;
     float sl2;  // scale * log2(e)
     RopeTurns turns;
@@ -30,16 +38,35 @@ struct PagedArgs {
 
 __device__ __forceinline__ int seq_len(const PagedArgs& a, int s) {
     const long long most = static_cast<long long>(a.max_pages) << a.page_log2;
-    return static_cast<int>(min(max(static_cast<long long>(__ldg(a.lens + s)), 0ll), most));
+    return static_cast<int>(min(max(static_cast<long long>(__ldcg(a.lens + s)), 0ll), most));
 }
 __device__ __forceinline__ int seq_nodes(const PagedArgs& a, int s) {
-    return a.B > 0 ? min(max(__ldg(a.n_nodes + s), 0), a.B) : 0;
+    return a.B > 0 ? min(max(__ldcg(a.n_nodes + s), 0), a.B) : 0;
 }
 
-// Shares of a list of length `all`: where share i begins, which one place x is in.
-__device__ __forceinline__ long long share_begin(long long all, int shares, int i) { return all * i / shares; }
-__device__ __forceinline__ int share_at(long long all, int shares, long long x) {
-    return static_cast<int>(((x + 1) * shares - 1) / all);
+// A list of length `all` in `count` shares of all / count places, the first
+// all % count of them one longer.
+struct Shares {
+    long long each;
+    int more, count;
+    __device__ __forceinline__ Shares(long long all, int most, int least) {
+        count = static_cast<int>(min(static_cast<long long>(most), (all + least - 1) / least));
+        if (all < (1ll << 32)) {  // (a 64-bit division takes long)
+            const uint32_t q = static_cast<uint32_t>(all) / static_cast<uint32_t>(count);
+            each = q;
+            more = static_cast<int>(static_cast<uint32_t>(all) - q * static_cast<uint32_t>(count));
+        } else {
+            each = all / count;
+            more = static_cast<int>(all - each * count);
+        }
+    }
+    __device__ __forceinline__ long long begin(int i) const { return each * i + min(i, more); }
+    __device__ __forceinline__ int length(int i) const { return static_cast<int>(each) + (i < more); }
+};
+
+// x / d of a place in a sequence's part of the list.
+__device__ __forceinline__ int place_div(long long x, int d) {
+    return x < (1ll << 32) ? static_cast<int>(static_cast<uint32_t>(x) / static_cast<uint32_t>(d)) : static_cast<int>(x / d);
 }
 
 __device__ __forceinline__ float exp2_fast(float x) {

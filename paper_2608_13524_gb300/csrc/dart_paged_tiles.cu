@@ -71,6 +71,24 @@ struct TileArgs {
     float *side_ks, *side_vs;   // [nseq][Hkv][sk]
 };
 
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)));
+    return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)));
+    return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)),
+        "l"(*reinterpret_cast<uint64_t*>(&c)));
+    return *reinterpret_cast<float2*>(&r);
+}
+
 // Two e4m3 codes as an f16 pair: exact.
 __device__ __forceinline__ uint32_t codes_to_f16(uint32_t two) {
     uint32_t r;
@@ -115,8 +133,8 @@ __device__ __forceinline__ float put_row(uint16_t* row, int lane, const float (&
 template <bool kFp8>
 __global__ void __launch_bounds__(256) paged_prep_kernel(const __grid_constant__ TileArgs ta, const uint8_t* pool_k, const uint8_t* pool_v) {
     const PagedArgs& a = ta.p;
-    pdl_trigger();
     pdl_wait();
+    pdl_trigger();  // (after the wait: the next kernel reads lengths and pages before its own)
     const int lane = threadIdx.x & 31;
     const long long id = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) >> 5;
     const int head = static_cast<int>(id % a.Hkv), j = static_cast<int>(id / a.Hkv % ta.sk);
@@ -208,81 +226,89 @@ __global__ void __launch_bounds__(256) paged_prep_kernel(const __grid_constant__
 
 // ------------------------------------------------------------ the schedule
 
+// A place in the list: kv heads of a sequence one after the other, the units
+// (query tiles) of a head one after the other.  A unit's length in the list is
+// its tiles (its last row sees tree rows up to itself) and kTileCost.
 struct TilePlace {
-    int s, unit, tile;
-    int len, nodes, whole, tail, cost, nqt, units;  // of the sequence: whole cache tiles, cache tokens beside them, ...
+    int s, head, qt, tile;
+    int len, nodes, whole, tail, nqt;  // of the sequence: whole cache tiles, cache tokens beside them, units per head
     __device__ __forceinline__ void load(const PagedArgs& a) {
         len = seq_len(a, s);
         nodes = seq_nodes(a, s);
         whole = len / kKeys;
         tail = len % kKeys;
-        cost = whole + (tail + nodes) / kKeys + 1 + kTileCost;
-        nqt = ((nodes + 1) * a.G + kRows - 1) / kRows;
-        units = a.Hkv * nqt;
+        nqt = (((nodes + 1) << a.g_log2) + kRows - 1) / kRows;
     }
-    // Tiles of the unit: its last row sees tree rows up to itself.
-    __device__ __forceinline__ int tiles(const PagedArgs& a) const {
-        const int last = min(((unit % nqt + 1) * kRows - 1) / a.G, nodes);
-        return whole + (tail + last) / kKeys + 1;
+    __device__ __forceinline__ int tiles(const PagedArgs& a, int q) const {
+        return whole + (tail + min(((q + 1) * kRows - 1) >> a.g_log2, nodes)) / kKeys + 1;
+    }
+    __device__ __forceinline__ int head_cost(const PagedArgs& a) const {
+        int n = 0;
+        for (int q = 0; q < nqt; q++) n += tiles(a, q) + kTileCost;
+        return n;
     }
     __device__ __forceinline__ void next_unit(const PagedArgs& a) {
         tile = 0;
-        if (++unit == units) {
-            unit = 0;
-            if (++s < a.nseq) load(a);
+        if (++qt == nqt) {
+            qt = 0;
+            if (++head == a.Hkv) {
+                head = 0;
+                if (++s < a.nseq) load(a);
+            }
         }
     }
 };
 
-__device__ __forceinline__ long long tile_cost_before(const PagedArgs& a, int upto, int lane) {
-    long long n = 0;
-    for (int s = lane; s < upto; s += 32) {
+// By one warp: the list's length and, then, the place x of it (of its first 32
+// sequences a head's length is kept).
+struct TileList {
+    long long all;
+    int own;
+    __device__ __forceinline__ static int length(const PagedArgs& a, int s) {
+        if (s >= a.nseq) return 0;
         TilePlace p{};
         p.s = s;
         p.load(a);
-        n += static_cast<long long>(p.units) * p.cost;
+        return p.head_cost(a);
     }
+    __device__ __forceinline__ TileList(const PagedArgs& a, int lane) {
+        own = length(a, lane);
+        long long n = own;
+        for (int s = lane + 32; s < a.nseq; s += 32) n += length(a, s);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(kFull, n, o);
-    return n;
-}
-
-__device__ __forceinline__ TilePlace find_tile(const PagedArgs& a, long long x, int lane) {
-    long long done = 0;
-    TilePlace r{};
-    for (int s0 = 0; s0 < a.nseq; s0 += 32) {
-        TilePlace p{};
-        p.s = s0 + lane;
-        long long n = 0;
-        if (p.s < a.nseq) {
-            p.load(a);
-            n = static_cast<long long>(p.units) * p.cost;
-        }
-        long long upto = n;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long y = __shfl_up_sync(kFull, upto, o);
-            if (lane >= o) upto += y;
-        }
-        const unsigned hit = __ballot_sync(kFull, p.s < a.nseq && x < done + upto);
-        if (hit) {
-            const int l = __ffs(hit) - 1;
-            const long long rest = x - done - __shfl_sync(kFull, upto - n, l);
-            r.s = s0 + l;
-            r.load(a);
-            r.unit = static_cast<int>(rest / r.cost);
-            r.tile = static_cast<int>(rest - static_cast<long long>(r.unit) * r.cost);
-            return r;
-        }
-        done += __shfl_sync(kFull, upto, 31);
+        for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(kFull, n, o);
+        all = n * a.Hkv;
     }
-    r.s = a.nseq;
-    return r;
-}
-
-__device__ __forceinline__ int tile_shares(long long all, int ctas) {
-    return static_cast<int>(min(static_cast<long long>(ctas), (all + kMinTiles - 1) / kMinTiles));
-}
+    __device__ __forceinline__ TilePlace find(const PagedArgs& a, long long x, int lane) const {
+        long long done = 0;
+        TilePlace r{};
+        for (int s0 = 0; s0 < a.nseq; s0 += 32) {
+            int cost = s0 == 0 ? own : length(a, s0 + lane);
+            const long long n = static_cast<long long>(a.Hkv) * cost;
+            long long upto = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long y = __shfl_up_sync(kFull, upto, o);
+                if (lane >= o) upto += y;
+            }
+            const unsigned hit = __ballot_sync(kFull, x < done + upto);
+            if (hit) {
+                const int l = __ffs(hit) - 1;
+                const long long rest = x - done - __shfl_sync(kFull, upto - n, l);
+                cost = __shfl_sync(kFull, cost, l);
+                r.s = s0 + l;
+                r.load(a);
+                r.head = place_div(rest, cost);
+                r.tile = static_cast<int>(rest - static_cast<long long>(r.head) * cost);
+                for (int t; r.tile >= (t = r.tiles(a, r.qt) + kTileCost); r.qt++) r.tile -= t;
+                return r;
+            }
+            done += __shfl_sync(kFull, upto, 31);
+        }
+        r.s = a.nseq;
+        return r;
+    }
+};
 
 // A share's parts of units, one after the other.
 struct Walk {
@@ -291,16 +317,16 @@ struct Walk {
     int s, head, qt, t0, t1, tiles, whole, tail, nodes;  // the part at hand: tiles [t0, t1) of a unit of `tiles`
     __device__ __forceinline__ bool next(const PagedArgs& a) {
         while (left > 0) {
-            tiles = p.tiles(a);
+            tiles = p.tiles(a, p.qt);
             t0 = p.tile;
             t1 = static_cast<int>(min(static_cast<long long>(tiles), t0 + left));
             s = p.s;
-            head = p.unit / p.nqt;
-            qt = p.unit % p.nqt;
+            head = p.head;
+            qt = p.qt;
             whole = p.whole;
             tail = p.tail;
             nodes = p.nodes;
-            left -= p.cost - p.tile;
+            left -= tiles + kTileCost - t0;
             p.next_unit(a);
             if (t0 < t1) return true;
         }
@@ -457,16 +483,21 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = static_cast<uint32_t>(misc[0]);
-    pdl_wait();
-
-    const long long all = tile_cost_before(a, a.nseq, lane);
-    const int shares = tile_shares(all, gridDim.x);
+    // The preparation kernel lets this one start when all before it has ended:
+    // lengths, page numbers and pages may be read at once, only what it writes
+    // has to be waited for (pdl_wait below).
     Walk w{};
-    long long begin = 0;
-    if (static_cast<int>(blockIdx.x) < shares) {
-        begin = share_begin(all, shares, blockIdx.x);
-        w.left = share_begin(all, shares, blockIdx.x + 1) - begin;
-        w.p = find_tile(a, begin, lane);
+    {
+        const TileList list(a, lane);
+        const Shares shares(list.all, gridDim.x, kMinTiles);
+        if (static_cast<int>(blockIdx.x) < shares.count) {
+            w.left = shares.length(blockIdx.x);
+            w.p = list.find(a, shares.begin(blockIdx.x), lane);
+        }
+        if (threadIdx.x == 0) {
+            a.plan->places[blockIdx.x] = make_int4(w.p.s, w.p.head * 256 + w.p.qt, w.p.tile, 0);
+            if (blockIdx.x == 0) a.plan->count = shares.count;
+        }
     }
 
     if (warp < G_::kFirstSoft) {
@@ -477,11 +508,11 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
             const uint64_t policy = (a.B + 1) * a.G <= kRows ? l2_policy_evict_first() : l2_policy_evict_last();
             auto page_at = [&](int t) {
                 return t < w.whole && lane < per_tile
-                           ? __ldg(a.table + static_cast<long long>(w.s) * a.max_pages + static_cast<long long>(t) * per_tile + lane)
+                           ? __ldcg(a.table + static_cast<long long>(w.s) * a.max_pages + static_cast<long long>(t) * per_tile + lane)
                            : 0;
             };
             int n = 0;       // bf16: tiles so far; e4m3: whole cache tiles so far
-            bool have = w.next(a), ok = true;
+            bool have = w.next(a), ok = true, waited = false;
             int t = w.t0, page = have ? page_at(t) : 0;
             while (have && ok) {
                 // this tile, then the next one's page numbers, which are there when it is its turn
@@ -494,6 +525,10 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                 }
                 if (have) page = page_at(t);
                 if (kFp8 && !cache_tile) continue;  // (the converting warps read side tiles themselves)
+                if (!cache_tile && !waited) {
+                    pdl_wait();
+                    waited = true;
+                }
                 long long row = a.pool_rows;  // past the pool: zeros
                 if (cache_tile && lane < per_tile) {
                     if (my_page >= 0 && my_page < a.num_pages)
@@ -627,12 +662,13 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
             mbar_arrive(&q_ready[part & 1]);
         };
         bool have = w.next(a), ok = true;
+        pdl_wait();
         if (have) load_q(w, 0);
         int n = 0;
         for (int part = 0; have; part++) {
             const int s = w.s, head = w.head, t0 = w.t0, t1 = w.t1, whole = w.whole, tail = w.tail, nodes = w.nodes;
             const bool full_unit = t0 == 0 && t1 == w.tiles;
-            const int row = w.qt * kRows + r, b = row / a.G;
+            const int row = w.qt * kRows + r, b = row >> a.g_log2;
             const bool row_ok = b <= nodes;
             // m_run: the row's reference; e4m3: vref, a power of two above every value
             // scale so far, joins it as vshift, so that P = 2^(s - m) / vref * 2^7 times a
@@ -671,10 +707,12 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
 #pragma unroll
                         for (int c = 0; c < 64; c += 4) {
                             const float4 y = *reinterpret_cast<const float4*>(ks + c);
-                            sv[c] *= y.x;
-                            sv[c + 1] *= y.y;
-                            sv[c + 2] *= y.z;
-                            sv[c + 3] *= y.w;
+                            const float2 u = mul2(make_float2(sv[c], sv[c + 1]), make_float2(y.x, y.y));
+                            const float2 v = mul2(make_float2(sv[c + 2], sv[c + 3]), make_float2(y.z, y.w));
+                            sv[c] = u.x;
+                            sv[c + 1] = u.y;
+                            sv[c + 2] = v.x;
+                            sv[c + 3] = v.y;
                         }
                     }
                     if (all_seen) {
@@ -742,23 +780,26 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                 // P = 2^(s - m) as bf16 pairs; hidden keys hold -inf and give 0 (so does
                 // every key of a row that has seen no visible key: m = -inf)
                 const float nm = m_run == -INFINITY ? 0.0f : -(m_run + vshift);
-                float lsum = 0.0f;
+                float2 sum0 = make_float2(0.0f, 0.0f), sum1 = sum0;
                 uint32_t pk[32];
 #pragma unroll
                 for (int c = 0; c < 64; c += 4) {
-                    float4 y = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
-                    if (kFp8) y = *reinterpret_cast<const float4*>(ks + kKeys + c);
-                    const float by[4] = {y.x, y.y, y.z, y.w};
-                    float p[4];
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        p[e] = ex2(fmaf(sv[c + e], rs, nm));
-                        lsum += p[e];
-                        if (kFp8) p[e] *= by[e];
+                    float2 x = fma2(make_float2(sv[c], sv[c + 1]), make_float2(rs, rs), make_float2(nm, nm));
+                    float2 z = fma2(make_float2(sv[c + 2], sv[c + 3]), make_float2(rs, rs), make_float2(nm, nm));
+                    x = make_float2(ex2(x.x), ex2(x.y));
+                    z = make_float2(ex2(z.x), ex2(z.y));
+                    sum0 = add2(sum0, x);
+                    sum1 = add2(sum1, z);
+                    if (kFp8) {
+                        const float4 y = *reinterpret_cast<const float4*>(ks + kKeys + c);
+                        x = mul2(x, make_float2(y.x, y.y));
+                        z = mul2(z, make_float2(y.z, y.w));
                     }
-                    pk[c >> 1] = kFp8 ? pack_f16x2(p[0], p[1]) : pack_bf16x2(p[0], p[1]);
-                    pk[(c >> 1) + 1] = kFp8 ? pack_f16x2(p[2], p[3]) : pack_bf16x2(p[2], p[3]);
+                    pk[c >> 1] = kFp8 ? pack_f16x2(x.x, x.y) : pack_bf16x2(x.x, x.y);
+                    pk[(c >> 1) + 1] = kFp8 ? pack_f16x2(z.x, z.y) : pack_bf16x2(z.x, z.y);
                 }
+                sum0 = add2(sum0, sum1);
+                const float lsum = sum0.x + sum0.y;
                 tmem_st32(tl + kPCol + (n & 1) * 64 + wg * 32, pk);
                 tmem_wait_st();
                 l += lsum;
@@ -791,7 +832,7 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
             if (row_ok) {
                 if (full_unit) {
                     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-                    uint4* d = reinterpret_cast<uint4*>(a.out + ((static_cast<long long>(s) * (a.B + 1) + b) * a.Hq + head * a.G + row % a.G) * kHeadDim + cb);
+                    uint4* d = reinterpret_cast<uint4*>(a.out + ((static_cast<long long>(s) * (a.B + 1) + b) * a.Hq + head * a.G + (row & (a.G - 1))) * kHeadDim + cb);
 #pragma unroll
                     for (int e = 0; e < 8; e++)
                         d[e] = make_uint4(pack_bf16x2(o[8 * e] * inv, o[8 * e + 1] * inv), pack_bf16x2(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
@@ -809,11 +850,15 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
         // ---------------------------------------------------------- raw tiles to operands (e4m3): a thread per key
         reg_less<kRegsConvert>();
         const int key = threadIdx.x - (G_::kFirstSoft + 8) * 32;
-        bool ok = true;
+        bool ok = true, waited = false;
         int n = 0, raw = 0;  // tiles, whole cache tiles so far
         while (ok && w.next(a)) {
             for (int t = w.t0; t < w.t1 && ok; t++, n++) {
                 const bool cache_tile = t < w.whole;
+                if (!cache_tile && !waited) {
+                    pdl_wait();
+                    waited = true;
+                }
                 const int st = n % kStages;
                 float* sc = scales + (n % G_::kRing) * 2 * kKeys;
                 for (int kv = 0; kv < 2 && ok; kv++) {
@@ -887,31 +932,36 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
 }
 
 // Joins the parts of the units that several CTAs shared, in the order of
-// their keys.  One block per 16 rows of a unit, 16 threads (8 elements each)
-// a row.
-__global__ void __launch_bounds__(256) paged_tiles_join_kernel(const __grid_constant__ PagedArgs a, int ctas) {
+// their keys.  Blocks 8 (i - 1) .. + 7 work if share i begins inside a unit that
+// share i - 1 began: 16 rows each, 16 threads (8 elements each) a row.
+__global__ void __launch_bounds__(256) paged_tiles_join_kernel(const __grid_constant__ PagedArgs a) {
     pdl_trigger();
+    const int tid = threadIdx.x, i = blockIdx.x / 8 + 1, eighth = blockIdx.x % 8;
     pdl_wait();
-    const int tid = threadIdx.x, lane = tid & 31;
-    const int most = ((a.B + 1) * a.G + kRows - 1) / kRows, eighth = blockIdx.x % 8, u = blockIdx.x / 8;
-    const int s = u / (a.Hkv * most);
+    const int count = a.plan->count;
+    if (i >= count) return;
+    const int4 at = a.plan->places[i], prev = a.plan->places[i - 1];
+    if (at.z == 0 || (prev.x == at.x && prev.y == at.y && prev.z > 0)) return;
     TilePlace p{};
-    p.s = s;
+    p.s = at.x;
+    p.head = at.y / 256;
+    p.qt = at.y % 256;
     p.load(a);
-    p.unit = u % (a.Hkv * most);
-    if (p.unit >= p.units) return;
-    const int tiles = p.tiles(a), head = p.unit / p.nqt, row0 = (p.unit % p.nqt) * kRows + eighth * 16;
-    if (row0 >= (p.nodes + 1) * a.G) return;
-    const long long all = tile_cost_before(a, a.nseq, lane);
-    const int shares = tile_shares(all, ctas);
-    const long long first = tile_cost_before(a, s, lane) + static_cast<long long>(p.unit) * p.cost;
-    const int c0 = share_at(all, shares, first), c1 = share_at(all, shares, first + tiles - 1);
-    if (c0 == c1) return;
-    const int r = eighth * 16 + (tid >> 4), d8 = tid & 15, row = row0 + (tid >> 4), b = row / a.G;
+    const int tiles = p.tiles(a, p.qt), s = p.s, head = p.head;
+    if (at.z >= tiles) return;  // (the unit ended in share i - 1)
+    const int r = eighth * 16 + (tid >> 4), d8 = tid & 15, row = p.qt * kRows + r, b = row >> a.g_log2;
     if (b > p.nodes) return;
+    auto in_unit = [&](int c) {
+        if (c >= count) return false;
+        const int4 x = a.plan->places[c];
+        return x.x == at.x && x.y == at.y && x.z < tiles;
+    };
+    const int c0 = i - 1;
+    int c1 = i;
+    while (in_unit(c1 + 1)) c1++;
     float top = -INFINITY, l = 0.0f, o[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     for (int c = c0; c <= c1; c++) {
-        const TilePart* x = static_cast<const TilePart*>(a.parts) + 2 * c + (share_begin(all, shares, c) > first ? 0 : 1);
+        const TilePart* x = static_cast<const TilePart*>(a.parts) + 2 * c + (c < i ? 1 : 0);
         const float2 ml = x->ml[r];
         const float4 y = *reinterpret_cast<const float4*>(&x->o[r][8 * d8]), z = *reinterpret_cast<const float4*>(&x->o[r][8 * d8 + 4]);
         if (ml.x == -INFINITY) continue;
@@ -923,7 +973,7 @@ __global__ void __launch_bounds__(256) paged_tiles_join_kernel(const __grid_cons
         for (int k = 0; k < 8; k++) o[k] = o[k] * old + v[k] * by;
     }
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-    __nv_bfloat16* d = a.out + ((static_cast<long long>(s) * (a.B + 1) + b) * a.Hq + head * a.G + row % a.G) * kHeadDim + 8 * d8;
+    __nv_bfloat16* d = a.out + ((static_cast<long long>(s) * (a.B + 1) + b) * a.Hq + head * a.G + (row & (a.G - 1))) * kHeadDim + 8 * d8;
     *reinterpret_cast<uint4*>(d) = make_uint4(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv),
                                               pack_bf16x2(o[4] * inv, o[5] * inv), pack_bf16x2(o[6] * inv, o[7] * inv));
 }
@@ -938,7 +988,7 @@ TileWs tile_ws(int nseq, int B, int Hq, int Hkv) {
     w.sk = (kKeys - 1 + B + 1 + kKeys - 1) / kKeys * kKeys;
     auto up = [](size_t n) { return (n + 255) & ~static_cast<size_t>(255); };
     const size_t side = up(static_cast<size_t>(nseq) * Hkv * w.sk * kHeadDim * 2);
-    w.q = up(sizeof(TilePart) * 2 * kMaxSms);
+    w.q = up(sizeof(SharePlan) + sizeof(TilePart) * 2 * kMaxSms);
     w.k = w.q + up(static_cast<size_t>(nseq) * (B + 1) * Hq * kHeadDim * 2);
     w.v = w.k + side;
     w.qs = w.v + side;
@@ -984,8 +1034,7 @@ int launch_paged_tiles(PagedArgs a, const dart_kv_cache& cache, uint8_t* workspa
     e = fp8 ? launch_pdl(paged_tiles_kernel<true>, dim3(sms), dim3(TGeo<true>::kThreads), TGeo<true>::kSmem, st, tmK, tmV, tmSk, tmSv, ta)
             : launch_pdl(paged_tiles_kernel<false>, dim3(sms), dim3(TGeo<false>::kThreads), TGeo<false>::kSmem, st, tmK, tmV, tmSk, tmSv, ta);
     if (e != cudaSuccess) return DART_ERR_CUDA;
-    const int units = a.nseq * a.Hkv * (((a.B + 1) * a.G + kRows - 1) / kRows);
-    return launch_pdl(paged_tiles_join_kernel, dim3(units * 8), dim3(256), 0, st, a, sms) == cudaSuccess ? DART_OK : DART_ERR_CUDA;
+    return launch_pdl(paged_tiles_join_kernel, dim3(8 * (sms - 1)), dim3(256), 0, st, a) == cudaSuccess ? DART_OK : DART_ERR_CUDA;
 }
 
 }  // namespace dart
