@@ -67,11 +67,11 @@ template <typename T>
 __device__ __forceinline__ float load_logit(const T* row, int i);
 template <>
 __device__ __forceinline__ float load_logit<float>(const float* row, int i) {
-    return clean(__ldg(row + i));
+    return clean(ld_plain(row + i));
 }
 template <>
 __device__ __forceinline__ float load_logit<__nv_bfloat16>(const __nv_bfloat16* row, int i) {
-    return clean(__bfloat162float(__ldg(row + i)));
+    return clean(__bfloat162float(ld_plain(row + i)));
 }
 
 // The logits of one 16-byte vector: cleaned words, their values, and the
@@ -147,7 +147,7 @@ __device__ __forceinline__ void hold(const T* row, const Share& s, uint4 (&held)
 #pragma unroll
     for (int q = 0; q < kHeld; q++) {
         const int v = s.v0 + threadIdx.x + q * kVerifyThreads;
-        held[q] = v < s.v1 ? __ldg(vec + v) : make_uint4(none, none, none, none);
+        held[q] = v < s.v1 ? ld_plain(vec + v) : make_uint4(none, none, none, none);
     }
 }
 // The element that this thread has beside vectors, -1 if none.
@@ -241,10 +241,10 @@ __global__ void __launch_bounds__(kVerifyThreads, 1) verify_tree_kernel(const Ve
     Share share = share_of<T, kCtas>(base, a.V, rank);
     uint4 held[kHeld];
     hold(base, share, held);
-    float u = sampling ? __ldg(a.u + static_cast<long long>(s) * R) : 0.0f;
-    const int nn = min(max(__ldg(a.n_nodes + s), 0), a.B);
+    float u = sampling ? ld_plain(a.u + static_cast<long long>(s) * R) : 0.0f;
+    const int nn = min(max(ld_plain(a.n_nodes + s), 0), a.B);
     for (int i = tid; i < nn; i += kVerifyThreads) {
-        const int p = __ldg(a.parents + static_cast<long long>(s) * a.B + i), t = __ldg(a.tokens + static_cast<long long>(s) * a.B + i);
+        const int p = ld_plain(a.parents + static_cast<long long>(s) * a.B + i), t = ld_plain(a.tokens + static_cast<long long>(s) * a.B + i);
         // a child comes after its parent, which ends every walk
         sm.parent[i] = p >= -1 && p < i && t >= 0 && t < a.V ? p + 1 : -1;
         sm.token[i] = t;
@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 1) verify_tree_kernel(const Ve
             held[q] = Vec<T>::clean4(held[q]);
             st.m = fmaxf(st.m, Vec<T>::top(held[q]));
         }
-        for (int v = v_more; v < share.v1; v += kVerifyThreads) st.m = fmaxf(st.m, Vec<T>::top(Vec<T>::clean4(__ldg(vec + v))));
+        for (int v = v_more; v < share.v1; v += kVerifyThreads) st.m = fmaxf(st.m, Vec<T>::top(Vec<T>::clean4(ld_plain(vec + v))));
         if (st.m != -INFINITY) {
             auto add = [&](const uint4& w) {
                 float z[n], x = 0.0f;
@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 1) verify_tree_kernel(const Ve
             if (odd >= 0) st.sum += fast_exp2((odd_z - st.m) * c);
 #pragma unroll
             for (int q = 0; q < kHeld; q++) add(held[q]);
-            for (int v = v_more; v < share.v1; v += kVerifyThreads) add(Vec<T>::clean4(__ldg(vec + v)));
+            for (int v = v_more; v < share.v1; v += kVerifyThreads) add(Vec<T>::clean4(ld_plain(vec + v)));
         }
         if (!sampling && __any_sync(kFull, st.m != -INFINITY)) {
             const float top = f32_unord(__reduce_max_sync(kFull, f32_ord(st.m)));
@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 1) verify_tree_kernel(const Ve
                 };
 #pragma unroll
                 for (int q = 0; q < kHeld; q++) seek(held[q], share.v0 + tid + q * kVerifyThreads);
-                for (int v = v_more; v < share.v1; v += kVerifyThreads) seek(Vec<T>::clean4(__ldg(vec + v)), v);
+                for (int v = v_more; v < share.v1; v += kVerifyThreads) seek(Vec<T>::clean4(ld_plain(vec + v)), v);
             }
         }
 #pragma unroll
@@ -424,21 +424,21 @@ __global__ void __launch_bounds__(kVerifyThreads, 1) verify_tree_kernel(const Ve
 #pragma unroll
                     for (int e = 0; e < n; e++) {
                         const int i = t0 + e - noise0;
-                        const float x = i >= 0 && i < noise_n ? sm.noise[i] : __ldg(noise + t0 + e);
+                        const float x = i >= 0 && i < noise_n ? sm.noise[i] : ld_plain(noise + t0 + e);
                         if (!((child >> (q * n + e)) & 1u)) offer(z[e], x, t0 + e);
                     }
                 }
             }
             for (int v = v_more; v < share.v1; v += kVerifyThreads) {
                 float z[n];
-                Vec<T>::get(Vec<T>::clean4(__ldg(vec + v)), z);
+                Vec<T>::get(Vec<T>::clean4(ld_plain(vec + v)), z);
 #pragma unroll
                 for (int e = 0; e < n; e++) {
                     const int t = share.first + v * n + e;
-                    if (!is_child(t)) offer(z[e], __ldg(noise + t), t);
+                    if (!is_child(t)) offer(z[e], ld_plain(noise + t), t);
                 }
             }
-            if (odd >= 0 && !is_child(odd)) offer(odd_z, __ldg(noise + odd), odd);
+            if (odd >= 0 && !is_child(odd)) offer(odd_z, ld_plain(noise + odd), odd);
             w = cluster_merge<kCtas>(sm, w, rank, parity, 0.0f);
             parity ^= 1;
             if (w.m != -INFINITY)
@@ -459,7 +459,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 1) verify_tree_kernel(const Ve
             row = kids.node[next] + 1;
             share = share_of<T, kCtas>(base + static_cast<long long>(row) * a.ld, a.V, rank);
             hold(base + static_cast<long long>(row) * a.ld, share, held);
-            if (sampling) u = __ldg(a.u + static_cast<long long>(s) * R + row);
+            if (sampling) u = ld_plain(a.u + static_cast<long long>(s) * R + row);
         }
         if (rank == kCtas - 1 && warp == kVerifyWarps - 1 && lane == 0) {
             const long long o = static_cast<long long>(s) * R + step;

@@ -115,15 +115,15 @@ __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const __gr
     const int chunk = static_cast<int>(group % a.chunks);
     const long long token = group / a.chunks;
     const int s = static_cast<int>(token / a.R), i = static_cast<int>(token % a.R);
-    bool use = s < a.nseq && i < __ldg(a.n_rows + min(s, a.nseq - 1));
+    bool use = s < a.nseq && i < ld_plain(a.n_rows + min(s, a.nseq - 1));
     long long src = 0, dst = 0;
     int pos = 0;
     if (use) {
-        const int src_row = a.rows ? __ldg(a.rows + token) : i;
+        const int src_row = a.rows ? ld_plain(a.rows + token) : i;
         const long long most = static_cast<long long>(a.max_pages) << a.page_log2;
-        const long long p = min(max(static_cast<long long>(__ldg(a.lens + s)), 0ll), most) + i;
+        const long long p = min(max(static_cast<long long>(ld_plain(a.lens + s)), 0ll), most) + i;
         int page = -1;
-        if (p < most) page = __ldg(a.table + static_cast<long long>(s) * a.max_pages + (p >> a.page_log2));
+        if (p < most) page = ld_plain(a.table + static_cast<long long>(s) * a.max_pages + (p >> a.page_log2));
         if (src_row < 0 || src_row >= a.R || page < 0 || page >= a.num_pages) {
             if (a.status && j == 0) atomicOr(a.status, kDevBounds);
             use = false;

@@ -113,6 +113,14 @@ __device__ __forceinline__ unsigned long long globaltimer_ns() {
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// A plain load, for what an earlier kernel wrote: it stays behind pdl_wait.  (A
+// __ldg is an invariant load to the compiler, which may move it up; where its
+// address is known early it then reads what was there before.)
+template <typename T>
+__device__ __forceinline__ T ld_plain(const T* p) {
+    return *p;
+}
+
 __device__ __forceinline__ void named_bar_sync(int id, int nthreads) {
     asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
 }

@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     };
     auto page_at = [&](int key) {
-        return __ldg(a.table + static_cast<long long>(load.s) * a.max_pages + (key >> a.page_log2));
+        return ld_plain(a.table + static_cast<long long>(load.s) * a.max_pages + (key >> a.page_log2));
     };
     int page[2] = {0, 0};  // of `load`, read a chunk ahead of its use (two where pages are smaller than chunks)
     auto look_up = [&]() {
@@ -325,12 +325,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int e = 0; e < 8; e++) x[i][e] = 0.0f;
             if (b <= nodes) {
-                const int pos = len + (b > 0 ? __ldg(a.depths + static_cast<long long>(s) * a.B + b - 1) : 0);
+                const int pos = len + (b > 0 ? ld_plain(a.depths + static_cast<long long>(s) * a.B + b - 1) : 0);
                 const __nv_bfloat16* src = a.q + (seq_row + b) * a.q_stride + (head * a.G + (r & (a.G - 1))) * kHeadDim;
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
                     const int d0 = 8 * k_piece<kFp8>(i, t);
-                    const uint4 u = __ldg(reinterpret_cast<const uint4*>(src + d0)), w = __ldg(reinterpret_cast<const uint4*>(src + d0 + 64));
+                    const uint4 u = ld_plain(reinterpret_cast<const uint4*>(src + d0)), w = ld_plain(reinterpret_cast<const uint4*>(src + d0 + 64));
                     const uint32_t uw[4] = {u.x, u.y, u.z, u.w}, ww[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
                     for (int e = 0; e < 8; e++) {
@@ -606,13 +606,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int e = 0; e < 4; e++) w[i][e] = 0u;
                 if (j <= nodes) {
-                    const int pos = len + (j > 0 ? __ldg(a.depths + static_cast<long long>(s) * a.B + j - 1) : 0);
+                    const int pos = len + (j > 0 ? ld_plain(a.depths + static_cast<long long>(s) * a.B + j - 1) : 0);
                     const __nv_bfloat16* k = a.k + (seq_row + j) * a.k_stride + head * kHeadDim;
 #pragma unroll
                     for (int i = 0; i < 2; i++) {
                         const int d0 = 8 * k_piece<kFp8>(i, t);
-                        const uint4 x = __ldg(reinterpret_cast<const uint4*>(k + d0));
-                        const uint4 y = __ldg(reinterpret_cast<const uint4*>(k + d0 + 64));
+                        const uint4 x = ld_plain(reinterpret_cast<const uint4*>(k + d0));
+                        const uint4 y = ld_plain(reinterpret_cast<const uint4*>(k + d0 + 64));
                         const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
                         for (int e = 0; e < 4; e++) {
@@ -659,7 +659,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const int j = key0 + slot_row(qq, 2 * t + e), b = (row0 + g + 8 * h) >> a.g_log2;
                         bool see = j <= nodes && b <= nodes;
                         if (see && j > 0)
-                            see = b > 0 && ((__ldg(a.mask + (static_cast<long long>(s) * a.B + b - 1) * a.mw + ((j - 1) >> 6)) >> ((j - 1) & 63)) & 1ull);
+                            see = b > 0 && ((ld_plain(a.mask + (static_cast<long long>(s) * a.B + b - 1) * a.mw + ((j - 1) >> 6)) >> ((j - 1) & 63)) & 1ull);
                         sc[qq][2 * h + e] = see ? sc[qq][2 * h + e] * rs[h] : -INFINITY;
                     }
             soften(sc);
@@ -676,7 +676,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             values_bf16(p, [&](int half, int qq, int e) {
                 const int j = key0 + slot_row(qq, 2 * t + e);
                 if (j > nodes) return make_uint4(0, 0, 0, 0);
-                return __ldg(reinterpret_cast<const uint4*>(a.v + (seq_row + j) * a.v_stride + head * kHeadDim + 8 * (kFp8 ? 2 * g + half : g + 8 * half)));
+                return ld_plain(reinterpret_cast<const uint4*>(a.v + (seq_row + j) * a.v_stride + head * kHeadDim + 8 * (kFp8 ? 2 * g + half : g + 8 * half)));
             });
         }
 

@@ -21,10 +21,12 @@
 // warp 1 issues the MMAs; warps 2-9 are two softmax warpgroups (thread = query
 // row = TMEM lane; warpgroup wg owns key and output columns [64 wg, 64 wg +
 // 64), the two warps of a lane quarter exchange maxima and sums).  With e4m3
-// pages all operands are f16: four more warps turn raw tiles into f16 codes
-// (exact, one conversion instruction per pair; bf16 took six), while the
-// scales are applied to scores and probabilities; queries and side rows are
-// f16 with a power of two per row, which no magnitude can overflow.  TMEM (512 columns): S
+// pages all operands are f16: four more warps turn raw tiles into f16, each
+// key's codes times its scale over a power of two that the tile (K) or the
+// unit so far (V) has in common; queries and side rows are f16 with a power
+// of two per row.  So nothing can overflow, and the softmax has one factor a
+// tile to apply instead of one a key (64 broadcast reads of a key's scale from
+// shared memory, twice, took 0.5 us of a tile's 1.6).  TMEM (512 columns): S
 // [0,128), O [128,256), P [256,384) in two buffers, Q [384,512) in two.
 // A row's running maximum is raised (and O rescaled) only when a tile exceeds
 // it by more than 2^8.  Every wait is bounded.
@@ -51,32 +53,34 @@ constexpr int kHalf = kKeys * 128;       // 128 rows of one 128-byte swizzle col
 constexpr int kTile = 2 * kHalf;         // 128 keys of bf16
 constexpr int kSoft = 256;               // softmax threads
 constexpr int kPairBar = 2;              // named barriers 2 .. 5
+constexpr int kConvBar = 6;
 constexpr float kSlack8 = 8.0f;          // log2 units: P <= 2^8 between rescales
-constexpr int kTileCost = 1;             // of a unit beside its tiles, in tiles
+// What a unit costs beside its tiles (its queries, its result, the pause between
+// its last tile and the next unit's first), in tiles: eight trees of 512 nodes over
+// e4m3 pages 490 us with 1, 433 with 3, 401 with 5.
+constexpr int kTileCost = 5;
 constexpr int kMinTiles = 2;             // of a share
 constexpr uint32_t kSCol = 0, kOCol = 128, kPCol = 256, kQCol = 384;
 
+// Rows that threads of a warp read or write one each are kept a 16-byte piece
+// after the other: piece c of row r of a 128-row tile at [c][r].
 struct TilePart {
-    float o[kRows][kHeadDim];
+    float4 o[kHeadDim / 4][kRows];
     float2 ml[kRows];
 };
 
 struct TileArgs {
     PagedArgs p;
     int sk;                    // side keys per sequence and kv head (a multiple of 128)
+    int nqt;                    // query tiles of a kv head of a full tree
     // bf16, or f16 (e4m3 pages) with a factor per row:
-    uint16_t* qr;               // [nseq][Hkv][(B + 1) * G][128]
-    uint16_t *side_k, *side_v;  // [nseq][Hkv][sk][128]
-    float* q_scale;             // [nseq][Hkv][(B + 1) * G], with scale * log2(e) in it
+    uint4* qr;                  // [nseq][Hkv][nqt][16 pieces][128 rows]
+    uint4 *side_k, *side_v;     // [nseq][Hkv][sk] rows; e4m3 pages: [nseq][Hkv][sk / 128][16 pieces][128]
+    float* q_scale;             // [nseq][Hkv][nqt][128], with scale * log2(e) in it
     float *side_ks, *side_vs;   // [nseq][Hkv][sk]
 };
 
 // Two fp32 operations in one instruction.
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)));
-    return *reinterpret_cast<float2*>(&r);
-}
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     uint64_t r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)));
@@ -102,125 +106,164 @@ __device__ __forceinline__ uint32_t pack_f16x2(float a, float b) {
 
 // ------------------------------------------------------------ preparation
 
-// A row of 128 values, four to a lane (2 lane, 2 lane + 1 and the same 64
-// further), as bf16; or as f16 scaled by a power of two to a largest element
-// in [1, 2), and the factor that undoes it.
-template <bool kF16>
-__device__ __forceinline__ float put_row(uint16_t* row, int lane, const float (&x)[4]) {
-    uint32_t w[2];
-    float factor = 1.0f;
-    if (kF16) {
-        float mx = fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3])));
-        mx = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(mx)));
-        const int ex = min(max(static_cast<int>(__float_as_uint(mx) >> 23) - 127, -100), 120);
-        const float down = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
-        factor = __uint_as_float(static_cast<uint32_t>(127 + ex) << 23);
-        const __half2 h0 = __floats2half2_rn(x[0] * down, x[1] * down), h1 = __floats2half2_rn(x[2] * down, x[3] * down);
-        w[0] = *reinterpret_cast<const uint32_t*>(&h0);
-        w[1] = *reinterpret_cast<const uint32_t*>(&h1);
-    } else {
-        w[0] = pack_bf16x2(x[0], x[1]);
-        w[1] = pack_bf16x2(x[2], x[3]);
+// 16 of a row's 128 values: elements 8 p .. 8 p + 7 and 64 + 8 p .. of lane p of
+// a group of 8.
+struct Piece {
+    float lo[8], hi[8];
+};
+__device__ __forceinline__ Piece unpack_piece(const uint4& a, const uint4& b) {
+    const uint32_t u[4] = {a.x, a.y, a.z, a.w}, w[4] = {b.x, b.y, b.z, b.w};
+    Piece x;
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        x.lo[2 * e] = bf16_lo(u[e]);
+        x.lo[2 * e + 1] = bf16_hi(u[e]);
+        x.hi[2 * e] = bf16_lo(w[e]);
+        x.hi[2 * e + 1] = bf16_hi(w[e]);
     }
-    uint32_t* d = reinterpret_cast<uint32_t*>(row) + lane;
-    d[0] = w[0];
-    d[32] = w[1];
+    return x;
+}
+// As bf16, or as f16 scaled by a power of two to a largest element of the row
+// in [1, 2); returns the factor that undoes it.  (All lanes of the warp.)
+template <bool kF16>
+__device__ __forceinline__ float pack_piece(const Piece& x, uint4* lo, uint4* hi) {
+    float down = 1.0f, factor = 1.0f;
+    if (kF16) {
+        float mx = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; e++) mx = fmaxf(mx, fmaxf(fabsf(x.lo[e]), fabsf(x.hi[e])));
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, o));
+        const int ex = min(max(static_cast<int>(__float_as_uint(mx) >> 23) - 127, -100), 120);
+        down = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+        factor = __uint_as_float(static_cast<uint32_t>(127 + ex) << 23);
+    }
+    auto two = [&](float a, float b) { return kF16 ? pack_f16x2(a * down, b * down) : pack_bf16x2(a, b); };
+    *lo = make_uint4(two(x.lo[0], x.lo[1]), two(x.lo[2], x.lo[3]), two(x.lo[4], x.lo[5]), two(x.lo[6], x.lo[7]));
+    *hi = make_uint4(two(x.hi[0], x.hi[1]), two(x.hi[2], x.hi[3]), two(x.hi[4], x.hi[5]), two(x.hi[6], x.hi[7]));
     return factor;
 }
 
-// One warp per (sequence, side row, kv head): the side row's key and value,
-// and, if it is a tree row, the rotated queries of its G heads.
+// One block per side row of a sequence; groups of 8 threads take its keys and
+// values, head by head, and, if it is a tree row, the rotated queries.
+constexpr int kPrepThreads = 256, kGroups = kPrepThreads / 8;
 template <bool kFp8>
-__global__ void __launch_bounds__(256) paged_prep_kernel(const __grid_constant__ TileArgs ta, const uint8_t* pool_k, const uint8_t* pool_v) {
+__global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_constant__ TileArgs ta, const uint8_t* pool_k, const uint8_t* pool_v) {
+    __shared__ float2 turn_of[kHeadDim / 2];  // cos, sin
     const PagedArgs& a = ta.p;
     pdl_wait();
     pdl_trigger();  // (after the wait: the next kernel reads lengths and pages before its own)
-    const int lane = threadIdx.x & 31;
-    const long long id = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) >> 5;
-    const int head = static_cast<int>(id % a.Hkv), j = static_cast<int>(id / a.Hkv % ta.sk);
-    const int s = static_cast<int>(id / a.Hkv / ta.sk);
-    if (s >= a.nseq) return;
+    const int tid = threadIdx.x, p = tid & 7, group = tid >> 3, s = blockIdx.x, j = blockIdx.y;
     const int len = seq_len(a, s), nodes = seq_nodes(a, s), tail = len % kKeys, b = j - tail;
-    const long long side = (static_cast<long long>(s) * a.Hkv + head) * ta.sk + j;
-    uint16_t *sk = ta.side_k + side * kHeadDim, *sv = ta.side_v + side * kHeadDim;
-    float ks = 1.0f, vs = 1.0f;
+    const bool needed = j < (tail + nodes) / kKeys * kKeys + kKeys;
+    auto put_side = [&](int kv, int head, const uint4& lo, const uint4& hi) {
+        uint4* d = kv ? ta.side_v : ta.side_k;
+        const long long row = (static_cast<long long>(s) * a.Hkv + head) * ta.sk + j;
+        if (kFp8) {
+            d += (row >> 7) * (16 * kKeys) + (row & 127);
+            d[p * kKeys] = lo;
+            d[(8 + p) * kKeys] = hi;
+        } else {
+            d[row * 16 + p] = lo;
+            d[row * 16 + 8 + p] = hi;
+        }
+    };
+    auto put_scale = [&](int kv, int head, float x) {
+        if (kFp8 && p == 0) (kv ? ta.side_vs : ta.side_ks)[(static_cast<long long>(s) * a.Hkv + head) * ta.sk + j] = x;
+    };
     if (b < 0) {
         // a token of the cache: its codes or values as they are
         const int key = len - tail + j;
-        const int page = __ldg(a.table + static_cast<long long>(s) * a.max_pages + (key >> a.page_log2));
-        uint32_t k[2] = {0u, 0u}, v[2] = {0u, 0u};
-        if (page < 0 || page >= a.num_pages) {
-            if (a.status && lane == 0) atomicOr(a.status, kDevBounds);
-        } else {
-            const long long row = ((static_cast<long long>(page) * a.Hkv + head) << a.page_log2) + (key & ((1 << a.page_log2) - 1));
-            if (kFp8) {
-                ks = __ldg(a.ks + row);
-                vs = __ldg(a.vs + row);
+        const int page = ld_plain(a.table + static_cast<long long>(s) * a.max_pages + (key >> a.page_log2));
+        const bool there = page >= 0 && page < a.num_pages;
+        if (!there && a.status && tid == 0) atomicOr(a.status, kDevBounds);
+        for (int i = group; i < 2 * a.Hkv; i += kGroups) {
+            const int kv = i >= a.Hkv, head = i - kv * a.Hkv;
+            const long long row = there ? ((static_cast<long long>(page) * a.Hkv + head) << a.page_log2) + (key & ((1 << a.page_log2) - 1)) : 0;
+            const uint8_t* pool = kv ? pool_v : pool_k;
+            uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
+            if (there && kFp8) {
+                const uint2 x = *reinterpret_cast<const uint2*>(pool + row * kHeadDim + 8 * p), y = *reinterpret_cast<const uint2*>(pool + row * kHeadDim + 64 + 8 * p);
+                lo = make_uint4(codes_to_f16(x.x), codes_to_f16(x.x >> 16), codes_to_f16(x.y), codes_to_f16(x.y >> 16));
+                hi = make_uint4(codes_to_f16(y.x), codes_to_f16(y.x >> 16), codes_to_f16(y.y), codes_to_f16(y.y >> 16));
+            } else if (there) {
+                lo = reinterpret_cast<const uint4*>(pool)[row * 16 + p];
+                hi = reinterpret_cast<const uint4*>(pool)[row * 16 + 8 + p];
             }
-#pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const long long at = row * kHeadDim + 64 * h + 2 * lane;
-                if (kFp8) {
-                    const uint16_t x = *reinterpret_cast<const uint16_t*>(pool_k + at), y = *reinterpret_cast<const uint16_t*>(pool_v + at);
-                    k[h] = codes_to_f16(x);
-                    v[h] = codes_to_f16(y);
-                } else {
-                    k[h] = *reinterpret_cast<const uint32_t*>(pool_k + at * 2);
-                    v[h] = *reinterpret_cast<const uint32_t*>(pool_v + at * 2);
-                }
-            }
+            put_side(kv, head, lo, hi);
+            if (kFp8) put_scale(kv, head, there ? ld_plain((kv ? a.vs : a.ks) + row) : 1.0f);
         }
-        reinterpret_cast<uint32_t*>(sk)[lane] = k[0];
-        reinterpret_cast<uint32_t*>(sk)[lane + 32] = k[1];
-        reinterpret_cast<uint32_t*>(sv)[lane] = v[0];
-        reinterpret_cast<uint32_t*>(sv)[lane + 32] = v[1];
-    } else {
-        float k[4] = {0.0f, 0.0f, 0.0f, 0.0f}, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (b <= a.B) {
-            const long long in = static_cast<long long>(s) * (a.B + 1) + b;
-            const long long q_row = (static_cast<long long>(s) * a.Hkv + head) * (a.B + 1) * a.G + static_cast<long long>(b) * a.G;
-            const bool node = b <= nodes;
-            float s0 = 0.0f, c0 = 0.0f, s1 = 0.0f, c1 = 0.0f;
-            auto get = [&](const __nv_bfloat16* src, float (&x)[4]) {
-                const uint32_t* p = reinterpret_cast<const uint32_t*>(src) + lane;
-                const uint32_t lo = __ldg(p), hi = __ldg(p + 32);
-                x[0] = bf16_lo(lo);
-                x[1] = bf16_hi(lo);
-                x[2] = bf16_lo(hi);
-                x[3] = bf16_hi(hi);
-            };
-            auto turn = [&](float (&x)[4]) {
-                const float y[4] = {x[0] * c0 - x[2] * s0, x[1] * c1 - x[3] * s1, x[2] * c0 + x[0] * s0, x[3] * c1 + x[1] * s1};
-#pragma unroll
-                for (int e = 0; e < 4; e++) x[e] = y[e];
-            };
-            if (node) {
-                get(a.k + in * a.k_stride + head * kHeadDim, k);
-                get(a.v + in * a.v_stride + head * kHeadDim, v);
-                const int pos = len + (b > 0 ? __ldg(a.depths + static_cast<long long>(s) * a.B + b - 1) : 0);
-                rope_sincos(a.turns.f[2 * lane], pos, &s0, &c0);
-                rope_sincos(a.turns.f[2 * lane + 1], pos, &s1, &c1);
-                turn(k);
-            }
-#pragma unroll 4
-            for (int g = 0; g < a.G; g++) {
-                float q[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                if (node) {
-                    get(a.q + in * a.q_stride + (head * a.G + g) * kHeadDim, q);
-                    turn(q);
-                } else {
-                    reinterpret_cast<uint2*>(a.out + (in * a.Hq + head * a.G + g) * kHeadDim)[lane] = make_uint2(0u, 0u);
-                }
-                const float factor = put_row<kFp8>(ta.qr + (q_row + g) * kHeadDim, lane, q);
-                if (kFp8 && lane == 0) ta.q_scale[q_row + g] = factor * a.sl2;
-            }
-        }
-        ks = put_row<kFp8>(sk, lane, k);
-        vs = put_row<kFp8>(sv, lane, v);
+        return;
     }
-    if (kFp8 && lane == 0) {
-        ta.side_ks[side] = ks;
-        ta.side_vs[side] = vs;
+    if (b > nodes) {
+        // no tree row: zeros where a tile reads them, and as output of rows that are no node
+        if (needed)
+            for (int i = group; i < 2 * a.Hkv; i += kGroups) {
+                const int kv = i >= a.Hkv, head = i - kv * a.Hkv;
+                put_side(kv, head, make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u));
+                put_scale(kv, head, 0.0f);
+            }
+        if (b <= a.B) {
+            uint4* out = reinterpret_cast<uint4*>(a.out + (static_cast<long long>(s) * (a.B + 1) + b) * a.Hq * kHeadDim);
+            for (int i = tid; i < a.Hq * 16; i += kPrepThreads) out[i] = make_uint4(0u, 0u, 0u, 0u);
+        }
+        return;
+    }
+    const long long in = static_cast<long long>(s) * (a.B + 1) + b;
+    const int rows = a.Hq + 2 * a.Hkv;  // queries, keys, values
+    auto source = [&](int i) {
+        return i < a.Hq ? a.q + in * a.q_stride + i * kHeadDim
+                        : i < a.Hq + a.Hkv ? a.k + in * a.k_stride + (i - a.Hq) * kHeadDim : a.v + in * a.v_stride + (i - a.Hq - a.Hkv) * kHeadDim;
+    };
+    constexpr int kBatch = 2;  // rows of a group on their way at a time
+    for (int i0 = 0; i0 < rows; i0 += kBatch * kGroups) {
+        uint4 raw[kBatch][2];
+#pragma unroll
+        for (int u = 0; u < kBatch; u++) {
+            const int i = i0 + u * kGroups + group;
+            raw[u][0] = raw[u][1] = make_uint4(0u, 0u, 0u, 0u);
+            if (i < rows) {
+                raw[u][0] = ld_plain(reinterpret_cast<const uint4*>(source(i)) + p);
+                raw[u][1] = ld_plain(reinterpret_cast<const uint4*>(source(i)) + 8 + p);
+            }
+        }
+        if (i0 == 0) {  // the position's angles meanwhile
+            const int pos = len + (b > 0 ? ld_plain(a.depths + static_cast<long long>(s) * a.B + b - 1) : 0);
+            if (tid < kHeadDim / 2) {
+                float sn, cs;
+                rope_sincos(a.turns.f[tid], pos, &sn, &cs);
+                turn_of[tid] = make_float2(cs, sn);
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; u++) {
+            if (i0 + u * kGroups >= rows) break;  // (whole warps stay together)
+            const int i = i0 + u * kGroups + group;
+            Piece x = unpack_piece(raw[u][0], raw[u][1]);
+            if (i < a.Hq + a.Hkv)
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    const float2 t = turn_of[8 * p + e];
+                    const float lo = x.lo[e], hi = x.hi[e];
+                    x.lo[e] = lo * t.x - hi * t.y;
+                    x.hi[e] = hi * t.x + lo * t.y;
+                }
+            uint4 lo, hi;
+            const float factor = pack_piece<kFp8>(x, &lo, &hi);
+            if (i < a.Hq) {
+                const int head = i >> a.g_log2, row = (b << a.g_log2) + (i & (a.G - 1));
+                const long long tile = (static_cast<long long>(s) * a.Hkv + head) * ta.nqt + (row >> 7);
+                uint4* d = ta.qr + tile * (16 * kRows) + (row & 127);
+                d[p * kRows] = lo;
+                d[(8 + p) * kRows] = hi;
+                if (kFp8 && p == 0) ta.q_scale[tile * kRows + (row & 127)] = factor * a.sl2;
+            } else if (i < rows) {
+                const int kv = i >= a.Hq + a.Hkv, head = i - a.Hq - kv * a.Hkv;
+                put_side(kv, head, lo, hi);
+                put_scale(kv, head, factor);
+            }
+        }
     }
 }
 
@@ -376,20 +419,24 @@ __device__ __forceinline__ void mma_pv(uint32_t d, uint32_t p, uint32_t v_lo, ui
     if constexpr (kk + 1 < kKeys / 16) mma_pv<kk + 1>(d, p, v_lo, idesc, first);
 }
 
+// A power of two above x >= 0.
+__device__ __forceinline__ float above(float x) {
+    return __uint_as_float((min(max(__float_as_uint(x) >> 23, 27u), 252u) + 1u) << 23);
+}
+
 template <bool kFp8>
 struct TGeo {
     // bf16: three operand tiles of K and of V.  e4m3: two of each, and raw
     // tiles of half the size before them.
     static constexpr int kStages = kFp8 ? 2 : 3;
     static constexpr int kRawK = kFp8 ? 3 : 0, kRawV = kFp8 ? 2 : 0;
-    static constexpr int kRing = 4;  // scales outlive their tiles' operands
+    static constexpr int kRing = 4;  // a tile's factors outlive its operands
     static constexpr int kOps = 2 * kStages * kTile;
     static constexpr int kRaw = (kRawK + kRawV) * kHalf;
     static constexpr int kRawScales = kRawK * 2 * kKeys * 4;
-    static constexpr int kScales = kFp8 ? kRing * 2 * kKeys * 4 : 0;
     static constexpr int kBars = 4 * kStages + 2 * (kRawK + kRawV) + (kFp8 ? kRing : 0) + 9 + 1;
-    static constexpr int kExchange = 2 * kRows * 4 + 8 * 4 + kRing * 4 * 4;
-    static constexpr int kSmem = kOps + kRaw + kRawScales + kScales + kBars * 8 + kExchange + 16;
+    static constexpr int kExchange = 2 * kRows * 4 + 8 * 4 + kRing * 8 + kRing * 4 * 8;
+    static constexpr int kSmem = kOps + kRaw + kRawScales + kBars * 8 + kExchange + 16;
     // e4m3: warpgroups (producer, MMA, two idle warps), softmax, softmax, converters
     static constexpr int kThreads = kFp8 ? 512 : 64 + kSoft;
     static constexpr int kFirstSoft = kFp8 ? 4 : 2;
@@ -397,13 +444,37 @@ struct TGeo {
 
 __device__ __forceinline__ uint32_t tile_swz(int row, int piece) { return static_cast<uint32_t>(row * 128 + ((piece ^ (row & 7)) << 4)); }
 
+// 8 x 8 pieces of 16 bytes, a row per lane of 8: afterwards lane j has piece j of
+// all 8 rows.
+__device__ __forceinline__ void transpose8(uint4 (&y)[8], int lane) {
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) {
+        const bool up = lane & o;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            if (i & o) continue;
+            uint4 &a = y[i], &b = y[i | o];  // (this lane keeps a if its bit is clear, else b)
+            const uint4 give = up ? a : b;
+            uint4 got;
+            got.x = __shfl_xor_sync(kFull, give.x, o);
+            got.y = __shfl_xor_sync(kFull, give.y, o);
+            got.z = __shfl_xor_sync(kFull, give.z, o);
+            got.w = __shfl_xor_sync(kFull, give.w, o);
+            if (up)
+                a = got;
+            else
+                b = got;
+        }
+    }
+}
+
 // Bits [o, o + 64) of a row of mask words (o >= -128; bits outside are 0).
 __device__ __forceinline__ uint64_t mask_bits(const uint64_t* m, int mw, int o) {
     if (o <= -64) return 0ull;
-    if (o < 0) return __ldg(m) << -o;
+    if (o < 0) return ld_plain(m) << -o;
     const int w = o >> 6, sh = o & 63;
-    uint64_t r = w < mw ? __ldg(m + w) >> sh : 0ull;
-    if (sh && w + 1 < mw) r |= __ldg(m + w + 1) << (64 - sh);
+    uint64_t r = w < mw ? ld_plain(m + w) >> sh : 0ull;
+    if (sh && w + 1 < mw) r |= ld_plain(m + w + 1) << (64 - sh);
     return r;
 }
 
@@ -421,8 +492,7 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
     uint8_t* rK = sV + kStages * kTile;  // raw tiles
     uint8_t* rV = rK + G_::kRawK * kHalf;
     float* raw_scales = reinterpret_cast<float*>(rV + G_::kRawV * kHalf);  // [raw K stage][K, V][key]
-    float* scales = raw_scales + G_::kRawK * 2 * kKeys;                    // [tile % 4][K, V][key]
-    uint64_t* k_full = reinterpret_cast<uint64_t*>(scales + G_::kScales / 4);
+    uint64_t* k_full = reinterpret_cast<uint64_t*>(raw_scales + G_::kRawK * 2 * kKeys);
     uint64_t* k_empty = k_full + kStages;   // S of the tile done
     uint64_t* v_full = k_empty + kStages;
     uint64_t* v_empty = v_full + kStages;   // PV of the tile done
@@ -440,8 +510,9 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
     uint64_t* tdown = o_free + 1;
     float* xch = reinterpret_cast<float*>(k_full + G_::kBars);  // [2][128] row max / sum exchange
     int* xok = reinterpret_cast<int*>(xch + 2 * kRows);         // [2][4] "no wait failed"
-    float* vtop = reinterpret_cast<float*>(xok + 8);            // [tile % 4][converting warp] largest value scale
-    int* misc = reinterpret_cast<int*>(vtop + G_::kRing * 4);   // TMEM base, abort
+    float2* tile_ref = reinterpret_cast<float2*>(xok + 8);      // [tile % 4] powers of two of K and V
+    float2* conv_top = tile_ref + G_::kRing;                    // [tile % 4][converting warp] largest scales
+    int* misc = reinterpret_cast<int*>(conv_top + G_::kRing * 4);  // TMEM base, abort
     volatile int* abort = &misc[1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_trigger();
@@ -462,7 +533,7 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
             mbar_init(&rv_empty[i], 128);
         }
         if (kFp8)
-            for (int i = 0; i < G_::kRing; i++) mbar_init(&sc_full[i], 128);
+            for (int i = 0; i < G_::kRing; i++) mbar_init(&sc_full[i], 1);
         mbar_init(s_full, 1);
         mbar_init(s_empty, kSoft);
         for (int i = 0; i < 2; i++) {
@@ -644,13 +715,12 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
         const uint32_t tl = tmem + (static_cast<uint32_t>(qd * 32) << 16);
         // this thread's half of its row's query into Q buffer `part & 1`
         auto load_q = [&](const Walk& x, int part) {
-            const int rows = (x.nodes + 1) * a.G, row = x.qt * kRows + r;
+            const bool in = x.qt * kRows + r < (x.nodes + 1) << a.g_log2;
             uint32_t q[32];
-            const uint4* src = reinterpret_cast<const uint4*>(
-                ta.qr + ((static_cast<long long>(x.s) * a.Hkv + x.head) * (a.B + 1) * a.G + row) * kHeadDim + cb);
+            const uint4* src = ta.qr + ((static_cast<long long>(x.s) * a.Hkv + x.head) * ta.nqt + x.qt) * (16 * kRows) + 8 * wg * kRows + r;
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                const uint4 y = row < rows ? __ldg(src + e) : make_uint4(0u, 0u, 0u, 0u);
+                const uint4 y = in ? __ldcg(src + e * kRows) : make_uint4(0u, 0u, 0u, 0u);
                 q[4 * e] = y.x;
                 q[4 * e + 1] = y.y;
                 q[4 * e + 2] = y.z;
@@ -670,12 +740,12 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
             const bool full_unit = t0 == 0 && t1 == w.tiles;
             const int row = w.qt * kRows + r, b = row >> a.g_log2;
             const bool row_ok = b <= nodes;
-            // m_run: the row's reference; e4m3: vref, a power of two above every value
-            // scale so far, joins it as vshift, so that P = 2^(s - m) / vref * 2^7 times a
-            // scale stays below 2^15 in f16, and 2^-31 of the largest weight still counts
-            float m_run = -INFINITY, l = 0.0f, vref = 0.0f, vshift = 0.0f;
-            float rs = a.sl2;  // scores in log2 units = products (with the keys' scales) * rs
-            if (kFp8 && row_ok) rs = __ldg(ta.q_scale + (static_cast<long long>(s) * a.Hkv + head) * (a.B + 1) * a.G + row);
+            // m_run: the row's reference; e4m3: O is in units of vref, and P has a factor
+            // 2^7 (at most 2^15 in f16), so that 2^-31 of the largest weight still counts
+            constexpr float kBoost = kFp8 ? 7.0f : 0.0f;
+            float m_run = -INFINITY, l = 0.0f, vref = 0.0f;
+            float rs = a.sl2;  // scores in log2 units = products * rs (e4m3: * the tile's power of two of K)
+            if (kFp8 && row_ok) rs = __ldcg(ta.q_scale + ((static_cast<long long>(s) * a.Hkv + head) * ta.nqt + w.qt) * kRows + r);
             for (int t = t0; t < t1; t++, n++) {
                 // visible keys of this row among this warpgroup's 64 of the tile
                 uint64_t vis = row_ok ? ~0ull : 0ull;
@@ -692,8 +762,7 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                 // Both warps of the lane quarter reach both pair barriers of every
                 // iteration and leave the loop at the same point: a failed wait is
                 // exchanged with the row max and acted on after the barriers.
-                const float* ks = scales + (n % G_::kRing) * 2 * kKeys + cb;
-                if (kFp8 && ok && !warp_wait(&sc_full[n % G_::kRing], static_cast<uint32_t>(n / G_::kRing) & 1u, abort)) ok = false;
+                if (kFp8 && ok && !warp_wait<1>(&sc_full[n % G_::kRing], static_cast<uint32_t>(n / G_::kRing) & 1u, abort)) ok = false;
                 if (ok && !warp_wait<1>(s_full, static_cast<uint32_t>(n) & 1u, abort)) ok = false;
                 if (!ok) attn_timeout(a.status, abort);
                 float sv[64];
@@ -703,18 +772,6 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                     tmem_ld64(tl + kSCol + cb, sv);
                     tc_fence_before();
                     mbar_arrive(s_empty);
-                    if (kFp8) {
-#pragma unroll
-                        for (int c = 0; c < 64; c += 4) {
-                            const float4 y = *reinterpret_cast<const float4*>(ks + c);
-                            const float2 u = mul2(make_float2(sv[c], sv[c + 1]), make_float2(y.x, y.y));
-                            const float2 v = mul2(make_float2(sv[c + 2], sv[c + 3]), make_float2(y.z, y.w));
-                            sv[c] = u.x;
-                            sv[c + 1] = u.y;
-                            sv[c + 2] = v.x;
-                            sv[c + 3] = v.y;
-                        }
-                    }
                     if (all_seen) {
 #pragma unroll
                         for (int c = 0; c < 64; c += 2) mx = fmaxf(mx, fmaxf(sv[c], sv[c + 1]));
@@ -733,22 +790,19 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                 ok = ok && xok[(1 - wg) * 4 + qd] != 0;
                 named_bar_sync(pair_bar, 64);  // both read before the next tile's write
                 if (!ok) break;
-                const float mx2 = mx * rs;
-                bool resc = mx2 > m_run + kSlack8;
-                const float m_new = resc ? mx2 : m_run;
-                float shift = vshift;
+                float rt = rs, vnew = 0.0f;
                 if (kFp8) {
-                    const float4 y = *reinterpret_cast<const float4*>(vtop + (n % G_::kRing) * 4);
-                    const float top = fmaxf(fmaxf(y.x, y.y), fmaxf(y.z, y.w));
-                    if (top > vref) {  // (the same in every thread)
-                        const uint32_t ex = min(max(__float_as_uint(top) >> 23, 27u), 252u) + 1u;
-                        vref = __uint_as_float(ex << 23);
-                        shift = static_cast<float>(static_cast<int>(ex) - 127) - 7.0f;
-                        resc = true;
-                    }
+                    const float2 ref = tile_ref[n % G_::kRing];
+                    rt *= ref.x;
+                    vnew = ref.y;
                 }
-                const float alpha = resc ? (m_run == -INFINITY ? 0.0f : ex2((m_run + vshift) - (m_new + shift))) : 1.0f;
-                vshift = shift;
+                const float mx2 = mx * rt;
+                const bool higher = mx2 > m_run + kSlack8;
+                const bool resc = higher || (kFp8 && vnew != vref);  // (vref: the same in every thread)
+                const float m_new = higher ? mx2 : m_run;
+                const float alpha = higher ? ex2(m_run - m_new) : 1.0f;
+                const float alpha_o = kFp8 ? alpha * (vref / vnew) : alpha;
+                vref = vnew;
                 // P buffer n & 1 was last read by PV(n - 2); O must be stable (PV(n - 1)
                 // done) only when it is rescaled.  On a timeout this tile is
                 // skipped; the pair leaves the loop together at the next exchange.
@@ -770,7 +824,7 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                         float o[16];
                         tmem_ld16(tl + kOCol + cb + c0, o);
 #pragma unroll
-                        for (int e = 0; e < 16; e++) o[e] *= alpha;
+                        for (int e = 0; e < 16; e++) o[e] *= alpha_o;
                         tmem_st16(tl + kOCol + cb + c0, o);
                     }
                     tmem_wait_st();
@@ -779,22 +833,17 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                 m_run = m_new;
                 // P = 2^(s - m) as bf16 pairs; hidden keys hold -inf and give 0 (so does
                 // every key of a row that has seen no visible key: m = -inf)
-                const float nm = m_run == -INFINITY ? 0.0f : -(m_run + vshift);
+                const float nm = m_run == -INFINITY ? 0.0f : kBoost - m_run;
                 float2 sum0 = make_float2(0.0f, 0.0f), sum1 = sum0;
                 uint32_t pk[32];
 #pragma unroll
                 for (int c = 0; c < 64; c += 4) {
-                    float2 x = fma2(make_float2(sv[c], sv[c + 1]), make_float2(rs, rs), make_float2(nm, nm));
-                    float2 z = fma2(make_float2(sv[c + 2], sv[c + 3]), make_float2(rs, rs), make_float2(nm, nm));
+                    float2 x = fma2(make_float2(sv[c], sv[c + 1]), make_float2(rt, rt), make_float2(nm, nm));
+                    float2 z = fma2(make_float2(sv[c + 2], sv[c + 3]), make_float2(rt, rt), make_float2(nm, nm));
                     x = make_float2(ex2(x.x), ex2(x.y));
                     z = make_float2(ex2(z.x), ex2(z.y));
                     sum0 = add2(sum0, x);
                     sum1 = add2(sum1, z);
-                    if (kFp8) {
-                        const float4 y = *reinterpret_cast<const float4*>(ks + kKeys + c);
-                        x = mul2(x, make_float2(y.x, y.y));
-                        z = mul2(z, make_float2(y.z, y.w));
-                    }
                     pk[c >> 1] = kFp8 ? pack_f16x2(x.x, x.y) : pack_bf16x2(x.x, x.y);
                     pk[(c >> 1) + 1] = kFp8 ? pack_f16x2(z.x, z.y) : pack_bf16x2(z.x, z.y);
                 }
@@ -829,61 +878,96 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
             tmem_ld64(tl + kOCol + cb, o);
             tc_fence_before();
             mbar_arrive(o_free);
-            if (row_ok) {
-                if (full_unit) {
-                    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-                    uint4* d = reinterpret_cast<uint4*>(a.out + ((static_cast<long long>(s) * (a.B + 1) + b) * a.Hq + head * a.G + (row & (a.G - 1))) * kHeadDim + cb);
+            if (full_unit) {
+                // rows in whole lines: 8 lanes exchange their rows' 8 pieces
+                const float inv = l > 0.0f ? (kFp8 ? vref : 1.0f) / l : 0.0f;
+                uint4 y[8];
 #pragma unroll
-                    for (int e = 0; e < 8; e++)
-                        d[e] = make_uint4(pack_bf16x2(o[8 * e] * inv, o[8 * e + 1] * inv), pack_bf16x2(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
-                                          pack_bf16x2(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_bf16x2(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
-                } else {
-                    TilePart* d = static_cast<TilePart*>(a.parts) + 2 * blockIdx.x + (t0 > 0 ? 0 : 1);
-                    float4* dst = reinterpret_cast<float4*>(&d->o[r][cb]);
+                for (int e = 0; e < 8; e++)
+                    y[e] = make_uint4(pack_bf16x2(o[8 * e] * inv, o[8 * e + 1] * inv), pack_bf16x2(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
+                                      pack_bf16x2(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_bf16x2(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+                transpose8(y, lane);
 #pragma unroll
-                    for (int e = 0; e < 16; e++) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-                    if (wg == 0) d->ml[r] = make_float2(m_run + vshift, l);
+                for (int e = 0; e < 8; e++) {
+                    const int their = row - (lane & 7) + e, tb = their >> a.g_log2;  // row of lane 8 (lane / 8) + e
+                    if (tb <= nodes)
+                        reinterpret_cast<uint4*>(a.out + ((static_cast<long long>(s) * (a.B + 1) + tb) * a.Hq + head * a.G + (their & (a.G - 1))) * kHeadDim + cb)[lane & 7] = y[e];
                 }
+            } else if (row_ok) {
+                TilePart* d = reinterpret_cast<TilePart*>(a.parts) + 2 * blockIdx.x + (t0 > 0 ? 0 : 1);
+#pragma unroll
+                for (int e = 0; e < 16; e++) {
+                    const float by = kFp8 ? vref : 1.0f;
+                    d->o[wg * 16 + e][r] = make_float4(o[4 * e] * by, o[4 * e + 1] * by, o[4 * e + 2] * by, o[4 * e + 3] * by);
+                }
+                if (wg == 0) d->ml[r] = make_float2(m_run, l);
             }
         }
-    } else {
+    } else if constexpr (kFp8) {
         // ---------------------------------------------------------- raw tiles to operands (e4m3): a thread per key
         reg_less<kRegsConvert>();
         const int key = threadIdx.x - (G_::kFirstSoft + 8) * 32;
-        bool ok = true, waited = false;
+        bool ok = true, stop = false, waited = false;
         int n = 0, raw = 0;  // tiles, whole cache tiles so far
-        while (ok && w.next(a)) {
-            for (int t = w.t0; t < w.t1 && ok; t++, n++) {
+        // The four warps meet at a barrier in every tile, so they leave together: one
+        // whose wait failed says so at the next tile's.
+        while (!stop && w.next(a)) {
+            float vref = 0.0f;  // of the part's tiles so far
+            for (int t = w.t0; t < w.t1; t++, n++) {
                 const bool cache_tile = t < w.whole;
                 if (!cache_tile && !waited) {
                     pdl_wait();
                     waited = true;
                 }
-                const int st = n % kStages;
-                float* sc = scales + (n % G_::kRing) * 2 * kKeys;
+                const int st = n % kStages, rk = raw % G_::kRawK, rv = raw % G_::kRawV;
+                const long long side = (static_cast<long long>(w.s) * a.Hkv + w.head) * ta.sk + (t - w.whole) * kKeys + key;
+                if (ok && cache_tile && !warp_wait(&rk_full[rk], static_cast<uint32_t>(raw / G_::kRawK) & 1u, abort)) ok = false;
+                const float ks = cache_tile ? raw_scales[rk * 2 * kKeys + key] : __ldcg(ta.side_ks + side);
+                const float vs = cache_tile ? raw_scales[rk * 2 * kKeys + kKeys + key] : __ldcg(ta.side_vs + side);
+                float2 top = make_float2(__uint_as_float(__reduce_max_sync(kFull, __float_as_uint(fmaxf(ks, 0.0f)))),
+                                         __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(fmaxf(vs, 0.0f)))));
+                if (!ok) top.x = -1.0f;
+                if (lane == 0) conv_top[(n % G_::kRing) * 4 + (warp & 3)] = top;
+                named_bar_sync(kConvBar, 128);
+                float low = top.x;
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const float2 x = conv_top[(n % G_::kRing) * 4 + i];
+                    low = fminf(low, x.x);
+                    top = make_float2(fmaxf(top.x, x.x), fmaxf(top.y, x.y));
+                }
+                if (low < 0.0f) {
+                    ok = false;
+                    stop = true;
+                    break;
+                }
+                const float kref = above(top.x);
+                vref = fmaxf(vref, above(top.y));
+                if (key == 0) {
+                    tile_ref[n % G_::kRing] = make_float2(kref, vref);
+                    mbar_arrive(&sc_full[n % G_::kRing]);
+                }
                 for (int kv = 0; kv < 2 && ok; kv++) {
-                    const int stages = kv ? G_::kRawV : G_::kRawK, rs = cache_tile ? raw % stages : 0;
+                    const float ratio = kv ? vs / vref : ks / kref;  // at most 1
+                    const __half hi = __float2half_rn(ratio);
+                    const __half2 by = __half2half2(hi), rest = __half2half2(__float2half_rn(ratio - __half2float(hi)));
+                    // codes * ratio, rounded once to f16
+                    auto times = [&](uint32_t x) {
+                        const __half2 c = *reinterpret_cast<const __half2*>(&x);
+                        const __half2 r = __hfma2(c, by, __hmul2(c, rest));
+                        return *reinterpret_cast<const uint32_t*>(&r);
+                    };
+                    auto times4 = [&](uint32_t x, uint32_t y, uint32_t z, uint32_t w4) { return make_uint4(times(x), times(y), times(z), times(w4)); };
                     uint4 x[8];
                     if (cache_tile) {
-                        if (!warp_wait(&(kv ? rv_full : rk_full)[rs], static_cast<uint32_t>(raw / stages) & 1u, abort)) {
+                        if (kv && !warp_wait(&rv_full[rv], static_cast<uint32_t>(raw / G_::kRawV) & 1u, abort)) {
                             ok = false;
                             break;
                         }
-                        const uint8_t* src = (kv ? rV : rK) + rs * kHalf;
+                        const uint8_t* src = kv ? rV + rv * kHalf : rK + rk * kHalf;
 #pragma unroll
                         for (int c = 0; c < 8; c++) x[c] = *reinterpret_cast<const uint4*>(src + tile_swz(key, c));
                     }
-                    const long long side = (static_cast<long long>(w.s) * a.Hkv + w.head) * ta.sk + (t - w.whole) * kKeys + key;
-                    if (kv == 0) {
-                        const float vsc = cache_tile ? raw_scales[rs * 2 * kKeys + kKeys + key] : __ldg(ta.side_vs + side);
-                        sc[key] = cache_tile ? raw_scales[rs * 2 * kKeys + key] : __ldg(ta.side_ks + side);
-                        sc[kKeys + key] = vsc;
-                        const float top = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(fmaxf(vsc, 0.0f))));
-                        if (lane == 0) vtop[(n % G_::kRing) * 4 + (warp & 3)] = top;
-                        __syncwarp();
-                        mbar_arrive(&sc_full[n % G_::kRing]);
-                    }
-                    if (cache_tile) mbar_arrive(&(kv ? rv_empty : rk_empty)[rs]);
                     if (!warp_wait(&(kv ? v_empty : k_empty)[st], (static_cast<uint32_t>(n / kStages) & 1u) ^ 1u, abort)) {
                         ok = false;
                         break;
@@ -892,30 +976,26 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                     if (cache_tile) {
 #pragma unroll
                         for (int c = 0; c < 8; c++) {
-                            const uint32_t u[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
-                            uint32_t y[8];
-#pragma unroll
-                            for (int e = 0; e < 4; e++) {
-                                y[2 * e] = codes_to_f16(u[e]);
-                                y[2 * e + 1] = codes_to_f16(u[e] >> 16);
-                            }
                             uint8_t* d = dst + (c >> 2) * kHalf;
-                            *reinterpret_cast<uint4*>(d + tile_swz(key, (2 * c) & 7)) = make_uint4(y[0], y[1], y[2], y[3]);
-                            *reinterpret_cast<uint4*>(d + tile_swz(key, (2 * c + 1) & 7)) = make_uint4(y[4], y[5], y[6], y[7]);
+                            *reinterpret_cast<uint4*>(d + tile_swz(key, (2 * c) & 7)) =
+                                times4(codes_to_f16(x[c].x), codes_to_f16(x[c].x >> 16), codes_to_f16(x[c].y), codes_to_f16(x[c].y >> 16));
+                            *reinterpret_cast<uint4*>(d + tile_swz(key, (2 * c + 1) & 7)) =
+                                times4(codes_to_f16(x[c].z), codes_to_f16(x[c].z >> 16), codes_to_f16(x[c].w), codes_to_f16(x[c].w >> 16));
                         }
                     } else {
-                        const uint4* src = reinterpret_cast<const uint4*>((kv ? ta.side_v : ta.side_k) + side * kHeadDim);
+                        const uint4* src = (kv ? ta.side_v : ta.side_k) + (side >> 7) * (16 * kKeys) + key;
 #pragma unroll
                         for (int h = 0; h < 2; h++) {
-                            uint4 y[8];
 #pragma unroll
-                            for (int c = 0; c < 8; c++) y[c] = __ldg(src + 8 * h + c);
+                            for (int c = 0; c < 8; c++) x[c] = __ldcg(src + (8 * h + c) * kKeys);
 #pragma unroll
-                            for (int c = 0; c < 8; c++) *reinterpret_cast<uint4*>(dst + h * kHalf + tile_swz(key, c)) = y[c];
+                            for (int c = 0; c < 8; c++)
+                                *reinterpret_cast<uint4*>(dst + h * kHalf + tile_swz(key, c)) = times4(x[c].x, x[c].y, x[c].z, x[c].w);
                         }
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the MMAs read it
                     mbar_arrive(&(kv ? v_full : k_full)[st]);
+                    if (cache_tile) mbar_arrive(kv ? &rv_empty[rv] : &rk_empty[rk]);  // (what was read from it is in use)
                 }
                 if (cache_tile) raw++;
             }
@@ -949,7 +1029,7 @@ __global__ void __launch_bounds__(256) paged_tiles_join_kernel(const __grid_cons
     p.load(a);
     const int tiles = p.tiles(a, p.qt), s = p.s, head = p.head;
     if (at.z >= tiles) return;  // (the unit ended in share i - 1)
-    const int r = eighth * 16 + (tid >> 4), d8 = tid & 15, row = p.qt * kRows + r, b = row >> a.g_log2;
+    const int r = eighth * 16 + (tid & 15), d8 = tid >> 4, row = p.qt * kRows + r, b = row >> a.g_log2;
     if (b > p.nodes) return;
     auto in_unit = [&](int c) {
         if (c >= count) return false;
@@ -963,7 +1043,7 @@ __global__ void __launch_bounds__(256) paged_tiles_join_kernel(const __grid_cons
     for (int c = c0; c <= c1; c++) {
         const TilePart* x = static_cast<const TilePart*>(a.parts) + 2 * c + (c < i ? 1 : 0);
         const float2 ml = x->ml[r];
-        const float4 y = *reinterpret_cast<const float4*>(&x->o[r][8 * d8]), z = *reinterpret_cast<const float4*>(&x->o[r][8 * d8 + 4]);
+        const float4 y = x->o[2 * d8][r], z = x->o[2 * d8 + 1][r];
         if (ml.x == -INFINITY) continue;
         const float up = fmaxf(top, ml.x), old = top == -INFINITY ? 0.0f : ex2(top - up), by = ex2(ml.x - up);
         top = up;
@@ -984,15 +1064,16 @@ struct TileWs {
     size_t q, k, v, qs, ks, vs, total;
 };
 TileWs tile_ws(int nseq, int B, int Hq, int Hkv) {
+    const size_t q_rows = static_cast<size_t>(nseq) * Hkv * (((B + 1) * (Hq / Hkv) + kRows - 1) / kRows) * kRows;
     TileWs w;
     w.sk = (kKeys - 1 + B + 1 + kKeys - 1) / kKeys * kKeys;
     auto up = [](size_t n) { return (n + 255) & ~static_cast<size_t>(255); };
     const size_t side = up(static_cast<size_t>(nseq) * Hkv * w.sk * kHeadDim * 2);
     w.q = up(sizeof(SharePlan) + sizeof(TilePart) * 2 * kMaxSms);
-    w.k = w.q + up(static_cast<size_t>(nseq) * (B + 1) * Hq * kHeadDim * 2);
+    w.k = w.q + up(q_rows * kHeadDim * 2);
     w.v = w.k + side;
     w.qs = w.v + side;
-    w.ks = w.qs + up(static_cast<size_t>(nseq) * (B + 1) * Hq * 4);
+    w.ks = w.qs + up(q_rows * 4);
     w.vs = w.ks + up(static_cast<size_t>(nseq) * Hkv * w.sk * 4);
     w.total = w.vs + up(static_cast<size_t>(nseq) * Hkv * w.sk * 4);
     return w;
@@ -1015,9 +1096,10 @@ int launch_paged_tiles(PagedArgs a, const dart_kv_cache& cache, uint8_t* workspa
     TileArgs ta{};
     ta.p = a;
     ta.sk = w.sk;
-    ta.qr = reinterpret_cast<uint16_t*>(workspace + w.q);
-    ta.side_k = reinterpret_cast<uint16_t*>(workspace + w.k);
-    ta.side_v = reinterpret_cast<uint16_t*>(workspace + w.v);
+    ta.nqt = ((a.B + 1) * a.G + kRows - 1) / kRows;
+    ta.qr = reinterpret_cast<uint4*>(workspace + w.q);
+    ta.side_k = reinterpret_cast<uint4*>(workspace + w.k);
+    ta.side_v = reinterpret_cast<uint4*>(workspace + w.v);
     ta.q_scale = reinterpret_cast<float*>(workspace + w.qs);
     ta.side_ks = reinterpret_cast<float*>(workspace + w.ks);
     ta.side_vs = reinterpret_cast<float*>(workspace + w.vs);
@@ -1026,10 +1108,10 @@ int launch_paged_tiles(PagedArgs a, const dart_kv_cache& cache, uint8_t* workspa
     if (!encode_rows(&tmK, cache.k, a.pool_rows, fp8, cache.page_size) || !encode_rows(&tmV, cache.v, a.pool_rows, fp8, cache.page_size) ||
         !encode_rows(&tmSk, ta.side_k, side_rows, false, kKeys) || !encode_rows(&tmSv, ta.side_v, side_rows, false, kKeys))
         return DART_ERR_CUDA;
-    const dim3 prep(static_cast<unsigned>((side_rows + 7) / 8));
+    const dim3 prep(static_cast<unsigned>(a.nseq), static_cast<unsigned>(w.sk));
     const uint8_t *pk = static_cast<const uint8_t*>(cache.k), *pv = static_cast<const uint8_t*>(cache.v);
-    cudaError_t e = fp8 ? launch_pdl(paged_prep_kernel<true>, prep, dim3(256), 0, st, ta, pk, pv)
-                        : launch_pdl(paged_prep_kernel<false>, prep, dim3(256), 0, st, ta, pk, pv);
+    cudaError_t e = fp8 ? launch_pdl(paged_prep_kernel<true>, prep, dim3(kPrepThreads), 0, st, ta, pk, pv)
+                        : launch_pdl(paged_prep_kernel<false>, prep, dim3(kPrepThreads), 0, st, ta, pk, pv);
     if (e != cudaSuccess) return DART_ERR_CUDA;
     e = fp8 ? launch_pdl(paged_tiles_kernel<true>, dim3(sms), dim3(TGeo<true>::kThreads), TGeo<true>::kSmem, st, tmK, tmV, tmSk, tmSv, ta)
             : launch_pdl(paged_tiles_kernel<false>, dim3(sms), dim3(TGeo<false>::kThreads), TGeo<false>::kSmem, st, tmK, tmV, tmSk, tmSv, ta);

@@ -161,6 +161,20 @@ def test_every_call_gives_the_same_bits(dart):
         assert torch.equal(run(dart, x), run(dart, x))
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+def test_many_calls_give_the_same_bits(dart, fp8):
+    """Hundreds of calls of a shape whose shares switch from cache tiles to tree
+    tiles early, where a slot freed too soon would be refilled under its reader."""
+    x = sd.attn_data(2, 1024, [700, 2000], 64, fp8, 8, 2, 7101, fill=0.97)
+    att = dart.PagedTreeAttention(dart.KVCache(*x.pool), 2, x.B, x.max_pages, 8, rope_theta=THETA)
+    first = None
+    for _ in range(300):
+        out = att(*x.dev, x.table, x.d_lens, *x.tree)
+        torch.cuda.synchronize()
+        first = out.clone() if first is None else first
+        assert torch.equal(out, first)
+
+
 def test_split_does_not_show(dart):
     """One sequence alone (its keys shared by all SMs) and among 60 others
     (many sequences to an SM): the same result within two roundings."""
