@@ -53,7 +53,7 @@ constexpr int kHalf = kKeys * 128;       // 128 rows of one 128-byte swizzle col
 constexpr int kTile = 2 * kHalf;         // 128 keys of bf16
 constexpr int kSoft = 256;               // softmax threads
 constexpr int kPairBar = 2;              // named barriers 2 .. 5
-constexpr int kConvBar = 6;
+constexpr int kConvBar = 6;              // 6: the warps that convert K, 7: V
 constexpr float kSlack8 = 8.0f;          // log2 units: P <= 2^8 between rescales
 // What a unit costs beside its tiles (its queries, its result, the pause between
 // its last tile and the next unit's first), in tiles: eight trees of 512 nodes over
@@ -382,7 +382,7 @@ struct Walk {
 // Registers move between warpgroups, out of the 4 x 128 a thread that the
 // e4m3 kernel is launched with (128 are too few for the softmax's 64 scores a
 // thread).
-constexpr int kRegsIssue = 88, kRegsSoft = 168, kRegsConvert = 88;
+constexpr int kRegsIssue = 96, kRegsSoft = 160, kRegsConvert = 96;
 static_assert(kRegsIssue + 2 * kRegsSoft + kRegsConvert <= 4 * 128, "more than the launch has");
 template <int kRegs>
 __device__ __forceinline__ void reg_less() {
@@ -433,9 +433,9 @@ struct TGeo {
     static constexpr int kRing = 4;  // a tile's factors outlive its operands
     static constexpr int kOps = 2 * kStages * kTile;
     static constexpr int kRaw = (kRawK + kRawV) * kHalf;
-    static constexpr int kRawScales = kRawK * 2 * kKeys * 4;
+    static constexpr int kRawScales = (kRawK + kRawV) * kKeys * 4;
     static constexpr int kBars = 4 * kStages + 2 * (kRawK + kRawV) + (kFp8 ? kRing : 0) + 9 + 1;
-    static constexpr int kExchange = 2 * kRows * 4 + 8 * 4 + kRing * 8 + kRing * 4 * 8;
+    static constexpr int kExchange = 2 * kRows * 4 + 8 * 4 + kRing * 8 + kRing * 4 * 4;
     static constexpr int kSmem = kOps + kRaw + kRawScales + kBars * 8 + kExchange + 16;
     // e4m3: warpgroups (producer, MMA, two idle warps), softmax, softmax, converters
     static constexpr int kThreads = kFp8 ? 512 : 64 + kSoft;
@@ -491,8 +491,8 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
     uint8_t* sV = sK + kStages * kTile;
     uint8_t* rK = sV + kStages * kTile;  // raw tiles
     uint8_t* rV = rK + G_::kRawK * kHalf;
-    float* raw_scales = reinterpret_cast<float*>(rV + G_::kRawV * kHalf);  // [raw K stage][K, V][key]
-    uint64_t* k_full = reinterpret_cast<uint64_t*>(raw_scales + G_::kRawK * 2 * kKeys);
+    float* raw_scales = reinterpret_cast<float*>(rV + G_::kRawV * kHalf);  // [raw K stages, raw V stages][key]
+    uint64_t* k_full = reinterpret_cast<uint64_t*>(raw_scales + (G_::kRawK + G_::kRawV) * kKeys);
     uint64_t* k_empty = k_full + kStages;   // S of the tile done
     uint64_t* v_full = k_empty + kStages;
     uint64_t* v_empty = v_full + kStages;   // PV of the tile done
@@ -511,29 +511,29 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
     float* xch = reinterpret_cast<float*>(k_full + G_::kBars);  // [2][128] row max / sum exchange
     int* xok = reinterpret_cast<int*>(xch + 2 * kRows);         // [2][4] "no wait failed"
     float2* tile_ref = reinterpret_cast<float2*>(xok + 8);      // [tile % 4] powers of two of K and V
-    float2* conv_top = tile_ref + G_::kRing;                    // [tile % 4][converting warp] largest scales
-    int* misc = reinterpret_cast<int*>(conv_top + G_::kRing * 4);  // TMEM base, abort
+    float* conv_top = reinterpret_cast<float*>(tile_ref + G_::kRing);  // [K, V][tile % 4][warp] largest scales
+    int* misc = reinterpret_cast<int*>(conv_top + 4 * G_::kRing);      // TMEM base, abort
     volatile int* abort = &misc[1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_trigger();
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; i++) {
-            mbar_init(&k_full[i], kFp8 ? 128 : 1);
+            mbar_init(&k_full[i], kFp8 ? 64 : 1);
             mbar_init(&k_empty[i], 1);
-            mbar_init(&v_full[i], kFp8 ? 128 : 1);
+            mbar_init(&v_full[i], kFp8 ? 64 : 1);
             mbar_init(&v_empty[i], 1);
         }
         for (int i = 0; i < G_::kRawK; i++) {
             mbar_init(&rk_full[i], 1);
-            mbar_init(&rk_empty[i], 128);
+            mbar_init(&rk_empty[i], 64);
         }
         for (int i = 0; i < G_::kRawV; i++) {
             mbar_init(&rv_full[i], 1);
-            mbar_init(&rv_empty[i], 128);
+            mbar_init(&rv_empty[i], 64);
         }
         if (kFp8)
-            for (int i = 0; i < G_::kRing; i++) mbar_init(&sc_full[i], 1);
+            for (int i = 0; i < G_::kRing; i++) mbar_init(&sc_full[i], 2);
         mbar_init(s_full, 1);
         mbar_init(s_empty, kSoft);
         for (int i = 0; i < 2; i++) {
@@ -617,7 +617,7 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                     ok = warp_wait<kWaitPolls>(empty, (static_cast<uint32_t>(n / stages) & 1u) ^ 1u, abort);
                     if (!ok) break;
                     if (lane == 0)
-                        mbar_arrive_expect_tx(full, kFp8 ? kHalf + (kv ? 0 : 2 * kKeys * 4) : kTile);
+                        mbar_arrive_expect_tx(full, kFp8 ? kHalf + kKeys * 4 : kTile);
                     __syncwarp();
                     if (!cache_tile) {
                         if (lane < 2)
@@ -626,11 +626,9 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                         const uint32_t at = static_cast<uint32_t>(lane << a.page_log2) * 128;
                         tma_load_2d(dst + at, tm, full, 0, static_cast<int>(row), policy);
                         if (!kFp8) tma_load_2d(dst + kHalf + at, tm, full, 64, static_cast<int>(row), policy);
-                        if (kFp8 && kv == 0) {
+                        if (kFp8) {
                             const long long sr = row < a.pool_rows ? row : 0;
-                            float* sc = raw_scales + st * 2 * kKeys + (lane << a.page_log2);
-                            bulk_load(sc, a.ks + sr, 4u << a.page_log2, full);
-                            bulk_load(sc + kKeys, a.vs + sr, 4u << a.page_log2, full);
+                            bulk_load(raw_scales + (kv * G_::kRawK + st) * kKeys + (lane << a.page_log2), (kv ? a.vs : a.ks) + sr, 4u << a.page_log2, full);
                         }
                     }
                 }
@@ -766,8 +764,13 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                 if (ok && !warp_wait<1>(s_full, static_cast<uint32_t>(n) & 1u, abort)) ok = false;
                 if (!ok) attn_timeout(a.status, abort);
                 float sv[64];
-                float mx = -INFINITY;
+                float mx = -INFINITY, rt = rs, vnew = 0.0f;
                 if (ok) {
+                    if (kFp8) {  // (before s_empty: after S(n + 1) the place may be written again)
+                        const float2 ref = tile_ref[n % G_::kRing];
+                        rt *= ref.x;
+                        vnew = ref.y;
+                    }
                     tc_fence_after();
                     tmem_ld64(tl + kSCol + cb, sv);
                     tc_fence_before();
@@ -790,12 +793,6 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                 ok = ok && xok[(1 - wg) * 4 + qd] != 0;
                 named_bar_sync(pair_bar, 64);  // both read before the next tile's write
                 if (!ok) break;
-                float rt = rs, vnew = 0.0f;
-                if (kFp8) {
-                    const float2 ref = tile_ref[n % G_::kRing];
-                    rt *= ref.x;
-                    vnew = ref.y;
-                }
                 const float mx2 = mx * rt;
                 const bool higher = mx2 > m_run + kSlack8;
                 const bool resc = higher || (kFp8 && vnew != vref);  // (vref: the same in every thread)
@@ -906,98 +903,104 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
     } else if constexpr (kFp8) {
         // ---------------------------------------------------------- raw tiles to operands (e4m3): a thread per key
         reg_less<kRegsConvert>();
-        const int key = threadIdx.x - (G_::kFirstSoft + 8) * 32;
+        // Two warps for K, two for V, on their own; a thread takes keys `key` and key + 64.
+        const int cw = warp - (G_::kFirstSoft + 8), kv = cw >> 1, key = (cw & 1) * 32 + lane;
+        uint64_t* raw_full = kv ? rv_full : rk_full;
+        uint64_t* raw_empty = kv ? rv_empty : rk_empty;
+        uint64_t* op_full = kv ? v_full : k_full;
+        uint64_t* op_empty = kv ? v_empty : k_empty;
+        const uint8_t* raw_tile = kv ? rV : rK;
+        uint8_t* op_tile = kv ? sV : sK;
+        const int raw_stages = kv ? G_::kRawV : G_::kRawK;
+        const float* side_scale = kv ? ta.side_vs : ta.side_ks;
+        const uint4* side_rows = kv ? ta.side_v : ta.side_k;
+        float* pair_top = conv_top + kv * 2 * G_::kRing;
         bool ok = true, stop = false, waited = false;
         int n = 0, raw = 0;  // tiles, whole cache tiles so far
-        // The four warps meet at a barrier in every tile, so they leave together: one
-        // whose wait failed says so at the next tile's.
+        // The two warps meet at a barrier in every tile, so they leave together: one whose
+        // wait failed says so at the next tile's.
         while (!stop && w.next(a)) {
-            float vref = 0.0f;  // of the part's tiles so far
+            float vref = 0.0f;  // (V) of the part's tiles so far
             for (int t = w.t0; t < w.t1; t++, n++) {
                 const bool cache_tile = t < w.whole;
                 if (!cache_tile && !waited) {
                     pdl_wait();
                     waited = true;
                 }
-                const int st = n % kStages, rk = raw % G_::kRawK, rv = raw % G_::kRawV;
+                const int st = n % kStages, rs = raw % raw_stages;
                 const long long side = (static_cast<long long>(w.s) * a.Hkv + w.head) * ta.sk + (t - w.whole) * kKeys + key;
-                if (ok && cache_tile && !warp_wait(&rk_full[rk], static_cast<uint32_t>(raw / G_::kRawK) & 1u, abort)) ok = false;
-                const float ks = cache_tile ? raw_scales[rk * 2 * kKeys + key] : __ldcg(ta.side_ks + side);
-                const float vs = cache_tile ? raw_scales[rk * 2 * kKeys + kKeys + key] : __ldcg(ta.side_vs + side);
-                float2 top = make_float2(__uint_as_float(__reduce_max_sync(kFull, __float_as_uint(fmaxf(ks, 0.0f)))),
-                                         __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(fmaxf(vs, 0.0f)))));
-                if (!ok) top.x = -1.0f;
-                if (lane == 0) conv_top[(n % G_::kRing) * 4 + (warp & 3)] = top;
-                named_bar_sync(kConvBar, 128);
-                float low = top.x;
+                if (ok && cache_tile && !warp_wait(&raw_full[rs], static_cast<uint32_t>(raw / raw_stages) & 1u, abort)) ok = false;
+                float sc[2];
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const float2 x = conv_top[(n % G_::kRing) * 4 + i];
-                    low = fminf(low, x.x);
-                    top = make_float2(fmaxf(top.x, x.x), fmaxf(top.y, x.y));
-                }
-                if (low < 0.0f) {
+                for (int h = 0; h < 2; h++)
+                    sc[h] = cache_tile ? raw_scales[(kv * G_::kRawK + rs) * kKeys + key + 64 * h] : __ldcg(side_scale + side + 64 * h);
+                const float mine = fmaxf(fmaxf(sc[0], sc[1]), 0.0f);
+                float top = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(mine)));
+                if (lane == 0) pair_top[(n % G_::kRing) * 2 + (cw & 1)] = ok ? top : -1.0f;
+                named_bar_sync(kConvBar + kv, 64);
+                const float2 both = *reinterpret_cast<const float2*>(pair_top + (n % G_::kRing) * 2);
+                if (fminf(both.x, both.y) < 0.0f) {
                     ok = false;
                     stop = true;
                     break;
                 }
-                const float kref = above(top.x);
-                vref = fmaxf(vref, above(top.y));
+                float ref = above(fmaxf(both.x, both.y));
+                if (kv) ref = vref = fmaxf(vref, ref);
                 if (key == 0) {
-                    tile_ref[n % G_::kRing] = make_float2(kref, vref);
+                    (kv ? tile_ref[n % G_::kRing].y : tile_ref[n % G_::kRing].x) = ref;
                     mbar_arrive(&sc_full[n % G_::kRing]);
                 }
-                for (int kv = 0; kv < 2 && ok; kv++) {
-                    const float ratio = kv ? vs / vref : ks / kref;  // at most 1
-                    const __half hi = __float2half_rn(ratio);
-                    const __half2 by = __half2half2(hi), rest = __half2half2(__float2half_rn(ratio - __half2float(hi)));
-                    // codes * ratio, rounded once to f16
+                if (!warp_wait(&op_empty[st], (static_cast<uint32_t>(n / kStages) & 1u) ^ 1u, abort)) {
+                    ok = false;
+                    if (cache_tile) raw++;
+                    continue;
+                }
+                const float inv = __uint_as_float(0x7F000000u - __float_as_uint(ref));  // 1 / ref
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    // the key's scale over the common power of two, at most 1, rounded to f16: that
+                    // moves the key's scores or its values by 2^-12 of themselves at most, as
+                    // much as the rounding of an operand does
+                    const __half2 by = __float2half2_rn(sc[h] * inv);
                     auto times = [&](uint32_t x) {
-                        const __half2 c = *reinterpret_cast<const __half2*>(&x);
-                        const __half2 r = __hfma2(c, by, __hmul2(c, rest));
+                        const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&x), by);
                         return *reinterpret_cast<const uint32_t*>(&r);
                     };
-                    auto times4 = [&](uint32_t x, uint32_t y, uint32_t z, uint32_t w4) { return make_uint4(times(x), times(y), times(z), times(w4)); };
+                    const int row = key + 64 * h;
+                    uint8_t* dst = op_tile + st * kTile;
                     uint4 x[8];
                     if (cache_tile) {
-                        if (kv && !warp_wait(&rv_full[rv], static_cast<uint32_t>(raw / G_::kRawV) & 1u, abort)) {
-                            ok = false;
-                            break;
-                        }
-                        const uint8_t* src = kv ? rV + rv * kHalf : rK + rk * kHalf;
+                        const uint8_t* src = raw_tile + rs * kHalf;
 #pragma unroll
-                        for (int c = 0; c < 8; c++) x[c] = *reinterpret_cast<const uint4*>(src + tile_swz(key, c));
-                    }
-                    if (!warp_wait(&(kv ? v_empty : k_empty)[st], (static_cast<uint32_t>(n / kStages) & 1u) ^ 1u, abort)) {
-                        ok = false;
-                        break;
-                    }
-                    uint8_t* dst = (kv ? sV : sK) + st * kTile;
-                    if (cache_tile) {
+                        for (int c = 0; c < 8; c++) x[c] = *reinterpret_cast<const uint4*>(src + tile_swz(row, c));
 #pragma unroll
                         for (int c = 0; c < 8; c++) {
                             uint8_t* d = dst + (c >> 2) * kHalf;
-                            *reinterpret_cast<uint4*>(d + tile_swz(key, (2 * c) & 7)) =
-                                times4(codes_to_f16(x[c].x), codes_to_f16(x[c].x >> 16), codes_to_f16(x[c].y), codes_to_f16(x[c].y >> 16));
-                            *reinterpret_cast<uint4*>(d + tile_swz(key, (2 * c + 1) & 7)) =
-                                times4(codes_to_f16(x[c].z), codes_to_f16(x[c].z >> 16), codes_to_f16(x[c].w), codes_to_f16(x[c].w >> 16));
+                            *reinterpret_cast<uint4*>(d + tile_swz(row, (2 * c) & 7)) =
+                                make_uint4(times(codes_to_f16(x[c].x)), times(codes_to_f16(x[c].x >> 16)), times(codes_to_f16(x[c].y)), times(codes_to_f16(x[c].y >> 16)));
+                            *reinterpret_cast<uint4*>(d + tile_swz(row, (2 * c + 1) & 7)) =
+                                make_uint4(times(codes_to_f16(x[c].z)), times(codes_to_f16(x[c].z >> 16)), times(codes_to_f16(x[c].w)), times(codes_to_f16(x[c].w >> 16)));
                         }
                     } else {
-                        const uint4* src = (kv ? ta.side_v : ta.side_k) + (side >> 7) * (16 * kKeys) + key;
+                        const uint4* src = side_rows + (side >> 7) * (16 * kKeys) + row;
 #pragma unroll
-                        for (int h = 0; h < 2; h++) {
+                        for (int q = 0; q < 2; q++) {
 #pragma unroll
-                            for (int c = 0; c < 8; c++) x[c] = __ldcg(src + (8 * h + c) * kKeys);
+                            for (int c = 0; c < 8; c++) x[c] = __ldcg(src + (8 * q + c) * kKeys);
 #pragma unroll
                             for (int c = 0; c < 8; c++)
-                                *reinterpret_cast<uint4*>(dst + h * kHalf + tile_swz(key, c)) = times4(x[c].x, x[c].y, x[c].z, x[c].w);
+                                *reinterpret_cast<uint4*>(dst + q * kHalf + tile_swz(row, c)) = make_uint4(times(x[c].x), times(x[c].y), times(x[c].z), times(x[c].w));
                         }
                     }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the MMAs read it
-                    mbar_arrive(&(kv ? v_full : k_full)[st]);
-                    if (cache_tile) mbar_arrive(kv ? &rv_empty[rv] : &rk_empty[rk]);  // (what was read from it is in use)
                 }
-                if (cache_tile) raw++;
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the MMAs read it
+                mbar_arrive(&op_full[st]);
+                if (cache_tile) {
+                    // Only now, when what was read from it is in use: an arrival right after the
+                    // loads let the slot be refilled before they had returned.
+                    mbar_arrive(&raw_empty[rs]);
+                    raw++;
+                }
             }
         }
         if (!ok) attn_timeout(a.status, abort);
