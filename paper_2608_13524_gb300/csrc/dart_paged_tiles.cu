@@ -47,6 +47,9 @@
 namespace dart {
 namespace {
 
+// Where K and V tiles come from: bf16 pages; e4m3 pages, converted in the CTA;
+// e4m3 pages that paged_widen_kernel has laid out as f16 tiles before.
+enum Source { kPages, kCodes, kWidened };
 constexpr int kRows = 128;               // query rows per unit (MMA M)
 constexpr int kKeys = 128;               // keys per tile
 constexpr int kHalf = kKeys * 128;       // 128 rows of one 128-byte swizzle column
@@ -78,6 +81,10 @@ struct TileArgs {
     uint4 *side_k, *side_v;     // [nseq][Hkv][sk] rows; e4m3 pages: [nseq][Hkv][sk / 128][16 pieces][128]
     float* q_scale;             // [nseq][Hkv][nqt][128], with scale * log2(e) in it
     float *side_ks, *side_vs;   // [nseq][Hkv][sk]
+    // kWidened: all tiles of a kv head, f16 times a power of two each of K and V
+    int wide_tiles;             // room per sequence and kv head
+    uint4 *wide_k, *wide_v;     // [nseq][Hkv][wide_tiles * 128] rows
+    float2* wide_refs;          // [nseq][Hkv][wide_tiles]
 };
 
 // Two fp32 operations in one instruction.
@@ -267,6 +274,99 @@ __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_c
     }
 }
 
+// The logarithm of a power of two.
+__device__ __forceinline__ float log2_of(float x) { return static_cast<float>(static_cast<int>(__float_as_uint(x) >> 23) - 127); }
+// A power of two above x >= 0.
+__device__ __forceinline__ float above(float x) {
+    return __uint_as_float((min(max(__float_as_uint(x) >> 23, 27u), 252u) + 1u) << 23);
+}
+
+// ------------------------------------------------------------ e4m3 pages as f16 tiles
+
+// One block per tile of a sequence and kv head (whole cache tiles, then side
+// tiles): codes times their key's scale over a power of two that the tile's
+// keys (and, apart, values) have in common, rounded once to f16.  Converting in
+// the tiles kernel costs 0.8 us a tile of every unit, and this 2 us a tile once.
+__global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant__ TileArgs ta, const uint8_t* pool_k, const uint8_t* pool_v) {
+    __shared__ float scale_of[2 * kKeys];
+    __shared__ float top_of[8];
+    const PagedArgs& a = ta.p;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int head = blockIdx.x % a.Hkv, s = blockIdx.x / a.Hkv, t = blockIdx.y;
+    pdl_wait();
+    pdl_trigger();
+    const int len = seq_len(a, s), nodes = seq_nodes(a, s), whole = len / kKeys, tail = len % kKeys;
+    if (t > whole + (tail + nodes) / kKeys) return;
+    const bool cache_tile = t < whole;
+    auto pool_row = [&](int key) -> long long {  // of a key of the tile; -1: no such page
+        const int at = t * kKeys + key;
+        const int page = ld_plain(a.table + static_cast<long long>(s) * a.max_pages + (at >> a.page_log2));
+        if (page < 0 || page >= a.num_pages) return -1;
+        return ((static_cast<long long>(page) * a.Hkv + head) << a.page_log2) + (at & ((1 << a.page_log2) - 1));
+    };
+    const long long side = (static_cast<long long>(s) * a.Hkv + head) * ta.sk + (t - whole) * kKeys;
+    {
+        const int kv = tid >> 7, key = tid & 127;
+        float sc = 0.0f;
+        if (cache_tile) {
+            const long long row = pool_row(key);
+            if (row >= 0)
+                sc = ld_plain((kv ? a.vs : a.ks) + row);
+            else if (a.status)
+                atomicOr(a.status, kDevBounds);
+        } else {
+            sc = __ldcg((kv ? ta.side_vs : ta.side_ks) + side + key);
+        }
+        scale_of[tid] = sc;
+        const float top = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(fmaxf(sc, 0.0f))));
+        if (lane == 0) top_of[warp] = top;
+    }
+    __syncthreads();
+    float ref[2];
+#pragma unroll
+    for (int kv = 0; kv < 2; kv++) ref[kv] = above(fmaxf(fmaxf(top_of[4 * kv], top_of[4 * kv + 1]), fmaxf(top_of[4 * kv + 2], top_of[4 * kv + 3])));
+    const long long tile = (static_cast<long long>(s) * a.Hkv + head) * ta.wide_tiles + t;
+    if (tid == 0) ta.wide_refs[tile] = make_float2(ref[0], ref[1]);
+    // groups of 8 lanes a row, 16 elements a lane
+    const int p = tid & 7, group = tid >> 3;
+#pragma unroll
+    for (int i = 0; i < 2 * kKeys / 32; i++) {
+        const int kv = i >= kKeys / 32, key = (i * 32 + group) & 127;
+        const __half2 by = __float2half2_rn(scale_of[kv * kKeys + key] * __uint_as_float(0x7F000000u - __float_as_uint(ref[kv])));
+        uint32_t x[8];
+        if (cache_tile) {
+            const long long row = pool_row(key);
+            uint4 c = make_uint4(0u, 0u, 0u, 0u);
+            if (row >= 0) c = ld_plain(reinterpret_cast<const uint4*>(kv ? pool_v : pool_k) + row * 8 + p);
+            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                x[2 * e] = codes_to_f16(w[e]);
+                x[2 * e + 1] = codes_to_f16(w[e] >> 16);
+            }
+        } else {
+            const uint4* src = (kv ? ta.side_v : ta.side_k) + (side >> 7) * (16 * kKeys) + key;
+            const uint4 c = __ldcg(src + 2 * p * kKeys), d = __ldcg(src + (2 * p + 1) * kKeys);
+            x[0] = c.x;
+            x[1] = c.y;
+            x[2] = c.z;
+            x[3] = c.w;
+            x[4] = d.x;
+            x[5] = d.y;
+            x[6] = d.z;
+            x[7] = d.w;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&x[e]), by);
+            x[e] = *reinterpret_cast<const uint32_t*>(&r);
+        }
+        uint4* d = (kv ? ta.wide_v : ta.wide_k) + (tile * kKeys + key) * 16 + 2 * p;
+        d[0] = make_uint4(x[0], x[1], x[2], x[3]);
+        d[1] = make_uint4(x[4], x[5], x[6], x[7]);
+    }
+}
+
 // ------------------------------------------------------------ the schedule
 
 // A place in the list: kv heads of a sequence one after the other, the units
@@ -419,27 +519,23 @@ __device__ __forceinline__ void mma_pv(uint32_t d, uint32_t p, uint32_t v_lo, ui
     if constexpr (kk + 1 < kKeys / 16) mma_pv<kk + 1>(d, p, v_lo, idesc, first);
 }
 
-// A power of two above x >= 0.
-__device__ __forceinline__ float above(float x) {
-    return __uint_as_float((min(max(__float_as_uint(x) >> 23, 27u), 252u) + 1u) << 23);
-}
-
-template <bool kFp8>
+template <Source kSource>
 struct TGeo {
-    // bf16: three operand tiles of K and of V.  e4m3: two of each, and raw
-    // tiles of half the size before them.
-    static constexpr int kStages = kFp8 ? 2 : 3;
-    static constexpr int kRawK = kFp8 ? 3 : 0, kRawV = kFp8 ? 2 : 0;
+    static constexpr bool kConv = kSource == kCodes;
+    // Three operand tiles of K and of V; converted ones two of each, and raw tiles of
+    // half the size before them.
+    static constexpr int kStages = kConv ? 2 : 3;
+    static constexpr int kRawK = kConv ? 3 : 0, kRawV = kConv ? 2 : 0;
     static constexpr int kRing = 4;  // a tile's factors outlive its operands
     static constexpr int kOps = 2 * kStages * kTile;
     static constexpr int kRaw = (kRawK + kRawV) * kHalf;
     static constexpr int kRawScales = (kRawK + kRawV) * kKeys * 4;
-    static constexpr int kBars = 4 * kStages + 2 * (kRawK + kRawV) + (kFp8 ? kRing : 0) + 9 + 1;
+    static constexpr int kBars = 4 * kStages + 2 * (kRawK + kRawV) + (kConv ? kRing : 0) + 9 + 1;
     static constexpr int kExchange = 2 * kRows * 4 + 8 * 4 + kRing * 8 + kRing * 4 * 4;
     static constexpr int kSmem = kOps + kRaw + kRawScales + kBars * 8 + kExchange + 16;
-    // e4m3: warpgroups (producer, MMA, two idle warps), softmax, softmax, converters
-    static constexpr int kThreads = kFp8 ? 512 : 64 + kSoft;
-    static constexpr int kFirstSoft = kFp8 ? 4 : 2;
+    // kCodes: warpgroups (producer, MMA, two idle warps), softmax, softmax, converters
+    static constexpr int kThreads = kConv ? 512 : 64 + kSoft;
+    static constexpr int kFirstSoft = kConv ? 4 : 2;
 };
 
 __device__ __forceinline__ uint32_t tile_swz(int row, int piece) { return static_cast<uint32_t>(row * 128 + ((piece ^ (row & 7)) << 4)); }
@@ -478,12 +574,14 @@ __device__ __forceinline__ uint64_t mask_bits(const uint64_t* m, int mw, int o) 
     return r;
 }
 
-template <bool kFp8>
-__global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
+template <Source kSource>
+__global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
     paged_tiles_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                        const __grid_constant__ CUtensorMap tmSk, const __grid_constant__ CUtensorMap tmSv,
                        const __grid_constant__ TileArgs ta) {
-    using G_ = TGeo<kFp8>;
+    using G_ = TGeo<kSource>;
+    constexpr bool kConv = kSource == kCodes;  // converting warps
+    constexpr bool kF16 = kSource != kPages;   // f16 operands, with a factor per row of Q and per tile of K and V
     constexpr int kStages = G_::kStages;
     const PagedArgs& a = ta.p;
     extern __shared__ __align__(1024) uint8_t tiles_smem[];
@@ -501,7 +599,7 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
     uint64_t* rv_full = rk_empty + G_::kRawK;
     uint64_t* rv_empty = rv_full + G_::kRawV;
     uint64_t* sc_full = rv_empty + G_::kRawV;
-    uint64_t* s_full = sc_full + (kFp8 ? G_::kRing : 0);
+    uint64_t* s_full = sc_full + (kConv ? G_::kRing : 0);
     uint64_t* s_empty = s_full + 1;         // softmax has S in registers
     uint64_t* p_full = s_empty + 1;         // [2] by P buffer (P(n + 1) may be there before P(n) is waited for)
     uint64_t* pv_done = p_full + 2;         // [2] by P buffer
@@ -519,9 +617,9 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; i++) {
-            mbar_init(&k_full[i], kFp8 ? 64 : 1);
+            mbar_init(&k_full[i], kConv ? 64 : 1);
             mbar_init(&k_empty[i], 1);
-            mbar_init(&v_full[i], kFp8 ? 64 : 1);
+            mbar_init(&v_full[i], kConv ? 64 : 1);
             mbar_init(&v_empty[i], 1);
         }
         for (int i = 0; i < G_::kRawK; i++) {
@@ -532,7 +630,7 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
             mbar_init(&rv_full[i], 1);
             mbar_init(&rv_empty[i], 64);
         }
-        if (kFp8)
+        if (kConv)
             for (int i = 0; i < G_::kRing; i++) mbar_init(&sc_full[i], 2);
         mbar_init(s_full, 1);
         mbar_init(s_empty, kSoft);
@@ -572,30 +670,31 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
     }
 
     if (warp < G_::kFirstSoft) {
-        if (kFp8) reg_less<kRegsIssue>();
+        if (kConv) reg_less<kRegsIssue>();
         if (warp == 0) {
             // ---------------------------------------------------------- loads: the whole warp, a lane per page
             const int per_tile = kKeys >> a.page_log2;  // pages of a tile
             const uint64_t policy = (a.B + 1) * a.G <= kRows ? l2_policy_evict_first() : l2_policy_evict_last();
             auto page_at = [&](int t) {
-                return t < w.whole && lane < per_tile
+                return kSource != kWidened && t < w.whole && lane < per_tile
                            ? __ldcg(a.table + static_cast<long long>(w.s) * a.max_pages + static_cast<long long>(t) * per_tile + lane)
                            : 0;
             };
             int n = 0;       // bf16: tiles so far; e4m3: whole cache tiles so far
-            bool have = w.next(a), ok = true, waited = false;
+            bool have = w.next(a), ok = true, waited = kSource == kWidened;
+            if (waited) pdl_wait();
             int t = w.t0, page = have ? page_at(t) : 0;
             while (have && ok) {
                 // this tile, then the next one's page numbers, which are there when it is its turn
                 const int head = w.head, s = w.s, tt = t, my_page = page;
-                const bool cache_tile = tt < w.whole;
-                const int side_row = (tt - w.whole) * kKeys;
+                const bool cache_tile = kSource != kWidened && tt < w.whole;
+                const int laid_row = kSource == kWidened ? ((s * a.Hkv + head) * ta.wide_tiles + tt) * kKeys : (s * a.Hkv + head) * ta.sk + (tt - w.whole) * kKeys;
                 if (++t == w.t1) {
                     have = w.next(a);
                     t = w.t0;
                 }
                 if (have) page = page_at(t);
-                if (kFp8 && !cache_tile) continue;  // (the converting warps read side tiles themselves)
+                if (kConv && !cache_tile) continue;  // (the converting warps read side tiles themselves)
                 if (!cache_tile && !waited) {
                     pdl_wait();
                     waited = true;
@@ -608,25 +707,25 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                         atomicOr(a.status, kDevBounds);
                 }
                 for (int kv = 0; kv < 2 && ok; kv++) {
-                    const int stages = kFp8 ? (kv ? G_::kRawV : G_::kRawK) : kStages;
+                    const int stages = kConv ? (kv ? G_::kRawV : G_::kRawK) : kStages;
                     const int st = n % stages;
-                    uint64_t* full = (kFp8 ? (kv ? rv_full : rk_full) : (kv ? v_full : k_full)) + st;
-                    uint64_t* empty = (kFp8 ? (kv ? rv_empty : rk_empty) : (kv ? v_empty : k_empty)) + st;
-                    uint8_t* dst = kFp8 ? (kv ? rV : rK) + st * kHalf : (kv ? sV : sK) + st * kTile;
+                    uint64_t* full = (kConv ? (kv ? rv_full : rk_full) : (kv ? v_full : k_full)) + st;
+                    uint64_t* empty = (kConv ? (kv ? rv_empty : rk_empty) : (kv ? v_empty : k_empty)) + st;
+                    uint8_t* dst = kConv ? (kv ? rV : rK) + st * kHalf : (kv ? sV : sK) + st * kTile;
                     const CUtensorMap* tm = cache_tile ? (kv ? &tmV : &tmK) : (kv ? &tmSv : &tmSk);
                     ok = warp_wait<kWaitPolls>(empty, (static_cast<uint32_t>(n / stages) & 1u) ^ 1u, abort);
                     if (!ok) break;
                     if (lane == 0)
-                        mbar_arrive_expect_tx(full, kFp8 ? kHalf + kKeys * 4 : kTile);
+                        mbar_arrive_expect_tx(full, kConv ? kHalf + kKeys * 4 : kTile);
                     __syncwarp();
                     if (!cache_tile) {
                         if (lane < 2)
-                            tma_load_2d(dst + lane * kHalf, tm, full, 64 * lane, (s * a.Hkv + head) * ta.sk + side_row, policy);
+                            tma_load_2d(dst + lane * kHalf, tm, full, 64 * lane, laid_row, policy);
                     } else if (lane < per_tile) {
                         const uint32_t at = static_cast<uint32_t>(lane << a.page_log2) * 128;
                         tma_load_2d(dst + at, tm, full, 0, static_cast<int>(row), policy);
-                        if (!kFp8) tma_load_2d(dst + kHalf + at, tm, full, 64, static_cast<int>(row), policy);
-                        if (kFp8) {
+                        if (!kConv) tma_load_2d(dst + kHalf + at, tm, full, 64, static_cast<int>(row), policy);
+                        if (kConv) {
                             const long long sr = row < a.pool_rows ? row : 0;
                             bulk_load(raw_scales + (kv * G_::kRawK + st) * kKeys + (lane << a.page_log2), (kv ? a.vs : a.ks) + sr, 4u << a.page_log2, full);
                         }
@@ -638,8 +737,8 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
             if (*abort) {
                 // copies still in flight must land before the CTA exits
                 for (int kv = 0; kv < 2; kv++) {
-                    const int stages = kFp8 ? (kv ? G_::kRawV : G_::kRawK) : kStages;
-                    uint64_t* full = kFp8 ? (kv ? rv_full : rk_full) : (kv ? v_full : k_full);
+                    const int stages = kConv ? (kv ? G_::kRawV : G_::kRawK) : kStages;
+                    uint64_t* full = kConv ? (kv ? rv_full : rk_full) : (kv ? v_full : k_full);
                     // (the tile at which a wait failed may have its K under way)
                     for (int i = max(n - stages, 0); i < n + (kv == 0 && !ok ? 1 : 0); i++)
                         if (lane == 0) attn_drain(&full[i % stages], static_cast<uint32_t>(i / stages) & 1u);
@@ -649,8 +748,8 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
             // ---------------------------------------------------------- MMAs
             if (lane == 0) {
                 // (operand types: bf16 1, f16 0 in bits 7 and 10)
-                constexpr uint32_t idesc_s = idesc_bf16_f32(kRows, kKeys) & (kFp8 ? ~((1u << 7) | (1u << 10)) : ~0u);
-                constexpr uint32_t idesc_pv = (idesc_bf16_f32(kRows, kHeadDim) & (kFp8 ? ~((1u << 7) | (1u << 10)) : ~0u)) | (1u << 16);  // B (= V) MN-major
+                constexpr uint32_t idesc_s = idesc_bf16_f32(kRows, kKeys) & (kF16 ? ~((1u << 7) | (1u << 10)) : ~0u);
+                constexpr uint32_t idesc_pv = (idesc_bf16_f32(kRows, kHeadDim) & (kF16 ? ~((1u << 7) | (1u << 10)) : ~0u)) | (1u << 16);  // B (= V) MN-major
                 const uint32_t k_lo = smem_u32(sK) >> 4, v_lo = smem_u32(sV) >> 4;
                 auto issue_s = [&](int n, int part) -> bool {
                     const int st = n % kStages;
@@ -706,7 +805,7 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
         }
     } else if (warp < G_::kFirstSoft + 8) {
         // ---------------------------------------------------------- softmax
-        if (kFp8) reg_more<kRegsSoft>();
+        if (kConv) reg_more<kRegsSoft>();
         const int qd = warp & 3, wg = (warp - G_::kFirstSoft) >> 2, cb = wg * 64;
         const int r = qd * 32 + lane;  // query row of the unit = TMEM lane
         const int pair_bar = kPairBar + qd;
@@ -738,12 +837,16 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
             const bool full_unit = t0 == 0 && t1 == w.tiles;
             const int row = w.qt * kRows + r, b = row >> a.g_log2;
             const bool row_ok = b <= nodes;
-            // m_run: the row's reference; e4m3: O is in units of vref, and P has a factor
-            // 2^7 (at most 2^15 in f16), so that 2^-31 of the largest weight still counts
-            constexpr float kBoost = kFp8 ? 7.0f : 0.0f;
+            // m_run: the row's reference.  f16: O is in units of vref, the largest of the
+            // tiles' powers of two so far; P has a factor 2^7 (at most 2^15), so that 2^-31
+            // of the largest weight still counts, and its tile's power of two over vref
+            constexpr float kBoost = kF16 ? 7.0f : 0.0f;
             float m_run = -INFINITY, l = 0.0f, vref = 0.0f;
-            float rs = a.sl2;  // scores in log2 units = products * rs (e4m3: * the tile's power of two of K)
-            if (kFp8 && row_ok) rs = __ldcg(ta.q_scale + ((static_cast<long long>(s) * a.Hkv + head) * ta.nqt + w.qt) * kRows + r);
+            float rs = a.sl2;  // scores in log2 units = products * rs (f16: * the tile's power of two of K)
+            if (kF16 && row_ok) rs = __ldcg(ta.q_scale + ((static_cast<long long>(s) * a.Hkv + head) * ta.nqt + w.qt) * kRows + r);
+            float2 ref_ahead = make_float2(1.0f, 1.0f);  // (kWidened: read a tile ahead)
+            const float2* refs = ta.wide_refs + (static_cast<long long>(s) * a.Hkv + head) * ta.wide_tiles;
+            if (kSource == kWidened) ref_ahead = __ldcg(refs + t0);
             for (int t = t0; t < t1; t++, n++) {
                 // visible keys of this row among this warpgroup's 64 of the tile
                 uint64_t vis = row_ok ? ~0ull : 0ull;
@@ -760,16 +863,17 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                 // Both warps of the lane quarter reach both pair barriers of every
                 // iteration and leave the loop at the same point: a failed wait is
                 // exchanged with the row max and acted on after the barriers.
-                if (kFp8 && ok && !warp_wait<1>(&sc_full[n % G_::kRing], static_cast<uint32_t>(n / G_::kRing) & 1u, abort)) ok = false;
+                if (kConv && ok && !warp_wait<1>(&sc_full[n % G_::kRing], static_cast<uint32_t>(n / G_::kRing) & 1u, abort)) ok = false;
                 if (ok && !warp_wait<1>(s_full, static_cast<uint32_t>(n) & 1u, abort)) ok = false;
                 if (!ok) attn_timeout(a.status, abort);
                 float sv[64];
-                float mx = -INFINITY, rt = rs, vnew = 0.0f;
+                float mx = -INFINITY, rt = rs, vtile = 0.0f;
                 if (ok) {
-                    if (kFp8) {  // (before s_empty: after S(n + 1) the place may be written again)
-                        const float2 ref = tile_ref[n % G_::kRing];
+                    if (kF16) {  // (before s_empty: after S(n + 1) the place may be written again)
+                        const float2 ref = kConv ? tile_ref[n % G_::kRing] : ref_ahead;
                         rt *= ref.x;
-                        vnew = ref.y;
+                        vtile = ref.y;
+                        if (kSource == kWidened && t + 1 < t1) ref_ahead = __ldcg(refs + t + 1);
                     }
                     tc_fence_after();
                     tmem_ld64(tl + kSCol + cb, sv);
@@ -795,11 +899,16 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                 if (!ok) break;
                 const float mx2 = mx * rt;
                 const bool higher = mx2 > m_run + kSlack8;
-                const bool resc = higher || (kFp8 && vnew != vref);  // (vref: the same in every thread)
+                const bool resc = higher || (kF16 && vtile > vref);  // (vref: the same in every thread)
                 const float m_new = higher ? mx2 : m_run;
                 const float alpha = higher ? ex2(m_run - m_new) : 1.0f;
-                const float alpha_o = kFp8 ? alpha * (vref / vnew) : alpha;
-                vref = vnew;
+                float alpha_o = alpha, down = 1.0f;  // (down: P's part for the tile's power of two; 2^-60 is as good as nothing)
+                if (kF16) {
+                    const float vnew = fmaxf(vref, vtile);
+                    alpha_o *= vref / vnew;
+                    down = fmaxf(vtile / vnew, 8.6736173798840355e-19f);
+                    vref = vnew;
+                }
                 // P buffer n & 1 was last read by PV(n - 2); O must be stable (PV(n - 1)
                 // done) only when it is rescaled.  On a timeout this tile is
                 // skipped; the pair leaves the loop together at the next exchange.
@@ -830,7 +939,7 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                 m_run = m_new;
                 // P = 2^(s - m) as bf16 pairs; hidden keys hold -inf and give 0 (so does
                 // every key of a row that has seen no visible key: m = -inf)
-                const float nm = m_run == -INFINITY ? 0.0f : kBoost - m_run;
+                const float nm = m_run == -INFINITY ? 0.0f : kBoost - m_run + (kF16 ? log2_of(down) : 0.0f);
                 float2 sum0 = make_float2(0.0f, 0.0f), sum1 = sum0;
                 uint32_t pk[32];
 #pragma unroll
@@ -841,14 +950,14 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                     z = make_float2(ex2(z.x), ex2(z.y));
                     sum0 = add2(sum0, x);
                     sum1 = add2(sum1, z);
-                    pk[c >> 1] = kFp8 ? pack_f16x2(x.x, x.y) : pack_bf16x2(x.x, x.y);
-                    pk[(c >> 1) + 1] = kFp8 ? pack_f16x2(z.x, z.y) : pack_bf16x2(z.x, z.y);
+                    pk[c >> 1] = kF16 ? pack_f16x2(x.x, x.y) : pack_bf16x2(x.x, x.y);
+                    pk[(c >> 1) + 1] = kF16 ? pack_f16x2(z.x, z.y) : pack_bf16x2(z.x, z.y);
                 }
                 sum0 = add2(sum0, sum1);
                 const float lsum = sum0.x + sum0.y;
                 tmem_st32(tl + kPCol + (n & 1) * 64 + wg * 32, pk);
                 tmem_wait_st();
-                l += lsum;
+                l += kF16 ? lsum * __uint_as_float(0x7F000000u - __float_as_uint(down)) : lsum;  // (1 / down)
                 tc_fence_before();
                 mbar_arrive(&p_full[n & 1]);
                 if (t == t0) {
@@ -877,7 +986,7 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
             mbar_arrive(o_free);
             if (full_unit) {
                 // rows in whole lines: 8 lanes exchange their rows' 8 pieces
-                const float inv = l > 0.0f ? (kFp8 ? vref : 1.0f) / l : 0.0f;
+                const float inv = l > 0.0f ? (kF16 ? vref : 1.0f) / l : 0.0f;
                 uint4 y[8];
 #pragma unroll
                 for (int e = 0; e < 8; e++)
@@ -894,13 +1003,13 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                 TilePart* d = reinterpret_cast<TilePart*>(a.parts) + 2 * blockIdx.x + (t0 > 0 ? 0 : 1);
 #pragma unroll
                 for (int e = 0; e < 16; e++) {
-                    const float by = kFp8 ? vref : 1.0f;
+                    const float by = kF16 ? vref : 1.0f;
                     d->o[wg * 16 + e][r] = make_float4(o[4 * e] * by, o[4 * e + 1] * by, o[4 * e + 2] * by, o[4 * e + 3] * by);
                 }
                 if (wg == 0) d->ml[r] = make_float2(m_run, l);
             }
         }
-    } else if constexpr (kFp8) {
+    } else if constexpr (kConv) {
         // ---------------------------------------------------------- raw tiles to operands (e4m3): a thread per key
         reg_less<kRegsConvert>();
         // Two warps for K, two for V, on their own; a thread takes keys `key` and key + 64.
@@ -920,7 +1029,6 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
         // The two warps meet at a barrier in every tile, so they leave together: one whose
         // wait failed says so at the next tile's.
         while (!stop && w.next(a)) {
-            float vref = 0.0f;  // (V) of the part's tiles so far
             for (int t = w.t0; t < w.t1; t++, n++) {
                 const bool cache_tile = t < w.whole;
                 if (!cache_tile && !waited) {
@@ -944,8 +1052,7 @@ __global__ void __launch_bounds__(TGeo<kFp8>::kThreads, 1)
                     stop = true;
                     break;
                 }
-                float ref = above(fmaxf(both.x, both.y));
-                if (kv) ref = vref = fmaxf(vref, ref);
+                const float ref = above(fmaxf(both.x, both.y));
                 if (key == 0) {
                     (kv ? tile_ref[n % G_::kRing].y : tile_ref[n % G_::kRing].x) = ref;
                     mbar_arrive(&sc_full[n % G_::kRing]);
@@ -1061,65 +1168,100 @@ __global__ void __launch_bounds__(256) paged_tiles_join_kernel(const __grid_cons
                                               pack_bf16x2(o[4] * inv, o[5] * inv), pack_bf16x2(o[6] * inv, o[7] * inv));
 }
 
-// Workspace: partial results, rotated queries, side keys, side values.
+// e4m3 pages are widened first where a kv head has at least this many query
+// tiles, each of which would convert all keys again (a tile of a unit takes 1.1
+// us from f16 tiles and 1.9 converted, widening a tile 2), and where the f16
+// tiles of the longest sequences take at most 4 GB.
+constexpr int kWidenTiles = 4;
+constexpr size_t kWidenBytes = static_cast<size_t>(4) << 30;
+
+// Workspace: partial results, queries, side rows, their factors, f16 tiles.
 struct TileWs {
-    int sk;
-    size_t q, k, v, qs, ks, vs, total;
+    int sk, nqt, wide_tiles;
+    size_t q, k, v, qs, ks, vs, wk, wv, refs, total;
 };
-TileWs tile_ws(int nseq, int B, int Hq, int Hkv) {
-    const size_t q_rows = static_cast<size_t>(nseq) * Hkv * (((B + 1) * (Hq / Hkv) + kRows - 1) / kRows) * kRows;
-    TileWs w;
+TileWs tile_ws(int nseq, int B, int Hq, const dart_kv_cache& cache, int max_pages) {
+    TileWs w{};
+    const int Hkv = cache.Hkv;
     w.sk = (kKeys - 1 + B + 1 + kKeys - 1) / kKeys * kKeys;
+    w.nqt = ((B + 1) * (Hq / Hkv) + kRows - 1) / kRows;
+    const size_t heads = static_cast<size_t>(nseq) * Hkv, q_rows = heads * w.nqt * kRows;
     auto up = [](size_t n) { return (n + 255) & ~static_cast<size_t>(255); };
-    const size_t side = up(static_cast<size_t>(nseq) * Hkv * w.sk * kHeadDim * 2);
     w.q = up(sizeof(SharePlan) + sizeof(TilePart) * 2 * kMaxSms);
     w.k = w.q + up(q_rows * kHeadDim * 2);
-    w.v = w.k + side;
-    w.qs = w.v + side;
+    w.v = w.k + up(heads * w.sk * kHeadDim * 2);
+    w.qs = w.v + up(heads * w.sk * kHeadDim * 2);
     w.ks = w.qs + up(q_rows * 4);
-    w.vs = w.ks + up(static_cast<size_t>(nseq) * Hkv * w.sk * 4);
-    w.total = w.vs + up(static_cast<size_t>(nseq) * Hkv * w.sk * 4);
+    w.vs = w.ks + up(heads * w.sk * 4);
+    w.wk = w.vs + up(heads * w.sk * 4);
+    const long long tiles = static_cast<long long>(max_pages) * cache.page_size / kKeys + w.sk / kKeys;
+    const size_t each = heads * tiles * kTile;
+    if (cache.dtype == DART_KV_E4M3 && w.nqt >= kWidenTiles && each <= kWidenBytes / 2 && tiles <= 65535) w.wide_tiles = static_cast<int>(tiles);
+    const size_t wide = w.wide_tiles ? each : 0;
+    w.wv = w.wk + wide;
+    w.refs = w.wv + wide;
+    w.total = w.refs + up(heads * w.wide_tiles * 8);
     return w;
 }
 
 }  // namespace
 
 size_t paged_tiles_workspace(const dart_paged_attn_config& c, const dart_kv_cache& cache) {
-    return tile_ws(c.nseq, c.B, c.Hq, cache.Hkv).total;
+    return tile_ws(c.nseq, c.B, c.Hq, cache, c.max_pages).total;
 }
 
-bool paged_tiles_prepare_device() {
-    return cudaFuncSetAttribute(paged_tiles_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, TGeo<false>::kSmem) == cudaSuccess &&
-           cudaFuncSetAttribute(paged_tiles_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, TGeo<true>::kSmem) == cudaSuccess;
+template <Source kSource>
+static bool allow_smem() {
+    return cudaFuncSetAttribute(paged_tiles_kernel<kSource>, cudaFuncAttributeMaxDynamicSharedMemorySize, TGeo<kSource>::kSmem) == cudaSuccess;
+}
+bool paged_tiles_prepare_device() { return allow_smem<kPages>() && allow_smem<kCodes>() && allow_smem<kWidened>(); }
+
+template <Source kSource>
+static cudaError_t launch_tiles(int sms, cudaStream_t st, const CUtensorMap& k, const CUtensorMap& v, const CUtensorMap& side_k,
+                                const CUtensorMap& side_v, const TileArgs& ta) {
+    return launch_pdl(paged_tiles_kernel<kSource>, dim3(sms), dim3(TGeo<kSource>::kThreads), TGeo<kSource>::kSmem, st, k, v, side_k, side_v, ta);
 }
 
 int launch_paged_tiles(PagedArgs a, const dart_kv_cache& cache, uint8_t* workspace, int sms, cudaStream_t st) {
     const bool fp8 = cache.dtype == DART_KV_E4M3;
-    const TileWs w = tile_ws(a.nseq, a.B, a.Hq, a.Hkv);
+    const TileWs w = tile_ws(a.nseq, a.B, a.Hq, cache, a.max_pages);
+    const bool wide = w.wide_tiles > 0;
     TileArgs ta{};
     ta.p = a;
     ta.sk = w.sk;
-    ta.nqt = ((a.B + 1) * a.G + kRows - 1) / kRows;
+    ta.nqt = w.nqt;
     ta.qr = reinterpret_cast<uint4*>(workspace + w.q);
     ta.side_k = reinterpret_cast<uint4*>(workspace + w.k);
     ta.side_v = reinterpret_cast<uint4*>(workspace + w.v);
     ta.q_scale = reinterpret_cast<float*>(workspace + w.qs);
     ta.side_ks = reinterpret_cast<float*>(workspace + w.ks);
     ta.side_vs = reinterpret_cast<float*>(workspace + w.vs);
-    const long long side_rows = static_cast<long long>(a.nseq) * a.Hkv * w.sk;
+    ta.wide_tiles = w.wide_tiles;
+    ta.wide_k = reinterpret_cast<uint4*>(workspace + w.wk);
+    ta.wide_v = reinterpret_cast<uint4*>(workspace + w.wv);
+    ta.wide_refs = reinterpret_cast<float2*>(workspace + w.refs);
+    const long long heads = static_cast<long long>(a.nseq) * a.Hkv, side_rows = heads * w.sk;
     CUtensorMap tmK, tmV, tmSk, tmSv;
-    if (!encode_rows(&tmK, cache.k, a.pool_rows, fp8, cache.page_size) || !encode_rows(&tmV, cache.v, a.pool_rows, fp8, cache.page_size) ||
-        !encode_rows(&tmSk, ta.side_k, side_rows, false, kKeys) || !encode_rows(&tmSv, ta.side_v, side_rows, false, kKeys))
-        return DART_ERR_CUDA;
+    // f16 tiles are 16-bit rows to the copies, as bf16 rows are
+    const bool maps = wide ? encode_rows(&tmK, ta.wide_k, heads * w.wide_tiles * kKeys, false, kKeys) && encode_rows(&tmV, ta.wide_v, heads * w.wide_tiles * kKeys, false, kKeys)
+                           : encode_rows(&tmK, cache.k, a.pool_rows, fp8, cache.page_size) && encode_rows(&tmV, cache.v, a.pool_rows, fp8, cache.page_size) &&
+                                 encode_rows(&tmSk, ta.side_k, side_rows, false, kKeys) && encode_rows(&tmSv, ta.side_v, side_rows, false, kKeys);
+    if (!maps) return DART_ERR_CUDA;
+    if (wide) {
+        tmSk = tmK;  // (side tiles lie among the others)
+        tmSv = tmV;
+    }
     const dim3 prep(static_cast<unsigned>(a.nseq), static_cast<unsigned>(w.sk));
     const uint8_t *pk = static_cast<const uint8_t*>(cache.k), *pv = static_cast<const uint8_t*>(cache.v);
     cudaError_t e = fp8 ? launch_pdl(paged_prep_kernel<true>, prep, dim3(kPrepThreads), 0, st, ta, pk, pv)
                         : launch_pdl(paged_prep_kernel<false>, prep, dim3(kPrepThreads), 0, st, ta, pk, pv);
-    if (e != cudaSuccess) return DART_ERR_CUDA;
-    e = fp8 ? launch_pdl(paged_tiles_kernel<true>, dim3(sms), dim3(TGeo<true>::kThreads), TGeo<true>::kSmem, st, tmK, tmV, tmSk, tmSv, ta)
-            : launch_pdl(paged_tiles_kernel<false>, dim3(sms), dim3(TGeo<false>::kThreads), TGeo<false>::kSmem, st, tmK, tmV, tmSk, tmSv, ta);
-    if (e != cudaSuccess) return DART_ERR_CUDA;
-    return launch_pdl(paged_tiles_join_kernel, dim3(8 * (sms - 1)), dim3(256), 0, st, a) == cudaSuccess ? DART_OK : DART_ERR_CUDA;
+    if (e == cudaSuccess && wide)
+        e = launch_pdl(paged_widen_kernel, dim3(static_cast<unsigned>(heads), static_cast<unsigned>(w.wide_tiles)), dim3(256), 0, st, ta, pk, pv);
+    if (e == cudaSuccess)
+        e = wide ? launch_tiles<kWidened>(sms, st, tmK, tmV, tmSk, tmSv, ta)
+                 : fp8 ? launch_tiles<kCodes>(sms, st, tmK, tmV, tmSk, tmSv, ta) : launch_tiles<kPages>(sms, st, tmK, tmV, tmSk, tmSv, ta);
+    if (e == cudaSuccess) e = launch_pdl(paged_tiles_join_kernel, dim3(8 * (sms - 1)), dim3(256), 0, st, a);
+    return e == cudaSuccess ? DART_OK : DART_ERR_CUDA;
 }
 
 }  // namespace dart
