@@ -234,7 +234,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     long long left = shares.length(share);  // places of this share not yet worked on
     Place<kFp8> use = list.find(a, shares.begin(share), lane), load = use;
     if (lane == 0) {
-        a.plan->places[share] = make_int4(use.s, use.unit, use.chunk, 0);
+        a.plan->places[share] = make_int4(use.s, use.unit, use.chunk, use.chunks);
+        a.plan->nodes[share] = use.nodes;
         if (share == 0) a.plan->count = shares.count;
     }
     long long to_load = left;  // places not yet loaded
@@ -726,7 +727,6 @@ __global__ void __launch_bounds__(kThreads, 1)
 // began: 16 threads (8 elements each) per row, and where a unit has fewer than
 // 16 rows as many more groups of threads, each with every n-th part, joined in
 // order through shared memory.
-template <bool kFp8>
 __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_constant__ PagedArgs a) {
     __shared__ float2 ml_of[kUnitRows];
     __shared__ float sum_of[kUnitRows][kHeadDim];
@@ -734,22 +734,17 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
     pdl_trigger();
     const int tid = threadIdx.x, lane = tid & 31, i = blockIdx.x + 1;
     pdl_wait();
-    const int count = a.plan->count;
-    if (i >= count) return;
+    // all that has to be known in one go (the kernel is a chain of loads)
+    const int count = a.plan->count, nodes = a.plan->nodes[i];
     const int4 at = a.plan->places[i], prev = a.plan->places[i - 1];
-    if (at.z == 0 || (prev.x == at.x && prev.y == at.y && prev.z > 0)) return;
-    Place<kFp8> p{};
-    p.s = at.x;
-    p.load(a);
-    if (at.z >= p.chunks) return;  // (the unit ended in share i - 1; what is left of it in the list is its other costs)
+    int4 next = a.plan->places[min(i + 1 + tid, kWarps * kMaxSms - 1)];
+    if (i >= count || at.z == 0 || at.z >= at.w) return;  // (from at.w on the place stands for a unit's other costs)
+    if (prev.x == at.x && prev.y == at.y && prev.z > 0) return;
     // the last share that holds chunks of the unit
     int end = i;
-    for (int c0 = i + 1;; c0 += kThreads) {
-        bool in = false;
-        if (c0 + tid < count) {
-            const int4 x = a.plan->places[c0 + tid];
-            in = x.x == at.x && x.y == at.y && x.z < p.chunks;
-        }
+    for (int from = i + 1;; from += kThreads) {
+        if (from > i + 1) next = a.plan->places[min(from + tid, kWarps * kMaxSms - 1)];
+        const bool in = from + tid < count && next.x == at.x && next.y == at.y && next.z < at.w;
         const unsigned out = __ballot_sync(kFull, !in);
         if (lane == 0) ends[tid >> 5] = out ? __ffs(out) - 1 : 32;
         __syncthreads();
@@ -762,8 +757,8 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
         __syncthreads();
         if (n < kThreads) break;
     }
-    const int s = p.s, groups = p.groups(a), head = at.y / groups, row0 = (at.y % groups) * kUnitRows;
-    const int rows = min(kUnitRows, ((p.nodes + 1) << a.g_log2) - row0);
+    const int s = at.x, groups = (((nodes + 1) << a.g_log2) + kUnitRows - 1) / kUnitRows, head = at.y / groups, row0 = (at.y % groups) * kUnitRows;
+    const int rows = min(kUnitRows, ((nodes + 1) << a.g_log2) - row0);
     int span = 1;  // rows rounded up to a power of two; 16 / span thread groups
     while (span < rows) span *= 2;
     const int slot_of_row = tid >> 4, d8 = tid & 15, r = slot_of_row % span, part0 = slot_of_row / span, step = kUnitRows / span;
@@ -773,17 +768,18 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
     const int c0 = i - 1, c1 = end;
     float top = -INFINITY, l = 0.0f, o[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     if (live)
+#pragma unroll 4
         for (int c = c0 + part0; c <= c1; c += step) {
             const Part* x = slot(c);
             const float2 ml = x->ml[r];
             const float4 u = *reinterpret_cast<const float4*>(&x->o[r][8 * d8]), v = *reinterpret_cast<const float4*>(&x->o[r][8 * d8 + 4]);
-            if (ml.x == -INFINITY) continue;
-            const float up = fmaxf(top, ml.x), old = top == -INFINITY ? 0.0f : exp2_fast(top - up), by = exp2_fast(ml.x - up);
+            const bool any = ml.x != -INFINITY;
+            const float up = fmaxf(top, ml.x), old = top == -INFINITY ? 0.0f : exp2_fast(top - up), by = any ? exp2_fast(ml.x - up) : 0.0f;
             top = up;
-            l = l * old + ml.y * by;
+            l = l * old + (any ? ml.y * by : 0.0f);
             const float w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int k = 0; k < 8; k++) o[k] = o[k] * old + w[k] * by;
+            for (int k = 0; k < 8; k++) o[k] = o[k] * old + (any ? w[k] * by : 0.0f);
         }
     // the groups' results, one after the other
     for (int q = 1; q < step; q++) {
@@ -925,7 +921,7 @@ int dart_paged_attention(const dart_paged_attn_config* cfg, const dart_kv_cache*
                         : launch_pdl(paged_rows_kernel<false>, dim3(ctas), dim3(kThreads), Geo<false>::kSmem, st, tmK, tmV, a);
     if (e != cudaSuccess) return DART_ERR_CUDA;
     const dim3 seams(kWarps * ctas - 1);
-    e = fp8 ? launch_pdl(paged_join_kernel<true>, seams, dim3(kThreads), 0, st, a) : launch_pdl(paged_join_kernel<false>, seams, dim3(kThreads), 0, st, a);
+    e = launch_pdl(paged_join_kernel, seams, dim3(kThreads), 0, st, a);
     if (e != cudaSuccess) return DART_ERR_CUDA;
     return DART_OK;
 }

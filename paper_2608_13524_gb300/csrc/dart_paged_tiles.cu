@@ -151,19 +151,41 @@ __device__ __forceinline__ float pack_piece(const Piece& x, uint4* lo, uint4* hi
     return factor;
 }
 
-// One block per side row of a sequence; groups of 8 threads take its keys and
-// values, head by head, and, if it is a tree row, the rotated queries.
+// Blocks 0 .. B of a sequence: a tree row's keys and values (side rows), head by
+// head by groups of 8 threads, and its rotated queries; blocks from B + 1 on: the
+// side rows that are no tree rows.
 constexpr int kPrepThreads = 256, kGroups = kPrepThreads / 8;
 template <bool kFp8>
 __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_constant__ TileArgs ta, const uint8_t* pool_k, const uint8_t* pool_v) {
     __shared__ float2 turn_of[kHeadDim / 2];  // cos, sin
     const PagedArgs& a = ta.p;
+    const int tid = threadIdx.x, p = tid & 7, group = tid >> 3, s = blockIdx.x, b = blockIdx.y;
+    const long long in = static_cast<long long>(s) * (a.B + 1) + b;
+    const int rows = a.Hq + 2 * a.Hkv;  // queries, keys, values of a tree row
+    auto source = [&](int i) {
+        return i < a.Hq ? a.q + in * a.q_stride + i * kHeadDim
+                        : i < a.Hq + a.Hkv ? a.k + in * a.k_stride + (i - a.Hq) * kHeadDim : a.v + in * a.v_stride + (i - a.Hq - a.Hkv) * kHeadDim;
+    };
+    constexpr int kBatch = 2;  // rows of a group on their way at a time
+    uint4 raw[kBatch][2];
+    auto fetch = [&](int i0) {
+#pragma unroll
+        for (int u = 0; u < kBatch; u++) {
+            const int i = i0 + u * kGroups + group;
+            raw[u][0] = raw[u][1] = make_uint4(0u, 0u, 0u, 0u);
+            if (i < rows) {
+                raw[u][0] = ld_plain(reinterpret_cast<const uint4*>(source(i)) + p);
+                raw[u][1] = ld_plain(reinterpret_cast<const uint4*>(source(i)) + 8 + p);
+            }
+        }
+    };
     pdl_wait();
     pdl_trigger();  // (after the wait: the next kernel reads lengths and pages before its own)
-    const int tid = threadIdx.x, p = tid & 7, group = tid >> 3, s = blockIdx.x, j = blockIdx.y;
-    const int len = seq_len(a, s), nodes = seq_nodes(a, s), tail = len % kKeys, b = j - tail;
-    const bool needed = j < (tail + nodes) / kKeys * kKeys + kKeys;
-    auto put_side = [&](int kv, int head, const uint4& lo, const uint4& hi) {
+    if (b <= a.B) fetch(0);  // (whatever the length and the number of nodes are)
+    const int depth = b > 0 && b <= a.B ? ld_plain(a.depths + static_cast<long long>(s) * a.B + b - 1) : 0;
+    const int len = seq_len(a, s), nodes = seq_nodes(a, s), tail = len % kKeys;
+    const int end = (tail + nodes) / kKeys * kKeys + kKeys;  // side rows that a tile reads
+    auto put_side = [&](int kv, int head, int j, const uint4& lo, const uint4& hi) {
         uint4* d = kv ? ta.side_v : ta.side_k;
         const long long row = (static_cast<long long>(s) * a.Hkv + head) * ta.sk + j;
         if (kFp8) {
@@ -175,15 +197,18 @@ __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_c
             d[row * 16 + 8 + p] = hi;
         }
     };
-    auto put_scale = [&](int kv, int head, float x) {
+    auto put_scale = [&](int kv, int head, int j, float x) {
         if (kFp8 && p == 0) (kv ? ta.side_vs : ta.side_ks)[(static_cast<long long>(s) * a.Hkv + head) * ta.sk + j] = x;
     };
-    if (b < 0) {
-        // a token of the cache: its codes or values as they are
+    if (b > a.B) {
+        int j = b - a.B - 1;  // of the side rows that are no tree rows: before them, then after them
+        if (j >= tail) j += nodes + 1;
+        if (j >= end) return;
+        // a token of the cache: its codes or values as they are; zeros after the nodes
         const int key = len - tail + j;
-        const int page = ld_plain(a.table + static_cast<long long>(s) * a.max_pages + (key >> a.page_log2));
+        const int page = j < tail ? ld_plain(a.table + static_cast<long long>(s) * a.max_pages + (key >> a.page_log2)) : -1;
         const bool there = page >= 0 && page < a.num_pages;
-        if (!there && a.status && tid == 0) atomicOr(a.status, kDevBounds);
+        if (j < tail && !there && a.status && tid == 0) atomicOr(a.status, kDevBounds);
         for (int i = group; i < 2 * a.Hkv; i += kGroups) {
             const int kv = i >= a.Hkv, head = i - kv * a.Hkv;
             const long long row = there ? ((static_cast<long long>(page) * a.Hkv + head) << a.page_log2) + (key & ((1 << a.page_log2) - 1)) : 0;
@@ -197,52 +222,24 @@ __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_c
                 lo = reinterpret_cast<const uint4*>(pool)[row * 16 + p];
                 hi = reinterpret_cast<const uint4*>(pool)[row * 16 + 8 + p];
             }
-            put_side(kv, head, lo, hi);
-            if (kFp8) put_scale(kv, head, there ? ld_plain((kv ? a.vs : a.ks) + row) : 1.0f);
+            put_side(kv, head, j, lo, hi);
+            if (kFp8) put_scale(kv, head, j, there ? ld_plain((kv ? a.vs : a.ks) + row) : 0.0f);
         }
         return;
     }
-    if (b > nodes) {
-        // no tree row: zeros where a tile reads them, and as output of rows that are no node
-        if (needed)
-            for (int i = group; i < 2 * a.Hkv; i += kGroups) {
-                const int kv = i >= a.Hkv, head = i - kv * a.Hkv;
-                put_side(kv, head, make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u));
-                put_scale(kv, head, 0.0f);
-            }
-        if (b <= a.B) {
-            uint4* out = reinterpret_cast<uint4*>(a.out + (static_cast<long long>(s) * (a.B + 1) + b) * a.Hq * kHeadDim);
-            for (int i = tid; i < a.Hq * 16; i += kPrepThreads) out[i] = make_uint4(0u, 0u, 0u, 0u);
-        }
+    if (b > nodes) {  // no node: zeros as output
+        uint4* out = reinterpret_cast<uint4*>(a.out + in * a.Hq * kHeadDim);
+        for (int i = tid; i < a.Hq * 16; i += kPrepThreads) out[i] = make_uint4(0u, 0u, 0u, 0u);
         return;
     }
-    const long long in = static_cast<long long>(s) * (a.B + 1) + b;
-    const int rows = a.Hq + 2 * a.Hkv;  // queries, keys, values
-    auto source = [&](int i) {
-        return i < a.Hq ? a.q + in * a.q_stride + i * kHeadDim
-                        : i < a.Hq + a.Hkv ? a.k + in * a.k_stride + (i - a.Hq) * kHeadDim : a.v + in * a.v_stride + (i - a.Hq - a.Hkv) * kHeadDim;
-    };
-    constexpr int kBatch = 2;  // rows of a group on their way at a time
+    if (tid < kHeadDim / 2) {
+        float sn, cs;
+        rope_sincos(a.turns.f[tid], len + depth, &sn, &cs);
+        turn_of[tid] = make_float2(cs, sn);
+    }
+    __syncthreads();
     for (int i0 = 0; i0 < rows; i0 += kBatch * kGroups) {
-        uint4 raw[kBatch][2];
-#pragma unroll
-        for (int u = 0; u < kBatch; u++) {
-            const int i = i0 + u * kGroups + group;
-            raw[u][0] = raw[u][1] = make_uint4(0u, 0u, 0u, 0u);
-            if (i < rows) {
-                raw[u][0] = ld_plain(reinterpret_cast<const uint4*>(source(i)) + p);
-                raw[u][1] = ld_plain(reinterpret_cast<const uint4*>(source(i)) + 8 + p);
-            }
-        }
-        if (i0 == 0) {  // the position's angles meanwhile
-            const int pos = len + (b > 0 ? ld_plain(a.depths + static_cast<long long>(s) * a.B + b - 1) : 0);
-            if (tid < kHeadDim / 2) {
-                float sn, cs;
-                rope_sincos(a.turns.f[tid], pos, &sn, &cs);
-                turn_of[tid] = make_float2(cs, sn);
-            }
-            __syncthreads();
-        }
+        if (i0 > 0) fetch(i0);
 #pragma unroll
         for (int u = 0; u < kBatch; u++) {
             if (i0 + u * kGroups >= rows) break;  // (whole warps stay together)
@@ -267,8 +264,8 @@ __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_c
                 if (kFp8 && p == 0) ta.q_scale[tile * kRows + (row & 127)] = factor * a.sl2;
             } else if (i < rows) {
                 const int kv = i >= a.Hq + a.Hkv, head = i - a.Hq - kv * a.Hkv;
-                put_side(kv, head, lo, hi);
-                put_scale(kv, head, factor);
+                put_side(kv, head, tail + b, lo, hi);
+                put_scale(kv, head, tail + b, factor);
             }
         }
     }
@@ -289,6 +286,7 @@ __device__ __forceinline__ float above(float x) {
 // the tiles kernel costs 0.8 us a tile of every unit, and this 2 us a tile once.
 __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant__ TileArgs ta, const uint8_t* pool_k, const uint8_t* pool_v) {
     __shared__ float scale_of[2 * kKeys];
+    __shared__ int row_of[kKeys];  // of the pool; -1: no such page
     __shared__ float top_of[8];
     const PagedArgs& a = ta.p;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -298,25 +296,33 @@ __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant_
     const int len = seq_len(a, s), nodes = seq_nodes(a, s), whole = len / kKeys, tail = len % kKeys;
     if (t > whole + (tail + nodes) / kKeys) return;
     const bool cache_tile = t < whole;
-    auto pool_row = [&](int key) -> long long {  // of a key of the tile; -1: no such page
-        const int at = t * kKeys + key;
-        const int page = ld_plain(a.table + static_cast<long long>(s) * a.max_pages + (at >> a.page_log2));
-        if (page < 0 || page >= a.num_pages) return -1;
-        return ((static_cast<long long>(page) * a.Hkv + head) << a.page_log2) + (at & ((1 << a.page_log2) - 1));
-    };
     const long long side = (static_cast<long long>(s) * a.Hkv + head) * ta.sk + (t - whole) * kKeys;
+    if (cache_tile && tid < kKeys) {
+        const int at = t * kKeys + tid;
+        const int page = ld_plain(a.table + static_cast<long long>(s) * a.max_pages + (at >> a.page_log2));
+        const bool there = page >= 0 && page < a.num_pages;
+        if (!there && a.status) atomicOr(a.status, kDevBounds);
+        row_of[tid] = there ? static_cast<int>(((static_cast<long long>(page) * a.Hkv + head) << a.page_log2) + (at & ((1 << a.page_log2) - 1))) : -1;
+    }
+    __syncthreads();
+    // groups of 8 lanes a row, 16 elements a lane: on their way while the scales are compared
+    const int p = tid & 7, group = tid >> 3;
+    constexpr int kRounds = 2 * kKeys / 32;
+    uint4 c[kRounds];
+    if (cache_tile)
+#pragma unroll
+        for (int i = 0; i < kRounds; i++) {
+            const int row = row_of[(i * 32 + group) & 127];
+            c[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (row >= 0) c[i] = ld_plain(reinterpret_cast<const uint4*>(i >= kRounds / 2 ? pool_v : pool_k) + static_cast<long long>(row) * 8 + p);
+        }
     {
         const int kv = tid >> 7, key = tid & 127;
         float sc = 0.0f;
-        if (cache_tile) {
-            const long long row = pool_row(key);
-            if (row >= 0)
-                sc = ld_plain((kv ? a.vs : a.ks) + row);
-            else if (a.status)
-                atomicOr(a.status, kDevBounds);
-        } else {
+        if (!cache_tile)
             sc = __ldcg((kv ? ta.side_vs : ta.side_ks) + side + key);
-        }
+        else if (row_of[key] >= 0)
+            sc = ld_plain((kv ? a.vs : a.ks) + row_of[key]);
         scale_of[tid] = sc;
         const float top = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(fmaxf(sc, 0.0f))));
         if (lane == 0) top_of[warp] = top;
@@ -327,18 +333,13 @@ __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant_
     for (int kv = 0; kv < 2; kv++) ref[kv] = above(fmaxf(fmaxf(top_of[4 * kv], top_of[4 * kv + 1]), fmaxf(top_of[4 * kv + 2], top_of[4 * kv + 3])));
     const long long tile = (static_cast<long long>(s) * a.Hkv + head) * ta.wide_tiles + t;
     if (tid == 0) ta.wide_refs[tile] = make_float2(ref[0], ref[1]);
-    // groups of 8 lanes a row, 16 elements a lane
-    const int p = tid & 7, group = tid >> 3;
 #pragma unroll
-    for (int i = 0; i < 2 * kKeys / 32; i++) {
-        const int kv = i >= kKeys / 32, key = (i * 32 + group) & 127;
+    for (int i = 0; i < kRounds; i++) {
+        const int kv = i >= kRounds / 2, key = (i * 32 + group) & 127;
         const __half2 by = __float2half2_rn(scale_of[kv * kKeys + key] * __uint_as_float(0x7F000000u - __float_as_uint(ref[kv])));
         uint32_t x[8];
         if (cache_tile) {
-            const long long row = pool_row(key);
-            uint4 c = make_uint4(0u, 0u, 0u, 0u);
-            if (row >= 0) c = ld_plain(reinterpret_cast<const uint4*>(kv ? pool_v : pool_k) + row * 8 + p);
-            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+            const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
 #pragma unroll
             for (int e = 0; e < 4; e++) {
                 x[2 * e] = codes_to_f16(w[e]);
@@ -346,15 +347,15 @@ __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant_
             }
         } else {
             const uint4* src = (kv ? ta.side_v : ta.side_k) + (side >> 7) * (16 * kKeys) + key;
-            const uint4 c = __ldcg(src + 2 * p * kKeys), d = __ldcg(src + (2 * p + 1) * kKeys);
-            x[0] = c.x;
-            x[1] = c.y;
-            x[2] = c.z;
-            x[3] = c.w;
-            x[4] = d.x;
-            x[5] = d.y;
-            x[6] = d.z;
-            x[7] = d.w;
+            const uint4 y = __ldcg(src + 2 * p * kKeys), z = __ldcg(src + (2 * p + 1) * kKeys);
+            x[0] = y.x;
+            x[1] = y.y;
+            x[2] = y.z;
+            x[3] = y.w;
+            x[4] = z.x;
+            x[5] = z.y;
+            x[6] = z.z;
+            x[7] = z.w;
         }
 #pragma unroll
         for (int e = 0; e < 8; e++) {
@@ -664,7 +665,8 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
             w.p = list.find(a, shares.begin(blockIdx.x), lane);
         }
         if (threadIdx.x == 0) {
-            a.plan->places[blockIdx.x] = make_int4(w.p.s, w.p.head * 256 + w.p.qt, w.p.tile, 0);
+            a.plan->places[blockIdx.x] = make_int4(w.p.s, w.p.head * 256 + w.p.qt, w.p.tile, w.left > 0 ? w.p.tiles(a, w.p.qt) : 0);
+            a.plan->nodes[blockIdx.x] = w.p.nodes;
             if (blockIdx.x == 0) a.plan->count = shares.count;
         }
     }
@@ -1126,41 +1128,44 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
 // share i - 1 began: 16 rows each, 16 threads (8 elements each) a row.
 __global__ void __launch_bounds__(256) paged_tiles_join_kernel(const __grid_constant__ PagedArgs a) {
     pdl_trigger();
-    const int tid = threadIdx.x, i = blockIdx.x / 8 + 1, eighth = blockIdx.x % 8;
+    const int tid = threadIdx.x, lane = tid & 31, i = blockIdx.x / 8 + 1, eighth = blockIdx.x % 8;
     pdl_wait();
-    const int count = a.plan->count;
-    if (i >= count) return;
+    // all that has to be known in one go (the kernel is a chain of loads)
+    const int count = a.plan->count, nodes = a.plan->nodes[i];
     const int4 at = a.plan->places[i], prev = a.plan->places[i - 1];
-    if (at.z == 0 || (prev.x == at.x && prev.y == at.y && prev.z > 0)) return;
-    TilePlace p{};
-    p.s = at.x;
-    p.head = at.y / 256;
-    p.qt = at.y % 256;
-    p.load(a);
-    const int tiles = p.tiles(a, p.qt), s = p.s, head = p.head;
-    if (at.z >= tiles) return;  // (the unit ended in share i - 1)
-    const int r = eighth * 16 + (tid & 15), d8 = tid >> 4, row = p.qt * kRows + r, b = row >> a.g_log2;
-    if (b > p.nodes) return;
-    auto in_unit = [&](int c) {
-        if (c >= count) return false;
-        const int4 x = a.plan->places[c];
-        return x.x == at.x && x.y == at.y && x.z < tiles;
-    };
+    const int4 next = a.plan->places[min(i + 1 + lane, kMaxSms - 1)];
+    if (i >= count || at.z == 0 || at.z >= at.w) return;  // (from at.w on the place stands for a unit's other costs)
+    if (prev.x == at.x && prev.y == at.y && prev.z > 0) return;
+    const int s = at.x, head = at.y / 256, qt = at.y % 256;
+    const int r = eighth * 16 + (tid & 15), d8 = tid >> 4, row = qt * kRows + r, b = row >> a.g_log2;
     const int c0 = i - 1;
-    int c1 = i;
-    while (in_unit(c1 + 1)) c1++;
+    int c1 = i;  // the last share that holds tiles of the unit
+    {
+        const unsigned out = __ballot_sync(kFull, !(i + 1 + lane < count && next.x == at.x && next.y == at.y && next.z < at.w));
+        if (out) {
+            c1 += __ffs(out) - 1;
+        } else {
+            c1 += 32;
+            for (; c1 + 1 < count; c1++) {
+                const int4 x = a.plan->places[c1 + 1];
+                if (x.x != at.x || x.y != at.y || x.z >= at.w) break;
+            }
+        }
+    }
+    if (b > nodes) return;
     float top = -INFINITY, l = 0.0f, o[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
     for (int c = c0; c <= c1; c++) {
         const TilePart* x = static_cast<const TilePart*>(a.parts) + 2 * c + (c < i ? 1 : 0);
         const float2 ml = x->ml[r];
         const float4 y = x->o[2 * d8][r], z = x->o[2 * d8 + 1][r];
-        if (ml.x == -INFINITY) continue;
-        const float up = fmaxf(top, ml.x), old = top == -INFINITY ? 0.0f : ex2(top - up), by = ex2(ml.x - up);
+        const bool any = ml.x != -INFINITY;
+        const float up = fmaxf(top, ml.x), old = top == -INFINITY ? 0.0f : ex2(top - up), by = any ? ex2(ml.x - up) : 0.0f;
         top = up;
-        l = l * old + ml.y * by;
+        l = l * old + (any ? ml.y * by : 0.0f);
         const float v[8] = {y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
 #pragma unroll
-        for (int k = 0; k < 8; k++) o[k] = o[k] * old + v[k] * by;
+        for (int k = 0; k < 8; k++) o[k] = o[k] * old + (any ? v[k] * by : 0.0f);
     }
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
     __nv_bfloat16* d = a.out + ((static_cast<long long>(s) * (a.B + 1) + b) * a.Hq + head * a.G + (row & (a.G - 1))) * kHeadDim + 8 * d8;
@@ -1251,7 +1256,8 @@ int launch_paged_tiles(PagedArgs a, const dart_kv_cache& cache, uint8_t* workspa
         tmSk = tmK;  // (side tiles lie among the others)
         tmSv = tmV;
     }
-    const dim3 prep(static_cast<unsigned>(a.nseq), static_cast<unsigned>(w.sk));
+    // tree rows, up to 127 cache tokens before them, up to 127 rows of zeros after them
+    const dim3 prep(static_cast<unsigned>(a.nseq), static_cast<unsigned>(a.B + 1 + 2 * (kKeys - 1)));
     const uint8_t *pk = static_cast<const uint8_t*>(cache.k), *pv = static_cast<const uint8_t*>(cache.v);
     cudaError_t e = fp8 ? launch_pdl(paged_prep_kernel<true>, prep, dim3(kPrepThreads), 0, st, ta, pk, pv)
                         : launch_pdl(paged_prep_kernel<false>, prep, dim3(kPrepThreads), 0, st, ta, pk, pv);
