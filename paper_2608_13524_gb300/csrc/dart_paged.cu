@@ -1,7 +1,7 @@
 // Tree attention over the paged cache.  Contract: include/dart_cache.h.
 //
 // paged_rows_kernel: few query rows a sequence (decoding), bound by HBM.  A
-// unit of work is 16 query rows of one kv head of one sequence (a row = a tree
+// unit of work is the query rows of one kv head of one sequence (a row = a tree
 // row and one of the G query heads that share the kv head) against all keys
 // that the rows may see: the sequence's cache, then its tree rows, in chunks
 // of 16 (bf16) or 32 (e4m3) keys.  The chunks of all units form one list,
@@ -12,10 +12,13 @@
 // waits for another.  Units that several warps share are left as partial
 // results in the workspace, which paged_join_kernel joins in order.
 //
-// The products are warp-wide 16 x 8 x 16 matrix instructions: with at most 16
-// rows a chunk of 16 bf16 keys takes 8 KB from HBM for 32 of them, far below
-// any tensor rate, and scores and probabilities stay in registers (a 128-row
-// tile of the tensor-memory path would be 7/8 empty).
+// The products are warp-wide 16 x 8 x 16 matrix instructions with keys (for
+// S^T = K Q^T) and head dimensions (O^T = V^T P^T) along the 16 and rows along
+// the 8, once for up to 8 rows and twice (kN = 2) for up to 16: with rows along
+// the 16, 8 rows took as many products and accumulators as 16.  A chunk of 16
+// bf16 keys takes 8 KB from HBM for 24 kN of them, far below any tensor rate,
+// and scores and probabilities stay in registers (a 128-row tile of the
+// tensor-memory path would be 7/8 empty or more).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -47,15 +50,16 @@ bool encode_rows(CUtensorMap* m, const void* base, long long rows, bool fp8, int
 
 namespace {
 
-constexpr int kUnitRows = 16;
-constexpr int kWarps = 8;
-constexpr int kThreads = kWarps * 32;
 constexpr float kSlack = 8.0f;  // log2 units a score may exceed the row's reference by
 
+template <int kN>
 struct Part {  // a unit's partial result
-    float o[kUnitRows][kHeadDim];
-    float2 ml[kUnitRows];  // reference (log2 units), sum
+    float o[8 * kN][kHeadDim];
+    float2 ml[8 * kN];  // reference (log2 units), sum
 };
+
+// Warps of a CTA: as many as their registers allow.
+__host__ __device__ constexpr int rows_warps(int n) { return n == 1 ? 12 : 8; }
 
 // ------------------------------------------------------------ the schedule
 
@@ -68,12 +72,11 @@ struct Chunk {
     static constexpr int kUnitCost = kFp8 ? 4 : 6;
 };
 
-// A place in the list of chunks: sequence, unit of the sequence (row group
-// fastest, then kv head), chunk of the unit.
+// A place in the list of chunks: sequence, kv head, chunk of the unit.
 template <bool kFp8>
 struct Place {
-    int s, unit, chunk;
-    int len, nodes, ctx_chunks, chunks, cost, units;  // of the sequence; cost: the unit's length in the list
+    int s, head, chunk;
+    int len, nodes, ctx_chunks, chunks, cost;  // of the sequence; cost: the unit's length in the list
     __device__ __forceinline__ void load(const PagedArgs& a) {
         constexpr int kKeys = Chunk<kFp8>::kKeys;
         len = seq_len(a, s);
@@ -81,13 +84,11 @@ struct Place {
         ctx_chunks = (len + kKeys - 1) / kKeys;
         chunks = ctx_chunks + (nodes + 1 + 15) / 16;  // (tree rows: 16 at a time)
         cost = chunks + Chunk<kFp8>::kUnitCost;
-        units = a.Hkv * ((((nodes + 1) << a.g_log2) + kUnitRows - 1) / kUnitRows);
     }
-    __device__ __forceinline__ int groups(const PagedArgs& a) const { return units / a.Hkv; }
     __device__ __forceinline__ void next_unit(const PagedArgs& a) {
         chunk = 0;
-        if (++unit == units) {
-            unit = 0;
+        if (++head == a.Hkv) {
+            head = 0;
             if (++s < a.nseq) load(a);
         }
     }
@@ -103,7 +104,7 @@ struct List {
         Place<kFp8> p{};
         p.s = s;
         p.load(a);
-        return static_cast<long long>(p.units) * p.cost;
+        return static_cast<long long>(a.Hkv) * p.cost;
     }
     __device__ __forceinline__ List(const PagedArgs& a, int lane) {
         own = length(a, lane);
@@ -130,8 +131,8 @@ struct List {
                 const long long rest = x - done - __shfl_sync(kFull, upto - n, l);
                 r.s = s0 + l;
                 r.load(a);
-                r.unit = place_div(rest, r.cost);
-                r.chunk = static_cast<int>(rest - static_cast<long long>(r.unit) * r.cost);
+                r.head = place_div(rest, r.cost);
+                r.chunk = static_cast<int>(rest - static_cast<long long>(r.head) * r.cost);
                 return r;
             }
             done += __shfl_sync(kFull, upto, 31);
@@ -158,14 +159,30 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Two e4m3 codes (low, high byte) as an f16 pair: exact.
-__device__ __forceinline__ uint32_t e4m3_to_f16(uint32_t two) {
+// The e4m3 codes of the low or the high half of a word as an f16 pair: exact.
+__device__ __forceinline__ uint32_t codes_lo(uint32_t w) {
     uint32_t r;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(static_cast<uint16_t>(two)));
+    asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %1;\n cvt.rn.f16x2.e4m3x2 %0, l;\n}" : "=r"(r) : "r"(w));
     return r;
 }
-// Row of a 16-key chunk behind key slot (n-tile q, column n) of the products:
-// chosen so that both the reads of K (lanes g, t: row slot_row(q, g), 16-byte
+__device__ __forceinline__ uint32_t codes_hi(uint32_t w) {
+    uint32_t r;
+    asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %1;\n cvt.rn.f16x2.e4m3x2 %0, h;\n}" : "=r"(r) : "r"(w));
+    return r;
+}
+// The transpose of an 8 x 8 matrix of 16-bit values (lane 4 r + c: row r,
+// columns 2 c, 2 c + 1).
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+// Row of a 16-key chunk behind key slot 8 q + n of the products: chosen so that
+// both the reads of K (lanes g, t: row slot_row(q, g), 16-byte
 // pieces t, t + 4, ...) and of V (rows slot_row(q, 2t + e), piece g) touch
 // every bank once under the 128-byte swizzle.
 __device__ __forceinline__ int slot_row(int q, int n) {
@@ -176,22 +193,18 @@ __device__ __forceinline__ uint32_t swz(int row, int piece) {  // byte offset in
     return static_cast<uint32_t>(row * 128 + ((piece ^ (row & 7)) << 4));
 }
 
-template <bool kFp8>
+template <bool kFp8, int kN>
 struct Geo {
     static constexpr int kKeys = Chunk<kFp8>::kKeys;
     static constexpr int kSubs = kKeys / 16;                             // products of 16 keys
     static constexpr int kTile = kKeys * kHeadDim * (kFp8 ? 1 : 2);      // K or V of a chunk
-    static constexpr int kStages = 3;
+    static constexpr int kWarps = rows_warps(kN), kThreads = 32 * kWarps;
+    static constexpr int kStages = kN == 1 ? 2 : 3;
     static constexpr int kRing = kWarps * kStages * 2 * kTile;           // 192 KB
     static constexpr int kScales = kFp8 ? kWarps * kStages * 2 * kKeys * 4 : 0;
     static constexpr int kSmem = kRing + kScales + kWarps * kStages * 8;
 };
 
-// Element of the head behind column n of n-tile j of the output products.
-template <bool kFp8>
-__device__ __forceinline__ int out_dim(int n, int j) {
-    return kFp8 ? 16 * n + j : (j < 8 ? 8 * n + j : 64 + 8 * n + j - 8);
-}
 // 16-byte piece (8 bf16) of a row of the head that step pair i of thread t
 // covers; i and i + 2 are 64 elements apart, as RoPE's pairs are.
 template <bool kFp8>
@@ -199,11 +212,12 @@ __device__ __forceinline__ int k_piece(int i, int t) {
     return kFp8 ? 8 * (i >> 1) + 2 * t + (i & 1) : 8 * (i >> 1) + t + 4 * (i & 1);
 }
 
-template <bool kFp8>
-__global__ void __launch_bounds__(kThreads, 1)
+template <bool kFp8, int kN>
+__global__ void __launch_bounds__(32 * rows_warps(kN), 1)
     paged_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                       const __grid_constant__ PagedArgs a) {
-    using G_ = Geo<kFp8>;
+    using G_ = Geo<kFp8, kN>;
+    constexpr int kWarps = G_::kWarps, kThreads = G_::kThreads;
     constexpr int kKeys = G_::kKeys, kSubs = G_::kSubs, kTile = G_::kTile, kStages = G_::kStages;
     extern __shared__ __align__(1024) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -234,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     long long left = shares.length(share);  // places of this share not yet worked on
     Place<kFp8> use = list.find(a, shares.begin(share), lane), load = use;
     if (lane == 0) {
-        a.plan->places[share] = make_int4(use.s, use.unit, use.chunk, use.chunks);
+        a.plan->places[share] = make_int4(use.s, use.head, use.chunk, use.chunks);
         a.plan->nodes[share] = use.nodes;
         if (share == 0) a.plan->count = shares.count;
     }
@@ -242,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     int n_load = 0, n_use = 0;
     int failed = 0;
     volatile int* abort = &failed;
-    const uint64_t policy = (a.B + 1) * a.G <= kUnitRows ? l2_policy_evict_first() : l2_policy_evict_last();
+    const uint64_t policy = l2_policy_evict_first();  // (every key is read once)
     const int page_mask = (1 << a.page_log2) - 1;
 
     // Moves `load` to the next chunk of the cache in this share (or past it).
@@ -265,7 +279,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto issue = [&]() {  // loads the chunk at `load`
         if (lane == 0) {
             const int st = n_load % kStages;
-            const int head = load.unit / load.groups(a);
             uint8_t* k = ring + st * 2 * kTile;
             uint8_t* v = k + kTile;
             float* sc = scales + st * 2 * kKeys;
@@ -278,7 +291,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int key = load.chunk * kKeys + 16 * h;
                 if (h == 0 || key < load.len) {
                     if (page[h] >= 0 && page[h] < a.num_pages)
-                        row = ((static_cast<long long>(page[h]) * a.Hkv + head) << a.page_log2) + (key & page_mask);
+                        row = ((static_cast<long long>(page[h]) * a.Hkv + load.head) << a.page_log2) + (key & page_mask);
                     else if (a.status)
                         atomicOr(a.status, kDevBounds);
                 }
@@ -306,20 +319,19 @@ __global__ void __launch_bounds__(kThreads, 1)
     while (left > 0) {
         // ---- this warp's part of a unit: chunks [c0, c1)
         const int c0 = use.chunk, c1 = static_cast<int>(min(static_cast<long long>(use.chunks), c0 + left));
-        const int groups = use.groups(a), head = use.unit / groups, row0 = (use.unit % groups) * kUnitRows;
-        const int s = use.s, len = use.len, nodes = use.nodes, ctx_chunks = use.ctx_chunks, chunks = use.chunks;
+        const int s = use.s, head = use.head, len = use.len, nodes = use.nodes, ctx_chunks = use.ctx_chunks, chunks = use.chunks;
         const long long seq_row = static_cast<long long>(s) * (a.B + 1);
         left -= use.cost - c0;
         use.next_unit(a);
         if (c0 >= c1) continue;  // (the part of a unit's length that stands for its other costs)
 
-        // the rows' queries, rotated, as operands: rows g and g + 8, step pair i
-        // covers the 8 elements of piece k_piece(i, t) in steps 2 i, 2 i + 1
-        uint32_t q[8][4], lo[8][4];
-        float rs[2];  // scores in log2 units = products * rs
+        // the queries of rows 8 n + g, rotated, as operands: step pair i covers the 8
+        // elements of piece k_piece(i, t) in steps 2 i, 2 i + 1
+        uint32_t q[kN][8][2], lo[kN][8][2];
+        float rs[kN][2];  // of rows 8 n + 2 t, + 1: scores in log2 units = products * rs
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const int r = row0 + g + 8 * h, b = r >> a.g_log2;
+        for (int n = 0; n < kN; n++) {
+            const int r = 8 * n + g, b = r >> a.g_log2;
             float x[4][8];
 #pragma unroll
             for (int i = 0; i < 4; i++)
@@ -344,11 +356,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 }
             }
-            rs[h] = a.sl2;
-            float down = 1.0f;
+            float down = 1.0f, up = a.sl2;
             if (kFp8) {
                 // scaled by a power of two to a largest element in [1, 2): f16 then
-                // rounds it to 2^-11 whatever the queries' magnitude
+                // rounds it to 2^-11 whatever the query's magnitude
                 float mx = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 4; i++)
@@ -358,104 +369,135 @@ __global__ void __launch_bounds__(kThreads, 1)
                 mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, 2));
                 const int ex = min(max(static_cast<int>(__float_as_uint(mx) >> 23) - 127, -100), 120);
                 down = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
-                rs[h] *= __uint_as_float(static_cast<uint32_t>(127 + ex) << 23);
+                up *= __uint_as_float(static_cast<uint32_t>(127 + ex) << 23);
             }
+            rs[n][0] = __shfl_sync(kFull, up, 8 * t);
+            rs[n][1] = __shfl_sync(kFull, up, 8 * t + 4);
 #pragma unroll
             for (int i = 0; i < 4; i++)
 #pragma unroll
                 for (int e = 0; e < 4; e++) {  // words of the piece: elements 2 e, 2 e + 1
                     uint32_t w;
                     if (kFp8) {
-                        const __half2 hw = __floats2half2_rn(x[i][2 * e] * down, x[i][2 * e + 1] * down);
-                        w = *reinterpret_cast<const uint32_t*>(&hw);
+                        w = pack_f16(x[i][2 * e] * down, x[i][2 * e + 1] * down);
                     } else {
                         // bf16 and what it leaves: with one bf16 term the queries' rounding
                         // alone would move the output as much as its own rounding does
                         w = pack_bf16x2(x[i][2 * e], x[i][2 * e + 1]);
-                        lo[2 * i + (e >> 1)][h + 2 * (e & 1)] = pack_bf16x2(x[i][2 * e] - bf16_lo(w), x[i][2 * e + 1] - bf16_hi(w));
+                        lo[n][2 * i + (e >> 1)][e & 1] = pack_bf16x2(x[i][2 * e] - bf16_lo(w), x[i][2 * e + 1] - bf16_hi(w));
                     }
-                    q[2 * i + (e >> 1)][h + 2 * (e & 1)] = w;
+                    q[n][2 * i + (e >> 1)][e & 1] = w;
                 }
         }
-        float acc[16][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+        // O^T: product j has elements j of piece g (bf16 pages) or 16 g + j (e4m3) in [0, 1],
+        // the same 64 (bf16) or 8 further in [2, 3], of rows 8 n + 2 t, + 1
+        float acc[kN][8][4], m[kN][2], l[kN][2];
         // e4m3: the accumulators are in units of vref / 128, vref a power of two
         // above every value scale so far, so that f16 probabilities (p <= 2^8 times
         // scale / vref <= 1 times 2^7) neither overflow nor lose small weights
         // (2^-31 of the largest still counts)
         float vref = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 16; j++)
+        for (int n = 0; n < kN; n++) {
+            m[n][0] = m[n][1] = -INFINITY;
+            l[n][0] = l[n][1] = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 4; e++) acc[j][e] = 0.0f;
+            for (int j = 0; j < 8; j++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) acc[n][j][e] = 0.0f;
+        }
 
-        // New scores sc[.][2 h + e] of rows g + 8 h: raises the references where one is
-        // exceeded by more than 2^8, and turns the scores into probabilities.
+        // New scores sc[sub][n][2 qq + e] of key slot 8 qq + g and row 8 n + 2 t + e:
+        // raises the references where one is exceeded by more than 2^8, and turns the
+        // scores into probabilities.
         auto soften = [&](auto& sc) {
-            constexpr int n = sizeof(sc) / sizeof(sc[0]);
-            float mx[2] = {-INFINITY, -INFINITY};
+            constexpr int subs = sizeof(sc) / sizeof(sc[0]);
+            float mx[kN][2];
+            bool over = false;
 #pragma unroll
-            for (int j = 0; j < n; j++)
+            for (int n = 0; n < kN; n++)
 #pragma unroll
-                for (int h = 0; h < 2; h++) mx[h] = fmaxf(mx[h], fmaxf(sc[j][2 * h], sc[j][2 * h + 1]));
-            if (__any_sync(kFull, mx[0] > m[0] + kSlack || mx[1] > m[1] + kSlack)) {
+                for (int e = 0; e < 2; e++) {
+                    mx[n][e] = -INFINITY;
 #pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    float x = fmaxf(mx[h], __shfl_xor_sync(kFull, mx[h], 1));
-                    x = fmaxf(m[h], fmaxf(x, __shfl_xor_sync(kFull, x, 2)));
-                    const float alpha = m[h] == -INFINITY ? 0.0f : exp2_fast(m[h] - x);
-                    m[h] = x;
-                    l[h] *= alpha;
-#pragma unroll
-                    for (int j = 0; j < 16; j++) {
-                        acc[j][2 * h] *= alpha;
-                        acc[j][2 * h + 1] *= alpha;
-                    }
+                    for (int j = 0; j < subs; j++) mx[n][e] = fmaxf(mx[n][e], fmaxf(sc[j][n][e], sc[j][n][2 + e]));
+                    over |= mx[n][e] > m[n][e] + kSlack;
                 }
-            }
+            if (__any_sync(kFull, over)) {
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const float ref = m[h] == -INFINITY ? 0.0f : m[h];
-#pragma unroll
-                for (int j = 0; j < n; j++)
+                for (int n = 0; n < kN; n++)
 #pragma unroll
                     for (int e = 0; e < 2; e++) {
-                        const float w = exp2_fast(sc[j][2 * h + e] - ref);
-                        l[h] += w;
-                        sc[j][2 * h + e] = w;
+                        float x = mx[n][e];
+#pragma unroll
+                        for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(kFull, x, o));
+                        x = fmaxf(m[n][e], x);
+                        const float alpha = m[n][e] == -INFINITY ? 0.0f : exp2_fast(m[n][e] - x);
+                        m[n][e] = x;
+                        l[n][e] *= alpha;
+#pragma unroll
+                        for (int j = 0; j < 8; j++) {
+                            acc[n][j][e] *= alpha;
+                            acc[n][j][2 + e] *= alpha;
+                        }
                     }
             }
-        };
-        // O += P V of 16 keys with bf16 values: word(half, q, e) = 16 bytes of key
-        // slot (q, e): piece g of each half of the row (bf16 pages), or
-        // pieces 2 g, 2 g + 1 (tree rows beside e4m3 pages)
-        auto values_bf16 = [&](const uint32_t (&p)[4], auto&& piece) {
 #pragma unroll
-            for (int half = 0; half < 2; half++) {
-                uint32_t x[2][2][4];
+            for (int n = 0; n < kN; n++)
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    const float ref = m[n][e] == -INFINITY ? 0.0f : m[n][e];
+#pragma unroll
+                    for (int j = 0; j < subs; j++)
+#pragma unroll
+                        for (int qq = 0; qq < 2; qq++) {
+                            const float w = exp2_fast(sc[j][n][2 * qq + e] - ref);
+                            l[n][e] += w;
+                            sc[j][n][2 * qq + e] = w;
+                        }
+                }
+        };
+        // O^T += V^T P^T of 16 keys with bf16 values: piece(half, q, e) = 16 bytes of
+        // key slot (q, 2 t + e): piece g of each half of the row (bf16 pages), or
+        // pieces 2 g, 2 g + 1 (tree rows beside e4m3 pages)
+        auto values_bf16 = [&](const float (&w)[kN][4], auto&& piece) {
+            uint32_t p[kN][2];
+#pragma unroll
+            for (int n = 0; n < kN; n++) {
+                p[n][0] = transpose_8x8(pack_bf16x2(w[n][0], w[n][1]));
+                p[n][1] = transpose_8x8(pack_bf16x2(w[n][2], w[n][3]));
+            }
+            uint32_t x[2][2][2][4];  // [half][q][e][word]
+#pragma unroll
+            for (int half = 0; half < 2; half++)
 #pragma unroll
                 for (int qq = 0; qq < 2; qq++)
 #pragma unroll
                     for (int e = 0; e < 2; e++) {
                         const uint4 y = piece(half, qq, e);
-                        x[qq][e][0] = y.x;
-                        x[qq][e][1] = y.y;
-                        x[qq][e][2] = y.z;
-                        x[qq][e][3] = y.w;
+                        x[half][qq][e][0] = y.x;
+                        x[half][qq][e][1] = y.y;
+                        x[half][qq][e][2] = y.z;
+                        x[half][qq][e][3] = y.w;
                     }
 #pragma unroll
-                for (int w = 0; w < 4; w++) {
-                    mma_bf16(acc[8 * half + 2 * w], p, __byte_perm(x[0][0][w], x[0][1][w], 0x5410), __byte_perm(x[1][0][w], x[1][1][w], 0x5410));
-                    mma_bf16(acc[8 * half + 2 * w + 1], p, __byte_perm(x[0][0][w], x[0][1][w], 0x7632), __byte_perm(x[1][0][w], x[1][1][w], 0x7632));
+            for (int j = 0; j < 4; j++)
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const uint32_t sel = h ? 0x7632 : 0x5410;
+                    const uint32_t v[4] = {__byte_perm(x[0][0][0][j], x[0][0][1][j], sel), __byte_perm(x[1][0][0][j], x[1][0][1][j], sel),
+                                           __byte_perm(x[0][1][0][j], x[0][1][1][j], sel), __byte_perm(x[1][1][0][j], x[1][1][1][j], sel)};
+#pragma unroll
+                    for (int n = 0; n < kN; n++) mma_bf16(acc[n][2 * j + h], v, p[n][0], p[n][1]);
                 }
-            }
         };
 
         // ---- the cache
         const int c_ctx = min(c1, ctx_chunks);
         for (int c = c0; c < c_ctx; c++) {
             const int st = n_use % kStages, key0 = c * kKeys;
-            const uint8_t* kt = ring + st * 2 * kTile;
-            const uint8_t* vt = kt + kTile;
+            uint8_t* kt = ring + st * 2 * kTile;
+            uint8_t* vt = kt + kTile;
             const float* sck = scales + st * 2 * kKeys;
             if (!failed) {
                 const bool got = mbar_wait_inline(bar + st, static_cast<uint32_t>(n_use / kStages) & 1u, abort);
@@ -465,75 +507,109 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
             if (!failed) {
-                const bool tail = key0 + kKeys > len;
-                float sc[2 * kSubs][4];  // [8 keys][row g: keys 2t, 2t + 1; row g + 8: the same]
+                const int there = len - key0;  // keys of the chunk that exist
+                if (there < kKeys) {
+                    // anything may lie behind the last one: zeros for V, which P = 0 would
+                    // not hide (these stores are ordered before the slot's next copy below)
+                    for (int i = lane; i < (kKeys - there) * 8; i += 32) {
 #pragma unroll
-                for (int j = 0; j < 2 * kSubs; j++)
+                        for (int half = 0; half < (kFp8 ? 1 : 2); half++)
+                            *reinterpret_cast<uint4*>(vt + half * (kTile / 2) + swz(there + (i >> 3), i & 7)) = make_uint4(0, 0, 0, 0);
+                    }
+                    __syncwarp();
+                }
+                float sc[kSubs][kN][4];  // [16 keys][8 rows][slot g: rows 2t, 2t + 1; slot 8 + g: the same]
 #pragma unroll
-                    for (int e = 0; e < 4; e++) sc[j][e] = 0.0f;
+                for (int j = 0; j < kSubs; j++)
+#pragma unroll
+                    for (int n = 0; n < kN; n++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) sc[j][n][e] = 0.0f;
                 if (kFp8) {
 #pragma unroll
-                    for (int i = 0; i < 2; i++) {
-                        uint4 x[2 * kSubs];
+                    for (int i = 0; i < 2; i++)
 #pragma unroll
-                        for (int j = 0; j < 2 * kSubs; j++) x[j] = *reinterpret_cast<const uint4*>(kt + swz(slot_row(j, g), t + 4 * i));
+                        for (int j = 0; j < kSubs; j++) {
+                            const uint4 x = *reinterpret_cast<const uint4*>(kt + swz(16 * j + slot_row(0, g), t + 4 * i));
+                            const uint4 y = *reinterpret_cast<const uint4*>(kt + swz(16 * j + slot_row(1, g), t + 4 * i));
+                            const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-                        for (int j = 0; j < 2 * kSubs; j++) {
-                            mma_f16(sc[j], q[4 * i], e4m3_to_f16(x[j].x), e4m3_to_f16(x[j].x >> 16));
-                            mma_f16(sc[j], q[4 * i + 1], e4m3_to_f16(x[j].y), e4m3_to_f16(x[j].y >> 16));
-                            mma_f16(sc[j], q[4 * i + 2], e4m3_to_f16(x[j].z), e4m3_to_f16(x[j].z >> 16));
-                            mma_f16(sc[j], q[4 * i + 3], e4m3_to_f16(x[j].w), e4m3_to_f16(x[j].w >> 16));
+                            for (int e = 0; e < 4; e++) {
+                                const uint32_t k[4] = {codes_lo(xw[e]), codes_lo(yw[e]), codes_hi(xw[e]), codes_hi(yw[e])};
+#pragma unroll
+                                for (int n = 0; n < kN; n++) mma_f16(sc[j][n], k, q[n][4 * i + e][0], q[n][4 * i + e][1]);
+                            }
                         }
-                    }
                 } else {
-                    float sl[2 * kSubs][4];
+                    float sl[kSubs][kN][4];
 #pragma unroll
-                    for (int j = 0; j < 2 * kSubs; j++)
+                    for (int j = 0; j < kSubs; j++)
 #pragma unroll
-                        for (int e = 0; e < 4; e++) sl[j][e] = 0.0f;
+                        for (int n = 0; n < kN; n++)
+#pragma unroll
+                            for (int e = 0; e < 4; e++) sl[j][n][e] = 0.0f;
 #pragma unroll
                     for (int i = 0; i < 4; i++)
 #pragma unroll
-                        for (int j = 0; j < 2 * kSubs; j++) {
-                            const uint4 x = *reinterpret_cast<const uint4*>(kt + (i >> 1) * (kTile / 2) + swz(slot_row(j, g), t + 4 * (i & 1)));
-                            mma_bf16(sc[j], q[2 * i], x.x, x.y);
-                            mma_bf16(sl[j], lo[2 * i], x.x, x.y);
-                            mma_bf16(sc[j], q[2 * i + 1], x.z, x.w);
-                            mma_bf16(sl[j], lo[2 * i + 1], x.z, x.w);
+                        for (int j = 0; j < kSubs; j++) {
+                            const uint8_t* half = kt + (i >> 1) * (kTile / 2);
+                            const uint4 x = *reinterpret_cast<const uint4*>(half + swz(16 * j + slot_row(0, g), t + 4 * (i & 1)));
+                            const uint4 y = *reinterpret_cast<const uint4*>(half + swz(16 * j + slot_row(1, g), t + 4 * (i & 1)));
+                            const uint32_t k0[4] = {x.x, y.x, x.y, y.y}, k1[4] = {x.z, y.z, x.w, y.w};
+#pragma unroll
+                            for (int n = 0; n < kN; n++) {
+                                mma_bf16(sc[j][n], k0, q[n][2 * i][0], q[n][2 * i][1]);
+                                mma_bf16(sl[j][n], k0, lo[n][2 * i][0], lo[n][2 * i][1]);
+                                mma_bf16(sc[j][n], k1, q[n][2 * i + 1][0], q[n][2 * i + 1][1]);
+                                mma_bf16(sl[j][n], k1, lo[n][2 * i + 1][0], lo[n][2 * i + 1][1]);
+                            }
                         }
 #pragma unroll
-                    for (int j = 0; j < 2 * kSubs; j++)
+                    for (int j = 0; j < kSubs; j++)
 #pragma unroll
-                        for (int e = 0; e < 4; e++) sc[j][e] += sl[j][e];
+                        for (int n = 0; n < kN; n++)
+#pragma unroll
+                            for (int e = 0; e < 4; e++) sc[j][n][e] += sl[j][n][e];
                 }
-                float vs[2 * kSubs][2];
+                float vs[kSubs][2];  // value scales of slots g, 8 + g
 #pragma unroll
-                for (int j = 0; j < 2 * kSubs; j++)
+                for (int j = 0; j < kSubs; j++)
 #pragma unroll
-                    for (int e = 0; e < 2; e++) {
-                        const int key = slot_row(j, 2 * t + e);
+                    for (int qq = 0; qq < 2; qq++) {
+                        const int key = 16 * j + slot_row(qq, g);
                         const float by = kFp8 ? sck[key] : 1.0f;
-                        if (kFp8) vs[j][e] = sck[kKeys + key];
-                        sc[j][e] *= kFp8 ? rs[0] * by : rs[0];
-                        sc[j][2 + e] *= kFp8 ? rs[1] * by : rs[1];
-                        if (tail && key0 + key >= len) {  // (anything may lie there)
-                            sc[j][e] = sc[j][2 + e] = -INFINITY;
-                            vs[j][e] = 0.0f;
-                        }
+                        vs[j][qq] = kFp8 ? sck[kKeys + key] : 1.0f;
+#pragma unroll
+                        for (int n = 0; n < kN; n++)
+#pragma unroll
+                            for (int e = 0; e < 2; e++) sc[j][n][2 * qq + e] *= kFp8 ? rs[n][e] * by : rs[n][e];
                     }
+                if (there < kKeys) {
+#pragma unroll
+                    for (int j = 0; j < kSubs; j++)
+#pragma unroll
+                        for (int qq = 0; qq < 2; qq++)
+                            if (16 * j + slot_row(qq, g) >= there) {
+#pragma unroll
+                                for (int n = 0; n < kN; n++) sc[j][n][2 * qq] = sc[j][n][2 * qq + 1] = -INFINITY;
+                                vs[j][qq] = 0.0f;
+                            }
+                }
                 if (kFp8) {
                     float top = 0.0f;
 #pragma unroll
-                    for (int j = 0; j < 2 * kSubs; j++) top = fmaxf(top, fmaxf(vs[j][0], vs[j][1]));
+                    for (int j = 0; j < kSubs; j++) top = fmaxf(top, fmaxf(vs[j][0], vs[j][1]));
                     if (__any_sync(kFull, top > vref)) {
                         top = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(top)));  // (not negative)
                         const float raised = __uint_as_float(min(max(__float_as_uint(top) >> 23, 27u), 252u) + 1u << 23);
                         const float alpha = vref / raised;
                         vref = raised;
 #pragma unroll
-                        for (int j = 0; j < 16; j++)
+                        for (int n = 0; n < kN; n++)
 #pragma unroll
-                            for (int e = 0; e < 4; e++) acc[j][e] *= alpha;
+                            for (int j = 0; j < 8; j++)
+#pragma unroll
+                                for (int e = 0; e < 4; e++) acc[n][j][e] *= alpha;
                     }
                 }
                 soften(sc);
@@ -541,48 +617,48 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const float inv = vref > 0.0f ? 128.0f / vref : 0.0f;  // (0: all scales are)
 #pragma unroll
                     for (int u = 0; u < kSubs; u++) {
-                        uint32_t p[4];
+                        const float w0 = vs[u][0] * inv, w1 = vs[u][1] * inv;
+                        uint32_t p[kN][2];
 #pragma unroll
-                        for (int qq = 0; qq < 2; qq++) {
-                            const float w0 = vs[2 * u + qq][0] * inv, w1 = vs[2 * u + qq][1] * inv;
-#pragma unroll
-                            for (int h = 0; h < 2; h++) {
-                                const __half2 x = __floats2half2_rn(sc[2 * u + qq][2 * h] * w0, sc[2 * u + qq][2 * h + 1] * w1);
-                                p[2 * qq + h] = *reinterpret_cast<const uint32_t*>(&x);
-                            }
+                        for (int n = 0; n < kN; n++) {
+                            p[n][0] = transpose_8x8(pack_f16(sc[u][n][0] * w0, sc[u][n][1] * w0));
+                            p[n][1] = transpose_8x8(pack_f16(sc[u][n][2] * w1, sc[u][n][3] * w1));
                         }
                         uint32_t x[2][2][4];
 #pragma unroll
                         for (int qq = 0; qq < 2; qq++)
 #pragma unroll
                             for (int e = 0; e < 2; e++) {
-                                const int row = slot_row(2 * u + qq, 2 * t + e);
-                                uint4 y = *reinterpret_cast<const uint4*>(vt + swz(row, g));
-                                if (tail && key0 + row >= len) y = make_uint4(0, 0, 0, 0);
+                                const uint4 y = *reinterpret_cast<const uint4*>(vt + swz(16 * u + slot_row(qq, 2 * t + e), g));
                                 x[qq][e][0] = y.x;
                                 x[qq][e][1] = y.y;
                                 x[qq][e][2] = y.z;
                                 x[qq][e][3] = y.w;
                             }
 #pragma unroll
-                        for (int w = 0; w < 4; w++)
+                        for (int w = 0; w < 2; w++)
 #pragma unroll
-                            for (int b = 0; b < 2; b++) {  // elements 4 w + 2 b, + 1 of both keys of a pair
-                                const uint32_t s0 = __byte_perm(x[0][0][w], x[0][1][w], b ? 0x7362 : 0x5140);
-                                const uint32_t s1 = __byte_perm(x[1][0][w], x[1][1][w], b ? 0x7362 : 0x5140);
-                                mma_f16(acc[4 * w + 2 * b], p, e4m3_to_f16(s0), e4m3_to_f16(s1));
-                                mma_f16(acc[4 * w + 2 * b + 1], p, e4m3_to_f16(s0 >> 16), e4m3_to_f16(s1 >> 16));
+                            for (int b = 0; b < 2; b++) {
+                                // elements 4 w + 2 b, + 1 of piece g (words w), and 8 further (words 2 + w), of
+                                // both keys of a pair
+                                const uint32_t sel = b ? 0x7362 : 0x5140;
+                                const uint32_t v0 = __byte_perm(x[0][0][w], x[0][1][w], sel), v1 = __byte_perm(x[0][0][2 + w], x[0][1][2 + w], sel);
+                                const uint32_t v2 = __byte_perm(x[1][0][w], x[1][1][w], sel), v3 = __byte_perm(x[1][0][2 + w], x[1][1][2 + w], sel);
+                                const uint32_t first[4] = {codes_lo(v0), codes_lo(v1), codes_lo(v2), codes_lo(v3)};
+                                const uint32_t second[4] = {codes_hi(v0), codes_hi(v1), codes_hi(v2), codes_hi(v3)};
+#pragma unroll
+                                for (int n = 0; n < kN; n++) {
+                                    mma_f16(acc[n][4 * w + 2 * b], first, p[n][0], p[n][1]);
+                                    mma_f16(acc[n][4 * w + 2 * b + 1], second, p[n][0], p[n][1]);
+                                }
                             }
                     }
                 } else {
-                    const uint32_t p[4] = {pack_bf16x2(sc[0][0], sc[0][1]), pack_bf16x2(sc[0][2], sc[0][3]),
-                                           pack_bf16x2(sc[1][0], sc[1][1]), pack_bf16x2(sc[1][2], sc[1][3])};
-                    values_bf16(p, [&](int half, int qq, int e) {
-                        const int row = slot_row(qq, 2 * t + e);
-                        const uint4 y = *reinterpret_cast<const uint4*>(vt + half * (kTile / 2) + swz(row, g));
-                        return tail && key0 + row >= len ? make_uint4(0, 0, 0, 0) : y;
+                    values_bf16(sc[0], [&](int half, int qq, int e) {
+                        return *reinterpret_cast<const uint4*>(vt + half * (kTile / 2) + swz(slot_row(qq, 2 * t + e), g));
                     });
                 }
+                if (there < kKeys) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             }
             __syncwarp();  // every lane has read the stage
             n_use++;
@@ -592,20 +668,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         // ---- the tree rows, 16 at a time, read and rotated here
         for (int c = max(c0, ctx_chunks); c < c1; c++) {
             const int key0 = (c - ctx_chunks) * 16;
-            float sc[2][4];
+            uint32_t w[2][4][4];  // [key slot 8 qq + g][piece][word]
 #pragma unroll
-            for (int qq = 0; qq < 2; qq++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) sc[qq][e] = 0.0f;
-#pragma unroll 1
             for (int qq = 0; qq < 2; qq++) {
-                if (key0 + 8 * qq > nodes) break;
                 const int j = key0 + slot_row(qq, g);
-                uint32_t w[4][4];
 #pragma unroll
                 for (int i = 0; i < 4; i++)
 #pragma unroll
-                    for (int e = 0; e < 4; e++) w[i][e] = 0u;
+                    for (int e = 0; e < 4; e++) w[qq][i][e] = 0u;
                 if (j <= nodes) {
                     const int pos = len + (j > 0 ? ld_plain(a.depths + static_cast<long long>(s) * a.B + j - 1) : 0);
                     const __nv_bfloat16* k = a.k + (seq_row + j) * a.k_stride + head * kHeadDim;
@@ -621,60 +691,59 @@ __global__ void __launch_bounds__(kThreads, 1)
                             rope_sincos(a.turns.f[d0 + 2 * e], pos, &s0, &k0);
                             rope_sincos(a.turns.f[d0 + 2 * e + 1], pos, &s1, &k1);
                             const float x0 = bf16_lo(xw[e]), x1 = bf16_hi(xw[e]), y0 = bf16_lo(yw[e]), y1 = bf16_hi(yw[e]);
-                            w[i][e] = pack_bf16x2(x0 * k0 - y0 * s0, x1 * k1 - y1 * s1);
-                            w[i + 2][e] = pack_bf16x2(y0 * k0 + x0 * s0, y1 * k1 + x1 * s1);
+                            w[qq][i][e] = pack_bf16x2(x0 * k0 - y0 * s0, x1 * k1 - y1 * s1);
+                            w[qq][i + 2][e] = pack_bf16x2(y0 * k0 + x0 * s0, y1 * k1 + x1 * s1);
                         }
                     }
                 }
-                __syncwarp();
-                float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            }
+            __syncwarp();
+            float sc[1][kN][4];
 #pragma unroll
-                for (int i = 0; i < 8; i++) {
+            for (int n = 0; n < kN; n++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) sc[0][n][e] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const uint32_t k[4] = {w[0][i >> 1][2 * (i & 1)], w[1][i >> 1][2 * (i & 1)], w[0][i >> 1][2 * (i & 1) + 1], w[1][i >> 1][2 * (i & 1) + 1]};
+#pragma unroll
+                for (int n = 0; n < kN; n++) {
                     if (kFp8) {  // the queries as bf16: tree keys may leave f16's range
-                        uint32_t qb[4];
+                        uint32_t qb[2];
 #pragma unroll
-                        for (int e = 0; e < 4; e++) {
-                            const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&q[i][e]));
+                        for (int e = 0; e < 2; e++) {
+                            const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&q[n][i][e]));
                             qb[e] = pack_bf16x2(x.x, x.y);
                         }
-                        mma_bf16(d, qb, w[i >> 1][2 * (i & 1)], w[i >> 1][2 * (i & 1) + 1]);
+                        mma_bf16(sc[0][n], k, qb[0], qb[1]);
                     } else {
-                        mma_bf16(d, q[i], w[i >> 1][2 * (i & 1)], w[i >> 1][2 * (i & 1) + 1]);
-                        mma_bf16(d, lo[i], w[i >> 1][2 * (i & 1)], w[i >> 1][2 * (i & 1) + 1]);
+                        mma_bf16(sc[0][n], k, q[n][i][0], q[n][i][1]);
+                        mma_bf16(sc[0][n], k, lo[n][i][0], lo[n][i][1]);
                     }
-                }
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    if (qq == 0)
-                        sc[0][e] = d[e];
-                    else
-                        sc[1][e] = d[e];
                 }
             }
 #pragma unroll
-            for (int qq = 0; qq < 2; qq++)
+            for (int n = 0; n < kN; n++)
 #pragma unroll
-                for (int e = 0; e < 2; e++)
+                for (int qq = 0; qq < 2; qq++)
 #pragma unroll
-                    for (int h = 0; h < 2; h++) {
-                        const int j = key0 + slot_row(qq, 2 * t + e), b = (row0 + g + 8 * h) >> a.g_log2;
+                    for (int e = 0; e < 2; e++) {
+                        const int j = key0 + slot_row(qq, g), b = (8 * n + 2 * t + e) >> a.g_log2;
                         bool see = j <= nodes && b <= nodes;
                         if (see && j > 0)
                             see = b > 0 && ((ld_plain(a.mask + (static_cast<long long>(s) * a.B + b - 1) * a.mw + ((j - 1) >> 6)) >> ((j - 1) & 63)) & 1ull);
-                        sc[qq][2 * h + e] = see ? sc[qq][2 * h + e] * rs[h] : -INFINITY;
+                        sc[0][n][2 * qq + e] = see ? sc[0][n][2 * qq + e] * rs[n][e] : -INFINITY;
                     }
             soften(sc);
             if (kFp8) {
                 if (vref == 0.0f) vref = 1.0f;
                 const float inv = 128.0f / vref;
 #pragma unroll
-                for (int qq = 0; qq < 2; qq++)
+                for (int n = 0; n < kN; n++)
 #pragma unroll
-                    for (int e = 0; e < 4; e++) sc[qq][e] *= inv;
+                    for (int e = 0; e < 4; e++) sc[0][n][e] *= inv;
             }
-            const uint32_t p[4] = {pack_bf16x2(sc[0][0], sc[0][1]), pack_bf16x2(sc[0][2], sc[0][3]), pack_bf16x2(sc[1][0], sc[1][1]),
-                                   pack_bf16x2(sc[1][2], sc[1][3])};
-            values_bf16(p, [&](int half, int qq, int e) {
+            values_bf16(sc[0], [&](int half, int qq, int e) {
                 const int j = key0 + slot_row(qq, 2 * t + e);
                 if (j > nodes) return make_uint4(0, 0, 0, 0);
                 return ld_plain(reinterpret_cast<const uint4*>(a.v + (seq_row + j) * a.v_stride + head * kHeadDim + 8 * (kFp8 ? 2 * g + half : g + 8 * half)));
@@ -683,36 +752,35 @@ __global__ void __launch_bounds__(kThreads, 1)
 
         // ---- the result, or this part of it
         const bool whole = c0 == 0 && c1 == chunks;
-        Part* part = static_cast<Part*>(a.parts) + 2 * static_cast<long long>(share) + (c0 > 0 ? 0 : 1);
+        Part<kN>* part = static_cast<Part<kN>*>(a.parts) + 2 * static_cast<long long>(share) + (c0 > 0 ? 0 : 1);
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            l[h] += __shfl_xor_sync(kFull, l[h], 1);
-            l[h] += __shfl_xor_sync(kFull, l[h], 2);
-            const int r = row0 + g + 8 * h, b = r >> a.g_log2;
-            if (b > nodes) continue;
-            float by = kFp8 ? vref * 0.0078125f : 1.0f;
-            if (whole) by = l[h] > 0.0f ? by / l[h] : 0.0f;
+        for (int n = 0; n < kN; n++)
 #pragma unroll
-            for (int e = 0; e < 2; e++)
+            for (int e = 0; e < 2; e++) {
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) l[n][e] += __shfl_xor_sync(kFull, l[n][e], o);
+                const int r = 8 * n + 2 * t + e, b = r >> a.g_log2;
+                if (b > nodes) continue;
+                float by = kFp8 ? vref * 0.0078125f : 1.0f;
+                if (whole) by = l[n][e] > 0.0f ? by / l[n][e] : 0.0f;
 #pragma unroll
                 for (int half = 0; half < 2; half++) {
-                    // 8 elements from out_dim(2 t + e, 8 half) on
-                    const int d = out_dim<kFp8>(2 * t + e, 8 * half);
+                    const int d = kFp8 ? 16 * g + 8 * half : 64 * half + 8 * g;  // of the 8 elements
                     float o[8];
 #pragma unroll
-                    for (int k = 0; k < 8; k++) o[k] = acc[8 * half + k][2 * h + e] * by;
+                    for (int k = 0; k < 8; k++) o[k] = acc[n][k][2 * half + e] * by;
                     if (whole) {
                         __nv_bfloat16* dst = a.out + ((seq_row + b) * a.Hq + head * a.G + (r & (a.G - 1))) * kHeadDim + d;
                         *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]),
                                                                     pack_bf16x2(o[4], o[5]), pack_bf16x2(o[6], o[7]));
                     } else {
-                        float4* dst = reinterpret_cast<float4*>(&part->o[g + 8 * h][d]);
+                        float4* dst = reinterpret_cast<float4*>(&part->o[r][d]);
                         dst[0] = make_float4(o[0], o[1], o[2], o[3]);
                         dst[1] = make_float4(o[4], o[5], o[6], o[7]);
                     }
                 }
-            if (!whole && t == 0) part->ml[g + 8 * h] = make_float2(m[h], l[h]);
-        }
+                if (!whole && g == 0) part->ml[r] = make_float2(m[n][e], l[n][e]);
+            }
     }
     if (failed) {  // copies in flight land before the CTA ends
         const unsigned long long t0 = globaltimer_ns();
@@ -724,53 +792,54 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // Joins the parts of the units that several warps shared, in the order of
 // their keys.  Block i works if share i begins inside a unit that share i - 1
-// began: 16 threads (8 elements each) per row, and where a unit has fewer than
-// 16 rows as many more groups of threads, each with every n-th part, joined in
-// order through shared memory.
-__global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_constant__ PagedArgs a) {
-    __shared__ float2 ml_of[kUnitRows];
-    __shared__ float sum_of[kUnitRows][kHeadDim];
-    __shared__ int ends[kThreads / 32];
+// began: 16 threads (8 elements each) per row, and as many more groups of
+// threads as fit, each with every n-th part, joined in order through shared
+// memory.
+constexpr int kJoinThreads = 256;
+template <int kN>
+__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_constant__ PagedArgs a) {
+    __shared__ float2 ml_of[8 * kN];
+    __shared__ float sum_of[8 * kN][kHeadDim];
+    __shared__ int ends[kJoinThreads / 32];
     pdl_trigger();
     const int tid = threadIdx.x, lane = tid & 31, i = blockIdx.x + 1;
     pdl_wait();
     // all that has to be known in one go (the kernel is a chain of loads)
     const int count = a.plan->count, nodes = a.plan->nodes[i];
     const int4 at = a.plan->places[i], prev = a.plan->places[i - 1];
-    int4 next = a.plan->places[min(i + 1 + tid, kWarps * kMaxSms - 1)];
+    int4 next = a.plan->places[min(i + 1 + tid, kMaxShares - 1)];
     if (i >= count || at.z == 0 || at.z >= at.w) return;  // (from at.w on the place stands for a unit's other costs)
     if (prev.x == at.x && prev.y == at.y && prev.z > 0) return;
     // the last share that holds chunks of the unit
     int end = i;
-    for (int from = i + 1;; from += kThreads) {
-        if (from > i + 1) next = a.plan->places[min(from + tid, kWarps * kMaxSms - 1)];
+    for (int from = i + 1;; from += kJoinThreads) {
+        if (from > i + 1) next = a.plan->places[min(from + tid, kMaxShares - 1)];
         const bool in = from + tid < count && next.x == at.x && next.y == at.y && next.z < at.w;
         const unsigned out = __ballot_sync(kFull, !in);
         if (lane == 0) ends[tid >> 5] = out ? __ffs(out) - 1 : 32;
         __syncthreads();
         int n = 0;
-        for (int w = 0; w < kThreads / 32; w++) {
+        for (int w = 0; w < kJoinThreads / 32; w++) {
             n += ends[w];
             if (ends[w] < 32) break;
         }
         end += n;
         __syncthreads();
-        if (n < kThreads) break;
+        if (n < kJoinThreads) break;
     }
-    const int s = at.x, groups = (((nodes + 1) << a.g_log2) + kUnitRows - 1) / kUnitRows, head = at.y / groups, row0 = (at.y % groups) * kUnitRows;
-    const int rows = min(kUnitRows, ((nodes + 1) << a.g_log2) - row0);
-    int span = 1;  // rows rounded up to a power of two; 16 / span thread groups
+    const int s = at.x, head = at.y, rows = (nodes + 1) << a.g_log2;
+    int span = 1;  // rows rounded up to a power of two
     while (span < rows) span *= 2;
-    const int slot_of_row = tid >> 4, d8 = tid & 15, r = slot_of_row % span, part0 = slot_of_row / span, step = kUnitRows / span;
+    const int slot_of_row = tid >> 4, d8 = tid & 15, r = slot_of_row % span, part0 = slot_of_row / span, step = kJoinThreads / 16 / span;
     const bool live = r < rows;
     // share i - 1 began the unit (its second slot), the others went on with it
-    auto slot = [&](int c) { return static_cast<const Part*>(a.parts) + 2 * static_cast<long long>(c) + (c < i ? 1 : 0); };
+    auto slot = [&](int c) { return static_cast<const Part<kN>*>(a.parts) + 2 * static_cast<long long>(c) + (c < i ? 1 : 0); };
     const int c0 = i - 1, c1 = end;
     float top = -INFINITY, l = 0.0f, o[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     if (live)
 #pragma unroll 4
         for (int c = c0 + part0; c <= c1; c += step) {
-            const Part* x = slot(c);
+            const Part<kN>* x = slot(c);
             const float2 ml = x->ml[r];
             const float4 u = *reinterpret_cast<const float4*>(&x->o[r][8 * d8]), v = *reinterpret_cast<const float4*>(&x->o[r][8 * d8 + 4]);
             const bool any = ml.x != -INFINITY;
@@ -801,7 +870,7 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
     }
     if (part0 != 0 || !live) return;
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-    __nv_bfloat16* d = a.out + ((static_cast<long long>(s) * (a.B + 1) + ((row0 + r) >> a.g_log2)) * a.Hq + head * a.G + ((row0 + r) & (a.G - 1))) * kHeadDim + 8 * d8;
+    __nv_bfloat16* d = a.out + ((static_cast<long long>(s) * (a.B + 1) + (r >> a.g_log2)) * a.Hq + head * a.G + (r & (a.G - 1))) * kHeadDim + 8 * d8;
     *reinterpret_cast<uint4*>(d) = make_uint4(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv),
                                               pack_bf16x2(o[4] * inv, o[5] * inv), pack_bf16x2(o[6] * inv, o[7] * inv));
 }
@@ -820,9 +889,10 @@ bool valid_cfg(const dart_paged_attn_config* c, const dart_kv_cache* cache) {
            static_cast<long long>(c->nseq) * cache->Hkv * (c->B + 256) <= (1ll << 30);
 }
 
-// Which kernel: rows that fit one 16-row product are streamed from HBM, more
-// are 128-row tiles of the tensor-memory path.
-bool few_rows(const dart_paged_attn_config& c, const dart_kv_cache& cache) { return (c.B + 1) * (c.Hq / cache.Hkv) <= kUnitRows; }
+// Which kernel: a few rows are streamed from HBM, more are 128-row tiles of the
+// tensor-memory path.
+constexpr int kFewRows = 16;
+bool few_rows(const dart_paged_attn_config& c, const dart_kv_cache& cache) { return (c.B + 1) * (c.Hq / cache.Hkv) <= kFewRows; }
 
 // The device's number of SMs; 0 if it is not sm_103a, -1 on an error.  The
 // shared-memory opt-in of the kernels is set on the first call per device.
@@ -837,12 +907,30 @@ int device_sms(int dev) {
         cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return -1;
     if (major != 10 || minor != 3) return 0;
-    if (cudaFuncSetAttribute(paged_rows_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<false>::kSmem) != cudaSuccess ||
-        cudaFuncSetAttribute(paged_rows_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<true>::kSmem) != cudaSuccess)
+    if (cudaFuncSetAttribute(paged_rows_kernel<false, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<false, 1>::kSmem) != cudaSuccess ||
+        cudaFuncSetAttribute(paged_rows_kernel<true, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<true, 1>::kSmem) != cudaSuccess ||
+        cudaFuncSetAttribute(paged_rows_kernel<false, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<false, 2>::kSmem) != cudaSuccess ||
+        cudaFuncSetAttribute(paged_rows_kernel<true, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<true, 2>::kSmem) != cudaSuccess)
         return -1;
     if (!paged_tiles_prepare_device()) return -1;
     known[dev].store(sms, std::memory_order_release);
     return sms;
+}
+
+template <int kN>
+constexpr size_t rows_workspace() {
+    static_assert(rows_warps(kN) * kMaxSms <= kMaxShares, "the plan holds every share");
+    return sizeof(SharePlan) + sizeof(Part<kN>) * 2 * rows_warps(kN) * kMaxSms;
+}
+
+template <bool kFp8, int kN>
+int launch_rows(const PagedArgs& a, const dart_kv_cache& cache, int ctas, cudaStream_t st) {
+    using G_ = Geo<kFp8, kN>;
+    const int box = kFp8 && cache.page_size >= 32 ? 32 : 16;
+    CUtensorMap tmK, tmV;
+    if (!encode_rows(&tmK, cache.k, a.pool_rows, kFp8, box) || !encode_rows(&tmV, cache.v, a.pool_rows, kFp8, box)) return DART_ERR_CUDA;
+    if (launch_pdl(paged_rows_kernel<kFp8, kN>, dim3(ctas), dim3(G_::kThreads), G_::kSmem, st, tmK, tmV, a) != cudaSuccess) return DART_ERR_CUDA;
+    return launch_pdl(paged_join_kernel<kN>, dim3(G_::kWarps * ctas - 1), dim3(kJoinThreads), 0, st, a) == cudaSuccess ? DART_OK : DART_ERR_CUDA;
 }
 
 }  // namespace
@@ -854,7 +942,7 @@ extern "C" {
 
 size_t dart_paged_attention_workspace(const dart_paged_attn_config* cfg, const dart_kv_cache* cache) {
     if (!valid_cfg(cfg, cache)) return 0;
-    if (few_rows(*cfg, *cache)) return sizeof(SharePlan) + sizeof(Part) * 2 * kWarps * kMaxSms;
+    if (few_rows(*cfg, *cache)) return (cfg->B + 1) * (cfg->Hq / cache->Hkv) <= 8 ? rows_workspace<1>() : rows_workspace<2>();
     return paged_tiles_workspace(*cfg, *cache);
 }
 
@@ -913,17 +1001,9 @@ int dart_paged_attention(const dart_paged_attn_config* cfg, const dart_kv_cache*
     a.turns = rope_turns(c.rope_theta);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (!few_rows(c, *cache)) return launch_paged_tiles(a, *cache, static_cast<uint8_t*>(workspace), std::min(sms, kMaxSms), st);
-    const int box = fp8 && cache->page_size >= 32 ? 32 : 16;
-    CUtensorMap tmK, tmV;
-    if (!encode_rows(&tmK, cache->k, a.pool_rows, fp8, box) || !encode_rows(&tmV, cache->v, a.pool_rows, fp8, box)) return DART_ERR_CUDA;
     const int ctas = std::min(sms, kMaxSms);
-    cudaError_t e = fp8 ? launch_pdl(paged_rows_kernel<true>, dim3(ctas), dim3(kThreads), Geo<true>::kSmem, st, tmK, tmV, a)
-                        : launch_pdl(paged_rows_kernel<false>, dim3(ctas), dim3(kThreads), Geo<false>::kSmem, st, tmK, tmV, a);
-    if (e != cudaSuccess) return DART_ERR_CUDA;
-    const dim3 seams(kWarps * ctas - 1);
-    e = launch_pdl(paged_join_kernel, seams, dim3(kThreads), 0, st, a);
-    if (e != cudaSuccess) return DART_ERR_CUDA;
-    return DART_OK;
+    if ((c.B + 1) * a.G <= 8) return fp8 ? launch_rows<true, 1>(a, *cache, ctas, st) : launch_rows<false, 1>(a, *cache, ctas, st);
+    return fp8 ? launch_rows<true, 2>(a, *cache, ctas, st) : launch_rows<false, 2>(a, *cache, ctas, st);
 }
 
 }  // extern "C"

@@ -11,15 +11,15 @@
 
 namespace dart {
 
-constexpr int kMaxSms = 160;  // shares are counted by SMs; the workspace has room for this many
+constexpr int kMaxSms = 160, kMaxShares = 12 * kMaxSms;  // shares are counted by SMs; the workspace has room for this many
 
 // Where the shares of a call begin, for the kernel that joins split units:
 // places[i] = sequence, unit, place in the unit, places of the unit that are
 // work; nodes[i]: nodes of the sequence.
 struct SharePlan {
     int count, pad[3];
-    int4 places[8 * kMaxSms];
-    int nodes[8 * kMaxSms];
+    int4 places[kMaxShares];
+    int nodes[kMaxShares];
 };
 
 struct PagedArgs {
