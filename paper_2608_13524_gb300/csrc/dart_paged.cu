@@ -69,7 +69,7 @@ __host__ __device__ constexpr int rows_warps(int n) { return n == 1 ? 12 : 8; }
 template <bool kFp8>
 struct Chunk {
     static constexpr int kKeys = kFp8 ? 32 : 16;
-    static constexpr int kUnitCost = kFp8 ? 4 : 6;
+    static constexpr int kUnitCost = kFp8 ? 6 : 9;
 };
 
 // A place in the list of chunks: sequence, kv head, chunk of the unit.
