@@ -494,17 +494,24 @@ __device__ __forceinline__ void reg_more() {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs));
 }
 
-// D[tmem] (+)= A[tmem] * B[smem] at fixed offsets from the operands' bases: the
-// descriptor is put together here, since a register pair for each of 32 of
-// them is more than the issuing thread has.  `lo`: address >> 4, and the
-// leading offset of an MN-major operand.
+// D[tmem] (+)= A[tmem] * B[smem] at fixed offsets from the operands' bases, by
+// one lane of a converged warp: operands that the whole warp agrees on stay in
+// uniform registers, while a single thread's would be moved there one by one for
+// every product (66 cycles each, as long as the product takes).  `lo`: address >>
+// 4, and the leading offset of an MN-major operand.
 constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);  // stride, version, 128-byte swizzle
 template <int kAOff, int kBOff>
 __device__ __forceinline__ void mma_at(uint32_t tmem_d, uint32_t tmem_a, uint32_t lo, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n .reg .pred p;\n .reg .b32 x, y;\n .reg .b64 d;\n setp.ne.b32 p, %4, 0;\n add.u32 x, %1, %5;\n add.u32 y, %2, %6;\n"
-        " mov.b64 d, {y, %7};\n tcgen05.mma.cta_group::1.kind::f16 [%0], [x], d, %3, p;\n}\n" ::"r"(tmem_d),
+        "{\n .reg .pred p, e;\n .reg .b32 x, y;\n .reg .b64 d;\n setp.ne.b32 p, %4, 0;\n add.u32 x, %1, %5;\n add.u32 y, %2, %6;\n"
+        " mov.b64 d, {y, %7};\n elect.sync _|e, 0xffffffff;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], d, %3, p;\n}\n" ::"r"(tmem_d),
         "r"(tmem_a), "r"(lo), "r"(idesc), "r"(accumulate), "n"(kAOff), "n"(kBOff), "r"(kDescHigh)
+        : "memory");
+}
+__device__ __forceinline__ void commit_elected(uint64_t* bar) {
+    asm volatile(
+        "{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n"
+        " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(smem_u32(bar))
         : "memory");
 }
 // S = Q K^T (K-major K: 32 bytes a step, 64 elements a swizzle column) and
@@ -532,7 +539,7 @@ struct TGeo {
     static constexpr int kRaw = (kRawK + kRawV) * kHalf;
     static constexpr int kRawScales = (kRawK + kRawV) * kKeys * 4;
     static constexpr int kBars = 4 * kStages + 2 * (kRawK + kRawV) + (kConv ? kRing : 0) + 9 + 1;
-    static constexpr int kExchange = 2 * kRows * 4 + 8 * 4 + kRing * 8 + kRing * 4 * 4;
+    static constexpr int kExchange = 4 * kRows * 4 + 16 * 4 + kRing * 8 + kRing * 4 * 4;
     static constexpr int kSmem = kOps + kRaw + kRawScales + kBars * 8 + kExchange + 16;
     // kCodes: warpgroups (producer, MMA, two idle warps), softmax, softmax, converters
     static constexpr int kThreads = kConv ? 512 : 64 + kSoft;
@@ -607,9 +614,9 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
     uint64_t* q_ready = pv_done + 2;        // [2] by Q buffer
     uint64_t* o_free = q_ready + 2;         // the unit's O has been read
     uint64_t* tdown = o_free + 1;
-    float* xch = reinterpret_cast<float*>(k_full + G_::kBars);  // [2][128] row max / sum exchange
-    int* xok = reinterpret_cast<int*>(xch + 2 * kRows);         // [2][4] "no wait failed"
-    float2* tile_ref = reinterpret_cast<float2*>(xok + 8);      // [tile % 4] powers of two of K and V
+    float* xch = reinterpret_cast<float*>(k_full + G_::kBars);  // [2][warpgroup][128] row max / sum exchange
+    int* xok = reinterpret_cast<int*>(xch + 4 * kRows);         // [2][warpgroup][4] "no wait failed"
+    float2* tile_ref = reinterpret_cast<float2*>(xok + 16);      // [tile % 4] powers of two of K and V
     float* conv_top = reinterpret_cast<float*>(tile_ref + G_::kRing);  // [K, V][tile % 4][warp] largest scales
     int* misc = reinterpret_cast<int*>(conv_top + 4 * G_::kRing);      // TMEM base, abort
     volatile int* abort = &misc[1];
@@ -634,13 +641,13 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
         if (kConv)
             for (int i = 0; i < G_::kRing; i++) mbar_init(&sc_full[i], 2);
         mbar_init(s_full, 1);
-        mbar_init(s_empty, kSoft);
+        mbar_init(s_empty, kSoft / 32);
         for (int i = 0; i < 2; i++) {
-            mbar_init(&p_full[i], kSoft);
+            mbar_init(&p_full[i], kSoft / 32);
             mbar_init(&pv_done[i], 1);
-            mbar_init(&q_ready[i], kSoft);
+            mbar_init(&q_ready[i], kSoft / 32);
         }
-        mbar_init(o_free, kSoft);
+        mbar_init(o_free, kSoft / 32);
         mbar_init(tdown, 1);
         misc[1] = 0;
         fence_mbar_init();
@@ -748,26 +755,26 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
             }
         } else if (warp == 1) {
             // ---------------------------------------------------------- MMAs
-            if (lane == 0) {
+            {
                 // (operand types: bf16 1, f16 0 in bits 7 and 10)
                 constexpr uint32_t idesc_s = idesc_bf16_f32(kRows, kKeys) & (kF16 ? ~((1u << 7) | (1u << 10)) : ~0u);
                 constexpr uint32_t idesc_pv = (idesc_bf16_f32(kRows, kHeadDim) & (kF16 ? ~((1u << 7) | (1u << 10)) : ~0u)) | (1u << 16);  // B (= V) MN-major
-                const uint32_t k_lo = smem_u32(sK) >> 4, v_lo = smem_u32(sV) >> 4;
+                const uint32_t k_lo = smem_u32(sK) >> 4, v_lo = smem_u32(sV) >> 4, base = __shfl_sync(kFull, tmem, 0);
                 auto issue_s = [&](int n, int part) -> bool {
                     const int st = n % kStages;
-                    if (!mbar_wait_inline(&k_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort) ||
-                        (n > 0 && !mbar_wait_inline(s_empty, static_cast<uint32_t>(n - 1) & 1u, abort)))
+                    if (!warp_wait(&k_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort) ||
+                        (n > 0 && !warp_wait(s_empty, static_cast<uint32_t>(n - 1) & 1u, abort)))
                         return false;
                     tc_fence_after();
-                    mma_s(tmem + kSCol, tmem + kQCol + (part & 1) * 64, (k_lo + st * (kTile >> 4)) & 0x3FFFu, idesc_s);
-                    tc_commit(s_full);
-                    tc_commit(&k_empty[st]);
+                    mma_s(base + kSCol, base + kQCol + __shfl_sync(kFull, part & 1, 0) * 64, __shfl_sync(kFull, (k_lo + st * (kTile >> 4)) & 0x3FFFu, 0), idesc_s);
+                    commit_elected(s_full);
+                    commit_elected(&k_empty[st]);
                     return true;
                 };
                 bool have = w.next(a), ok = true;
                 int n = 0, part = 0, t = w.t0, t1 = w.t1, t0 = w.t0;
                 if (have) {
-                    ok = mbar_wait_inline(&q_ready[0], 0, abort);
+                    ok = warp_wait(&q_ready[0], 0, abort);
                     tc_fence_after();
                     ok = ok && issue_s(0, 0);
                 }
@@ -780,27 +787,28 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                         t = t0 = w.t0;
                         t1 = w.t1;
                         part++;
-                        if (have) ok = mbar_wait_inline(&q_ready[part & 1], static_cast<uint32_t>(part >> 1) & 1u, abort);
+                        if (have) ok = warp_wait(&q_ready[part & 1], static_cast<uint32_t>(part >> 1) & 1u, abort);
                     }
                     if (have && ok) {
                         tc_fence_after();
                         ok = issue_s(n + 1, part);
                     }
                     const int st = n % kStages;
-                    ok = ok && mbar_wait_inline(&p_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, abort) &&
-                         mbar_wait_inline(&v_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort) &&
-                         (!first || my_part == 0 || mbar_wait_inline(o_free, static_cast<uint32_t>(my_part - 1) & 1u, abort));
+                    ok = ok && warp_wait(&p_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, abort) &&
+                         warp_wait(&v_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort) &&
+                         (!first || my_part == 0 || warp_wait(o_free, static_cast<uint32_t>(my_part - 1) & 1u, abort));
                     if (!ok) break;
                     tc_fence_after();
-                    mma_pv(tmem + kOCol, tmem + kPCol + (n & 1) * 64, ((v_lo + st * (kTile >> 4)) & 0x3FFFu) | ((kHalf >> 4) << 16), idesc_pv,
-                           first ? 1u : 0u);
-                    tc_commit(&v_empty[st]);
-                    tc_commit(&pv_done[n & 1]);
+                    mma_pv(base + kOCol, base + kPCol + __shfl_sync(kFull, n & 1, 0) * 64,
+                           __shfl_sync(kFull, ((v_lo + st * (kTile >> 4)) & 0x3FFFu) | ((kHalf >> 4) << 16), 0), idesc_pv, __shfl_sync(kFull, first ? 1u : 0u, 0));
+                    commit_elected(&v_empty[st]);
+                    commit_elected(&pv_done[n & 1]);
                     n++;
                 }
                 if (!ok) {
-                    attn_timeout(a.status, abort);
-                    tc_commit(tdown);
+                    if (lane == 0) attn_timeout(a.status, abort);
+                    __syncwarp();
+                    commit_elected(tdown);
                     attn_drain(tdown, 0);
                 }
             }
@@ -812,6 +820,24 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
         const int r = qd * 32 + lane;  // query row of the unit = TMEM lane
         const int pair_bar = kPairBar + qd;
         const uint32_t tl = tmem + (static_cast<uint32_t>(qd * 32) << 16);
+        auto arrive = [&](uint64_t* bar) {  // of the whole warp
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+        };
+        // The maximum or sum of a row and "no wait failed" of the lane quarter's two warps:
+        // two places in turn, so that one barrier an exchange is enough.
+        int turn = 0;
+        auto exchange = [&](float x, bool& ok) {
+            float* xc = xch + turn * 2 * kRows;
+            int* xo = xok + turn * 8;
+            turn ^= 1;
+            xc[wg * kRows + r] = x;
+            if (lane == 0) xo[wg * 4 + qd] = ok ? 1 : 0;
+            named_bar_sync(pair_bar, 64);
+            ok = ok && xo[(1 - wg) * 4 + qd] != 0;
+            return xc[(1 - wg) * kRows + r];
+        };
         // this thread's half of its row's query into Q buffer `part & 1`
         auto load_q = [&](const Walk& x, int part) {
             const bool in = x.qt * kRows + r < (x.nodes + 1) << a.g_log2;
@@ -827,8 +853,7 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
             }
             tmem_st32(tl + kQCol + (part & 1) * 64 + wg * 32, q);
             tmem_wait_st();
-            tc_fence_before();
-            mbar_arrive(&q_ready[part & 1]);
+            arrive(&q_ready[part & 1]);
         };
         bool have = w.next(a), ok = true;
         pdl_wait();
@@ -851,20 +876,22 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
             if (kSource == kWidened) ref_ahead = __ldcg(refs + t0);
             for (int t = t0; t < t1; t++, n++) {
                 // visible keys of this row among this warpgroup's 64 of the tile
-                uint64_t vis = row_ok ? ~0ull : 0ull;
-                if (t >= whole && row_ok) {
+                // (of a whole cache tile all, in a row of no node too: it is not written)
+                uint64_t vis = ~0ull;
+                bool all_seen = true;
+                if (t >= whole) {
                     const int o = (t - whole) * kKeys + cb - tail - 1;  // tree node of the first key (negative: cache, row 0)
                     vis = 0ull;
-                    if (b > 0 && o < nodes) {
+                    if (b > 0 && row_ok && o < nodes) {
                         vis = mask_bits(a.mask + (static_cast<long long>(s) * a.B + b - 1) * a.mw, a.mw, o);
                         if (nodes - o < 64) vis &= (1ull << (nodes - o)) - 1ull;
                     }
                     if (o < 0) vis |= o <= -64 ? ~0ull : (1ull << -o) - 1ull;
+                    all_seen = __all_sync(kFull, vis == ~0ull);
                 }
-                const bool all_seen = __all_sync(kFull, vis == ~0ull);
-                // Both warps of the lane quarter reach both pair barriers of every
-                // iteration and leave the loop at the same point: a failed wait is
-                // exchanged with the row max and acted on after the barriers.
+                // Both warps of the lane quarter reach the exchange of every iteration and
+                // leave the loop at the same point: a failed wait is exchanged with the row
+                // max and acted on after it.
                 if (kConv && ok && !warp_wait<1>(&sc_full[n % G_::kRing], static_cast<uint32_t>(n / G_::kRing) & 1u, abort)) ok = false;
                 if (ok && !warp_wait<1>(s_full, static_cast<uint32_t>(n) & 1u, abort)) ok = false;
                 if (!ok) attn_timeout(a.status, abort);
@@ -879,25 +906,21 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                     }
                     tc_fence_after();
                     tmem_ld64(tl + kSCol + cb, sv);
-                    tc_fence_before();
-                    mbar_arrive(s_empty);
-                    if (all_seen) {
+                    arrive(s_empty);
+                    if (!all_seen) {
 #pragma unroll
-                        for (int c = 0; c < 64; c += 2) mx = fmaxf(mx, fmaxf(sv[c], sv[c + 1]));
-                    } else {
-#pragma unroll
-                        for (int c = 0; c < 64; c++) {
+                        for (int c = 0; c < 64; c++)
                             if (!((vis >> c) & 1ull)) sv[c] = -INFINITY;
-                            mx = fmaxf(mx, sv[c]);
-                        }
                     }
+                    // (four chains: one alone is a third of the tile's time in latencies)
+                    float m4[4] = {sv[0], sv[1], sv[2], sv[3]};
+#pragma unroll
+                    for (int c = 4; c < 60; c += 8)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) m4[e] = fmaxf(m4[e], fmaxf(sv[c + e], sv[c + 4 + e]));
+                    mx = fmaxf(fmaxf(fmaxf(m4[0], sv[60]), fmaxf(m4[1], sv[61])), fmaxf(fmaxf(m4[2], sv[62]), fmaxf(m4[3], sv[63])));
                 }
-                xch[wg * kRows + r] = mx;
-                if (lane == 0) xok[wg * 4 + qd] = ok ? 1 : 0;
-                named_bar_sync(pair_bar, 64);
-                mx = fmaxf(mx, xch[(1 - wg) * kRows + r]);
-                ok = ok && xok[(1 - wg) * 4 + qd] != 0;
-                named_bar_sync(pair_bar, 64);  // both read before the next tile's write
+                mx = fmaxf(mx, exchange(mx, ok));
                 if (!ok) break;
                 const float mx2 = mx * rt;
                 const bool higher = mx2 > m_run + kSlack8;
@@ -960,8 +983,7 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 tmem_st32(tl + kPCol + (n & 1) * 64 + wg * 32, pk);
                 tmem_wait_st();
                 l += kF16 ? lsum * __uint_as_float(0x7F000000u - __float_as_uint(down)) : lsum;  // (1 / down)
-                tc_fence_before();
-                mbar_arrive(&p_full[n & 1]);
+                arrive(&p_full[n & 1]);
                 if (t == t0) {
                     // the next part's queries: that buffer's last reader, the part before
                     // this one, is done, since this part's S has been seen
@@ -974,18 +996,12 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 attn_timeout(a.status, abort);
                 ok = false;
             }
-            xch[wg * kRows + r] = l;
-            if (lane == 0) xok[wg * 4 + qd] = ok ? 1 : 0;
-            named_bar_sync(pair_bar, 64);
-            l += xch[(1 - wg) * kRows + r];
-            ok = ok && xok[(1 - wg) * 4 + qd] != 0;
-            named_bar_sync(pair_bar, 64);
+            l += exchange(l, ok);
             if (!ok) break;
             tc_fence_after();
             float o[64];
             tmem_ld64(tl + kOCol + cb, o);
-            tc_fence_before();
-            mbar_arrive(o_free);
+            arrive(o_free);
             if (full_unit) {
                 // rows in whole lines: 8 lanes exchange their rows' 8 pieces
                 const float inv = l > 0.0f ? (kF16 ? vref : 1.0f) / l : 0.0f;
