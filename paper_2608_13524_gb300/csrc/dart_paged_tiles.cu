@@ -100,6 +100,12 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
     return *reinterpret_cast<float2*>(&r);
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
 // Two e4m3 codes as an f16 pair: exact.
 __device__ __forceinline__ uint32_t codes_to_f16(uint32_t two) {
     uint32_t r;
@@ -572,6 +578,12 @@ __device__ __forceinline__ void transpose8(uint4 (&y)[8], int lane) {
     }
 }
 
+// A wait of a whole warp: where the phase has ended already, as it has most of the
+// time, one poll and one vote.
+__device__ __forceinline__ bool soon(uint64_t* bar, uint32_t parity, volatile int* abort) {
+    return __all_sync(kFull, mbar_try_wait(bar, parity)) || warp_wait<1>(bar, parity, abort);
+}
+
 // Bits [o, o + 64) of a row of mask words (o >= -128; bits outside are 0).
 __device__ __forceinline__ uint64_t mask_bits(const uint64_t* m, int mw, int o) {
     if (o <= -64) return 0ull;
@@ -892,8 +904,8 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 // Both warps of the lane quarter reach the exchange of every iteration and
                 // leave the loop at the same point: a failed wait is exchanged with the row
                 // max and acted on after it.
-                if (kConv && ok && !warp_wait<1>(&sc_full[n % G_::kRing], static_cast<uint32_t>(n / G_::kRing) & 1u, abort)) ok = false;
-                if (ok && !warp_wait<1>(s_full, static_cast<uint32_t>(n) & 1u, abort)) ok = false;
+                if (kConv && ok && !soon(&sc_full[n % G_::kRing], static_cast<uint32_t>(n / G_::kRing) & 1u, abort)) ok = false;
+                if (ok && !soon(s_full, static_cast<uint32_t>(n) & 1u, abort)) ok = false;
                 if (!ok) attn_timeout(a.status, abort);
                 float sv[64];
                 float mx = -INFINITY, rt = rs, vtile = 0.0f;
@@ -912,13 +924,13 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                         for (int c = 0; c < 64; c++)
                             if (!((vis >> c) & 1ull)) sv[c] = -INFINITY;
                     }
-                    // (four chains: one alone is a third of the tile's time in latencies)
+                    // (four chains: one alone would be a third of the tile's time in latencies)
                     float m4[4] = {sv[0], sv[1], sv[2], sv[3]};
 #pragma unroll
                     for (int c = 4; c < 60; c += 8)
 #pragma unroll
-                        for (int e = 0; e < 4; e++) m4[e] = fmaxf(m4[e], fmaxf(sv[c + e], sv[c + 4 + e]));
-                    mx = fmaxf(fmaxf(fmaxf(m4[0], sv[60]), fmaxf(m4[1], sv[61])), fmaxf(fmaxf(m4[2], sv[62]), fmaxf(m4[3], sv[63])));
+                        for (int e = 0; e < 4; e++) m4[e] = max3(m4[e], sv[c + e], sv[c + 4 + e]);
+                    mx = max3(max3(m4[0], m4[1], sv[60]), max3(m4[2], m4[3], sv[61]), fmaxf(sv[62], sv[63]));
                 }
                 mx = fmaxf(mx, exchange(mx, ok));
                 if (!ok) break;
@@ -934,17 +946,12 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                     down = fmaxf(vtile / vnew, 8.6736173798840355e-19f);
                     vref = vnew;
                 }
-                // P buffer n & 1 was last read by PV(n - 2); O must be stable (PV(n - 1)
-                // done) only when it is rescaled.  On a timeout this tile is
-                // skipped; the pair leaves the loop together at the next exchange.
-                if (n > 1 && !warp_wait<1>(&pv_done[n & 1], (static_cast<uint32_t>(n >> 1) & 1u) ^ 1u, abort)) {
-                    attn_timeout(a.status, abort);
-                    ok = false;
-                    continue;
-                }
-                tc_fence_after();
+                // P buffer n & 1 was last read by PV(n - 2), which was issued before S(n) and so
+                // ended before s_full's arrival; O must be stable (PV(n - 1) done) only when
+                // it is rescaled.  On a timeout this tile is skipped; the pair leaves the loop
+                // together at the next exchange.
                 if (t > t0 && __any_sync(kFull, resc)) {
-                    if (!warp_wait<1>(&pv_done[(n - 1) & 1], static_cast<uint32_t>((n - 1) >> 1) & 1u, abort)) {
+                    if (!soon(&pv_done[(n - 1) & 1], static_cast<uint32_t>((n - 1) >> 1) & 1u, abort)) {
                         attn_timeout(a.status, abort);
                         ok = false;
                         continue;
@@ -992,7 +999,7 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 }
             }
             // the pair leaves together: an `ok` lost after the last exchange is exchanged here
-            if (ok && !warp_wait<1>(&pv_done[(n - 1) & 1], static_cast<uint32_t>((n - 1) >> 1) & 1u, abort)) {
+            if (ok && !soon(&pv_done[(n - 1) & 1], static_cast<uint32_t>((n - 1) >> 1) & 1u, abort)) {
                 attn_timeout(a.status, abort);
                 ok = false;
             }
