@@ -774,8 +774,8 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 const uint32_t k_lo = smem_u32(sK) >> 4, v_lo = smem_u32(sV) >> 4, base = __shfl_sync(kFull, tmem, 0);
                 auto issue_s = [&](int n, int part) -> bool {
                     const int st = n % kStages;
-                    if (!warp_wait(&k_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort) ||
-                        (n > 0 && !warp_wait(s_empty, static_cast<uint32_t>(n - 1) & 1u, abort)))
+                    if (!soon(&k_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort) ||
+                        (n > 0 && !soon(s_empty, static_cast<uint32_t>(n - 1) & 1u, abort)))
                         return false;
                     tc_fence_after();
                     mma_s(base + kSCol, base + kQCol + __shfl_sync(kFull, part & 1, 0) * 64, __shfl_sync(kFull, (k_lo + st * (kTile >> 4)) & 0x3FFFu, 0), idesc_s);
@@ -786,7 +786,7 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 bool have = w.next(a), ok = true;
                 int n = 0, part = 0, t = w.t0, t1 = w.t1, t0 = w.t0;
                 if (have) {
-                    ok = warp_wait(&q_ready[0], 0, abort);
+                    ok = soon(&q_ready[0], 0, abort);
                     tc_fence_after();
                     ok = ok && issue_s(0, 0);
                 }
@@ -799,16 +799,16 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                         t = t0 = w.t0;
                         t1 = w.t1;
                         part++;
-                        if (have) ok = warp_wait(&q_ready[part & 1], static_cast<uint32_t>(part >> 1) & 1u, abort);
+                        if (have) ok = soon(&q_ready[part & 1], static_cast<uint32_t>(part >> 1) & 1u, abort);
                     }
                     if (have && ok) {
                         tc_fence_after();
                         ok = issue_s(n + 1, part);
                     }
                     const int st = n % kStages;
-                    ok = ok && warp_wait(&p_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, abort) &&
-                         warp_wait(&v_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort) &&
-                         (!first || my_part == 0 || warp_wait(o_free, static_cast<uint32_t>(my_part - 1) & 1u, abort));
+                    ok = ok && soon(&p_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, abort) &&
+                         soon(&v_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort) &&
+                         (!first || my_part == 0 || soon(o_free, static_cast<uint32_t>(my_part - 1) & 1u, abort));
                     if (!ok) break;
                     tc_fence_after();
                     mma_pv(base + kOCol, base + kPCol + __shfl_sync(kFull, n & 1, 0) * 64,
@@ -942,8 +942,9 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 float alpha_o = alpha, down = 1.0f;  // (down: P's part for the tile's power of two; 2^-60 is as good as nothing)
                 if (kF16) {
                     const float vnew = fmaxf(vref, vtile);
-                    alpha_o *= vref / vnew;
-                    down = fmaxf(vtile / vnew, 8.6736173798840355e-19f);
+                    const float inv = __uint_as_float(0x7F000000u - __float_as_uint(vnew));  // (powers of two: exact)
+                    alpha_o *= vref * inv;
+                    down = fmaxf(vtile * inv, 8.6736173798840355e-19f);
                     vref = vnew;
                 }
                 // P buffer n & 1 was last read by PV(n - 2), which was issued before S(n) and so
@@ -1062,7 +1063,7 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 }
                 const int st = n % kStages, rs = raw % raw_stages;
                 const long long side = (static_cast<long long>(w.s) * a.Hkv + w.head) * ta.sk + (t - w.whole) * kKeys + key;
-                if (ok && cache_tile && !warp_wait(&raw_full[rs], static_cast<uint32_t>(raw / raw_stages) & 1u, abort)) ok = false;
+                if (ok && cache_tile && !soon(&raw_full[rs], static_cast<uint32_t>(raw / raw_stages) & 1u, abort)) ok = false;
                 float sc[2];
 #pragma unroll
                 for (int h = 0; h < 2; h++)
@@ -1082,7 +1083,7 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                     (kv ? tile_ref[n % G_::kRing].y : tile_ref[n % G_::kRing].x) = ref;
                     mbar_arrive(&sc_full[n % G_::kRing]);
                 }
-                if (!warp_wait(&op_empty[st], (static_cast<uint32_t>(n / kStages) & 1u) ^ 1u, abort)) {
+                if (!soon(&op_empty[st], (static_cast<uint32_t>(n / kStages) & 1u) ^ 1u, abort)) {
                     ok = false;
                     if (cache_tile) raw++;
                     continue;
