@@ -501,12 +501,23 @@ def _rows(t, name, shape, dev):
     return t.data_ptr(), sr
 
 
-def _current(stream):
-    """The current device and the CUDA handle of `stream` (None: its current one)."""
+def _current(stream, own):
+    """The current device, which has to be `own`, where an object's memory is,
+    and the CUDA handle of `stream` (None: its current one)."""
     dev = torch.cuda.current_device()
+    if dev != own:
+        raise ValueError(f"made on device {own}, called with {dev} as the current one")
     if stream is None:
         return dev, torch._C._cuda_getCurrentRawStream(dev)
     return dev, stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _status(t, dev):
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.numel() < 1 or t.get_device() != dev:
+        raise _bad(t, "status", torch.int32, (1,))
+    return t.data_ptr()
 
 
 class KVCache:
@@ -524,7 +535,7 @@ class KVCache:
         ptr = [_expect(k, "k", k.dtype, k.shape, dev), _expect(v, "v", k.dtype, k.shape, dev)]
         ptr += [_expect(x, m, torch.float32, (n, heads, page), dev) if fp8 else None
                 for x, m in ((k_scale, "k_scale"), (v_scale, "v_scale"))]
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.k, self.v, self.k_scale, self.v_scale, self.dev = k, v, k_scale, v_scale, dev
         self.num_pages, self.Hkv, self.page_size, self.dh = n, heads, page, dh
         self.c = DartKvCache(n, page, heads, dh, DART_KV_E4M3 if fp8 else DART_KV_BF16, *ptr)
         self.ref = C.byref(self.c)
@@ -540,7 +551,7 @@ class KVCache:
         """Writes n_rows[s] tokens of every sequence from position lens[s] on:
         the rows rows[s, :n_rows[s]] of k and v [nseq, R, Hkv, dh] bf16 (rows
         None: the first ones).  lens is not advanced."""
-        dev, st = _current(stream)
+        dev, st = _current(stream, self.dev)
         nseq, R = k.shape[:2]
         shape = (nseq, R, self.Hkv, self.dh)
         kp, ks = _rows(k, "k", shape, dev)
@@ -550,7 +561,7 @@ class KVCache:
             self.ref, nseq, pages, _expect(page_table, "page_table", torch.int32, (nseq, pages), dev),
             _expect(lens, "lens", torch.int32, (nseq,), dev), R, kp, ks, vp, vs,
             None if rows is None else _expect(rows, "rows", torch.int32, (nseq, R), dev),
-            _expect(n_rows, "n_rows", torch.int32, (nseq,), dev), rope_theta, _ptr(status), st), "dart_cache_append")
+            _expect(n_rows, "n_rows", torch.int32, (nseq,), dev), rope_theta, _status(status, dev), st), "dart_cache_append")
 
 
 class PagedTreeAttention:
@@ -565,6 +576,7 @@ class PagedTreeAttention:
         n = int(lib().dart_paged_attention_workspace(self.ref, cache.ref))
         if n == 0:
             raise DartError(DART_ERR_INVALID, "dart_paged_attention_workspace")
+        _current(None, cache.dev)
         self.workspace = _empty((n,), dtype=torch.uint8, device="cuda")
         self.out = _empty((nseq, B + 1, Hq, cache.dh), dtype=torch.bfloat16, device="cuda")
 
@@ -573,8 +585,8 @@ class PagedTreeAttention:
         (row 0: the last verified token), page_table [nseq, max_pages] and
         lens [nseq] int32; depths [nseq, B] int32, mask [nseq, B, ceil(B / 64)]
         int64 and n_nodes [nseq] int32 as emitted.  Returns self.out."""
-        dev, st = _current(stream)
         kv, (nseq, R, Hq, dh) = self.cache, self.out.shape
+        dev, st = _current(stream, kv.dev)
         qp, qs = _rows(q, "q", (nseq, R, Hq, dh), dev)
         kp, ks = _rows(k_tree, "k_tree", (nseq, R, kv.Hkv, dh), dev)
         vp, vs = _rows(v_tree, "v_tree", (nseq, R, kv.Hkv, dh), dev)
@@ -586,7 +598,7 @@ class PagedTreeAttention:
         _check(lib().dart_paged_attention(
             self.ref, kv.ref, _expect(page_table, "page_table", torch.int32, (nseq, self.max_pages), dev),
             _expect(lens, "lens", torch.int32, (nseq,), dev), qp, qs, kp, ks, vp, vs, *tree, self.out.data_ptr(),
-            self.workspace.data_ptr(), self.workspace.numel(), _ptr(status), st), "dart_paged_attention")
+            self.workspace.data_ptr(), self.workspace.numel(), _status(status, dev), st), "dart_paged_attention")
         return self.out
 
 
@@ -601,6 +613,7 @@ class TreeVerifier:
         self.cfg = DartVerifyConfig(self.nseq, self.B, self.V, DART_F32, self.V, float(temperature))
         self.ref = C.byref(self.cfg)
         i32 = lambda *shape: _empty(shape, dtype=torch.int32, device="cuda")  # noqa: E731
+        self.dev = torch.cuda.current_device()
         self.out = dict(n_rows=i32(nseq), rows=i32(nseq, B + 1), tokens=i32(nseq, B + 1),
                         logp=_empty((nseq, B + 1), dtype=torch.float32, device="cuda"))
         self.out_ptr = tuple(self.out[m].data_ptr() for m in ("n_rows", "rows", "tokens", "logp"))
@@ -610,7 +623,7 @@ class TreeVerifier:
         parents [nseq, B] and n_nodes [nseq] int32 as emitted; u [nseq, B + 1]
         uniform and noise [nseq, V] Exp(1) fp32 (temperature 0: none).
         Returns the dict of outputs: what KVCache.append takes is in it."""
-        dev, st = _current(stream)
+        dev, st = _current(stream, self.dev)
         nseq, B, V = self.nseq, self.B, self.V
         f32 = logits.dtype is torch.float32
         if not f32 and logits.dtype is not torch.bfloat16 or logits.shape != (nseq, B + 1, V) or logits.get_device() != dev:

@@ -134,6 +134,17 @@ def test_binding_refuses_what_a_pointer_hides():
         dart.KVCache(z.to(torch.float8_e4m3fn), z.to(torch.float8_e4m3fn))
 
 
+def test_binding_refuses_another_device_and_a_status_on_the_host(monkeypatch):
+    import torch
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    with pytest.raises(ValueError, match="made on device 0"):
+        dart._current(7, 0)
+    assert dart._current(7, 1) == (1, 7)
+    with pytest.raises(ValueError, match="status"):
+        dart._status(torch.zeros(1, dtype=torch.int32), 1)
+    assert dart._status(None, 1) is None
+
+
 # ------------------------------------------------------------ the oracle
 
 def test_oracle_attention_is_the_contiguous_oracle():
