@@ -511,7 +511,10 @@ int clusters_at_once(int dev) {
 
 template <typename T>
 int launch_verify(const VerifyArgs& a, int nseq, int dev, cudaStream_t st) {
-    // 16 CTAs a sequence as long as all clusters run at once, else 8
+    // 16 CTAs a sequence up to half as many again as run at once (the last begin when
+    // the first end), else 8.  V = 151936, 16 CTAs / 8: one sequence 27.6 / 31.1 us,
+    // four 13.7 / 16.9 (short walks), eight 31.2 / 36.2, ten 27.7 / 32.0, fourteen 42.7 /
+    // 32.0, 64 134 / 91; V = 32000, eight 34.3 / 33.4.
     const int large = clusters_at_once<T, 16>(dev), small = clusters_at_once<T, 8>(dev);
     if (!large || !small) return DART_ERR_CUDA;
     auto go = [&](auto ctas) {
@@ -519,7 +522,7 @@ int launch_verify(const VerifyArgs& a, int nseq, int dev, cudaStream_t st) {
         return launch_pdl_cluster(verify_tree_kernel<T, kCtas>, dim3(static_cast<unsigned>(nseq) * kCtas), dim3(kVerifyThreads),
                                   sizeof(VerifySmem<kCtas>) + kNoise * 4, st, kCtas, a);
     };
-    const cudaError_t e = nseq <= large ? go(std::integral_constant<int, 16>{}) : go(std::integral_constant<int, 8>{});
+    const cudaError_t e = nseq <= large + large / 2 ? go(std::integral_constant<int, 16>{}) : go(std::integral_constant<int, 8>{});
     return e == cudaSuccess ? DART_OK : DART_ERR_CUDA;
 }
 
