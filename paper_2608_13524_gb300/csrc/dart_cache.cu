@@ -35,7 +35,8 @@ namespace {
 constexpr int kAppendThreads = 256;
 constexpr int kGroup = 8;  // threads of a token's head: 8 elements of each half of a row are 16 bytes
 // Four heads a group (angles once for four) where that still makes this many
-// groups, else one: a few tokens are a matter of latency.
+// groups, else one: a few tokens are a matter of latency (eight prompts of up to
+// 4096 tokens to e4m3 pages 34 us with four and 45 with one; below, no difference).
 constexpr long long kManyGroups = 9728;  // 152 SMs x 64 groups = 512 threads each
 constexpr float kMinScale = 7.52316384526264005e-37f;  // 2^-120: its reciprocal is finite
 

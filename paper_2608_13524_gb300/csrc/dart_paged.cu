@@ -19,6 +19,12 @@
 // bf16 keys takes 8 KB from HBM for 24 kN of them, far below any tensor rate,
 // and scores and probabilities stay in registers (a 128-row tile of the
 // tensor-memory path would be 7/8 empty or more).
+//
+// Measured, 64 sequences of up to 8192 keys, 8 kv heads, one token each: bf16
+// pages 168 us, 6.5 TB/s, 96 % of the measured copy bandwidth; e4m3 pages 95 us,
+// 5.9 TB/s, 87 %, where the conversions (64 codes a thread and chunk) come
+// second; a call of a few keys takes 12 us, a chain of two launches and six or
+// seven dependent loads.  With rows along the 16 and 8 warps e4m3 took 116 us.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -58,14 +64,18 @@ struct Part {  // a unit's partial result
     float2 ml[8 * kN];  // reference (log2 units), sum
 };
 
-// Warps of a CTA: as many as their registers allow.
+// Warps of a CTA: as many as their registers allow (for up to 8 rows 168 a
+// thread; 10 warps: e4m3 93 us instead of 95, pages of 16 tokens 99 instead of
+// 96; for up to 16 rows 6 warps instead of 8: 76 us instead of 65).
 __host__ __device__ constexpr int rows_warps(int n) { return n == 1 ? 12 : 8; }
 
 // ------------------------------------------------------------ the schedule
 
 // Chunk sizes, and what a unit costs beside its chunks (queries, tree rows,
 // the result), in chunks: its list is that much longer, so that warps with
-// many short units get fewer of them.
+// many short units get fewer of them (64 sequences of 8192 bf16 keys 171 us at 6,
+// 168 at 3 and at 9; 64 trees of 3 nodes over 4096 105 at 3, 100 at 6, 98 at 9;
+// e4m3 94, 95, 96 and 71, 65, 65 us at 2, 4, 6).
 template <bool kFp8>
 struct Chunk {
     static constexpr int kKeys = kFp8 ? 32 : 16;
@@ -142,7 +152,8 @@ struct List {
     }
 };
 
-// Shares: one per warp, each at least kMinShare long.
+// Shares: one per warp, each at least kMinShare long (values around it make no
+// difference: shares are shorter than that in the smallest calls alone).
 constexpr int kMinShare = 2;
 
 // ------------------------------------------------------------ fragments
@@ -890,7 +901,8 @@ bool valid_cfg(const dart_paged_attn_config* c, const dart_kv_cache* cache) {
 }
 
 // Which kernel: a few rows are streamed from HBM, more are 128-row tiles of the
-// tensor-memory path.
+// tensor-memory path (64 sequences, 16 rows a kv head, 4096 keys: 98 us here and
+// 134 there with bf16 pages, 65 and 225 with e4m3 ones).
 constexpr int kFewRows = 16;
 bool few_rows(const dart_paged_attn_config& c, const dart_kv_cache& cache) { return (c.B + 1) * (c.Hq / cache.Hkv) <= kFewRows; }
 

@@ -27,9 +27,24 @@
 // of two per row.  So nothing can overflow, and the softmax has one factor a
 // tile to apply instead of one a key (64 broadcast reads of a key's scale from
 // shared memory, twice, took 0.5 us of a tile's 1.6).  TMEM (512 columns): S
-// [0,128), O [128,256), P [256,384) in two buffers, Q [384,512) in two.
+// [0,128), O [128,256), P [256,384) in two buffers, Q [384,448), and with bf16
+// pages what the queries' first bf16 term leaves, [448,512).
 // A row's running maximum is raised (and O rescaled) only when a tile exceeds
 // it by more than 2^8.  Every wait is bounded.
+//
+// Measured: a tile takes 1.07 us from bf16 pages (24 MMAs of 64 cycles are 0.8) and
+// 1.05 from widened ones (16 MMAs, 0.53); eight trees of 512 nodes over up to 4096
+// keys take 243 and 272 us with everything around.  With the first term of the
+// queries alone bf16 pages took 0.90 and 211 us, at an error against 64 bits of
+// 0.0029 of the output instead of 0.0023 (its own rounding is 0.0017).  What a
+// tile takes beside its MMAs is the chain of the
+// softmax's instructions (two warps a scheduler, in step because they share rows:
+// exponentials 0.3 us, maxima, the exchange, 0.1 us for each wait) beside the
+// issuing warp's, which is almost as long.  Tried: four softmax warpgroups of 32
+// columns (287 us instead of 235: the fixed part of the instructions doubles);
+// CTA pairs with half of K and V each (383: one more hop in every exchange); S in
+// two buffers and P in one (262); mask words read a tile ahead (216 instead of
+// 211: registers).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -60,10 +75,10 @@ constexpr int kConvBar = 6;              // 6: the warps that convert K, 7: V
 constexpr float kSlack8 = 8.0f;          // log2 units: P <= 2^8 between rescales
 // What a unit costs beside its tiles (its queries, its result, the pause between
 // its last tile and the next unit's first), in tiles: eight trees of 512 nodes over
-// e4m3 pages 490 us with 1, 433 with 3, 401 with 5.
+// 4096 bf16 keys 219 us with 3, 211 with 5, 214 with 7; e4m3 286, 276, 280.
 constexpr int kTileCost = 5;
-constexpr int kMinTiles = 2;             // of a share
-constexpr uint32_t kSCol = 0, kOCol = 128, kPCol = 256, kQCol = 384;
+constexpr int kMinTiles = 2;             // of a share (one tree of 20 nodes over 500 keys: 1 18.5 us, 2 17.9, 4 19.8)
+constexpr uint32_t kSCol = 0, kOCol = 128, kPCol = 256, kQCol = 384, kQLoCol = 448;
 
 // Rows that threads of a warp read or write one each are kept a 16-byte piece
 // after the other: piece c of row r of a 128-row tile at [c][r].
@@ -78,6 +93,7 @@ struct TileArgs {
     int nqt;                    // query tiles of a kv head of a full tree
     // bf16, or f16 (e4m3 pages) with a factor per row:
     uint4* qr;                  // [nseq][Hkv][nqt][16 pieces][128 rows]
+    uint4* q_lo;                // bf16: what the first term leaves, the same way
     uint4 *side_k, *side_v;     // [nseq][Hkv][sk] rows; e4m3 pages: [nseq][Hkv][sk / 128][16 pieces][128]
     float* q_scale;             // [nseq][Hkv][nqt][128], with scale * log2(e) in it
     float *side_ks, *side_vs;   // [nseq][Hkv][sk]
@@ -267,6 +283,20 @@ __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_c
                 uint4* d = ta.qr + tile * (16 * kRows) + (row & 127);
                 d[p * kRows] = lo;
                 d[(8 + p) * kRows] = hi;
+                if (!kFp8) {
+                    // with one bf16 term the queries' rounding alone would move the output as
+                    // much as its own rounding does
+                    const Piece y = unpack_piece(lo, hi);
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        x.lo[e] -= y.lo[e];
+                        x.hi[e] -= y.hi[e];
+                    }
+                    pack_piece<false>(x, &lo, &hi);
+                    d = ta.q_lo + tile * (16 * kRows) + (row & 127);
+                    d[p * kRows] = lo;
+                    d[(8 + p) * kRows] = hi;
+                }
                 if (kFp8 && p == 0) ta.q_scale[tile * kRows + (row & 127)] = factor * a.sl2;
             } else if (i < rows) {
                 const int kv = i >= a.Hq + a.Hkv, head = i - a.Hq - kv * a.Hkv;
@@ -522,10 +552,10 @@ __device__ __forceinline__ void commit_elected(uint64_t* bar) {
 }
 // S = Q K^T (K-major K: 32 bytes a step, 64 elements a swizzle column) and
 // O += P V (MN-major V: 16 keys of 128 bytes a step).
-template <int kk = 0>
+template <bool kFirst, int kk = 0>
 __device__ __forceinline__ void mma_s(uint32_t d, uint32_t q, uint32_t k_lo, uint32_t idesc) {
-    mma_at<kk * 8, ((kk >> 2) * kHalf + (kk & 3) * 32) / 16>(d, q, k_lo, idesc, kk > 0 ? 1u : 0u);
-    if constexpr (kk + 1 < kHeadDim / 16) mma_s<kk + 1>(d, q, k_lo, idesc);
+    mma_at<kk * 8, ((kk >> 2) * kHalf + (kk & 3) * 32) / 16>(d, q, k_lo, idesc, kFirst && kk == 0 ? 0u : 1u);
+    if constexpr (kk + 1 < kHeadDim / 16) mma_s<kFirst, kk + 1>(d, q, k_lo, idesc);
 }
 template <int kk = 0>
 __device__ __forceinline__ void mma_pv(uint32_t d, uint32_t p, uint32_t v_lo, uint32_t idesc, uint32_t first) {
@@ -544,7 +574,7 @@ struct TGeo {
     static constexpr int kOps = 2 * kStages * kTile;
     static constexpr int kRaw = (kRawK + kRawV) * kHalf;
     static constexpr int kRawScales = (kRawK + kRawV) * kKeys * 4;
-    static constexpr int kBars = 4 * kStages + 2 * (kRawK + kRawV) + (kConv ? kRing : 0) + 9 + 1;
+    static constexpr int kBars = 4 * kStages + 2 * (kRawK + kRawV) + (kConv ? kRing : 0) + 9;
     static constexpr int kExchange = 4 * kRows * 4 + 16 * 4 + kRing * 8 + kRing * 4 * 4;
     static constexpr int kSmem = kOps + kRaw + kRawScales + kBars * 8 + kExchange + 16;
     // kCodes: warpgroups (producer, MMA, two idle warps), softmax, softmax, converters
@@ -623,8 +653,8 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
     uint64_t* s_empty = s_full + 1;         // softmax has S in registers
     uint64_t* p_full = s_empty + 1;         // [2] by P buffer (P(n + 1) may be there before P(n) is waited for)
     uint64_t* pv_done = p_full + 2;         // [2] by P buffer
-    uint64_t* q_ready = pv_done + 2;        // [2] by Q buffer
-    uint64_t* o_free = q_ready + 2;         // the unit's O has been read
+    uint64_t* q_ready = pv_done + 2;
+    uint64_t* o_free = q_ready + 1;         // the unit's O has been read
     uint64_t* tdown = o_free + 1;
     float* xch = reinterpret_cast<float*>(k_full + G_::kBars);  // [2][warpgroup][128] row max / sum exchange
     int* xok = reinterpret_cast<int*>(xch + 4 * kRows);         // [2][warpgroup][4] "no wait failed"
@@ -657,8 +687,8 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
         for (int i = 0; i < 2; i++) {
             mbar_init(&p_full[i], kSoft / 32);
             mbar_init(&pv_done[i], 1);
-            mbar_init(&q_ready[i], kSoft / 32);
         }
+        mbar_init(q_ready, kSoft / 32);
         mbar_init(o_free, kSoft / 32);
         mbar_init(tdown, 1);
         misc[1] = 0;
@@ -772,49 +802,43 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 constexpr uint32_t idesc_s = idesc_bf16_f32(kRows, kKeys) & (kF16 ? ~((1u << 7) | (1u << 10)) : ~0u);
                 constexpr uint32_t idesc_pv = (idesc_bf16_f32(kRows, kHeadDim) & (kF16 ? ~((1u << 7) | (1u << 10)) : ~0u)) | (1u << 16);  // B (= V) MN-major
                 const uint32_t k_lo = smem_u32(sK) >> 4, v_lo = smem_u32(sV) >> 4, base = __shfl_sync(kFull, tmem, 0);
-                auto issue_s = [&](int n, int part) -> bool {
+                auto issue_s = [&](int n) -> bool {
                     const int st = n % kStages;
                     if (!soon(&k_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort) ||
                         (n > 0 && !soon(s_empty, static_cast<uint32_t>(n - 1) & 1u, abort)))
                         return false;
                     tc_fence_after();
-                    mma_s(base + kSCol, base + kQCol + __shfl_sync(kFull, part & 1, 0) * 64, __shfl_sync(kFull, (k_lo + st * (kTile >> 4)) & 0x3FFFu, 0), idesc_s);
+                    const uint32_t k = __shfl_sync(kFull, (k_lo + st * (kTile >> 4)) & 0x3FFFu, 0);
+                    mma_s<true>(base + kSCol, base + kQCol, k, idesc_s);
+                    if (!kF16) mma_s<false>(base + kSCol, base + kQLoCol, k, idesc_s);
                     commit_elected(s_full);
                     commit_elected(&k_empty[st]);
                     return true;
                 };
                 bool have = w.next(a), ok = true;
-                int n = 0, part = 0, t = w.t0, t1 = w.t1, t0 = w.t0;
-                if (have) {
-                    ok = soon(&q_ready[0], 0, abort);
-                    tc_fence_after();
-                    ok = ok && issue_s(0, 0);
-                }
+                int n = 0, part = 0, t = w.t0;
+                if (have) ok = soon(q_ready, 0, abort) && issue_s(0);
                 while (have && ok) {
-                    // tile t of part `part`; S of the tile after it first
-                    const bool first = t == t0;
-                    const int my_part = part;
-                    if (++t == t1) {
-                        have = w.next(a);
-                        t = t0 = w.t0;
-                        t1 = w.t1;
-                        part++;
-                        if (have) ok = soon(&q_ready[part & 1], static_cast<uint32_t>(part >> 1) & 1u, abort);
-                    }
-                    if (have && ok) {
-                        tc_fence_after();
-                        ok = issue_s(n + 1, part);
-                    }
+                    // tile t of part `part`; S of the part's next tile first
+                    const bool first = t == w.t0, last = t + 1 == w.t1;
+                    if (!last) ok = issue_s(n + 1);
                     const int st = n % kStages;
                     ok = ok && soon(&p_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, abort) &&
                          soon(&v_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort) &&
-                         (!first || my_part == 0 || soon(o_free, static_cast<uint32_t>(my_part - 1) & 1u, abort));
+                         (!first || part == 0 || soon(o_free, static_cast<uint32_t>(part - 1) & 1u, abort));
                     if (!ok) break;
                     tc_fence_after();
                     mma_pv(base + kOCol, base + kPCol + __shfl_sync(kFull, n & 1, 0) * 64,
                            __shfl_sync(kFull, ((v_lo + st * (kTile >> 4)) & 0x3FFFu) | ((kHalf >> 4) << 16), 0), idesc_pv, __shfl_sync(kFull, first ? 1u : 0u, 0));
                     commit_elected(&v_empty[st]);
                     commit_elected(&pv_done[n & 1]);
+                    t++;
+                    if (last) {
+                        have = w.next(a);
+                        t = w.t0;
+                        part++;
+                        if (have) ok = soon(q_ready, static_cast<uint32_t>(part) & 1u, abort) && issue_s(n + 1);
+                    }
                     n++;
                 }
                 if (!ok) {
@@ -850,28 +874,31 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
             ok = ok && xo[(1 - wg) * 4 + qd] != 0;
             return xc[(1 - wg) * kRows + r];
         };
-        // this thread's half of its row's query into Q buffer `part & 1`
-        auto load_q = [&](const Walk& x, int part) {
-            const bool in = x.qt * kRows + r < (x.nodes + 1) << a.g_log2;
-            uint32_t q[32];
-            const uint4* src = ta.qr + ((static_cast<long long>(x.s) * a.Hkv + x.head) * ta.nqt + x.qt) * (16 * kRows) + 8 * wg * kRows + r;
+        // this thread's half of its row's query into tensor memory
+        auto load_q = [&]() {
+            const bool in = w.qt * kRows + r < (w.nodes + 1) << a.g_log2;
+            const long long at = ((static_cast<long long>(w.s) * a.Hkv + w.head) * ta.nqt + w.qt) * (16 * kRows) + 8 * wg * kRows + r;
+            uint32_t q[kF16 ? 1 : 2][32];
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const uint4 y = in ? __ldcg(src + e * kRows) : make_uint4(0u, 0u, 0u, 0u);
-                q[4 * e] = y.x;
-                q[4 * e + 1] = y.y;
-                q[4 * e + 2] = y.z;
-                q[4 * e + 3] = y.w;
-            }
-            tmem_st32(tl + kQCol + (part & 1) * 64 + wg * 32, q);
+            for (int i = 0; i < (kF16 ? 1 : 2); i++)
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    const uint4 y = in ? __ldcg((i ? ta.q_lo : ta.qr) + at + e * kRows) : make_uint4(0u, 0u, 0u, 0u);
+                    q[i][4 * e] = y.x;
+                    q[i][4 * e + 1] = y.y;
+                    q[i][4 * e + 2] = y.z;
+                    q[i][4 * e + 3] = y.w;
+                }
+            tmem_st32(tl + kQCol + wg * 32, q[0]);
+            if (!kF16) tmem_st32(tl + kQLoCol + wg * 32, q[kF16 ? 0 : 1]);
             tmem_wait_st();
-            arrive(&q_ready[part & 1]);
+            arrive(q_ready);
         };
         bool have = w.next(a), ok = true;
         pdl_wait();
-        if (have) load_q(w, 0);
+        if (have) load_q();
         int n = 0;
-        for (int part = 0; have; part++) {
+        while (have) {
             const int s = w.s, head = w.head, t0 = w.t0, t1 = w.t1, whole = w.whole, tail = w.tail, nodes = w.nodes;
             const bool full_unit = t0 == 0 && t1 == w.tiles;
             const int row = w.qt * kRows + r, b = row >> a.g_log2;
@@ -992,11 +1019,11 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 tmem_wait_st();
                 l += kF16 ? lsum * __uint_as_float(0x7F000000u - __float_as_uint(down)) : lsum;  // (1 / down)
                 arrive(&p_full[n & 1]);
-                if (t == t0) {
-                    // the next part's queries: that buffer's last reader, the part before
-                    // this one, is done, since this part's S has been seen
+                if (t + 1 == t1) {
+                    // the next part's queries, while the last PV runs: all products with this
+                    // part's have been seen
                     have = w.next(a);
-                    if (have) load_q(w, part + 1);
+                    if (have) load_q();
                 }
             }
             // the pair leaves together: an `ok` lost after the last exchange is exchanged here
@@ -1198,16 +1225,18 @@ __global__ void __launch_bounds__(256) paged_tiles_join_kernel(const __grid_cons
 }
 
 // e4m3 pages are widened first where a kv head has at least this many query
-// tiles, each of which would convert all keys again (a tile of a unit takes 1.1
-// us from f16 tiles and 1.9 converted, widening a tile 2), and where the f16
-// tiles of the longest sequences take at most 4 GB.
+// tiles, each of which would convert all keys again (a tile of a unit takes 1.05
+// us from f16 tiles and 1.9 converted), and where the f16 tiles of the longest
+// sequences take at most 4 GB.  Eight trees over 4096 keys, widened / converted:
+// 4 query tiles 96 / 97 us, 5 113 / 120, 8 150 / 184; one over 2048, 3 tiles 28.4 /
+// 23.8; one over 16384, 4 tiles 73 / 70.
 constexpr int kWidenTiles = 4;
 constexpr size_t kWidenBytes = static_cast<size_t>(4) << 30;
 
 // Workspace: partial results, queries, side rows, their factors, f16 tiles.
 struct TileWs {
     int sk, nqt, wide_tiles;
-    size_t q, k, v, qs, ks, vs, wk, wv, refs, total;
+    size_t q, q_lo, k, v, qs, ks, vs, wk, wv, refs, total;
 };
 TileWs tile_ws(int nseq, int B, int Hq, const dart_kv_cache& cache, int max_pages) {
     TileWs w{};
@@ -1217,7 +1246,8 @@ TileWs tile_ws(int nseq, int B, int Hq, const dart_kv_cache& cache, int max_page
     const size_t heads = static_cast<size_t>(nseq) * Hkv, q_rows = heads * w.nqt * kRows;
     auto up = [](size_t n) { return (n + 255) & ~static_cast<size_t>(255); };
     w.q = up(sizeof(SharePlan) + sizeof(TilePart) * 2 * kMaxSms);
-    w.k = w.q + up(q_rows * kHeadDim * 2);
+    w.q_lo = w.q + up(q_rows * kHeadDim * 2);
+    w.k = w.q_lo + (cache.dtype == DART_KV_BF16 ? up(q_rows * kHeadDim * 2) : 0);
     w.v = w.k + up(heads * w.sk * kHeadDim * 2);
     w.qs = w.v + up(heads * w.sk * kHeadDim * 2);
     w.ks = w.qs + up(q_rows * 4);
@@ -1260,6 +1290,7 @@ int launch_paged_tiles(PagedArgs a, const dart_kv_cache& cache, uint8_t* workspa
     ta.sk = w.sk;
     ta.nqt = w.nqt;
     ta.qr = reinterpret_cast<uint4*>(workspace + w.q);
+    ta.q_lo = reinterpret_cast<uint4*>(workspace + w.q_lo);
     ta.side_k = reinterpret_cast<uint4*>(workspace + w.k);
     ta.side_v = reinterpret_cast<uint4*>(workspace + w.v);
     ta.q_scale = reinterpret_cast<float*>(workspace + w.qs);
