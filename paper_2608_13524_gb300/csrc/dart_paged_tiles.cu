@@ -4,17 +4,18 @@
 //
 // Launches of a call:
 //   paged_prep_kernel  rotated queries, one row per (kv head, tree row, head
-//       of the group); and, per sequence and kv head, the "side" keys and
+//       of the group), with bf16 pages as two bf16 terms; and, per sequence and kv head, the "side" keys and
 //       values: the last len % 128 cache tokens (in bf16), the tree rows
 //       (keys rotated), zeros up to a multiple of 128.  So all other cache
 //       tiles are whole, need no mask, and nothing unwritten is ever read.
+//   paged_widen_kernel  e4m3 pages that several query tiles read: as f16 tiles.
 //   paged_tiles_kernel  a unit is 128 query rows of a kv head against the
 //       whole cache tiles and the side tiles that its rows may see.  The
 //       tiles of all units form one list that the CTAs (one per SM) share
 //       evenly: ragged lengths, one long sequence and many short ones load
 //       every SM alike.  A CTA runs through its units without a pause: loads
-//       run ahead across units, and a unit's queries are in tensor memory
-//       before the unit before it has ended.
+//       run ahead across units, and a unit's queries are written while the
+//       last product of the unit before runs.
 //   paged_tiles_join_kernel  joins the units that several CTAs shared.
 //
 // Roles in a CTA: warp 0 loads tiles by TMA, page by page (K ring, V ring);
@@ -34,17 +35,16 @@
 //
 // Measured: a tile takes 1.07 us from bf16 pages (24 MMAs of 64 cycles are 0.8) and
 // 1.05 from widened ones (16 MMAs, 0.53); eight trees of 512 nodes over up to 4096
-// keys take 243 and 272 us with everything around.  With the first term of the
+// keys take 241 and 270 us with everything around.  With the first term of the
 // queries alone bf16 pages took 0.90 and 211 us, at an error against 64 bits of
-// 0.0029 of the output instead of 0.0023 (its own rounding is 0.0017).  What a
-// tile takes beside its MMAs is the chain of the
-// softmax's instructions (two warps a scheduler, in step because they share rows:
-// exponentials 0.3 us, maxima, the exchange, 0.1 us for each wait) beside the
-// issuing warp's, which is almost as long.  Tried: four softmax warpgroups of 32
-// columns (287 us instead of 235: the fixed part of the instructions doubles);
-// CTA pairs with half of K and V each (383: one more hop in every exchange); S in
-// two buffers and P in one (262); mask words read a tile ahead (216 instead of
-// 211: registers).
+// 0.0029 of the output instead of 0.0023 (its own rounding is 0.0017).  What a tile takes
+// beside its MMAs is the chain of the softmax's instructions (two warps a
+// scheduler, in step because they share rows: exponentials 0.3 us, maxima, the
+// exchange, 0.1 us for each wait) beside the issuing warp's, which is almost as
+// long.  Tried, when those eight trees took 235 us with bf16 pages: four softmax warpgroups of 32
+// columns (287 us: the fixed part of the instructions doubles); CTA pairs with half
+// of K and V each (383: one more hop in every exchange); S in two buffers and P in
+// one (262); later, mask words read a tile ahead (216 instead of 211: registers).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -75,8 +75,8 @@ constexpr int kConvBar = 6;              // 6: the warps that convert K, 7: V
 constexpr float kSlack8 = 8.0f;          // log2 units: P <= 2^8 between rescales
 // What a unit costs beside its tiles (its queries, its result, the pause between
 // its last tile and the next unit's first), in tiles: eight trees of 512 nodes over
-// 4096 bf16 keys 219 us with 3, 211 with 5, 214 with 7; e4m3 286, 276, 280.
-constexpr int kTileCost = 5;
+// 4096 bf16 keys 241 us with 3 and 4, 245 with 6; e4m3 273, 270, 274.
+constexpr int kTileCost = 4;
 constexpr int kMinTiles = 2;             // of a share (one tree of 20 nodes over 500 keys: 1 18.5 us, 2 17.9, 4 19.8)
 constexpr uint32_t kSCol = 0, kOCol = 128, kPCol = 256, kQCol = 384, kQLoCol = 448;
 
