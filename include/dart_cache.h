@@ -27,7 +27,8 @@
  * outside [0, max_pages * page_size] counts as the nearer end, and no page
  * outside [0, num_pages) is accessed -- its use sets value 4 in *status (a
  * device int the caller zeroes; may be NULL) and leaves the results of that
- * sequence unspecified.
+ * sequence unspecified.  What a call reads must not change before the stream
+ * has reached its end.
  */
 #ifndef DART_CACHE_H
 #define DART_CACHE_H
@@ -63,8 +64,8 @@ typedef struct {
  * 2^-32 of a turn) in fp32.  bf16 pools hold the rounded values; e4m3 pools
  * scale = max |x| / 448 of the token's head (at least 2^-120; 1 if it is all
  * zero) and x / scale rounded to e4m3.  A NaN stays one in its place, an
- * infinity makes the whole head NaN when it is read.  Positions past max_pages * page_size are not written and set value 4
- * in *status.  No other slot changes; lens is not advanced.  Two tokens of
+ * infinity makes the whole head NaN when it is read.  Positions past
+ * max_pages * page_size are not written and set value 4 in *status.  No other slot changes; lens is not advanced.  Two tokens of
  * one call must not fall on one slot (two sequences that share a page and
  * both write in it). */
 int dart_cache_append(const dart_kv_cache *cache, int nseq, int max_pages, const int32_t *page_table,

@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
         a.plan->nodes[share] = use.nodes;
         if (share == 0) a.plan->count = shares.count;
     }
-    long long to_load = left;  // places not yet loaded
+    long long to_load = load.s < a.nseq ? left : 0;  // places not yet loaded
     int n_load = 0, n_use = 0;
     int failed = 0;
     volatile int* abort = &failed;
@@ -275,6 +275,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
         while (to_load > 0 && load.chunk >= load.ctx_chunks) {
             to_load -= load.cost - load.chunk;
             load.next_unit(a);
+            if (load.s >= a.nseq) to_load = 0;
         }
     };
     auto page_at = [&](int key) {
@@ -327,7 +328,8 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
     look_up();
     while (to_load > 0 && n_load < kStages) issue();
 
-    while (left > 0) {
+    // (s: in case the lengths change under the call, which leaves its results open)
+    while (left > 0 && use.s < a.nseq) {
         // ---- this warp's part of a unit: chunks [c0, c1)
         const int c0 = use.chunk, c1 = static_cast<int>(min(static_cast<long long>(use.chunks), c0 + left));
         const int s = use.s, head = use.head, len = use.len, nodes = use.nodes, ctx_chunks = use.ctx_chunks, chunks = use.chunks;

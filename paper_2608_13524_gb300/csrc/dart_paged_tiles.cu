@@ -496,7 +496,7 @@ struct Walk {
     long long left;  // places of the share from p on
     int s, head, qt, t0, t1, tiles, whole, tail, nodes;  // the part at hand: tiles [t0, t1) of a unit of `tiles`
     __device__ __forceinline__ bool next(const PagedArgs& a) {
-        while (left > 0) {
+        while (left > 0 && p.s < a.nseq) {  // (s: in case the lengths change under the call)
             tiles = p.tiles(a, p.qt);
             t0 = p.tile;
             t1 = static_cast<int>(min(static_cast<long long>(tiles), t0 + left));

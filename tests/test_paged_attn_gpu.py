@@ -162,6 +162,19 @@ def test_every_call_gives_the_same_bits(dart):
 
 
 @pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("B", [0, 3, 20, 130])
+def test_powers_of_two_pass_through(dart, B, fp8):
+    """Keys times 2^60, queries times 2^-60 and values times 2^50: every rounding
+    is relative to a power of two, so the bits are those of the plain call."""
+    x = sd.attn_data(2, B, [300, 900], 64, fp8, 8, 2, 7106)
+    plain = run(dart, x).clone()
+    k, v, ks, vs = x.pool
+    x.pool = [k, v, ks * 2.0 ** 60, vs * 2.0 ** 50] if fp8 else [k * 2.0 ** 60, v * 2.0 ** 50, None, None]
+    x.dev = tuple((t.float() * 2.0 ** e).to(torch.bfloat16) for t, e in zip(x.dev, (-60, 60, 50)))
+    assert torch.equal(run(dart, x).float(), plain.float() * 2.0 ** 50)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
 def test_many_calls_give_the_same_bits(dart, fp8):
     """Hundreds of calls of a shape whose shares switch from cache tiles to tree
     tiles early, where a slot freed too soon would be refilled under its reader."""
