@@ -188,6 +188,35 @@ def test_many_calls_give_the_same_bits(dart, fp8):
         assert torch.equal(out, first)
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("B", [2, 5])
+def test_more_sequences_than_lanes(dart, B, fp8):
+    """Ragged sequences (every seventh empty) beyond a warp's lanes, few rows and tiles."""
+    lens = [0 if i % 7 == 3 else 5 + (53 * i) % 300 for i in range(75)]
+    x = sd.attn_data(len(lens), B, lens, 16, fp8, 8, 2, 7107, fill=0.8)
+    rows = [(s, r) for s in (0, 3, 31, 32, 33, 63, 64, 74) for r in range(int(x.n_nodes[s]) + 1)]
+    check(x, run(dart, x), rows)
+
+
+def test_two_calls_at_once(dart):
+    """Two handles over one cache, on two streams with nothing between them: each
+    has its own workspace, so each gives what it gives alone."""
+    x = sd.attn_data(2, 90, [3000, 1500], 64, True, 8, 2, 7108)
+    y = sd.attn_data(2, 0, [3000, 1500], 64, True, 8, 2, 7108)
+    cache = dart.KVCache(*x.pool)
+    tree = dart.PagedTreeAttention(cache, 2, 90, x.max_pages, 8, rope_theta=THETA)
+    token = dart.PagedTreeAttention(cache, 2, 0, x.max_pages, 8, rope_theta=THETA)
+    calls = [lambda st=None: tree(*x.dev, x.table, x.d_lens, *x.tree, stream=st),
+             lambda st=None: token(*y.dev, x.table, x.d_lens, stream=st)]
+    alone = [c().clone() for c in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(20):
+        got = [c(st) for c, st in zip(calls, streams)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(alone, got))
+
+
 def test_split_does_not_show(dart):
     """One sequence alone (its keys shared by all SMs) and among 60 others
     (many sequences to an SM): the same result within two roundings."""
