@@ -65,9 +65,9 @@ typedef struct {
  * scale = max |x| / 448 of the token's head (at least 2^-120; 1 if it is all
  * zero) and x / scale rounded to e4m3.  A NaN stays one in its place, an
  * infinity makes the whole head NaN when it is read.  Positions past
- * max_pages * page_size are not written and set value 4 in *status.  No other slot changes; lens is not advanced.  Two tokens of
- * one call must not fall on one slot (two sequences that share a page and
- * both write in it). */
+ * max_pages * page_size are not written and set value 4 in *status.  No other
+ * slot changes; lens is not advanced.  Two tokens of one call must not fall on
+ * one slot (two sequences that share a page and both write in it). */
 int dart_cache_append(const dart_kv_cache *cache, int nseq, int max_pages, const int32_t *page_table,
                       const int32_t *lens, int R, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
                       const int32_t *rows, const int32_t *n_rows, float rope_theta, int *status, void *stream);
@@ -82,7 +82,8 @@ typedef struct {
 } dart_paged_attn_config;
 
 /* Device workspace (bytes) of dart_paged_attention; 0 on an invalid
- * configuration. */
+ * configuration.  For large trees over e4m3 pages it has room for the f16 form
+ * of max_pages pages a sequence, where that takes at most 4 GB. */
 size_t dart_paged_attention_workspace(const dart_paged_attn_config *cfg, const dart_kv_cache *cache);
 
 /* One tree-attention layer over the cache:

@@ -21,8 +21,8 @@
 // tensor-memory path would be 7/8 empty or more).
 //
 // Measured, 64 sequences of up to 8192 keys, 8 kv heads, one token each: bf16
-// pages 168 us, 6.5 TB/s, 96 % of the measured copy bandwidth; e4m3 pages 95 us,
-// 5.9 TB/s, 87 %, where the conversions (64 codes a thread and chunk) come
+// pages 170 us, 6.4 TB/s, 94 % of the measured copy bandwidth; e4m3 pages 94 us,
+// 6.0 TB/s, 88 %, where the conversions (64 codes a thread and chunk) come
 // second; a call of a few keys takes 12 us, a chain of two launches and six or
 // seven dependent loads.  With rows along the 16 and 8 warps e4m3 took 116 us.
 #include <cuda.h>
@@ -73,13 +73,14 @@ __host__ __device__ constexpr int rows_warps(int n) { return n == 1 ? 12 : 8; }
 
 // Chunk sizes, and what a unit costs beside its chunks (queries, tree rows,
 // the result), in chunks: its list is that much longer, so that warps with
-// many short units get fewer of them (64 sequences of 8192 bf16 keys 171 us at 6,
-// 168 at 3 and at 9; 64 trees of 3 nodes over 4096 105 at 3, 100 at 6, 98 at 9;
-// e4m3 94, 95, 96 and 71, 65, 65 us at 2, 4, 6).
+// many short units get fewer of them.  kTokenCost: without a tree (256 sequences of
+// up to 1024 e4m3 keys 56.5 us at 1, 54 at 2, 55.5 at 3, 56.5 at 6; bf16 97 at 2, 95 at
+// 3 to 7, 97 at 9).  kUnitCost: 64 trees of 3 nodes over 4096 keys, bf16 105 us at 3,
+// 100 at 6, 98 at 9; e4m3 71, 65, 65 at 2, 4, 6.
 template <bool kFp8>
 struct Chunk {
     static constexpr int kKeys = kFp8 ? 32 : 16;
-    static constexpr int kUnitCost = kFp8 ? 6 : 9;
+    static constexpr int kUnitCost = kFp8 ? 6 : 9, kTokenCost = kFp8 ? 2 : 5;
 };
 
 // A place in the list of chunks: sequence, kv head, chunk of the unit.
@@ -93,7 +94,7 @@ struct Place {
         nodes = seq_nodes(a, s);
         ctx_chunks = (len + kKeys - 1) / kKeys;
         chunks = ctx_chunks + (nodes + 1 + 15) / 16;  // (tree rows: 16 at a time)
-        cost = chunks + Chunk<kFp8>::kUnitCost;
+        cost = chunks + (a.B == 0 ? Chunk<kFp8>::kTokenCost : Chunk<kFp8>::kUnitCost);
     }
     __device__ __forceinline__ void next_unit(const PagedArgs& a) {
         chunk = 0;
@@ -213,7 +214,8 @@ struct Geo {
     static constexpr int kStages = kN == 1 ? 2 : 3;
     static constexpr int kRing = kWarps * kStages * 2 * kTile;           // 192 KB
     static constexpr int kScales = kFp8 ? kWarps * kStages * 2 * kKeys * 4 : 0;
-    static constexpr int kSmem = kRing + kScales + kWarps * kStages * 8;
+    static constexpr int kTurns = kWarps * (kHeadDim / 2) * 8;            // a position's angles, of each warp
+    static constexpr int kSmem = kRing + kScales + kTurns + kWarps * kStages * 8;
 };
 
 // 16-byte piece (8 bf16) of a row of the head that step pair i of thread t
@@ -235,7 +237,8 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
     pdl_trigger();
     uint8_t* ring = smem + warp * kStages * 2 * kTile;
     float* scales = reinterpret_cast<float*>(smem + G_::kRing) + warp * kStages * 2 * kKeys;  // [stage][K, V][key]
-    uint64_t* bar = reinterpret_cast<uint64_t*>(smem + G_::kRing + G_::kScales) + warp * kStages;
+    float2* turns = reinterpret_cast<float2*>(smem + G_::kRing + G_::kScales) + warp * (kHeadDim / 2);
+    uint64_t* bar = reinterpret_cast<uint64_t*>(smem + G_::kRing + G_::kScales + G_::kTurns) + warp * kStages;
     if (lane == 0) {
         for (int i = 0; i < kStages; i++) mbar_init(bar + i, 1);
         fence_mbar_init();
@@ -338,6 +341,35 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
         use.next_unit(a);
         if (c0 >= c1) continue;  // (the part of a unit's length that stands for its other costs)
 
+        // Single tokens all have the position `len`: its angles once, two a lane, instead of
+        // the 16 of every thread's pieces, for the queries and again for the key (1024
+        // sequences of up to 512 e4m3 keys 211 us with those, 115 so).
+        if (a.B == 0) {
+            __syncwarp();
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                float sn, cs;
+                rope_sincos(a.turns.f[32 * h + lane], len, &sn, &cs);
+                turns[32 * h + lane] = make_float2(cs, sn);
+            }
+            __syncwarp();
+        }
+        // cosines and sines of elements d0 .. d0 + 7 at a position
+        auto angles = [&](int d0, int pos, float (&cs)[8], float (&sn)[8]) {
+            if (a.B == 0) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float4 x = *reinterpret_cast<const float4*>(turns + d0 + e);
+                    cs[e] = x.x;
+                    sn[e] = x.y;
+                    cs[e + 1] = x.z;
+                    sn[e + 1] = x.w;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e++) rope_sincos(a.turns.f[d0 + e], pos, &sn[e], &cs[e]);
+            }
+        };
         // the queries of rows 8 n + g, rotated, as operands: step pair i covers the 8
         // elements of piece k_piece(i, t) in steps 2 i, 2 i + 1
         uint32_t q[kN][8][2], lo[kN][8][2];
@@ -358,14 +390,14 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                     const int d0 = 8 * k_piece<kFp8>(i, t);
                     const uint4 u = ld_plain(reinterpret_cast<const uint4*>(src + d0)), w = ld_plain(reinterpret_cast<const uint4*>(src + d0 + 64));
                     const uint32_t uw[4] = {u.x, u.y, u.z, u.w}, ww[4] = {w.x, w.y, w.z, w.w};
+                    float cs[8], sn[8];
+                    angles(d0, pos, cs, sn);
 #pragma unroll
                     for (int e = 0; e < 8; e++) {
-                        float sn, cs;
-                        rope_sincos(a.turns.f[d0 + e], pos, &sn, &cs);
                         const float x1 = e & 1 ? bf16_hi(uw[e >> 1]) : bf16_lo(uw[e >> 1]);
                         const float x2 = e & 1 ? bf16_hi(ww[e >> 1]) : bf16_lo(ww[e >> 1]);
-                        x[i][e] = x1 * cs - x2 * sn;
-                        x[i + 2][e] = x2 * cs + x1 * sn;
+                        x[i][e] = x1 * cs[e] - x2 * sn[e];
+                        x[i + 2][e] = x2 * cs[e] + x1 * sn[e];
                     }
                 }
             }
@@ -698,11 +730,11 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                         const uint4 x = ld_plain(reinterpret_cast<const uint4*>(k + d0));
                         const uint4 y = ld_plain(reinterpret_cast<const uint4*>(k + d0 + 64));
                         const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+                        float cs[8], sn[8];
+                        angles(d0, pos, cs, sn);
 #pragma unroll
                         for (int e = 0; e < 4; e++) {
-                            float s0, k0, s1, k1;
-                            rope_sincos(a.turns.f[d0 + 2 * e], pos, &s0, &k0);
-                            rope_sincos(a.turns.f[d0 + 2 * e + 1], pos, &s1, &k1);
+                            const float k0 = cs[2 * e], s0 = sn[2 * e], k1 = cs[2 * e + 1], s1 = sn[2 * e + 1];
                             const float x0 = bf16_lo(xw[e]), x1 = bf16_hi(xw[e]), y0 = bf16_lo(yw[e]), y1 = bf16_hi(yw[e]);
                             w[qq][i][e] = pack_bf16x2(x0 * k0 - y0 * s0, x1 * k1 - y1 * s1);
                             w[qq][i + 2][e] = pack_bf16x2(y0 * k0 + x0 * s0, y1 * k1 + x1 * s1);
