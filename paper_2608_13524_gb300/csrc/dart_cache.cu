@@ -36,7 +36,7 @@ constexpr int kAppendThreads = 256;
 constexpr int kGroup = 8;  // threads of a token's head: 8 elements of each half of a row are 16 bytes
 // Four heads a group (angles once for four) where that still makes this many
 // groups, else one: a few tokens are a matter of latency (eight prompts of up to
-// 4096 tokens to e4m3 pages 34 us with four and 45 with one; below, no difference).
+// 4096 tokens to e4m3 pages 35 us with four, 45 with one; below, no difference).
 constexpr long long kManyGroups = 9728;  // 152 SMs x 64 groups = 512 threads each
 constexpr float kMinScale = 7.52316384526264005e-37f;  // 2^-120: its reciprocal is finite
 
@@ -92,8 +92,12 @@ __device__ __forceinline__ void store_e4m3(uint8_t* pool, float* scales, long lo
     for (int e = 0; e < 8; e++) amax = fmaxf(amax, fmaxf(fabsf(x.lo[e]), fabsf(x.hi[e])));
 #pragma unroll
     for (int o = kGroup / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(kFull, amax, o));
-    const float scale = amax > 0.0f ? fmaxf(amax / 448.0f, kMinScale) : 1.0f;
-    const float inv = 1.0f / scale;
+    // codes by 448 / amax and not the rounded scale's reciprocal: quotients that lie
+    // halfway between two codes (values of few bits often do) stay there.  (The scale
+    // itself, two roundings from amax / 448, moves what is read by 2^-23 of it.)
+    const bool plain = amax >= 448.0f * kMinScale;
+    const float scale = plain ? amax * (1.0f / 448.0f) : amax > 0.0f ? kMinScale : 1.0f;
+    const float inv = plain ? 448.0f / amax : amax > 0.0f ? 1.0f / kMinScale : 1.0f;
     if (!use) return;
     uint8_t* d = pool + row * kHeadDim + 8 * j;
     *reinterpret_cast<uint2*>(d) = to_e4m3(x.lo, inv);
