@@ -39,6 +39,7 @@ constexpr int kGroup = 8;  // threads of a token's head: 8 elements of each half
 // 4096 tokens to e4m3 pages 35 us with four, 45 with one; below, no difference).
 constexpr long long kManyGroups = 9728;  // 152 SMs x 64 groups = 512 threads each
 constexpr float kMinScale = 7.52316384526264005e-37f;  // 2^-120: its reciprocal is finite
+constexpr float kSmallScale = 8.27180612553027675e-25f, kSmallUp = 1.152921504606846976e18f;  // 2^-80, 2^60
 
 struct AppendArgs {
     int nseq, max_pages, R, Hkv, chunks, page_log2, num_pages;
@@ -66,12 +67,20 @@ __device__ __forceinline__ void unpack(const uint4& a, const uint4& b, Row& x) {
     }
 }
 
-__device__ __forceinline__ uint2 to_e4m3(const float (&x)[8], float inv) {
+// x / scale, each quotient rounded once to fp32 (two at a time): the product with the
+// rounded reciprocal is at most a unit off, its remainder is exact in one fma, and a
+// second fma corrects it (Markstein's division).  Infinities and NaN give NaN.
+__device__ __forceinline__ float2 quotients(float a, float b, float scale, float inv) {
+    const float2 q = fma2(make_float2(a, b), make_float2(inv, inv), make_float2(-0.0f, -0.0f));
+    const float2 r = fma2(q, make_float2(scale, scale), make_float2(-a, -b));
+    return fma2(r, make_float2(-inv, -inv), q);  // (in this form -0 stays -0)
+}
+__device__ __forceinline__ uint2 to_e4m3(const float (&x)[8], float scale, float inv) {
     uint32_t r[2];
 #pragma unroll
     for (int h = 0; h < 2; h++) {
-        const uint32_t a = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * h] * inv, x[4 * h + 1] * inv), __NV_SATFINITE, __NV_E4M3);
-        const uint32_t b = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * h + 2] * inv, x[4 * h + 3] * inv), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t a = __nv_cvt_float2_to_fp8x2(quotients(x[4 * h], x[4 * h + 1], scale, inv), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t b = __nv_cvt_float2_to_fp8x2(quotients(x[4 * h + 2], x[4 * h + 3], scale, inv), __NV_SATFINITE, __NV_E4M3);
         r[h] = a | (b << 16);
     }
     return make_uint2(r[0], r[1]);
@@ -86,22 +95,27 @@ __device__ __forceinline__ void store_bf16(uint8_t* pool, long long row, int j, 
 }
 
 // One scale for the 128 values of the group (every thread of the warp calls it).
-__device__ __forceinline__ void store_e4m3(uint8_t* pool, float* scales, long long row, int j, const Row& x, bool use) {
+__device__ __forceinline__ void store_e4m3(uint8_t* pool, float* scales, long long row, int j, Row x, bool use) {
     float amax = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; e++) amax = fmaxf(amax, fmaxf(fabsf(x.lo[e]), fabsf(x.hi[e])));
 #pragma unroll
     for (int o = kGroup / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(kFull, amax, o));
-    // codes by 448 / amax and not the rounded scale's reciprocal: quotients that lie
-    // halfway between two codes (values of few bits often do) stay there.  (The scale
-    // itself, two roundings from amax / 448, moves what is read by 2^-23 of it.)
-    const bool plain = amax >= 448.0f * kMinScale;
-    const float scale = plain ? amax * (1.0f / 448.0f) : amax > 0.0f ? kMinScale : 1.0f;
-    const float inv = plain ? 448.0f / amax : amax > 0.0f ? 1.0f / kMinScale : 1.0f;
+    const float scale = amax > 0.0f ? fmaxf(__fdiv_rn(amax, 448.0f), kMinScale) : 1.0f;
     if (!use) return;
+    float by = scale;
+    if (scale < kSmallScale) {  // (rare) a remainder would lie below the floats: both sides times 2^60
+        by *= kSmallUp;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            x.lo[e] *= kSmallUp;
+            x.hi[e] *= kSmallUp;
+        }
+    }
+    const float inv = __frcp_rn(by);
     uint8_t* d = pool + row * kHeadDim + 8 * j;
-    *reinterpret_cast<uint2*>(d) = to_e4m3(x.lo, inv);
-    *reinterpret_cast<uint2*>(d + 64) = to_e4m3(x.hi, inv);
+    *reinterpret_cast<uint2*>(d) = to_e4m3(x.lo, by, inv);
+    *reinterpret_cast<uint2*>(d + 64) = to_e4m3(x.hi, by, inv);
     if (j == 0) scales[row] = scale;
 }
 
