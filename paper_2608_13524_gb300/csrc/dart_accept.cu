@@ -78,8 +78,8 @@ __device__ __forceinline__ float load_logit<__nv_bfloat16>(const __nv_bfloat16* 
     return clean(__bfloat162float(ld_plain(row + i)));
 }
 
-// The logits of one 16-byte vector: cleaned words, their values, and the
-// values' maximum (bf16: two at a time).
+// The logits of one 16-byte vector: words without NaN, their values as load_logit
+// gives them, and the values' maximum (bf16: two at a time).
 template <typename T>
 struct Vec;
 template <>
@@ -102,10 +102,10 @@ struct Vec<float> {
 template <>
 struct Vec<__nv_bfloat16> {
     static constexpr int n = 8;
+    // (+inf stays until a value is fp32: the largest float is no bf16)
     static __device__ __forceinline__ uint32_t clean2(uint32_t w) {
-        const __nv_bfloat162 low = __halves2bfloat162(__ushort_as_bfloat16(0xFF80), __ushort_as_bfloat16(0xFF80));   // -inf
-        const __nv_bfloat162 high = __halves2bfloat162(__ushort_as_bfloat16(0x7F7F), __ushort_as_bfloat16(0x7F7F));  // largest
-        const __nv_bfloat162 r = __hmin2(__hmax2(*reinterpret_cast<const __nv_bfloat162*>(&w), low), high);
+        const __nv_bfloat162 low = __halves2bfloat162(__ushort_as_bfloat16(0xFF80), __ushort_as_bfloat16(0xFF80));  // -inf
+        const __nv_bfloat162 r = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&w), low);
         return *reinterpret_cast<const uint32_t*>(&r);
     }
     static __device__ __forceinline__ uint4 clean4(const uint4& w) {
@@ -115,14 +115,14 @@ struct Vec<__nv_bfloat16> {
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            z[2 * e] = __uint_as_float(u[e] << 16);
-            z[2 * e + 1] = __uint_as_float(u[e] & 0xFFFF0000u);
+            z[2 * e] = fminf(__uint_as_float(u[e] << 16), FLT_MAX);
+            z[2 * e + 1] = fminf(__uint_as_float(u[e] & 0xFFFF0000u), FLT_MAX);
         }
     }
     static __device__ __forceinline__ float top(const uint4& w) {
         auto two = [](uint32_t x) { return *reinterpret_cast<const __nv_bfloat162*>(&x); };
         const __nv_bfloat162 r = __hmax2(__hmax2(two(w.x), two(w.y)), __hmax2(two(w.z), two(w.w)));
-        return fmaxf(__low2float(r), __high2float(r));
+        return fminf(fmaxf(__low2float(r), __high2float(r)), FLT_MAX);
     }
 };
 

@@ -1,0 +1,59 @@
+"""Verification of the tree at the edges of its contract, against the fp64
+oracle: infinite logits in both types, children without a share of their own,
+masked tokens, rows with many children, and rows longer than a thread's
+registers hold.  Tolerance of log p: see test_verify_tree_gpu.py."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import serve
+from test_verify_tree_gpu import LOGP, check, dart, data, run, up  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+F32_MAX = 3.4028235e38
+TYPES = [torch.float32, torch.bfloat16]
+
+
+def device_logits(z, dtype, ld=None):
+    """z [nseq][R][V] as dtype on the GPU (its values have to be of that type),
+    rows `ld` apart, and what the oracle takes."""
+    t = torch.from_numpy(z).to(dtype)
+    d = t.cuda()
+    if ld:
+        wide = torch.full((*z.shape[:2], ld), 1e30, dtype=dtype, device="cuda")
+        wide[..., :z.shape[2]] = d
+        d = wide[..., :z.shape[2]]
+    return t.float().numpy(), d
+
+
+@pytest.mark.parametrize("ld", [None, 301, 305])
+@pytest.mark.parametrize("T", [0.0, 1.0, 0.7])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_infinite_logits(dart, dtype, T, ld):  # noqa: F811
+    """+inf counts as the largest float wherever it stands: on a child, beside
+    the children, on both, among the elements that no 16-byte vector holds."""
+    V, B, inf = 300, 4, np.inf
+    g = np.random.default_rng(21)
+    z = g.standard_normal((12, B + 1, V)).astype(np.float32)
+    tokens = np.tile(np.array([5, 9, 1, 2], np.int32), (12, 1))
+    parents = np.tile(np.array([-1, -1, 0, 1], np.int32), (12, 1))
+    u = np.full((12, B + 1), 0.25, np.float32)
+    z[0, 0, 9] = inf                                       # a child
+    z[1, 0, 77] = inf                                      # no child
+    z[2, 0, [9, 77]] = inf                                 # both: half of the mass each
+    z[3, 0, [9, 77]] = inf; u[3] = 0.75                    # noqa: E702
+    z[4, 0, [5, 9]] = inf                                  # two children
+    z[5, 0, [5, 9]] = inf; u[5] = 0.75                     # noqa: E702
+    z[6, 0, [77, 299]] = inf                               # the last element of the row
+    z[7, 0, [0, 77]] = inf                                 # the first
+    z[8, 0, 20] = float(torch.finfo(dtype).max); z[8, 0, 77] = inf   # noqa: E702  (fp32: equal, so a tie)
+    z[9, 0, 9] = inf; z[9, 2] = z[9, 0]; z[9, 4, 298] = inf          # noqa: E702  further down a branch
+    z[10, 0, [1, 296, 299]] = inf; u[10] = 0.9             # noqa: E702
+    z[11, 0, :] = inf; u[11] = 0.999                       # noqa: E702  everywhere
+    zf, d = device_logits(torch.from_numpy(z).to(dtype).float().numpy(), dtype, ld)
+    noise = np.maximum(g.exponential(size=(12, V)), 1e-9).astype(np.float32)
+    n = np.full(12, B, np.int32)
+    out = run(dart, d, tokens, parents, n, T, u, noise)
+    torch.cuda.synchronize()
+    check(out, serve.verify(zf, tokens, parents, n, T, u, noise), B + 1)
