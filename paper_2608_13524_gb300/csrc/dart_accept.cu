@@ -387,7 +387,9 @@ __global__ void __launch_bounds__(kVerifyThreads, 1) verify_tree_kernel(const Ve
                     if (lane >= o) x += y;
                 }
                 x += run;
-                const unsigned hit = __ballot_sync(kFull, k < nk && goal < x);
+                // (e: the lanes' sums are rounded each in its own order, so one without a share
+                // of its own may lie above its neighbour's)
+                const unsigned hit = __ballot_sync(kFull, e > 0.0f && goal < x);
                 if (hit) next = k0 + __ffs(hit) - 1;
                 run = __shfl_sync(kFull, x, 31);
             } else {

@@ -57,3 +57,22 @@ def test_infinite_logits(dart, dtype, T, ld):  # noqa: F811
     out = run(dart, d, tokens, parents, n, T, u, noise)
     torch.cuda.synchronize()
     check(out, serve.verify(zf, tokens, parents, n, T, u, noise), B + 1)
+
+
+def test_a_child_without_a_share_is_not_kept(dart):  # noqa: F811
+    """Four children before one whose token an earlier sibling has and one with
+    p = 0: whatever u is, on the border between their neighbours too, neither
+    is kept."""
+    factors, steps = np.linspace(1.02, 1.98, 16), np.arange(-64, 64)
+    nseq, V, B = len(factors) * len(steps), 16, 5
+    z = np.full((nseq, B + 1, V), -300.0, np.float32)
+    z[:, :, 0] = z[:, :, 15] = 0.0
+    z[:, :, [1, 2]] = (np.log(np.repeat(factors, len(steps))) - 24 * np.log(2)).astype(np.float32)[:, None, None]
+    tokens = np.tile(np.array([0, 1, 2, 1, 3], np.int32), (nseq, 1))
+    parents = np.full((nseq, B), -1, np.int32)
+    u = np.zeros((nseq, B + 1), np.float32)
+    u[:, 0] = np.tile(0.5 + steps * 2.0 ** -24, len(factors))
+    out = run(dart, up(z), tokens, parents, np.full(nseq, B, np.int32), 1.0, u, np.ones((nseq, V), np.float32))
+    kept = out["rows"][:, 1].cpu().numpy()
+    assert set(kept.tolist()) <= {-1, 1, 2, 3}, np.unique(kept, return_counts=True)
+    assert (kept == -1).any() and (kept == 1).any()
