@@ -123,8 +123,9 @@ int dart_ancestor_mask(const int32_t *parents, const int32_t *n_nodes, int nseq,
  *     is kept and its row comes next.  If u lies beyond the children, the walk
  *     stops with the token of the largest p / e among the tokens of no child
  *     (ties: the lowest), e = noise[s][token] an Exp(1) number: a draw from
- *     what the children leave.  (If they leave no token of finite logit, the
- *     last child with p > 0 is kept instead.)
+ *     what the children leave.  A token with p below 2^-126 of the row's
+ *     largest (a mask of a low but finite logit, say) is not drawn; if the
+ *     children leave no other, the last child with p > 0 is kept instead.
  *   T = 0: the token of the largest logit (ties: the lowest) is next; the
  *     child that has it is kept, else the walk stops.
  * A child whose token an earlier sibling has, whose token is outside [0, V),

@@ -82,6 +82,7 @@ def verify(logits, tokens, parents, n_nodes, T, u=None, noise=None):
                         break
                 rest = z.copy()
                 rest[list(seen)] = -np.inf
+                rest[e < 2.0 ** -126] = -np.inf
                 if keep is None and rest.max() == -np.inf:
                     keep = next((i for i in reversed(kids) if e[int(tokens[s, i])] > 0), None)
                 if keep is None and rest.max() > -np.inf:

@@ -40,6 +40,7 @@ constexpr int kMaxNodes = 1024;
 constexpr int kNodesPerThread = kMaxNodes / kVerifyThreads;
 constexpr int kHeld = 4;            // vectors of a row that a thread holds in registers
 constexpr int kFetched = 4;         // children whose rows are fetched ahead
+constexpr float kLeastLog2 = -126.0f;  // of exp((z - m) / T): below it a token is as good as masked
 constexpr int kNoise = 20480;       // noise in shared memory (80 KB): the shares of V <= 163000
 
 struct VerifyArgs {
@@ -410,7 +411,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 1) verify_tree_kernel(const Ve
             const uint32_t child = sm.child[tid];
             RowStat w{-INFINITY, 0.0f, 0x7FFFFFFF, 0};
             auto offer = [&](float z, float e, int t) {  // (tokens of a thread are not in ascending order only at the odd ones)
-                const float x = (z - m) * c - fast_log2(e);
+                const float lp = (z - m) * c, x = lp >= kLeastLog2 ? lp - fast_log2(e) : -INFINITY;
                 if (x > w.m || (x == w.m && t < w.arg)) {
                     w.m = x;
                     w.arg = t;
@@ -450,7 +451,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 1) verify_tree_kernel(const Ve
             if (w.m != -INFINITY)
                 tok = w.arg;
             else
-                next = last;  // nothing is left beside the children
+                next = last;  // nothing with a probability is left beside the children
             if (next >= 0) {
                 sm.child[tid] = 0;
                 __syncthreads();

@@ -76,3 +76,26 @@ def test_a_child_without_a_share_is_not_kept(dart):  # noqa: F811
     kept = out["rows"][:, 1].cpu().numpy()
     assert set(kept.tolist()) <= {-1, 1, 2, 3}, np.unique(kept, return_counts=True)
     assert (kept == -1).any() and (kept == 1).any()
+
+
+@pytest.mark.parametrize("low", [-F32_MAX, -1e30, -300.0], ids=str)
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_a_masked_token_is_never_drawn(dart, dtype, low):  # noqa: F811
+    """The children hold all of the mass, the other tokens are masked by a low
+    logit instead of -inf, and u is the last number below 1: rounding may put it
+    past the children, but a token of p = 0 does not follow."""
+    nseq, V, B = 512, 600, 20
+    g = np.random.default_rng(22)
+    low = float(torch.tensor(low).to(dtype)) if low > -1e38 else float(torch.finfo(dtype).min)
+    z = np.full((nseq, B + 1, V), low, np.float32)
+    z[:, :, :B] = g.standard_normal((nseq, B + 1, B)) * 3
+    zf, d = device_logits(torch.from_numpy(z).to(dtype).float().numpy(), dtype)
+    tokens, parents = np.tile(np.arange(B, dtype=np.int32), (nseq, 1)), np.full((nseq, B), -1, np.int32)
+    u = np.full((nseq, B + 1), 1 - 2.0 ** -24, np.float32)
+    noise = np.maximum(g.exponential(size=(nseq, V)), 1e-9).astype(np.float32)
+    out = run(dart, d, tokens, parents, np.full(nseq, B, np.int32), 1.0, u, noise)
+    first = out["tokens"][:, 0].cpu().numpy()
+    assert ((first >= 0) & (first < B)).all(), np.unique(first[first >= B])
+    want = zf[np.arange(nseq), 0, first]
+    lp = want - np.log(np.exp(zf[:, 0, :B].astype(np.float64)).sum(1))
+    assert np.abs(out["logp"][:, 0].cpu().numpy() - lp).max() <= LOGP
