@@ -51,6 +51,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cstdint>
 #include <cstring>
 
@@ -926,7 +927,8 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 if (ok) {
                     if (kF16) {  // (before s_empty: after S(n + 1) the place may be written again)
                         const float2 ref = kConv ? tile_ref[n % G_::kRing] : ref_ahead;
-                        rt *= ref.x;
+                        // not 0, where both factors are tiny (rows of zeros): hidden keys are -inf by now
+                        rt = fmaxf(rt * ref.x, FLT_MIN);
                         vtile = ref.y;
                         if (kSource == kWidened && t + 1 < t1) ref_ahead = __ldcg(refs + t + 1);
                     }
