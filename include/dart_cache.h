@@ -90,8 +90,9 @@ size_t dart_paged_attention_workspace(const dart_paged_attn_config *cfg, const d
  *   q    = RoPE(Q[s][r][h], position of r)
  *   keys = cache tokens 0 .. lens[s] - 1 of kv head g = h / (Hq / Hkv),
  *          RoPE(k[s][j][g], position of j) for row j = 0 and, where bit j - 1
- *          of mask[s][r - 1] is set, for row j (bits of rows > n_nodes[s] are
- *          ignored); row 0 sees itself and the cache alone
+ *          of mask[s][r - 1] is set, for row j <= r (ancestors come before
+ *          their descendants: bits of rows > r are ignored, in every row);
+ *          row 0 sees itself and the cache alone
  *   out[s][r][h] = softmax(scale * q . keys) . values;  rows > n_nodes[s]: 0
  * Layouts (bf16 unless stated): q [nseq * R] rows of Hq * dh, k and v
  * [nseq * R] rows of Hkv * dh, each with a stride between rows (elements, a

@@ -776,7 +776,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                         const int j = key0 + slot_row(qq, g), b = (8 * n + 2 * t + e) >> a.g_log2;
                         bool see = j <= nodes && b <= nodes;
                         if (see && j > 0)
-                            see = b > 0 && ((ld_plain(a.mask + (static_cast<long long>(s) * a.B + b - 1) * a.mw + ((j - 1) >> 6)) >> ((j - 1) & 63)) & 1ull);
+                            see = j <= b && ((ld_plain(a.mask + (static_cast<long long>(s) * a.B + b - 1) * a.mw + ((j - 1) >> 6)) >> ((j - 1) & 63)) & 1ull);
                         sc[0][n][2 * qq + e] = see ? sc[0][n][2 * qq + e] * rs[n][e] : -INFINITY;
                     }
             soften(sc);

@@ -909,9 +909,9 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 if (t >= whole) {
                     const int o = (t - whole) * kKeys + cb - tail - 1;  // tree node of the first key (negative: cache, row 0)
                     vis = 0ull;
-                    if (b > 0 && row_ok && o < nodes) {
+                    if (b > 0 && row_ok && o < b) {  // (bits beyond the row's own are not used)
                         vis = mask_bits(a.mask + (static_cast<long long>(s) * a.B + b - 1) * a.mw, a.mw, o);
-                        if (nodes - o < 64) vis &= (1ull << (nodes - o)) - 1ull;
+                        if (b - o < 64) vis &= (1ull << (b - o)) - 1ull;
                     }
                     if (o < 0) vis |= o <= -64 ? ~0ull : (1ull << -o) - 1ull;
                     all_seen = __all_sync(kFull, vis == ~0ull);

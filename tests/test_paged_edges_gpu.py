@@ -1,5 +1,5 @@
 """Paged tree attention at the edges of its contract, against the fp64 oracle:
-zero queries and keys, products below the floats.
+zero queries and keys, products below the floats, mask bits of later rows.
 Tolerances: see test_paged_attn_gpu.py."""
 import numpy as np
 import pytest
@@ -71,3 +71,22 @@ def test_a_new_pool_without_scales(dart, fp8):  # noqa: F811
         x.ctx = [(np.zeros_like(k), np.zeros_like(v)) for k, v in x.ctx]
         scaled(x, 0.0, 0.0)
         check(x, run(dart, x, cache))
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_mask_bits_of_later_rows_are_not_used(dart, shape, fp8):  # noqa: F811
+    """Ancestors come before their descendants; bits beyond a row's own are
+    garbage in every kernel, in the same 128 keys as the row's own or not."""
+    B, Hq, Hkv = shape
+    x = sd.attn_data(2, B, [100, 0], 16, fp8, Hq, Hkv, 7204, fill=0.9)
+    plain = run(dart, x).clone()
+    depths, mask, n = x.tree
+    words = mask.cpu().numpy().view(np.uint64).copy()
+    bits = np.unpackbits(words.view(np.uint8).reshape(2, B, -1), axis=-1, bitorder="little")
+    for i in range(B):
+        bits[:, i, i + 1:] = 1
+    later = np.packbits(bits, axis=-1, bitorder="little").view(np.int64)
+    x.tree = (depths, torch.from_numpy(np.ascontiguousarray(later.reshape(mask.shape))).cuda(), n)
+    assert torch.equal(run(dart, x), plain)
+    check(x, plain)
