@@ -40,6 +40,7 @@
 #include "../../include/dart_cache.h"
 #include "dart_kernels.h"
 #include "dart_paged.cuh"
+#include "dart_ring.h"
 
 namespace dart {
 
@@ -267,7 +268,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
         if (share == 0) a.plan->count = shares.count;
     }
     long long to_load = load.s < a.nseq ? left : 0;  // places not yet loaded
-    int n_load = 0, n_use = 0;
+    StageRing<kStages> fills;
     int failed = 0;
     volatile int* abort = &failed;
     const uint64_t policy = l2_policy_evict_first();  // (every key is read once)
@@ -293,7 +294,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
     };
     auto issue = [&]() {  // loads the chunk at `load`
         if (lane == 0) {
-            const int st = n_load % kStages;
+            const int st = fills.stage(fills.filled);
             uint8_t* k = ring + st * 2 * kTile;
             uint8_t* v = k + kTile;
             float* sc = scales + st * 2 * kKeys;
@@ -323,13 +324,13 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                 }
             }
         }
-        n_load++;
+        fills.filled++;
         to_load--;
         load.chunk++;
         look_up();
     };
     look_up();
-    while (to_load > 0 && n_load < kStages) issue();
+    while (to_load > 0 && fills.room()) issue();
 
     // (s: in case the lengths change under the call, which leaves its results open)
     while (left > 0 && use.s < a.nseq) {
@@ -540,12 +541,12 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
         // ---- the cache
         const int c_ctx = min(c1, ctx_chunks);
         for (int c = c0; c < c_ctx; c++) {
-            const int st = n_use % kStages, key0 = c * kKeys;
+            const int st = fills.stage(fills.used), key0 = c * kKeys;
             uint8_t* kt = ring + st * 2 * kTile;
             uint8_t* vt = kt + kTile;
             const float* sck = scales + st * 2 * kKeys;
             if (!failed) {
-                const bool got = mbar_wait_inline(bar + st, static_cast<uint32_t>(n_use / kStages) & 1u, abort);
+                const bool got = mbar_wait_inline(bar + st, fills.parity(fills.used), abort);
                 if (!__all_sync(kFull, got)) {
                     failed = 1;
                     if (a.status && lane == 0) atomicOr(a.status, kDevTimeout);
@@ -706,7 +707,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                 if (there < kKeys) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             }
             __syncwarp();  // every lane has read the stage
-            n_use++;
+            fills.passed(failed);
             if (!failed && to_load > 0) issue();
         }
 
@@ -829,8 +830,8 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
     }
     if (failed) {  // copies in flight land before the CTA ends
         const unsigned long long t0 = globaltimer_ns();
-        for (int i = n_use; i < n_load; i++)
-            while (!mbar_try_wait(bar + i % kStages, static_cast<uint32_t>(i / kStages) & 1u))
+        for (int i = fills.used; i < fills.filled; i++)
+            while (!mbar_try_wait(bar + fills.stage(i), fills.parity(i)))
                 if (globaltimer_ns() - t0 > kWaitLimitNs) break;
     }
 }
