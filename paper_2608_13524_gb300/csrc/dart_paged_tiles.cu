@@ -720,7 +720,7 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                            : 0;
             };
             int n = 0;       // bf16: tiles so far; e4m3: whole cache tiles so far
-            bool have = w.next(a), ok = true, waited = kSource == kWidened;
+            bool have = w.next(a), ok = true, waited = kSource == kWidened, k_ahead = false;  // (k_ahead: tile n's K is on its way, its V is not)
             if (waited) pdl_wait();
             int t = w.t0, page = have ? page_at(t) : 0;
             while (have && ok) {
@@ -754,6 +754,7 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                     const CUtensorMap* tm = cache_tile ? (kv ? &tmV : &tmK) : (kv ? &tmSv : &tmSk);
                     ok = warp_wait<kWaitPolls>(empty, (static_cast<uint32_t>(n / stages) & 1u) ^ 1u, abort);
                     if (!ok) break;
+                    k_ahead = kv == 0;
                     if (lane == 0)
                         mbar_arrive_expect_tx(full, kConv ? kHalf + kKeys * 4 : kTile);
                     __syncwarp();
@@ -773,15 +774,14 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 if (ok) n++;
             }
             if (!ok && lane == 0) attn_timeout(a.status, abort);
-            if (*abort) {
-                // copies still in flight must land before the CTA exits
-                for (int kv = 0; kv < 2; kv++) {
-                    const int stages = kConv ? (kv ? G_::kRawV : G_::kRawK) : kStages;
-                    uint64_t* full = kConv ? (kv ? rv_full : rk_full) : (kv ? v_full : k_full);
-                    // (the tile at which a wait failed may have its K under way)
-                    for (int i = max(n - stages, 0); i < n + (kv == 0 && !ok ? 1 : 0); i++)
-                        if (lane == 0) attn_drain(&full[i % stages], static_cast<uint32_t>(i / stages) & 1u);
-                }
+            // The last copies land before the CTA ends, whoever gives up a wait, and when (in a
+            // good run their readers have waited for them, and this costs nothing).
+            for (int kv = 0; kv < 2; kv++) {
+                const int stages = kConv ? (kv ? G_::kRawV : G_::kRawK) : kStages;
+                uint64_t* full = kConv ? (kv ? rv_full : rk_full) : (kv ? v_full : k_full);
+                const int fills = n + (kv == 0 && k_ahead ? 1 : 0);
+                for (int i = max(fills - stages, 0); i < fills; i++)
+                    if (lane == 0) attn_drain(&full[i % stages], static_cast<uint32_t>(i / stages) & 1u);
             }
         } else if (warp == 1) {
             // ---------------------------------------------------------- MMAs
