@@ -611,7 +611,6 @@ class TreeVerifier:
     def __init__(self, nseq, B, V, temperature=1.0):
         self.nseq, self.B, self.V = int(nseq), int(B), int(V)
         self.cfg = DartVerifyConfig(self.nseq, self.B, self.V, DART_F32, self.V, float(temperature))
-        self.ref = C.byref(self.cfg)
         i32 = lambda *shape: _empty(shape, dtype=torch.int32, device="cuda")  # noqa: E731
         self.dev = torch.cuda.current_device()
         self.out = dict(n_rows=i32(nseq), rows=i32(nseq, B + 1), tokens=i32(nseq, B + 1),
@@ -631,13 +630,13 @@ class TreeVerifier:
         ss, ld, one = logits.stride()
         if one != 1 and V > 1 or ss != (B + 1) * ld and nseq > 1:
             raise ValueError("logits: dense rows, one stride between all of them expected")
-        cfg = self.cfg
+        cfg = DartVerifyConfig.from_buffer_copy(self.cfg)  # (of this call alone: two threads may be here)
         cfg.dtype, cfg.ld = DART_F32 if f32 else DART_BF16, ld
         rnd = (None, None)
         if cfg.temperature > 0:
             rnd = _expect(u, "u", torch.float32, (nseq, B + 1), dev), _expect(noise, "noise", torch.float32, (nseq, V), dev)
         _check(lib().dart_verify_tree(
-            self.ref, logits.data_ptr(), _expect(tokens, "tokens", torch.int32, (nseq, B), dev),
+            C.byref(cfg), logits.data_ptr(), _expect(tokens, "tokens", torch.int32, (nseq, B), dev),
             _expect(parents, "parents", torch.int32, (nseq, B), dev), _expect(n_nodes, "n_nodes", torch.int32, (nseq,), dev),
             *rnd, *self.out_ptr, st), "dart_verify_tree")
         return self.out
