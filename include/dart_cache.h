@@ -60,12 +60,13 @@ typedef struct {
  *   k, v   bf16: row r of sequence s at element (s * R + r) * stride, its Hkv
  *          heads of dh elements one after the other; stride (a multiple of
  *          8, >= Hkv * dh) makes slices of a fused projection possible
- * K is rotated at the token's position (rotate-half form, angles exact to
- * 2^-32 of a turn) in fp32.  bf16 pools hold the rounded values; e4m3 pools
+ * K is rotated at the token's position p (rotate-half form, angles to 2^-26 +
+ * p 2^-54 of a turn) in fp32.  bf16 pools hold the rounded values; e4m3 pools
  * scale = max |x| / 448 of the token's head (at least 2^-120; 1 if it is all
- * zero) and x / scale rounded to e4m3.  A NaN stays one in its place, an
- * infinity makes the whole head NaN when it is read.  Positions past
- * max_pages * page_size are not written and set value 4 in *status.  No other
+ * zero) and x / scale, quotients rounded to fp32 and then to e4m3.  A NaN stays
+ * one in its place (in K in its rotated pair), an infinity makes the whole head
+ * NaN when it is read.  Positions past max_pages * page_size are not written
+ * and set value 4 in *status.  No other
  * slot changes; lens is not advanced.  Two tokens of one call must not fall on
  * one slot (two sequences that share a page and both write in it). */
 int dart_cache_append(const dart_kv_cache *cache, int nseq, int max_pages, const int32_t *page_table,

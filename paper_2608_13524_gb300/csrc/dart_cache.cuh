@@ -11,10 +11,11 @@ namespace dart {
 
 constexpr int kHeadDim = 128;
 
-// RoPE frequencies as fractions of a turn in units of 2^-64:
-// round(theta^(-2t/dh) / (2 pi) * 2^64).  pos * f modulo 2^64 is the exact
-// fraction of a turn of the rounded frequency, so far positions lose nothing
-// (an fp32 product is off by pos * 2^-24 radians).
+// RoPE frequencies as fractions of a turn in units of 2^-64: the integer part of
+// theta^(-2t/dh) / (2 pi) * 2^64, computed in fp64.  pos * f modulo 2^64 is the
+// exact fraction of a turn of that frequency, so far positions lose nothing but
+// pos * 2^-54 of a turn of the frequency's own (an fp32 product is off by
+// pos * 2^-24 radians).
 struct RopeTurns {
     uint64_t f[kHeadDim / 2];
 };
@@ -31,7 +32,8 @@ inline const RopeTurns& rope_turns(float theta) {
 }
 
 // cos and sin of position pos at frequency f: the top 32 bits of the turn, as
-// half turns in [-1, 1).
+// half turns in [-1, 1), rounded to fp32 (2^-26 of a turn at most, which moves a
+// rotated pair by 2^-23.3 of its length).
 __device__ __forceinline__ void rope_sincos(uint64_t f, int pos, float* sn, float* cs) {
     const int32_t top = static_cast<int32_t>((static_cast<uint64_t>(static_cast<int64_t>(pos)) * f) >> 32);
     sincospif(static_cast<float>(top) * 4.656612873077392578e-10f, sn, cs);  // 2^-31
