@@ -1,12 +1,26 @@
-"""Cache writes: e4m3 codes and scales bit by bit."""
+"""Cache writes: the form for many tokens (four heads a group of threads), and
+e4m3 codes and scales bit by bit.  Tolerances: see test_cache_append_gpu.py."""
 import numpy as np
 import pytest
 import torch
 
 import serve_data as sd
-from test_cache_append_gpu import THETA, dart, setup, up  # noqa: F401
+from test_cache_append_gpu import THETA, check, dart, setup, up  # noqa: F401
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("Hkv,R,path", [(5, 2500, False), (6, 2500, True), (8, 2449, False), (4, 4900, False)])
+def test_many_tokens(dart, Hkv, R, path, fp8):  # noqa: F811
+    """At least 9728 groups, heads that do not fill the last group of four among them."""
+    lens, n_rows = [3, 130], [R, R - 600]
+    cache, pool, table, dk, dv, k, v, rows = setup(dart, 2, R, lens, n_rows, 64, fp8, Hkv, 8200 + Hkv, path)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    cache.append(dk, dv, up(table), up(lens), up(n_rows), rows=None if rows is None else up(rows), rope_theta=THETA, status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    check(cache, pool, table, k, v, lens, n_rows, rows, 64, fp8)
 
 
 @pytest.mark.parametrize("scale", [1.0, 1e-30, 1e-33, 3e-36, 1e36])

@@ -99,3 +99,74 @@ def test_a_masked_token_is_never_drawn(dart, dtype, low):  # noqa: F811
     want = zf[np.arange(nseq), 0, first]
     lp = want - np.log(np.exp(zf[:, 0, :B].astype(np.float64)).sum(1))
     assert np.abs(out["logp"][:, 0].cpu().numpy() - lp).max() <= LOGP
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("T", [0.0, 1.0])
+@pytest.mark.parametrize("kids", [31, 32, 33, 64, 200])
+def test_many_children_of_one_row(dart, kids, T, dtype):  # noqa: F811
+    """Repeated tokens on both sides of the 32nd child, u in the middle of the
+    first, the last and the border children's shares, and beyond all of them."""
+    V, B = 400, 210
+    g = np.random.default_rng(23)
+    picks = sorted({0, 1, kids // 2, kids - 1} | ({31, 32, 33} & set(range(kids))))
+    nseq = len(picks) + 1
+    row = torch.from_numpy(g.standard_normal(V).astype(np.float32)).to(dtype).float().numpy()
+    toks = g.permutation(V)[:B].astype(np.int32)
+    for a, b in ((2, 0), (28, 5), (35, 3), (40, 36), (100, 30)):  # child a repeats child b
+        if a < kids and a not in picks:
+            toks[a] = toks[b]
+    z = np.tile(row, (nseq, B + 1, 1))
+    parents = np.full((nseq, B), 0, np.int32)  # the others: children of the first node
+    parents[:, :kids] = -1
+    tokens = np.tile(toks, (nseq, 1))
+    p = np.exp(row.astype(np.float64))
+    p /= p.sum()
+    share = np.array([0.0 if toks[i] in toks[:i] else p[toks[i]] for i in range(kids)])
+    upto = np.cumsum(share)
+    u = np.full((nseq, B + 1), 0.9999, np.float32)
+    for s, i in enumerate(picks):
+        u[s, 0] = upto[i] - share[i] / 2
+        if T == 0:
+            z[s, 0, toks[i]] = 10.0
+    u[nseq - 1, 0] = (upto[-1] + 1) / 2
+    noise = np.maximum(g.exponential(size=(nseq, V)), 1e-9).astype(np.float32)
+    zf, d = device_logits(z, dtype)
+    n = np.full(nseq, B, np.int32)
+    out = run(dart, d, tokens, parents, n, T, u, noise)
+    want = serve.verify(zf, tokens, parents, n, T, u, noise)
+    assert [w[0][1] for w in want[:-1]] == [i + 1 for i in picks]  # (the oracle keeps the children that were meant)
+    check(out, want, B + 1)
+
+
+@pytest.mark.parametrize("T", [0.0, 0.9])
+@pytest.mark.parametrize("nseq,V,dtype", [(1, 151936, torch.float32), (24, 70001, torch.float32), (24, 20011, torch.bfloat16),
+                                          (24, 150000, torch.bfloat16)], ids=str)
+def test_long_rows_and_many_sequences(dart, nseq, V, dtype, T):  # noqa: F811
+    """Rows beyond the vectors that a thread holds, with children, the largest
+    logit and the token that follows among the elements behind them, and the
+    clusters of many sequences."""
+    B = 6
+    g = np.random.default_rng(24)
+    ctas = 16 if nseq == 1 else 8
+    width = 4 if dtype == torch.float32 else 8
+    share = V // width // ctas
+    behind = np.concatenate([np.arange(min(512 * 4, share - 1), share) + r * share for r in range(ctas)]) * width
+    behind = behind[behind < V - width]
+    z = g.standard_normal((nseq, B + 1, V)).astype(np.float32)
+    tokens = np.zeros((nseq, B), np.int32)
+    parents = np.tile(np.array([-1, -1, -1, 0, 1, 3], np.int32), (nseq, 1))
+    last = g.choice(behind, nseq)
+    for s in range(nseq):
+        tokens[s] = g.choice(np.setdiff1d(behind, last[s]), B, replace=False) + g.integers(0, width, B)
+        z[s, 0, tokens[s, s % 3]] = 16.0
+        for r in range(1, B + 1):
+            z[s, r, last[s] + 1] = 16.0
+    zf, d = device_logits(torch.from_numpy(z).to(dtype).float().numpy(), dtype)
+    u = np.full((nseq, B + 1), 0.5, np.float32)
+    noise = np.maximum(g.exponential(size=(nseq, V)), 1e-3).astype(np.float32)
+    n = np.full(nseq, B, np.int32)
+    out = run(dart, d, tokens, parents, n, T, u, noise)
+    want = serve.verify(zf, tokens, parents, n, T, u, noise)
+    assert any(len(w[0]) > 1 for w in want)
+    check(out, want, B + 1)
