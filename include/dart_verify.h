@@ -130,8 +130,9 @@ int dart_ancestor_mask(const int32_t *parents, const int32_t *n_nodes, int nseq,
  *     child that has it is kept, else the walk stops.
  * A child whose token an earlier sibling has, whose token is outside [0, V),
  * whose parent is not an earlier node or -1, or that is not below n_nodes, is
- * never kept.  A NaN logit counts as -inf, +inf as the largest float; a row
- * without a finite logit keeps no child and gives the token -1.
+ * never kept.  A NaN logit counts as -inf, +inf as the largest number of the
+ * logits' type; a row without any other than -inf keeps no child and gives the
+ * token -1.
  */
 typedef struct {
     int nseq;          /* sequences, >= 1 */

@@ -54,8 +54,10 @@ struct VerifyArgs {
     float* logp;
 };
 
-// NaN counts as -inf (fmaxf takes the number), +inf as the largest float.
-__device__ __forceinline__ float clean(float z) { return fminf(fmaxf(z, -INFINITY), FLT_MAX); }
+// NaN counts as -inf (fmaxf takes the number), +inf as the largest number of the logits' type
+// (a bf16 one, too: single elements and vectors have to agree).
+constexpr float kBf16Max = 3.38953138925153547590470800371487866880e38f;  // 0x7F7F
+__device__ __forceinline__ float clean(float z, float most) { return fminf(fmaxf(z, -INFINITY), most); }
 __device__ __forceinline__ float fast_exp2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -72,23 +74,23 @@ template <typename T>
 __device__ __forceinline__ float load_logit(const T* row, int i);
 template <>
 __device__ __forceinline__ float load_logit<float>(const float* row, int i) {
-    return clean(ld_plain(row + i));
+    return clean(ld_plain(row + i), FLT_MAX);
 }
 template <>
 __device__ __forceinline__ float load_logit<__nv_bfloat16>(const __nv_bfloat16* row, int i) {
-    return clean(__bfloat162float(ld_plain(row + i)));
+    return clean(__bfloat162float(ld_plain(row + i)), kBf16Max);
 }
 
-// The logits of one 16-byte vector: words without NaN, their values as load_logit
-// gives them, and the values' maximum (bf16: two at a time).
+// The logits of one 16-byte vector: cleaned words, their values, and the values'
+// maximum (bf16: two at a time).
 template <typename T>
 struct Vec;
 template <>
 struct Vec<float> {
     static constexpr int n = 4;
     static __device__ __forceinline__ uint4 clean4(const uint4& w) {
-        return make_uint4(__float_as_uint(clean(__uint_as_float(w.x))), __float_as_uint(clean(__uint_as_float(w.y))),
-                          __float_as_uint(clean(__uint_as_float(w.z))), __float_as_uint(clean(__uint_as_float(w.w))));
+        auto one = [](uint32_t x) { return __float_as_uint(clean(__uint_as_float(x), FLT_MAX)); };
+        return make_uint4(one(w.x), one(w.y), one(w.z), one(w.w));
     }
     static __device__ __forceinline__ void get(const uint4& w, float (&z)[4]) {
         z[0] = __uint_as_float(w.x);
@@ -103,10 +105,10 @@ struct Vec<float> {
 template <>
 struct Vec<__nv_bfloat16> {
     static constexpr int n = 8;
-    // (+inf stays until a value is fp32: the largest float is no bf16)
     static __device__ __forceinline__ uint32_t clean2(uint32_t w) {
-        const __nv_bfloat162 low = __halves2bfloat162(__ushort_as_bfloat16(0xFF80), __ushort_as_bfloat16(0xFF80));  // -inf
-        const __nv_bfloat162 r = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&w), low);
+        const __nv_bfloat162 low = __halves2bfloat162(__ushort_as_bfloat16(0xFF80), __ushort_as_bfloat16(0xFF80));   // -inf
+        const __nv_bfloat162 high = __halves2bfloat162(__ushort_as_bfloat16(0x7F7F), __ushort_as_bfloat16(0x7F7F));  // kBf16Max
+        const __nv_bfloat162 r = __hmin2(__hmax2(*reinterpret_cast<const __nv_bfloat162*>(&w), low), high);
         return *reinterpret_cast<const uint32_t*>(&r);
     }
     static __device__ __forceinline__ uint4 clean4(const uint4& w) {
@@ -116,14 +118,14 @@ struct Vec<__nv_bfloat16> {
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            z[2 * e] = fminf(__uint_as_float(u[e] << 16), FLT_MAX);
-            z[2 * e + 1] = fminf(__uint_as_float(u[e] & 0xFFFF0000u), FLT_MAX);
+            z[2 * e] = __uint_as_float(u[e] << 16);
+            z[2 * e + 1] = __uint_as_float(u[e] & 0xFFFF0000u);
         }
     }
     static __device__ __forceinline__ float top(const uint4& w) {
         auto two = [](uint32_t x) { return *reinterpret_cast<const __nv_bfloat162*>(&x); };
         const __nv_bfloat162 r = __hmax2(__hmax2(two(w.x), two(w.y)), __hmax2(two(w.z), two(w.w)));
-        return fminf(fmaxf(__low2float(r), __high2float(r)), FLT_MAX);
+        return fmaxf(__low2float(r), __high2float(r));
     }
 };
 
@@ -410,9 +412,10 @@ __global__ void __launch_bounds__(kVerifyThreads, 1) verify_tree_kernel(const Ve
             __syncthreads();
             const uint32_t child = sm.child[tid];
             RowStat w{-INFINITY, 0.0f, 0x7FFFFFFF, 0};
+            const float least = m + kLeastLog2 / c;
             auto offer = [&](float z, float e, int t) {  // (tokens of a thread are not in ascending order only at the odd ones)
-                const float lp = (z - m) * c, x = lp >= kLeastLog2 ? lp - fast_log2(e) : -INFINITY;
-                if (x > w.m || (x == w.m && t < w.arg)) {
+                const float x = (z - m) * c - fast_log2(e);
+                if (z >= least && (x > w.m || (x == w.m && t < w.arg))) {
                     w.m = x;
                     w.arg = t;
                 }

@@ -31,8 +31,8 @@ def device_logits(z, dtype, ld=None):
 @pytest.mark.parametrize("T", [0.0, 1.0, 0.7])
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 def test_infinite_logits(dart, dtype, T, ld):  # noqa: F811
-    """+inf counts as the largest float wherever it stands: on a child, beside
-    the children, on both, among the elements that no 16-byte vector holds."""
+    """+inf counts as the largest number of the type wherever it stands: on a child,
+    beside the children, on both, among the elements that no 16-byte vector holds."""
     V, B, inf = 300, 4, np.inf
     g = np.random.default_rng(21)
     z = g.standard_normal((12, B + 1, V)).astype(np.float32)
@@ -47,11 +47,12 @@ def test_infinite_logits(dart, dtype, T, ld):  # noqa: F811
     z[5, 0, [5, 9]] = inf; u[5] = 0.75                     # noqa: E702
     z[6, 0, [77, 299]] = inf                               # the last element of the row
     z[7, 0, [0, 77]] = inf                                 # the first
-    z[8, 0, 20] = float(torch.finfo(dtype).max); z[8, 0, 77] = inf   # noqa: E702  (fp32: equal, so a tie)
+    z[8, 0, 20] = float(torch.finfo(dtype).max); z[8, 0, 77] = inf   # noqa: E702  (equal: a tie)
     z[9, 0, 9] = inf; z[9, 2] = z[9, 0]; z[9, 4, 298] = inf          # noqa: E702  further down a branch
     z[10, 0, [1, 296, 299]] = inf; u[10] = 0.9             # noqa: E702
     z[11, 0, :] = inf; u[11] = 0.999                       # noqa: E702  everywhere
     zf, d = device_logits(torch.from_numpy(z).to(dtype).float().numpy(), dtype, ld)
+    zf = np.minimum(zf, float(torch.finfo(dtype).max))
     noise = np.maximum(g.exponential(size=(12, V)), 1e-9).astype(np.float32)
     n = np.full(12, B, np.int32)
     out = run(dart, d, tokens, parents, n, T, u, noise)
