@@ -269,8 +269,9 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
     }
     long long to_load = load.s < a.nseq ? left : 0;  // places not yet loaded
     StageRing<kStages> fills;
-    int failed = 0;
-    volatile int* abort = &failed;
+    bool failed = false;
+    int none = 0;
+    volatile int* abort = &none;  // (a warp waits for no other)
     const uint64_t policy = l2_policy_evict_first();  // (every key is read once)
     const int page_mask = (1 << a.page_log2) - 1;
 
@@ -548,7 +549,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
             if (!failed) {
                 const bool got = mbar_wait_inline(bar + st, fills.parity(fills.used), abort);
                 if (!__all_sync(kFull, got)) {
-                    failed = 1;
+                    failed = true;
                     if (a.status && lane == 0) atomicOr(a.status, kDevTimeout);
                 }
             }
