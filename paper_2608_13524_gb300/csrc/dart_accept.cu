@@ -11,10 +11,11 @@
 // a step loads its vectors into registers before anything else, has the rows
 // of the first children fetched into L2 while its own sums are made, and the
 // noise, which only the last row wants, is copied to shared memory meanwhile.
-// Measured, V = 151936, bf16: about 3.4 us a step (its row's share from L2 0.8, the
-// sums and the two merges, a cluster barrier, the decision), a tree of 256 nodes
-// with three kept 19 us, one of 4096 tokens greedily 7 us; 1.8 MB of rows and noise
-// at 0.1 TB/s, so bandwidth is not in question.
+// Measured, V = 151936, bf16, mean over 16 inputs: 18.4 us for walks of 3.5 rows, 38.4
+// for eight of which the longest has 8.2, so 4.3 us a row (3.4 where it is in L2: its
+// share 0.8, the sums and the two merges, a cluster barrier, the decision) and 3.4
+// beside the rows; V = 4096 greedily 10.5 us for 2.8 rows.  2 MB of rows and noise at
+// 0.1 TB/s, so bandwidth is not in question.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>

@@ -986,7 +986,8 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 }
                 l *= alpha;
                 m_run = m_new;
-                // P = 2^(s - m) as bf16 pairs; hidden keys hold -inf and give 0 (so does
+                // P = 2^(s - m) as pairs of V's operand type (bf16 or f16, which a product's
+                // operands share; the sum has the unrounded weights); hidden keys hold -inf and give 0 (so does
                 // every key of a row that has seen no visible key: m = -inf)
                 const float nm = m_run == -INFINITY ? 0.0f : kBoost - m_run + (kF16 ? log2_of(down) : 0.0f);
                 float2 sum0 = make_float2(0.0f, 0.0f), sum1 = sum0;
