@@ -495,7 +495,7 @@ def _rows(t, name, shape, dev):
     if sd != 1 or (sh != dh and heads > 1):
         raise ValueError(f"{name}: the heads of a row have to lie one after the other")
     if R == 1:
-        sr = ss if nseq > 1 else max(sr, heads * dh)
+        sr = ss if nseq > 1 else heads * dh
     elif ss != R * sr and nseq > 1:
         raise ValueError(f"{name}: one stride between all rows of all sequences expected")
     return t.data_ptr(), sr

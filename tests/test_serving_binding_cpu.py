@@ -35,3 +35,14 @@ def test_a_call_of_a_verifier_keeps_its_own_configuration(monkeypatch):
 
     call(torch.zeros(1, 3, 7))
     assert seen == [(dart.DART_F32, 7), (dart.DART_BF16, 12), (dart.DART_F32, 7)]
+
+
+def test_the_stride_of_a_single_row_does_not_matter():
+    """One row of one sequence: the strides of its dimensions of length 1 may be
+    anything, and are no reason to refuse it."""
+    flat = torch.zeros(4096, dtype=torch.bfloat16)
+    for ss, sr in ((5, 1001), (1, 1), (0, 0), (1001, 3)):
+        assert dart._rows(flat.as_strided((1, 1, 2, 128), (ss, sr, 128, 1)), "q", (1, 1, 2, 128), -1) == (flat.data_ptr(), 256)
+    # one row each of several sequences: the stride between them; several rows of one: between these
+    assert dart._rows(flat.as_strided((3, 1, 2, 128), (264, 7, 128, 1)), "q", (3, 1, 2, 128), -1)[1] == 264
+    assert dart._rows(flat.as_strided((1, 3, 2, 128), (7, 264, 128, 1)), "q", (1, 3, 2, 128), -1)[1] == 264
