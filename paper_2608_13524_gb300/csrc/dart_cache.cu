@@ -70,7 +70,8 @@ __device__ __forceinline__ void unpack(const uint4& a, const uint4& b, Row& x) {
 
 // x / scale, each quotient rounded once to fp32 (two at a time): the product with the
 // rounded reciprocal is at most a unit off, its remainder is exact in one fma, and a
-// second fma corrects it (Markstein's division).  Infinities and NaN give NaN.
+// second fma corrects it (P. Markstein, IBM J. Res. Dev. 34, 1990).  Infinities and NaN
+// give NaN.
 __device__ __forceinline__ float2 quotients(float a, float b, float scale, float inv) {
     const float2 q = fma2(make_float2(a, b), make_float2(inv, inv), make_float2(-0.0f, -0.0f));
     const float2 r = fma2(q, make_float2(scale, scale), make_float2(-a, -b));
