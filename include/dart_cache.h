@@ -4,13 +4,17 @@
  *
  * dart_tree_attention (include/dart_verify.h) takes one contiguous bf16
  * context of one length.  Here sequences of different lengths share a pool of
- * pages, in bf16 or in 8 bits, and the pass has the row of the last verified
+ * pages, in bf16, 8 or 4 bits, and the pass has the row of the last verified
  * token (the root of the draft tree) beside the tree's nodes, so that with no
  * nodes it is the decoding of single tokens.
  *
- *   K, V pools   [num_pages][Hkv][page_size][dh], bf16 or e4m3
- *   their scales [num_pages][Hkv][page_size] fp32 (e4m3 only): an element
- *                stands for code * scale; K is stored rotated (RoPE)
+ *   K, V pools   [num_pages][Hkv][page_size][dh], bf16, e4m3 or e2m1 (two
+ *                codes a byte, the even element's in its low half)
+ *   their scales [num_pages][Hkv][page_size] fp32 (e4m3 and e2m1), >= 0
+ *   their blocks [num_pages][Hkv][page_size][dh / 16] e4m3 (e2m1 only), >= 0:
+ *                an element stands for code * scale, or code * block * scale
+ *                with the block scale of its 16 elements.  K is stored
+ *                rotated (RoPE)
  *   page_table   [nseq][max_pages] int32: token p of sequence s is slot
  *                p % page_size of page page_table[s][p / page_size]
  *   lens         [nseq] int32: tokens of each sequence in the cache
@@ -42,15 +46,17 @@ extern "C" {
 
 #define DART_KV_BF16 0
 #define DART_KV_E4M3 1
+#define DART_KV_E2M1 2
 
 typedef struct {
     int num_pages; /* pages in the pool, >= 1 */
     int page_size; /* tokens per page: 16, 32, 64 or 128 */
     int Hkv;       /* kv heads, >= 1 */
     int dh;        /* head dimension; 128 */
-    int dtype;     /* DART_KV_BF16 or DART_KV_E4M3 */
+    int dtype;     /* DART_KV_BF16, DART_KV_E4M3 or DART_KV_E2M1 */
     void *k, *v;   /* the pools, 16-byte aligned */
     float *k_scale, *v_scale; /* 16-byte aligned; NULL for bf16 */
+    void *k_block, *v_block;  /* e2m1: the block scales, 16-byte aligned; not looked at for other types */
 } dart_kv_cache;
 
 /* Writes n_rows[s] (clamped to [0, R]) tokens of every sequence into its
@@ -65,13 +71,32 @@ typedef struct {
  * scale = max |x| / 448 of the token's head (at least 2^-120; 1 if it is all
  * zero) and x / scale, quotients rounded to fp32 and then to e4m3.  A NaN stays
  * one in its place (in K in its rotated pair), an infinity makes the whole head
- * NaN when it is read.  Positions past max_pages * page_size are not written
+ * NaN when it is read.
+ * e2m1 pools: a row's scale is a power of two, 2^-10 times the one at or below
+ * its largest magnitude (at least 2^-120; 1 if it is all zero), so that x /
+ * scale is exact; a block scale is its 16 elements' largest magnitude / scale /
+ * 6 rounded to e4m3 (at most 342; it may be 0), and a code x / scale / block
+ * rounded to e2m1, both to nearest, ties to even, magnitudes above 6 to 6.
+ * A NaN or an infinity makes its block (in K, that of its rotated pair too)
+ * NaN when it is read and counts for no scale.
+ * Positions past max_pages * page_size are not written
  * and set value 4 in *status.  No other
  * slot changes; lens is not advanced.  Two tokens of one call must not fall on
  * one slot (two sequences that share a page and both write in it). */
 int dart_cache_append(const dart_kv_cache *cache, int nseq, int max_pages, const int32_t *page_table,
                       const int32_t *lens, int R, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
                       const int32_t *rows, const int32_t *n_rows, float rope_theta, int *status, void *stream);
+
+/* Gives tokens of the cache back: tokens lens[s] .. lens[s] + n_rows[s] - 1
+ * (n_rows clamped to [0, R]) of every sequence as rows 0, 1, ... of sequence s
+ * of k and v (bf16, rows with strides as in dart_cache_append): code * block *
+ * scale rounded to bf16, K as it is stored (rotated).  Rows from n_rows[s] on
+ * and what lies between rows are not written; a position past max_pages *
+ * page_size or a page outside [0, num_pages) leaves its row as it was and sets
+ * value 4 in *status. */
+int dart_cache_read(const dart_kv_cache *cache, int nseq, int max_pages, const int32_t *page_table,
+                    const int32_t *lens, int R, void *k, int64_t k_stride, void *v, int64_t v_stride,
+                    const int32_t *n_rows, int *status, void *stream);
 
 typedef struct {
     int nseq;         /* sequences, >= 1 */

@@ -5,11 +5,18 @@
 #include <cmath>
 #include <cstdint>
 
+#include "../../include/dart_cache.h"
 #include "dart_device.cuh"
 
 namespace dart {
 
 constexpr int kHeadDim = 128;
+constexpr int kBlockDim = 16, kBlocks = kHeadDim / kBlockDim;  // elements of a block scale (e2m1), block scales of a row
+
+// Bytes of a row of head elements in pages of type DART_KV_*.
+__host__ __device__ constexpr int row_bytes(int type) {
+    return type == DART_KV_BF16 ? 2 * kHeadDim : type == DART_KV_E4M3 ? kHeadDim : kHeadDim / 2;
+}
 
 // RoPE frequencies as fractions of a turn in units of 2^-64: the integer part of
 // theta^(-2t/dh) / (2 pi) * 2^64, computed in fp64.  pos * f modulo 2^64 is the
@@ -44,6 +51,27 @@ __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w 
 __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
+}
+
+// The eight e2m1 codes of a word as f16 pairs, elements 2 i, 2 i + 1 in x[i]: exact.
+__device__ __forceinline__ void e2m1_f16(uint32_t word, uint32_t (&x)[4]) {
+    asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n"
+        " cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}"
+        : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
+        : "r"(word));
+}
+// Two e4m3 codes as an f16 pair: exact.
+__device__ __forceinline__ uint32_t e4m3_f16(uint32_t two) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(static_cast<uint16_t>(two)));
+    return r;
+}
+// Products of f16 pairs (of an e2m1 code and a block scale: at most 6 significant
+// bits between 2^-10 and 2688, exact).
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
 

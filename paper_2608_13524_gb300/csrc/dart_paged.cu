@@ -44,14 +44,15 @@
 
 namespace dart {
 
-bool encode_rows(CUtensorMap* m, const void* base, long long rows, bool fp8, int box_rows) {
+bool encode_rows(CUtensorMap* m, const void* base, long long rows, int type, int box_rows) {
     EncodeTiledFn fn = tensor_map_encoder();
     if (!fn) return false;
-    const cuuint64_t dims[2] = {kHeadDim, static_cast<cuuint64_t>(rows)};
-    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(kHeadDim) * (fp8 ? 1 : 2)};
-    const cuuint32_t box[2] = {fp8 ? 128u : 64u, static_cast<cuuint32_t>(box_rows)}, estr[2] = {1, 1};
-    return fn(m, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides,
-              box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+    const bool bytes = type != DART_KV_BF16, four = type == DART_KV_E2M1;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(four ? kHeadDim / 2 : kHeadDim), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(row_bytes(type))};
+    const cuuint32_t box[2] = {type == DART_KV_E4M3 ? 128u : 64u, static_cast<cuuint32_t>(box_rows)}, estr[2] = {1, 1};
+    return fn(m, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides,
+              box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, four ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -78,24 +79,24 @@ __host__ __device__ constexpr int rows_warps(int n) { return n == 1 ? 12 : 8; }
 // up to 1024 e4m3 keys 56.5 us at 1, 54 at 2, 55.5 at 3, 56.5 at 6; bf16 97 at 2, 95 at
 // 3 to 7, 97 at 9).  kUnitCost: 64 trees of 3 nodes over 4096 keys, bf16 105 us at 3,
 // 100 at 6, 98 at 9; e4m3 71, 65, 65 at 2, 4, 6.
-template <bool kFp8>
+template <int kType>
 struct Chunk {
-    static constexpr int kKeys = kFp8 ? 32 : 16;
-    static constexpr int kUnitCost = kFp8 ? 6 : 9, kTokenCost = kFp8 ? 2 : 5;
+    static constexpr int kKeys = kType == DART_KV_BF16 ? 16 : 32;
+    static constexpr int kUnitCost = kType == DART_KV_BF16 ? 9 : 6, kTokenCost = kType == DART_KV_BF16 ? 5 : 2;
 };
 
 // A place in the list of chunks: sequence, kv head, chunk of the unit.
-template <bool kFp8>
+template <int kType>
 struct Place {
     int s, head, chunk;
     int len, nodes, ctx_chunks, chunks, cost;  // of the sequence; cost: the unit's length in the list
     __device__ __forceinline__ void load(const PagedArgs& a) {
-        constexpr int kKeys = Chunk<kFp8>::kKeys;
+        constexpr int kKeys = Chunk<kType>::kKeys;
         len = seq_len(a, s);
         nodes = seq_nodes(a, s);
         ctx_chunks = (len + kKeys - 1) / kKeys;
         chunks = ctx_chunks + (nodes + 1 + 15) / 16;  // (tree rows: 16 at a time)
-        cost = chunks + (a.B == 0 ? Chunk<kFp8>::kTokenCost : Chunk<kFp8>::kUnitCost);
+        cost = chunks + (a.B == 0 ? Chunk<kType>::kTokenCost : Chunk<kType>::kUnitCost);
     }
     __device__ __forceinline__ void next_unit(const PagedArgs& a) {
         chunk = 0;
@@ -108,12 +109,12 @@ struct Place {
 
 // By one warp: the list's length and, then, the place x of it (of its first 32
 // sequences the lengths are kept).
-template <bool kFp8>
+template <int kType>
 struct List {
     long long all, own;  // own: length of sequence `lane`
     __device__ __forceinline__ static long long length(const PagedArgs& a, int s) {
         if (s >= a.nseq) return 0;
-        Place<kFp8> p{};
+        Place<kType> p{};
         p.s = s;
         p.load(a);
         return static_cast<long long>(a.Hkv) * p.cost;
@@ -126,9 +127,9 @@ struct List {
         for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(kFull, n, o);
         all = n;
     }
-    __device__ __forceinline__ Place<kFp8> find(const PagedArgs& a, long long x, int lane) const {
+    __device__ __forceinline__ Place<kType> find(const PagedArgs& a, long long x, int lane) const {
         long long done = 0;
-        Place<kFp8> r{};
+        Place<kType> r{};
         for (int s0 = 0; s0 < a.nseq; s0 += 32) {
             const long long n = s0 == 0 ? own : length(a, s0 + lane);
             long long upto = n;
@@ -201,36 +202,43 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
 __device__ __forceinline__ int slot_row(int q, int n) {
     return q * 8 + ((((n >> 2) ^ n) & 1) << 2) + (n & 2) + (n & 1);
 }
+// The same for 64-byte rows of e2m1 codes and their swizzle: 8-byte pieces t, t + 4 of row
+// slot_row4(q, g), piece g of rows slot_row4(q, 2t + e).
+__device__ __forceinline__ int slot_row4(int q, int n) { return q * 8 + (((n ^ (n >> 2)) & 1) << 2) + ((n >> 2) << 1) + ((n >> 1) & 1); }
 
 __device__ __forceinline__ uint32_t swz(int row, int piece) {  // byte offset in a tile of 128-byte rows
     return static_cast<uint32_t>(row * 128 + ((piece ^ (row & 7)) << 4));
 }
 
-template <bool kFp8, int kN>
+template <int kType, int kN>
 struct Geo {
-    static constexpr int kKeys = Chunk<kFp8>::kKeys;
+    static constexpr int kKeys = Chunk<kType>::kKeys;
     static constexpr int kSubs = kKeys / 16;                             // products of 16 keys
-    static constexpr int kTile = kKeys * kHeadDim * (kFp8 ? 1 : 2);      // K or V of a chunk
+    static constexpr int kTile = kKeys * row_bytes(kType);               // K or V of a chunk
     static constexpr int kWarps = rows_warps(kN), kThreads = 32 * kWarps;
-    static constexpr int kStages = kN == 1 ? 2 : 3;
-    static constexpr int kRing = kWarps * kStages * 2 * kTile;           // 192 KB
-    static constexpr int kScales = kFp8 ? kWarps * kStages * 2 * kKeys * 4 : 0;
+    static constexpr int kStages = kType == DART_KV_E2M1 ? (kN == 1 ? 3 : 5) : kN == 1 ? 2 : 3;
+    static constexpr int kRing = kWarps * kStages * 2 * kTile;           // 192 KB (e2m1: 144, 160)
+    // e4m3, e2m1: a key's scale; e2m1: its block scales
+    static constexpr int kScale = (kType == DART_KV_BF16 ? 0 : 4) + (kType == DART_KV_E2M1 ? kBlocks : 0);
+    static constexpr int kScales = kWarps * kStages * 2 * kKeys * kScale;
     static constexpr int kTurns = kWarps * (kHeadDim / 2) * 8;            // a position's angles, of each warp
     static constexpr int kSmem = kRing + kScales + kTurns + kWarps * kStages * 8;
 };
 
 // 16-byte piece (8 bf16) of a row of the head that step pair i of thread t
 // covers; i and i + 2 are 64 elements apart, as RoPE's pairs are.
-template <bool kFp8>
+template <bool kF16>
 __device__ __forceinline__ int k_piece(int i, int t) {
-    return kFp8 ? 8 * (i >> 1) + 2 * t + (i & 1) : 8 * (i >> 1) + t + 4 * (i & 1);
+    return kF16 ? 8 * (i >> 1) + 2 * t + (i & 1) : 8 * (i >> 1) + t + 4 * (i & 1);
 }
 
-template <bool kFp8, int kN>
+template <int kType, int kN>
 __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
     paged_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                       const __grid_constant__ PagedArgs a) {
-    using G_ = Geo<kFp8, kN>;
+    using G_ = Geo<kType, kN>;
+    constexpr bool kF16 = kType != DART_KV_BF16;   // f16 operands; a scale a key
+    constexpr bool kFour = kType == DART_KV_E2M1;  // block scales beside it
     constexpr int kWarps = G_::kWarps, kThreads = G_::kThreads;
     constexpr int kKeys = G_::kKeys, kSubs = G_::kSubs, kTile = G_::kTile, kStages = G_::kStages;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -238,6 +246,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
     pdl_trigger();
     uint8_t* ring = smem + warp * kStages * 2 * kTile;
     float* scales = reinterpret_cast<float*>(smem + G_::kRing) + warp * kStages * 2 * kKeys;  // [stage][K, V][key]
+    uint8_t* blocks = smem + G_::kRing + kWarps * kStages * 2 * kKeys * 4 + warp * kStages * 2 * kKeys * kBlocks;  // [stage][K, V][key][8]
     float2* turns = reinterpret_cast<float2*>(smem + G_::kRing + G_::kScales) + warp * (kHeadDim / 2);
     uint64_t* bar = reinterpret_cast<uint64_t*>(smem + G_::kRing + G_::kScales + G_::kTurns) + warp * kStages;
     if (lane == 0) {
@@ -256,12 +265,12 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
             for (int j = tid; j < a.Hq * kHeadDim / 8; j += kThreads) o[j] = make_uint4(0, 0, 0, 0);
         }
 
-    const List<kFp8> list(a, lane);
+    const List<kType> list(a, lane);
     const int share = warp * gridDim.x + blockIdx.x;
     const Shares shares(list.all, kWarps * gridDim.x, kMinShare);
     if (share >= shares.count) return;
     long long left = shares.length(share);  // places of this share not yet worked on
-    Place<kFp8> use = list.find(a, shares.begin(share), lane), load = use;
+    Place<kType> use = list.find(a, shares.begin(share), lane), load = use;
     if (lane == 0) {
         a.plan->places[share] = make_int4(use.s, use.head, use.chunk, use.chunks);
         a.plan->nodes[share] = use.nodes;
@@ -283,6 +292,8 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
             if (load.s >= a.nseq) to_load = 0;
         }
     };
+    // row of a 16-key chunk behind a key slot
+    auto row_of = [](int q, int n) { return kFour ? slot_row4(q, n) : slot_row(q, n); };
     auto page_at = [&](int key) {
         return ld_plain(a.table + static_cast<long long>(load.s) * a.max_pages + (key >> a.page_log2));
     };
@@ -291,7 +302,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
         settle();
         if (to_load <= 0) return;
         page[0] = page_at(load.chunk * kKeys);
-        if (kFp8 && a.page_log2 == 4 && load.chunk * kKeys + 16 < load.len) page[1] = page_at(load.chunk * kKeys + 16);
+        if (kF16 && a.page_log2 == 4 && load.chunk * kKeys + 16 < load.len) page[1] = page_at(load.chunk * kKeys + 16);
     };
     auto issue = [&]() {  // loads the chunk at `load`
         if (lane == 0) {
@@ -299,10 +310,11 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
             uint8_t* k = ring + st * 2 * kTile;
             uint8_t* v = k + kTile;
             float* sc = scales + st * 2 * kKeys;
-            const bool halves = kFp8 && a.page_log2 == 4;
-            mbar_arrive_expect_tx(bar + st, 2 * kTile + (kFp8 ? 2 * kKeys * 4 : 0));
+            uint8_t* bl = blocks + st * 2 * kKeys * kBlocks;
+            const bool halves = kF16 && a.page_log2 == 4;
+            mbar_arrive_expect_tx(bar + st, 2 * kTile + 2 * kKeys * G_::kScale);
 #pragma unroll
-            for (int h = 0; h < (kFp8 ? 2 : 1); h++) {
+            for (int h = 0; h < (kF16 ? 2 : 1); h++) {
                 if (h == 1 && !halves) break;
                 long long row = a.pool_rows;  // past the pool: zeros
                 const int key = load.chunk * kKeys + 16 * h;
@@ -314,11 +326,15 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                 }
                 tma_load_2d(k + h * kTile / 2, &tmK, bar + st, 0, static_cast<int>(row), policy);
                 tma_load_2d(v + h * kTile / 2, &tmV, bar + st, 0, static_cast<int>(row), policy);
-                if (kFp8) {
+                if (kF16) {
                     const long long sr = row < a.pool_rows ? row : 0;
                     const uint32_t bytes = halves ? 64 : 128;
                     bulk_load(sc + 16 * h, a.ks + sr, bytes, bar + st);
                     bulk_load(sc + kKeys + 16 * h, a.vs + sr, bytes, bar + st);
+                    if (kFour) {
+                        bulk_load(bl + 16 * h * kBlocks, a.kb + sr * kBlocks, 2 * bytes, bar + st);
+                        bulk_load(bl + (kKeys + 16 * h) * kBlocks, a.vb + sr * kBlocks, 2 * bytes, bar + st);
+                    }
                 } else {
                     tma_load_2d(k + kTile / 2, &tmK, bar + st, 64, static_cast<int>(row), policy);
                     tma_load_2d(v + kTile / 2, &tmV, bar + st, 64, static_cast<int>(row), policy);
@@ -389,7 +405,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                 const __nv_bfloat16* src = a.q + (seq_row + b) * a.q_stride + (head * a.G + (r & (a.G - 1))) * kHeadDim;
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
-                    const int d0 = 8 * k_piece<kFp8>(i, t);
+                    const int d0 = 8 * k_piece<kF16>(i, t);
                     const uint4 u = ld_plain(reinterpret_cast<const uint4*>(src + d0)), w = ld_plain(reinterpret_cast<const uint4*>(src + d0 + 64));
                     const uint32_t uw[4] = {u.x, u.y, u.z, u.w}, ww[4] = {w.x, w.y, w.z, w.w};
                     float cs[8], sn[8];
@@ -404,7 +420,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                 }
             }
             float down = 1.0f, up = a.sl2;
-            if (kFp8) {
+            if (kF16) {
                 // scaled by a power of two to a largest element in [1, 2): f16 then
                 // rounds it to 2^-11 whatever the query's magnitude
                 float mx = 0.0f;
@@ -425,7 +441,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
 #pragma unroll
                 for (int e = 0; e < 4; e++) {  // words of the piece: elements 2 e, 2 e + 1
                     uint32_t w;
-                    if (kFp8) {
+                    if (kF16) {
                         w = pack_f16(x[i][2 * e] * down, x[i][2 * e + 1] * down);
                     } else {
                         // bf16 and what it leaves: with one bf16 term the queries' rounding
@@ -549,6 +565,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
             uint8_t* kt = ring + st * 2 * kTile;
             uint8_t* vt = kt + kTile;
             const float* sck = scales + st * 2 * kKeys;
+            uint8_t* blk = blocks + st * 2 * kKeys * kBlocks;
             if (!failed) {
                 const bool got = mbar_wait_inline(bar + st, fills.parity(fills.used), abort);
                 if (!__all_sync(kFull, got)) {
@@ -561,10 +578,16 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                 if (there < kKeys) {
                     // anything may lie behind the last one: zeros for V, which P = 0 would
                     // not hide (these stores are ordered before the slot's next copy below)
-                    for (int i = lane; i < (kKeys - there) * 8; i += 32) {
+                    if (kFour) {  // (in any order: the rows are whole)
+                        for (int i = lane; i < (kKeys - there) * 4; i += 32)
+                            *reinterpret_cast<uint4*>(vt + there * 64 + i * 16) = make_uint4(0, 0, 0, 0);
+                        if (lane < kKeys - there) *reinterpret_cast<uint2*>(blk + (kKeys + there + lane) * kBlocks) = make_uint2(0, 0);
+                    } else {
+                        for (int i = lane; i < (kKeys - there) * 8; i += 32) {
 #pragma unroll
-                        for (int half = 0; half < (kFp8 ? 1 : 2); half++)
-                            *reinterpret_cast<uint4*>(vt + half * (kTile / 2) + swz(there + (i >> 3), i & 7)) = make_uint4(0, 0, 0, 0);
+                            for (int half = 0; half < (kF16 ? 1 : 2); half++)
+                                *reinterpret_cast<uint4*>(vt + half * (kTile / 2) + swz(there + (i >> 3), i & 7)) = make_uint4(0, 0, 0, 0);
+                        }
                     }
                     __syncwarp();
                 }
@@ -575,7 +598,31 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                     for (int n = 0; n < kN; n++)
 #pragma unroll
                         for (int e = 0; e < 4; e++) sc[j][n][e] = 0.0f;
-                if (kFp8) {
+                if constexpr (kFour) {
+#pragma unroll
+                    for (int j = 0; j < kSubs; j++) {
+                        const int r0 = 16 * j + row_of(0, g), r1 = 16 * j + row_of(1, g);
+                        const uint2 b0 = *reinterpret_cast<const uint2*>(blk + r0 * kBlocks), b1 = *reinterpret_cast<const uint2*>(blk + r1 * kBlocks);
+#pragma unroll
+                        for (int i = 0; i < 2; i++) {  // block t + 4 i of both keys
+                            const uint32_t s0 = e4m3_f16(__byte_perm(i ? b0.y : b0.x, 0u, t * 0x11)), s1 = e4m3_f16(__byte_perm(i ? b1.y : b1.x, 0u, t * 0x11));
+                            const uint2 x = *reinterpret_cast<const uint2*>(kt + swz64(r0, (t + 4 * i) >> 1) + 8 * (t & 1));
+                            const uint2 y = *reinterpret_cast<const uint2*>(kt + swz64(r1, (t + 4 * i) >> 1) + 8 * (t & 1));
+#pragma unroll
+                            for (int w = 0; w < 2; w++) {
+                                uint32_t xw[4], yw[4];
+                                e2m1_f16(w ? x.y : x.x, xw);
+                                e2m1_f16(w ? y.y : y.x, yw);
+#pragma unroll
+                                for (int h = 0; h < 2; h++) {
+                                    const uint32_t k[4] = {mul_f16x2(xw[2 * h], s0), mul_f16x2(yw[2 * h], s1), mul_f16x2(xw[2 * h + 1], s0), mul_f16x2(yw[2 * h + 1], s1)};
+#pragma unroll
+                                    for (int n = 0; n < kN; n++) mma_f16(sc[j][n], k, q[n][4 * i + 2 * w + h][0], q[n][4 * i + 2 * w + h][1]);
+                                }
+                            }
+                        }
+                    }
+                } else if constexpr (kF16) {
 #pragma unroll
                     for (int i = 0; i < 2; i++)
 #pragma unroll
@@ -626,26 +673,26 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                 for (int j = 0; j < kSubs; j++)
 #pragma unroll
                     for (int qq = 0; qq < 2; qq++) {
-                        const int key = 16 * j + slot_row(qq, g);
-                        const float by = kFp8 ? sck[key] : 1.0f;
-                        vs[j][qq] = kFp8 ? sck[kKeys + key] : 1.0f;
+                        const int key = 16 * j + row_of(qq, g);
+                        const float by = kF16 ? sck[key] : 1.0f;
+                        vs[j][qq] = kF16 ? sck[kKeys + key] : 1.0f;
 #pragma unroll
                         for (int n = 0; n < kN; n++)
 #pragma unroll
-                            for (int e = 0; e < 2; e++) sc[j][n][2 * qq + e] *= kFp8 ? rs[n][e] * by : rs[n][e];
+                            for (int e = 0; e < 2; e++) sc[j][n][2 * qq + e] *= kF16 ? rs[n][e] * by : rs[n][e];
                     }
                 if (there < kKeys) {
 #pragma unroll
                     for (int j = 0; j < kSubs; j++)
 #pragma unroll
                         for (int qq = 0; qq < 2; qq++)
-                            if (16 * j + slot_row(qq, g) >= there) {
+                            if (16 * j + row_of(qq, g) >= there) {
 #pragma unroll
                                 for (int n = 0; n < kN; n++) sc[j][n][2 * qq] = sc[j][n][2 * qq + 1] = -INFINITY;
                                 vs[j][qq] = 0.0f;
                             }
                 }
-                if (kFp8) {
+                if (kF16) {
                     float top = 0.0f;
 #pragma unroll
                     for (int j = 0; j < kSubs; j++) top = fmaxf(top, fmaxf(vs[j][0], vs[j][1]));
@@ -663,7 +710,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                     }
                 }
                 soften(sc);
-                if (kFp8) {
+                if constexpr (kF16) {
                     const float inv = vref > 0.0f ? 128.0f / vref : 0.0f;  // (0: all scales are)
 #pragma unroll
                     for (int u = 0; u < kSubs; u++) {
@@ -673,6 +720,43 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                         for (int n = 0; n < kN; n++) {
                             p[n][0] = transpose_8x8(pack_f16(sc[u][n][0] * w0, sc[u][n][1] * w0));
                             p[n][1] = transpose_8x8(pack_f16(sc[u][n][2] * w1, sc[u][n][3] * w1));
+                        }
+                        if constexpr (kFour) {
+                            // block g of two neighbouring slots' keys: words of 8 codes, and both block scales
+                            uint2 x[2][2];
+                            uint32_t by[2];
+#pragma unroll
+                            for (int qq = 0; qq < 2; qq++) {
+                                uint32_t b[2];
+#pragma unroll
+                                for (int e = 0; e < 2; e++) {
+                                    const int row = 16 * u + row_of(qq, 2 * t + e);
+                                    x[qq][e] = *reinterpret_cast<const uint2*>(vt + swz64(row, g >> 1) + 8 * (g & 1));
+                                    b[e] = *reinterpret_cast<const uint32_t*>(blk + (kKeys + row) * kBlocks + (g & 4));
+                                }
+                                by[qq] = e4m3_f16(__byte_perm(b[0], b[1], (g & 3) * 0x11 + 0x40));
+                            }
+#pragma unroll
+                            for (int odd = 0; odd < 2; odd++) {  // elements 2 j + odd of both words
+                                constexpr uint32_t kLow = 0x0F0F0F0Fu;
+                                uint32_t v[2][2][4];  // [keys][word][j]
+#pragma unroll
+                                for (int qq = 0; qq < 2; qq++)
+#pragma unroll
+                                    for (int w = 0; w < 2; w++) {
+                                        const uint32_t c0 = w ? x[qq][0].y : x[qq][0].x, c1 = w ? x[qq][1].y : x[qq][1].x;
+                                        e2m1_f16(odd ? ((c0 >> 4) & kLow) | (c1 & ~kLow) : (c0 & kLow) | ((c1 << 4) & ~kLow), v[qq][w]);
+#pragma unroll
+                                        for (int j = 0; j < 4; j++) v[qq][w][j] = mul_f16x2(v[qq][w][j], by[qq]);
+                                    }
+#pragma unroll
+                                for (int j = 0; j < 4; j++) {
+                                    const uint32_t both[4] = {v[0][0][j], v[0][1][j], v[1][0][j], v[1][1][j]};
+#pragma unroll
+                                    for (int n = 0; n < kN; n++) mma_f16(acc[n][2 * j + odd], both, p[n][0], p[n][1]);
+                                }
+                            }
+                            continue;
                         }
                         uint32_t x[2][2][4];
 #pragma unroll
@@ -732,7 +816,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                     const __nv_bfloat16* k = a.k + (seq_row + j) * a.k_stride + head * kHeadDim;
 #pragma unroll
                     for (int i = 0; i < 2; i++) {
-                        const int d0 = 8 * k_piece<kFp8>(i, t);
+                        const int d0 = 8 * k_piece<kF16>(i, t);
                         const uint4 x = ld_plain(reinterpret_cast<const uint4*>(k + d0));
                         const uint4 y = ld_plain(reinterpret_cast<const uint4*>(k + d0 + 64));
                         const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
@@ -759,7 +843,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                 const uint32_t k[4] = {w[0][i >> 1][2 * (i & 1)], w[1][i >> 1][2 * (i & 1)], w[0][i >> 1][2 * (i & 1) + 1], w[1][i >> 1][2 * (i & 1) + 1]};
 #pragma unroll
                 for (int n = 0; n < kN; n++) {
-                    if (kFp8) {
+                    if (kF16) {
                         // the queries as one bf16 term (rounded once more, by as much as the
                         // tree keys are): tree keys may leave f16's range
                         uint32_t qb[2];
@@ -788,7 +872,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                         sc[0][n][2 * qq + e] = see ? sc[0][n][2 * qq + e] * rs[n][e] : -INFINITY;
                     }
             soften(sc);
-            if (kFp8) {
+            if (kF16) {
                 if (vref == 0.0f) vref = 1.0f;
                 const float inv = 128.0f / vref;
 #pragma unroll
@@ -799,7 +883,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
             values_bf16(sc[0], [&](int half, int qq, int e) {
                 const int j = key0 + slot_row(qq, 2 * t + e);
                 if (j > nodes) return make_uint4(0, 0, 0, 0);
-                return ld_plain(reinterpret_cast<const uint4*>(a.v + (seq_row + j) * a.v_stride + head * kHeadDim + 8 * (kFp8 ? 2 * g + half : g + 8 * half)));
+                return ld_plain(reinterpret_cast<const uint4*>(a.v + (seq_row + j) * a.v_stride + head * kHeadDim + 8 * (kF16 ? 2 * g + half : g + 8 * half)));
             });
         }
 
@@ -814,11 +898,11 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                 for (int o = 4; o < 32; o <<= 1) l[n][e] += __shfl_xor_sync(kFull, l[n][e], o);
                 const int r = 8 * n + 2 * t + e, b = r >> a.g_log2;
                 if (b > nodes) continue;
-                float by = kFp8 ? vref * 0.0078125f : 1.0f;
+                float by = kF16 ? vref * 0.0078125f : 1.0f;
                 if (whole) by = l[n][e] > 0.0f ? by / l[n][e] : 0.0f;
 #pragma unroll
                 for (int half = 0; half < 2; half++) {
-                    const int d = kFp8 ? 16 * g + 8 * half : 64 * half + 8 * g;  // of the 8 elements
+                    const int d = kF16 ? 16 * g + 8 * half : 64 * half + 8 * g;  // of the 8 elements
                     float o[8];
 #pragma unroll
                     for (int k = 0; k < 8; k++) o[k] = acc[n][k][2 * half + e] * by;
@@ -948,6 +1032,12 @@ bool valid_cfg(const dart_paged_attn_config* c, const dart_kv_cache* cache) {
 constexpr int kFewRows = 16;
 bool few_rows(const dart_paged_attn_config& c, const dart_kv_cache& cache) { return (c.B + 1) * (c.Hq / cache.Hkv) <= kFewRows; }
 
+template <int kType>
+bool allow_rows_smem() {
+    return cudaFuncSetAttribute(paged_rows_kernel<kType, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<kType, 1>::kSmem) == cudaSuccess &&
+           cudaFuncSetAttribute(paged_rows_kernel<kType, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<kType, 2>::kSmem) == cudaSuccess;
+}
+
 // The device's number of SMs; 0 if it is not sm_103a, -1 on an error.  The
 // shared-memory opt-in of the kernels is set on the first call per device.
 int device_sms(int dev) {
@@ -961,10 +1051,7 @@ int device_sms(int dev) {
         cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return -1;
     if (major != 10 || minor != 3) return 0;
-    if (cudaFuncSetAttribute(paged_rows_kernel<false, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<false, 1>::kSmem) != cudaSuccess ||
-        cudaFuncSetAttribute(paged_rows_kernel<true, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<true, 1>::kSmem) != cudaSuccess ||
-        cudaFuncSetAttribute(paged_rows_kernel<false, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<false, 2>::kSmem) != cudaSuccess ||
-        cudaFuncSetAttribute(paged_rows_kernel<true, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<true, 2>::kSmem) != cudaSuccess)
+    if (!allow_rows_smem<DART_KV_BF16>() || !allow_rows_smem<DART_KV_E4M3>() || !allow_rows_smem<DART_KV_E2M1>())
         return -1;
     if (!paged_tiles_prepare_device()) return -1;
     known[dev].store(sms, std::memory_order_release);
@@ -977,13 +1064,13 @@ constexpr size_t rows_workspace() {
     return sizeof(SharePlan) + sizeof(Part<kN>) * 2 * rows_warps(kN) * kMaxSms;
 }
 
-template <bool kFp8, int kN>
+template <int kType, int kN>
 int launch_rows(const PagedArgs& a, const dart_kv_cache& cache, int ctas, cudaStream_t st) {
-    using G_ = Geo<kFp8, kN>;
-    const int box = kFp8 && cache.page_size >= 32 ? 32 : 16;
+    using G_ = Geo<kType, kN>;
+    const int box = kType != DART_KV_BF16 && cache.page_size >= 32 ? 32 : 16;
     CUtensorMap tmK, tmV;
-    if (!encode_rows(&tmK, cache.k, a.pool_rows, kFp8, box) || !encode_rows(&tmV, cache.v, a.pool_rows, kFp8, box)) return DART_ERR_CUDA;
-    if (launch_pdl(paged_rows_kernel<kFp8, kN>, dim3(ctas), dim3(G_::kThreads), G_::kSmem, st, tmK, tmV, a) != cudaSuccess) return DART_ERR_CUDA;
+    if (!encode_rows(&tmK, cache.k, a.pool_rows, kType, box) || !encode_rows(&tmV, cache.v, a.pool_rows, kType, box)) return DART_ERR_CUDA;
+    if (launch_pdl(paged_rows_kernel<kType, kN>, dim3(ctas), dim3(G_::kThreads), G_::kSmem, st, tmK, tmV, a) != cudaSuccess) return DART_ERR_CUDA;
     return launch_pdl(paged_join_kernel<kN>, dim3(G_::kWarps * ctas - 1), dim3(kJoinThreads), 0, st, a) == cudaSuccess ? DART_OK : DART_ERR_CUDA;
 }
 
@@ -1021,7 +1108,6 @@ int dart_paged_attention(const dart_paged_attn_config* cfg, const dart_kv_cache*
     const int sms = device_sms(dev);
     if (sms <= 0) return sms < 0 ? DART_ERR_CUDA : DART_ERR_UNSUPPORTED;
 
-    const bool fp8 = cache->dtype == DART_KV_E4M3;
     PagedArgs a{};
     a.nseq = c.nseq;
     a.B = c.B;
@@ -1047,6 +1133,8 @@ int dart_paged_attention(const dart_paged_attn_config* cfg, const dart_kv_cache*
     a.v_stride = v_stride;
     a.ks = cache->k_scale;
     a.vs = cache->v_scale;
+    a.kb = static_cast<const uint8_t*>(cache->k_block);
+    a.vb = static_cast<const uint8_t*>(cache->v_block);
     a.out = static_cast<__nv_bfloat16*>(out);
     a.plan = static_cast<SharePlan*>(workspace);
     a.parts = static_cast<uint8_t*>(workspace) + sizeof(SharePlan);
@@ -1056,8 +1144,10 @@ int dart_paged_attention(const dart_paged_attn_config* cfg, const dart_kv_cache*
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (!few_rows(c, *cache)) return launch_paged_tiles(a, *cache, static_cast<uint8_t*>(workspace), std::min(sms, kMaxSms), st);
     const int ctas = std::min(sms, kMaxSms);
-    if ((c.B + 1) * a.G <= 8) return fp8 ? launch_rows<true, 1>(a, *cache, ctas, st) : launch_rows<false, 1>(a, *cache, ctas, st);
-    return fp8 ? launch_rows<true, 2>(a, *cache, ctas, st) : launch_rows<false, 2>(a, *cache, ctas, st);
+    const bool eight = (c.B + 1) * a.G <= 8;
+    if (cache->dtype == DART_KV_E2M1) return eight ? launch_rows<DART_KV_E2M1, 1>(a, *cache, ctas, st) : launch_rows<DART_KV_E2M1, 2>(a, *cache, ctas, st);
+    if (cache->dtype == DART_KV_E4M3) return eight ? launch_rows<DART_KV_E4M3, 1>(a, *cache, ctas, st) : launch_rows<DART_KV_E4M3, 2>(a, *cache, ctas, st);
+    return eight ? launch_rows<DART_KV_BF16, 1>(a, *cache, ctas, st) : launch_rows<DART_KV_BF16, 2>(a, *cache, ctas, st);
 }
 
 }  // extern "C"

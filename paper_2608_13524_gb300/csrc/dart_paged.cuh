@@ -30,6 +30,7 @@ struct PagedArgs {
     const __nv_bfloat16 *q, *k, *v;
     long long q_stride, k_stride, v_stride;
     const float *ks, *vs;
+    const uint8_t *kb, *vb;  // block scales (e2m1)
     __nv_bfloat16* out;
     void* parts;  // partial results, two per share: of the unit begun before it, of the unit that goes on after it
     SharePlan* plan;
@@ -77,10 +78,16 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 
+// Byte offset of 16-byte piece `piece` of a row in a tile of 64-byte rows.
+__device__ __forceinline__ uint32_t swz64(int row, int piece) {
+    return static_cast<uint32_t>(row * 64 + ((piece ^ ((row >> 1) & 3)) << 4));
+}
+
 bool valid_cache(const dart_kv_cache* c);
 bool valid_cache_pointers(const dart_kv_cache* c);
-// Rows of dh elements (the whole pool) in boxes of box_rows rows by 128 bytes.
-bool encode_rows(CUtensorMap* m, const void* base, long long rows, bool fp8, int box_rows);
+// Rows of dh elements of type DART_KV_* (the whole pool) in boxes of box_rows rows
+// by 128 bytes (e2m1: 64, a whole row), swizzled over as many.
+bool encode_rows(CUtensorMap* m, const void* base, long long rows, int type, int box_rows);
 
 // 128-row tiles on the tensor-memory path (dart_paged_tiles.cu).
 size_t paged_tiles_workspace(const dart_paged_attn_config& c, const dart_kv_cache& cache);

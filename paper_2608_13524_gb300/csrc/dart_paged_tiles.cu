@@ -63,9 +63,9 @@
 namespace dart {
 namespace {
 
-// Where K and V tiles come from: bf16 pages; e4m3 pages, converted in the CTA;
-// e4m3 pages that paged_widen_kernel has laid out as f16 tiles before.
-enum Source { kPages, kCodes, kWidened };
+// Where K and V tiles come from: bf16 pages; e4m3 or e2m1 pages, converted in the
+// CTA; pages of either that paged_widen_kernel has laid out as f16 tiles before.
+enum Source { kPages, kCodes, kCodes4, kWidened };
 constexpr int kRows = 128;               // query rows per unit (MMA M)
 constexpr int kKeys = 128;               // keys per tile
 constexpr int kHalf = kKeys * 128;       // 128 rows of one 128-byte swizzle column
@@ -110,12 +110,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
-// Two e4m3 codes as an f16 pair: exact.
-__device__ __forceinline__ uint32_t codes_to_f16(uint32_t two) {
-    uint32_t r;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(static_cast<uint16_t>(two)));
-    return r;
-}
 __device__ __forceinline__ uint32_t pack_f16x2(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -165,8 +159,9 @@ __device__ __forceinline__ float pack_piece(const Piece& x, uint4* lo, uint4* hi
 // head by groups of 8 threads, and its rotated queries; blocks from B + 1 on: the
 // side rows that are no tree rows.
 constexpr int kPrepThreads = 256, kGroups = kPrepThreads / 8;
-template <bool kFp8>
+template <int kType>
 __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_constant__ TileArgs ta, const uint8_t* pool_k, const uint8_t* pool_v) {
+    constexpr bool kF16 = kType != DART_KV_BF16;
     __shared__ float2 turn_of[kHeadDim / 2];  // cos, sin
     const PagedArgs& a = ta.p;
     const int tid = threadIdx.x, p = tid & 7, group = tid >> 3, s = blockIdx.x, b = blockIdx.y;
@@ -198,7 +193,7 @@ __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_c
     auto put_side = [&](int kv, int head, int j, const uint4& lo, const uint4& hi) {
         uint4* d = kv ? ta.side_v : ta.side_k;
         const long long row = (static_cast<long long>(s) * a.Hkv + head) * ta.sk + j;
-        if (kFp8) {
+        if (kF16) {
             d += (row >> 7) * (16 * kKeys) + (row & 127);
             d[p * kKeys] = lo;
             d[(8 + p) * kKeys] = hi;
@@ -208,7 +203,7 @@ __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_c
         }
     };
     auto put_scale = [&](int kv, int head, int j, float x) {
-        if (kFp8 && p == 0) (kv ? ta.side_vs : ta.side_ks)[(static_cast<long long>(s) * a.Hkv + head) * ta.sk + j] = x;
+        if (kF16 && p == 0) (kv ? ta.side_vs : ta.side_ks)[(static_cast<long long>(s) * a.Hkv + head) * ta.sk + j] = x;
     };
     if (b > a.B) {
         int j = b - a.B - 1;  // of the side rows that are no tree rows: before them, then after them
@@ -224,16 +219,25 @@ __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_c
             const long long row = there ? ((static_cast<long long>(page) * a.Hkv + head) << a.page_log2) + (key & ((1 << a.page_log2) - 1)) : 0;
             const uint8_t* pool = kv ? pool_v : pool_k;
             uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
-            if (there && kFp8) {
+            if (there && kType == DART_KV_E2M1) {
+                const uint32_t* src = reinterpret_cast<const uint32_t*>(pool + row * row_bytes(kType));
+                const uint2 bl = *reinterpret_cast<const uint2*>((kv ? a.vb : a.kb) + row * kBlocks);
+                const uint32_t by_lo = e4m3_f16(__byte_perm(bl.x, 0u, (p >> 1) * 0x11)), by_hi = e4m3_f16(__byte_perm(bl.y, 0u, (p >> 1) * 0x11));
+                uint32_t x[4], y[4];
+                e2m1_f16(src[p], x);
+                e2m1_f16(src[8 + p], y);
+                lo = make_uint4(mul_f16x2(x[0], by_lo), mul_f16x2(x[1], by_lo), mul_f16x2(x[2], by_lo), mul_f16x2(x[3], by_lo));
+                hi = make_uint4(mul_f16x2(y[0], by_hi), mul_f16x2(y[1], by_hi), mul_f16x2(y[2], by_hi), mul_f16x2(y[3], by_hi));
+            } else if (there && kType == DART_KV_E4M3) {
                 const uint2 x = *reinterpret_cast<const uint2*>(pool + row * kHeadDim + 8 * p), y = *reinterpret_cast<const uint2*>(pool + row * kHeadDim + 64 + 8 * p);
-                lo = make_uint4(codes_to_f16(x.x), codes_to_f16(x.x >> 16), codes_to_f16(x.y), codes_to_f16(x.y >> 16));
-                hi = make_uint4(codes_to_f16(y.x), codes_to_f16(y.x >> 16), codes_to_f16(y.y), codes_to_f16(y.y >> 16));
+                lo = make_uint4(e4m3_f16(x.x), e4m3_f16(x.x >> 16), e4m3_f16(x.y), e4m3_f16(x.y >> 16));
+                hi = make_uint4(e4m3_f16(y.x), e4m3_f16(y.x >> 16), e4m3_f16(y.y), e4m3_f16(y.y >> 16));
             } else if (there) {
                 lo = reinterpret_cast<const uint4*>(pool)[row * 16 + p];
                 hi = reinterpret_cast<const uint4*>(pool)[row * 16 + 8 + p];
             }
             put_side(kv, head, j, lo, hi);
-            if (kFp8) put_scale(kv, head, j, there ? ld_plain((kv ? a.vs : a.ks) + row) : 0.0f);
+            if (kF16) put_scale(kv, head, j, there ? ld_plain((kv ? a.vs : a.ks) + row) : 0.0f);
         }
         return;
     }
@@ -264,14 +268,14 @@ __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_c
                     x.hi[e] = hi * t.x + lo * t.y;
                 }
             uint4 lo, hi;
-            const float factor = pack_piece<kFp8>(x, &lo, &hi);
+            const float factor = pack_piece<kF16>(x, &lo, &hi);
             if (i < a.Hq) {
                 const int head = i >> a.g_log2, row = (b << a.g_log2) + (i & (a.G - 1));
                 const long long tile = (static_cast<long long>(s) * a.Hkv + head) * ta.nqt + (row >> 7);
                 uint4* d = ta.qr + tile * (16 * kRows) + (row & 127);
                 d[p * kRows] = lo;
                 d[(8 + p) * kRows] = hi;
-                if (!kFp8) {
+                if (!kF16) {
                     // with one bf16 term the queries' rounding alone would move the output as
                     // much as its own rounding does
                     const Piece y = unpack_piece(lo, hi);
@@ -285,7 +289,7 @@ __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_c
                     d[p * kRows] = lo;
                     d[(8 + p) * kRows] = hi;
                 }
-                if (kFp8 && p == 0) ta.q_scale[tile * kRows + (row & 127)] = factor * a.sl2;
+                if (kF16 && p == 0) ta.q_scale[tile * kRows + (row & 127)] = factor * a.sl2;
             } else if (i < rows) {
                 const int kv = i >= a.Hq + a.Hkv, head = i - a.Hq - kv * a.Hkv;
                 put_side(kv, head, tail + b, lo, hi);
@@ -302,12 +306,13 @@ __device__ __forceinline__ float above(float x) {
     return __uint_as_float((min(max(__float_as_uint(x) >> 23, 27u), 252u) + 1u) << 23);
 }
 
-// ------------------------------------------------------------ e4m3 pages as f16 tiles
+// ------------------------------------------------------------ e4m3 or e2m1 pages as f16 tiles
 
 // One block per tile of a sequence and kv head (whole cache tiles, then side
-// tiles): codes times their key's scale over a power of two that the tile's
-// keys (and, apart, values) have in common, rounded once to f16.  Converting in
-// the tiles kernel costs 0.8 us a tile of every unit, and this 2 us a tile once.
+// tiles): codes times their key's scale (e2m1: and block scale) over a power of two
+// that the tile's keys (and, apart, values) have in common, rounded once to f16.
+// Converting in the tiles kernel costs 0.8 us a tile of every unit, and this 2 us a tile once.
+template <int kType>
 __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant__ TileArgs ta, const uint8_t* pool_k, const uint8_t* pool_v) {
     __shared__ float scale_of[2 * kKeys];
     __shared__ int row_of[kKeys];  // of the pool; -1: no such page
@@ -332,13 +337,20 @@ __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant_
     // groups of 8 lanes a row, 16 elements a lane: on their way while the scales are compared
     const int p = tid & 7, group = tid >> 3;
     constexpr int kRounds = 2 * kKeys / 32;
-    uint4 c[kRounds];
+    uint4 c[kRounds];  // (e2m1: two words, and the block scale)
     if (cache_tile)
 #pragma unroll
         for (int i = 0; i < kRounds; i++) {
             const int row = row_of[(i * 32 + group) & 127];
             c[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (row >= 0) c[i] = ld_plain(reinterpret_cast<const uint4*>(i >= kRounds / 2 ? pool_v : pool_k) + static_cast<long long>(row) * 8 + p);
+            if (row < 0) continue;
+            const uint8_t* pool = i >= kRounds / 2 ? pool_v : pool_k;
+            if (kType == DART_KV_E2M1) {
+                const uint2 x = ld_plain(reinterpret_cast<const uint2*>(pool) + static_cast<long long>(row) * 8 + p);
+                c[i] = make_uint4(x.x, x.y, ld_plain((i >= kRounds / 2 ? a.vb : a.kb) + static_cast<long long>(row) * kBlocks + p), 0u);
+            } else {
+                c[i] = ld_plain(reinterpret_cast<const uint4*>(pool) + static_cast<long long>(row) * 8 + p);
+            }
         }
     {
         const int kv = tid >> 7, key = tid & 127;
@@ -360,14 +372,25 @@ __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant_
 #pragma unroll
     for (int i = 0; i < kRounds; i++) {
         const int kv = i >= kRounds / 2, key = (i * 32 + group) & 127;
-        const __half2 by = __float2half2_rn(scale_of[kv * kKeys + key] * __uint_as_float(0x7F000000u - __float_as_uint(ref[kv])));
+        float factor = scale_of[kv * kKeys + key] * __uint_as_float(0x7F000000u - __float_as_uint(ref[kv]));
         uint32_t x[8];
-        if (cache_tile) {
+        if (cache_tile && kType == DART_KV_E2M1) {
+            const uint32_t block = e4m3_f16(c[i].z);
+            factor *= __low2float(*reinterpret_cast<const __half2*>(&block));
+            uint32_t lo[4], hi[4];
+            e2m1_f16(c[i].x, lo);
+            e2m1_f16(c[i].y, hi);
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                x[e] = lo[e];
+                x[4 + e] = hi[e];
+            }
+        } else if (cache_tile) {
             const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
 #pragma unroll
             for (int e = 0; e < 4; e++) {
-                x[2 * e] = codes_to_f16(w[e]);
-                x[2 * e + 1] = codes_to_f16(w[e] >> 16);
+                x[2 * e] = e4m3_f16(w[e]);
+                x[2 * e + 1] = e4m3_f16(w[e] >> 16);
             }
         } else {
             const uint4* src = (kv ? ta.side_v : ta.side_k) + (side >> 7) * (16 * kKeys) + key;
@@ -381,6 +404,7 @@ __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant_
             x[6] = z.z;
             x[7] = z.w;
         }
+        const __half2 by = __float2half2_rn(factor);
 #pragma unroll
         for (int e = 0; e < 8; e++) {
             const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&x[e]), by);
@@ -553,19 +577,21 @@ __device__ __forceinline__ void mma_pv(uint32_t d, uint32_t p, uint32_t v_lo, ui
 
 template <Source kSource>
 struct TGeo {
-    static constexpr bool kConv = kSource == kCodes;
+    static constexpr bool kConv = kSource == kCodes || kSource == kCodes4, kFour = kSource == kCodes4;
     // Three operand tiles of K and of V; converted ones two of each, and raw tiles of
     // half the size before them.
     static constexpr int kStages = kConv ? 2 : 3;
     static constexpr int kRawK = kConv ? 3 : 0, kRawV = kConv ? 2 : 0;
     static constexpr int kRing = 4;  // a tile's factors outlive its operands
     static constexpr int kOps = 2 * kStages * kTile;
-    static constexpr int kRaw = (kRawK + kRawV) * kHalf;
-    static constexpr int kRawScales = (kRawK + kRawV) * kKeys * 4;
+    static constexpr int kRawTile = kFour ? kHalf / 2 : kHalf;
+    static constexpr int kRaw = (kRawK + kRawV) * kRawTile;
+    static constexpr int kRawScale = kFour ? 4 + kBlocks : 4;  // bytes of a key
+    static constexpr int kRawScales = (kRawK + kRawV) * kKeys * kRawScale;
     static constexpr int kBars = 4 * kStages + 2 * (kRawK + kRawV) + (kConv ? kRing : 0) + 9;
     static constexpr int kExchange = 4 * kRows * 4 + 16 * 4 + kRing * 8 + kRing * 4 * 4;
     static constexpr int kSmem = kOps + kRaw + kRawScales + kBars * 8 + kExchange + 16;
-    // kCodes: warpgroups (producer, MMA, two idle warps), softmax, softmax, converters
+    // kConv: warpgroups (producer, MMA, two idle warps), softmax, softmax, converters
     static constexpr int kThreads = kConv ? 512 : 64 + kSoft;
     static constexpr int kFirstSoft = kConv ? 4 : 2;
 };
@@ -618,7 +644,8 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                        const __grid_constant__ CUtensorMap tmSk, const __grid_constant__ CUtensorMap tmSv,
                        const __grid_constant__ TileArgs ta) {
     using G_ = TGeo<kSource>;
-    constexpr bool kConv = kSource == kCodes;  // converting warps
+    constexpr bool kConv = G_::kConv;          // converting warps
+    constexpr bool kFour = G_::kFour;
     constexpr bool kF16 = kSource != kPages;   // f16 operands, with a factor per row of Q and per tile of K and V
     constexpr int kStages = G_::kStages;
     const PagedArgs& a = ta.p;
@@ -626,9 +653,10 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
     uint8_t* sK = tiles_smem;
     uint8_t* sV = sK + kStages * kTile;
     uint8_t* rK = sV + kStages * kTile;  // raw tiles
-    uint8_t* rV = rK + G_::kRawK * kHalf;
-    float* raw_scales = reinterpret_cast<float*>(rV + G_::kRawV * kHalf);  // [raw K stages, raw V stages][key]
-    uint64_t* k_full = reinterpret_cast<uint64_t*>(raw_scales + (G_::kRawK + G_::kRawV) * kKeys);
+    uint8_t* rV = rK + G_::kRawK * G_::kRawTile;
+    float* raw_scales = reinterpret_cast<float*>(rV + G_::kRawV * G_::kRawTile);  // [raw K stages, raw V stages][key]
+    uint8_t* raw_blocks = reinterpret_cast<uint8_t*>(raw_scales + (G_::kRawK + G_::kRawV) * kKeys);  // [the same][key][8]
+    uint64_t* k_full = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(raw_scales) + G_::kRawScales);
     uint64_t* k_empty = k_full + kStages;   // S of the tile done
     uint64_t* v_full = k_empty + kStages;
     uint64_t* v_empty = v_full + kStages;   // PV of the tile done
@@ -750,24 +778,26 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                     const int st = n % stages;
                     uint64_t* full = (kConv ? (kv ? rv_full : rk_full) : (kv ? v_full : k_full)) + st;
                     uint64_t* empty = (kConv ? (kv ? rv_empty : rk_empty) : (kv ? v_empty : k_empty)) + st;
-                    uint8_t* dst = kConv ? (kv ? rV : rK) + st * kHalf : (kv ? sV : sK) + st * kTile;
+                    uint8_t* dst = kConv ? (kv ? rV : rK) + st * G_::kRawTile : (kv ? sV : sK) + st * kTile;
                     const CUtensorMap* tm = cache_tile ? (kv ? &tmV : &tmK) : (kv ? &tmSv : &tmSk);
                     ok = warp_wait<kWaitPolls>(empty, (static_cast<uint32_t>(n / stages) & 1u) ^ 1u, abort);
                     if (!ok) break;
                     k_ahead = kv == 0;
                     if (lane == 0)
-                        mbar_arrive_expect_tx(full, kConv ? kHalf + kKeys * 4 : kTile);
+                        mbar_arrive_expect_tx(full, kConv ? G_::kRawTile + kKeys * G_::kRawScale : kTile);
                     __syncwarp();
                     if (!cache_tile) {
                         if (lane < 2)
                             tma_load_2d(dst + lane * kHalf, tm, full, 64 * lane, laid_row, policy);
                     } else if (lane < per_tile) {
-                        const uint32_t at = static_cast<uint32_t>(lane << a.page_log2) * 128;
+                        const uint32_t at = static_cast<uint32_t>(lane << a.page_log2) * (kFour ? 64 : 128);
                         tma_load_2d(dst + at, tm, full, 0, static_cast<int>(row), policy);
                         if (!kConv) tma_load_2d(dst + kHalf + at, tm, full, 64, static_cast<int>(row), policy);
                         if (kConv) {
                             const long long sr = row < a.pool_rows ? row : 0;
-                            bulk_load(raw_scales + (kv * G_::kRawK + st) * kKeys + (lane << a.page_log2), (kv ? a.vs : a.ks) + sr, 4u << a.page_log2, full);
+                            const int first = (kv * G_::kRawK + st) * kKeys + (lane << a.page_log2);
+                            bulk_load(raw_scales + first, (kv ? a.vs : a.ks) + sr, 4u << a.page_log2, full);
+                            if (kFour) bulk_load(raw_blocks + first * kBlocks, (kv ? a.vb : a.kb) + sr * kBlocks, static_cast<uint32_t>(kBlocks) << a.page_log2, full);
                         }
                     }
                 }
@@ -1119,17 +1149,36 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                     const int row = key + 64 * h;
                     uint8_t* dst = op_tile + st * kTile;
                     uint4 x[8];
-                    if (cache_tile) {
-                        const uint8_t* src = raw_tile + rs * kHalf;
+                    if (kFour && cache_tile) {
+                        // codes times (block scale * scale over the common power of two), rounded to f16:
+                        // exact where the scale is a power of two, as the cache writes leave it
+                        const uint8_t* src = raw_tile + rs * G_::kRawTile;
+                        const uint2 bl = *reinterpret_cast<const uint2*>(raw_blocks + ((kv * G_::kRawK + rs) * kKeys + row) * kBlocks);
+#pragma unroll
+                        for (int c = 0; c < 4; c++) x[c] = *reinterpret_cast<const uint4*>(src + swz64(row, c));
+#pragma unroll
+                        for (int c = 0; c < 8; c++) {  // block c: 32 bytes
+                            const uint32_t wide = e4m3_f16((c < 4 ? bl.x : bl.y) >> (8 * (c & 3)));
+                            const __half2 of = __float2half2_rn(__low2float(*reinterpret_cast<const __half2*>(&wide)) * (sc[h] * inv));
+                            const uint32_t f = *reinterpret_cast<const uint32_t*>(&of);
+                            uint32_t lo[4], hi[4];
+                            e2m1_f16(c & 1 ? x[c >> 1].z : x[c >> 1].x, lo);
+                            e2m1_f16(c & 1 ? x[c >> 1].w : x[c >> 1].y, hi);
+                            uint8_t* d = dst + (c >> 2) * kHalf;
+                            *reinterpret_cast<uint4*>(d + tile_swz(row, (2 * c) & 7)) = make_uint4(mul_f16x2(lo[0], f), mul_f16x2(lo[1], f), mul_f16x2(lo[2], f), mul_f16x2(lo[3], f));
+                            *reinterpret_cast<uint4*>(d + tile_swz(row, (2 * c + 1) & 7)) = make_uint4(mul_f16x2(hi[0], f), mul_f16x2(hi[1], f), mul_f16x2(hi[2], f), mul_f16x2(hi[3], f));
+                        }
+                    } else if (cache_tile) {
+                        const uint8_t* src = raw_tile + rs * G_::kRawTile;
 #pragma unroll
                         for (int c = 0; c < 8; c++) x[c] = *reinterpret_cast<const uint4*>(src + tile_swz(row, c));
 #pragma unroll
                         for (int c = 0; c < 8; c++) {
                             uint8_t* d = dst + (c >> 2) * kHalf;
                             *reinterpret_cast<uint4*>(d + tile_swz(row, (2 * c) & 7)) =
-                                make_uint4(times(codes_to_f16(x[c].x)), times(codes_to_f16(x[c].x >> 16)), times(codes_to_f16(x[c].y)), times(codes_to_f16(x[c].y >> 16)));
+                                make_uint4(times(e4m3_f16(x[c].x)), times(e4m3_f16(x[c].x >> 16)), times(e4m3_f16(x[c].y)), times(e4m3_f16(x[c].y >> 16)));
                             *reinterpret_cast<uint4*>(d + tile_swz(row, (2 * c + 1) & 7)) =
-                                make_uint4(times(codes_to_f16(x[c].z)), times(codes_to_f16(x[c].z >> 16)), times(codes_to_f16(x[c].w)), times(codes_to_f16(x[c].w >> 16)));
+                                make_uint4(times(e4m3_f16(x[c].z)), times(e4m3_f16(x[c].z >> 16)), times(e4m3_f16(x[c].w)), times(e4m3_f16(x[c].w >> 16)));
                         }
                     } else {
                         const uint4* src = side_rows + (side >> 7) * (16 * kKeys) + row;
@@ -1245,7 +1294,7 @@ TileWs tile_ws(int nseq, int B, int Hq, const dart_kv_cache& cache, int max_page
     w.wk = w.vs + up(heads * w.sk * 4);
     const long long tiles = static_cast<long long>(max_pages) * cache.page_size / kKeys + w.sk / kKeys;
     const size_t each = heads * tiles * kTile;
-    if (cache.dtype == DART_KV_E4M3 && w.nqt >= kWidenTiles && each <= kWidenBytes / 2 && tiles <= 65535) w.wide_tiles = static_cast<int>(tiles);
+    if (cache.dtype != DART_KV_BF16 && w.nqt >= kWidenTiles && each <= kWidenBytes / 2 && tiles <= 65535) w.wide_tiles = static_cast<int>(tiles);
     const size_t wide = w.wide_tiles ? each : 0;
     w.wv = w.wk + wide;
     w.refs = w.wv + wide;
@@ -1263,7 +1312,7 @@ template <Source kSource>
 static bool allow_smem() {
     return cudaFuncSetAttribute(paged_tiles_kernel<kSource>, cudaFuncAttributeMaxDynamicSharedMemorySize, TGeo<kSource>::kSmem) == cudaSuccess;
 }
-bool paged_tiles_prepare_device() { return allow_smem<kPages>() && allow_smem<kCodes>() && allow_smem<kWidened>(); }
+bool paged_tiles_prepare_device() { return allow_smem<kPages>() && allow_smem<kCodes>() && allow_smem<kCodes4>() && allow_smem<kWidened>(); }
 
 template <Source kSource>
 static cudaError_t launch_tiles(int sms, cudaStream_t st, const CUtensorMap& k, const CUtensorMap& v, const CUtensorMap& side_k,
@@ -1272,7 +1321,7 @@ static cudaError_t launch_tiles(int sms, cudaStream_t st, const CUtensorMap& k, 
 }
 
 int launch_paged_tiles(PagedArgs a, const dart_kv_cache& cache, uint8_t* workspace, int sms, cudaStream_t st) {
-    const bool fp8 = cache.dtype == DART_KV_E4M3;
+    const bool e4m3 = cache.dtype == DART_KV_E4M3, e2m1 = cache.dtype == DART_KV_E2M1;
     const TileWs w = tile_ws(a.nseq, a.B, a.Hq, cache, a.max_pages);
     const bool wide = w.wide_tiles > 0;
     TileArgs ta{};
@@ -1293,9 +1342,9 @@ int launch_paged_tiles(PagedArgs a, const dart_kv_cache& cache, uint8_t* workspa
     const long long heads = static_cast<long long>(a.nseq) * a.Hkv, side_rows = heads * w.sk;
     CUtensorMap tmK, tmV, tmSk, tmSv;
     // f16 tiles are 16-bit rows to the copies, as bf16 rows are
-    const bool maps = wide ? encode_rows(&tmK, ta.wide_k, heads * w.wide_tiles * kKeys, false, kKeys) && encode_rows(&tmV, ta.wide_v, heads * w.wide_tiles * kKeys, false, kKeys)
-                           : encode_rows(&tmK, cache.k, a.pool_rows, fp8, cache.page_size) && encode_rows(&tmV, cache.v, a.pool_rows, fp8, cache.page_size) &&
-                                 encode_rows(&tmSk, ta.side_k, side_rows, false, kKeys) && encode_rows(&tmSv, ta.side_v, side_rows, false, kKeys);
+    const bool maps = wide ? encode_rows(&tmK, ta.wide_k, heads * w.wide_tiles * kKeys, DART_KV_BF16, kKeys) && encode_rows(&tmV, ta.wide_v, heads * w.wide_tiles * kKeys, DART_KV_BF16, kKeys)
+                           : encode_rows(&tmK, cache.k, a.pool_rows, cache.dtype, cache.page_size) && encode_rows(&tmV, cache.v, a.pool_rows, cache.dtype, cache.page_size) &&
+                                 encode_rows(&tmSk, ta.side_k, side_rows, DART_KV_BF16, kKeys) && encode_rows(&tmSv, ta.side_v, side_rows, DART_KV_BF16, kKeys);
     if (!maps) return DART_ERR_CUDA;
     if (wide) {
         tmSk = tmK;  // (side tiles lie among the others)
@@ -1304,13 +1353,17 @@ int launch_paged_tiles(PagedArgs a, const dart_kv_cache& cache, uint8_t* workspa
     // tree rows, up to 127 cache tokens before them, up to 127 rows of zeros after them
     const dim3 prep(static_cast<unsigned>(a.nseq), static_cast<unsigned>(a.B + 1 + 2 * (kKeys - 1)));
     const uint8_t *pk = static_cast<const uint8_t*>(cache.k), *pv = static_cast<const uint8_t*>(cache.v);
-    cudaError_t e = fp8 ? launch_pdl(paged_prep_kernel<true>, prep, dim3(kPrepThreads), 0, st, ta, pk, pv)
-                        : launch_pdl(paged_prep_kernel<false>, prep, dim3(kPrepThreads), 0, st, ta, pk, pv);
+    const dim3 pb(kPrepThreads), wg(static_cast<unsigned>(heads), static_cast<unsigned>(w.wide_tiles)), wb(256);
+    cudaError_t e = e2m1   ? launch_pdl(paged_prep_kernel<DART_KV_E2M1>, prep, pb, 0, st, ta, pk, pv)
+                    : e4m3 ? launch_pdl(paged_prep_kernel<DART_KV_E4M3>, prep, pb, 0, st, ta, pk, pv)
+                           : launch_pdl(paged_prep_kernel<DART_KV_BF16>, prep, pb, 0, st, ta, pk, pv);
     if (e == cudaSuccess && wide)
-        e = launch_pdl(paged_widen_kernel, dim3(static_cast<unsigned>(heads), static_cast<unsigned>(w.wide_tiles)), dim3(256), 0, st, ta, pk, pv);
+        e = e2m1 ? launch_pdl(paged_widen_kernel<DART_KV_E2M1>, wg, wb, 0, st, ta, pk, pv) : launch_pdl(paged_widen_kernel<DART_KV_E4M3>, wg, wb, 0, st, ta, pk, pv);
     if (e == cudaSuccess)
-        e = wide ? launch_tiles<kWidened>(sms, st, tmK, tmV, tmSk, tmSv, ta)
-                 : fp8 ? launch_tiles<kCodes>(sms, st, tmK, tmV, tmSk, tmSv, ta) : launch_tiles<kPages>(sms, st, tmK, tmV, tmSk, tmSv, ta);
+        e = wide   ? launch_tiles<kWidened>(sms, st, tmK, tmV, tmSk, tmSv, ta)
+            : e2m1 ? launch_tiles<kCodes4>(sms, st, tmK, tmV, tmSk, tmSv, ta)
+            : e4m3 ? launch_tiles<kCodes>(sms, st, tmK, tmV, tmSk, tmSv, ta)
+                   : launch_tiles<kPages>(sms, st, tmK, tmV, tmSk, tmSv, ta);
     if (e == cudaSuccess) e = launch_pdl(paged_tiles_join_kernel, dim3(8 * (sms - 1)), dim3(256), 0, st, a);
     return e == cudaSuccess ? DART_OK : DART_ERR_CUDA;
 }

@@ -25,7 +25,7 @@ DART_ERR_UNSUPPORTED = -6
 DART_ERR_BOUNDS = -7
 DART_F32 = 0
 DART_BF16 = 1
-DART_KV_BF16, DART_KV_E4M3 = 0, 1
+DART_KV_BF16, DART_KV_E4M3, DART_KV_E2M1 = 0, 1, 2
 DART_AUTO, DART_ON, DART_OFF = 0, 1, 2
 DART_VARIANT_CHAIN_DDTREE = 1
 DART_VARIANT_SEQ_HEAP = 2
@@ -53,7 +53,8 @@ class DartAttnConfig(C.Structure):
 
 class DartKvCache(C.Structure):
     _fields_ = [("num_pages", C.c_int), ("page_size", C.c_int), ("Hkv", C.c_int), ("dh", C.c_int), ("dtype", C.c_int),
-                ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+                ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("k_block", C.c_void_p), ("v_block", C.c_void_p)]
 
 
 class DartPagedAttnConfig(C.Structure):
@@ -124,6 +125,7 @@ def lib():
             "dart_tree_attention_tiles": (i, [C.POINTER(DartAttnConfig), i]),
             "dart_ancestor_mask": (i, [vp, vp, i, i, vp, vp]),
             "dart_cache_append": (i, [C.POINTER(DartKvCache), i, i, vp, vp, i, vp, i64, vp, i64, vp, vp, f, vp, vp]),
+            "dart_cache_read": (i, [C.POINTER(DartKvCache), i, i, vp, vp, i, vp, i64, vp, i64, vp, vp, vp]),
             "dart_paged_attention_workspace": (C.c_size_t, [C.POINTER(DartPagedAttnConfig), C.POINTER(DartKvCache)]),
             "dart_paged_attention": (i, [C.POINTER(DartPagedAttnConfig), C.POINTER(DartKvCache), vp, vp, vp, i64, vp, i64, vp,
                                          i64, vp, vp, vp, vp, vp, C.c_size_t, vp, vp]),
@@ -520,32 +522,46 @@ def _status(t, dev):
     return t.data_ptr()
 
 
+_KV_TYPES = {torch.bfloat16: DART_KV_BF16, torch.float8_e4m3fn: DART_KV_E4M3, torch.float4_e2m1fn_x2: DART_KV_E2M1}
+
+
 class KVCache:
     """Pages of keys and values: k, v [num_pages, Hkv, page_size, 128] bfloat16,
-    or float8_e4m3fn with fp32 scales [num_pages, Hkv, page_size]."""
+    or float8_e4m3fn with fp32 scales [num_pages, Hkv, page_size], or
+    float4_e2m1fn_x2 [num_pages, Hkv, page_size, 64] with such scales and block
+    scales [num_pages, Hkv, page_size, 8] float8_e4m3fn."""
 
-    def __init__(self, k, v, k_scale=None, v_scale=None):
-        if k.dim() != 4 or k.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
-            raise ValueError("k: [num_pages, Hkv, page_size, dh] bfloat16 or float8_e4m3fn expected")
+    def __init__(self, k, v, k_scale=None, v_scale=None, k_block=None, v_block=None):
+        if k.dim() != 4 or k.dtype not in _KV_TYPES:
+            raise ValueError("k: [num_pages, Hkv, page_size, dh] bfloat16, float8_e4m3fn or float4_e2m1fn_x2 expected")
         n, heads, page, dh = k.shape
-        fp8 = k.dtype == torch.float8_e4m3fn
-        if fp8 != (k_scale is not None) or fp8 != (v_scale is not None):
-            raise ValueError("scales belong to float8_e4m3fn pages, and to those alone")
+        kind = _KV_TYPES[k.dtype]
+        coded, four = kind != DART_KV_BF16, kind == DART_KV_E2M1
+        if coded != (k_scale is not None) or coded != (v_scale is not None):
+            raise ValueError("scales belong to float8_e4m3fn and float4_e2m1fn_x2 pages, and to those alone")
+        if four != (k_block is not None) or four != (v_block is not None):
+            raise ValueError("block scales belong to float4_e2m1fn_x2 pages, and to those alone")
         dev = torch.cuda.current_device()
         ptr = [_expect(k, "k", k.dtype, k.shape, dev), _expect(v, "v", k.dtype, k.shape, dev)]
-        ptr += [_expect(x, m, torch.float32, (n, heads, page), dev) if fp8 else None
+        ptr += [_expect(x, m, torch.float32, (n, heads, page), dev) if coded else None
                 for x, m in ((k_scale, "k_scale"), (v_scale, "v_scale"))]
-        self.k, self.v, self.k_scale, self.v_scale, self.dev = k, v, k_scale, v_scale, dev
-        self.num_pages, self.Hkv, self.page_size, self.dh = n, heads, page, dh
-        self.c = DartKvCache(n, page, heads, dh, DART_KV_E4M3 if fp8 else DART_KV_BF16, *ptr)
+        ptr += [_expect(x, m, torch.float8_e4m3fn, (n, heads, page, dh // 8), dev) if four else None
+                for x, m in ((k_block, "k_block"), (v_block, "v_block"))]
+        self.k, self.v, self.k_scale, self.v_scale, self.k_block, self.v_block = k, v, k_scale, v_scale, k_block, v_block
+        self.dev, self.num_pages, self.Hkv, self.page_size, self.dh = dev, n, heads, page, dh * 2 if four else dh
+        self.c = DartKvCache(n, page, heads, self.dh, kind, *ptr)
         self.ref = C.byref(self.c)
 
     @classmethod
     def new(cls, num_pages, page_size, Hkv, dh=128, dtype=torch.bfloat16):
         """An empty pool on the current device."""
-        shape, kw = (num_pages, Hkv, page_size, dh), dict(device="cuda")
-        scales = [torch.zeros(shape[:3], **kw) for _ in range(2)] if dtype == torch.float8_e4m3fn else []
-        return cls(torch.zeros(shape, dtype=dtype, **kw), torch.zeros(shape, dtype=dtype, **kw), *scales)
+        shape, kw = (num_pages, Hkv, page_size), dict(device="cuda")
+        if dtype == torch.float4_e2m1fn_x2:
+            k, v = (torch.zeros(shape + (dh // 2,), dtype=torch.uint8, **kw).view(dtype) for _ in range(2))
+            blocks = [torch.zeros(shape + (dh // 16,), dtype=torch.float8_e4m3fn, **kw) for _ in range(2)]
+            return cls(k, v, *(torch.zeros(shape, **kw) for _ in range(2)), *blocks)
+        scales = [torch.zeros(shape, **kw) for _ in range(2)] if dtype == torch.float8_e4m3fn else []
+        return cls(*(torch.zeros(shape + (dh,), dtype=dtype, **kw) for _ in range(2)), *scales)
 
     def append(self, k, v, page_table, lens, n_rows, rows=None, rope_theta=1.0e6, status=None, stream=None):
         """Writes n_rows[s] tokens of every sequence from position lens[s] on:
@@ -562,6 +578,21 @@ class KVCache:
             _expect(lens, "lens", torch.int32, (nseq,), dev), R, kp, ks, vp, vs,
             None if rows is None else _expect(rows, "rows", torch.int32, (nseq, R), dev),
             _expect(n_rows, "n_rows", torch.int32, (nseq,), dev), rope_theta, _status(status, dev), st), "dart_cache_append")
+
+    def read(self, k, v, page_table, lens, n_rows, status=None, stream=None):
+        """Writes tokens lens[s] .. lens[s] + n_rows[s] - 1 of every sequence
+        into the first rows of k and v [nseq, R, Hkv, dh] bf16, K as it is
+        stored (rotated).  Rows behind n_rows[s] stay as they are."""
+        dev, st = _current(stream, self.dev)
+        nseq, R = k.shape[:2]
+        shape = (nseq, R, self.Hkv, self.dh)
+        kp, ks = _rows(k, "k", shape, dev)
+        vp, vs = _rows(v, "v", shape, dev)
+        pages = page_table.shape[-1]
+        _check(lib().dart_cache_read(
+            self.ref, nseq, pages, _expect(page_table, "page_table", torch.int32, (nseq, pages), dev),
+            _expect(lens, "lens", torch.int32, (nseq,), dev), R, kp, ks, vp, vs,
+            _expect(n_rows, "n_rows", torch.int32, (nseq,), dev), _status(status, dev), st), "dart_cache_read")
 
 
 class PagedTreeAttention:
