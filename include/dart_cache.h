@@ -98,6 +98,78 @@ int dart_cache_read(const dart_kv_cache *cache, int nseq, int max_pages, const i
                     const int32_t *lens, int R, void *k, int64_t k_stride, void *v, int64_t v_stride,
                     const int32_t *n_rows, int *status, void *stream);
 
+/* Copies whole pages, keys and values with their scales: the first *count
+ * (clamped to [0, max_pairs]) pairs (from, to) of pairs [max_pairs][2], as
+ * dart_page_pool_reserve and dart_page_pool_compact leave them.  No page may be
+ * the `to` of two pairs, or the `to` of one and the `from` of another.  A pair
+ * with a page outside [0, num_pages) is skipped and sets value 4 in *status. */
+int dart_cache_copy_pages(const dart_kv_cache *cache, const int32_t *pairs, int max_pairs, const int32_t *count,
+                          int *status, void *stream);
+
+/* ---- who holds which page --------------------------------------------------
+ *
+ * The pages of a cache (or of several that share a table, one for each layer)
+ * and the sequences that hold them; sequences may share pages.  All of it is
+ * device memory, so that the calls need no host step and can be captured:
+ *   refs  [num_pages]         sequences that hold each page; 0: a free page
+ *   table [nseq][max_pages]   the page tables: entries [0, held[s]) of row s are
+ *                             pages, what stands behind them is not looked at
+ *   held  [nseq]              pages of each sequence
+ * A fresh pool is all zeros.  page_table of the other calls is `table`, lens
+ * are the caller's.  Held counts are clamped to [0, max_pages], lengths to [0,
+ * max_pages * page_size].  A table entry that should be a page and lies outside
+ * [0, num_pages) sets value 4 in *status and counts for nothing.  Results do not
+ * depend on the order in which threads run.  One call at a time works on a
+ * pool: calls on different streams have to be ordered by events.
+ * `workspace`: dart_page_pool_workspace bytes, 256-byte aligned, in use until
+ * the stream reaches the call's end; nothing is kept in it between calls. */
+typedef struct {
+    int num_pages; /* >= 1 */
+    int page_size; /* tokens per page: 16, 32, 64 or 128 */
+    int nseq;      /* sequences, >= 1 */
+    int max_pages; /* row length of table, >= 1; nseq * max_pages and max_pages * page_size <= 2^30 */
+    int32_t *refs; /* 16-byte aligned */
+    int32_t *table;
+    int32_t *held;
+} dart_page_pool;
+
+size_t dart_page_pool_workspace(const dart_page_pool *pool); /* 0: invalid */
+
+/* Sequences become continuations of others, all at once from the state before
+ * the call: parents[s] = s leaves sequence s as it is; p != s makes it a copy of
+ * sequence p (it gives its pages back and holds the first ceil(lens[p] /
+ * page_size) of p's instead, lens[s] = lens[p]); -1 ends it (it gives its
+ * pages back, lens[s] = 0).  Any other value leaves s as it is and sets value
+ * 4 in *status.  lens [nseq] is changed in place. */
+int dart_page_pool_select(const dart_page_pool *pool, const int32_t *parents, int32_t *lens, void *workspace,
+                          size_t workspace_bytes, int *status, void *stream);
+
+/* Room for n_rows[s] more tokens from position lens[s] on, on pages that no
+ * other sequence holds: of the pages that these tokens fall on, the ones that
+ * sequence s does not have yet or shares are replaced by free ones, lowest
+ * numbers first in the order of sequences and then positions.  Where a shared
+ * page has tokens before lens[s], the pair (it, its replacement) is listed in
+ * pairs [max_pairs][2] (max_pairs >= nseq), in the order of sequences, for
+ * dart_cache_copy_pages, which has to come before the pages' next use; *count is
+ * their number.  Two sequences that share a page and are both given room in it
+ * get a copy each.  A sequence that the table's row or the free pages do not
+ * suffice for (and, for the free pages, every later one that needs some) is
+ * left as it is and sets value 8 in *status.  n_rows[s] <= 0 asks for nothing. */
+int dart_page_pool_reserve(const dart_page_pool *pool, const int32_t *lens, const int32_t *n_rows, int32_t *pairs,
+                           int max_pairs, int32_t *count, void *workspace, size_t workspace_bytes, int *status,
+                           void *stream);
+
+/* Gives back every page behind the first ceil(lens[s] / page_size) of sequence s. */
+int dart_page_pool_trim(const dart_page_pool *pool, const int32_t *lens, int *status, void *stream);
+
+/* Moves the pages in use to the front: with n of them, those with numbers >= n
+ * go to the free numbers below n, both in ascending order; refs and table
+ * follow, and pairs [max_pairs][2] (max_pairs >= num_pages / 2), *count list
+ * the moves for dart_cache_copy_pages, which has to come before the pages'
+ * next use. */
+int dart_page_pool_compact(const dart_page_pool *pool, int32_t *pairs, int max_pairs, int32_t *count, void *workspace,
+                           size_t workspace_bytes, int *status, void *stream);
+
 typedef struct {
     int nseq;         /* sequences, >= 1 */
     int B;            /* tree nodes per sequence, 0..1024; R = B + 1 rows */

@@ -361,6 +361,55 @@ __global__ void __launch_bounds__(kAppendThreads) cache_read_kernel(const __grid
     v.store(a.v + token * a.v_stride + head * kHeadDim + kBlockDim * j);
 }
 
+// ------------------------------------------------------------ whole pages
+
+constexpr int kCopyThreads = 256, kCopyVecs = 4;  // 16-byte vectors of a thread on their way at a time
+constexpr int kSlice = kCopyThreads * kCopyVecs;   // vectors of a unit of work, 16 KB
+
+struct CopyArgs {
+    int max_pairs, num_pages, slices;
+    const int2* pairs;
+    const int32_t* count;
+    uint4* base[6];     // pages of keys and values, their scales, their block scales
+    int page_vecs[6];   // 16-byte vectors of a page in each; 0: none
+    int* status;
+};
+
+// A unit is 16 KB of a page's arrays, one after the other, so that a few copies of
+// large pages and many of small ones load every SM alike.
+__global__ void __launch_bounds__(kCopyThreads) cache_copy_kernel(const __grid_constant__ CopyArgs a) {
+    pdl_trigger();
+    pdl_wait();
+    const int n = min(max(ld_plain(a.count), 0), a.max_pairs);
+    const long long units = static_cast<long long>(n) * a.slices;
+    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+        const int pair = static_cast<int>(u / a.slices), slice = static_cast<int>(u - static_cast<long long>(pair) * a.slices);
+        const int2 p = ld_plain(a.pairs + pair);
+        if (p.x < 0 || p.x >= a.num_pages || p.y < 0 || p.y >= a.num_pages) {
+            if (a.status && slice == 0 && threadIdx.x == 0) atomicOr(a.status, kDevBounds);
+            continue;
+        }
+        uint4 x[kCopyVecs];
+        uint4* to[kCopyVecs];
+#pragma unroll
+        for (int e = 0; e < kCopyVecs; e++) {
+            int v = slice * kSlice + e * kCopyThreads + static_cast<int>(threadIdx.x);
+            to[e] = nullptr;
+#pragma unroll
+            for (int i = 0; i < 6; i++) {
+                if (to[e] == nullptr && v < a.page_vecs[i]) {
+                    x[e] = __ldcs(a.base[i] + static_cast<long long>(p.x) * a.page_vecs[i] + v);
+                    to[e] = a.base[i] + static_cast<long long>(p.y) * a.page_vecs[i] + v;
+                }
+                v -= to[e] == nullptr ? a.page_vecs[i] : 0;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < kCopyVecs; e++)
+            if (to[e]) *to[e] = x[e];
+    }
+}
+
 // 0: an sm_103a device is the current one.
 int check_device() {
     int dev = 0, major = 0, minor = 0;
@@ -465,4 +514,33 @@ extern "C" int dart_cache_read(const dart_kv_cache* cache, int nseq, int max_pag
                           : cache->dtype == DART_KV_E4M3 ? launch_pdl(cache_read_kernel<DART_KV_E4M3>, grid, block, 0, st, a)
                                                          : launch_pdl(cache_read_kernel<DART_KV_BF16>, grid, block, 0, st, a);
     return e == cudaSuccess ? DART_OK : DART_ERR_CUDA;
+}
+
+extern "C" int dart_cache_copy_pages(const dart_kv_cache* cache, const int32_t* pairs, int max_pairs, const int32_t* count, int* status,
+                                     void* stream) {
+    if (!valid_cache(cache) || !valid_cache_pointers(cache)) return DART_ERR_INVALID;
+    if (max_pairs < 1 || !aligned(pairs, 8) || !aligned(count, 4) || (status && !aligned(status, 4))) return DART_ERR_INVALID;
+    CopyArgs a{};
+    a.max_pairs = max_pairs;
+    a.num_pages = cache->num_pages;
+    a.pairs = reinterpret_cast<const int2*>(pairs);
+    a.count = count;
+    a.status = status;
+    const int rows = cache->Hkv * cache->page_size;  // (of a page: a multiple of 16)
+    void* const base[6] = {cache->k, cache->v, cache->k_scale, cache->v_scale, cache->k_block, cache->v_block};
+    long long vecs = 0;
+    for (int i = 0; i < 6; i++) {
+        const int bytes = i < 2 ? row_bytes(cache->dtype) : i < 4 ? (cache->dtype == DART_KV_BF16 ? 0 : 4) : cache->dtype == DART_KV_E2M1 ? kBlocks : 0;
+        const long long all = static_cast<long long>(rows) * bytes / 16;
+        a.base[i] = static_cast<uint4*>(base[i]);
+        a.page_vecs[i] = static_cast<int>(all);
+        vecs += all;
+    }
+    if (vecs > 2147483647ll - kSlice) return DART_ERR_INVALID;
+    if (const int rc = check_device()) return rc;
+    a.slices = static_cast<int>((vecs + kSlice - 1) / kSlice);
+    // every SM with as many blocks as it holds, fewer where there cannot be that many units
+    const long long units = static_cast<long long>(max_pairs) * a.slices;
+    const dim3 grid(static_cast<unsigned>(std::min(units, 8ll * 152)));
+    return launch_pdl(cache_copy_kernel, grid, dim3(kCopyThreads), 0, static_cast<cudaStream_t>(stream), a) == cudaSuccess ? DART_OK : DART_ERR_CUDA;
 }

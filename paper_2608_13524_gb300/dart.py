@@ -57,6 +57,11 @@ class DartKvCache(C.Structure):
                 ("k_block", C.c_void_p), ("v_block", C.c_void_p)]
 
 
+class DartPagePool(C.Structure):
+    _fields_ = [("num_pages", C.c_int), ("page_size", C.c_int), ("nseq", C.c_int), ("max_pages", C.c_int),
+                ("refs", C.c_void_p), ("table", C.c_void_p), ("held", C.c_void_p)]
+
+
 class DartPagedAttnConfig(C.Structure):
     _fields_ = [("nseq", C.c_int), ("B", C.c_int), ("max_pages", C.c_int), ("Hq", C.c_int), ("rope_theta", C.c_float),
                 ("scale", C.c_float)]
@@ -126,6 +131,12 @@ def lib():
             "dart_ancestor_mask": (i, [vp, vp, i, i, vp, vp]),
             "dart_cache_append": (i, [C.POINTER(DartKvCache), i, i, vp, vp, i, vp, i64, vp, i64, vp, vp, f, vp, vp]),
             "dart_cache_read": (i, [C.POINTER(DartKvCache), i, i, vp, vp, i, vp, i64, vp, i64, vp, vp, vp]),
+            "dart_cache_copy_pages": (i, [C.POINTER(DartKvCache), vp, i, vp, vp, vp]),
+            "dart_page_pool_workspace": (C.c_size_t, [C.POINTER(DartPagePool)]),
+            "dart_page_pool_select": (i, [C.POINTER(DartPagePool), vp, vp, vp, C.c_size_t, vp, vp]),
+            "dart_page_pool_reserve": (i, [C.POINTER(DartPagePool), vp, vp, vp, i, vp, vp, C.c_size_t, vp, vp]),
+            "dart_page_pool_trim": (i, [C.POINTER(DartPagePool), vp, vp, vp]),
+            "dart_page_pool_compact": (i, [C.POINTER(DartPagePool), vp, i, vp, vp, C.c_size_t, vp, vp]),
             "dart_paged_attention_workspace": (C.c_size_t, [C.POINTER(DartPagedAttnConfig), C.POINTER(DartKvCache)]),
             "dart_paged_attention": (i, [C.POINTER(DartPagedAttnConfig), C.POINTER(DartKvCache), vp, vp, vp, i64, vp, i64, vp,
                                          i64, vp, vp, vp, vp, vp, C.c_size_t, vp, vp]),
@@ -593,6 +604,70 @@ class KVCache:
             self.ref, nseq, pages, _expect(page_table, "page_table", torch.int32, (nseq, pages), dev),
             _expect(lens, "lens", torch.int32, (nseq,), dev), R, kp, ks, vp, vs,
             _expect(n_rows, "n_rows", torch.int32, (nseq,), dev), _status(status, dev), st), "dart_cache_read")
+
+    def copy_pages(self, pairs, count, status=None, stream=None):
+        """Copies pages pairs[i, 0] to pages pairs[i, 1], i < count: what
+        PagePool.reserve and PagePool.compact return."""
+        dev, st = _current(stream, self.dev)
+        n = pairs.shape[0]
+        _check(lib().dart_cache_copy_pages(
+            self.ref, _expect(pairs, "pairs", torch.int32, (n, 2), dev), n, _expect(count, "count", torch.int32, (1,), dev),
+            _status(status, dev), st), "dart_cache_copy_pages")
+
+
+class PagePool:
+    """Which pages sequences hold, pages that several share among them: refs
+    [num_pages], table [nseq, max_pages] (the page_table of KVCache and
+    PagedTreeAttention) and held [nseq], int32, all zero at first; and pairs,
+    count, the copies that the last reserve or compact asks for.  Nothing waits
+    for the host.  `lens` are the caller's."""
+
+    def __init__(self, num_pages, page_size, nseq, max_pages):
+        self.num_pages, self.page_size, self.nseq, self.max_pages = int(num_pages), int(page_size), int(nseq), int(max_pages)
+        c = DartPagePool(self.num_pages, self.page_size, self.nseq, self.max_pages, None, None, None)
+        n = int(lib().dart_page_pool_workspace(C.byref(c)))
+        if n == 0:
+            raise DartError(DART_ERR_INVALID, "dart_page_pool_workspace")
+        i32 = lambda *shape: _empty(shape, dtype=torch.int32, device="cuda")  # noqa: E731
+        self.dev = torch.cuda.current_device()
+        self.refs, self.table, self.held = i32(self.num_pages).zero_(), i32(self.nseq, self.max_pages).zero_(), i32(self.nseq).zero_()
+        self.pairs, self.count = i32(max(self.nseq, self.num_pages // 2), 2).fill_(-1), i32(1).zero_()
+        self.workspace = _empty((n,), dtype=torch.uint8, device="cuda")
+        c.refs, c.table, c.held = self.refs.data_ptr(), self.table.data_ptr(), self.held.data_ptr()
+        self.c, self.ref = c, C.byref(c)
+        self.ws = self.workspace.data_ptr(), n
+
+    def _seq(self, t, name, dev):
+        return _expect(t, name, torch.int32, (self.nseq,), dev)
+
+    def select(self, parents, lens, status=None, stream=None):
+        """Sequence s becomes a continuation of sequence parents[s] (s: stays as
+        it is, -1: ends), all at once; lens follows in place."""
+        dev, st = _current(stream, self.dev)
+        _check(lib().dart_page_pool_select(self.ref, self._seq(parents, "parents", dev), self._seq(lens, "lens", dev), *self.ws,
+                                           _status(status, dev), st), "dart_page_pool_select")
+
+    def reserve(self, lens, n_rows, status=None, stream=None):
+        """Room for n_rows[s] tokens from position lens[s] on, on pages that no
+        other sequence holds.  Returns (pairs, count) for KVCache.copy_pages."""
+        dev, st = _current(stream, self.dev)
+        _check(lib().dart_page_pool_reserve(self.ref, self._seq(lens, "lens", dev), self._seq(n_rows, "n_rows", dev), self.pairs.data_ptr(),
+                                            self.pairs.shape[0], self.count.data_ptr(), *self.ws, _status(status, dev), st),
+               "dart_page_pool_reserve")
+        return self.pairs, self.count
+
+    def trim(self, lens, status=None, stream=None):
+        """Gives back the pages behind lens[s] tokens."""
+        dev, st = _current(stream, self.dev)
+        _check(lib().dart_page_pool_trim(self.ref, self._seq(lens, "lens", dev), _status(status, dev), st), "dart_page_pool_trim")
+
+    def compact(self, status=None, stream=None):
+        """Moves the pages in use to the front.  Returns (pairs, count) for
+        KVCache.copy_pages."""
+        dev, st = _current(stream, self.dev)
+        _check(lib().dart_page_pool_compact(self.ref, self.pairs.data_ptr(), self.pairs.shape[0], self.count.data_ptr(), *self.ws,
+                                            _status(status, dev), st), "dart_page_pool_compact")
+        return self.pairs, self.count
 
 
 class PagedTreeAttention:
