@@ -61,6 +61,12 @@ __device__ __forceinline__ void e2m1_f16(uint32_t word, uint32_t (&x)[4]) {
         : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
         : "r"(word));
 }
+// Elements 4 half .. 4 half + 3 alone.
+__device__ __forceinline__ void e2m1_f16(uint32_t word, int half, uint32_t (&x)[2]) {
+    asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %2;\n cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n}"
+        : "=r"(x[0]), "=r"(x[1])
+        : "r"(half ? word >> 16 : word));
+}
 // Two e4m3 codes as an f16 pair: exact.
 __device__ __forceinline__ uint32_t e4m3_f16(uint32_t two) {
     uint32_t r;

@@ -4,7 +4,7 @@
 // unit of work is the query rows of one kv head of one sequence (a row = a tree
 // row and one of the G query heads that share the kv head) against all keys
 // that the rows may see: the sequence's cache, then its tree rows, in chunks
-// of 16 (bf16) or 32 (e4m3) keys.  The chunks of all units form one list,
+// of 16 (bf16), 32 (e4m3) or 64 (e2m1) keys.  The chunks of all units form one list,
 // which the warps of the GPU share evenly, so that ragged lengths and a single
 // long sequence load every SM alike; lengths are read on the device, so the
 // split is made there.  A warp streams its chunks through a ring of TMA stages
@@ -25,6 +25,10 @@
 // 6.0 TB/s, 88 %, where the conversions (64 codes a thread and chunk) come
 // second; a call of a few keys takes 12 us, a chain of two launches and six or
 // seven dependent loads.  With rows along the 16 and 8 warps e4m3 took 116 us.
+// e2m1 pages 80 us (4.1 TB/s, 60 %): 331 instructions per 16 keys, half of them the
+// conversions and the products with block scales, issue 56 % active with 2.75 warps a
+// scheduler, DRAM 52 %.  Larger chunks pay the copies' issue (six a chunk) less often and
+// give the scores' products four chains instead of two: 91 us with chunks of 32 keys.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -69,7 +73,10 @@ struct Part {  // a unit's partial result
 // Warps of a CTA: as many as their registers allow (for up to 8 rows 168 a
 // thread; 10 warps: e4m3 93 us instead of 95, pages of 16 tokens 99 instead of
 // 96; for up to 16 rows 6 warps instead of 8: 76 us instead of 65).
-__host__ __device__ constexpr int rows_warps(int n) { return n == 1 ? 12 : 8; }
+// e2m1, up to 8 rows: 11, as many as shared memory holds two chunks of 64 keys for (64
+// sequences of up to 8192 keys, one token each: 9 warps 94 us, 10 85, 11 80; chunks of 32
+// keys with 12 warps 91, 14 95, 16 86).
+__host__ __device__ constexpr int rows_warps(int type, int n) { return n > 1 ? 8 : type == DART_KV_E2M1 ? 11 : 12; }
 
 // ------------------------------------------------------------ the schedule
 
@@ -78,25 +85,26 @@ __host__ __device__ constexpr int rows_warps(int n) { return n == 1 ? 12 : 8; }
 // many short units get fewer of them.  kTokenCost: without a tree (256 sequences of
 // up to 1024 e4m3 keys 56.5 us at 1, 54 at 2, 55.5 at 3, 56.5 at 6; bf16 97 at 2, 95 at
 // 3 to 7, 97 at 9).  kUnitCost: 64 trees of 3 nodes over 4096 keys, bf16 105 us at 3,
-// 100 at 6, 98 at 9; e4m3 71, 65, 65 at 2, 4, 6.
-template <int kType>
+// 100 at 6, 98 at 9; e4m3 71, 65, 65 at 2, 4, 6.  Chunks of 64 keys: half of that (1024
+// sequences of up to 512 e2m1 keys, kTokenCost 1 162 us, 2 166).
+template <int kType, int kN>
 struct Chunk {
-    static constexpr int kKeys = kType == DART_KV_BF16 ? 16 : 32;
-    static constexpr int kUnitCost = kType == DART_KV_BF16 ? 9 : 6, kTokenCost = kType == DART_KV_BF16 ? 5 : 2;
+    static constexpr int kKeys = kType == DART_KV_BF16 ? 16 : kType == DART_KV_E2M1 && kN == 1 ? 64 : 32;
+    static constexpr int kUnitCost = kType == DART_KV_BF16 ? 9 : kKeys == 64 ? 3 : 6, kTokenCost = kType == DART_KV_BF16 ? 5 : kKeys == 64 ? 1 : 2;
 };
 
 // A place in the list of chunks: sequence, kv head, chunk of the unit.
-template <int kType>
+template <int kType, int kN>
 struct Place {
     int s, head, chunk;
     int len, nodes, ctx_chunks, chunks, cost;  // of the sequence; cost: the unit's length in the list
     __device__ __forceinline__ void load(const PagedArgs& a) {
-        constexpr int kKeys = Chunk<kType>::kKeys;
+        constexpr int kKeys = Chunk<kType, kN>::kKeys;
         len = seq_len(a, s);
         nodes = seq_nodes(a, s);
         ctx_chunks = (len + kKeys - 1) / kKeys;
         chunks = ctx_chunks + (nodes + 1 + 15) / 16;  // (tree rows: 16 at a time)
-        cost = chunks + (a.B == 0 ? Chunk<kType>::kTokenCost : Chunk<kType>::kUnitCost);
+        cost = chunks + (a.B == 0 ? Chunk<kType, kN>::kTokenCost : Chunk<kType, kN>::kUnitCost);
     }
     __device__ __forceinline__ void next_unit(const PagedArgs& a) {
         chunk = 0;
@@ -109,12 +117,12 @@ struct Place {
 
 // By one warp: the list's length and, then, the place x of it (of its first 32
 // sequences the lengths are kept).
-template <int kType>
+template <int kType, int kN>
 struct List {
     long long all, own;  // own: length of sequence `lane`
     __device__ __forceinline__ static long long length(const PagedArgs& a, int s) {
         if (s >= a.nseq) return 0;
-        Place<kType> p{};
+        Place<kType, kN> p{};
         p.s = s;
         p.load(a);
         return static_cast<long long>(a.Hkv) * p.cost;
@@ -127,9 +135,9 @@ struct List {
         for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(kFull, n, o);
         all = n;
     }
-    __device__ __forceinline__ Place<kType> find(const PagedArgs& a, long long x, int lane) const {
+    __device__ __forceinline__ Place<kType, kN> find(const PagedArgs& a, long long x, int lane) const {
         long long done = 0;
-        Place<kType> r{};
+        Place<kType, kN> r{};
         for (int s0 = 0; s0 < a.nseq; s0 += 32) {
             const long long n = s0 == 0 ? own : length(a, s0 + lane);
             long long upto = n;
@@ -155,9 +163,9 @@ struct List {
     }
 };
 
-// Shares: one per warp, each at least kMinShare long (values around it make no
+// Shares: one per warp, each at least this long (values around it make no
 // difference: shares are shorter than that in the smallest calls alone).
-constexpr int kMinShare = 2;
+constexpr int min_share(int chunk_keys) { return chunk_keys == 64 ? 1 : 2; }
 
 // ------------------------------------------------------------ fragments
 
@@ -212,12 +220,12 @@ __device__ __forceinline__ uint32_t swz(int row, int piece) {  // byte offset in
 
 template <int kType, int kN>
 struct Geo {
-    static constexpr int kKeys = Chunk<kType>::kKeys;
+    static constexpr int kKeys = Chunk<kType, kN>::kKeys;
     static constexpr int kSubs = kKeys / 16;                             // products of 16 keys
     static constexpr int kTile = kKeys * row_bytes(kType);               // K or V of a chunk
-    static constexpr int kWarps = rows_warps(kN), kThreads = 32 * kWarps;
-    static constexpr int kStages = kType == DART_KV_E2M1 ? (kN == 1 ? 3 : 5) : kN == 1 ? 2 : 3;
-    static constexpr int kRing = kWarps * kStages * 2 * kTile;           // 192 KB (e2m1: 144, 160)
+    static constexpr int kWarps = rows_warps(kType, kN), kThreads = 32 * kWarps;
+    static constexpr int kStages = kType == DART_KV_E2M1 ? (kN == 1 ? 2 : 4) : kN == 1 ? 2 : 3;
+    static constexpr int kRing = kWarps * kStages * 2 * kTile;           // 192 KB (e2m1: 176, 128)
     // e4m3, e2m1: a key's scale; e2m1: its block scales
     static constexpr int kScale = (kType == DART_KV_BF16 ? 0 : 4) + (kType == DART_KV_E2M1 ? kBlocks : 0);
     static constexpr int kScales = kWarps * kStages * 2 * kKeys * kScale;
@@ -233,7 +241,7 @@ __device__ __forceinline__ int k_piece(int i, int t) {
 }
 
 template <int kType, int kN>
-__global__ void __launch_bounds__(32 * rows_warps(kN), 1)
+__global__ void __launch_bounds__(32 * rows_warps(kType, kN), 1)
     paged_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                       const __grid_constant__ PagedArgs a) {
     using G_ = Geo<kType, kN>;
@@ -265,12 +273,12 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
             for (int j = tid; j < a.Hq * kHeadDim / 8; j += kThreads) o[j] = make_uint4(0, 0, 0, 0);
         }
 
-    const List<kType> list(a, lane);
+    const List<kType, kN> list(a, lane);
     const int share = warp * gridDim.x + blockIdx.x;
-    const Shares shares(list.all, kWarps * gridDim.x, kMinShare);
+    const Shares shares(list.all, kWarps * gridDim.x, min_share(kKeys));
     if (share >= shares.count) return;
     long long left = shares.length(share);  // places of this share not yet worked on
-    Place<kType> use = list.find(a, shares.begin(share), lane), load = use;
+    Place<kType, kN> use = list.find(a, shares.begin(share), lane), load = use;
     if (lane == 0) {
         a.plan->places[share] = make_int4(use.s, use.head, use.chunk, use.chunks);
         a.plan->nodes[share] = use.nodes;
@@ -282,7 +290,8 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
     int none = 0;
     volatile int* abort = &none;  // (a warp waits for no other)
     const uint64_t policy = l2_policy_evict_first();  // (every key is read once)
-    const int page_mask = (1 << a.page_log2) - 1;
+    const int page_mask = (1 << a.page_log2) - 1, pool_rows = static_cast<int>(a.pool_rows);
+    constexpr int kRow = kType == DART_KV_BF16 ? 128 : row_bytes(kType);  // of a tile in shared memory (bf16: two halves)
 
     // Moves `load` to the next chunk of the cache in this share (or past it).
     auto settle = [&]() {
@@ -297,47 +306,46 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
     auto page_at = [&](int key) {
         return ld_plain(a.table + static_cast<long long>(load.s) * a.max_pages + (key >> a.page_log2));
     };
-    int page[2] = {0, 0};  // of `load`, read a chunk ahead of its use (two where pages are smaller than chunks)
+    // A chunk's tokens lie in up to kKeys / 16 pages, one after the other: lane h has page h
+    // of `load`'s, read a chunk ahead of its use (-2: no token falls there).
+    constexpr int kKeysLog2 = kKeys == 16 ? 4 : kKeys == 32 ? 5 : 6;
+    const int seg_log2 = min(a.page_log2, kKeysLog2), segs = kKeys >> seg_log2;
+    int page = 0;
     auto look_up = [&]() {
         settle();
         if (to_load <= 0) return;
-        page[0] = page_at(load.chunk * kKeys);
-        if (kF16 && a.page_log2 == 4 && load.chunk * kKeys + 16 < load.len) page[1] = page_at(load.chunk * kKeys + 16);
+        const int key = load.chunk * kKeys + ((lane & (segs - 1)) << seg_log2);
+        page = key < load.len ? page_at(key) : -2;
     };
     auto issue = [&]() {  // loads the chunk at `load`
-        if (lane == 0) {
-            const int st = fills.stage(fills.filled);
-            uint8_t* k = ring + st * 2 * kTile;
-            uint8_t* v = k + kTile;
-            float* sc = scales + st * 2 * kKeys;
-            uint8_t* bl = blocks + st * 2 * kKeys * kBlocks;
-            const bool halves = kF16 && a.page_log2 == 4;
-            mbar_arrive_expect_tx(bar + st, 2 * kTile + 2 * kKeys * G_::kScale);
+        const int st = fills.stage(fills.filled);
+        if (lane == 0) mbar_arrive_expect_tx(bar + st, 2 * kTile + 2 * kKeys * G_::kScale);
+        const int off = (load.chunk * kKeys) & page_mask;
 #pragma unroll
-            for (int h = 0; h < (kF16 ? 2 : 1); h++) {
-                if (h == 1 && !halves) break;
-                long long row = a.pool_rows;  // past the pool: zeros
-                const int key = load.chunk * kKeys + 16 * h;
-                if (h == 0 || key < load.len) {
-                    if (page[h] >= 0 && page[h] < a.num_pages)
-                        row = ((static_cast<long long>(page[h]) * a.Hkv + load.head) << a.page_log2) + (key & page_mask);
-                    else if (a.status)
-                        atomicOr(a.status, kDevBounds);
-                }
-                tma_load_2d(k + h * kTile / 2, &tmK, bar + st, 0, static_cast<int>(row), policy);
-                tma_load_2d(v + h * kTile / 2, &tmV, bar + st, 0, static_cast<int>(row), policy);
+        for (int h = 0; h < kKeys / 16; h++) {
+            if (h >= segs) break;
+            const int pg = __shfl_sync(kFull, page, h);
+            if (lane == 0) {
+                uint8_t* k = ring + st * 2 * kTile + (h << seg_log2) * kRow;
+                uint8_t* v = k + kTile;
+                const bool there = pg >= 0 && pg < a.num_pages;
+                if (!there && pg != -2 && a.status) atomicOr(a.status, kDevBounds);
+                const int from = there ? ((pg * a.Hkv + load.head) << a.page_log2) + off : 0;
+                const int row = there ? from : pool_rows;  // past the pool: zeros
+                tma_load_2d(k, &tmK, bar + st, 0, row, policy);
+                tma_load_2d(v, &tmV, bar + st, 0, row, policy);
                 if (kF16) {
-                    const long long sr = row < a.pool_rows ? row : 0;
-                    const uint32_t bytes = halves ? 64 : 128;
-                    bulk_load(sc + 16 * h, a.ks + sr, bytes, bar + st);
-                    bulk_load(sc + kKeys + 16 * h, a.vs + sr, bytes, bar + st);
+                    float* sc = scales + st * 2 * kKeys + (h << seg_log2);
+                    bulk_load(sc, a.ks + from, 4u << seg_log2, bar + st);
+                    bulk_load(sc + kKeys, a.vs + from, 4u << seg_log2, bar + st);
                     if (kFour) {
-                        bulk_load(bl + 16 * h * kBlocks, a.kb + sr * kBlocks, 2 * bytes, bar + st);
-                        bulk_load(bl + (kKeys + 16 * h) * kBlocks, a.vb + sr * kBlocks, 2 * bytes, bar + st);
+                        uint8_t* bl = blocks + (st * 2 * kKeys + (h << seg_log2)) * kBlocks;
+                        bulk_load(bl, a.kb + static_cast<long long>(from) * kBlocks, static_cast<uint32_t>(kBlocks) << seg_log2, bar + st);
+                        bulk_load(bl + kKeys * kBlocks, a.vb + static_cast<long long>(from) * kBlocks, static_cast<uint32_t>(kBlocks) << seg_log2, bar + st);
                     }
                 } else {
-                    tma_load_2d(k + kTile / 2, &tmK, bar + st, 64, static_cast<int>(row), policy);
-                    tma_load_2d(v + kTile / 2, &tmV, bar + st, 64, static_cast<int>(row), policy);
+                    tma_load_2d(k + kTile / 2, &tmK, bar + st, 64, row, policy);
+                    tma_load_2d(v + kTile / 2, &tmV, bar + st, 64, row, policy);
                 }
             }
         }
@@ -581,7 +589,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
                     if (kFour) {  // (in any order: the rows are whole)
                         for (int i = lane; i < (kKeys - there) * 4; i += 32)
                             *reinterpret_cast<uint4*>(vt + there * 64 + i * 16) = make_uint4(0, 0, 0, 0);
-                        if (lane < kKeys - there) *reinterpret_cast<uint2*>(blk + (kKeys + there + lane) * kBlocks) = make_uint2(0, 0);
+                        for (int i = lane; i < kKeys - there; i += 32) *reinterpret_cast<uint2*>(blk + (kKeys + there + i) * kBlocks) = make_uint2(0, 0);
                     } else {
                         for (int i = lane; i < (kKeys - there) * 8; i += 32) {
 #pragma unroll
@@ -599,28 +607,37 @@ __global__ void __launch_bounds__(32 * rows_warps(kN), 1)
 #pragma unroll
                         for (int e = 0; e < 4; e++) sc[j][n][e] = 0.0f;
                 if constexpr (kFour) {
+                    // step by step for all subs in turn: products that do not wait for one another
 #pragma unroll
-                    for (int j = 0; j < kSubs; j++) {
-                        const int r0 = 16 * j + row_of(0, g), r1 = 16 * j + row_of(1, g);
-                        const uint2 b0 = *reinterpret_cast<const uint2*>(blk + r0 * kBlocks), b1 = *reinterpret_cast<const uint2*>(blk + r1 * kBlocks);
+                    for (int i = 0; i < 2; i++) {  // block t + 4 i of all keys
+                        uint2 x[kSubs][2];
+                        uint32_t by[kSubs][2];
 #pragma unroll
-                        for (int i = 0; i < 2; i++) {  // block t + 4 i of both keys
-                            const uint32_t s0 = e4m3_f16(__byte_perm(i ? b0.y : b0.x, 0u, t * 0x11)), s1 = e4m3_f16(__byte_perm(i ? b1.y : b1.x, 0u, t * 0x11));
-                            const uint2 x = *reinterpret_cast<const uint2*>(kt + swz64(r0, (t + 4 * i) >> 1) + 8 * (t & 1));
-                            const uint2 y = *reinterpret_cast<const uint2*>(kt + swz64(r1, (t + 4 * i) >> 1) + 8 * (t & 1));
+                        for (int j = 0; j < kSubs; j++)
 #pragma unroll
-                            for (int w = 0; w < 2; w++) {
-                                uint32_t xw[4], yw[4];
-                                e2m1_f16(w ? x.y : x.x, xw);
-                                e2m1_f16(w ? y.y : y.x, yw);
+                            for (int qq = 0; qq < 2; qq++) {
+                                const int row = 16 * j + row_of(qq, g);
+                                x[j][qq] = *reinterpret_cast<const uint2*>(kt + swz64(row, (t + 4 * i) >> 1) + 8 * (t & 1));
+                                const uint32_t b = *reinterpret_cast<const uint32_t*>(blk + row * kBlocks + 4 * i);
+                                by[j][qq] = e4m3_f16(__byte_perm(b, 0u, t * 0x11));
+                            }
 #pragma unroll
-                                for (int h = 0; h < 2; h++) {
-                                    const uint32_t k[4] = {mul_f16x2(xw[2 * h], s0), mul_f16x2(yw[2 * h], s1), mul_f16x2(xw[2 * h + 1], s0), mul_f16x2(yw[2 * h + 1], s1)};
+                        for (int w = 0; w < 2; w++)
+#pragma unroll
+                            for (int h = 0; h < 2; h++)
+#pragma unroll
+                                for (int j = 0; j < kSubs; j++) {
+                                    uint32_t k[4];
+#pragma unroll
+                                    for (int qq = 0; qq < 2; qq++) {
+                                        uint32_t two[2];
+                                        e2m1_f16(w ? x[j][qq].y : x[j][qq].x, h, two);
+                                        k[qq] = mul_f16x2(two[0], by[j][qq]);
+                                        k[2 + qq] = mul_f16x2(two[1], by[j][qq]);
+                                    }
 #pragma unroll
                                     for (int n = 0; n < kN; n++) mma_f16(sc[j][n], k, q[n][4 * i + 2 * w + h][0], q[n][4 * i + 2 * w + h][1]);
                                 }
-                            }
-                        }
                     }
                 } else if constexpr (kF16) {
 #pragma unroll
@@ -1060,14 +1077,15 @@ int device_sms(int dev) {
 
 template <int kN>
 constexpr size_t rows_workspace() {
-    static_assert(rows_warps(kN) * kMaxSms <= kMaxShares, "the plan holds every share");
-    return sizeof(SharePlan) + sizeof(Part<kN>) * 2 * rows_warps(kN) * kMaxSms;
+    constexpr int kWarps = std::max(rows_warps(DART_KV_BF16, kN), rows_warps(DART_KV_E2M1, kN));
+    static_assert(kWarps * kMaxSms <= kMaxShares, "the plan holds every share");
+    return sizeof(SharePlan) + sizeof(Part<kN>) * 2 * kWarps * kMaxSms;
 }
 
 template <int kType, int kN>
 int launch_rows(const PagedArgs& a, const dart_kv_cache& cache, int ctas, cudaStream_t st) {
     using G_ = Geo<kType, kN>;
-    const int box = kType != DART_KV_BF16 && cache.page_size >= 32 ? 32 : 16;
+    const int box = std::min(cache.page_size, Chunk<kType, kN>::kKeys);
     CUtensorMap tmK, tmV;
     if (!encode_rows(&tmK, cache.k, a.pool_rows, kType, box) || !encode_rows(&tmV, cache.v, a.pool_rows, kType, box)) return DART_ERR_CUDA;
     if (launch_pdl(paged_rows_kernel<kType, kN>, dim3(ctas), dim3(G_::kThreads), G_::kSmem, st, tmK, tmV, a) != cudaSuccess) return DART_ERR_CUDA;
