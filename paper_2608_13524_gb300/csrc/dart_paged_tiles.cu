@@ -8,7 +8,7 @@
 //       values: the last len % 128 cache tokens (in bf16), the tree rows
 //       (keys rotated), zeros up to a multiple of 128.  So all other cache
 //       tiles are whole, need no mask, and nothing unwritten is ever read.
-//   paged_widen_kernel  e4m3 pages that several query tiles read: as f16 tiles.
+//   paged_widen_kernel  e4m3 or e2m1 pages that several query tiles read: as f16 tiles.
 //   paged_tiles_kernel  a unit is 128 query rows of a kv head against the
 //       whole cache tiles and the side tiles that its rows may see.  The
 //       tiles of all units form one list that the CTAs (one per SM) share
@@ -21,30 +21,36 @@
 // Roles in a CTA: warp 0 loads tiles by TMA, page by page (K ring, V ring);
 // warp 1 issues the MMAs; warps 2-9 are two softmax warpgroups (thread = query
 // row = TMEM lane; warpgroup wg owns key and output columns [64 wg, 64 wg +
-// 64), the two warps of a lane quarter exchange maxima and sums).  With e4m3
-// pages all operands are f16: four more warps turn raw tiles into f16, each
+// 64), the two warps of a lane quarter exchange maxima and sums).  With e4m3 or e2m1
+// pages all operands are f16: eight more warps turn raw tiles into f16, each
 // key's codes times its scale over a power of two that the tile (K) or the
 // unit so far (V) has in common; queries and side rows are f16 with a power
 // of two per row.  So nothing can overflow, and the softmax has one factor a
 // tile to apply instead of one a key (64 broadcast reads of a key's scale from
 // shared memory, twice, took 0.5 us of a tile's 1.6).  TMEM (512 columns): S
-// [0,128), O [128,256), P [256,384) in two buffers, Q [384,448), and with bf16
-// pages what the queries' first bf16 term leaves, [448,512).
+// [0,256) in two buffers, each of which P takes over (S(n + 1) is there when the softmax
+// comes to it), O [256,384), Q [384,448), and with bf16 pages what the queries' first
+// bf16 term leaves, [448,512).
 // A row's running maximum is raised (and O rescaled) only when a tile exceeds
 // it by more than 2^8.  Every wait is bounded.
 //
-// Measured: a tile takes 1.07 us from bf16 pages (24 MMAs of 64 cycles are 0.8) and
-// 1.05 from widened ones (16 MMAs, 0.53); eight trees of 512 nodes over up to 4096
-// keys take 241 and 270 us with everything around.  With the first term of the
-// queries alone bf16 pages took 0.90 and 211 us, at an error against 64 bits of
+// Measured: a tile takes 1.07 us from bf16 pages (24 MMAs of 66 cycles are 0.8), 1.05 from
+// widened ones (16 MMAs, 0.53), 1.35 from e2m1 pages that the CTA converts; eight trees of 512
+// nodes over up to 4096 keys take 238 and 264 us with everything around.  With the first
+// term of the queries alone bf16 pages took 0.90 and 211 us, at an error against 64 bits of
 // 0.0029 of the output instead of 0.0023 (its own rounding is 0.0017).  What a tile takes
-// beside its MMAs is the chain of the softmax's instructions (two warps a
-// scheduler, in step because they share rows: exponentials 0.3 us, maxima, the
-// exchange, 0.1 us for each wait) beside the issuing warp's, which is almost as
-// long.  Tried, when those eight trees took 235 us with bf16 pages: four softmax warpgroups of 32
-// columns (287 us: the fixed part of the instructions doubles); CTA pairs with half
-// of K and V each (383: one more hop in every exchange); S in two buffers and P in
-// one (262); later, mask words read a tile ahead (216 instead of 211: registers).
+// beside its MMAs is the chain of the softmax: about 580 cycles from one tile's P to the next
+// one's scores, 670 to the row's maximum, 830 to P, most of them latencies of operations
+// that share a queue (TMEM loads and stores, barriers, exchanges).  Registers count: what is
+// spilled goes to L2, since shared memory leaves the L1 cache no room (480 bytes in the
+// kernel of four converting warps and 128 registers a thread: one tree of 17 rows over
+// 131072 e2m1 keys 126 us; eight warps, 96 registers and a part's numbers in shared memory
+// 95; next part's queries fetched a tile early, at 312 bytes of spills, 370 us for the eight
+// trees).  Tried: four softmax warpgroups of 32 columns (287 us where two took 235: the
+// fixed part of the instructions doubles); CTA pairs with half of K and V each (383: one more
+// hop in every exchange); two streams of tiles, of four warps with 128 columns a thread or of eight
+// warps with 64, scores read twice (307 both, where one stream took 270: S(n + 2) waits for
+// PV(n)); weights formed before the maximum is known (274).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -72,14 +78,13 @@ constexpr int kHalf = kKeys * 128;       // 128 rows of one 128-byte swizzle col
 constexpr int kTile = 2 * kHalf;         // 128 keys of bf16
 constexpr int kSoft = 256;               // softmax threads
 constexpr int kPairBar = 2;              // named barriers 2 .. 5
-constexpr int kConvBar = 6;              // 6: the warps that convert K, 7: V
 constexpr float kSlack8 = 8.0f;          // log2 units: P <= 2^8 between rescales
 // What a unit costs beside its tiles (its queries, its result, the pause between
 // its last tile and the next unit's first), in tiles: eight trees of 512 nodes over
 // 4096 bf16 keys 241 us with 3 and 4, 245 with 6; e4m3 273, 270, 274.
 constexpr int kTileCost = 4;
 constexpr int kMinTiles = 2;             // of a share (one tree of 20 nodes over 500 keys: 1 18.5 us, 2 17.9, 4 19.8)
-constexpr uint32_t kSCol = 0, kOCol = 128, kPCol = 256, kQCol = 384, kQLoCol = 448;
+constexpr uint32_t kSCol = 0, kOCol = 256, kQCol = 384, kQLoCol = 448;  // S: two of 128 columns
 
 // Rows that threads of a warp read or write one each are kept a 16-byte piece
 // after the other: piece c of row r of a 128-row tile at [c][r].
@@ -311,7 +316,6 @@ __device__ __forceinline__ float above(float x) {
 // One block per tile of a sequence and kv head (whole cache tiles, then side
 // tiles): codes times their key's scale (e2m1: and block scale) over a power of two
 // that the tile's keys (and, apart, values) have in common, rounded once to f16.
-// Converting in the tiles kernel costs 0.8 us a tile of every unit, and this 2 us a tile once.
 template <int kType>
 __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant__ TileArgs ta, const uint8_t* pool_k, const uint8_t* pool_v) {
     __shared__ float scale_of[2 * kKeys];
@@ -503,10 +507,12 @@ struct TileList {
 };
 
 // A share's parts of units, one after the other.
-struct Walk {
+struct UnitPart {
+    int s, head, qt, t0, t1, tiles, whole, tail, nodes;  // tiles [t0, t1) of a unit of `tiles`
+};
+struct Walk : UnitPart {  // (the part at hand)
     TilePlace p;
     long long left;  // places of the share from p on
-    int s, head, qt, t0, t1, tiles, whole, tail, nodes;  // the part at hand: tiles [t0, t1) of a unit of `tiles`
     __device__ __forceinline__ bool next(const PagedArgs& a) {
         while (left > 0 && p.s < a.nseq) {  // (s: in case the lengths change under the call)
             tiles = p.tiles(a, p.qt);
@@ -526,21 +532,26 @@ struct Walk {
     }
 };
 
-// ------------------------------------------------------------ the tiles
+// The softmax warps have no registers for that: theirs is in shared memory, and so are
+// the part at hand and the next one.
+struct WalkSlot {
+    Walk walk;
+    UnitPart part[2];
+    __device__ __forceinline__ bool next(const PagedArgs& a, int which, int lane) {  // by a whole warp
+        int more = 0;
+        __syncwarp();
+        if (lane == 0) {
+            Walk w = walk;
+            more = w.next(a);
+            walk = w;
+            part[which] = w;
+        }
+        __syncwarp();
+        return __shfl_sync(kFull, more, 0) != 0;
+    }
+};
 
-// Registers move between warpgroups, out of the 4 x 128 a thread that the
-// e4m3 kernel is launched with (128 are too few for the softmax's 64 scores a
-// thread).
-constexpr int kRegsIssue = 96, kRegsSoft = 160, kRegsConvert = 96;
-static_assert(kRegsIssue + 2 * kRegsSoft + kRegsConvert <= 4 * 128, "more than the launch has");
-template <int kRegs>
-__device__ __forceinline__ void reg_less() {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs));
-}
-template <int kRegs>
-__device__ __forceinline__ void reg_more() {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs));
-}
+// ------------------------------------------------------------ the tiles
 
 // D[tmem] (+)= A[tmem] * B[smem] at fixed offsets from the operands' bases, by
 // one lane of a converged warp: operands that the whole warp agrees on stay in
@@ -563,7 +574,8 @@ __device__ __forceinline__ void commit_elected(uint64_t* bar) {
         : "memory");
 }
 // S = Q K^T (K-major K: 32 bytes a step, 64 elements a swizzle column) and
-// O += P V (MN-major V: 16 keys of 128 bytes a step).
+// O += P V (MN-major V: 16 keys of 128 bytes a step; P of keys 64 .. 127 lies 64
+// columns behind that of keys 0 .. 63).
 template <bool kFirst, int kk = 0>
 __device__ __forceinline__ void mma_s(uint32_t d, uint32_t q, uint32_t k_lo, uint32_t idesc) {
     mma_at<kk * 8, ((kk >> 2) * kHalf + (kk & 3) * 32) / 16>(d, q, k_lo, idesc, kFirst && kk == 0 ? 0u : 1u);
@@ -571,7 +583,7 @@ __device__ __forceinline__ void mma_s(uint32_t d, uint32_t q, uint32_t k_lo, uin
 }
 template <int kk = 0>
 __device__ __forceinline__ void mma_pv(uint32_t d, uint32_t p, uint32_t v_lo, uint32_t idesc, uint32_t first) {
-    mma_at<kk * 8, kk * 2048 / 16>(d, p, v_lo, idesc, kk > 0 ? 1u : 1u - first);
+    mma_at<(kk >> 2) * 64 + (kk & 3) * 8, kk * 2048 / 16>(d, p, v_lo, idesc, kk > 0 ? 1u : 1u - first);
     if constexpr (kk + 1 < kKeys / 16) mma_pv<kk + 1>(d, p, v_lo, idesc, first);
 }
 
@@ -579,21 +591,21 @@ template <Source kSource>
 struct TGeo {
     static constexpr bool kConv = kSource == kCodes || kSource == kCodes4, kFour = kSource == kCodes4;
     // Three operand tiles of K and of V; converted ones two of each, and raw tiles of
-    // half the size before them.
+    // half or a quarter of the size before them.
     static constexpr int kStages = kConv ? 2 : 3;
-    static constexpr int kRawK = kConv ? 3 : 0, kRawV = kConv ? 2 : 0;
-    static constexpr int kRing = 4;  // a tile's factors outlive its operands
+    static constexpr int kRawK = kConv ? 3 : 0, kRawV = kFour ? 3 : kConv ? 2 : 0;
+    static constexpr int kRing = 8;  // a tile's factors outlive its operands: S runs up to two tiles ahead of the softmax, K two ahead of S
     static constexpr int kOps = 2 * kStages * kTile;
     static constexpr int kRawTile = kFour ? kHalf / 2 : kHalf;
     static constexpr int kRaw = (kRawK + kRawV) * kRawTile;
     static constexpr int kRawScale = kFour ? 4 + kBlocks : 4;  // bytes of a key
     static constexpr int kRawScales = (kRawK + kRawV) * kKeys * kRawScale;
     static constexpr int kBars = 4 * kStages + 2 * (kRawK + kRawV) + (kConv ? kRing : 0) + 9;
-    static constexpr int kExchange = 4 * kRows * 4 + 16 * 4 + kRing * 8 + kRing * 4 * 4;
+    static constexpr int kExchange = 4 * kRows * 4 + 16 * 4 + kRing * 8 + (kSoft / 32) * static_cast<int>(sizeof(WalkSlot));
     static constexpr int kSmem = kOps + kRaw + kRawScales + kBars * 8 + kExchange + 16;
-    // kConv: warpgroups (producer, MMA, two idle warps), softmax, softmax, converters
-    static constexpr int kThreads = kConv ? 512 : 64 + kSoft;
-    static constexpr int kFirstSoft = kConv ? 4 : 2;
+    // loads, MMAs, 8 softmax warps, kConv: 4 that convert K, 4 V
+    static constexpr int kFirstSoft = 2, kFirstConv = kFirstSoft + kSoft / 32;
+    static constexpr int kThreads = 32 * (kFirstConv + (kConv ? 8 : 0));
 };
 
 __device__ __forceinline__ uint32_t tile_swz(int row, int piece) { return static_cast<uint32_t>(row * 128 + ((piece ^ (row & 7)) << 4)); }
@@ -628,15 +640,22 @@ __device__ __forceinline__ bool soon(uint64_t* bar, uint32_t parity, volatile in
     return __all_sync(kFull, mbar_try_wait(bar, parity)) || warp_wait<1>(bar, parity, abort);
 }
 
-// Bits [o, o + 64) of a row of mask words (o >= -128; bits outside are 0).
-__device__ __forceinline__ uint64_t mask_bits(const uint64_t* m, int mw, int o) {
-    if (o <= -64) return 0ull;
-    if (o < 0) return ld_plain(m) << -o;
-    const int w = o >> 6, sh = o & 63;
-    uint64_t r = w < mw ? ld_plain(m + w) >> sh : 0ull;
-    if (sh && w + 1 < mw) r |= ld_plain(m + w + 1) << (64 - sh);
-    return r;
-}
+// The two words of a row of mask words that hold bits [o, o + 64) (o >= -128), and
+// those bits (outside the row they are 0).
+struct MaskWords {
+    uint64_t first, second;
+    __device__ __forceinline__ void load(const uint64_t* m, int mw, int o) {
+        const int w = max(o, 0) >> 6;
+        first = o > -64 && w < mw ? ld_plain(m + w) : 0ull;
+        second = o > 0 && w + 1 < mw ? ld_plain(m + w + 1) : 0ull;
+    }
+    __device__ __forceinline__ uint64_t bits(int o) const {
+        if (o <= -64) return 0ull;
+        if (o <= 0) return first << -o;
+        const int sh = o & 63;
+        return first >> sh | (sh ? second << (64 - sh) : 0ull);
+    }
+};
 
 template <Source kSource>
 __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
@@ -665,42 +684,40 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
     uint64_t* rv_full = rk_empty + G_::kRawK;
     uint64_t* rv_empty = rv_full + G_::kRawV;
     uint64_t* sc_full = rv_empty + G_::kRawV;
-    uint64_t* s_full = sc_full + (kConv ? G_::kRing : 0);
-    uint64_t* s_empty = s_full + 1;         // softmax has S in registers
-    uint64_t* p_full = s_empty + 1;         // [2] by P buffer (P(n + 1) may be there before P(n) is waited for)
-    uint64_t* pv_done = p_full + 2;         // [2] by P buffer
+    uint64_t* s_full = sc_full + (kConv ? G_::kRing : 0);  // [2] by S buffer
+    uint64_t* p_full = s_full + 2;          // [2] the same (P(n + 1) may be there before P(n) is waited for)
+    uint64_t* pv_done = p_full + 2;         // [2]
     uint64_t* q_ready = pv_done + 2;
     uint64_t* o_free = q_ready + 1;         // the unit's O has been read
     uint64_t* tdown = o_free + 1;
     float* xch = reinterpret_cast<float*>(k_full + G_::kBars);  // [2][warpgroup][128] row max / sum exchange
     int* xok = reinterpret_cast<int*>(xch + 4 * kRows);         // [2][warpgroup][4] "no wait failed"
-    float2* tile_ref = reinterpret_cast<float2*>(xok + 16);      // [tile % 4] powers of two of K and V
-    float* conv_top = reinterpret_cast<float*>(tile_ref + G_::kRing);  // [K, V][tile % 4][warp] largest scales
-    int* misc = reinterpret_cast<int*>(conv_top + 4 * G_::kRing);      // TMEM base, abort
+    float2* tile_ref = reinterpret_cast<float2*>(xok + 16);      // [tile % kRing] powers of two of K and V
+    WalkSlot* slots = reinterpret_cast<WalkSlot*>(tile_ref + G_::kRing);  // [softmax warp]
+    int* misc = reinterpret_cast<int*>(slots + kSoft / 32);      // TMEM base, abort
     volatile int* abort = &misc[1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_trigger();
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; i++) {
-            mbar_init(&k_full[i], kConv ? 64 : 1);
+            mbar_init(&k_full[i], kConv ? 4 : 1);
             mbar_init(&k_empty[i], 1);
-            mbar_init(&v_full[i], kConv ? 64 : 1);
+            mbar_init(&v_full[i], kConv ? 4 : 1);
             mbar_init(&v_empty[i], 1);
         }
         for (int i = 0; i < G_::kRawK; i++) {
             mbar_init(&rk_full[i], 1);
-            mbar_init(&rk_empty[i], 64);
+            mbar_init(&rk_empty[i], 4);
         }
         for (int i = 0; i < G_::kRawV; i++) {
             mbar_init(&rv_full[i], 1);
-            mbar_init(&rv_empty[i], 64);
+            mbar_init(&rv_empty[i], 4);
         }
         if (kConv)
             for (int i = 0; i < G_::kRing; i++) mbar_init(&sc_full[i], 2);
-        mbar_init(s_full, 1);
-        mbar_init(s_empty, kSoft / 32);
         for (int i = 0; i < 2; i++) {
+            mbar_init(&s_full[i], 1);
             mbar_init(&p_full[i], kSoft / 32);
             mbar_init(&pv_done[i], 1);
         }
@@ -737,7 +754,6 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
     }
 
     if (warp < G_::kFirstSoft) {
-        if (kConv) reg_less<kRegsIssue>();
         if (warp == 0) {
             // ---------------------------------------------------------- loads: the whole warp, a lane per page
             const int per_tile = kKeys >> a.page_log2;  // pages of a tile
@@ -820,16 +836,16 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 constexpr uint32_t idesc_s = idesc_bf16_f32(kRows, kKeys) & (kF16 ? ~((1u << 7) | (1u << 10)) : ~0u);
                 constexpr uint32_t idesc_pv = (idesc_bf16_f32(kRows, kHeadDim) & (kF16 ? ~((1u << 7) | (1u << 10)) : ~0u)) | (1u << 16);  // B (= V) MN-major
                 const uint32_t k_lo = smem_u32(sK) >> 4, v_lo = smem_u32(sV) >> 4, base = __shfl_sync(kFull, tmem, 0);
+                // S(n + 1) takes the place of P(n - 1): products run in the order of their issue, and
+                // PV(n - 1) was issued before it.
                 auto issue_s = [&](int n) -> bool {
                     const int st = n % kStages;
-                    if (!soon(&k_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort) ||
-                        (n > 0 && !soon(s_empty, static_cast<uint32_t>(n - 1) & 1u, abort)))
-                        return false;
+                    if (!soon(&k_full[st], static_cast<uint32_t>(n / kStages) & 1u, abort)) return false;
                     tc_fence_after();
-                    const uint32_t k = __shfl_sync(kFull, (k_lo + st * (kTile >> 4)) & 0x3FFFu, 0);
-                    mma_s<true>(base + kSCol, base + kQCol, k, idesc_s);
-                    if (!kF16) mma_s<false>(base + kSCol, base + kQLoCol, k, idesc_s);
-                    commit_elected(s_full);
+                    const uint32_t k = __shfl_sync(kFull, (k_lo + st * (kTile >> 4)) & 0x3FFFu, 0), d = base + kSCol + __shfl_sync(kFull, n & 1, 0) * kKeys;
+                    mma_s<true>(d, base + kQCol, k, idesc_s);
+                    if (!kF16) mma_s<false>(d, base + kQLoCol, k, idesc_s);
+                    commit_elected(&s_full[n & 1]);
                     commit_elected(&k_empty[st]);
                     return true;
                 };
@@ -846,7 +862,7 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                          (!first || part == 0 || soon(o_free, static_cast<uint32_t>(part - 1) & 1u, abort));
                     if (!ok) break;
                     tc_fence_after();
-                    mma_pv(base + kOCol, base + kPCol + __shfl_sync(kFull, n & 1, 0) * 64,
+                    mma_pv(base + kOCol, base + kSCol + __shfl_sync(kFull, n & 1, 0) * kKeys,
                            __shfl_sync(kFull, ((v_lo + st * (kTile >> 4)) & 0x3FFFu) | ((kHalf >> 4) << 16), 0), idesc_pv, __shfl_sync(kFull, first ? 1u : 0u, 0));
                     commit_elected(&v_empty[st]);
                     commit_elected(&pv_done[n & 1]);
@@ -867,9 +883,8 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 }
             }
         }
-    } else if (warp < G_::kFirstSoft + 8) {
+    } else if (warp < G_::kFirstConv) {
         // ---------------------------------------------------------- softmax
-        if (kConv) reg_more<kRegsSoft>();
         const int qd = warp & 3, wg = (warp - G_::kFirstSoft) >> 2, cb = wg * 64;
         const int r = qd * 32 + lane;  // query row of the unit = TMEM lane
         const int pair_bar = kPairBar + qd;
@@ -892,91 +907,127 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
             ok = ok && xo[(1 - wg) * 4 + qd] != 0;
             return xc[(1 - wg) * kRows + r];
         };
-        // this thread's half of its row's query into tensor memory
-        auto load_q = [&]() {
-            const bool in = w.qt * kRows + r < (w.nodes + 1) << a.g_log2;
-            const long long at = ((static_cast<long long>(w.s) * a.Hkv + w.head) * ta.nqt + w.qt) * (16 * kRows) + 8 * wg * kRows + r;
-            uint32_t q[kF16 ? 1 : 2][32];
+        WalkSlot& slot = slots[warp - G_::kFirstSoft];
+        if (lane == 0) slot.walk = w;
+        int which = 0;  // of the slot's parts: the next one
+        bool have = slot.next(a, 0, lane), ok = true;
+        float rs = a.sl2;  // scores in log2 units = products * rs (f16: * the tile's power of two of K)
+        float2 ref_ahead = make_float2(1.0f, 1.0f);  // (kWidened: a tile's powers of two, read a tile ahead)
+        auto refs = [&](const UnitPart& u) { return ta.wide_refs + (static_cast<long long>(u.s) * a.Hkv + u.head) * ta.wide_tiles; };
+        // this thread's half of its row's query into tensor memory, and what else the part begins with
+        auto load_q = [&](const UnitPart& u) {
+            const bool in = u.qt * kRows + r < (u.nodes + 1) << a.g_log2;
+            const long long unit = (static_cast<long long>(u.s) * a.Hkv + u.head) * ta.nqt + u.qt, at = unit * (16 * kRows) + 8 * wg * kRows + r;
 #pragma unroll
-            for (int i = 0; i < (kF16 ? 1 : 2); i++)
+            for (int i = 0; i < (kF16 ? 1 : 2); i++) {
+                uint32_t q[32];
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
                     const uint4 y = in ? __ldcg((i ? ta.q_lo : ta.qr) + at + e * kRows) : make_uint4(0u, 0u, 0u, 0u);
-                    q[i][4 * e] = y.x;
-                    q[i][4 * e + 1] = y.y;
-                    q[i][4 * e + 2] = y.z;
-                    q[i][4 * e + 3] = y.w;
+                    q[4 * e] = y.x;
+                    q[4 * e + 1] = y.y;
+                    q[4 * e + 2] = y.z;
+                    q[4 * e + 3] = y.w;
                 }
-            tmem_st32(tl + kQCol + wg * 32, q[0]);
-            if (!kF16) tmem_st32(tl + kQLoCol + wg * 32, q[kF16 ? 0 : 1]);
+                if (kF16) rs = in ? __ldcg(ta.q_scale + unit * kRows + r) : a.sl2;
+                if (kSource == kWidened) ref_ahead = __ldcg(refs(u) + u.t0);
+                tmem_st32(tl + (i ? kQLoCol : kQCol) + wg * 32, q);
+            }
             tmem_wait_st();
             arrive(q_ready);
         };
-        bool have = w.next(a), ok = true;
         pdl_wait();
-        if (have) load_q();
+        if (have) load_q(slot.part[0]);
         int n = 0;
         while (have) {
-            const int s = w.s, head = w.head, t0 = w.t0, t1 = w.t1, whole = w.whole, tail = w.tail, nodes = w.nodes;
-            const bool full_unit = t0 == 0 && t1 == w.tiles;
-            const int row = w.qt * kRows + r, b = row >> a.g_log2;
-            const bool row_ok = b <= nodes;
+            const UnitPart& u = slot.part[which];
+            which ^= 1;
+            const int t1 = u.t1, whole = u.whole;
+            auto node = [&]() { return (u.qt * kRows + r) >> a.g_log2; };  // tree row of this row
+            const bool idle = !__any_sync(kFull, node() <= u.nodes);  // (in both warps of the lane quarter)
             // m_run: the row's reference.  f16: O is in units of vref, the largest of the
             // tiles' powers of two so far; P has a factor 2^7 (at most 2^15), so that 2^-31
             // of the largest weight still counts, and its tile's power of two over vref
             constexpr float kBoost = kF16 ? 7.0f : 0.0f;
             float m_run = -INFINITY, l = 0.0f, vref = 0.0f;
-            float rs = a.sl2;  // scores in log2 units = products * rs (f16: * the tile's power of two of K)
-            if (kF16 && row_ok) rs = __ldcg(ta.q_scale + ((static_cast<long long>(s) * a.Hkv + head) * ta.nqt + w.qt) * kRows + r);
-            float2 ref_ahead = make_float2(1.0f, 1.0f);  // (kWidened: read a tile ahead)
-            const float2* refs = ta.wide_refs + (static_cast<long long>(s) * a.Hkv + head) * ta.wide_tiles;
-            if (kSource == kWidened) ref_ahead = __ldcg(refs + t0);
-            for (int t = t0; t < t1; t++, n++) {
+            // Mask words of side tiles, read a tile ahead.  first_node: tree node of the first key of
+            // this half of tile t (negative: cache, row 0).
+            auto first_node = [&](int t) { return (t - whole) * kKeys + cb - u.tail - 1; };
+            MaskWords words{};
+            auto fetch_words = [&](int t) {
+                if (t < whole) return;
+                const int b = node(), o = first_node(t);
+                if (b > 0 && b <= u.nodes && o < b) words.load(a.mask + (static_cast<long long>(u.s) * a.B + b - 1) * a.mw, a.mw, o);
+            };
+            fetch_words(u.t0);
+            for (int t = u.t0; t < t1; t++, n++) {
                 // visible keys of this row among this warpgroup's 64 of the tile
                 // (of a whole cache tile all, in a row of no node too: it is not written)
                 uint64_t vis = ~0ull;
                 bool all_seen = true;
-                if (t >= whole) {
-                    const int o = (t - whole) * kKeys + cb - tail - 1;  // tree node of the first key (negative: cache, row 0)
+                if (t >= whole && !idle) {
+                    const int b = node(), o = first_node(t);
                     vis = 0ull;
-                    if (b > 0 && row_ok && o < b) {  // (bits beyond the row's own are not used)
-                        vis = mask_bits(a.mask + (static_cast<long long>(s) * a.B + b - 1) * a.mw, a.mw, o);
+                    if (b > 0 && b <= u.nodes && o < b) {  // (bits beyond the row's own are not used)
+                        vis = words.bits(o);
                         if (b - o < 64) vis &= (1ull << (b - o)) - 1ull;
                     }
                     if (o < 0) vis |= o <= -64 ? ~0ull : (1ull << -o) - 1ull;
                     all_seen = __all_sync(kFull, vis == ~0ull);
                 }
+                if (t + 1 < t1) fetch_words(t + 1);
                 // Both warps of the lane quarter reach the exchange of every iteration and
                 // leave the loop at the same point: a failed wait is exchanged with the row
                 // max and acted on after it.
                 if (kConv && ok && !soon(&sc_full[n % G_::kRing], static_cast<uint32_t>(n / G_::kRing) & 1u, abort)) ok = false;
-                if (ok && !soon(s_full, static_cast<uint32_t>(n) & 1u, abort)) ok = false;
+                if (ok && !soon(&s_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, abort)) ok = false;
                 if (!ok) attn_timeout(a.status, abort);
-                float sv[64];
+                if (idle) {  // rows of no node: nothing of them is read
+                    if (!ok) break;
+                    arrive(&p_full[n & 1]);
+                    if (t + 1 == t1) {
+                        have = slot.next(a, which, lane);
+                        if (have) load_q(slot.part[which]);
+                    }
+                    continue;
+                }
+                const uint32_t s_at = tl + kSCol + (n & 1) * kKeys + cb;
+                // kConv: the scores are read twice, 32 at a time, for want of registers (96 a thread)
+                constexpr int kPart = kConv ? 32 : 64;
+                float sv[kPart];
                 float mx = -INFINITY, rt = rs, vtile = 0.0f;
+                auto scores = [&](int c0) {  // of keys [c0, c0 + kPart) of this half
+                    if constexpr (kConv)
+                        tmem_ld32(s_at + c0, sv);
+                    else
+                        tmem_ld64(s_at, sv);
+                    if (!all_seen) {
+                        const uint64_t see = vis >> c0;
+#pragma unroll
+                        for (int c = 0; c < kPart; c++)
+                            if (!((see >> c) & 1ull)) sv[c] = -INFINITY;
+                    }
+                };
                 if (ok) {
-                    if (kF16) {  // (before s_empty: after S(n + 1) the place may be written again)
+                    if (kF16) {
                         const float2 ref = kConv ? tile_ref[n % G_::kRing] : ref_ahead;
                         // not 0, where both factors are tiny (rows of zeros): hidden keys are -inf by now
                         rt = fmaxf(rt * ref.x, FLT_MIN);
                         vtile = ref.y;
-                        if (kSource == kWidened && t + 1 < t1) ref_ahead = __ldcg(refs + t + 1);
+                        if (kSource == kWidened && t + 1 < t1) ref_ahead = __ldcg(refs(u) + t + 1);
                     }
                     tc_fence_after();
-                    tmem_ld64(tl + kSCol + cb, sv);
-                    arrive(s_empty);
-                    if (!all_seen) {
-#pragma unroll
-                        for (int c = 0; c < 64; c++)
-                            if (!((vis >> c) & 1ull)) sv[c] = -INFINITY;
-                    }
                     // (four chains: one alone would be a third of the tile's time in latencies)
-                    float m4[4] = {sv[0], sv[1], sv[2], sv[3]};
+                    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int c = 4; c < 60; c += 8)
+                    for (int c0 = 0; c0 < 64; c0 += kPart) {
+                        scores(c0);
 #pragma unroll
-                        for (int e = 0; e < 4; e++) m4[e] = max3(m4[e], sv[c + e], sv[c + 4 + e]);
-                    mx = max3(max3(m4[0], m4[1], sv[60]), max3(m4[2], m4[3], sv[61]), fmaxf(sv[62], sv[63]));
+                        for (int c = 0; c < kPart; c += 8)
+#pragma unroll
+                            for (int e = 0; e < 4; e++) m4[e] = max3(m4[e], sv[c + e], sv[c + 4 + e]);
+                    }
+                    mx = max3(m4[0], m4[1], fmaxf(m4[2], m4[3]));
                 }
                 mx = fmaxf(mx, exchange(mx, ok));
                 if (!ok) break;
@@ -993,11 +1044,10 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                     down = fmaxf(vtile * inv, 8.6736173798840355e-19f);
                     vref = vnew;
                 }
-                // P buffer n & 1 was last read by PV(n - 2), which was issued before S(n) and so
-                // ended before s_full's arrival; O must be stable (PV(n - 1) done) only when
-                // it is rescaled.  On a timeout this tile is skipped; the pair leaves the loop
+                // P takes the place of the scores that this thread has read; O must be stable
+                // (PV(n - 1) done) only when it is rescaled.  On a timeout this tile is skipped; the pair leaves the loop
                 // together at the next exchange.
-                if (t > t0 && __any_sync(kFull, resc)) {
+                if (t > u.t0 && __any_sync(kFull, resc)) {
                     if (!soon(&pv_done[(n - 1) & 1], static_cast<uint32_t>((n - 1) >> 1) & 1u, abort)) {
                         attn_timeout(a.status, abort);
                         ok = false;
@@ -1021,29 +1071,34 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 // every key of a row that has seen no visible key: m = -inf)
                 const float nm = m_run == -INFINITY ? 0.0f : kBoost - m_run + (kF16 ? log2_of(down) : 0.0f);
                 float2 sum0 = make_float2(0.0f, 0.0f), sum1 = sum0;
-                uint32_t pk[32];
 #pragma unroll
-                for (int c = 0; c < 64; c += 4) {
-                    float2 x = fma2(make_float2(sv[c], sv[c + 1]), make_float2(rt, rt), make_float2(nm, nm));
-                    float2 z = fma2(make_float2(sv[c + 2], sv[c + 3]), make_float2(rt, rt), make_float2(nm, nm));
-                    x = make_float2(ex2(x.x), ex2(x.y));
-                    z = make_float2(ex2(z.x), ex2(z.y));
-                    sum0 = add2(sum0, x);
-                    sum1 = add2(sum1, z);
-                    pk[c >> 1] = kF16 ? pack_f16x2(x.x, x.y) : pack_bf16x2(x.x, x.y);
-                    pk[(c >> 1) + 1] = kF16 ? pack_f16x2(z.x, z.y) : pack_bf16x2(z.x, z.y);
+                for (int h = 0; h < 64; h += 32) {
+                    if (kConv) scores(h);
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        const int c = kConv ? i : h + i;
+                        float2 x = fma2(make_float2(sv[c], sv[c + 1]), make_float2(rt, rt), make_float2(nm, nm));
+                        float2 z = fma2(make_float2(sv[c + 2], sv[c + 3]), make_float2(rt, rt), make_float2(nm, nm));
+                        x = make_float2(ex2(x.x), ex2(x.y));
+                        z = make_float2(ex2(z.x), ex2(z.y));
+                        sum0 = add2(sum0, x);
+                        sum1 = add2(sum1, z);
+                        pk[i >> 1] = kF16 ? pack_f16x2(x.x, x.y) : pack_bf16x2(x.x, x.y);
+                        pk[(i >> 1) + 1] = kF16 ? pack_f16x2(z.x, z.y) : pack_bf16x2(z.x, z.y);
+                    }
+                    tmem_st16u(s_at + (h >> 1), pk);
                 }
                 sum0 = add2(sum0, sum1);
                 const float lsum = sum0.x + sum0.y;
-                tmem_st32(tl + kPCol + (n & 1) * 64 + wg * 32, pk);
                 tmem_wait_st();
                 l += kF16 ? lsum * __uint_as_float(0x7F000000u - __float_as_uint(down)) : lsum;  // (1 / down)
                 arrive(&p_full[n & 1]);
                 if (t + 1 == t1) {
                     // the next part's queries, while the last PV runs: all products with this
                     // part's have been seen
-                    have = w.next(a);
-                    if (have) load_q();
+                    have = slot.next(a, which, lane);
+                    if (have) load_q(slot.part[which]);
                 }
             }
             // the pair leaves together: an `ok` lost after the last exchange is exchanged here
@@ -1051,42 +1106,59 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 attn_timeout(a.status, abort);
                 ok = false;
             }
+            if (idle) {
+                if (!ok) break;
+                arrive(o_free);
+                continue;
+            }
             l += exchange(l, ok);
             if (!ok) break;
             tc_fence_after();
-            float o[64];
-            tmem_ld64(tl + kOCol + cb, o);
-            arrive(o_free);
-            if (full_unit) {
+            const int b = node(), row = u.qt * kRows + r;
+            const bool row_ok = b <= u.nodes;
+            if (u.t0 == 0 && t1 == u.tiles) {
                 // rows in whole lines: 8 lanes exchange their rows' 8 pieces
                 const float inv = l > 0.0f ? (kF16 ? vref : 1.0f) / l : 0.0f;
                 uint4 y[8];
 #pragma unroll
-                for (int e = 0; e < 8; e++)
-                    y[e] = make_uint4(pack_bf16x2(o[8 * e] * inv, o[8 * e + 1] * inv), pack_bf16x2(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
-                                      pack_bf16x2(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_bf16x2(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+                for (int h = 0; h < 8; h += 4) {
+                    float o[32];
+                    tmem_ld32(tl + kOCol + cb + 8 * h, o);
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        y[h + e] = make_uint4(pack_bf16x2(o[8 * e] * inv, o[8 * e + 1] * inv), pack_bf16x2(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
+                                              pack_bf16x2(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_bf16x2(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+                }
+                arrive(o_free);
                 transpose8(y, lane);
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
                     const int their = row - (lane & 7) + e, tb = their >> a.g_log2;  // row of lane 8 (lane / 8) + e
-                    if (tb <= nodes)
-                        reinterpret_cast<uint4*>(a.out + ((static_cast<long long>(s) * (a.B + 1) + tb) * a.Hq + head * a.G + (their & (a.G - 1))) * kHeadDim + cb)[lane & 7] = y[e];
+                    if (tb <= u.nodes)
+                        reinterpret_cast<uint4*>(a.out + ((static_cast<long long>(u.s) * (a.B + 1) + tb) * a.Hq + u.head * a.G + (their & (a.G - 1))) * kHeadDim + cb)[lane & 7] = y[e];
                 }
-            } else if (row_ok) {
-                TilePart* d = reinterpret_cast<TilePart*>(a.parts) + 2 * blockIdx.x + (t0 > 0 ? 0 : 1);
+            } else {
+                TilePart* d = reinterpret_cast<TilePart*>(a.parts) + 2 * blockIdx.x + (u.t0 > 0 ? 0 : 1);
 #pragma unroll
-                for (int e = 0; e < 16; e++) {
-                    const float by = kF16 ? vref : 1.0f;
-                    d->o[wg * 16 + e][r] = make_float4(o[4 * e] * by, o[4 * e + 1] * by, o[4 * e + 2] * by, o[4 * e + 3] * by);
+                for (int h = 0; h < 16; h += 8) {
+                    float o[32];
+                    tmem_ld32(tl + kOCol + cb + 4 * h, o);
+                    if (h == 8) arrive(o_free);
+                    if (!row_ok) continue;
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        const float by = kF16 ? vref : 1.0f;
+                        d->o[wg * 16 + h + e][r] = make_float4(o[4 * e] * by, o[4 * e + 1] * by, o[4 * e + 2] * by, o[4 * e + 3] * by);
+                    }
                 }
-                if (wg == 0) d->ml[r] = make_float2(m_run, l);
+                if (row_ok && wg == 0) d->ml[r] = make_float2(m_run, l);
             }
         }
     } else if constexpr (kConv) {
-        // ---------------------------------------------------------- raw tiles to operands (e4m3): a thread per key
-        reg_less<kRegsConvert>();
-        // Two warps for K, two for V, on their own; a thread takes keys `key` and key + 64.
-        const int cw = warp - (G_::kFirstSoft + 8), kv = cw >> 1, key = (cw & 1) * 32 + lane;
+        // ---------------------------------------------------------- raw tiles to operands: a thread per key
+        // Four warps for K, four for V, each on its own: a warp looks at all the tile's scales for
+        // itself, which costs less than to meet the others.
+        const int cw = warp - G_::kFirstConv, kv = cw >> 2, row = (cw & 3) * 32 + lane;
         uint64_t* raw_full = kv ? rv_full : rk_full;
         uint64_t* raw_empty = kv ? rv_empty : rk_empty;
         uint64_t* op_full = kv ? v_full : k_full;
@@ -1096,12 +1168,9 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
         const int raw_stages = kv ? G_::kRawV : G_::kRawK;
         const float* side_scale = kv ? ta.side_vs : ta.side_ks;
         const uint4* side_rows = kv ? ta.side_v : ta.side_k;
-        float* pair_top = conv_top + kv * 2 * G_::kRing;
-        bool ok = true, stop = false, waited = false;
+        bool ok = true, waited = false;
         int n = 0, raw = 0;  // tiles, whole cache tiles so far
-        // The two warps meet at a barrier in every tile, so they leave together: one whose
-        // wait failed says so at the next tile's.
-        while (!stop && w.next(a)) {
+        while (ok && w.next(a)) {
             for (int t = w.t0; t < w.t1; t++, n++) {
                 const bool cache_tile = t < w.whole;
                 if (!cache_tile && !waited) {
@@ -1109,44 +1178,30 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                     waited = true;
                 }
                 const int st = n % kStages, rs = raw % raw_stages;
-                const long long side = (static_cast<long long>(w.s) * a.Hkv + w.head) * ta.sk + (t - w.whole) * kKeys + key;
-                if (ok && cache_tile && !soon(&raw_full[rs], static_cast<uint32_t>(raw / raw_stages) & 1u, abort)) ok = false;
-                float sc[2];
-#pragma unroll
-                for (int h = 0; h < 2; h++)
-                    sc[h] = cache_tile ? raw_scales[(kv * G_::kRawK + rs) * kKeys + key + 64 * h] : __ldcg(side_scale + side + 64 * h);
-                const float mine = fmaxf(fmaxf(sc[0], sc[1]), 0.0f);
-                float top = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(mine)));
-                if (lane == 0) pair_top[(n % G_::kRing) * 2 + (cw & 1)] = ok ? top : -1.0f;
-                named_bar_sync(kConvBar + kv, 64);
-                const float2 both = *reinterpret_cast<const float2*>(pair_top + (n % G_::kRing) * 2);
-                if (fminf(both.x, both.y) < 0.0f) {
-                    ok = false;
-                    stop = true;
-                    break;
-                }
-                const float ref = above(fmaxf(both.x, both.y));
-                if (key == 0) {
+                const long long side = (static_cast<long long>(w.s) * a.Hkv + w.head) * ta.sk + (t - w.whole) * kKeys;
+                ok = !cache_tile || soon(&raw_full[rs], static_cast<uint32_t>(raw / raw_stages) & 1u, abort);
+                if (!ok) break;
+                const float* scale_of = raw_scales + (kv * G_::kRawK + rs) * kKeys;
+                const float4 four = cache_tile ? reinterpret_cast<const float4*>(scale_of)[lane] : __ldcg(reinterpret_cast<const float4*>(side_scale + side) + lane);
+                const float sc = cache_tile ? scale_of[row] : __ldcg(side_scale + side + row);
+                const float most = fmaxf(max3(four.x, four.y, four.z), fmaxf(four.w, 0.0f));
+                const float ref = above(__uint_as_float(__reduce_max_sync(kFull, __float_as_uint(most))));
+                if (row == 0) {
                     (kv ? tile_ref[n % G_::kRing].y : tile_ref[n % G_::kRing].x) = ref;
                     mbar_arrive(&sc_full[n % G_::kRing]);
                 }
-                if (!soon(&op_empty[st], (static_cast<uint32_t>(n / kStages) & 1u) ^ 1u, abort)) {
-                    ok = false;
-                    if (cache_tile) raw++;
-                    continue;
-                }
+                ok = soon(&op_empty[st], (static_cast<uint32_t>(n / kStages) & 1u) ^ 1u, abort);
+                if (!ok) break;
                 const float inv = __uint_as_float(0x7F000000u - __float_as_uint(ref));  // 1 / ref
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
+                {
                     // the key's scale over the common power of two, at most 1, rounded to f16: that
                     // moves the key's scores or its values by 2^-12 of themselves at most, as
                     // much as the rounding of an operand does
-                    const __half2 by = __float2half2_rn(sc[h] * inv);
+                    const __half2 by = __float2half2_rn(sc * inv);
                     auto times = [&](uint32_t x) {
                         const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&x), by);
                         return *reinterpret_cast<const uint32_t*>(&r);
                     };
-                    const int row = key + 64 * h;
                     uint8_t* dst = op_tile + st * kTile;
                     uint4 x[8];
                     if (kFour && cache_tile) {
@@ -1159,7 +1214,7 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
 #pragma unroll
                         for (int c = 0; c < 8; c++) {  // block c: 32 bytes
                             const uint32_t wide = e4m3_f16((c < 4 ? bl.x : bl.y) >> (8 * (c & 3)));
-                            const __half2 of = __float2half2_rn(__low2float(*reinterpret_cast<const __half2*>(&wide)) * (sc[h] * inv));
+                            const __half2 of = __float2half2_rn(__low2float(*reinterpret_cast<const __half2*>(&wide)) * (sc * inv));
                             const uint32_t f = *reinterpret_cast<const uint32_t*>(&of);
                             uint32_t lo[4], hi[4];
                             e2m1_f16(c & 1 ? x[c >> 1].z : x[c >> 1].x, lo);
@@ -1193,13 +1248,14 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                     }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the MMAs read it
-                mbar_arrive(&op_full[st]);
-                if (cache_tile) {
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&op_full[st]);
                     // Only now, when what was read from it is in use: an arrival right after the
                     // loads let the slot be refilled before they had returned.
-                    mbar_arrive(&raw_empty[rs]);
-                    raw++;
+                    if (cache_tile) mbar_arrive(&raw_empty[rs]);
                 }
+                raw += cache_tile;
             }
         }
         if (!ok) attn_timeout(a.status, abort);
