@@ -990,20 +990,31 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
     auto slot = [&](int c) { return static_cast<const Part<kN>*>(a.parts) + 2 * static_cast<long long>(c) + (c < i ? 1 : 0); };
     const int c0 = i - 1, c1 = end;
     float top = -INFINITY, l = 0.0f, o[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    if (live)
-#pragma unroll 4
-        for (int c = c0 + part0; c <= c1; c += step) {
-            const Part<kN>* x = slot(c);
-            const float2 ml = x->ml[r];
-            const float4 u = *reinterpret_cast<const float4*>(&x->o[r][8 * d8]), v = *reinterpret_cast<const float4*>(&x->o[r][8 * d8 + 4]);
-            const bool any = ml.x != -INFINITY;
-            const float up = fmaxf(top, ml.x), old = top == -INFINITY ? 0.0f : exp2_fast(top - up), by = any ? exp2_fast(ml.x - up) : 0.0f;
-            top = up;
-            l = l * old + (any ? ml.y * by : 0.0f);
-            const float w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+    constexpr int kBatch = 4;  // parts on their way at a time
+    for (int first = c0 + part0; live && first <= c1; first += kBatch * step) {
+        float2 ml[kBatch];
+        float4 y[kBatch], z[kBatch];
 #pragma unroll
-            for (int k = 0; k < 8; k++) o[k] = o[k] * old + (any ? w[k] * by : 0.0f);
+        for (int u = 0; u < kBatch; u++) {
+            const int c = first + u * step;
+            ml[u] = make_float2(-INFINITY, 0.0f);
+            if (c > c1) continue;
+            const Part<kN>* x = slot(c);
+            ml[u] = x->ml[r];
+            y[u] = *reinterpret_cast<const float4*>(&x->o[r][8 * d8]);
+            z[u] = *reinterpret_cast<const float4*>(&x->o[r][8 * d8 + 4]);
         }
+#pragma unroll
+        for (int u = 0; u < kBatch; u++) {
+            if (ml[u].x == -INFINITY) continue;
+            const float up = fmaxf(top, ml[u].x), old = top == -INFINITY ? 0.0f : exp2_fast(top - up), by = exp2_fast(ml[u].x - up);
+            top = up;
+            l = l * old + ml[u].y * by;
+            const float w[8] = {y[u].x, y[u].y, y[u].z, y[u].w, z[u].x, z[u].y, z[u].z, z[u].w};
+#pragma unroll
+            for (int k = 0; k < 8; k++) o[k] = o[k] * old + w[k] * by;
+        }
+    }
     // the groups' results, one after the other
     for (int q = 1; q < step; q++) {
         __syncthreads();

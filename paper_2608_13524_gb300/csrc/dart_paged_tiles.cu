@@ -35,8 +35,8 @@
 // it by more than 2^8.  Every wait is bounded.
 //
 // Measured: a tile takes 1.07 us from bf16 pages (24 MMAs of 66 cycles are 0.8), 1.05 from
-// widened ones (16 MMAs, 0.53), 1.35 from e2m1 pages that the CTA converts; eight trees of 512
-// nodes over up to 4096 keys take 238 and 264 us with everything around.  With the first
+// widened ones (16 MMAs, 0.53), 1.3 from e2m1 pages that the CTA converts; eight trees of 512
+// nodes over up to 4096 keys take 238 and 255 us with everything around.  With the first
 // term of the queries alone bf16 pages took 0.90 and 211 us, at an error against 64 bits of
 // 0.0029 of the output instead of 0.0023 (its own rounding is 0.0017).  What a tile takes
 // beside its MMAs is the chain of the softmax: about 580 cycles from one tile's P to the next
@@ -45,7 +45,7 @@
 // spilled goes to L2, since shared memory leaves the L1 cache no room (480 bytes in the
 // kernel of four converting warps and 128 registers a thread: one tree of 17 rows over
 // 131072 e2m1 keys 126 us; eight warps, 96 registers and a part's numbers in shared memory
-// 95; next part's queries fetched a tile early, at 312 bytes of spills, 370 us for the eight
+// 89; next part's queries fetched a tile early, at 312 bytes of spills, 370 us for the eight
 // trees).  Tried: four softmax warpgroups of 32 columns (287 us where two took 235: the
 // fixed part of the instructions doubles); CTA pairs with half of K and V each (383: one more
 // hop in every exchange); two streams of tiles, of four warps with 128 columns a thread or of eight
@@ -160,120 +160,181 @@ __device__ __forceinline__ float pack_piece(const Piece& x, uint4* lo, uint4* hi
     return factor;
 }
 
-// Blocks 0 .. B of a sequence: a tree row's keys and values (side rows), head by
-// head by groups of 8 threads, and its rotated queries; blocks from B + 1 on: the
-// side rows that are no tree rows.
-constexpr int kPrepThreads = 256, kGroups = kPrepThreads / 8;
-template <int kType>
+// The first blocks of a sequence take kTree tree rows each: their keys and values (side
+// rows) and rotated queries, head by head by groups of 8 threads.  The others take
+// kTokens side rows each that are no tree rows: tokens of the cache before them and, with bf16
+// pages, zeros after them (who reads f16 side rows puts zeros there itself).  Bound by
+// latencies: 64 trees of 32 rows 61 us with a row a block, 254 of them without a tree row.
+constexpr int kPrepThreads = 256, kGroups = kPrepThreads / 8, kTokens = 16;
+template <int kType, int kTree>
 __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_constant__ TileArgs ta, const uint8_t* pool_k, const uint8_t* pool_v) {
     constexpr bool kF16 = kType != DART_KV_BF16;
-    __shared__ float2 turn_of[kHeadDim / 2];  // cos, sin
+    __shared__ float2 turn_of[kTree][kHeadDim / 2];  // cos, sin
+    __shared__ int row_of[kTokens];                  // of the pool, of head 0; -1: no such page
     const PagedArgs& a = ta.p;
-    const int tid = threadIdx.x, p = tid & 7, group = tid >> 3, s = blockIdx.x, b = blockIdx.y;
-    const long long in = static_cast<long long>(s) * (a.B + 1) + b;
-    const int rows = a.Hq + 2 * a.Hkv;  // queries, keys, values of a tree row
-    auto source = [&](int i) {
-        return i < a.Hq ? a.q + in * a.q_stride + i * kHeadDim
-                        : i < a.Hq + a.Hkv ? a.k + in * a.k_stride + (i - a.Hq) * kHeadDim : a.v + in * a.v_stride + (i - a.Hq - a.Hkv) * kHeadDim;
+    const int tid = threadIdx.x, p = tid & 7, group = tid >> 3, s = blockIdx.x;
+    const int tree_blocks = (a.B + kTree) / kTree;  // of B + 1 rows
+    const bool tree = static_cast<int>(blockIdx.y) < tree_blocks;
+    const int b0 = blockIdx.y * kTree, b_end = min(b0 + kTree, a.B + 1);
+    const long long in = static_cast<long long>(s) * (a.B + 1);
+    const int rows = a.Hq + 2 * a.Hkv, jobs = (b_end - b0) * rows;  // queries, keys, values of a tree row
+    auto source = [&](int job) {
+        const int b = b0 + job / rows, i = job % rows;
+        return i < a.Hq ? a.q + (in + b) * a.q_stride + i * kHeadDim
+                        : i < a.Hq + a.Hkv ? a.k + (in + b) * a.k_stride + (i - a.Hq) * kHeadDim : a.v + (in + b) * a.v_stride + (i - a.Hq - a.Hkv) * kHeadDim;
     };
     constexpr int kBatch = 2;  // rows of a group on their way at a time
-    uint4 raw[kBatch][2];
-    auto fetch = [&](int i0) {
+    uint4 ahead[kBatch][2];
+    auto fetch = [&](int job0) {
 #pragma unroll
         for (int u = 0; u < kBatch; u++) {
-            const int i = i0 + u * kGroups + group;
-            raw[u][0] = raw[u][1] = make_uint4(0u, 0u, 0u, 0u);
-            if (i < rows) {
-                raw[u][0] = ld_plain(reinterpret_cast<const uint4*>(source(i)) + p);
-                raw[u][1] = ld_plain(reinterpret_cast<const uint4*>(source(i)) + 8 + p);
+            const int job = job0 + u * kGroups + group;
+            ahead[u][0] = ahead[u][1] = make_uint4(0u, 0u, 0u, 0u);
+            if (job < jobs) {
+                const uint4* src = reinterpret_cast<const uint4*>(source(job));
+                ahead[u][0] = ld_plain(src + p);
+                ahead[u][1] = ld_plain(src + 8 + p);
             }
         }
     };
     pdl_wait();
     pdl_trigger();  // (after the wait: the next kernel reads lengths and pages before its own)
-    if (b <= a.B) fetch(0);  // (whatever the length and the number of nodes are)
-    const int depth = b > 0 && b <= a.B ? ld_plain(a.depths + static_cast<long long>(s) * a.B + b - 1) : 0;
+    if (tree) fetch(0);  // (whatever the length and the number of nodes are)
     const int len = seq_len(a, s), nodes = seq_nodes(a, s), tail = len % kKeys;
-    const int end = (tail + nodes) / kKeys * kKeys + kKeys;  // side rows that a tile reads
-    auto put_side = [&](int kv, int head, int j, const uint4& lo, const uint4& hi) {
-        uint4* d = kv ? ta.side_v : ta.side_k;
+    // piece i of side row j (of 16 bytes)
+    auto side_piece = [&](int kv, int head, int j, int i) {
         const long long row = (static_cast<long long>(s) * a.Hkv + head) * ta.sk + j;
-        if (kF16) {
-            d += (row >> 7) * (16 * kKeys) + (row & 127);
-            d[p * kKeys] = lo;
-            d[(8 + p) * kKeys] = hi;
-        } else {
-            d[row * 16 + p] = lo;
-            d[row * 16 + 8 + p] = hi;
-        }
+        return (kv ? ta.side_v : ta.side_k) + (kF16 ? (row >> 7) * (16 * kKeys) + i * kKeys + (row & 127) : row * 16 + i);
     };
-    auto put_scale = [&](int kv, int head, int j, float x) {
-        if (kF16 && p == 0) (kv ? ta.side_vs : ta.side_ks)[(static_cast<long long>(s) * a.Hkv + head) * ta.sk + j] = x;
-    };
-    if (b > a.B) {
-        int j = b - a.B - 1;  // of the side rows that are no tree rows: before them, then after them
-        if (j >= tail) j += nodes + 1;
-        if (j >= end) return;
-        // a token of the cache: its codes or values as they are; zeros after the nodes
-        const int key = len - tail + j;
-        const int page = j < tail ? ld_plain(a.table + static_cast<long long>(s) * a.max_pages + (key >> a.page_log2)) : -1;
-        const bool there = page >= 0 && page < a.num_pages;
-        if (j < tail && !there && a.status && tid == 0) atomicOr(a.status, kDevBounds);
-        for (int i = group; i < 2 * a.Hkv; i += kGroups) {
-            const int kv = i >= a.Hkv, head = i - kv * a.Hkv;
-            const long long row = there ? ((static_cast<long long>(page) * a.Hkv + head) << a.page_log2) + (key & ((1 << a.page_log2) - 1)) : 0;
-            const uint8_t* pool = kv ? pool_v : pool_k;
-            uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
-            if (there && kType == DART_KV_E2M1) {
-                const uint32_t* src = reinterpret_cast<const uint32_t*>(pool + row * row_bytes(kType));
-                const uint2 bl = *reinterpret_cast<const uint2*>((kv ? a.vb : a.kb) + row * kBlocks);
-                const uint32_t by_lo = e4m3_f16(__byte_perm(bl.x, 0u, (p >> 1) * 0x11)), by_hi = e4m3_f16(__byte_perm(bl.y, 0u, (p >> 1) * 0x11));
-                uint32_t x[4], y[4];
-                e2m1_f16(src[p], x);
-                e2m1_f16(src[8 + p], y);
-                lo = make_uint4(mul_f16x2(x[0], by_lo), mul_f16x2(x[1], by_lo), mul_f16x2(x[2], by_lo), mul_f16x2(x[3], by_lo));
-                hi = make_uint4(mul_f16x2(y[0], by_hi), mul_f16x2(y[1], by_hi), mul_f16x2(y[2], by_hi), mul_f16x2(y[3], by_hi));
-            } else if (there && kType == DART_KV_E4M3) {
-                const uint2 x = *reinterpret_cast<const uint2*>(pool + row * kHeadDim + 8 * p), y = *reinterpret_cast<const uint2*>(pool + row * kHeadDim + 64 + 8 * p);
-                lo = make_uint4(e4m3_f16(x.x), e4m3_f16(x.x >> 16), e4m3_f16(x.y), e4m3_f16(x.y >> 16));
-                hi = make_uint4(e4m3_f16(y.x), e4m3_f16(y.x >> 16), e4m3_f16(y.y), e4m3_f16(y.y >> 16));
-            } else if (there) {
-                lo = reinterpret_cast<const uint4*>(pool)[row * 16 + p];
-                hi = reinterpret_cast<const uint4*>(pool)[row * 16 + 8 + p];
+    auto side_scale = [&](int kv, int head, int j) { return (kv ? ta.side_vs : ta.side_ks) + (static_cast<long long>(s) * a.Hkv + head) * ta.sk + j; };
+    if (!tree) {
+        const int list = tail + (kF16 ? 0 : (tail + nodes) / kKeys * kKeys + kKeys - (tail + nodes + 1));  // side rows that are no tree rows
+        const int j0 = (blockIdx.y - tree_blocks) * kTokens, j_end = min(j0 + kTokens, list);
+        if (j0 >= j_end) return;
+        if (tid < j_end - j0) {
+            const int j = j0 + tid, key = len - tail + j;
+            int row = -1;
+            if (j < tail) {
+                const int page = ld_plain(a.table + static_cast<long long>(s) * a.max_pages + (key >> a.page_log2));
+                if (page >= 0 && page < a.num_pages)
+                    row = static_cast<int>(((static_cast<long long>(page) * a.Hkv) << a.page_log2) + (key & ((1 << a.page_log2) - 1)));
+                else if (a.status)
+                    atomicOr(a.status, kDevBounds);
             }
-            put_side(kv, head, j, lo, hi);
-            if (kF16) put_scale(kv, head, j, there ? ld_plain((kv ? a.vs : a.ks) + row) : 0.0f);
+            row_of[tid] = row;
+        }
+        __syncthreads();
+        if (kF16) {
+            // a warp a head's keys or values: 16 tokens by 2 of their 8 blocks of 16 elements at a time
+            const int warp = tid >> 5, token = tid & 15, first = (tid >> 4) & 1;
+            if (j0 + token >= j_end) return;
+            const int row0 = row_of[token];
+            for (int i = warp; i < 2 * a.Hkv; i += kPrepThreads / 32) {
+                const int kv = i >= a.Hkv, head = i - kv * a.Hkv, j = j0 + token;
+                const long long row = row0 + (static_cast<long long>(head) << a.page_log2);
+                const uint8_t* src = (kv ? pool_v : pool_k) + row * row_bytes(kType);
+                uint4 x[4];
+                uint32_t block[4];
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const int c = 2 * e + first;
+                    x[e] = make_uint4(0u, 0u, 0u, 0u);
+                    block[e] = 0u;
+                    if (row0 < 0) continue;
+                    if (kType == DART_KV_E2M1) {
+                        const uint2 y = ld_plain(reinterpret_cast<const uint2*>(src) + c);
+                        x[e].x = y.x;
+                        x[e].y = y.y;
+                        block[e] = ld_plain((kv ? a.vb : a.kb) + row * kBlocks + c);
+                    } else {
+                        x[e] = ld_plain(reinterpret_cast<const uint4*>(src) + c);
+                    }
+                }
+                if (first == 0) *side_scale(kv, head, j) = row0 >= 0 ? ld_plain((kv ? a.vs : a.ks) + row) : 0.0f;
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    uint32_t y[8];
+                    if (kType == DART_KV_E2M1) {
+                        const uint32_t by = e4m3_f16(block[e] | block[e] << 8);
+                        uint32_t lo[4], hi[4];
+                        e2m1_f16(x[e].x, lo);
+                        e2m1_f16(x[e].y, hi);
+#pragma unroll
+                        for (int k = 0; k < 4; k++) {
+                            y[k] = mul_f16x2(lo[k], by);
+                            y[4 + k] = mul_f16x2(hi[k], by);
+                        }
+                    } else {
+                        const uint32_t w[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
+#pragma unroll
+                        for (int k = 0; k < 4; k++) {
+                            y[2 * k] = e4m3_f16(w[k]);
+                            y[2 * k + 1] = e4m3_f16(w[k] >> 16);
+                        }
+                    }
+                    uint4* d = side_piece(kv, head, j, 2 * (2 * e + first));
+                    d[0] = make_uint4(y[0], y[1], y[2], y[3]);
+                    d[kKeys] = make_uint4(y[4], y[5], y[6], y[7]);
+                }
+            }
+        } else {
+            for (int i = group; i < (j_end - j0) * 2 * a.Hkv; i += kGroups) {
+                const int token = i / (2 * a.Hkv), rest = i % (2 * a.Hkv), kv = rest >= a.Hkv, head = rest - kv * a.Hkv;
+                int j = j0 + token;
+                uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
+                if (row_of[token] >= 0) {
+                    const uint4* src = reinterpret_cast<const uint4*>(kv ? pool_v : pool_k) + (row_of[token] + (static_cast<long long>(head) << a.page_log2)) * 16;
+                    lo = src[p];
+                    hi = src[8 + p];
+                }
+                if (j >= tail) j += nodes + 1;
+                uint4* d = side_piece(kv, head, j, p);
+                d[0] = lo;
+                d[8] = hi;
+            }
         }
         return;
     }
-    if (b > nodes) {  // no node: zeros as output
-        uint4* out = reinterpret_cast<uint4*>(a.out + in * a.Hq * kHeadDim);
+    for (int b = max(b0, nodes + 1); b < b_end; b++) {  // no node: zeros as output
+        uint4* out = reinterpret_cast<uint4*>(a.out + (in + b) * a.Hq * kHeadDim);
         for (int i = tid; i < a.Hq * 16; i += kPrepThreads) out[i] = make_uint4(0u, 0u, 0u, 0u);
-        return;
     }
-    if (tid < kHeadDim / 2) {
-        float sn, cs;
-        rope_sincos(a.turns.f[tid], len + depth, &sn, &cs);
-        turn_of[tid] = make_float2(cs, sn);
+    if (b0 > nodes) return;
+    if (tid < kTree * (kHeadDim / 2)) {
+        const int b = b0 + tid / (kHeadDim / 2), e = tid % (kHeadDim / 2);
+        if (b <= nodes) {
+            const int depth = b > 0 ? ld_plain(a.depths + static_cast<long long>(s) * a.B + b - 1) : 0;
+            float sn, cs;
+            rope_sincos(a.turns.f[e], len + depth, &sn, &cs);
+            turn_of[tid / (kHeadDim / 2)][e] = make_float2(cs, sn);
+        }
     }
     __syncthreads();
-    for (int i0 = 0; i0 < rows; i0 += kBatch * kGroups) {
-        if (i0 > 0) fetch(i0);
+    for (int job0 = 0; job0 < jobs; job0 += kBatch * kGroups) {
+        uint4 raw[kBatch][2];
 #pragma unroll
         for (int u = 0; u < kBatch; u++) {
-            if (i0 + u * kGroups >= rows) break;  // (whole warps stay together)
-            const int i = i0 + u * kGroups + group;
+            raw[u][0] = ahead[u][0];
+            raw[u][1] = ahead[u][1];
+        }
+        if (kTree > 1 || job0 + kBatch * kGroups < jobs) fetch(job0 + kBatch * kGroups);
+#pragma unroll
+        for (int u = 0; u < kBatch; u++) {
+            if (job0 + u * kGroups >= jobs) break;  // (whole warps stay together)
+            const int job = min(job0 + u * kGroups + group, jobs - 1), tr = job / rows, b = b0 + tr, i = job % rows;
+            const bool use = job0 + u * kGroups + group < jobs && b <= nodes;
             Piece x = unpack_piece(raw[u][0], raw[u][1]);
             if (i < a.Hq + a.Hkv)
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
-                    const float2 t = turn_of[8 * p + e];
+                    const float2 t = turn_of[tr][8 * p + e];
                     const float lo = x.lo[e], hi = x.hi[e];
                     x.lo[e] = lo * t.x - hi * t.y;
                     x.hi[e] = hi * t.x + lo * t.y;
                 }
             uint4 lo, hi;
             const float factor = pack_piece<kF16>(x, &lo, &hi);
+            if (!use) continue;
             if (i < a.Hq) {
                 const int head = i >> a.g_log2, row = (b << a.g_log2) + (i & (a.G - 1));
                 const long long tile = (static_cast<long long>(s) * a.Hkv + head) * ta.nqt + (row >> 7);
@@ -295,10 +356,12 @@ __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_c
                     d[(8 + p) * kRows] = hi;
                 }
                 if (kF16 && p == 0) ta.q_scale[tile * kRows + (row & 127)] = factor * a.sl2;
-            } else if (i < rows) {
+            } else {
                 const int kv = i >= a.Hq + a.Hkv, head = i - a.Hq - kv * a.Hkv;
-                put_side(kv, head, tail + b, lo, hi);
-                put_scale(kv, head, tail + b, factor);
+                uint4* d = side_piece(kv, head, tail + b, p);
+                d[0] = lo;
+                d[kF16 ? 8 * kKeys : 8] = hi;
+                if (kF16 && p == 0) *side_scale(kv, head, tail + b) = factor;
             }
         }
     }
@@ -324,11 +387,15 @@ __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant_
     const PagedArgs& a = ta.p;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int head = blockIdx.x % a.Hkv, s = blockIdx.x / a.Hkv, t = blockIdx.y;
-    pdl_wait();
+    // Cache tiles need nothing of the preparation, which lets this kernel start when all before
+    // it has ended.  (The last tiles of a head are never of the cache, so this kernel does
+    // not end before the preparation.)
     pdl_trigger();
     const int len = seq_len(a, s), nodes = seq_nodes(a, s), whole = len / kKeys, tail = len % kKeys;
-    if (t > whole + (tail + nodes) / kKeys) return;
     const bool cache_tile = t < whole;
+    if (!cache_tile) pdl_wait();
+    if (t > whole + (tail + nodes) / kKeys) return;
+    const int live = cache_tile ? kKeys : tail + nodes + 1 - (t - whole) * kKeys;  // rows of a side tile that exist
     const long long side = (static_cast<long long>(s) * a.Hkv + head) * ta.sk + (t - whole) * kKeys;
     if (cache_tile && tid < kKeys) {
         const int at = t * kKeys + tid;
@@ -360,7 +427,7 @@ __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant_
         const int kv = tid >> 7, key = tid & 127;
         float sc = 0.0f;
         if (!cache_tile)
-            sc = __ldcg((kv ? ta.side_vs : ta.side_ks) + side + key);
+            sc = key < live ? __ldcg((kv ? ta.side_vs : ta.side_ks) + side + key) : 0.0f;
         else if (row_of[key] >= 0)
             sc = ld_plain((kv ? a.vs : a.ks) + row_of[key]);
         scale_of[tid] = sc;
@@ -398,7 +465,8 @@ __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant_
             }
         } else {
             const uint4* src = (kv ? ta.side_v : ta.side_k) + (side >> 7) * (16 * kKeys) + key;
-            const uint4 y = __ldcg(src + 2 * p * kKeys), z = __ldcg(src + (2 * p + 1) * kKeys);
+            const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+            const uint4 y = key < live ? __ldcg(src + 2 * p * kKeys) : none, z = key < live ? __ldcg(src + (2 * p + 1) * kKeys) : none;
             x[0] = y.x;
             x[1] = y.y;
             x[2] = y.z;
@@ -1182,8 +1250,18 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 ok = !cache_tile || soon(&raw_full[rs], static_cast<uint32_t>(raw / raw_stages) & 1u, abort);
                 if (!ok) break;
                 const float* scale_of = raw_scales + (kv * G_::kRawK + rs) * kKeys;
-                const float4 four = cache_tile ? reinterpret_cast<const float4*>(scale_of)[lane] : __ldcg(reinterpret_cast<const float4*>(side_scale + side) + lane);
-                const float sc = cache_tile ? scale_of[row] : __ldcg(side_scale + side + row);
+                const int live = cache_tile ? kKeys : w.tail + w.nodes + 1 - (t - w.whole) * kKeys;  // rows that exist
+                float4 four;
+                float sc;
+                if (cache_tile) {
+                    four = reinterpret_cast<const float4*>(scale_of)[lane];
+                    sc = scale_of[row];
+                } else {
+                    const float* of = side_scale + side;
+                    auto scale = [&](int i) { return i < live ? __ldcg(of + i) : 0.0f; };
+                    four = make_float4(scale(lane), scale(lane + 32), scale(lane + 64), scale(lane + 96));
+                    sc = scale(row);
+                }
                 const float most = fmaxf(max3(four.x, four.y, four.z), fmaxf(four.w, 0.0f));
                 const float ref = above(__uint_as_float(__reduce_max_sync(kFull, __float_as_uint(most))));
                 if (row == 0) {
@@ -1209,19 +1287,22 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                         // exact where the scale is a power of two, as the cache writes leave it
                         const uint8_t* src = raw_tile + rs * G_::kRawTile;
                         const uint2 bl = *reinterpret_cast<const uint2*>(raw_blocks + ((kv * G_::kRawK + rs) * kKeys + row) * kBlocks);
+#pragma unroll 4
+                        for (int c = 0; c < 4; c++) {  // blocks 2 c, 2 c + 1: 64 bytes
+                            const uint4 y = *reinterpret_cast<const uint4*>(src + swz64(row, c));
+                            const uint32_t wide = e4m3_f16((c < 2 ? bl.x : bl.y) >> (16 * (c & 1)));
+                            const float2 of = __half22float2(*reinterpret_cast<const __half2*>(&wide));
+                            uint8_t* d = dst + (c >> 1) * kHalf;
 #pragma unroll
-                        for (int c = 0; c < 4; c++) x[c] = *reinterpret_cast<const uint4*>(src + swz64(row, c));
-#pragma unroll
-                        for (int c = 0; c < 8; c++) {  // block c: 32 bytes
-                            const uint32_t wide = e4m3_f16((c < 4 ? bl.x : bl.y) >> (8 * (c & 3)));
-                            const __half2 of = __float2half2_rn(__low2float(*reinterpret_cast<const __half2*>(&wide)) * (sc * inv));
-                            const uint32_t f = *reinterpret_cast<const uint32_t*>(&of);
-                            uint32_t lo[4], hi[4];
-                            e2m1_f16(c & 1 ? x[c >> 1].z : x[c >> 1].x, lo);
-                            e2m1_f16(c & 1 ? x[c >> 1].w : x[c >> 1].y, hi);
-                            uint8_t* d = dst + (c >> 2) * kHalf;
-                            *reinterpret_cast<uint4*>(d + tile_swz(row, (2 * c) & 7)) = make_uint4(mul_f16x2(lo[0], f), mul_f16x2(lo[1], f), mul_f16x2(lo[2], f), mul_f16x2(lo[3], f));
-                            *reinterpret_cast<uint4*>(d + tile_swz(row, (2 * c + 1) & 7)) = make_uint4(mul_f16x2(hi[0], f), mul_f16x2(hi[1], f), mul_f16x2(hi[2], f), mul_f16x2(hi[3], f));
+                            for (int e = 0; e < 2; e++) {
+                                const __half2 by = __float2half2_rn((e ? of.y : of.x) * (sc * inv));
+                                const uint32_t f = *reinterpret_cast<const uint32_t*>(&by);
+                                uint32_t lo[4], hi[4];
+                                e2m1_f16(e ? y.z : y.x, lo);
+                                e2m1_f16(e ? y.w : y.y, hi);
+                                *reinterpret_cast<uint4*>(d + tile_swz(row, (4 * c + 2 * e) & 7)) = make_uint4(mul_f16x2(lo[0], f), mul_f16x2(lo[1], f), mul_f16x2(lo[2], f), mul_f16x2(lo[3], f));
+                                *reinterpret_cast<uint4*>(d + tile_swz(row, (4 * c + 2 * e + 1) & 7)) = make_uint4(mul_f16x2(hi[0], f), mul_f16x2(hi[1], f), mul_f16x2(hi[2], f), mul_f16x2(hi[3], f));
+                            }
                         }
                     } else if (cache_tile) {
                         const uint8_t* src = raw_tile + rs * G_::kRawTile;
@@ -1237,8 +1318,13 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                         }
                     } else {
                         const uint4* src = side_rows + (side >> 7) * (16 * kKeys) + row;
-#pragma unroll
+#pragma unroll 1
                         for (int q = 0; q < 2; q++) {
+                            if (row >= live) {
+#pragma unroll
+                                for (int c = 0; c < 8; c++) *reinterpret_cast<uint4*>(dst + q * kHalf + tile_swz(row, c)) = make_uint4(0u, 0u, 0u, 0u);
+                                continue;
+                            }
 #pragma unroll
                             for (int c = 0; c < 8; c++) x[c] = __ldcg(src + (8 * q + c) * kKeys);
 #pragma unroll
@@ -1300,18 +1386,29 @@ __global__ void __launch_bounds__(256) paged_tiles_join_kernel(const __grid_cons
     }
     if (b > nodes) return;
     float top = -INFINITY, l = 0.0f, o[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-    for (int c = c0; c <= c1; c++) {
-        const TilePart* x = static_cast<const TilePart*>(a.parts) + 2 * c + (c < i ? 1 : 0);
-        const float2 ml = x->ml[r];
-        const float4 y = x->o[2 * d8][r], z = x->o[2 * d8 + 1][r];
-        const bool any = ml.x != -INFINITY;
-        const float up = fmaxf(top, ml.x), old = top == -INFINITY ? 0.0f : ex2(top - up), by = any ? ex2(ml.x - up) : 0.0f;
-        top = up;
-        l = l * old + (any ? ml.y * by : 0.0f);
-        const float v[8] = {y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
+    constexpr int kBatch = 8;  // parts on their way at a time
+    for (int c = c0; c <= c1; c += kBatch) {
+        float2 ml[kBatch];
+        float4 y[kBatch], z[kBatch];
 #pragma unroll
-        for (int k = 0; k < 8; k++) o[k] = o[k] * old + (any ? v[k] * by : 0.0f);
+        for (int u = 0; u < kBatch; u++) {
+            ml[u] = make_float2(-INFINITY, 0.0f);
+            if (c + u > c1) continue;
+            const TilePart* x = static_cast<const TilePart*>(a.parts) + 2 * (c + u) + (c + u < i ? 1 : 0);
+            ml[u] = x->ml[r];
+            y[u] = x->o[2 * d8][r];
+            z[u] = x->o[2 * d8 + 1][r];
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; u++) {
+            if (ml[u].x == -INFINITY) continue;
+            const float up = fmaxf(top, ml[u].x), old = top == -INFINITY ? 0.0f : ex2(top - up), by = ex2(ml[u].x - up);
+            top = up;
+            l = l * old + ml[u].y * by;
+            const float v[8] = {y[u].x, y[u].y, y[u].z, y[u].w, z[u].x, z[u].y, z[u].z, z[u].w};
+#pragma unroll
+            for (int k = 0; k < 8; k++) o[k] = o[k] * old + v[k] * by;
+        }
     }
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
     __nv_bfloat16* d = a.out + ((static_cast<long long>(s) * (a.B + 1) + b) * a.Hq + head * a.G + (row & (a.G - 1))) * kHeadDim + 8 * d8;
@@ -1319,13 +1416,12 @@ __global__ void __launch_bounds__(256) paged_tiles_join_kernel(const __grid_cons
                                               pack_bf16x2(o[4] * inv, o[5] * inv), pack_bf16x2(o[6] * inv, o[7] * inv));
 }
 
-// e4m3 pages are widened first where a kv head has at least this many query
+// e4m3 and e2m1 pages are widened first where a kv head has at least this many query
 // tiles, each of which would convert all keys again (a tile of a unit takes 1.05
-// us from f16 tiles and 1.9 converted), and where the f16 tiles of the longest
-// sequences take at most 4 GB.  Eight trees over 4096 keys, widened / converted:
-// 4 query tiles 96 / 97 us, 5 113 / 120, 8 150 / 184; one over 2048, 3 tiles 28.4 /
-// 23.8; one over 16384, 4 tiles 73 / 70.
-constexpr int kWidenTiles = 4;
+// us from f16 tiles and 1.3 converted), and where the f16 tiles of the longest
+// sequences take at most 4 GB.  e2m1 pages, widened / converted: eight trees over 4096 keys,
+// 4 query tiles 86 / 89 us, 5 98 / 107, 8 138 / 157; two over 16384, 4 tiles 93 / 79.
+constexpr int kWidenTiles = 5;
 constexpr size_t kWidenBytes = static_cast<size_t>(4) << 30;
 
 // Workspace: partial results, queries, side rows, their factors, f16 tiles.
@@ -1406,13 +1502,18 @@ int launch_paged_tiles(PagedArgs a, const dart_kv_cache& cache, uint8_t* workspa
         tmSk = tmK;  // (side tiles lie among the others)
         tmSv = tmV;
     }
-    // tree rows, up to 127 cache tokens before them, up to 127 rows of zeros after them
-    const dim3 prep(static_cast<unsigned>(a.nseq), static_cast<unsigned>(a.B + 1 + 2 * (kKeys - 1)));
+    // Four tree rows a block where that leaves every SM a block.
+    const bool four = static_cast<long long>(a.nseq) * (a.B + 1) >= 4 * sms;
+    const int tree_blocks = four ? (a.B + 4) / 4 : a.B + 1;
+    // up to 127 cache tokens before the tree rows and, in bf16, up to 127 rows of zeros after them
+    const int others = e4m3 || e2m1 ? kKeys - 1 : 2 * (kKeys - 1);
+    const dim3 prep(static_cast<unsigned>(a.nseq), static_cast<unsigned>(tree_blocks + (others + kTokens - 1) / kTokens));
     const uint8_t *pk = static_cast<const uint8_t*>(cache.k), *pv = static_cast<const uint8_t*>(cache.v);
     const dim3 pb(kPrepThreads), wg(static_cast<unsigned>(heads), static_cast<unsigned>(w.wide_tiles)), wb(256);
-    cudaError_t e = e2m1   ? launch_pdl(paged_prep_kernel<DART_KV_E2M1>, prep, pb, 0, st, ta, pk, pv)
-                    : e4m3 ? launch_pdl(paged_prep_kernel<DART_KV_E4M3>, prep, pb, 0, st, ta, pk, pv)
-                           : launch_pdl(paged_prep_kernel<DART_KV_BF16>, prep, pb, 0, st, ta, pk, pv);
+    auto prepare = [&](auto* kernel) { return launch_pdl(kernel, prep, pb, 0, st, ta, pk, pv); };
+    cudaError_t e = e2m1   ? prepare(four ? paged_prep_kernel<DART_KV_E2M1, 4> : paged_prep_kernel<DART_KV_E2M1, 1>)
+                    : e4m3 ? prepare(four ? paged_prep_kernel<DART_KV_E4M3, 4> : paged_prep_kernel<DART_KV_E4M3, 1>)
+                           : prepare(four ? paged_prep_kernel<DART_KV_BF16, 4> : paged_prep_kernel<DART_KV_BF16, 1>);
     if (e == cudaSuccess && wide)
         e = e2m1 ? launch_pdl(paged_widen_kernel<DART_KV_E2M1>, wg, wb, 0, st, ta, pk, pv) : launch_pdl(paged_widen_kernel<DART_KV_E4M3>, wg, wb, 0, st, ta, pk, pv);
     if (e == cudaSuccess)
