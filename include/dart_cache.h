@@ -77,6 +77,8 @@ typedef struct {
  * scale is exact; a block scale is its 16 elements' largest magnitude / scale /
  * 6 rounded to e4m3 (at most 342; it may be 0), and a code x / scale / block
  * rounded to e2m1, both to nearest, ties to even, magnitudes above 6 to 6.
+ * What is rounded of K is its rotation to 2^-44 of a pair's length: where the one
+ * in fp32 leaves a scale or a code open, it is formed again.
  * A NaN or an infinity makes its block (in K, that of its rotated pair too)
  * NaN when it is read and counts for no scale.
  * Positions past max_pages * page_size are not written
