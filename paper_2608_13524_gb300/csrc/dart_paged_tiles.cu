@@ -50,7 +50,9 @@
 // fixed part of the instructions doubles); CTA pairs with half of K and V each (383: one more
 // hop in every exchange); two streams of tiles, of four warps with 128 columns a thread or of eight
 // warps with 64, scores read twice (307 both, where one stream took 270: S(n + 2) waits for
-// PV(n)); weights formed before the maximum is known (274).
+// PV(n)); weights formed before the maximum is known (274);
+// where those take 255, PV(n) and S(n + 2) issued in one go (257) and the next tile's scores
+// loaded while P is stored (280: tensor memory serves the products meanwhile).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
