@@ -24,6 +24,7 @@ struct SharePlan {
 
 struct PagedArgs {
     int nseq, B, Hq, Hkv, G, g_log2, max_pages, page_log2, num_pages, mw;
+    int unit_cost;  // (tiles) what a unit costs beside its tiles, in tiles
     long long pool_rows;
     const int32_t *table, *lens, *depths, *n_nodes;
     const uint64_t* mask;

@@ -22,7 +22,7 @@
 // warp 1 issues the MMAs; warps 2-9 are two softmax warpgroups (thread = query
 // row = TMEM lane; warpgroup wg owns key and output columns [64 wg, 64 wg +
 // 64), the two warps of a lane quarter exchange maxima and sums).  With e4m3 or e2m1
-// pages all operands are f16: eight more warps turn raw tiles into f16, each
+// pages all operands are f16: four more warps turn raw tiles into f16, each
 // key's codes times its scale over a power of two that the tile (K) or the
 // unit so far (V) has in common; queries and side rows are f16 with a power
 // of two per row.  So nothing can overflow, and the softmax has one factor a
@@ -35,23 +35,25 @@
 // it by more than 2^8.  Every wait is bounded.
 //
 // Measured: a tile takes 1.07 us from bf16 pages (24 MMAs of 66 cycles are 0.8), 1.05 from
-// widened ones (16 MMAs, 0.53), 1.3 from e2m1 pages that the CTA converts; eight trees of 512
+// widened ones (16 MMAs, 0.53), 1.4 from e2m1 pages that the CTA converts; eight trees of 512
 // nodes over up to 4096 keys take 238 and 255 us with everything around.  With the first
 // term of the queries alone bf16 pages took 0.90 and 211 us, at an error against 64 bits of
 // 0.0029 of the output instead of 0.0023 (its own rounding is 0.0017).  What a tile takes
 // beside its MMAs is the chain of the softmax: about 580 cycles from one tile's P to the next
 // one's scores, 670 to the row's maximum, 830 to P, most of them latencies of operations
-// that share a queue (TMEM loads and stores, barriers, exchanges).  Registers count: what is
-// spilled goes to L2, since shared memory leaves the L1 cache no room (480 bytes in the
-// kernel of four converting warps and 128 registers a thread: one tree of 17 rows over
-// 131072 e2m1 keys 126 us; eight warps, 96 registers and a part's numbers in shared memory
-// 89; next part's queries fetched a tile early, at 312 bytes of spills, 370 us for the eight
-// trees).  Tried: four softmax warpgroups of 32 columns (287 us where two took 235: the
+// that share a queue (TMEM loads and stores, barriers, exchanges).  Registers and
+// instructions count: what is spilled goes to L2, since shared memory leaves the L1 cache no
+// room (a part's numbers are in shared memory for that; without, 480 bytes of spills, one tree of
+// 17 rows over 131072 e2m1 keys 126 us instead of 91; the next part's queries fetched a tile
+// early, at 312 bytes, 370 us for the eight trees), and four kinds of warps share the
+// instruction cache (the two keys of a converting thread unrolled, 64 trees of 32 rows over
+// up to 4096 e2m1 keys 176 us instead of 140; eight converting warps, and so 96 registers, 148).
+// Tried: four softmax warpgroups of 32 columns (287 us where two took 235: the
 // fixed part of the instructions doubles); CTA pairs with half of K and V each (383: one more
 // hop in every exchange); two streams of tiles, of four warps with 128 columns a thread or of eight
 // warps with 64, scores read twice (307 both, where one stream took 270: S(n + 2) waits for
-// PV(n)); weights formed before the maximum is known (274);
-// where those take 255, PV(n) and S(n + 2) issued in one go (257) and the next tile's scores
+// PV(n)); weights formed before the maximum is known (274).
+// Where they take 255: PV(n) and S(n + 2) issued in one go (257) and the next tile's scores
 // loaded while P is stored (280: tensor memory serves the products meanwhile).
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -83,8 +85,10 @@ constexpr int kPairBar = 2;              // named barriers 2 .. 5
 constexpr float kSlack8 = 8.0f;          // log2 units: P <= 2^8 between rescales
 // What a unit costs beside its tiles (its queries, its result, the pause between
 // its last tile and the next unit's first), in tiles: eight trees of 512 nodes over
-// 4096 bf16 keys 241 us with 3 and 4, 245 with 6; e4m3 273, 270, 274.
-constexpr int kTileCost = 4;
+// 4096 bf16 keys 241 us with 3 and 4, 245 with 6; e4m3 273, 270, 274; e2m1 262, 255, 258.
+// Where a tile takes longer, because the CTA converts it, one less: 64 trees of 32
+// rows over up to 4096 e2m1 keys 143 us with 3, 144 with 4.
+constexpr int kTileCost = 4, kTileCostConverted = 3;
 constexpr int kMinTiles = 2;             // of a share (one tree of 20 nodes over 500 keys: 1 18.5 us, 2 17.9, 4 19.8)
 constexpr uint32_t kSCol = 0, kOCol = 256, kQCol = 384, kQLoCol = 448;  // S: two of 128 columns
 
@@ -494,7 +498,7 @@ __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant_
 
 // A place in the list: kv heads of a sequence one after the other, the units
 // (query tiles) of a head one after the other.  A unit's length in the list is
-// its tiles (its last row sees tree rows up to itself) and kTileCost.
+// its tiles (its last row sees tree rows up to itself) and unit_cost.
 struct TilePlace {
     int s, head, qt, tile;
     int len, nodes, whole, tail, nqt;  // of the sequence: whole cache tiles, cache tokens beside them, units per head
@@ -510,7 +514,7 @@ struct TilePlace {
     }
     __device__ __forceinline__ int head_cost(const PagedArgs& a) const {
         int n = 0;
-        for (int q = 0; q < nqt; q++) n += tiles(a, q) + kTileCost;
+        for (int q = 0; q < nqt; q++) n += tiles(a, q) + a.unit_cost;
         return n;
     }
     __device__ __forceinline__ void next_unit(const PagedArgs& a) {
@@ -566,7 +570,7 @@ struct TileList {
                 r.load(a);
                 r.head = place_div(rest, cost);
                 r.tile = static_cast<int>(rest - static_cast<long long>(r.head) * cost);
-                for (int t; r.tile >= (t = r.tiles(a, r.qt) + kTileCost); r.qt++) r.tile -= t;
+                for (int t; r.tile >= (t = r.tiles(a, r.qt) + a.unit_cost); r.qt++) r.tile -= t;
                 return r;
             }
             done += __shfl_sync(kFull, upto, 31);
@@ -594,7 +598,7 @@ struct Walk : UnitPart {  // (the part at hand)
             whole = p.whole;
             tail = p.tail;
             nodes = p.nodes;
-            left -= tiles + kTileCost - t0;
+            left -= tiles + a.unit_cost - t0;
             p.next_unit(a);
             if (t0 < t1) return true;
         }
@@ -675,7 +679,7 @@ struct TGeo {
     static constexpr int kSmem = kOps + kRaw + kRawScales + kBars * 8 + kExchange + 16;
     // loads, MMAs, 8 softmax warps, kConv: 4 that convert K, 4 V
     static constexpr int kFirstSoft = 2, kFirstConv = kFirstSoft + kSoft / 32;
-    static constexpr int kThreads = 32 * (kFirstConv + (kConv ? 8 : 0));
+    static constexpr int kThreads = 32 * (kFirstConv + (kConv ? 4 : 0));
 };
 
 __device__ __forceinline__ uint32_t tile_swz(int row, int piece) { return static_cast<uint32_t>(row * 128 + ((piece ^ (row & 7)) << 4)); }
@@ -771,18 +775,18 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; i++) {
-            mbar_init(&k_full[i], kConv ? 4 : 1);
+            mbar_init(&k_full[i], kConv ? 2 : 1);
             mbar_init(&k_empty[i], 1);
-            mbar_init(&v_full[i], kConv ? 4 : 1);
+            mbar_init(&v_full[i], kConv ? 2 : 1);
             mbar_init(&v_empty[i], 1);
         }
         for (int i = 0; i < G_::kRawK; i++) {
             mbar_init(&rk_full[i], 1);
-            mbar_init(&rk_empty[i], 4);
+            mbar_init(&rk_empty[i], 2);
         }
         for (int i = 0; i < G_::kRawV; i++) {
             mbar_init(&rv_full[i], 1);
-            mbar_init(&rv_empty[i], 4);
+            mbar_init(&rv_empty[i], 2);
         }
         if (kConv)
             for (int i = 0; i < G_::kRing; i++) mbar_init(&sc_full[i], 2);
@@ -1062,22 +1066,8 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                     continue;
                 }
                 const uint32_t s_at = tl + kSCol + (n & 1) * kKeys + cb;
-                // kConv: the scores are read twice, 32 at a time, for want of registers (96 a thread)
-                constexpr int kPart = kConv ? 32 : 64;
-                float sv[kPart];
+                float sv[64];
                 float mx = -INFINITY, rt = rs, vtile = 0.0f;
-                auto scores = [&](int c0) {  // of keys [c0, c0 + kPart) of this half
-                    if constexpr (kConv)
-                        tmem_ld32(s_at + c0, sv);
-                    else
-                        tmem_ld64(s_at, sv);
-                    if (!all_seen) {
-                        const uint64_t see = vis >> c0;
-#pragma unroll
-                        for (int c = 0; c < kPart; c++)
-                            if (!((see >> c) & 1ull)) sv[c] = -INFINITY;
-                    }
-                };
                 if (ok) {
                     if (kF16) {
                         const float2 ref = kConv ? tile_ref[n % G_::kRing] : ref_ahead;
@@ -1087,16 +1077,18 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                         if (kSource == kWidened && t + 1 < t1) ref_ahead = __ldcg(refs(u) + t + 1);
                     }
                     tc_fence_after();
+                    tmem_ld64(s_at, sv);
+                    if (!all_seen) {
+#pragma unroll
+                        for (int c = 0; c < 64; c++)
+                            if (!((vis >> c) & 1ull)) sv[c] = -INFINITY;
+                    }
                     // (four chains: one alone would be a third of the tile's time in latencies)
                     float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int c0 = 0; c0 < 64; c0 += kPart) {
-                        scores(c0);
+                    for (int c = 0; c < 64; c += 8)
 #pragma unroll
-                        for (int c = 0; c < kPart; c += 8)
-#pragma unroll
-                            for (int e = 0; e < 4; e++) m4[e] = max3(m4[e], sv[c + e], sv[c + 4 + e]);
-                    }
+                        for (int e = 0; e < 4; e++) m4[e] = max3(m4[e], sv[c + e], sv[c + 4 + e]);
                     mx = max3(m4[0], m4[1], fmaxf(m4[2], m4[3]));
                 }
                 mx = fmaxf(mx, exchange(mx, ok));
@@ -1124,7 +1116,7 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                         continue;
                     }
                     tc_fence_after();
-#pragma unroll
+#pragma unroll(kConv ? 1 : 4)  // (the less code, the better)
                     for (int c0 = 0; c0 < 64; c0 += 16) {
                         float o[16];
                         tmem_ld16(tl + kOCol + cb + c0, o);
@@ -1143,11 +1135,10 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 float2 sum0 = make_float2(0.0f, 0.0f), sum1 = sum0;
 #pragma unroll
                 for (int h = 0; h < 64; h += 32) {
-                    if (kConv) scores(h);
                     uint32_t pk[16];
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) {
-                        const int c = kConv ? i : h + i;
+                        const int c = h + i;
                         float2 x = fma2(make_float2(sv[c], sv[c + 1]), make_float2(rt, rt), make_float2(nm, nm));
                         float2 z = fma2(make_float2(sv[c + 2], sv[c + 3]), make_float2(rt, rt), make_float2(nm, nm));
                         x = make_float2(ex2(x.x), ex2(x.y));
@@ -1209,7 +1200,7 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 }
             } else {
                 TilePart* d = reinterpret_cast<TilePart*>(a.parts) + 2 * blockIdx.x + (u.t0 > 0 ? 0 : 1);
-#pragma unroll
+#pragma unroll(kConv ? 1 : 2)
                 for (int h = 0; h < 16; h += 8) {
                     float o[32];
                     tmem_ld32(tl + kOCol + cb + 4 * h, o);
@@ -1225,10 +1216,10 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
             }
         }
     } else if constexpr (kConv) {
-        // ---------------------------------------------------------- raw tiles to operands: a thread per key
-        // Four warps for K, four for V, each on its own: a warp looks at all the tile's scales for
+        // ---------------------------------------------------------- raw tiles to operands: a thread per two keys
+        // Two warps for K, two for V, each on its own: a warp looks at all the tile's scales for
         // itself, which costs less than to meet the others.
-        const int cw = warp - G_::kFirstConv, kv = cw >> 2, row = (cw & 3) * 32 + lane;
+        const int cw = warp - G_::kFirstConv, kv = cw >> 1, row0 = (cw & 1) * 32 + lane;
         uint64_t* raw_full = kv ? rv_full : rk_full;
         uint64_t* raw_empty = kv ? rv_empty : rk_empty;
         uint64_t* op_full = kv ? v_full : k_full;
@@ -1254,26 +1245,25 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 const float* scale_of = raw_scales + (kv * G_::kRawK + rs) * kKeys;
                 const int live = cache_tile ? kKeys : w.tail + w.nodes + 1 - (t - w.whole) * kKeys;  // rows that exist
                 float4 four;
-                float sc;
                 if (cache_tile) {
                     four = reinterpret_cast<const float4*>(scale_of)[lane];
-                    sc = scale_of[row];
                 } else {
                     const float* of = side_scale + side;
                     auto scale = [&](int i) { return i < live ? __ldcg(of + i) : 0.0f; };
                     four = make_float4(scale(lane), scale(lane + 32), scale(lane + 64), scale(lane + 96));
-                    sc = scale(row);
                 }
                 const float most = fmaxf(max3(four.x, four.y, four.z), fmaxf(four.w, 0.0f));
                 const float ref = above(__uint_as_float(__reduce_max_sync(kFull, __float_as_uint(most))));
-                if (row == 0) {
+                if (row0 == 0) {
                     (kv ? tile_ref[n % G_::kRing].y : tile_ref[n % G_::kRing].x) = ref;
                     mbar_arrive(&sc_full[n % G_::kRing]);
                 }
                 ok = soon(&op_empty[st], (static_cast<uint32_t>(n / kStages) & 1u) ^ 1u, abort);
                 if (!ok) break;
                 const float inv = __uint_as_float(0x7F000000u - __float_as_uint(ref));  // 1 / ref
-                {
+#pragma unroll 1
+                for (int row = row0; row < kKeys; row += 64) {
+                    const float sc = cache_tile ? scale_of[row] : row < live ? __ldcg(side_scale + side + row) : 0.0f;
                     // the key's scale over the common power of two, at most 1, rounded to f16: that
                     // moves the key's scores or its values by 2^-12 of themselves at most, as
                     // much as the rounding of an operand does
@@ -1479,6 +1469,7 @@ int launch_paged_tiles(PagedArgs a, const dart_kv_cache& cache, uint8_t* workspa
     const TileWs w = tile_ws(a.nseq, a.B, a.Hq, cache, a.max_pages);
     const bool wide = w.wide_tiles > 0;
     TileArgs ta{};
+    a.unit_cost = wide || !(e4m3 || e2m1) ? kTileCost : kTileCostConverted;
     ta.p = a;
     ta.sk = w.sk;
     ta.nqt = w.nqt;
