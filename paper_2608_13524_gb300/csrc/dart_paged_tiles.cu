@@ -36,7 +36,7 @@
 //
 // Measured: a tile takes 1.07 us from bf16 pages (24 MMAs of 66 cycles are 0.8), 1.05 from
 // widened ones (16 MMAs, 0.53), 1.4 from e2m1 pages that the CTA converts; eight trees of 512
-// nodes over up to 4096 keys take 238 and 255 us with everything around.  With the first
+// nodes over up to 4096 keys take 236 and 247 us with everything around.  With the first
 // term of the queries alone bf16 pages took 0.90 and 211 us, at an error against 64 bits of
 // 0.0029 of the output instead of 0.0023 (its own rounding is 0.0017).  What a tile takes
 // beside its MMAs is the chain of the softmax: about 580 cycles from one tile's P to the next
@@ -175,7 +175,7 @@ constexpr int kPrepThreads = 256, kGroups = kPrepThreads / 8, kTokens = 16;
 template <int kType, int kTree>
 __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_constant__ TileArgs ta, const uint8_t* pool_k, const uint8_t* pool_v) {
     constexpr bool kF16 = kType != DART_KV_BF16;
-    __shared__ float2 turn_of[kTree][kHeadDim / 2];  // cos, sin
+    __shared__ float2 turn_of[kTree][kHeadDim / 2];  // cos, sin; of element 8 p + e at [8 e + p]
     __shared__ int row_of[kTokens];                  // of the pool, of head 0; -1: no such page
     const PagedArgs& a = ta.p;
     const int tid = threadIdx.x, p = tid & 7, group = tid >> 3, s = blockIdx.x;
@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_c
             const int depth = b > 0 ? ld_plain(a.depths + static_cast<long long>(s) * a.B + b - 1) : 0;
             float sn, cs;
             rope_sincos(a.turns.f[e], len + depth, &sn, &cs);
-            turn_of[tid / (kHeadDim / 2)][e] = make_float2(cs, sn);
+            turn_of[tid / (kHeadDim / 2)][8 * (e % 8) + e / 8] = make_float2(cs, sn);
         }
     }
     __syncthreads();
@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_c
             if (i < a.Hq + a.Hkv)
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
-                    const float2 t = turn_of[tr][8 * p + e];
+                    const float2 t = turn_of[tr][8 * e + p];
                     const float lo = x.lo[e], hi = x.hi[e];
                     x.lo[e] = lo * t.x - hi * t.y;
                     x.hi[e] = hi * t.x + lo * t.y;
@@ -411,10 +411,10 @@ __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant_
         row_of[tid] = there ? static_cast<int>(((static_cast<long long>(page) * a.Hkv + head) << a.page_log2) + (at & ((1 << a.page_log2) - 1))) : -1;
     }
     __syncthreads();
-    // groups of 8 lanes a row, 16 elements a lane: on their way while the scales are compared
+    // groups of 8 lanes a row, 16-byte pieces p and 8 + p of it a lane: on their way while the scales are compared
     const int p = tid & 7, group = tid >> 3;
     constexpr int kRounds = 2 * kKeys / 32;
-    uint4 c[kRounds];  // (e2m1: two words, and the block scale)
+    uint4 c[kRounds];  // codes of both pieces (e2m1: a word each, and the row's block scales)
     if (cache_tile)
 #pragma unroll
         for (int i = 0; i < kRounds; i++) {
@@ -423,10 +423,13 @@ __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant_
             if (row < 0) continue;
             const uint8_t* pool = i >= kRounds / 2 ? pool_v : pool_k;
             if (kType == DART_KV_E2M1) {
-                const uint2 x = ld_plain(reinterpret_cast<const uint2*>(pool) + static_cast<long long>(row) * 8 + p);
-                c[i] = make_uint4(x.x, x.y, ld_plain((i >= kRounds / 2 ? a.vb : a.kb) + static_cast<long long>(row) * kBlocks + p), 0u);
+                const uint32_t* src = reinterpret_cast<const uint32_t*>(pool + static_cast<long long>(row) * row_bytes(kType));
+                const uint2 block = ld_plain(reinterpret_cast<const uint2*>(i >= kRounds / 2 ? a.vb : a.kb) + row);
+                c[i] = make_uint4(ld_plain(src + p), ld_plain(src + 8 + p), block.x, block.y);
             } else {
-                c[i] = ld_plain(reinterpret_cast<const uint4*>(pool) + static_cast<long long>(row) * 8 + p);
+                const uint2* src = reinterpret_cast<const uint2*>(pool + static_cast<long long>(row) * row_bytes(kType));
+                const uint2 x = ld_plain(src + p), y = ld_plain(src + 8 + p);
+                c[i] = make_uint4(x.x, x.y, y.x, y.y);
             }
         }
     {
@@ -449,48 +452,45 @@ __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant_
 #pragma unroll
     for (int i = 0; i < kRounds; i++) {
         const int kv = i >= kRounds / 2, key = (i * 32 + group) & 127;
-        float factor = scale_of[kv * kKeys + key] * __uint_as_float(0x7F000000u - __float_as_uint(ref[kv]));
-        uint32_t x[8];
+        const float factor = scale_of[kv * kKeys + key] * __uint_as_float(0x7F000000u - __float_as_uint(ref[kv]));
+        float of[2] = {factor, factor};
+        uint32_t x[2][4];
         if (cache_tile && kType == DART_KV_E2M1) {
-            const uint32_t block = e4m3_f16(c[i].z);
-            factor *= __low2float(*reinterpret_cast<const __half2*>(&block));
-            uint32_t lo[4], hi[4];
-            e2m1_f16(c[i].x, lo);
-            e2m1_f16(c[i].y, hi);
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                x[e] = lo[e];
-                x[4 + e] = hi[e];
-            }
+            const uint32_t block = e4m3_f16(__byte_perm(c[i].z, c[i].w, (p >> 1) * 0x11 + 0x40));
+            const float2 by = __half22float2(*reinterpret_cast<const __half2*>(&block));
+            of[0] *= by.x;
+            of[1] *= by.y;
+            e2m1_f16(c[i].x, x[0]);
+            e2m1_f16(c[i].y, x[1]);
         } else if (cache_tile) {
             const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
 #pragma unroll
             for (int e = 0; e < 4; e++) {
-                x[2 * e] = e4m3_f16(w[e]);
-                x[2 * e + 1] = e4m3_f16(w[e] >> 16);
+                x[e >> 1][2 * (e & 1)] = e4m3_f16(w[e]);
+                x[e >> 1][2 * (e & 1) + 1] = e4m3_f16(w[e] >> 16);
             }
         } else {
             const uint4* src = (kv ? ta.side_v : ta.side_k) + (side >> 7) * (16 * kKeys) + key;
-            const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-            const uint4 y = key < live ? __ldcg(src + 2 * p * kKeys) : none, z = key < live ? __ldcg(src + (2 * p + 1) * kKeys) : none;
-            x[0] = y.x;
-            x[1] = y.y;
-            x[2] = y.z;
-            x[3] = y.w;
-            x[4] = z.x;
-            x[5] = z.y;
-            x[6] = z.z;
-            x[7] = z.w;
-        }
-        const __half2 by = __float2half2_rn(factor);
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-            const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&x[e]), by);
-            x[e] = *reinterpret_cast<const uint32_t*>(&r);
+            for (int h = 0; h < 2; h++) {
+                const uint4 y = key < live ? __ldcg(src + (8 * h + p) * kKeys) : make_uint4(0u, 0u, 0u, 0u);
+                x[h][0] = y.x;
+                x[h][1] = y.y;
+                x[h][2] = y.z;
+                x[h][3] = y.w;
+            }
         }
-        uint4* d = (kv ? ta.wide_v : ta.wide_k) + (tile * kKeys + key) * 16 + 2 * p;
-        d[0] = make_uint4(x[0], x[1], x[2], x[3]);
-        d[1] = make_uint4(x[4], x[5], x[6], x[7]);
+        uint4* d = (kv ? ta.wide_v : ta.wide_k) + (tile * kKeys + key) * 16 + p;
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const __half2 by = __float2half2_rn(of[h]);
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&x[h][e]), by);
+                x[h][e] = *reinterpret_cast<const uint32_t*>(&r);
+            }
+            d[8 * h] = make_uint4(x[h][0], x[h][1], x[h][2], x[h][3]);
+        }
     }
 }
 
