@@ -455,7 +455,8 @@ __global__ void __launch_bounds__(kAppendThreads, 3) cache_append4_kernel(const 
     const long long group = static_cast<long long>(blockIdx.x) * (kAppendThreads / kGroup) + threadIdx.x / kGroup, four = group / kNear;
     const int chunk = static_cast<int>(four % a.chunks);
     const long long token = four / a.chunks * kNear + group % kNear;
-    const Place at = place_of(a, static_cast<int>(token / a.R), static_cast<int>(token % a.R), j == 0);
+    const bool there = token < static_cast<long long>(a.nseq) * a.R;  // (the last four may be fewer)
+    const Place at = place_of(a, there ? static_cast<int>(token / a.R) : a.nseq, static_cast<int>(token % a.R), j == 0);
     if (!__any_sync(kFull, at.use)) return;
     const int h0 = chunk * a.heads, h1 = min(h0 + a.heads, a.Hkv);
     uint4 next[4];
