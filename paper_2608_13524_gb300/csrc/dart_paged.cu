@@ -317,36 +317,31 @@ __global__ void __launch_bounds__(32 * rows_warps(kType, kN), 1)
         const int key = load.chunk * kKeys + ((lane & (segs - 1)) << seg_log2);
         page = key < load.len ? page_at(key) : -2;
     };
-    auto issue = [&]() {  // loads the chunk at `load`
+    auto issue = [&]() {  // loads the chunk at `load`: a lane a page
         const int st = fills.stage(fills.filled);
         if (lane == 0) mbar_arrive_expect_tx(bar + st, 2 * kTile + 2 * kKeys * G_::kScale);
-        const int off = (load.chunk * kKeys) & page_mask;
-#pragma unroll
-        for (int h = 0; h < kKeys / 16; h++) {
-            if (h >= segs) break;
-            const int pg = __shfl_sync(kFull, page, h);
-            if (lane == 0) {
-                uint8_t* k = ring + st * 2 * kTile + (h << seg_log2) * kRow;
-                uint8_t* v = k + kTile;
-                const bool there = pg >= 0 && pg < a.num_pages;
-                if (!there && pg != -2 && a.status) atomicOr(a.status, kDevBounds);
-                const int from = there ? ((pg * a.Hkv + load.head) << a.page_log2) + off : 0;
-                const int row = there ? from : pool_rows;  // past the pool: zeros
-                tma_load_2d(k, &tmK, bar + st, 0, row, policy);
-                tma_load_2d(v, &tmV, bar + st, 0, row, policy);
-                if (kF16) {
-                    float* sc = scales + st * 2 * kKeys + (h << seg_log2);
-                    bulk_load(sc, a.ks + from, 4u << seg_log2, bar + st);
-                    bulk_load(sc + kKeys, a.vs + from, 4u << seg_log2, bar + st);
-                    if (kFour) {
-                        uint8_t* bl = blocks + (st * 2 * kKeys + (h << seg_log2)) * kBlocks;
-                        bulk_load(bl, a.kb + static_cast<long long>(from) * kBlocks, static_cast<uint32_t>(kBlocks) << seg_log2, bar + st);
-                        bulk_load(bl + kKeys * kBlocks, a.vb + static_cast<long long>(from) * kBlocks, static_cast<uint32_t>(kBlocks) << seg_log2, bar + st);
-                    }
-                } else {
-                    tma_load_2d(k + kTile / 2, &tmK, bar + st, 64, row, policy);
-                    tma_load_2d(v + kTile / 2, &tmV, bar + st, 64, row, policy);
+        __syncwarp();
+        if (lane < segs) {
+            uint8_t* k = ring + st * 2 * kTile + (lane << seg_log2) * kRow;
+            uint8_t* v = k + kTile;
+            const bool there = page >= 0 && page < a.num_pages;
+            if (!there && page != -2 && a.status) atomicOr(a.status, kDevBounds);
+            const int from = there ? ((page * a.Hkv + load.head) << a.page_log2) + ((load.chunk * kKeys) & page_mask) : 0;
+            const int row = there ? from : pool_rows;  // past the pool: zeros
+            tma_load_2d(k, &tmK, bar + st, 0, row, policy);
+            tma_load_2d(v, &tmV, bar + st, 0, row, policy);
+            if (kF16) {
+                float* sc = scales + st * 2 * kKeys + (lane << seg_log2);
+                bulk_load(sc, a.ks + from, 4u << seg_log2, bar + st);
+                bulk_load(sc + kKeys, a.vs + from, 4u << seg_log2, bar + st);
+                if (kFour) {
+                    uint8_t* bl = blocks + (st * 2 * kKeys + (lane << seg_log2)) * kBlocks;
+                    bulk_load(bl, a.kb + static_cast<long long>(from) * kBlocks, static_cast<uint32_t>(kBlocks) << seg_log2, bar + st);
+                    bulk_load(bl + kKeys * kBlocks, a.vb + static_cast<long long>(from) * kBlocks, static_cast<uint32_t>(kBlocks) << seg_log2, bar + st);
                 }
+            } else {
+                tma_load_2d(k + kTile / 2, &tmK, bar + st, 64, row, policy);
+                tma_load_2d(v + kTile / 2, &tmV, bar + st, 64, row, policy);
             }
         }
         fills.filled++;
