@@ -218,6 +218,14 @@ __device__ __forceinline__ uint32_t swz(int row, int piece) {  // byte offset in
     return static_cast<uint32_t>(row * 128 + ((piece ^ (row & 7)) << 4));
 }
 
+// The unit that a warp comes to next and the places of its share from there on: in shared
+// memory, for want of registers.
+template <int kType, int kN>
+struct NextUnit {
+    Place<kType, kN> at;
+    long long left;
+};
+
 template <int kType, int kN>
 struct Geo {
     static constexpr int kKeys = Chunk<kType, kN>::kKeys;
@@ -230,7 +238,8 @@ struct Geo {
     static constexpr int kScale = (kType == DART_KV_BF16 ? 0 : 4) + (kType == DART_KV_E2M1 ? kBlocks : 0);
     static constexpr int kScales = kWarps * kStages * 2 * kKeys * kScale;
     static constexpr int kTurns = kWarps * (kHeadDim / 2) * 8;            // a position's angles, of each warp
-    static constexpr int kSmem = kRing + kScales + kTurns + kWarps * kStages * 8;
+    static constexpr int kBars = kWarps * kStages * 8;
+    static constexpr int kSmem = kRing + kScales + kTurns + kBars + kWarps * static_cast<int>(sizeof(NextUnit<kType, kN>));
 };
 
 // 16-byte piece (8 bf16) of a row of the head that step pair i of thread t
@@ -277,14 +286,17 @@ __global__ void __launch_bounds__(32 * rows_warps(kType, kN), 1)
     const int share = warp * gridDim.x + blockIdx.x;
     const Shares shares(list.all, kWarps * gridDim.x, min_share(kKeys));
     if (share >= shares.count) return;
-    long long left = shares.length(share);  // places of this share not yet worked on
-    Place<kType, kN> use = list.find(a, shares.begin(share), lane), load = use;
+    Place<kType, kN> load = list.find(a, shares.begin(share), lane);
+    int to_load = load.s < a.nseq ? shares.length(share) : 0;  // places of this share not yet loaded
+    NextUnit<kType, kN>& next = reinterpret_cast<NextUnit<kType, kN>*>(smem + G_::kRing + G_::kScales + G_::kTurns + G_::kBars)[warp];
     if (lane == 0) {
-        a.plan->places[share] = make_int4(use.s, use.head, use.chunk, use.chunks);
-        a.plan->nodes[share] = use.nodes;
+        a.plan->places[share] = make_int4(load.s, load.head, load.chunk, load.chunks);
+        a.plan->nodes[share] = load.nodes;
         if (share == 0) a.plan->count = shares.count;
+        next.at = load;
+        next.left = to_load;
     }
-    long long to_load = load.s < a.nseq ? left : 0;  // places not yet loaded
+    __syncwarp();
     StageRing<kStages> fills;
     bool failed = false;
     int none = 0;
@@ -353,13 +365,19 @@ __global__ void __launch_bounds__(32 * rows_warps(kType, kN), 1)
     while (to_load > 0 && fills.room()) issue();
 
     // (s: in case the lengths change under the call, which leaves its results open)
-    while (left > 0 && use.s < a.nseq) {
+    while (next.left > 0 && next.at.s < a.nseq) {
         // ---- this warp's part of a unit: chunks [c0, c1)
-        const int c0 = use.chunk, c1 = static_cast<int>(min(static_cast<long long>(use.chunks), c0 + left));
-        const int s = use.s, head = use.head, len = use.len, nodes = use.nodes, ctx_chunks = use.ctx_chunks, chunks = use.chunks;
+        const int c0 = next.at.chunk, chunks = next.at.chunks, c1 = static_cast<int>(min(static_cast<long long>(chunks), c0 + next.left));
+        const int s = next.at.s, head = next.at.head, len = next.at.len, nodes = next.at.nodes, ctx_chunks = next.at.ctx_chunks;
         const long long seq_row = static_cast<long long>(s) * (a.B + 1);
-        left -= use.cost - c0;
-        use.next_unit(a);
+        __syncwarp();
+        if (lane == 0) {
+            Place<kType, kN> p = next.at;
+            next.left -= p.cost - c0;
+            p.next_unit(a);
+            next.at = p;
+        }
+        __syncwarp();
         if (c0 >= c1) continue;  // (the part of a unit's length that stands for its other costs)
 
         // Single tokens all have the position `len`: its angles once, two a lane, instead of
