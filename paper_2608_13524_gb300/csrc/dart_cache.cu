@@ -40,7 +40,8 @@ constexpr int kGroup = 8;  // threads of a token's head: 8 elements of each half
 // Four heads a group (angles once for four) where that still makes this many
 // groups, else one: a few tokens are a matter of latency (eight prompts of up to
 // 4096 tokens to e4m3 pages 39.8 us with four, 67 % of the copy bandwidth, and 49.9
-// with one, to bf16 pages 40.4 and 44.1; below, no difference).
+// with one, to bf16 pages 40.4 and 44.1, to e2m1 pages and read back 78 and 103; below, no
+// difference or, for the rows that eight rounds kept, 9.3 us with one and 12.4 with four).
 constexpr long long kManyGroups = 9728;  // 152 SMs x 64 groups = 512 threads each
 constexpr float kMinScale = 7.52316384526264005e-37f;  // 2^-120: its reciprocal is finite
 constexpr float kSmallScale = 8.27180612553027675e-25f, kSmallUp = 1.152921504606846976e18f;  // 2^-80, 2^60

@@ -164,7 +164,8 @@ struct List {
 };
 
 // Shares: one per warp, each at least this long (values around it make no
-// difference: shares are shorter than that in the smallest calls alone).
+// difference: shares are shorter than that in the smallest calls alone).  Chunks of 64
+// keys: one token over 500 12.8 us with 1, 14.9 with 2.
 constexpr int min_share(int chunk_keys) { return chunk_keys == 64 ? 1 : 2; }
 
 // ------------------------------------------------------------ fragments

@@ -1495,7 +1495,8 @@ int launch_paged_tiles(PagedArgs a, const dart_kv_cache& cache, uint8_t* workspa
         tmSk = tmK;  // (side tiles lie among the others)
         tmSv = tmV;
     }
-    // Four tree rows a block where that leaves every SM a block.
+    // Four tree rows a block where that leaves every SM a block (one tree of 300 nodes over 2048 keys, four /
+    // one a block: 40.5 / 36.4 us; eight of 512 over up to 4096 246 / 251).
     const bool four = static_cast<long long>(a.nseq) * (a.B + 1) >= 4 * sms;
     const int tree_blocks = four ? (a.B + 4) / 4 : a.B + 1;
     // up to 127 cache tokens before the tree rows and, in bf16, up to 127 rows of zeros after them
