@@ -50,6 +50,8 @@ RUNS = [
     (9001, 16, 3, 4000, 20, 30000),
     (40000, 16, 300, 257, 12, 3000),
     (33000, 128, 1500, 20, 10, 1000),
+    (4096, 16, 60, 120, 25, 900),
+    (4000, 32, 16, 400, 25, 5000),
 ]
 
 
