@@ -9,6 +9,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstdint>
 
 #include "../../include/dart.h"
@@ -31,6 +32,22 @@ bool valid_cache_pointers(const dart_kv_cache* c) {
     if (!ok(c->k) || !ok(c->v)) return false;
     if (c->dtype == DART_KV_BF16) return !c->k_scale && !c->v_scale;
     return ok(c->k_scale) && ok(c->v_scale) && (c->dtype != DART_KV_E2M1 || (ok(c->k_block) && ok(c->v_block)));
+}
+
+int check_device() {
+    static std::atomic<int> known[64];  // 1: sm_103a, 2: another
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return DART_ERR_CUDA;
+    int k = known[dev].load(std::memory_order_relaxed);
+    if (k == 0) {
+        int major = 0, minor = 0;
+        if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+            cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess)
+            return DART_ERR_CUDA;
+        k = major == 10 && minor == 3 ? 1 : 2;
+        known[dev].store(k, std::memory_order_relaxed);
+    }
+    return k == 1 ? DART_OK : DART_ERR_UNSUPPORTED;
 }
 
 namespace {
@@ -672,14 +689,6 @@ __global__ void __launch_bounds__(kCopyThreads) cache_copy_kernel(const __grid_c
     }
 }
 
-// 0: an sm_103a device is the current one.
-int check_device() {
-    int dev = 0, major = 0, minor = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess)
-        return DART_ERR_CUDA;
-    return major == 10 && minor == 3 ? DART_OK : DART_ERR_UNSUPPORTED;
-}
 bool aligned(const void* p, uintptr_t n) { return p && (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
 }  // namespace

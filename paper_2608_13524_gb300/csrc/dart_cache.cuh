@@ -10,6 +10,8 @@
 
 namespace dart {
 
+int check_device();  // DART_OK: the current device is an sm_103a one
+
 constexpr int kHeadDim = 128;
 constexpr int kBlockDim = 16, kBlocks = kHeadDim / kBlockDim;  // elements of a block scale (e2m1), block scales of a row
 

@@ -787,36 +787,36 @@ __global__ void __launch_bounds__(32 * rows_warps(kType, kN), 1)
                                     for (int n = 0; n < kN; n++) mma_f16(acc[n][2 * j + odd], both, p[n][0], p[n][1]);
                                 }
                             }
-                            continue;
-                        }
-                        uint32_t x[2][2][4];
+                        } else {
+                            uint32_t x[2][2][4];
 #pragma unroll
-                        for (int qq = 0; qq < 2; qq++)
+                            for (int qq = 0; qq < 2; qq++)
 #pragma unroll
-                            for (int e = 0; e < 2; e++) {
-                                const uint4 y = *reinterpret_cast<const uint4*>(vt + swz(16 * u + slot_row(qq, 2 * t + e), g));
-                                x[qq][e][0] = y.x;
-                                x[qq][e][1] = y.y;
-                                x[qq][e][2] = y.z;
-                                x[qq][e][3] = y.w;
-                            }
-#pragma unroll
-                        for (int w = 0; w < 2; w++)
-#pragma unroll
-                            for (int b = 0; b < 2; b++) {
-                                // elements 4 w + 2 b, + 1 of piece g (words w), and 8 further (words 2 + w), of
-                                // both keys of a pair
-                                const uint32_t sel = b ? 0x7362 : 0x5140;
-                                const uint32_t v0 = __byte_perm(x[0][0][w], x[0][1][w], sel), v1 = __byte_perm(x[0][0][2 + w], x[0][1][2 + w], sel);
-                                const uint32_t v2 = __byte_perm(x[1][0][w], x[1][1][w], sel), v3 = __byte_perm(x[1][0][2 + w], x[1][1][2 + w], sel);
-                                const uint32_t first[4] = {codes_lo(v0), codes_lo(v1), codes_lo(v2), codes_lo(v3)};
-                                const uint32_t second[4] = {codes_hi(v0), codes_hi(v1), codes_hi(v2), codes_hi(v3)};
-#pragma unroll
-                                for (int n = 0; n < kN; n++) {
-                                    mma_f16(acc[n][4 * w + 2 * b], first, p[n][0], p[n][1]);
-                                    mma_f16(acc[n][4 * w + 2 * b + 1], second, p[n][0], p[n][1]);
+                                for (int e = 0; e < 2; e++) {
+                                    const uint4 y = *reinterpret_cast<const uint4*>(vt + swz(16 * u + slot_row(qq, 2 * t + e), g));
+                                    x[qq][e][0] = y.x;
+                                    x[qq][e][1] = y.y;
+                                    x[qq][e][2] = y.z;
+                                    x[qq][e][3] = y.w;
                                 }
-                            }
+#pragma unroll
+                            for (int w = 0; w < 2; w++)
+#pragma unroll
+                                for (int b = 0; b < 2; b++) {
+                                    // elements 4 w + 2 b, + 1 of piece g (words w), and 8 further (words 2 + w), of
+                                    // both keys of a pair
+                                    const uint32_t sel = b ? 0x7362 : 0x5140;
+                                    const uint32_t v0 = __byte_perm(x[0][0][w], x[0][1][w], sel), v1 = __byte_perm(x[0][0][2 + w], x[0][1][2 + w], sel);
+                                    const uint32_t v2 = __byte_perm(x[1][0][w], x[1][1][w], sel), v3 = __byte_perm(x[1][0][2 + w], x[1][1][2 + w], sel);
+                                    const uint32_t first[4] = {codes_lo(v0), codes_lo(v1), codes_lo(v2), codes_lo(v3)};
+                                    const uint32_t second[4] = {codes_hi(v0), codes_hi(v1), codes_hi(v2), codes_hi(v3)};
+#pragma unroll
+                                    for (int n = 0; n < kN; n++) {
+                                        mma_f16(acc[n][4 * w + 2 * b], first, p[n][0], p[n][1]);
+                                        mma_f16(acc[n][4 * w + 2 * b + 1], second, p[n][0], p[n][1]);
+                                    }
+                                }
+                        }
                     }
                 } else {
                     values_bf16(sc[0], [&](int half, int qq, int e) {

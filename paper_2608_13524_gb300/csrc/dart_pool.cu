@@ -18,6 +18,7 @@
 
 #include "../../include/dart.h"
 #include "../../include/dart_cache.h"
+#include "dart_cache.cuh"
 #include "dart_device.cuh"
 #include "dart_kernels.h"
 
@@ -439,11 +440,7 @@ int pool_args(const dart_page_pool* pool, const void* lens, bool needs_lens, con
     if ((needs_lens && !aligned(lens, 4)) || (status && !aligned(status, 4))) return DART_ERR_INVALID;
     const PoolWs w = pool_ws(*pool);
     if (needs_ws && (!aligned(workspace, 256) || bytes < w.total)) return DART_ERR_INVALID;
-    int dev = 0, major = 0, minor = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess)
-        return DART_ERR_CUDA;
-    if (major != 10 || minor != 3) return DART_ERR_UNSUPPORTED;
+    if (const int rc = check_device()) return rc;
     *a = PoolArgs{};
     a->num_pages = pool->num_pages;
     while ((1 << a->page_log2) < pool->page_size) a->page_log2++;
