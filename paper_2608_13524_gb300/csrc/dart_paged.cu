@@ -86,11 +86,13 @@ __host__ __device__ constexpr int rows_warps(int type, int n) { return n > 1 ? 8
 // up to 1024 e4m3 keys 56.5 us at 1, 54 at 2, 55.5 at 3, 56.5 at 6; bf16 97 at 2, 95 at
 // 3 to 7, 97 at 9).  kUnitCost: 64 trees of 3 nodes over 4096 keys, bf16 105 us at 3,
 // 100 at 6, 98 at 9; e4m3 71, 65, 65 at 2, 4, 6.  Chunks of 64 keys: half of that (1024
-// sequences of up to 512 e2m1 keys, kTokenCost 1 162 us, 2 166).
+// sequences of up to 512 e2m1 keys, kTokenCost 1 162 us, 2 166; trees of 3 nodes, kUnitCost 2,
+// 4, 6: 64 over up to 1000 keys 42, 41, 41 us, 16 over up to 16384 64, 65, 66).  Chunks of 32 e2m1
+// keys for up to 16 rows: 40, 75.
 template <int kType, int kN>
 struct Chunk {
-    static constexpr int kKeys = kType == DART_KV_BF16 ? 16 : kType == DART_KV_E2M1 && kN == 1 ? 64 : 32;
-    static constexpr int kUnitCost = kType == DART_KV_BF16 ? 9 : kKeys == 64 ? 3 : 6, kTokenCost = kType == DART_KV_BF16 ? 5 : kKeys == 64 ? 1 : 2;
+    static constexpr int kKeys = kType == DART_KV_BF16 ? 16 : kType == DART_KV_E2M1 ? 64 : 32;
+    static constexpr int kUnitCost = kType == DART_KV_BF16 ? 9 : kKeys == 64 ? (kN == 1 ? 3 : 4) : 6, kTokenCost = kType == DART_KV_BF16 ? 5 : kKeys == 64 ? 1 : 2;
 };
 
 // A place in the list of chunks: sequence, kv head, chunk of the unit.
@@ -233,7 +235,7 @@ struct Geo {
     static constexpr int kSubs = kKeys / 16;                             // products of 16 keys
     static constexpr int kTile = kKeys * row_bytes(kType);               // K or V of a chunk
     static constexpr int kWarps = rows_warps(kType, kN), kThreads = 32 * kWarps;
-    static constexpr int kStages = kType == DART_KV_E2M1 ? (kN == 1 ? 2 : 4) : kN == 1 ? 2 : 3;
+    static constexpr int kStages = kType == DART_KV_E2M1 ? 2 : kN == 1 ? 2 : 3;
     static constexpr int kRing = kWarps * kStages * 2 * kTile;           // 192 KB (e2m1: 176, 128)
     // e4m3, e2m1: a key's scale; e2m1: its block scales
     static constexpr int kScale = (kType == DART_KV_BF16 ? 0 : 4) + (kType == DART_KV_E2M1 ? kBlocks : 0);
