@@ -1071,8 +1071,8 @@ bool valid_cfg(const dart_paged_attn_config* c, const dart_kv_cache* cache) {
 }
 
 // Which kernel: a few rows are streamed from HBM, more are 128-row tiles of the
-// tensor-memory path (64 sequences, 16 rows a kv head, 4096 keys: 98 us here and
-// 134 there with bf16 pages, 65 and 225 with e4m3 ones).
+// tensor-memory path (64 sequences, 16 rows a kv head, 4096 keys, here and there: bf16
+// pages 99 and 106 us, e4m3 71 and 135, e2m1 80 and 134).
 constexpr int kFewRows = 16;
 bool few_rows(const dart_paged_attn_config& c, const dart_kv_cache& cache) { return (c.B + 1) * (c.Hq / cache.Hkv) <= kFewRows; }
 
