@@ -201,6 +201,10 @@ size_t dart_paged_attention_workspace(const dart_paged_attn_config *cfg, const d
  * if B = 0).  Nothing is written to the cache: dart_cache_append writes the
  * rows that the pass keeps.  Every key and value in use must be finite;
  * slots past lens[s] and rows past n_nodes[s] may hold anything.
+ * Over pages of codes values are weighed in f16, so those that lie far (2^-20
+ * and beyond) below the largest of their head and sequence keep fewer bits; rows
+ * of zeros (e2m1: whose block scales are all 0) count for nothing there, whatever
+ * their scale is.
  *   workspace: 256-byte aligned, used by this call only until the stream
  *   reaches its end (no state is kept between calls); two calls that may run
  *   at the same time need one each.

@@ -75,6 +75,12 @@ __device__ __forceinline__ uint32_t e4m3_f16(uint32_t two) {
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(static_cast<uint16_t>(two)));
     return r;
 }
+// Whether a row of codes has an element that is not 0, as far as that can be seen at little
+// cost: from an e2m1 row's block scales, from all e4m3 codes (bits of some, or'ed).  A row of
+// zeros may have any scale (1 where the cache writes left it), so it must have no part in
+// what other rows are measured by: beside values of 2^-13 it would leave their f16 weights 2^-23.
+__device__ __forceinline__ bool e2m1_in_use(const uint2& blocks) { return ((blocks.x | blocks.y) & 0x7F7F7F7Fu) != 0u; }
+__device__ __forceinline__ uint32_t e4m3_bits(const uint4& x) { return (x.x | x.y | x.z | x.w) & 0x7F7F7F7Fu; }
 // Products of f16 pairs (of an e2m1 code and a block scale: at most 6 significant
 // bits between 2^-10 and 2688, exact).
 __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {

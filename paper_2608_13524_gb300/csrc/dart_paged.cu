@@ -217,10 +217,6 @@ __device__ __forceinline__ int slot_row(int q, int n) {
 // slot_row4(q, g), piece g of rows slot_row4(q, 2t + e).
 __device__ __forceinline__ int slot_row4(int q, int n) { return q * 8 + (((n ^ (n >> 2)) & 1) << 2) + ((n >> 2) << 1) + ((n >> 1) & 1); }
 
-__device__ __forceinline__ uint32_t swz(int row, int piece) {  // byte offset in a tile of 128-byte rows
-    return static_cast<uint32_t>(row * 128 + ((piece ^ (row & 7)) << 4));
-}
-
 // The unit that a warp comes to next and the places of its share from there on: in shared
 // memory, for want of registers.
 template <int kType, int kN>
@@ -725,21 +721,42 @@ __global__ void __launch_bounds__(32 * rows_warps(kType, kN), 1)
                                 vs[j][qq] = 0.0f;
                             }
                 }
-                if (kF16) {
+                if constexpr (kF16) {
                     float top = 0.0f;
 #pragma unroll
                     for (int j = 0; j < kSubs; j++) top = fmaxf(top, fmaxf(vs[j][0], vs[j][1]));
                     if (__any_sync(kFull, top > vref)) {
+                        // (rare) Rows of zeros have no part in it.  Of e4m3 codes one of the largest
+                        // scale's rows is looked at first: the rest is code that is not at hand.
                         top = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(top)));  // (not negative)
-                        const float raised = __uint_as_float(min(max(__float_as_uint(top) >> 23, 27u), 252u) + 1u << 23);
-                        const float alpha = vref / raised;
-                        vref = raised;
+                        bool look = kFour;
+                        if (!kFour) {
+                            int row = -1;
 #pragma unroll
-                        for (int n = 0; n < kN; n++)
+                            for (int j = 0; j < kSubs; j++)
 #pragma unroll
-                            for (int j = 0; j < 8; j++)
+                                for (int qq = 0; qq < 2; qq++)
+                                    if (vs[j][qq] == top) row = 16 * j + row_of(qq, g);
+                            look = !e4m3_row_in_use(vt, __shfl_sync(kFull, row, __ffs(__ballot_sync(kFull, row >= 0)) - 1), lane);
+                        }
+                        if (look) {
+                            top = 0.0f;
+#pragma unroll 1
+                            for (int row = lane; row < kKeys; row += 32)
+                                if (row_in_use<kType>(vt, blk + kKeys * kBlocks, row)) top = fmaxf(top, sck[kKeys + row]);
+                            top = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(top)));
+                        }
+                        if (top > vref) {
+                            const float raised = __uint_as_float(min(max(__float_as_uint(top) >> 23, 27u), 252u) + 1u << 23);
+                            const float alpha = vref / raised;
+                            vref = raised;
 #pragma unroll
-                                for (int e = 0; e < 4; e++) acc[n][j][e] *= alpha;
+                            for (int n = 0; n < kN; n++)
+#pragma unroll
+                                for (int j = 0; j < 8; j++)
+#pragma unroll
+                                    for (int e = 0; e < 4; e++) acc[n][j][e] *= alpha;
+                        }
                     }
                 }
                 soften(sc);
@@ -747,7 +764,7 @@ __global__ void __launch_bounds__(32 * rows_warps(kType, kN), 1)
                     const float inv = vref > 0.0f ? 128.0f / vref : 0.0f;  // (0: all scales are)
 #pragma unroll
                     for (int u = 0; u < kSubs; u++) {
-                        const float w0 = vs[u][0] * inv, w1 = vs[u][1] * inv;
+                        const float w0 = fminf(vs[u][0] * inv, 128.0f), w1 = fminf(vs[u][1] * inv, 128.0f);  // (more: rows of zeros)
                         uint32_t p[kN][2];
 #pragma unroll
                         for (int n = 0; n < kN; n++) {

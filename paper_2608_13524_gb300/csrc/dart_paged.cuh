@@ -79,9 +79,25 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 
-// Byte offset of 16-byte piece `piece` of a row in a tile of 64-byte rows.
+// Byte offset of 16-byte piece `piece` of a row in a tile of 128-byte rows, of 64-byte rows.
+__device__ __forceinline__ uint32_t swz(int row, int piece) {
+    return static_cast<uint32_t>(row * 128 + ((piece ^ (row & 7)) << 4));
+}
 __device__ __forceinline__ uint32_t swz64(int row, int piece) {
     return static_cast<uint32_t>(row * 64 + ((piece ^ ((row >> 1) & 3)) << 4));
+}
+
+// The same of a row of a tile in shared memory: by one thread, and of e4m3 codes by a warp.
+template <int kType>
+__device__ __forceinline__ bool row_in_use(const uint8_t* tile, const uint8_t* blocks, int row) {
+    if (kType == DART_KV_E2M1) return e2m1_in_use(*reinterpret_cast<const uint2*>(blocks + row * kBlocks));
+    uint32_t any = 0;
+#pragma unroll
+    for (int c = 0; c < 8; c++) any |= e4m3_bits(*reinterpret_cast<const uint4*>(tile + swz(row, c)));
+    return any != 0u;
+}
+__device__ __forceinline__ bool e4m3_row_in_use(const uint8_t* tile, int row, int lane) {
+    return __any_sync(kFull, (*reinterpret_cast<const uint32_t*>(tile + row * kHeadDim + 4 * lane) & 0x7F7F7F7Fu) != 0u);
 }
 
 bool valid_cache(const dart_kv_cache* c);

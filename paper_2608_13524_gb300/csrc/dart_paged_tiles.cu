@@ -233,8 +233,8 @@ __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_c
         if (kF16) {
             // a warp a head's keys or values: 16 tokens by 2 of their 8 blocks of 16 elements at a time
             const int warp = tid >> 5, token = tid & 15, first = (tid >> 4) & 1;
-            if (j0 + token >= j_end) return;
-            const int row0 = row_of[token];
+            const bool in = j0 + token < j_end;  // (whole warps stay together)
+            const int row0 = in ? row_of[token] : -1;
             for (int i = warp; i < 2 * a.Hkv; i += kPrepThreads / 32) {
                 const int kv = i >= a.Hkv, head = i - kv * a.Hkv, j = j0 + token;
                 const long long row = row0 + (static_cast<long long>(head) << a.page_log2);
@@ -256,7 +256,12 @@ __global__ void __launch_bounds__(kPrepThreads) paged_prep_kernel(const __grid_c
                         x[e] = ld_plain(reinterpret_cast<const uint4*>(src) + c);
                     }
                 }
-                if (first == 0) *side_scale(kv, head, j) = row0 >= 0 ? ld_plain((kv ? a.vs : a.ks) + row) : 0.0f;
+                uint32_t any = 0;  // (a row of zeros has no part in the tile's power of two)
+#pragma unroll
+                for (int e = 0; e < 4; e++) any |= kType == DART_KV_E2M1 ? block[e] & 0x7Fu : e4m3_bits(x[e]);
+                any |= __shfl_xor_sync(kFull, any, 16);
+                if (!in) continue;
+                if (first == 0) *side_scale(kv, head, j) = any ? ld_plain((kv ? a.vs : a.ks) + row) : 0.0f;
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
                     uint32_t y[8];
@@ -380,6 +385,17 @@ __device__ __forceinline__ float above(float x) {
     return __uint_as_float((min(max(__float_as_uint(x) >> 23, 27u), 252u) + 1u) << 23);
 }
 
+// The warp's largest x >= 0.
+__device__ __forceinline__ float largest_of(float x) { return __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(x))); }
+// The largest scale of a tile of e4m3 codes among rows that are not all 0.  By a warp.
+__device__ __noinline__ float largest_in_use(const uint8_t* tile, const float* scales) {
+    float most = 0.0f;
+#pragma unroll 1
+    for (int row = threadIdx.x & 31; row < kKeys; row += 32)
+        if (row_in_use<DART_KV_E4M3>(tile, nullptr, row)) most = fmaxf(most, scales[row]);
+    return largest_of(most);
+}
+
 // ------------------------------------------------------------ e4m3 or e2m1 pages as f16 tiles
 
 // One block per tile of a sequence and kv head (whole cache tiles, then side
@@ -390,6 +406,7 @@ __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant_
     __shared__ float scale_of[2 * kKeys];
     __shared__ int row_of[kKeys];  // of the pool; -1: no such page
     __shared__ float top_of[8];
+    __shared__ bool used[2 * kKeys];
     const PagedArgs& a = ta.p;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int head = blockIdx.x % a.Hkv, s = blockIdx.x / a.Hkv, t = blockIdx.y;
@@ -439,6 +456,20 @@ __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant_
             sc = key < live ? __ldcg((kv ? ta.side_vs : ta.side_ks) + side + key) : 0.0f;
         else if (row_of[key] >= 0)
             sc = ld_plain((kv ? a.vs : a.ks) + row_of[key]);
+        if (cache_tile) {
+            // rows of zeros have no part in the powers of two
+#pragma unroll
+            for (int i = 0; i < kRounds; i++) {
+                if (kType == DART_KV_E2M1) {  // (the same in all lanes of the row)
+                    if (p == 0) used[i * 32 + group] = e2m1_in_use(make_uint2(c[i].z, c[i].w));
+                } else {
+                    const unsigned rows = __ballot_sync(kFull, e4m3_bits(c[i]) != 0u);
+                    if (p == 0) used[i * 32 + group] = (rows >> (lane & 24) & 0xFFu) != 0u;
+                }
+            }
+            __syncthreads();
+            if (!used[tid]) sc = 0.0f;
+        }
         scale_of[tid] = sc;
         const float top = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(fmaxf(sc, 0.0f))));
         if (lane == 0) top_of[warp] = top;
@@ -681,8 +712,6 @@ struct TGeo {
     static constexpr int kFirstSoft = 2, kFirstConv = kFirstSoft + kSoft / 32;
     static constexpr int kThreads = 32 * (kFirstConv + (kConv ? 4 : 0));
 };
-
-__device__ __forceinline__ uint32_t tile_swz(int row, int piece) { return static_cast<uint32_t>(row * 128 + ((piece ^ (row & 7)) << 4)); }
 
 // 8 x 8 pieces of 16 bytes, a row per lane of 8: afterwards lane j has piece j of
 // all 8 rows.
@@ -1232,6 +1261,7 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
         bool ok = true, waited = false;
         int n = 0, raw = 0;  // tiles, whole cache tiles so far
         while (ok && w.next(a)) {
+            float unit_top = 0.0f;  // the largest power of two of this part's tiles so far
             for (int t = w.t0; t < w.t1; t++, n++) {
                 const bool cache_tile = t < w.whole;
                 if (!cache_tile && !waited) {
@@ -1252,76 +1282,111 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                     auto scale = [&](int i) { return i < live ? __ldcg(of + i) : 0.0f; };
                     four = make_float4(scale(lane), scale(lane + 32), scale(lane + 64), scale(lane + 96));
                 }
-                const float most = fmaxf(max3(four.x, four.y, four.z), fmaxf(four.w, 0.0f));
-                const float ref = above(__uint_as_float(__reduce_max_sync(kFull, __float_as_uint(most))));
+                auto largest = [&]() { return largest_of(fmaxf(max3(four.x, four.y, four.z), fmaxf(four.w, 0.0f))); };
+                float top = largest();
+                ok = soon(&op_empty[st], (static_cast<uint32_t>(n / kStages) & 1u) ^ 1u, abort);
+                if (!ok) break;
+                if (cache_tile && top >= unit_top) {
+                    // (once a part, mostly) Rows of zeros have no part in it.  Of e4m3 codes one row of the
+                    // largest scale is looked at first: 64 trees of 32 rows over up to 4096 keys 142 us
+                    // without any of this, 146 with it, 151 where all rows are looked at.
+                    if (kFour) {
+                        const uint4* of = reinterpret_cast<const uint4*>(raw_blocks + ((kv * G_::kRawK + rs) * kKeys + 4 * lane) * kBlocks);
+                        const uint4 x = of[0], y = of[1];
+                        if (!e2m1_in_use(make_uint2(x.x, x.y))) four.x = 0.0f;
+                        if (!e2m1_in_use(make_uint2(x.z, x.w))) four.y = 0.0f;
+                        if (!e2m1_in_use(make_uint2(y.x, y.y))) four.z = 0.0f;
+                        if (!e2m1_in_use(make_uint2(y.z, y.w))) four.w = 0.0f;
+                        top = largest();
+                    } else {
+                        const int place = four.x == top ? 0 : four.y == top ? 1 : four.z == top ? 2 : four.w == top ? 3 : 4;
+                        const int row = __ffs(__ballot_sync(kFull, place < 4)) - 1;  // (of a lane; 0 where all scales are NaN or negative)
+                        const uint8_t* tile = raw_tile + rs * G_::kRawTile;
+                        if (!e4m3_row_in_use(tile, max(4 * row + __shfl_sync(kFull, place, max(row, 0)), 0) & (kKeys - 1), lane)) top = largest_in_use(tile, scale_of);
+                    }
+                }
+                const float ref = above(top);
+                unit_top = fmaxf(unit_top, ref);
                 if (row0 == 0) {
                     (kv ? tile_ref[n % G_::kRing].y : tile_ref[n % G_::kRing].x) = ref;
                     mbar_arrive(&sc_full[n % G_::kRing]);
                 }
-                ok = soon(&op_empty[st], (static_cast<uint32_t>(n / kStages) & 1u) ^ 1u, abort);
-                if (!ok) break;
                 const float inv = __uint_as_float(0x7F000000u - __float_as_uint(ref));  // 1 / ref
-#pragma unroll 1
-                for (int row = row0; row < kKeys; row += 64) {
-                    const float sc = cache_tile ? scale_of[row] : row < live ? __ldcg(side_scale + side + row) : 0.0f;
-                    // the key's scale over the common power of two, at most 1, rounded to f16: that
-                    // moves the key's scores or its values by 2^-12 of themselves at most, as
-                    // much as the rounding of an operand does
-                    const __half2 by = __float2half2_rn(sc * inv);
-                    auto times = [&](uint32_t x) {
-                        const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&x), by);
-                        return *reinterpret_cast<const uint32_t*>(&r);
-                    };
+                if (kFour && cache_tile) {
+                    // codes times (block scale * scale over the common power of two), rounded to f16:
+                    // exact where the scale is a power of two, as the cache writes leave it.  Two
+                    // blocks at a time, the next two on their way: those trees 140 us, one of 17 rows
+                    // over 131072 keys 91; without the loop 149 and 93, one step at a time 135 and 101.
+                    const uint8_t* src = raw_tile + rs * G_::kRawTile;
+                    const uint8_t* bl = raw_blocks + (kv * G_::kRawK + rs) * kKeys * kBlocks;
                     uint8_t* dst = op_tile + st * kTile;
-                    uint4 x[8];
-                    if (kFour && cache_tile) {
-                        // codes times (block scale * scale over the common power of two), rounded to f16:
-                        // exact where the scale is a power of two, as the cache writes leave it
-                        const uint8_t* src = raw_tile + rs * G_::kRawTile;
-                        const uint2 bl = *reinterpret_cast<const uint2*>(raw_blocks + ((kv * G_::kRawK + rs) * kKeys + row) * kBlocks);
-#pragma unroll 4
-                        for (int c = 0; c < 4; c++) {  // blocks 2 c, 2 c + 1: 64 bytes
-                            const uint4 y = *reinterpret_cast<const uint4*>(src + swz64(row, c));
-                            const uint32_t wide = e4m3_f16((c < 2 ? bl.x : bl.y) >> (16 * (c & 1)));
-                            const float2 of = __half22float2(*reinterpret_cast<const __half2*>(&wide));
-                            uint8_t* d = dst + (c >> 1) * kHalf;
+                    uint4 ahead = *reinterpret_cast<const uint4*>(src + swz64(row0, 0));
+                    uint32_t b_ahead = *reinterpret_cast<const uint16_t*>(bl + row0 * kBlocks);
+                    float s_ahead = scale_of[row0];
+#pragma unroll 2
+                    for (int i = 0; i < 8; i++) {
+                        const int row = row0 + 64 * (i >> 2), c = i & 3, nr = row0 + 64 * ((i + 1) >> 2 & 1), nc = (i + 1) & 3;
+                        const uint4 y = ahead;
+                        const float part = fminf(s_ahead * inv, 1.0f);
+                        const uint32_t wide = e4m3_f16(b_ahead);
+                        ahead = *reinterpret_cast<const uint4*>(src + swz64(nr, nc));
+                        b_ahead = *reinterpret_cast<const uint16_t*>(bl + nr * kBlocks + 2 * nc);
+                        s_ahead = scale_of[nr];
+                        const float2 of = __half22float2(*reinterpret_cast<const __half2*>(&wide));
+                        uint8_t* d = dst + (c >> 1) * kHalf;
 #pragma unroll
-                            for (int e = 0; e < 2; e++) {
-                                const __half2 by = __float2half2_rn((e ? of.y : of.x) * (sc * inv));
-                                const uint32_t f = *reinterpret_cast<const uint32_t*>(&by);
-                                uint32_t lo[4], hi[4];
-                                e2m1_f16(e ? y.z : y.x, lo);
-                                e2m1_f16(e ? y.w : y.y, hi);
-                                *reinterpret_cast<uint4*>(d + tile_swz(row, (4 * c + 2 * e) & 7)) = make_uint4(mul_f16x2(lo[0], f), mul_f16x2(lo[1], f), mul_f16x2(lo[2], f), mul_f16x2(lo[3], f));
-                                *reinterpret_cast<uint4*>(d + tile_swz(row, (4 * c + 2 * e + 1) & 7)) = make_uint4(mul_f16x2(hi[0], f), mul_f16x2(hi[1], f), mul_f16x2(hi[2], f), mul_f16x2(hi[3], f));
-                            }
+                        for (int e = 0; e < 2; e++) {
+                            const __half2 by = __float2half2_rn((e ? of.y : of.x) * part);
+                            const uint32_t f = *reinterpret_cast<const uint32_t*>(&by);
+                            uint32_t lo[4], hi[4];
+                            e2m1_f16(e ? y.z : y.x, lo);
+                            e2m1_f16(e ? y.w : y.y, hi);
+                            *reinterpret_cast<uint4*>(d + swz(row, (4 * c + 2 * e) & 7)) = make_uint4(mul_f16x2(lo[0], f), mul_f16x2(lo[1], f), mul_f16x2(lo[2], f), mul_f16x2(lo[3], f));
+                            *reinterpret_cast<uint4*>(d + swz(row, (4 * c + 2 * e + 1) & 7)) = make_uint4(mul_f16x2(hi[0], f), mul_f16x2(hi[1], f), mul_f16x2(hi[2], f), mul_f16x2(hi[3], f));
                         }
-                    } else if (cache_tile) {
-                        const uint8_t* src = raw_tile + rs * G_::kRawTile;
-#pragma unroll
-                        for (int c = 0; c < 8; c++) x[c] = *reinterpret_cast<const uint4*>(src + tile_swz(row, c));
-#pragma unroll
-                        for (int c = 0; c < 8; c++) {
-                            uint8_t* d = dst + (c >> 2) * kHalf;
-                            *reinterpret_cast<uint4*>(d + tile_swz(row, (2 * c) & 7)) =
-                                make_uint4(times(e4m3_f16(x[c].x)), times(e4m3_f16(x[c].x >> 16)), times(e4m3_f16(x[c].y)), times(e4m3_f16(x[c].y >> 16)));
-                            *reinterpret_cast<uint4*>(d + tile_swz(row, (2 * c + 1) & 7)) =
-                                make_uint4(times(e4m3_f16(x[c].z)), times(e4m3_f16(x[c].z >> 16)), times(e4m3_f16(x[c].w)), times(e4m3_f16(x[c].w >> 16)));
-                        }
-                    } else {
-                        const uint4* src = side_rows + (side >> 7) * (16 * kKeys) + row;
+                    }
+                } else {
 #pragma unroll 1
-                        for (int q = 0; q < 2; q++) {
-                            if (row >= live) {
+                    for (int row = row0; row < kKeys; row += 64) {
+                        const float sc = cache_tile ? scale_of[row] : row < live ? __ldcg(side_scale + side + row) : 0.0f;
+                        // the key's scale over the common power of two, at most 1, rounded to f16: that
+                        // moves the key's scores or its values by 2^-12 of themselves at most, as
+                        // much as the rounding of an operand does (a row of zeros may have a larger one)
+                        const float part = fminf(sc * inv, 1.0f);
+                        const __half2 by = __float2half2_rn(part);
+                        auto times = [&](uint32_t x) {
+                            const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&x), by);
+                            return *reinterpret_cast<const uint32_t*>(&r);
+                        };
+                        uint8_t* dst = op_tile + st * kTile;
+                        uint4 x[8];
+                        if (cache_tile) {
+                            const uint8_t* src = raw_tile + rs * G_::kRawTile;
 #pragma unroll
-                                for (int c = 0; c < 8; c++) *reinterpret_cast<uint4*>(dst + q * kHalf + tile_swz(row, c)) = make_uint4(0u, 0u, 0u, 0u);
-                                continue;
+                            for (int c = 0; c < 8; c++) x[c] = *reinterpret_cast<const uint4*>(src + swz(row, c));
+#pragma unroll
+                            for (int c = 0; c < 8; c++) {
+                                uint8_t* d = dst + (c >> 2) * kHalf;
+                                *reinterpret_cast<uint4*>(d + swz(row, (2 * c) & 7)) =
+                                    make_uint4(times(e4m3_f16(x[c].x)), times(e4m3_f16(x[c].x >> 16)), times(e4m3_f16(x[c].y)), times(e4m3_f16(x[c].y >> 16)));
+                                *reinterpret_cast<uint4*>(d + swz(row, (2 * c + 1) & 7)) =
+                                    make_uint4(times(e4m3_f16(x[c].z)), times(e4m3_f16(x[c].z >> 16)), times(e4m3_f16(x[c].w)), times(e4m3_f16(x[c].w >> 16)));
                             }
+                        } else {
+                            const uint4* src = side_rows + (side >> 7) * (16 * kKeys) + row;
+#pragma unroll 1
+                            for (int q = 0; q < 2; q++) {
+                                if (row >= live) {
 #pragma unroll
-                            for (int c = 0; c < 8; c++) x[c] = __ldcg(src + (8 * q + c) * kKeys);
+                                    for (int c = 0; c < 8; c++) *reinterpret_cast<uint4*>(dst + q * kHalf + swz(row, c)) = make_uint4(0u, 0u, 0u, 0u);
+                                    continue;
+                                }
 #pragma unroll
-                            for (int c = 0; c < 8; c++)
-                                *reinterpret_cast<uint4*>(dst + q * kHalf + tile_swz(row, c)) = make_uint4(times(x[c].x), times(x[c].y), times(x[c].z), times(x[c].w));
+                                for (int c = 0; c < 8; c++) x[c] = __ldcg(src + (8 * q + c) * kKeys);
+#pragma unroll
+                                for (int c = 0; c < 8; c++)
+                                    *reinterpret_cast<uint4*>(dst + q * kHalf + swz(row, c)) = make_uint4(times(x[c].x), times(x[c].y), times(x[c].z), times(x[c].w));
+                            }
                         }
                     }
                 }
