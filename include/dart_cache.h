@@ -156,10 +156,19 @@ int dart_page_pool_select(const dart_page_pool *pool, const int32_t *parents, in
  * their number.  Two sequences that share a page and are both given room in it
  * get a copy each.  A sequence that the table's row or the free pages do not
  * suffice for (and, for the free pages, every later one that needs some) is
- * left as it is and sets value 8 in *status.  n_rows[s] <= 0 asks for nothing. */
+ * left as it is and sets value 8 in *status.  n_rows[s] <= 0 asks for nothing.
+ * A sequence without room must not be written to: its table still has the pages
+ * that it shares, and behind those numbers that may be other sequences' pages.
+ * dart_page_pool_reserve_rows says so on the device: granted[s] is n_rows[s] where
+ * there is room, else 0 (also where n_rows[s] < 0); it is what dart_cache_append
+ * takes as n_rows and what the caller's lens grow by (or the smaller of it and the
+ * rows that are kept).  granted may be n_rows itself. */
 int dart_page_pool_reserve(const dart_page_pool *pool, const int32_t *lens, const int32_t *n_rows, int32_t *pairs,
                            int max_pairs, int32_t *count, void *workspace, size_t workspace_bytes, int *status,
                            void *stream);
+int dart_page_pool_reserve_rows(const dart_page_pool *pool, const int32_t *lens, const int32_t *n_rows,
+                                int32_t *granted, int32_t *pairs, int max_pairs, int32_t *count, void *workspace,
+                                size_t workspace_bytes, int *status, void *stream);
 
 /* Gives back every page behind the first ceil(lens[s] / page_size) of sequence s. */
 int dart_page_pool_trim(const dart_page_pool *pool, const int32_t *lens, int *status, void *stream);

@@ -46,6 +46,7 @@ struct PoolArgs {
     int ctas;                                                // of the cluster; 1: no cluster
     int32_t *refs, *table, *held, *lens, *pairs, *count;
     const int32_t *parents, *n_rows;
+    int32_t* granted;  // may be NULL
     // workspace
     int32_t* row;    // [nseq][max_pages]: select: new rows; reserve: which entries are new
     int32_t* list;   // [num_pages]: free pages, or holes, in ascending order
@@ -63,6 +64,10 @@ __device__ __forceinline__ bool in_pool(const PoolArgs& a, int page) { return pa
 __device__ __forceinline__ int held_of(const PoolArgs& a, int s) { return min(max(__ldcg(a.held + s), 0), a.max_pages); }
 __device__ __forceinline__ int len_of(const PoolArgs& a, int s) { return min(max(__ldcg(a.lens + s), 0), a.max_pages << a.page_log2); }
 __device__ __forceinline__ int pages_of(const PoolArgs& a, int tokens) { return (tokens + (1 << a.page_log2) - 1) >> a.page_log2; }
+// Pages that sequence s has with `rows` tokens more.
+__device__ __forceinline__ long long need_of(const PoolArgs& a, int s, int rows) {
+    return (static_cast<long long>(len_of(a, s)) + rows + (1 << a.page_log2) - 1) >> a.page_log2;
+}
 
 // body(s, i0): entries i0 .. of sequence s, for every unit of the tables, by a warp.
 template <typename Body>
@@ -197,7 +202,7 @@ __global__ void __launch_bounds__(kThreads, 1) pool_reserve_kernel(const __grid_
     // what each sequence needs: a warp each
     for (int s = rank * kWarps + warp; s < a.nseq; s += a.ctas * kWarps) {
         const int len = len_of(a, s), rows = ld_plain(a.n_rows + s), have = held_of(a, s), page = 1 << a.page_log2;
-        const long long need64 = rows > 0 ? (static_cast<long long>(len) + rows + page - 1) >> a.page_log2 : 0;
+        const long long need64 = rows > 0 ? need_of(a, s, rows) : 0;
         Grant g{};
         const bool fits = need64 <= a.max_pages;
         if (!fits && lane == 0 && a.status) atomicOr(a.status, kDevNoRoom);
@@ -252,6 +257,11 @@ __global__ void __launch_bounds__(kThreads, 1) pool_reserve_kernel(const __grid_
             if (!granted && want.x > 0 && a.status) atomicOr(a.status, kDevNoRoom);
             __stcg(&a.grant[s].offset, granted && want.x > 0 ? static_cast<int>(asked) + before : -1);
             __stcg(&a.grant[s].pair_at, pair_at);
+            if (a.granted) {
+                const int rows = ld_plain(a.n_rows + s);
+                const bool room = (granted || want.x == 0) && rows > 0 && need_of(a, s, rows) <= a.max_pages;
+                a.granted[s] = room ? rows : 0;
+            }
         }
         places += ok;
         copies += pairs;
@@ -472,6 +482,18 @@ int launch_pool(void (*kernel)(PoolArgs), const PoolArgs& a, void* stream) {
     return e == cudaSuccess ? DART_OK : DART_ERR_CUDA;
 }
 
+int reserve(const dart_page_pool* pool, const int32_t* lens, const int32_t* n_rows, int32_t* granted, int32_t* pairs, int max_pairs, int32_t* count,
+            void* workspace, size_t workspace_bytes, int* status, void* stream) {
+    PoolArgs a;
+    if (!aligned(n_rows, 4) || !aligned(pairs, 8) || !aligned(count, 4) || !pool || max_pairs < pool->nseq) return DART_ERR_INVALID;
+    if (const int rc = pool_args(pool, lens, true, workspace, workspace_bytes, true, status, &a)) return rc;
+    a.n_rows = n_rows;
+    a.granted = granted;
+    a.pairs = pairs;
+    a.count = count;
+    return launch_pool(pool_reserve_kernel, a, stream);
+}
+
 }  // namespace
 }  // namespace dart
 
@@ -492,13 +514,13 @@ int dart_page_pool_select(const dart_page_pool* pool, const int32_t* parents, in
 
 int dart_page_pool_reserve(const dart_page_pool* pool, const int32_t* lens, const int32_t* n_rows, int32_t* pairs, int max_pairs,
                            int32_t* count, void* workspace, size_t workspace_bytes, int* status, void* stream) {
-    PoolArgs a;
-    if (!aligned(n_rows, 4) || !aligned(pairs, 8) || !aligned(count, 4) || !pool || max_pairs < pool->nseq) return DART_ERR_INVALID;
-    if (const int rc = pool_args(pool, lens, true, workspace, workspace_bytes, true, status, &a)) return rc;
-    a.n_rows = n_rows;
-    a.pairs = pairs;
-    a.count = count;
-    return launch_pool(pool_reserve_kernel, a, stream);
+    return reserve(pool, lens, n_rows, nullptr, pairs, max_pairs, count, workspace, workspace_bytes, status, stream);
+}
+
+int dart_page_pool_reserve_rows(const dart_page_pool* pool, const int32_t* lens, const int32_t* n_rows, int32_t* granted, int32_t* pairs,
+                                int max_pairs, int32_t* count, void* workspace, size_t workspace_bytes, int* status, void* stream) {
+    if (!aligned(granted, 4)) return DART_ERR_INVALID;
+    return reserve(pool, lens, n_rows, granted, pairs, max_pairs, count, workspace, workspace_bytes, status, stream);
 }
 
 int dart_page_pool_trim(const dart_page_pool* pool, const int32_t* lens, int* status, void* stream) {

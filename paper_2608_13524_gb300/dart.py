@@ -135,6 +135,7 @@ def lib():
             "dart_page_pool_workspace": (C.c_size_t, [C.POINTER(DartPagePool)]),
             "dart_page_pool_select": (i, [C.POINTER(DartPagePool), vp, vp, vp, C.c_size_t, vp, vp]),
             "dart_page_pool_reserve": (i, [C.POINTER(DartPagePool), vp, vp, vp, i, vp, vp, C.c_size_t, vp, vp]),
+            "dart_page_pool_reserve_rows": (i, [C.POINTER(DartPagePool), vp, vp, vp, vp, i, vp, vp, C.c_size_t, vp, vp]),
             "dart_page_pool_trim": (i, [C.POINTER(DartPagePool), vp, vp, vp]),
             "dart_page_pool_compact": (i, [C.POINTER(DartPagePool), vp, i, vp, vp, C.c_size_t, vp, vp]),
             "dart_paged_attention_workspace": (C.c_size_t, [C.POINTER(DartPagedAttnConfig), C.POINTER(DartKvCache)]),
@@ -618,9 +619,10 @@ class KVCache:
 class PagePool:
     """Which pages sequences hold, pages that several share among them: refs
     [num_pages], table [nseq, max_pages] (the page_table of KVCache and
-    PagedTreeAttention) and held [nseq], int32, all zero at first; and pairs,
-    count, the copies that the last reserve or compact asks for.  Nothing waits
-    for the host.  `lens` are the caller's."""
+    PagedTreeAttention) and held [nseq], int32, all zero at first; pairs, count,
+    the copies that the last reserve or compact asks for; and granted [nseq], the
+    tokens that the last reserve found room for.  Nothing waits for the host.
+    `lens` are the caller's."""
 
     def __init__(self, num_pages, page_size, nseq, max_pages):
         self.num_pages, self.page_size, self.nseq, self.max_pages = int(num_pages), int(page_size), int(nseq), int(max_pages)
@@ -632,6 +634,7 @@ class PagePool:
         self.dev = torch.cuda.current_device()
         self.refs, self.table, self.held = i32(self.num_pages).zero_(), i32(self.nseq, self.max_pages).zero_(), i32(self.nseq).zero_()
         self.pairs, self.count = i32(max(self.nseq, self.num_pages // 2), 2).fill_(-1), i32(1).zero_()
+        self.granted = i32(self.nseq).zero_()
         self.workspace = _empty((n,), dtype=torch.uint8, device="cuda")
         c.refs, c.table, c.held = self.refs.data_ptr(), self.table.data_ptr(), self.held.data_ptr()
         self.c, self.ref = c, C.byref(c)
@@ -649,11 +652,14 @@ class PagePool:
 
     def reserve(self, lens, n_rows, status=None, stream=None):
         """Room for n_rows[s] tokens from position lens[s] on, on pages that no
-        other sequence holds.  Returns (pairs, count) for KVCache.copy_pages."""
+        other sequence holds.  Returns (pairs, count) for KVCache.copy_pages and
+        leaves in `granted` n_rows[s], or 0 where there is no room: the n_rows
+        of KVCache.append (the smaller of it and the rows that are kept)."""
         dev, st = _current(stream, self.dev)
-        _check(lib().dart_page_pool_reserve(self.ref, self._seq(lens, "lens", dev), self._seq(n_rows, "n_rows", dev), self.pairs.data_ptr(),
-                                            self.pairs.shape[0], self.count.data_ptr(), *self.ws, _status(status, dev), st),
-               "dart_page_pool_reserve")
+        _check(lib().dart_page_pool_reserve_rows(self.ref, self._seq(lens, "lens", dev), self._seq(n_rows, "n_rows", dev),
+                                                 self.granted.data_ptr(), self.pairs.data_ptr(), self.pairs.shape[0],
+                                                 self.count.data_ptr(), *self.ws, _status(status, dev), st),
+               "dart_page_pool_reserve_rows")
         return self.pairs, self.count
 
     def trim(self, lens, status=None, stream=None):
