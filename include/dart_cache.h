@@ -225,6 +225,13 @@ int dart_paged_attention(const dart_paged_attn_config *cfg, const dart_kv_cache 
                          const int32_t *n_nodes, void *out, void *workspace, size_t workspace_bytes, int *status,
                          void *stream);
 
+/* Test hook of dart_paged_attention's bounded waits, in a library compiled with
+ * -DDART_DEBUG: calls made from now on take the wait that softmax warp `warp` of
+ * each CTA of the 128-row tiles ends its part number `part` with for one that gave
+ * up (negative: none).  Nothing waits longer: the call ends with value 1 in
+ * *status.  Other builds: DART_ERR_UNSUPPORTED, unless both are negative. */
+int dart_test_paged_wait(int warp, int part);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1087,6 +1087,12 @@ bool valid_cfg(const dart_paged_attn_config* c, const dart_kv_cache* cache) {
            static_cast<long long>(c->nseq) * cache->Hkv * (c->B + 256) <= (1ll << 30);
 }
 
+#ifdef DART_DEBUG
+struct {
+    int warp, part;
+} fail_at = {-1, -1};  // (dart_test_paged_wait)
+#endif
+
 // Which kernel: a few rows are streamed from HBM, more are 128-row tiles of the
 // tensor-memory path (64 sequences, 16 rows a kv head, 4096 keys, here and there: bf16
 // pages 99 and 106 us, e4m3 71 and 135, e2m1 80 and 134).
@@ -1143,6 +1149,15 @@ using namespace dart;
 
 extern "C" {
 
+int dart_test_paged_wait(int warp, int part) {
+#ifdef DART_DEBUG
+    fail_at = {warp, part};
+    return DART_OK;
+#else
+    return warp < 0 && part < 0 ? DART_OK : DART_ERR_UNSUPPORTED;
+#endif
+}
+
 size_t dart_paged_attention_workspace(const dart_paged_attn_config* cfg, const dart_kv_cache* cache) {
     if (!valid_cfg(cfg, cache)) return 0;
     if (few_rows(*cfg, *cache)) return (cfg->B + 1) * (cfg->Hq / cache->Hkv) <= 8 ? rows_workspace<1>() : rows_workspace<2>();
@@ -1198,6 +1213,10 @@ int dart_paged_attention(const dart_paged_attn_config* cfg, const dart_kv_cache*
     a.kb = static_cast<const uint8_t*>(cache->k_block);
     a.vb = static_cast<const uint8_t*>(cache->v_block);
     a.out = static_cast<__nv_bfloat16*>(out);
+#ifdef DART_DEBUG
+    a.fail_warp = fail_at.warp;
+    a.fail_part = fail_at.part;
+#endif
     a.plan = static_cast<SharePlan*>(workspace);
     a.parts = static_cast<uint8_t*>(workspace) + sizeof(SharePlan);
     a.status = status;

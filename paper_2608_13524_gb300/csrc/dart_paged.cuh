@@ -38,6 +38,13 @@ struct PagedArgs {
     int* status;
     float sl2;  // scale * log2(e)
     RopeTurns turns;
+    // Debug builds: whether the last wait of a softmax warp's part is to count as failed (dart_test_paged_wait).
+#ifdef DART_DEBUG
+    int fail_warp, fail_part;
+    __device__ __forceinline__ bool test_wait_fails(int warp, int part) const { return warp == fail_warp && part == fail_part; }
+#else
+    __device__ __forceinline__ bool test_wait_fails(int, int) const { return false; }
+#endif
 };
 
 __device__ __forceinline__ int seq_len(const PagedArgs& a, int s) {

@@ -1041,7 +1041,7 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
         };
         pdl_wait();
         if (have) load_q(slot.part[0]);
-        int n = 0;
+        int n = 0, part = 0;
         while (have) {
             const UnitPart& u = slot.part[which];
             which ^= 1;
@@ -1191,18 +1191,18 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                     if (have) load_q(slot.part[which]);
                 }
             }
-            // the pair leaves together: an `ok` lost after the last exchange is exchanged here
-            if (ok && !soon(&pv_done[(n - 1) & 1], static_cast<uint32_t>((n - 1) >> 1) & 1u, abort)) {
+            // The pair leaves together: an `ok` lost after the last exchange is exchanged here, in a
+            // part without rows too (the next one may have some, and barriers that both have to reach).
+            if (ok && (!soon(&pv_done[(n - 1) & 1], static_cast<uint32_t>((n - 1) >> 1) & 1u, abort) || a.test_wait_fails(warp, part++))) {
                 attn_timeout(a.status, abort);
                 ok = false;
             }
+            l += exchange(l, ok);
+            if (!ok) break;
             if (idle) {
-                if (!ok) break;
                 arrive(o_free);
                 continue;
             }
-            l += exchange(l, ok);
-            if (!ok) break;
             tc_fence_after();
             const int b = node(), row = u.qt * kRows + r;
             const bool row_ok = b <= u.nodes;

@@ -141,6 +141,7 @@ def lib():
             "dart_paged_attention_workspace": (C.c_size_t, [C.POINTER(DartPagedAttnConfig), C.POINTER(DartKvCache)]),
             "dart_paged_attention": (i, [C.POINTER(DartPagedAttnConfig), C.POINTER(DartKvCache), vp, vp, vp, i64, vp, i64, vp,
                                          i64, vp, vp, vp, vp, vp, C.c_size_t, vp, vp]),
+            "dart_test_paged_wait": (i, [i, i]),
             "dart_verify_tree": (i, [C.POINTER(DartVerifyConfig), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
             "dart_destroy": (None, [vp]),
             "dart_status_string": (C.c_char_p, [i]),
@@ -712,6 +713,11 @@ class PagedTreeAttention:
             _expect(lens, "lens", torch.int32, (nseq,), dev), qp, qs, kp, ks, vp, vs, *tree, self.out.data_ptr(),
             self.workspace.data_ptr(), self.workspace.numel(), _status(status, dev), st), "dart_paged_attention")
         return self.out
+
+
+def dart_test_paged_wait(warp, part):
+    """Debug builds: a wait of later calls counts as failed (see dart_cache.h)."""
+    _check(lib().dart_test_paged_wait(int(warp), int(part)), "dart_test_paged_wait")
 
 
 # ------------------------------------------- which branch the target keeps (dart_verify.h)
