@@ -186,6 +186,7 @@ __device__ __forceinline__ float largest_of(const float2 (&x)[4]) {
 // sine and cosine by a unit, product and sum by half a unit), quotients by 2^-23 more; true
 // where that may decide a rounding of this thread's.  What is stored then is to be stored again.
 constexpr float kOff = 7e-7f;
+constexpr float kTinyRow = 7.88860905221011805e-31f;  // 2^-100
 template <bool kRotated>
 __device__ __forceinline__ bool store_e2m1(uint8_t* pool, uint8_t* blocks, float* scales, long long row, int j, const Pairs& x, bool use) {
     float lo = largest_of(x.lo), hi = largest_of(x.hi);
@@ -224,6 +225,7 @@ __device__ __forceinline__ bool store_e2m1(uint8_t* pool, uint8_t* blocks, float
         code_hi = to_e2m1(z, off_hi);
         away |= code_hi ^ to_e2m1(z, -off_hi);
         unsure = less != more || (away & 0x77777777u) || (__float_as_uint(top * (1.0f - kOff)) >> 23) != (__float_as_uint(top * (1.0f + kOff)) >> 23);
+        unsure = unsure || (top < kTinyRow && top > 0.0f);  // (up * inv may have left the floats, and products lie below them)
     } else {
         // quotients rounded once, as in `quotients` (-x * up is exact, and in this form -0 stays -0)
         auto divided = [&](const float2 (&v)[4], float by, float inv) {
@@ -326,6 +328,13 @@ __device__ __noinline__ void store_e2m1_exact(uint8_t* pool, uint8_t* blocks, fl
     float v[4];
 #pragma unroll
     for (int e = 0; e < 4; e++) v[e] = __bfloat162float(src[lane + 32 * e]);
+    // rows below 2^-60 times 2^60: the remainders of smaller ones would lie below the floats
+    uint32_t any = 0;
+#pragma unroll
+    for (int e = 0; e < 4; e++) any = max(any, fabsf(v[e]) < INFINITY ? __float_as_uint(fabsf(v[e])) : 0u);
+    const int lift = __reduce_max_sync(kFull, any) < __float_as_uint(8.673617379884035e-19f) ? 60 : 0;
+#pragma unroll
+    for (int e = 0; e < 4; e++) v[e] *= lift ? kSmallUp : 1.0f;
 #pragma unroll
     for (int e = 0; e < 2; e++) {
         Two sn, cs;
@@ -351,8 +360,8 @@ __device__ __noinline__ void store_e2m1_exact(uint8_t* pool, uint8_t* blocks, fl
     top = larger(top, Two{__shfl_xor_sync(kFull, top.hi, 16), __shfl_xor_sync(kFull, top.lo, 16)});
     const uint32_t bits = __float_as_uint(top.hi);
     // (a power of two less something has the exponent below)
-    const int ex = top.hi > 0.0f ? max(static_cast<int>(bits >> 23) - ((bits & 0x7FFFFFu) == 0u && top.lo < 0.0f ? 1 : 0) - 137, -120) : 0;
-    const float up = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+    const int ex = top.hi > 0.0f ? max(static_cast<int>(bits >> 23) - ((bits & 0x7FFFFFu) == 0u && top.lo < 0.0f ? 1 : 0) - 137 - lift, -120) : 0;
+    const float up = __uint_as_float(static_cast<uint32_t>(127 - ex - lift) << 23);
 #pragma unroll
     for (int e = 0; e < 4; e++) {
         const Two m{most[e].hi * up, most[e].lo * up}, y{x[e].hi * up, x[e].lo * up};
