@@ -535,7 +535,10 @@ def _status(t, dev):
     return t.data_ptr()
 
 
-_KV_TYPES = {torch.bfloat16: DART_KV_BF16, torch.float8_e4m3fn: DART_KV_E4M3, torch.float4_e2m1fn_x2: DART_KV_E2M1}
+_E2M1 = getattr(torch, "float4_e2m1fn_x2", None)  # (a torch without it has the other pages)
+_KV_TYPES = {torch.bfloat16: DART_KV_BF16, torch.float8_e4m3fn: DART_KV_E4M3}
+if _E2M1 is not None:
+    _KV_TYPES[_E2M1] = DART_KV_E2M1
 
 
 class KVCache:
@@ -569,7 +572,7 @@ class KVCache:
     def new(cls, num_pages, page_size, Hkv, dh=128, dtype=torch.bfloat16):
         """An empty pool on the current device."""
         shape, kw = (num_pages, Hkv, page_size), dict(device="cuda")
-        if dtype == torch.float4_e2m1fn_x2:
+        if dtype is not None and dtype == _E2M1:
             k, v = (torch.zeros(shape + (dh // 2,), dtype=torch.uint8, **kw).view(dtype) for _ in range(2))
             blocks = [torch.zeros(shape + (dh // 16,), dtype=torch.float8_e4m3fn, **kw) for _ in range(2)]
             return cls(k, v, *(torch.zeros(shape, **kw) for _ in range(2)), *blocks)
