@@ -1197,12 +1197,14 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                 attn_timeout(a.status, abort);
                 ok = false;
             }
-            l += exchange(l, ok);
-            if (!ok) break;
             if (idle) {
+                exchange(0.0f, ok);
+                if (!ok) break;
                 arrive(o_free);
                 continue;
             }
+            l += exchange(l, ok);
+            if (!ok) break;
             tc_fence_after();
             const int b = node(), row = u.qt * kRows + r;
             const bool row_ok = b <= u.nodes;
