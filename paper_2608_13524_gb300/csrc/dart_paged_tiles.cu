@@ -1416,7 +1416,12 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
 
 // Joins the parts of the units that several CTAs shared, in the order of
 // their keys.  Blocks 8 (i - 1) .. + 7 work if share i begins inside a unit that
-// share i - 1 began: 16 rows each, 16 threads (8 elements each) a row.
+// share i - 1 began: 16 rows each, 16 threads (8 elements each) a row.  kBatch parts are on their
+// way at a time: eight where a unit has several (107 registers), two where most have one or two,
+// so that more blocks run at once (2 and 8: one tree of 300 nodes over 2048 bf16 keys 30.7 and 32.1 us,
+// eight of 127 over up to 4096 66.5 and 70.5; one of 64 over 2048 22.5 and 20.4, of 16 over
+// 131072 100.7 and 94.4).
+template <int kBatch>
 __global__ void __launch_bounds__(256) paged_tiles_join_kernel(const __grid_constant__ PagedArgs a) {
     pdl_trigger();
     const int tid = threadIdx.x, lane = tid & 31, i = blockIdx.x / 8 + 1, eighth = blockIdx.x % 8;
@@ -1445,7 +1450,6 @@ __global__ void __launch_bounds__(256) paged_tiles_join_kernel(const __grid_cons
     }
     if (b > nodes) return;
     float top = -INFINITY, l = 0.0f, o[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    constexpr int kBatch = 8;  // parts on their way at a time
     for (int c = c0; c <= c1; c += kBatch) {
         float2 ml[kBatch];
         float4 y[kBatch], z[kBatch];
@@ -1582,7 +1586,7 @@ int launch_paged_tiles(PagedArgs a, const dart_kv_cache& cache, uint8_t* workspa
             : e2m1 ? launch_tiles<kCodes4>(sms, st, tmK, tmV, tmSk, tmSv, ta)
             : e4m3 ? launch_tiles<kCodes>(sms, st, tmK, tmV, tmSk, tmSv, ta)
                    : launch_tiles<kPages>(sms, st, tmK, tmV, tmSk, tmSv, ta);
-    if (e == cudaSuccess) e = launch_pdl(paged_tiles_join_kernel, dim3(8 * (sms - 1)), dim3(256), 0, st, a);
+    if (e == cudaSuccess) e = launch_pdl(heads * w.nqt * 4 <= sms ? paged_tiles_join_kernel<8> : paged_tiles_join_kernel<2>, dim3(8 * (sms - 1)), dim3(256), 0, st, a);
     return e == cudaSuccess ? DART_OK : DART_ERR_CUDA;
 }
 
