@@ -78,6 +78,10 @@ struct Part {  // a unit's partial result
 // keys with 12 warps 91, 14 95, 16 86).
 __host__ __device__ constexpr int rows_warps(int type, int n) { return n > 1 ? 8 : type == DART_KV_E2M1 ? 11 : 12; }
 
+// A unit whose cache values are measured by less than this is measured by 1 once tree rows
+// come to it: their weights are 128 over that, which times a tree value has to be a float.
+constexpr float kSmallRef = 9.31322574615478515625e-10f;  // 2^-30
+
 // ------------------------------------------------------------ the schedule
 
 // Chunk sizes, and what a unit costs beside its chunks (queries, tree rows,
@@ -923,7 +927,15 @@ __global__ void __launch_bounds__(32 * rows_warps(kType, kN), 1)
                     }
             soften(sc);
             if (kF16) {
-                if (vref == 0.0f) vref = 1.0f;
+                if (vref < kSmallRef) {
+#pragma unroll
+                    for (int n = 0; n < kN; n++)
+#pragma unroll
+                        for (int j = 0; j < 8; j++)
+#pragma unroll
+                            for (int e = 0; e < 4; e++) acc[n][j][e] *= vref;
+                    vref = 1.0f;
+                }
                 const float inv = 128.0f / vref;
 #pragma unroll
                 for (int n = 0; n < kN; n++)
