@@ -246,7 +246,12 @@ __global__ void __launch_bounds__(kThreads, 1) pool_reserve_kernel(const __grid_
     for (int s0 = 0; s0 < a.nseq; s0 += kThreads) {
         const int s = s0 + tid;
         int2 want = make_int2(0, 0);
-        if (s < a.nseq) want = __ldcg(reinterpret_cast<const int2*>(a.grant + s));
+        int rows = 0;
+        if (s < a.nseq) {
+            want = __ldcg(reinterpret_cast<const int2*>(a.grant + s));
+            rows = ld_plain(a.n_rows + s);
+        }
+        const bool fits = rows > 0 && need_of(a, min(s, a.nseq - 1), rows) <= a.max_pages;
         int tile;  // (at most nseq * max_pages, 2^30)
         const int before = block_sum(want.x, part, &tile);
         const bool granted = asked + before + want.x <= all_free;
@@ -257,11 +262,7 @@ __global__ void __launch_bounds__(kThreads, 1) pool_reserve_kernel(const __grid_
             if (!granted && want.x > 0 && a.status) atomicOr(a.status, kDevNoRoom);
             __stcg(&a.grant[s].offset, granted && want.x > 0 ? static_cast<int>(asked) + before : -1);
             __stcg(&a.grant[s].pair_at, pair_at);
-            if (a.granted) {
-                const int rows = ld_plain(a.n_rows + s);
-                const bool room = (granted || want.x == 0) && rows > 0 && need_of(a, s, rows) <= a.max_pages;
-                a.granted[s] = room ? rows : 0;
-            }
+            if (a.granted) a.granted[s] = fits && (granted || want.x == 0) ? rows : 0;
         }
         places += ok;
         copies += pairs;
