@@ -1566,9 +1566,11 @@ int launch_paged_tiles(PagedArgs a, const dart_kv_cache& cache, uint8_t* workspa
         tmSk = tmK;  // (side tiles lie among the others)
         tmSv = tmV;
     }
-    // Four tree rows a block where that leaves every SM a block (one tree of 300 nodes over 2048 keys, four /
-    // one a block: 40.5 / 36.4 us; eight of 512 over up to 4096 246 / 251).
-    const bool four = static_cast<long long>(a.nseq) * (a.B + 1) >= 4 * sms;
+    // Four tree rows a block from this many rows on (bf16 / e4m3 / e2m1, four and one a block: eight trees of
+    // 96 nodes over up to 4096 keys 67.4 and 63.6 / 84.6 and 81.8 / 81.7 and 79.3 us, of 150 79.6 and 78.9 / 93.8 and
+    // 96.8 / 91.1 and 94.0, of 512 234 and 239 / 248 and 253 / 245 and 249; 32 of 31 over up to 2048 52.7 and
+    // 54.2 / 60.5 and 59.4 / 57.3 and 56.9).
+    const bool four = static_cast<long long>(a.nseq) * (a.B + 1) >= 7 * sms;
     const int tree_blocks = four ? (a.B + 4) / 4 : a.B + 1;
     // up to 127 cache tokens before the tree rows and, in bf16, up to 127 rows of zeros after them
     const int others = e4m3 || e2m1 ? kKeys - 1 : 2 * (kKeys - 1);
