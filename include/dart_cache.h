@@ -75,10 +75,11 @@ typedef struct {
  * e2m1 pools: a row's scale is a power of two, 2^-10 times the one at or below
  * its largest magnitude (at least 2^-120; 1 if it is all zero), so that x /
  * scale is exact; a block scale is its 16 elements' largest magnitude / scale /
- * 6 rounded to e4m3 (at most 342; it may be 0), and a code x / scale / block
+ * 6 rounded to e4m3 (at most 352; it may be 0), and a code x / scale / block
  * rounded to e2m1, both to nearest, ties to even, magnitudes above 6 to 6.
- * What is rounded of K is its rotation to 2^-44 of a pair's length: where the one
- * in fp32 leaves a scale or a code open, it is formed again.
+ * What is rounded of K is its rotation at frequencies of 53 bits, to 2^-44 of a
+ * pair's length (against exact frequencies p 2^-52.6 more): where the one in fp32
+ * leaves a scale or a code open, it is formed again.
  * A NaN or an infinity makes its block (in K, that of its rotated pair too)
  * NaN when it is read and counts for no scale.
  * Positions past max_pages * page_size are not written
@@ -92,7 +93,7 @@ int dart_cache_append(const dart_kv_cache *cache, int nseq, int max_pages, const
 /* Gives tokens of the cache back: tokens lens[s] .. lens[s] + n_rows[s] - 1
  * (n_rows clamped to [0, R]) of every sequence as rows 0, 1, ... of sequence s
  * of k and v (bf16, rows with strides as in dart_cache_append): code * block *
- * scale rounded to bf16, K as it is stored (rotated).  Rows from n_rows[s] on
+ * scale rounded to fp32 and then to bf16, K as it is stored (rotated).  Rows from n_rows[s] on
  * and what lies between rows are not written; a position past max_pages *
  * page_size or a page outside [0, num_pages) leaves its row as it was and sets
  * value 4 in *status. */
@@ -191,8 +192,11 @@ typedef struct {
 } dart_paged_attn_config;
 
 /* Device workspace (bytes) of dart_paged_attention; 0 on an invalid
- * configuration.  For large trees over e4m3 pages it has room for the f16 form
- * of max_pages pages a sequence, where that takes at most 4 GB. */
+ * configuration.  For large trees over e4m3 or e2m1 pages (five tiles of 128 query
+ * rows a kv head and more) it has room for the f16 form of max_pages pages a
+ * sequence, whatever the lengths are: 512 bytes a token and kv head, where the
+ * pages themselves take 264 or 152.  Where that would be more than 4 GB it has
+ * none, and every query tile converts the pages for itself. */
 size_t dart_paged_attention_workspace(const dart_paged_attn_config *cfg, const dart_kv_cache *cache);
 
 /* One tree-attention layer over the cache:

@@ -319,7 +319,7 @@ __device__ __forceinline__ float e4m3_value(uint32_t code) {
     const uint32_t wide = e4m3_f16(code);
     return __low2float(*reinterpret_cast<const __half2*>(&wide));
 }
-// A row once more from its elements before the rotation, each to 2^-44 of its pair, by a
+// A row once more from its elements before the rotation, each to 2^-44 of its pair (at the frequencies in f), by a
 // warp: a lane has elements lane, lane + 32, + 64 and + 96.  It takes 2 us of latencies and of
 // fetching its instructions (in 64-bit floats 25: those run at a 64th of the rate).
 __device__ __noinline__ void store_e2m1_exact(uint8_t* pool, uint8_t* blocks, float* scales, long long row, const __nv_bfloat16* src, int pos, const uint64_t* f) {

@@ -1106,8 +1106,9 @@ struct {
 #endif
 
 // Which kernel: a few rows are streamed from HBM, more are 128-row tiles of the
-// tensor-memory path (64 sequences, 16 rows a kv head, 4096 keys, here and there: bf16
-// pages 99 and 106 us, e4m3 71 and 135, e2m1 80 and 134).
+// tensor-memory path (64 sequences, 16 rows a kv head, up to 4096 keys, here and there: bf16
+// pages 103 and 109 us, e4m3 66 and 141, e2m1 82 and 136; 16 over up to 16384 107 and 99, 64 and
+// 101, 67 and 104).
 constexpr int kFewRows = 16;
 bool few_rows(const dart_paged_attn_config& c, const dart_kv_cache& cache) { return (c.B + 1) * (c.Hq / cache.Hkv) <= kFewRows; }
 

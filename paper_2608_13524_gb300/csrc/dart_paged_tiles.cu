@@ -36,7 +36,7 @@
 //
 // Measured: a tile takes 1.07 us from bf16 pages (24 MMAs of 66 cycles are 0.8), 1.05 from
 // widened ones (16 MMAs, 0.53), 1.4 from e2m1 pages that the CTA converts; eight trees of 512
-// nodes over up to 4096 keys take 236 and 247 us with everything around.  With the first
+// nodes over up to 4096 keys take 234 and 243 (e4m3 248) us with everything around.  With the first
 // term of the queries alone bf16 pages took 0.90 and 211 us, at an error against 64 bits of
 // 0.0029 of the output instead of 0.0023 (its own rounding is 0.0017).  What a tile takes
 // beside its MMAs is the chain of the softmax: about 580 cycles from one tile's P to the next
@@ -400,7 +400,8 @@ __device__ __noinline__ float largest_in_use(const uint8_t* tile, const float* s
 
 // One block per tile of a sequence and kv head (whole cache tiles, then side
 // tiles): codes times their key's scale (e2m1: and block scale) over a power of two
-// that the tile's keys (and, apart, values) have in common, rounded once to f16.
+// that the tile's keys (and, apart, values) have in common: that factor rounded to f16 and
+// its product with the code again (both exact where scales are powers of two).
 template <int kType>
 __global__ void __launch_bounds__(256) paged_widen_kernel(const __grid_constant__ TileArgs ta, const uint8_t* pool_k, const uint8_t* pool_v) {
     __shared__ float scale_of[2 * kKeys];
@@ -708,7 +709,7 @@ struct TGeo {
     static constexpr int kBars = 4 * kStages + 2 * (kRawK + kRawV) + (kConv ? kRing : 0) + 9;
     static constexpr int kExchange = 4 * kRows * 4 + 16 * 4 + kRing * 8 + (kSoft / 32) * static_cast<int>(sizeof(WalkSlot));
     static constexpr int kSmem = kOps + kRaw + kRawScales + kBars * 8 + kExchange + 16;
-    // loads, MMAs, 8 softmax warps, kConv: 4 that convert K, 4 V
+    // loads, MMAs, 8 softmax warps, kConv: 2 that convert K, 2 V
     static constexpr int kFirstSoft = 2, kFirstConv = kFirstSoft + kSoft / 32;
     static constexpr int kThreads = 32 * (kFirstConv + (kConv ? 4 : 0));
 };
@@ -1481,9 +1482,11 @@ __global__ void __launch_bounds__(256) paged_tiles_join_kernel(const __grid_cons
 
 // e4m3 and e2m1 pages are widened first where a kv head has at least this many query
 // tiles, each of which would convert all keys again (a tile of a unit takes 1.05
-// us from f16 tiles and 1.3 converted), and where the f16 tiles of the longest
-// sequences take at most 4 GB.  e2m1 pages, widened / converted: eight trees over 4096 keys,
-// 4 query tiles 86 / 89 us, 5 98 / 107, 8 138 / 157; two over 16384, 4 tiles 93 / 79.
+// us from f16 tiles and 1.4 converted), and where the f16 tiles of the longest
+// sequences take at most 4 GB.  Widened / converted, eight trees over up to 4096 keys, 64
+// of them, two over up to 16384: 4 query tiles e4m3 81 / 81, 582 / 527, 86 / 76 us, e2m1 79 / 79,
+// 560 / 505, 82 / 77; 5 tiles (64 trees: up to 2048 keys) e4m3 93 / 100, 399 / 460, 97 / 90, e2m1
+// 90 / 97, 391 / 436, 94 / 93.
 constexpr int kWidenTiles = 5;
 constexpr size_t kWidenBytes = static_cast<size_t>(4) << 30;
 
