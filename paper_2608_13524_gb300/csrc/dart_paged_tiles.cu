@@ -979,12 +979,12 @@ __global__ void __launch_bounds__(TGeo<kSource>::kThreads, 1)
                     }
                     n++;
                 }
-                if (!ok) {
-                    if (lane == 0) attn_timeout(a.status, abort);
-                    __syncwarp();
-                    commit_elected(tdown);
-                    attn_drain(tdown, 0);
-                }
+                if (!ok && lane == 0) attn_timeout(a.status, abort);
+                // The last products end before tensor memory is given back, whoever gives up a wait (in a good
+                // run the softmax has waited for them, and this costs nothing).
+                __syncwarp();
+                commit_elected(tdown);
+                attn_drain(tdown, 0);
             }
         }
     } else if (warp < G_::kFirstConv) {
